@@ -580,6 +580,195 @@ pb_status pblock_lamb_step(const pb_lamb_config* cfg, int n_tensors,
                            float* trust_ratio, void* ws, size_t ws_bytes,
                            hipStream_t stream);
 
+/* ------------------------------------------------------- rotary positions
+ * The block has no positional terms of its own; these calls rotate Q and K
+ * between the in-projection and the attention, and their gradients after the
+ * attention backward (the stash and dZ then hold the rotated Q and K and, after
+ * pblock_rope_backward, the gradients of the unrotated ones).
+ *
+ * The leading rot_dim elements of each head turn in pairs, i = 0 .. rot_dim/2 - 1:
+ * elements (2i, 2i + 1) when interleaved, else (i, i + rot_dim/2), with
+ *
+ *   f_i = base^(-2i / rot_dim)                    PB_ROPE_PLAIN
+ *   f_i / factor                                  PB_ROPE_LINEAR
+ *   f_i (g + (1 - g) / factor)                    PB_ROPE_BY_PARTS
+ *       g = clamp((orig_len f_i / 2 pi - low_turns) / (high_turns - low_turns), 0, 1)
+ *   t = position f_i
+ *   forward:   (y_a, y_b) = magnitude (x_a cos t - x_b sin t, x_b cos t + x_a sin t)
+ *   backward:  the transposed map (t negated, the same magnitude): from the
+ *              gradient of y to that of x
+ *
+ * By parts: pairs that turn often within the trained length orig_len keep their
+ * frequency, the slow ones are interpolated (Peng et al. 2023); magnitude is the
+ * attention's rescaling that goes with it (1 for none).  The other elements of a
+ * head are passed through.  Angles are formed in 64 bits, the rotation in 32,
+ * rounded once.
+ *
+ * tensors[k] (1 to PB_ROPE_MAX_TENSORS, e.g. Q and K, of their own head counts):
+ *   element (token, head, e) of in at in[token*ld_in + head*head_dim + e], ld_in in
+ *   elements (>= heads*head_dim), out likewise.  out may be in with ld_out = ld_in
+ *   (in place; elements past rot_dim are then left alone); otherwise no memory of
+ *   any out may be in any other in or out.  Pointers are aligned to the element;
+ *   16-byte aligned pieces (head_dim, ld and rot_dim, or rot_dim/2 when not
+ *   interleaved, multiples of 16 bytes) run fastest.
+ * positions: int64 per token, device memory, any value (negative ones turn the
+ *   other way; beyond 2^31 the angles lose accuracy).  NULL: token t is at position
+ *   t mod seq.  seq is read only then.
+ * tokens may be 0 (nothing is launched).
+ * Errors: PB_ERR_INVALID_ARG for a bad config or pointer, PB_ERR_UNSUPPORTED for
+ * head_dim > 256, or too many tokens or heads. */
+#define PB_ROPE_MAX_TENSORS 4
+typedef enum { PB_ROPE_PLAIN = 0, PB_ROPE_LINEAR = 1, PB_ROPE_BY_PARTS = 2 } pb_rope_scaling;
+typedef struct {
+  int head_dim;      /* even, 2 .. 256                                        */
+  int rot_dim;       /* even, 2 .. head_dim                                   */
+  int interleaved;   /* 0 or 1                                                */
+  int scaling;       /* pb_rope_scaling                                       */
+  double base;       /* > 0, finite                                           */
+  double factor;     /* > 0, finite; not read by PB_ROPE_PLAIN                */
+  double orig_len;   /* > 0; this and the next two by PB_ROPE_BY_PARTS only   */
+  double low_turns;  /* 0 <= low_turns < high_turns                           */
+  double high_turns;
+  double magnitude;  /* > 0, finite                                           */
+  pb_dtype dtype;
+} pb_rope_config;
+typedef struct {
+  const void* in;
+  void* out;
+  size_t ld_in, ld_out;
+  int heads;         /* 1 .. 8192                                             */
+} pb_rope_tensor;
+pb_status pblock_rope_forward(const pb_rope_config* cfg, int n_tensors,
+                              const pb_rope_tensor* tensors, int64_t tokens,
+                              int64_t seq, const int64_t* positions,
+                              hipStream_t stream);
+pb_status pblock_rope_backward(const pb_rope_config* cfg, int n_tensors,
+                               const pb_rope_tensor* tensors, int64_t tokens,
+                               int64_t seq, const int64_t* positions,
+                               hipStream_t stream);
+
+/* ------------------------------------------------- root-mean-square norm
+ * Per row of a dense [rows, cols] matrix (any cols from 1 to 32768):
+ *
+ *   s = x + resid                    (resid NULL: s = x)
+ *   r = 1 / sqrt(mean(s^2) + eps)
+ *   y = s r gamma
+ *
+ * y is formed from the unrounded s, in 32 bits (64 with q8), and rounded once.
+ * Outputs, each left out when NULL, but y or q8 must be there:
+ *   sum  [rows, cols] act   s rounded, the next residual (NULL unless resid is
+ *                           given; may be x or resid)
+ *   y    [rows, cols] act   (may be x or resid, whichever sum is not)
+ *   q8   [rows, cols] OCP e4m3, with scales: q8 = y / scale rounded to nearest
+ *        even, scale = max(max|y| / 448, 2^-126) in fp32 over each group of
+ *        `group` columns of a row (32, 64 or 128; the last group of a row may be
+ *        short) or over the row (0).  scales [rows, ceil(cols / group)] (or
+ *        [rows]).  A row with a NaN or an infinity has NaN codes where y is NaN.
+ *   rstd [rows] fp32        r, for the backward
+ * gamma [cols] act.
+ *
+ * pblock_rmsnorm_backward: s [rows, cols] act is the forward's sum (x without a
+ * residual), dy the gradient of y, dsum (may be NULL) the gradient that reaches s
+ * from elsewhere (the residual's other use).  With g = dy gamma,
+ *   dx = dsum + r (g - s r^2 mean(g s))   act: the gradient of x, and of resid
+ *   dgamma = sum over rows of dy s r      [cols] fp32, overwritten
+ * dx may be dy, dsum or s.  ws: pblock_rmsnorm_workspace_bytes(cfg) bytes, 256-byte
+ * aligned.  Results do not depend on timing (fixed order, no atomics).
+ *
+ * Pointers are aligned to their element; cols a multiple of 8 with 16-byte aligned
+ * pointers (8 for q8) runs fastest.  rows may be 0 (the backward then writes zeros
+ * to dgamma).  Errors as above. */
+typedef struct {
+  int64_t rows;      /* 0 .. 2^31 - 1                                         */
+  int cols;          /* 1 .. 32768                                            */
+  int group;         /* q8 only: 0, 32, 64 or 128                             */
+  float eps;         /* >= 0, finite                                          */
+  pb_dtype dtype;
+} pb_rmsnorm_config;
+pb_status pblock_rmsnorm_forward(const pb_rmsnorm_config* cfg, const void* x,
+                                 const void* resid, const void* gamma,
+                                 void* sum, void* y, uint8_t* q8,
+                                 float* scales, float* rstd,
+                                 hipStream_t stream);
+size_t pblock_rmsnorm_workspace_bytes(const pb_rmsnorm_config* cfg);
+pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s,
+                                  const void* gamma, const float* rstd,
+                                  const void* dy, const void* dsum, void* dx,
+                                  float* dgamma, void* ws, size_t ws_bytes,
+                                  hipStream_t stream);
+
+/* ------------------------------------------------------------- Muon step
+ * An optimizer step that treats each weight as a matrix (Jordan et al. 2024), next
+ * to pblock_lamb_step: the momentum's update, made nearly orthogonal by `steps`
+ * Newton-Schulz steps, moves the weight.  Per matrix, with g = grad_scale grad:
+ *
+ *   M = momentum M + g
+ *   U = g + momentum M (nesterov), else M
+ *   X = U / (||U||_F + eps)
+ *   steps times: A = X X^T, X = a X + (b A + c A A) X,
+ *                (a, b, c) = (3.4445, -4.7750, 2.0315)
+ *   w = w (1 - lr weight_decay) - lr scale X
+ *
+ * (a matrix with more rows than columns goes through the products transposed; the
+ * result is the same).  param, momentum and grad are fp32, param and momentum
+ * updated in place; param_copy, when not NULL, receives the updated weights in
+ * copy_dtype.  Each is [rows, cols] with ld elements from row to row: a slice of a
+ * packed weight (rows of w_in; columns of w_out, ld = K_out) is a matrix of its
+ * own.  scale is the caller's rule for the shape (0.2 sqrt(max(rows, cols)), say).
+ * Matrices with rows = 0 or cols = 0 are allowed (nothing is touched).
+ *
+ * products: PB_F32 carries 22 bits of every factor (each fp16 value with its
+ * remainder, three matrix products for one): the update is as exact as fp32
+ * products make it.  PB_BF16 rounds the factors to fp16 (11 bits), one product, a
+ * third of the time: the update is off by 1e-3 to 8e-3 of its norm, the more the
+ * fewer directions hold most of it (fp32 sums, norms, M and w either way).
+ *
+ * pblock_orthogonalize: X alone, from in to out (may be the same memory with the
+ * same ld, else apart), both in dtype; PB_F32 products for PB_F32, PB_BF16 products
+ * for PB_BF16 (whose own rounding of the input moves the result by more).
+ *
+ * ws: the *_workspace_bytes, 256-byte aligned; nothing in it outlives the call, and
+ * calls that may overlap need one each (so do two captured graphs that may).
+ * Errors: PB_ERR_INVALID_ARG for a bad config, size, pointer (aligned to its
+ * element) or ld < cols, PB_ERR_UNSUPPORTED for a matrix too large, PB_ERR_WORKSPACE
+ * for a small ws.  Results do not depend on timing (fixed order, no atomics). */
+#define PB_MUON_MAX_TENSORS 16
+typedef struct {
+  float lr;            /* finite                                              */
+  float momentum;      /* 0 <= momentum < 1                                   */
+  float grad_scale;    /* finite                                              */
+  float eps;           /* > 0, finite                                         */
+  int nesterov;        /* 0 or 1                                              */
+  int steps;           /* 1 .. 16                                             */
+  pb_dtype products;
+} pb_muon_config;
+typedef struct {
+  float* param;
+  const float* grad;
+  float* momentum;
+  void* param_copy;    /* NULL or in copy_dtype                               */
+  int rows, cols;      /* min <= 65536, max <= 2^20                           */
+  size_t ld;           /* >= cols                                             */
+  float weight_decay;  /* >= 0, finite                                        */
+  float scale;         /* finite                                              */
+} pb_muon_tensor;
+size_t pblock_muon_workspace_bytes(const pb_muon_config* cfg, int n_tensors,
+                                   const pb_muon_tensor* tensors);
+pb_status pblock_muon_step(const pb_muon_config* cfg, int n_tensors,
+                           const pb_muon_tensor* tensors, pb_dtype copy_dtype,
+                           void* ws, size_t ws_bytes, hipStream_t stream);
+typedef struct {
+  const void* in;
+  void* out;
+  int rows, cols;
+  size_t ld_in, ld_out;
+} pb_ortho_tensor;
+size_t pblock_orthogonalize_workspace_bytes(int n_tensors,
+                                            const pb_ortho_tensor* tensors,
+                                            pb_dtype dtype);
+pb_status pblock_orthogonalize(int n_tensors, const pb_ortho_tensor* tensors,
+                               pb_dtype dtype, int steps, float eps, void* ws,
+                               size_t ws_bytes, hipStream_t stream);
 
 /* Human-readable name of a status, and a description of the most recent
  * failed check on the calling thread ("" if none). */

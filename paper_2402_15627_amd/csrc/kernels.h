@@ -73,6 +73,89 @@ int lamb_padded_chunks(long long numel);  // rounded up to a multiple of kLambGr
 void launch_lamb(const LambTable& t, const LambScalars& sc, Dt copy_dt, float2* partial,
                  double2* group, float* ratio, float* ratio_out, hipStream_t s);
 
+// ------------------------------------------------------- rotary positions
+// Up to kRopeMaxTensors tensors of `tokens` rows, each of its own number of heads of
+// head_dim elements, head h of token t at in + t ld_in + h head_dim.  turns[i] is
+// the turn of pair i per position (its frequency over 2 pi).  copy_rest[k]: the
+// elements past rot_dim are copied too (out is another buffer than in).
+constexpr int kRopeMaxTensors = 4;
+constexpr int kRopeMaxDim = 256;
+struct RopeArgs {
+  const void* in[kRopeMaxTensors];
+  void* out[kRopeMaxTensors];
+  long long ld_in[kRopeMaxTensors], ld_out[kRopeMaxTensors];
+  int heads[kRopeMaxTensors];
+  int copy_rest[kRopeMaxTensors];
+  int n;
+  int head_dim, rot_dim;
+  int backward;
+  float magnitude;
+  long long tokens, seq;
+  const long long* pos;  // one per token, or nullptr: token t is at t mod seq
+  double turns[kRopeMaxDim / 2];
+};
+void launch_rope(Dt dt, const RopeArgs& a, bool interleaved, hipStream_t s);
+
+// ------------------------------------------------- root-mean-square norm
+// Dense rows of cols <= 32768.  Absent: resid, sum, y, q8 (with scales) and rstd may
+// be nullptr.  group: columns that share a scale (0: the row; else 32, 64 or 128).
+struct RmsForward {
+  const void *x, *resid, *gamma;
+  void *sum, *y;
+  unsigned char* q8;
+  float *scales, *rstd;
+  long long rows;
+  int cols, group;
+  float eps;
+};
+void launch_rms_forward(Dt dt, const RmsForward& a, hipStream_t s);
+// part: rms_backward_parts(rows, cols) x cols floats.  dsum may be nullptr.
+struct RmsBackward {
+  const void *s, *gamma, *dy, *dsum;
+  const float* rstd;
+  void* dx;
+  float *dgamma, *part;
+  long long rows;
+  int cols;
+};
+int rms_backward_parts(long long rows, int cols);
+void launch_rms_backward(Dt dt, const RmsBackward& a, hipStream_t s);
+
+// ------------------------------------- orthogonalised updates (Newton-Schulz)
+// One matrix of a call.  The iterate X is the update or, where it has more rows than
+// columns, its transpose: m x n with m <= n, both padded to multiples of 64 with
+// zeros.  x, a and b hold fp16 planes (one, or a value and its remainder): X twice
+// (in turn), X X^T, and the polynomial of it.
+constexpr int kNsMaxTensors = 16;
+constexpr int kNsPad = 64;
+struct NsMat {
+  const void* src;  // gradient, or the matrix to orthogonalise
+  float* mom;       // Muon step only, like w, copy, decay and scale
+  float* w;
+  void* copy;       // nullptr: none
+  void* out;        // orthogonalisation alone
+  long long ld_src, ld_out;
+  _Float16 *x[2], *a, *b;
+  int rows, cols, m, n;  // of the tensor; of X, padded
+  float decay, scale;
+};
+struct NsTable {
+  NsMat mat[kNsMaxTensors];
+  int tile0[kNsMaxTensors + 1];  // 64 x 64 tiles of the tensors' own layout
+  int count;
+};
+struct NsScalars {
+  float lr, momentum, grad_scale, eps;
+  int nesterov;
+  int planes;  // 1: one fp16 product; 2: a value and its remainder, three products
+  int steps;
+};
+// Where the updates come from and go to.
+enum class NsMode { Muon, Bf16, F32 };
+// partial: a double per tile; norm: one per matrix.
+void launch_newton_schulz(const NsTable& t, const NsScalars& sc, NsMode mode, Dt copy_dt,
+                          double* partial, double* norm, hipStream_t s);
+
 // ------------------------------------------------------ reduce-scatter sum
 // y = x + bias + sum over q < n of parts[q], row-major [rows, H] (H a
 // multiple of 8), summed in fp32 in the order of q.

@@ -1,0 +1,258 @@
+// The Muon step's passes over its tensors, and the orthogonalisation of matrices
+// by Newton-Schulz steps (Muon: Jordan et al. 2024):
+//
+//   M = mu M + g,  U = g + mu M (Nesterov) or M;  X = U / (||U||_F + eps)
+//   `steps` times:  A = X X^T,  B = b A + c A A,  X = a X + B X
+//   w = w (1 - lr decay) - lr scale X
+//
+// with X of m <= n (U, or its transpose).  The odd polynomial a s + b s^3 + c s^5
+// moves every singular value of X in [0, 1] towards 1 and stays in [0, 1.203].
+//
+//   1. update: M in place, the sum of U^2 per 64 x 64 tile, in fp64
+//   2. norm:   1 / (||U||_F + eps) of each matrix
+//   3. init:   X's fp16 planes, padded to multiples of 64 with zeros
+//   4. the products (ns_gemm.hip), three launches a step for all matrices at once
+//   5. apply:  w, and its copy; or the orthogonalised matrix itself
+//
+// 1, 3 and 5 are HBM-bound: a 64 x 64 tile per workgroup, 256 contiguous bytes of
+// a row per 16 lanes; a tall matrix's tile is transposed through LDS.
+#include "common.h"
+#include "kernels.h"
+#include "ns_gemm.h"
+
+namespace pb {
+namespace {
+
+constexpr int kTile = 64;
+constexpr int kThreads = 256;
+
+PB_DEV int mat_of(const NsTable& t, int tile) {
+  int i = 0;
+#pragma unroll 1
+  for (int k = 1; k < t.count; ++k)
+    if (tile >= t.tile0[k]) i = k;
+  return i;
+}
+
+// Four columns c..c+3 of a row, of which `left` exist; p: the row's start.
+template <typename T>
+PB_DEV void load4_cols(const T* p, int c, int left, bool vec, float* v) {
+  if (vec && left >= 4) {
+    load4<T>(p + c, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = e < left ? load1<T>(p + c + e) : 0.f;
+  }
+}
+template <typename T>
+PB_DEV void store4_cols(T* p, int c, int left, bool vec, const float* v) {
+  if (vec && left >= 4) {
+    store4<T>(p + c, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < left) p[c + e] = (T)v[e];
+  }
+}
+
+// Whether four columns from a multiple of four on are one aligned access in every row.
+template <typename T>
+PB_DEV bool rows_vec(const void* p, long long ld) {
+  return ld % 4 == 0 && (uintptr_t)p % (4 * sizeof(T)) == 0;
+}
+
+// The tile of the tensor that this workgroup takes.
+struct TileAt {
+  int i, r0, c0;
+};
+PB_DEV TileAt tile_at(const NsTable& t) {
+  const int tile = blockIdx.x, i = mat_of(t, tile), k = tile - t.tile0[i];
+  const int across = (t.mat[i].cols + kTile - 1) / kTile;
+  return {i, k / across * kTile, k % across * kTile};
+}
+
+template <NsMode MODE>
+__global__ __launch_bounds__(kThreads) void ns_update_kernel(NsTable t, NsScalars sc,
+                                                             double* __restrict__ partial) {
+  using T = typename std::conditional<MODE == NsMode::Bf16, bf16, float>::type;
+  __shared__ double red[kThreads / 64];
+  const TileAt at = tile_at(t);
+  const NsMat& x = t.mat[at.i];
+  const bool vec = rows_vec<T>(x.src, x.ld_src) &&
+                   (MODE != NsMode::Muon || rows_vec<float>(x.mom, x.ld_src));
+  const int c = at.c0 + 4 * (threadIdx.x & 15), left = x.cols - c;
+  double ss = 0.0;
+  float g[4][4], m[4][4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r = at.r0 + (threadIdx.x >> 4) + 16 * k;
+    const bool in = r < x.rows && left > 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) g[k][e] = m[k][e] = 0.f;
+    if (in) load4_cols((const T*)x.src + r * x.ld_src, c, left, vec, g[k]);
+    if (MODE == NsMode::Muon && in) load4_cols(x.mom + r * x.ld_src, c, left, vec, m[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r = at.r0 + (threadIdx.x >> 4) + 16 * k;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float u = g[k][e];
+      if constexpr (MODE == NsMode::Muon) {
+        u *= sc.grad_scale;
+        m[k][e] = __builtin_fmaf(sc.momentum, m[k][e], u);
+        u = sc.nesterov ? __builtin_fmaf(sc.momentum, m[k][e], u) : m[k][e];
+      }
+      ss += (double)u * u;
+    }
+    if (MODE == NsMode::Muon && r < x.rows && left > 0)
+      store4_cols(x.mom + r * x.ld_src, c, left, vec, m[k]);
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) ss += __shfl_xor(ss, o, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
+  __syncthreads();
+  if (threadIdx.x == 0) partial[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// norm[i] = 1 / (||U|| + eps) of matrix i.
+__global__ __launch_bounds__(kThreads) void ns_norm_kernel(NsTable t, float eps,
+                                                           const double* __restrict__ partial,
+                                                           double* __restrict__ norm) {
+  __shared__ double red[kThreads / 64];
+  const int i = blockIdx.x;
+  double ss = 0.0;
+  for (int k = t.tile0[i] + threadIdx.x; k < t.tile0[i + 1]; k += kThreads) ss += partial[k];
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) ss += __shfl_xor(ss, o, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
+  __syncthreads();
+  if (threadIdx.x == 0)
+    norm[i] = 1.0 / (sqrt((red[0] + red[1]) + (red[2] + red[3])) + (double)eps);
+}
+
+// X's tile of 64 x 64 at (i0, j0) of its padded m x n from U's tile of the tensor.
+template <NsMode MODE, int PLANES>
+__global__ __launch_bounds__(kThreads) void ns_init_kernel(NsTable t, NsScalars sc,
+                                                           const double* __restrict__ norm) {
+  using T = typename std::conditional<MODE == NsMode::Bf16, bf16, float>::type;
+  __shared__ float lds[kTile][kTile + 1];
+  const TileAt at = tile_at(t);
+  const NsMat& x = t.mat[at.i];
+  const bool tall = x.rows > x.cols;
+  const bool vec = rows_vec<T>(x.src, x.ld_src) &&
+                   (MODE != NsMode::Muon || rows_vec<float>(x.mom, x.ld_src));
+  const double f = norm[at.i];  // (in fp32 that of a norm past 1e38 has lost its bits)
+  const int cl = 4 * (threadIdx.x & 15), c = at.c0 + cl, left = x.cols - c;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int rl = (threadIdx.x >> 4) + 16 * k, r = at.r0 + rl;
+    float u[4] = {0.f, 0.f, 0.f, 0.f}, g[4];
+    if (r < x.rows && left > 0) {
+      if constexpr (MODE == NsMode::Muon) {
+        load4_cols(x.mom + r * x.ld_src, c, left, vec, u);
+        if (sc.nesterov) {
+          load4_cols((const float*)x.src + r * x.ld_src, c, left, vec, g);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) u[e] = __builtin_fmaf(sc.momentum, u[e], g[e] * sc.grad_scale);
+        }
+      } else {
+        load4_cols((const T*)x.src + r * x.ld_src, c, left, vec, u);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float v = (float)(u[e] * f);
+      if (tall) lds[cl + e][rl] = v;
+      else lds[rl][cl + e] = v;
+    }
+  }
+  __syncthreads();
+  const int i0 = tall ? at.c0 : at.r0, j0 = tall ? at.r0 : at.c0;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int i = (threadIdx.x >> 3) + 32 * k, j = 8 * (threadIdx.x & 7);
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = lds[i][j + e];
+    ns_store8<PLANES>(x.x[0] + (size_t)(i0 + i) * x.n + j0 + j, (size_t)x.m * x.n, v, kNsScaleX);
+  }
+}
+
+// From the last iterate, in planes of x[last]: the weights' step and their copy, or
+// the matrix itself.
+template <NsMode MODE, int PLANES, typename CT>
+__global__ __launch_bounds__(kThreads) void ns_apply_kernel(NsTable t, NsScalars sc, int last) {
+  __shared__ float lds[kTile][kTile + 1];
+  const TileAt at = tile_at(t);
+  const NsMat& x = t.mat[at.i];
+  const bool tall = x.rows > x.cols;
+  const int i0 = tall ? at.c0 : at.r0, j0 = tall ? at.r0 : at.c0;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int i = (threadIdx.x >> 3) + 32 * k, j = 8 * (threadIdx.x & 7);
+    float v[8];
+    ns_load8<PLANES>(x.x[last] + (size_t)(i0 + i) * x.n + j0 + j, (size_t)x.m * x.n, v,
+                     1.0f / kNsScaleX);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (tall) lds[j + e][i] = v[e];
+      else lds[i][j + e] = v[e];
+    }
+  }
+  __syncthreads();
+  const int cl = 4 * (threadIdx.x & 15), c = at.c0 + cl, left = x.cols - c;
+  if (left <= 0) return;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int rl = (threadIdx.x >> 4) + 16 * k, r = at.r0 + rl;
+    if (r >= x.rows) continue;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = lds[rl][cl + e];
+    if constexpr (MODE == NsMode::Muon) {
+      const bool vec = rows_vec<float>(x.w, x.ld_src);
+      float w[4];
+      load4_cols(x.w + r * x.ld_src, c, left, vec, w);
+      const float keep = 1.0f - sc.lr * x.decay, step = sc.lr * x.scale;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = __builtin_fmaf(-step, v[e], w[e] * keep);
+      store4_cols(x.w + r * x.ld_src, c, left, vec, w);
+      if (x.copy)
+        store4_cols((CT*)x.copy + r * x.ld_src, c, left, rows_vec<CT>(x.copy, x.ld_src), w);
+    } else {
+      store4_cols((CT*)x.out + r * x.ld_out, c, left, rows_vec<CT>(x.out, x.ld_out), v);
+    }
+  }
+}
+
+template <NsMode MODE, int PLANES>
+void run(const NsTable& t, const NsScalars& sc, Dt copy_dt, double* partial, double* norm,
+         hipStream_t s) {
+  const int tiles = t.tile0[t.count];
+  ns_update_kernel<MODE><<<tiles, kThreads, 0, s>>>(t, sc, partial);
+  ns_norm_kernel<<<t.count, kThreads, 0, s>>>(t, sc.eps, partial, norm);
+  ns_init_kernel<MODE, PLANES><<<tiles, kThreads, 0, s>>>(t, sc, norm);
+  for (int k = 0; k < sc.steps; ++k) launch_ns_step(t, PLANES, k & 1, s);
+  const int last = sc.steps & 1;
+  if (MODE == NsMode::Bf16 || (MODE == NsMode::Muon && copy_dt == Dt::BF16))
+    ns_apply_kernel<MODE, PLANES, bf16><<<tiles, kThreads, 0, s>>>(t, sc, last);
+  else
+    ns_apply_kernel<MODE, PLANES, float><<<tiles, kThreads, 0, s>>>(t, sc, last);
+}
+
+}  // namespace
+
+void launch_newton_schulz(const NsTable& t, const NsScalars& sc, NsMode mode, Dt copy_dt,
+                          double* partial, double* norm, hipStream_t s) {
+  switch (mode) {
+    case NsMode::Muon:
+      if (sc.planes == 2) run<NsMode::Muon, 2>(t, sc, copy_dt, partial, norm, s);
+      else run<NsMode::Muon, 1>(t, sc, copy_dt, partial, norm, s);
+      break;
+    case NsMode::Bf16: run<NsMode::Bf16, 1>(t, sc, copy_dt, partial, norm, s); break;
+    case NsMode::F32: run<NsMode::F32, 2>(t, sc, copy_dt, partial, norm, s); break;
+  }
+}
+
+}  // namespace pb

@@ -1,0 +1,447 @@
+// C ABI of the operators around the block: rotary positions, the root-mean-square
+// norm, the Muon step and its orthogonalisation.  Argument checks are made on the
+// host before any HIP call.
+#include "abi.h"
+
+#include <math.h>
+
+#include <cmath>
+
+#include <algorithm>
+
+#include "kernels.h"
+
+using pb::align256;
+using pb::fail;
+using pb::finish_launches;
+
+namespace {
+
+constexpr long long kMaxInt = 2147483647LL;
+// Workgroups of 256 threads in a launch of fewer than 2^32 threads.
+constexpr long long kMaxBlocks = 1LL << 24;
+
+bool known(pb_dtype dt) { return dt == PB_BF16 || dt == PB_F32; }
+size_t size_of(pb_dtype dt) { return dt == PB_BF16 ? 2 : 4; }
+pb::Dt dt_of(pb_dtype dt) { return dt == PB_BF16 ? pb::Dt::BF16 : pb::Dt::F32; }
+
+pb_status check_ptr(const void* p, size_t align, const char* name) {
+  if (!p) return fail(PB_ERR_INVALID_ARG, "%s is NULL", name);
+  if ((uintptr_t)p % align)
+    return fail(PB_ERR_INVALID_ARG, "%s is not %zu-byte aligned", name, align);
+  return PB_OK;
+}
+pb_status check_opt(const void* p, size_t align, const char* name) {
+  return p ? check_ptr(p, align, name) : PB_OK;
+}
+pb_status check_ws(const void* ws, size_t bytes, size_t need) {
+  if (!need) return PB_OK;
+  if (!ws || (uintptr_t)ws % 256)
+    return fail(PB_ERR_INVALID_ARG, "ws is NULL or not 256-byte aligned");
+  if (bytes < need) return fail(PB_ERR_WORKSPACE, "ws_bytes=%zu < %zu needed", bytes, need);
+  return PB_OK;
+}
+
+// A call without any element: as finish_launches(), but no HIP call is made.
+pb_status nothing_to_do() {
+  pb::clear_error();
+  return PB_OK;
+}
+
+#define PB_CHECK(expr)                      \
+  do {                                      \
+    const pb_status st_ = (expr);           \
+    if (st_ != PB_OK) return st_;           \
+  } while (0)
+
+// ------------------------------------------------------- rotary positions
+pb_status check_rope(const pb_rope_config* c) {
+  if (!c) return fail(PB_ERR_INVALID_ARG, "cfg is NULL");
+  if (!known(c->dtype)) return fail(PB_ERR_INVALID_ARG, "unknown dtype %d", (int)c->dtype);
+  if (c->head_dim < 2 || c->head_dim % 2)
+    return fail(PB_ERR_INVALID_ARG, "head_dim=%d must be even and >= 2", c->head_dim);
+  if (c->head_dim > pb::kRopeMaxDim)
+    return fail(PB_ERR_UNSUPPORTED, "head_dim=%d > %d", c->head_dim, pb::kRopeMaxDim);
+  if (c->rot_dim < 2 || c->rot_dim % 2 || c->rot_dim > c->head_dim)
+    return fail(PB_ERR_INVALID_ARG, "rot_dim=%d must be even, in 2..head_dim=%d", c->rot_dim,
+                c->head_dim);
+  if (c->interleaved != 0 && c->interleaved != 1)
+    return fail(PB_ERR_INVALID_ARG, "interleaved must be 0 or 1");
+  if (!(c->base > 0.0) || !std::isfinite(c->base))
+    return fail(PB_ERR_INVALID_ARG, "base must be finite and > 0");
+  if (!(c->magnitude > 0.0) || !std::isfinite((float)c->magnitude))
+    return fail(PB_ERR_INVALID_ARG, "magnitude must be finite and > 0");
+  if (c->scaling < PB_ROPE_PLAIN || c->scaling > PB_ROPE_BY_PARTS)
+    return fail(PB_ERR_INVALID_ARG, "scaling=%d", c->scaling);
+  if (c->scaling != PB_ROPE_PLAIN && (!(c->factor > 0.0) || !std::isfinite(c->factor)))
+    return fail(PB_ERR_INVALID_ARG, "factor must be finite and > 0");
+  if (c->scaling == PB_ROPE_BY_PARTS) {
+    if (!(c->orig_len > 0.0) || !std::isfinite(c->orig_len))
+      return fail(PB_ERR_INVALID_ARG, "orig_len must be finite and > 0");
+    if (!(c->low_turns >= 0.0) || !(c->high_turns > c->low_turns) || !std::isfinite(c->high_turns))
+      return fail(PB_ERR_INVALID_ARG, "need 0 <= low_turns < high_turns, finite");
+  }
+  return PB_OK;
+}
+
+pb_status rope(const pb_rope_config* c, int n, const pb_rope_tensor* x, int64_t tokens,
+               int64_t seq, const int64_t* positions, bool backward, hipStream_t stream) {
+  PB_CHECK(check_rope(c));
+  if (n < 1 || n > PB_ROPE_MAX_TENSORS)
+    return fail(PB_ERR_INVALID_ARG, "n_tensors=%d must be in 1..%d", n, PB_ROPE_MAX_TENSORS);
+  if (!x) return fail(PB_ERR_INVALID_ARG, "tensors is NULL");
+  if (tokens < 0) return fail(PB_ERR_INVALID_ARG, "tokens=%lld", (long long)tokens);
+  if (tokens >= kMaxBlocks)
+    return fail(PB_ERR_UNSUPPORTED, "tokens=%lld >= 2^24", (long long)tokens);
+  if (!positions && seq < 1) return fail(PB_ERR_INVALID_ARG, "seq must be >= 1");
+  PB_CHECK(check_opt(positions, 8, "positions"));
+  static_assert(PB_ROPE_MAX_TENSORS == pb::kRopeMaxTensors, "tensor limit");
+  static_assert(sizeof(int64_t) == sizeof(long long), "positions");
+  pb::RopeArgs a{};
+  const size_t e = size_of(c->dtype);
+  for (int i = 0; i < n; ++i) {
+    if (x[i].heads < 1) return fail(PB_ERR_INVALID_ARG, "tensor %d: heads=%d", i, x[i].heads);
+    if (x[i].heads > 8192)
+      return fail(PB_ERR_UNSUPPORTED, "tensor %d: heads=%d > 8192", i, x[i].heads);
+    const size_t width = (size_t)x[i].heads * c->head_dim;
+    if (x[i].ld_in < width || x[i].ld_out < width)
+      return fail(PB_ERR_INVALID_ARG, "tensor %d: ld_in=%zu, ld_out=%zu < heads*head_dim=%zu", i,
+                  x[i].ld_in, x[i].ld_out, width);
+    if (std::max(x[i].ld_in, x[i].ld_out) > ((size_t)1 << 31))
+      return fail(PB_ERR_UNSUPPORTED, "tensor %d: ld over 2^31 elements", i);
+    if (tokens > 0) {
+      if (!x[i].in || (uintptr_t)x[i].in % e)
+        return fail(PB_ERR_INVALID_ARG, "tensor %d: in is NULL or misaligned", i);
+      if (!x[i].out || (uintptr_t)x[i].out % e)
+        return fail(PB_ERR_INVALID_ARG, "tensor %d: out is NULL or misaligned", i);
+    }
+    if (x[i].in == x[i].out && x[i].ld_in != x[i].ld_out)
+      return fail(PB_ERR_INVALID_ARG, "tensor %d: in place needs ld_out = ld_in", i);
+    a.in[i] = x[i].in;
+    a.out[i] = x[i].out;
+    a.ld_in[i] = (long long)x[i].ld_in;
+    a.ld_out[i] = (long long)x[i].ld_out;
+    a.heads[i] = x[i].heads;
+    a.copy_rest[i] = x[i].in != x[i].out;
+  }
+  a.n = n;
+  a.head_dim = c->head_dim;
+  a.rot_dim = c->rot_dim;
+  a.backward = backward;
+  a.magnitude = (float)c->magnitude;
+  a.tokens = tokens;
+  a.seq = positions ? 1 : std::min<int64_t>(seq, kMaxInt);
+  a.pos = (const long long*)positions;
+  const double two_pi = 6.283185307179586476925286766559;
+  for (int i = 0; i < c->rot_dim / 2; ++i) {
+    double f = pow(c->base, -2.0 * i / c->rot_dim);
+    if (c->scaling == PB_ROPE_LINEAR) f /= c->factor;
+    if (c->scaling == PB_ROPE_BY_PARTS) {
+      const double g = std::min(1.0, std::max(0.0, (c->orig_len * f / two_pi - c->low_turns) /
+                                                       (c->high_turns - c->low_turns)));
+      f *= g + (1.0 - g) / c->factor;
+    }
+    a.turns[i] = f / two_pi;
+  }
+  if (tokens == 0) return nothing_to_do();
+  pb::launch_rope(dt_of(c->dtype), a, c->interleaved != 0, stream);
+  return finish_launches();
+}
+
+// ------------------------------------------------- root-mean-square norm
+pb_status check_rms(const pb_rmsnorm_config* c) {
+  if (!c) return fail(PB_ERR_INVALID_ARG, "cfg is NULL");
+  if (!known(c->dtype)) return fail(PB_ERR_INVALID_ARG, "unknown dtype %d", (int)c->dtype);
+  if (c->rows < 0 || c->cols < 1)
+    return fail(PB_ERR_INVALID_ARG, "rows=%lld must be >= 0, cols=%d >= 1", (long long)c->rows,
+                c->cols);
+  if (c->rows > kMaxInt) return fail(PB_ERR_UNSUPPORTED, "rows=%lld > 2^31 - 1", (long long)c->rows);
+  if (c->cols > 32768)
+    return fail(PB_ERR_UNSUPPORTED, "cols=%d > 32768 (a row is kept in registers)", c->cols);
+  if (c->group != 0 && c->group != 32 && c->group != 64 && c->group != 128)
+    return fail(PB_ERR_INVALID_ARG, "group=%d must be 0, 32, 64 or 128", c->group);
+  if (!(c->eps >= 0.f) || !std::isfinite(c->eps))
+    return fail(PB_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  return PB_OK;
+}
+
+// ------------------------------------------------------------- Muon step
+static_assert(PB_MUON_MAX_TENSORS == pb::kNsMaxTensors, "tensor limit");
+
+// Workspace: partial sums, norms, then each matrix's planes.
+struct NsLayout {
+  size_t partial, norm, planes;  // offsets; planes: of the first matrix
+  size_t total;
+};
+
+int pad(int v) { return (v + pb::kNsPad - 1) / pb::kNsPad * pb::kNsPad; }
+
+pb_status ns_sizes(int i, int rows, int cols) {
+  if (rows < 0 || cols < 0)
+    return fail(PB_ERR_INVALID_ARG, "tensor %d: rows=%d, cols=%d", i, rows, cols);
+  if (std::min(rows, cols) > 65536 || std::max(rows, cols) > (1 << 20))
+    return fail(PB_ERR_UNSUPPORTED, "tensor %d: %d x %d is over 65536 x 2^20", i, rows, cols);
+  return PB_OK;
+}
+
+// Fills the sizes of t.mat[i] (an empty matrix is left out); false: too many tiles.
+bool ns_add(pb::NsTable& t, int rows, int cols) {
+  pb::NsMat& x = t.mat[t.count];
+  x.rows = rows;
+  x.cols = cols;
+  x.m = pad(std::min(rows, cols));
+  x.n = pad(std::max(rows, cols));
+  const long long tiles =
+      t.tile0[t.count] + (long long)(pad(rows) / pb::kNsPad) * (pad(cols) / pb::kNsPad);
+  t.tile0[++t.count] = (int)std::min(tiles, kMaxBlocks);
+  return tiles < kMaxBlocks;
+}
+
+// Places the planes of every matrix from base on (nullptr: sizes alone).
+NsLayout ns_layout(pb::NsTable& t, int planes, char* base) {
+  NsLayout L{};
+  L.norm = align256((size_t)t.tile0[t.count] * sizeof(double));
+  L.planes = L.norm + align256((size_t)t.count * sizeof(double));
+  size_t o = L.planes;
+  for (int i = 0; i < t.count; ++i) {
+    pb::NsMat& x = t.mat[i];
+    const size_t big = align256((size_t)planes * x.m * x.n * 2);
+    const size_t small = align256((size_t)planes * x.m * x.m * 2);
+    x.x[0] = (_Float16*)(base + o);
+    x.x[1] = (_Float16*)(base + o + big);
+    x.a = (_Float16*)(base + o + 2 * big);
+    x.b = (_Float16*)(base + o + 2 * big + small);
+    o += 2 * big + 2 * small;
+  }
+  L.total = t.count ? o : 0;
+  return L;
+}
+
+pb_status check_count(int n, const void* tensors) {
+  if (n < 1 || n > PB_MUON_MAX_TENSORS)
+    return fail(PB_ERR_INVALID_ARG, "n_tensors=%d must be in 1..%d", n, PB_MUON_MAX_TENSORS);
+  if (!tensors) return fail(PB_ERR_INVALID_ARG, "tensors is NULL");
+  return PB_OK;
+}
+
+// The table of a call's matrices without their pointers into the workspace.
+template <typename X>
+pb_status ns_table(int n, const X* x, pb::NsTable& t) {
+  PB_CHECK(check_count(n, x));
+  for (int i = 0; i < n; ++i) {
+    PB_CHECK(ns_sizes(i, x[i].rows, x[i].cols));
+    if (x[i].rows == 0 || x[i].cols == 0) continue;
+    if (!ns_add(t, x[i].rows, x[i].cols))
+      return fail(PB_ERR_UNSUPPORTED, "too many elements in one call");
+  }
+  return PB_OK;
+}
+
+pb_status check_steps(int steps, float eps) {
+  if (steps < 1 || steps > 16) return fail(PB_ERR_INVALID_ARG, "steps=%d must be in 1..16", steps);
+  if (!(eps > 0.f) || !std::isfinite(eps))
+    return fail(PB_ERR_INVALID_ARG, "eps=%g must be positive and finite", (double)eps);
+  return PB_OK;
+}
+
+void ns_launch(pb::NsTable& t, const pb::NsScalars& sc, pb::NsMode mode, pb::Dt copy_dt, char* ws,
+               hipStream_t stream) {
+  const NsLayout L = ns_layout(t, sc.planes, ws);
+  pb::launch_newton_schulz(t, sc, mode, copy_dt, (double*)(ws + L.partial), (double*)(ws + L.norm),
+                           stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+pb_status pblock_rope_forward(const pb_rope_config* cfg, int n_tensors,
+                              const pb_rope_tensor* tensors, int64_t tokens, int64_t seq,
+                              const int64_t* positions, hipStream_t stream) {
+  return rope(cfg, n_tensors, tensors, tokens, seq, positions, false, stream);
+}
+
+pb_status pblock_rope_backward(const pb_rope_config* cfg, int n_tensors,
+                               const pb_rope_tensor* tensors, int64_t tokens, int64_t seq,
+                               const int64_t* positions, hipStream_t stream) {
+  return rope(cfg, n_tensors, tensors, tokens, seq, positions, true, stream);
+}
+
+pb_status pblock_rmsnorm_forward(const pb_rmsnorm_config* cfg, const void* x, const void* resid,
+                                 const void* gamma, void* sum, void* y, uint8_t* q8, float* scales,
+                                 float* rstd, hipStream_t stream) {
+  PB_CHECK(check_rms(cfg));
+  const size_t e = size_of(cfg->dtype);
+  if (cfg->rows > 0) {
+    PB_CHECK(check_ptr(x, e, "x"));
+    PB_CHECK(check_opt(resid, e, "resid"));
+    PB_CHECK(check_opt(sum, e, "sum"));
+    PB_CHECK(check_opt(y, e, "y"));
+    PB_CHECK(check_opt(scales, 4, "scales"));
+    PB_CHECK(check_opt(rstd, 4, "rstd"));
+    if (!y && !q8) return fail(PB_ERR_INVALID_ARG, "y and q8 are both NULL");
+    if (!q8 != !scales) return fail(PB_ERR_INVALID_ARG, "q8 and scales come together");
+    if (sum && !resid) return fail(PB_ERR_INVALID_ARG, "sum without resid");
+    if (sum && sum == y) return fail(PB_ERR_INVALID_ARG, "sum and y are the same buffer");
+  }
+  PB_CHECK(check_ptr(gamma, e, "gamma"));
+  if (cfg->rows == 0) return nothing_to_do();
+  pb::RmsForward a{};
+  a.x = x;
+  a.resid = resid;
+  a.gamma = gamma;
+  a.sum = sum;
+  a.y = y;
+  a.q8 = q8;
+  a.scales = scales;
+  a.rstd = rstd;
+  a.rows = cfg->rows;
+  a.cols = cfg->cols;
+  a.group = cfg->group;
+  a.eps = cfg->eps;
+  pb::launch_rms_forward(dt_of(cfg->dtype), a, stream);
+  return finish_launches();
+}
+
+size_t pblock_rmsnorm_workspace_bytes(const pb_rmsnorm_config* cfg) {
+  if (check_rms(cfg) != PB_OK) return 0;
+  return align256((size_t)pb::rms_backward_parts(cfg->rows, cfg->cols) * cfg->cols * 4);
+}
+
+pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s, const void* gamma,
+                                  const float* rstd, const void* dy, const void* dsum, void* dx,
+                                  float* dgamma, void* ws, size_t ws_bytes, hipStream_t stream) {
+  PB_CHECK(check_rms(cfg));
+  const size_t e = size_of(cfg->dtype);
+  if (cfg->rows > 0) {
+    PB_CHECK(check_ptr(s, e, "s"));
+    PB_CHECK(check_ptr(rstd, 4, "rstd"));
+    PB_CHECK(check_ptr(dy, e, "dy"));
+    PB_CHECK(check_opt(dsum, e, "dsum"));
+    PB_CHECK(check_ptr(dx, e, "dx"));
+  }
+  PB_CHECK(check_ptr(gamma, e, "gamma"));
+  PB_CHECK(check_ptr(dgamma, 4, "dgamma"));
+  PB_CHECK(check_ws(ws, ws_bytes, pblock_rmsnorm_workspace_bytes(cfg)));
+  pb::RmsBackward a{};
+  a.s = s;
+  a.gamma = gamma;
+  a.dy = dy;
+  a.dsum = dsum;
+  a.rstd = rstd;
+  a.dx = dx;
+  a.dgamma = dgamma;
+  a.part = (float*)ws;
+  a.rows = cfg->rows;
+  a.cols = cfg->cols;
+  pb::launch_rms_backward(dt_of(cfg->dtype), a, stream);
+  return finish_launches();
+}
+
+size_t pblock_muon_workspace_bytes(const pb_muon_config* cfg, int n_tensors,
+                                   const pb_muon_tensor* tensors) {
+  pb::NsTable t{};
+  if (!cfg || !known(cfg->products) || ns_table(n_tensors, tensors, t) != PB_OK) return 0;
+  return ns_layout(t, cfg->products == PB_F32 ? 2 : 1, nullptr).total;
+}
+
+pb_status pblock_muon_step(const pb_muon_config* cfg, int n_tensors, const pb_muon_tensor* tensors,
+                           pb_dtype copy_dtype, void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (!cfg) return fail(PB_ERR_INVALID_ARG, "cfg is NULL");
+  if (!std::isfinite(cfg->lr)) return fail(PB_ERR_INVALID_ARG, "lr is not finite");
+  if (!(cfg->momentum >= 0.f && cfg->momentum < 1.f))
+    return fail(PB_ERR_INVALID_ARG, "momentum=%g must be in [0, 1)", (double)cfg->momentum);
+  if (!std::isfinite(cfg->grad_scale)) return fail(PB_ERR_INVALID_ARG, "grad_scale is not finite");
+  PB_CHECK(check_steps(cfg->steps, cfg->eps));
+  if (cfg->nesterov != 0 && cfg->nesterov != 1)
+    return fail(PB_ERR_INVALID_ARG, "nesterov must be 0 or 1");
+  if (!known(cfg->products)) return fail(PB_ERR_INVALID_ARG, "products=%d", (int)cfg->products);
+  if (!known(copy_dtype)) return fail(PB_ERR_INVALID_ARG, "copy_dtype=%d", (int)copy_dtype);
+  pb::NsTable t{};
+  PB_CHECK(ns_table(n_tensors, tensors, t));
+  int k = 0;
+  for (int i = 0; i < n_tensors; ++i) {
+    const pb_muon_tensor& x = tensors[i];
+    if (!(x.weight_decay >= 0.f) || !std::isfinite(x.weight_decay))
+      return fail(PB_ERR_INVALID_ARG, "tensor %d: weight_decay=%g", i, (double)x.weight_decay);
+    if (!std::isfinite(x.scale))
+      return fail(PB_ERR_INVALID_ARG, "tensor %d: scale=%g", i, (double)x.scale);
+    if (x.rows == 0 || x.cols == 0) continue;
+    if (x.ld < (size_t)x.cols || x.ld > ((size_t)1 << 31))
+      return fail(PB_ERR_INVALID_ARG, "tensor %d: ld=%zu outside cols=%d .. 2^31", i, x.ld, x.cols);
+    const char* names[3] = {"param", "grad", "momentum"};
+    const void* ptrs[3] = {x.param, x.grad, x.momentum};
+    for (int j = 0; j < 3; ++j)
+      if (!ptrs[j] || (uintptr_t)ptrs[j] % 4)
+        return fail(PB_ERR_INVALID_ARG, "tensor %d: %s is NULL or not 4-byte aligned", i, names[j]);
+    if (x.param_copy && (uintptr_t)x.param_copy % size_of(copy_dtype))
+      return fail(PB_ERR_INVALID_ARG, "tensor %d: param_copy is misaligned", i);
+    pb::NsMat& m = t.mat[k++];
+    m.src = x.grad;
+    m.mom = x.momentum;
+    m.w = x.param;
+    m.copy = x.param_copy;
+    m.ld_src = m.ld_out = (long long)x.ld;
+    m.decay = x.weight_decay;
+    m.scale = x.scale;
+  }
+  PB_CHECK(check_ws(ws, ws_bytes, pblock_muon_workspace_bytes(cfg, n_tensors, tensors)));
+  if (t.count == 0) return nothing_to_do();
+  pb::NsScalars sc{};
+  sc.lr = cfg->lr;
+  sc.momentum = cfg->momentum;
+  sc.grad_scale = cfg->grad_scale;
+  sc.eps = cfg->eps;
+  sc.nesterov = cfg->nesterov;
+  sc.planes = cfg->products == PB_F32 ? 2 : 1;
+  sc.steps = cfg->steps;
+  ns_launch(t, sc, pb::NsMode::Muon, dt_of(copy_dtype), (char*)ws, stream);
+  return finish_launches();
+}
+
+size_t pblock_orthogonalize_workspace_bytes(int n_tensors, const pb_ortho_tensor* tensors,
+                                            pb_dtype dtype) {
+  pb::NsTable t{};
+  if (!known(dtype) || ns_table(n_tensors, tensors, t) != PB_OK) return 0;
+  return ns_layout(t, dtype == PB_F32 ? 2 : 1, nullptr).total;
+}
+
+pb_status pblock_orthogonalize(int n_tensors, const pb_ortho_tensor* tensors, pb_dtype dtype,
+                               int steps, float eps, void* ws, size_t ws_bytes,
+                               hipStream_t stream) {
+  if (!known(dtype)) return fail(PB_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+  PB_CHECK(check_steps(steps, eps));
+  pb::NsTable t{};
+  PB_CHECK(ns_table(n_tensors, tensors, t));
+  const size_t e = size_of(dtype);
+  int k = 0;
+  for (int i = 0; i < n_tensors; ++i) {
+    const pb_ortho_tensor& x = tensors[i];
+    if (x.rows == 0 || x.cols == 0) continue;
+    if (!x.in || (uintptr_t)x.in % e)
+      return fail(PB_ERR_INVALID_ARG, "tensor %d: in is NULL or misaligned", i);
+    if (!x.out || (uintptr_t)x.out % e)
+      return fail(PB_ERR_INVALID_ARG, "tensor %d: out is NULL or misaligned", i);
+    for (size_t ld : {x.ld_in, x.ld_out})
+      if (ld < (size_t)x.cols || ld > ((size_t)1 << 31))
+        return fail(PB_ERR_INVALID_ARG, "tensor %d: ld=%zu outside cols=%d .. 2^31", i, ld, x.cols);
+    if (x.in == x.out && x.ld_in != x.ld_out)
+      return fail(PB_ERR_INVALID_ARG, "tensor %d: in place needs ld_out = ld_in", i);
+    pb::NsMat& m = t.mat[k++];
+    m.src = x.in;
+    m.out = x.out;
+    m.ld_src = (long long)x.ld_in;
+    m.ld_out = (long long)x.ld_out;
+  }
+  PB_CHECK(check_ws(ws, ws_bytes, pblock_orthogonalize_workspace_bytes(n_tensors, tensors, dtype)));
+  if (t.count == 0) return nothing_to_do();
+  pb::NsScalars sc{};
+  sc.eps = eps;
+  sc.steps = steps;
+  sc.planes = dtype == PB_F32 ? 2 : 1;
+  ns_launch(t, sc, dtype == PB_F32 ? pb::NsMode::F32 : pb::NsMode::Bf16, dt_of(dtype), (char*)ws,
+            stream);
+  return finish_launches();
+}
+
+}  // extern "C"

@@ -19,11 +19,14 @@
 #include <stdio.h>
 #include <string.h>
 
+#include "abi.h"
 #include "kernels.h"
 
 namespace {
-
 thread_local char g_err[512] = "";
+}
+
+namespace pb {
 
 pb_status fail(pb_status st, const char* fmt, ...) {
   va_list ap;
@@ -32,6 +35,23 @@ pb_status fail(pb_status st, const char* fmt, ...) {
   va_end(ap);
   return st;
 }
+
+void clear_error() { g_err[0] = '\0'; }
+
+pb_status finish_launches() {
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(PB_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+  clear_error();
+  return PB_OK;
+}
+
+}  // namespace pb
+
+namespace {
+
+using pb::align256;
+using pb::fail;
+using pb::finish_launches;
 
 // Records the caller's step events (the *_timed entry points) around the
 // launches of one step; ev may be NULL.
@@ -46,8 +66,6 @@ struct StepScope {
     if (ev && ev->end[step]) (void)hipEventRecord(ev->end[step], s);
   }
 };
-
-size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
 struct Dims {
   long long T, H, A, F, N_in, K_out, heads, d, B, S, W;
@@ -377,13 +395,6 @@ pb_status check_ptr(const void* p, const char* name) {
     pb_status _st = (expr);        \
     if (_st != PB_OK) return _st;  \
   } while (0)
-
-pb_status finish_launches() {
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(PB_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
-  g_err[0] = '\0';
-  return PB_OK;
-}
 
 pb::Dt dt_of(const pb_config* c) { return c->dtype == PB_BF16 ? pb::Dt::BF16 : pb::Dt::F32; }
 

@@ -11,7 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_float, c_int, c_size_t, c_void_p
+from ctypes import POINTER, c_double, c_float, c_int, c_int64, c_size_t, c_void_p
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libpblock.so")
@@ -44,9 +44,16 @@ EXPORTS = (
     "pblock_rs_out_proj_workspace_bytes", "pblock_rs_out_proj", "pblock_rs_reduce",
     "pblock_ag_dc_workspace_bytes", "pblock_ag_dc", "pblock_rs_dh_workspace_bytes", "pblock_rs_dh",
     "pblock_swattn_forward_noalloc",
+    "pblock_rope_forward", "pblock_rope_backward",
+    "pblock_rmsnorm_forward", "pblock_rmsnorm_workspace_bytes", "pblock_rmsnorm_backward",
+    "pblock_muon_workspace_bytes", "pblock_muon_step",
+    "pblock_orthogonalize_workspace_bytes", "pblock_orthogonalize",
 )
 NOALLOC_SCRATCH_BYTES = 32 << 20  # PB_NOALLOC_SCRATCH_BYTES
 LAMB_MAX_TENSORS = 16
+ROPE_MAX_TENSORS = 4
+MUON_MAX_TENSORS = 16
+ROPE_SCALING = ("plain", "linear", "by_parts")  # pb_rope_scaling
 
 # pb_step order of include/pblock.h
 STEPS = ("ln_fwd", "in_proj", "attn_fwd", "out_proj", "dc", "dw_out", "db_out", "attn_bwd", "dh",
@@ -86,6 +93,45 @@ class LambTensor(ctypes.Structure):
     _fields_ = [("param", c_void_p), ("grad", c_void_p), ("exp_avg", c_void_p),
                 ("exp_avg_sq", c_void_p), ("param_copy", c_void_p), ("numel", c_size_t),
                 ("weight_decay", c_float)]
+
+
+class RopeConfig(ctypes.Structure):
+    """pb_rope_config."""
+    _fields_ = [("head_dim", c_int), ("rot_dim", c_int), ("interleaved", c_int),
+                ("scaling", c_int), ("base", c_double), ("factor", c_double),
+                ("orig_len", c_double), ("low_turns", c_double), ("high_turns", c_double),
+                ("magnitude", c_double), ("dtype", c_int)]
+
+
+class RopeTensor(ctypes.Structure):
+    """pb_rope_tensor (device addresses as integers)."""
+    _fields_ = [("in_", c_void_p), ("out", c_void_p), ("ld_in", c_size_t), ("ld_out", c_size_t),
+                ("heads", c_int)]
+
+
+class RmsnormConfig(ctypes.Structure):
+    """pb_rmsnorm_config."""
+    _fields_ = [("rows", c_int64), ("cols", c_int), ("group", c_int), ("eps", c_float),
+                ("dtype", c_int)]
+
+
+class MuonConfig(ctypes.Structure):
+    """pb_muon_config."""
+    _fields_ = [("lr", c_float), ("momentum", c_float), ("grad_scale", c_float), ("eps", c_float),
+                ("nesterov", c_int), ("steps", c_int), ("products", c_int)]
+
+
+class MuonTensor(ctypes.Structure):
+    """pb_muon_tensor (device addresses as integers)."""
+    _fields_ = [("param", c_void_p), ("grad", c_void_p), ("momentum", c_void_p),
+                ("param_copy", c_void_p), ("rows", c_int), ("cols", c_int), ("ld", c_size_t),
+                ("weight_decay", c_float), ("scale", c_float)]
+
+
+class OrthoTensor(ctypes.Structure):
+    """pb_ortho_tensor (device addresses as integers)."""
+    _fields_ = [("in_", c_void_p), ("out", c_void_p), ("rows", c_int), ("cols", c_int),
+                ("ld_in", c_size_t), ("ld_out", c_size_t)]
 
 
 class PblockError(RuntimeError):
@@ -163,6 +209,20 @@ def load_library(path: str = LIB_PATH):
                                  c_size_t, P, c_int, POINTER(c_void_p), P]),
         "pblock_lamb_step": (c_int, [POINTER(LambConfig), c_int, POINTER(LambTensor), c_int, P, P,
                                      c_size_t, P]),
+        "pblock_rope_forward": (c_int, [POINTER(RopeConfig), c_int, POINTER(RopeTensor), c_int64,
+                                        c_int64, P, P]),
+        "pblock_rope_backward": (c_int, [POINTER(RopeConfig), c_int, POINTER(RopeTensor), c_int64,
+                                         c_int64, P, P]),
+        "pblock_rmsnorm_forward": (c_int, [POINTER(RmsnormConfig)] + [P] * 9),
+        "pblock_rmsnorm_workspace_bytes": (c_size_t, [POINTER(RmsnormConfig)]),
+        "pblock_rmsnorm_backward": (c_int, [POINTER(RmsnormConfig)] + [P] * 8 + [c_size_t, P]),
+        "pblock_muon_workspace_bytes": (c_size_t, [POINTER(MuonConfig), c_int,
+                                                   POINTER(MuonTensor)]),
+        "pblock_muon_step": (c_int, [POINTER(MuonConfig), c_int, POINTER(MuonTensor), c_int, P,
+                                     c_size_t, P]),
+        "pblock_orthogonalize_workspace_bytes": (c_size_t, [c_int, POINTER(OrthoTensor), c_int]),
+        "pblock_orthogonalize": (c_int, [c_int, POINTER(OrthoTensor), c_int, c_int, c_float, P,
+                                         c_size_t, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -516,6 +576,258 @@ def pblock_rs_reduce(cfg, tp, parts, x_shard, b_out, y_shard, stream=None):
     arr = (c_void_p * len(parts))(*[_ptr(t) for t in parts])
     _check(load_library().pblock_rs_reduce(ctypes.byref(cfg), int(tp), arr, _ptr(x_shard),
                                            _ptr(b_out), _ptr(y_shard), _stream(stream)))
+
+
+# ------------------------------------------- operators around the block
+# These calls also check what a tensor says of itself (type, size, device); raw
+# addresses are taken as they are.  They run on the tensors' device, whichever
+# device is current, by default on that device's current stream.
+def _dtype_of(name: str) -> int:
+    if name not in ("bf16", "f32"):
+        raise ValueError(f"dtype {name!r} is neither 'bf16' nor 'f32'")
+    return PB_BF16 if name == "bf16" else PB_F32
+
+
+def _torch_dtype(code: int):
+    import torch
+    return torch.bfloat16 if code == PB_BF16 else torch.float32
+
+
+def _expect(name, t, dtype=None, numel=None, contiguous=True):
+    if t is None or isinstance(t, int):
+        return
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} is {t.dtype}, not {dtype}")
+    if numel is not None and t.numel() != numel:
+        raise ValueError(f"{name} has {t.numel()} elements, not {numel}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name} is not contiguous")
+
+
+class _On:
+    """The device and stream of a call: those of its tensors."""
+
+    def __init__(self, tensors: dict, stream):
+        devices = {}
+        for name, t in tensors.items():
+            if t is None or isinstance(t, int):
+                continue
+            if t.device.type != "cuda":
+                raise ValueError(f"{name} is on {t.device}, not on a GPU")
+            devices.setdefault(t.device.index, name)
+        if len(devices) > 1:
+            a, b = list(devices.items())[:2]
+            raise ValueError(f"{a[1]} and {b[1]} are on different devices ({a[0]} and {b[0]})")
+        self.index = next(iter(devices), None)
+        at = getattr(getattr(stream, "device", None), "index", None)
+        if at is not None and self.index is not None and at != self.index:
+            raise ValueError(f"the stream is on device {at}, the tensors on {self.index}")
+        self.stream = stream
+
+    def __enter__(self):
+        import torch
+        self.guard = None
+        if self.index is not None and self.index != torch.cuda.current_device():
+            self.guard = torch.cuda.device(self.index)
+            self.guard.__enter__()
+        return _stream(self.stream)
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def rope_config(head_dim, rot_dim=None, interleaved=False, base=10000.0, scaling="plain",
+                factor=1.0, orig_len=0.0, low_turns=1.0, high_turns=32.0, magnitude=1.0,
+                dtype="bf16") -> RopeConfig:
+    """scaling: one of ROPE_SCALING; rot_dim: the whole head by default."""
+    if scaling not in ROPE_SCALING:
+        raise ValueError(f"scaling {scaling!r} is not one of {ROPE_SCALING}")
+    return RopeConfig(head_dim, head_dim if rot_dim is None else rot_dim, int(bool(interleaved)),
+                      ROPE_SCALING.index(scaling), base, factor, orig_len, low_turns, high_turns,
+                      magnitude, _dtype_of(dtype))
+
+
+def rope_tensor(x, ld, heads, out=None, ld_out=None) -> RopeTensor:
+    """A pb_rope_tensor: x and out are tensors (or addresses) whose first
+    element is that of token 0, head 0; ld and ld_out the elements from token
+    to token.  Without out, in place."""
+    r = RopeTensor(_ptr(x), _ptr(x if out is None else out), ld,
+                   ld if ld_out is None else ld_out, heads)
+    r.tensors = (x, out)  # kept alive, and for their checks
+    return r
+
+
+def _rope(fn, cfg, tensors, tokens, seq, positions, stream):
+    import torch
+    named = {"positions": positions}
+    act = _torch_dtype(cfg.dtype)
+    for i, r in enumerate(tensors):
+        for name, t, ld in zip(("in", "out"), getattr(r, "tensors", ()), (r.ld_in, r.ld_out)):
+            named[f"tensor {i}: {name}"] = t
+            _expect(f"tensor {i}: {name}", t, act, contiguous=False)
+            if t is None or isinstance(t, int) or tokens < 1:
+                continue
+            left = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+            need = (tokens - 1) * ld + r.heads * cfg.head_dim
+            if left < need:
+                raise ValueError(f"tensor {i}: {name} ends {need - left} elements short of "
+                                 f"{tokens} tokens")
+    _expect("positions", positions, torch.int64, tokens)
+    arr = (RopeTensor * len(tensors))(*tensors)
+    with _On(named, stream) as st:
+        _check(getattr(load_library(), fn)(ctypes.byref(cfg), len(tensors), arr, int(tokens),
+                                           int(tokens if seq is None else seq), _ptr(positions),
+                                           st))
+
+
+def pblock_rope_forward(cfg: RopeConfig, tensors, tokens, seq=None, positions=None, stream=None):
+    """tensors: a sequence of RopeTensor; positions: int64 [tokens], or None for
+    token mod seq (seq: tokens by default)."""
+    _rope("pblock_rope_forward", cfg, tensors, tokens, seq, positions, stream)
+
+
+def pblock_rope_backward(cfg: RopeConfig, tensors, tokens, seq=None, positions=None, stream=None):
+    """The gradients of pblock_rope_forward's inputs from those of its outputs."""
+    _rope("pblock_rope_backward", cfg, tensors, tokens, seq, positions, stream)
+
+
+def rmsnorm_config(rows, cols, eps=1e-5, dtype="bf16", group=0) -> RmsnormConfig:
+    """group: columns that share a scale of the 8-bit output (0: a row)."""
+    return RmsnormConfig(rows, cols, group, eps, _dtype_of(dtype))
+
+
+def pblock_rmsnorm_forward(cfg: RmsnormConfig, x, gamma, y=None, resid=None, sum_out=None, q8=None,
+                           scales=None, rstd=None, stream=None):
+    """q8: float8_e4m3fn (or uint8) [rows, cols]; scales: fp32 [rows, groups]."""
+    import torch
+    act, n = _torch_dtype(cfg.dtype), cfg.rows * cfg.cols
+    for name, t in (("x", x), ("resid", resid), ("sum_out", sum_out), ("y", y)):
+        _expect(name, t, act, n)
+    _expect("gamma", gamma, act, cfg.cols)
+    _expect("q8", q8, None, n)
+    if q8 is not None and not isinstance(q8, int) and q8.dtype not in (torch.float8_e4m3fn,
+                                                                       torch.uint8):
+        raise ValueError(f"q8 is {q8.dtype}, not float8_e4m3fn or uint8")
+    groups = -(-cfg.cols // cfg.group) if cfg.group > 0 else 1
+    _expect("scales", scales, torch.float32, cfg.rows * groups)
+    _expect("rstd", rstd, torch.float32, cfg.rows)
+    with _On(dict(x=x, gamma=gamma, y=y, resid=resid, sum_out=sum_out, q8=q8, scales=scales,
+                  rstd=rstd), stream) as st:
+        _check(load_library().pblock_rmsnorm_forward(
+            ctypes.byref(cfg), _ptr(x), _ptr(resid), _ptr(gamma), _ptr(sum_out), _ptr(y),
+            _ptr(q8), _ptr(scales), _ptr(rstd), st))
+
+
+def pblock_rmsnorm_workspace_bytes(cfg: RmsnormConfig) -> int:
+    """Bytes that pblock_rmsnorm_backward needs."""
+    return load_library().pblock_rmsnorm_workspace_bytes(ctypes.byref(cfg))
+
+
+def pblock_rmsnorm_backward(cfg: RmsnormConfig, s, gamma, rstd, dy, dx, dgamma, ws, dsum=None,
+                            stream=None):
+    """s: the forward's sum_out (its x where there was no residual)."""
+    import torch
+    act, n = _torch_dtype(cfg.dtype), cfg.rows * cfg.cols
+    for name, t in (("s", s), ("dy", dy), ("dsum", dsum), ("dx", dx)):
+        _expect(name, t, act, n)
+    _expect("gamma", gamma, act, cfg.cols)
+    _expect("rstd", rstd, torch.float32, cfg.rows)
+    _expect("dgamma", dgamma, torch.float32, cfg.cols)
+    with _On(dict(s=s, gamma=gamma, rstd=rstd, dy=dy, dsum=dsum, dx=dx, dgamma=dgamma, ws=ws),
+             stream) as st:
+        _check(load_library().pblock_rmsnorm_backward(
+            ctypes.byref(cfg), _ptr(s), _ptr(gamma), _ptr(rstd), _ptr(dy), _ptr(dsum), _ptr(dx),
+            _ptr(dgamma), _ptr(ws), _nbytes(ws), st))
+
+
+def muon_config(lr, momentum=0.95, nesterov=True, steps=5, eps=1e-7, grad_scale=1.0,
+                products="f32") -> MuonConfig:
+    """products: "f32" (22 bits of each factor) or "bf16" (one fp16 product, a
+    third of the time)."""
+    return MuonConfig(lr, momentum, grad_scale, eps, int(bool(nesterov)), int(steps),
+                      _dtype_of(products))
+
+
+def _rows(name, t, like=None):
+    """Elements from row to row of a matrix whose rows are contiguous."""
+    if t.dim() != 2:
+        raise ValueError(f"{name} has {t.dim()} dimensions, not 2")
+    if like is not None and t.shape != like.shape:
+        raise ValueError(f"{name} is {tuple(t.shape)}, not {tuple(like.shape)}")
+    r, c = t.shape
+    if (c > 1 and t.stride(1) != 1) or (r > 1 and t.stride(0) < c):
+        raise ValueError(f"{name}'s rows are not contiguous (strides {t.stride()})")
+    return t.stride(0) if r > 1 else max(c, 1)
+
+
+def muon_tensor(param, grad, momentum, param_copy=None, weight_decay=0.0, scale=1.0) -> MuonTensor:
+    """A pb_muon_tensor from matrices (or slices of packed weights, of one
+    stride from row to row): fp32 param, grad and momentum, and a copy."""
+    import torch
+    named = {"param": param, "grad": grad, "momentum": momentum, "param_copy": param_copy}
+    for name, t in named.items():
+        if t is None and name == "param_copy":
+            continue
+        if _rows(name, t, param) != _rows("param", param):
+            raise ValueError(f"{name} has another stride than param")
+        if name != "param_copy":
+            _expect(name, t, torch.float32, contiguous=False)
+    r = MuonTensor(_ptr(param), _ptr(grad), _ptr(momentum), _ptr(param_copy), param.shape[0],
+                   param.shape[1], _rows("param", param), weight_decay, scale)
+    r.tensors = named
+    return r
+
+
+def _named(tensors):
+    return {f"tensor {i}: {n}": t for i, r in enumerate(tensors)
+            for n, t in getattr(r, "tensors", {}).items()}
+
+
+def pblock_muon_workspace_bytes(cfg: MuonConfig, tensors) -> int:
+    """tensors: a sequence of MuonTensor."""
+    return load_library().pblock_muon_workspace_bytes(
+        ctypes.byref(cfg), len(tensors), (MuonTensor * len(tensors))(*tensors))
+
+
+def pblock_muon_step(cfg: MuonConfig, tensors, copy_dtype=PB_BF16, ws=None, stream=None):
+    """tensors: a sequence of MuonTensor; their copies are of copy_dtype."""
+    named = _named(tensors)
+    for name, t in named.items():
+        if name.endswith("param_copy") and copy_dtype in (PB_BF16, PB_F32):
+            _expect(name, t, _torch_dtype(copy_dtype), contiguous=False)
+    with _On(dict(named, ws=ws), stream) as st:
+        _check(load_library().pblock_muon_step(
+            ctypes.byref(cfg), len(tensors), (MuonTensor * len(tensors))(*tensors),
+            int(copy_dtype), _ptr(ws), _nbytes(ws), st))
+
+
+def ortho_tensor(x, out) -> OrthoTensor:
+    """A pb_ortho_tensor from two matrices of one shape and type (or one, in
+    place)."""
+    if out.dtype != x.dtype:
+        raise ValueError(f"out is {out.dtype}, x {x.dtype}")
+    ld, ld_out = _rows("x", x), _rows("out", out, x)
+    r = OrthoTensor(_ptr(x), _ptr(out), x.shape[0], x.shape[1], ld, ld_out)
+    r.tensors = {"x": x, "out": out}
+    return r
+
+
+def pblock_orthogonalize_workspace_bytes(tensors, dtype="bf16") -> int:
+    """tensors: a sequence of OrthoTensor."""
+    return load_library().pblock_orthogonalize_workspace_bytes(
+        len(tensors), (OrthoTensor * len(tensors))(*tensors), _dtype_of(dtype))
+
+
+def pblock_orthogonalize(tensors, dtype, ws, steps=5, eps=1e-7, stream=None):
+    """The orthogonalised matrices of OrthoTensors of dtype "bf16" or "f32"."""
+    code, named = _dtype_of(dtype), _named(tensors)
+    for name, t in named.items():
+        _expect(name, t, _torch_dtype(code), contiguous=False)
+    with _On(dict(named, ws=ws), stream) as st:
+        _check(load_library().pblock_orthogonalize(
+            len(tensors), (OrthoTensor * len(tensors))(*tensors), code, int(steps), eps, _ptr(ws),
+            _nbytes(ws), st))
 
 
 def pblock_status_string(status: int) -> str:

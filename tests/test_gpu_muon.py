@@ -1,0 +1,295 @@
+"""The Muon step and its orthogonalisation on the GPU against the fp64 oracle.
+
+How far the orthogonalised matrix may be off is taken, for each input, from the same
+iteration in numpy at the precision that the kernel holds its factors in: fp32 for
+"f32" products (22 bits a factor and fp32 sums on the GPU: at most four times the fp32
+iteration's own error and 2^-20), fp16 with the planes' powers of two for "bf16"
+products (twice its error, and the rounding of the result).  Errors are 2-norms
+relative to the result's.  M is one fused multiply-add of g (rounded once): 2^-23 of
+|mu M| + |g|.  w: three roundings, 2^-22 of |w|, and the update's error times its step.
+"""
+import numpy as np
+import pytest
+
+from oracle import operators_oracle as oo
+
+pytestmark = pytest.mark.gpu
+
+
+def _say(msg):
+    print(msg, flush=True)
+
+
+def f64(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+def half(v):
+    """fp16 with the power of two that keeps values high in its range (2^14 holds all
+    three matrices)."""
+    return (np.float32(v) * np.float32(16384)).astype(np.float16).astype(np.float32) / np.float32(16384)
+
+
+def off(a, b):
+    n = np.linalg.norm(b)
+    return np.linalg.norm(a - b) / n if n else float(np.linalg.norm(a))
+
+
+def allowed(u, ref, products, steps=5, out="f32"):
+    if products == "f32":
+        return 4 * off(oo.newton_schulz(u, steps, dtype=np.float32).astype(np.float64), ref) + 2.0 ** -20
+    e = off(oo.newton_schulz(u, steps, rnd=half, dtype=np.float32).astype(np.float64), ref)
+    return 2 * e + 2.0 ** -10 + (2.0 ** -8 if out == "bf16" else 0.0)
+
+
+# Where a matrix has one direction and equal elements, roundings add up instead of
+# averaging, and an fp32 iteration may happen to lose nothing: there the bound is the
+# sum.  With r = 2^-22 (a value with its remainder, rounded; and what a product leaves
+# out) and s the singular value, A = s^2 is off by 2 r of itself, b A + c A^2 by
+# 2 r 4.78 s^2 + 5 r 2.04 s^4 + 2.81 r, the product with X by 2.81 s r more and X's own
+# rounding: relative to the step's result 38, 9, 53, 10 and 52 r at the iterates of 1
+# (1, 0.701, 1.114, 0.721, 1.090, 0.696).  A step multiplies what it is given by
+# |s p'(s) / p(s)| = 0.72, 2.01, 0.83 and 1.19 there: 38, 36, 126, 115 and 189 r.
+COHERENT = 2.0 ** -14  # 256 r
+
+
+def matrix(rng, r, c, low=False):
+    u = rng.standard_normal((r, c))
+    if low:
+        u = 0.1 * u + rng.standard_normal((r, 4)) @ rng.standard_normal((4, c))
+    return u
+
+
+def place(a, dtype, ld, offset):
+    """The matrix in a buffer of rows ld apart, everything else 7."""
+    import torch
+    r, c = a.shape
+    buf = torch.full((offset + r * ld + 5,), 7.0, dtype=dtype, device="cuda")
+    v = buf[offset:offset + r * ld].view(r, ld)[:, :c] if r * ld else buf[:0].view(r, c)
+    v.copy_(torch.from_numpy(a))
+    return buf, v
+
+
+def untouched(buf, v, before):
+    import torch
+    keep = before.clone()
+    keep.as_strided(v.shape, v.stride(), v.storage_offset()).copy_(v)
+    return torch.equal(keep, buf)
+
+
+SIZES = [(1, 1), (1, 777), (777, 1), (5, 3), (64, 64), (65, 64), (128, 128), (130, 257), (300, 200),
+         (129, 1000), (1000, 129), (512, 512), (260, 2100)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("r,c", SIZES, ids=lambda v: str(v))
+def test_orthogonalize_matches_oracle(dtype, r, c):
+    import torch
+    from paper_2402_15627_amd import pblock as pb
+    _say(f"[gpu] orthogonalize {dtype} {r} x {c}")
+    act = torch.bfloat16 if dtype == "bf16" else torch.float32
+    rng = np.random.default_rng(r * 1000 + c)
+    for k, (ld, offset, std, low) in enumerate(((c, 0, 1.0, False), (c + 8, 8, 1e-4, False),
+                                                (c + 3, 1, 1e15, True))):
+        buf, x = place(std * matrix(rng, r, c, low), act, ld, offset)
+        before = buf.clone()
+        out_buf, out = place(np.zeros((r, c)), act, ld, offset)
+        out_before = out_buf.clone()
+        part = [pb.ortho_tensor(x, out)]
+        ws = torch.empty(pb.pblock_orthogonalize_workspace_bytes(part, dtype), dtype=torch.uint8,
+                         device="cuda").fill_(255)
+        pb.pblock_orthogonalize(part, dtype, ws)
+        torch.cuda.synchronize()
+        u = f64(x)
+        ref = oo.newton_schulz(u, eps=np.float64(np.float32(1e-7)))
+        e, tol = off(f64(out), ref), allowed(u, ref, dtype, out=dtype)
+        _say(f"      off {e:.2e} of {tol:.2e}")
+        assert e <= tol
+        assert torch.equal(buf, before) and untouched(out_buf, out, out_before)
+        pb.pblock_orthogonalize([pb.ortho_tensor(x, x)], dtype, ws)  # in place
+        assert torch.equal(x, out) and untouched(buf, x, before)
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 16])
+def test_orthogonalize_steps(steps):
+    import torch
+    from paper_2402_15627_amd import pblock as pb
+    _say(f"[gpu] orthogonalize steps={steps}")
+    u = np.float32(matrix(np.random.default_rng(steps), 100, 190)).astype(np.float64)
+    x = torch.from_numpy(u).float().cuda()
+    out = torch.empty_like(x)
+    part = [pb.ortho_tensor(x, out)]
+    ws = torch.empty(pb.pblock_orthogonalize_workspace_bytes(part, "f32"), dtype=torch.uint8, device="cuda")
+    pb.pblock_orthogonalize(part, "f32", ws, steps)
+    ref = oo.newton_schulz(u, steps)
+    assert off(f64(out), ref) <= allowed(u, ref, "f32", steps)
+
+
+def test_orthogonalize_extremes():
+    """Zeros stay zeros; a matrix below eps shrinks towards them; one value alone, the
+    largest of fp32, and a single NaN, which fills its matrix and no other."""
+    import torch
+    from paper_2402_15627_amd import pblock as pb
+    _say("[gpu] orthogonalize extremes")
+    xs = [torch.zeros(70, 90), torch.full((40, 30), 1e-12), torch.zeros(33, 65), torch.full((20, 80), 3e38),
+          torch.ones(64, 64), torch.randn(50, 64)]
+    xs[2][7, 60] = -3.4e38
+    xs[4][5, 5] = float("nan")
+    xs = [x.cuda() for x in xs]
+    outs = [torch.empty_like(x) for x in xs]
+    part = [pb.ortho_tensor(x, o) for x, o in zip(xs, outs)]
+    ws = torch.empty(pb.pblock_orthogonalize_workspace_bytes(part, "f32"), dtype=torch.uint8, device="cuda")
+    pb.pblock_orthogonalize(part, "f32", ws)
+    torch.cuda.synchronize()
+    assert not bool(outs[0].any()) and bool(torch.isnan(outs[4]).all())
+    for i in (1, 2, 3, 5):
+        u = f64(xs[i])
+        ref = oo.newton_schulz(u, eps=np.float64(np.float32(1e-7)))
+        assert off(f64(outs[i]), ref) <= (COHERENT if i in (1, 3) else allowed(u, ref, "f32")), i
+
+
+def make(shapes, seed, copy=True, copy_dtype="bf16", low=False):
+    """shapes: (rows, cols, ld, offset)."""
+    import torch
+    rng = np.random.default_rng(seed)
+    cd = torch.bfloat16 if copy_dtype == "bf16" else torch.float32
+    out = []
+    for k, (r, c, ld, offset) in enumerate(shapes):
+        s = {n: place(std * matrix(rng, r, c, low), torch.float32, ld, offset)
+             for n, std in (("w", 0.02), ("g", 1e-3), ("m", 5e-3))}
+        s["copy"] = place(np.zeros((r, c)), cd, ld, offset) if copy else (None, None)
+        s.update(wd=0.1 * (k % 2), scale=0.2 * max(r, c, 1) ** 0.5)
+        out.append(s)
+    return out
+
+
+MANY = [(256, 256, 256, 0), (1, 50, 50, 0), (100, 260, 512, 0), (0, 10, 10, 0), (260, 100, 512, 0),
+        (33, 71, 73, 1), (640, 128, 128, 4)]
+
+
+@pytest.mark.parametrize("products", ["f32", "bf16"])
+@pytest.mark.parametrize("nesterov,copy_dtype,gs", [(True, "bf16", 1.0), (False, "f32", 0.25)])
+def test_muon_step_matches_oracle(products, nesterov, copy_dtype, gs):
+    import torch
+    from paper_2402_15627_amd import pblock as pb
+    _say(f"[gpu] muon step {products} nesterov={nesterov}")
+    st = make(MANY, 3, copy_dtype=copy_dtype)
+    init = [{n: f64(s[n][1]) for n in ("w", "g", "m")} for s in st]
+    before = [{n: s[n][0].clone() for n in ("w", "g", "m", "copy")} for s in st]
+    cfg = pb.muon_config(0.02, 0.9, nesterov, grad_scale=gs, products=products)
+    lr, mu = np.float64(np.float32(0.02)), np.float64(np.float32(0.9))
+    part = [pb.muon_tensor(s["w"][1], s["g"][1], s["m"][1], s["copy"][1], s["wd"], s["scale"]) for s in st]
+    ws = torch.empty(pb.pblock_muon_workspace_bytes(cfg, part), dtype=torch.uint8, device="cuda").fill_(255)
+    pb.pblock_muon_step(cfg, part, pb.PB_BF16 if copy_dtype == "bf16" else pb.PB_F32, ws)
+    torch.cuda.synchronize()
+    for s, x, b in zip(st, init, before):
+        if x["w"].size == 0:
+            continue
+        wd, scale = float(np.float32(s["wd"])), float(np.float32(s["scale"]))
+        w, m, o = oo.muon_step(x["w"], x["g"], x["m"], lr, mu, nesterov, wd, scale, gs)
+        assert np.all(np.abs(f64(s["m"][1]) - m) <= 2.0 ** -23 * (np.abs(mu * x["m"]) + np.abs(gs * x["g"])))
+        u = gs * x["g"] + mu * m if nesterov else m
+        e = np.linalg.norm(f64(s["w"][1]) - w)
+        tol = allowed(u, o, products) * lr * scale * np.linalg.norm(o) + 2.0 ** -22 * np.linalg.norm(x["w"])
+        _say(f"      {x['w'].shape}: off {e:.2e} of {tol:.2e}")
+        assert e <= tol
+        assert torch.equal(s["copy"][1], s["w"][1].to(s["copy"][1].dtype))
+        for n in ("w", "m", "copy"):
+            assert untouched(s[n][0], s[n][1], b[n]), n
+        assert torch.equal(s["g"][0], b["g"])
+
+
+def test_muon_three_steps_and_split_calls():
+    """Matrices are independent: one call over all gives the bits of a call each; three
+    steps follow the oracle's."""
+    import torch
+    from paper_2402_15627_amd import pblock as pb
+    _say("[gpu] muon three steps, split calls")
+    shapes = [(64, 192, 192, 0), (192, 64, 64, 0), (130, 100, 100, 0)]
+    a, b = make(shapes, 9), make(shapes, 9)
+    ref = [{n: f64(s[n][1]) for n in ("w", "g", "m")} for s in a]
+    for step in range(3):
+        cfg = pb.muon_config(0.01, 0.95)
+        for group, calls in ((a, [a]), (b, [[x] for x in b])):
+            for c in calls:
+                part = [pb.muon_tensor(s["w"][1], s["g"][1], s["m"][1], s["copy"][1], s["wd"], s["scale"])
+                        for s in c]
+                ws = torch.empty(pb.pblock_muon_workspace_bytes(cfg, part), dtype=torch.uint8, device="cuda")
+                pb.pblock_muon_step(cfg, part, pb.PB_BF16, ws)
+        torch.cuda.synchronize()
+        for x, y, r in zip(a, b, ref):
+            for n in ("w", "m", "copy"):
+                assert torch.equal(x[n][1], y[n][1]), n
+            lr, mu = np.float64(np.float32(0.01)), np.float64(np.float32(0.95))
+            r["w"], r["m"], o = oo.muon_step(r["w"], r["g"], r["m"], lr, mu, True,
+                                             float(np.float32(x["wd"])), float(np.float32(x["scale"])))
+            tol = (step + 1) * (1e-5 * lr * x["scale"] * np.linalg.norm(o) + 2.0 ** -22 * np.linalg.norm(r["w"]))
+            assert np.linalg.norm(f64(x["w"][1]) - r["w"]) <= tol
+            rng = np.random.default_rng(100 * step + r["w"].size)
+            r["g"] = np.float32(1e-3 * rng.standard_normal(r["g"].shape)).astype(np.float64)
+            for s in (x, y):
+                s["g"][1].copy_(torch.from_numpy(r["g"]))
+
+
+def test_muon_rows_far_apart():
+    """Rows 2^20 elements apart: the last ones lie past 2^31 elements."""
+    import torch
+    from paper_2402_15627_amd import pblock as pb
+    _say("[gpu] muon, rows over 2.2e9 elements")
+    r, c, ld = 2100, 64, 1 << 20
+    flat = make([(r, c, c, 0)], 4, copy=False)[0]
+    wide = {}
+    for n in ("w", "g", "m"):
+        wide[n] = torch.empty(r, ld, device="cuda")[:, 100:100 + c]
+        wide[n].copy_(flat[n][1])
+    cfg = pb.muon_config(0.02)
+    for s in ({n: flat[n][1] for n in wide}, wide):
+        part = [pb.muon_tensor(s["w"], s["g"], s["m"], None, 0.1, 2.0)]
+        ws = torch.empty(pb.pblock_muon_workspace_bytes(cfg, part), dtype=torch.uint8, device="cuda")
+        pb.pblock_muon_step(cfg, part, pb.PB_BF16, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(wide["w"], flat["w"][1]) and torch.equal(wide["m"], flat["m"][1])
+
+
+def test_muon_streams_and_graph():
+    import torch
+    from paper_2402_15627_amd import pblock as pb
+    _say("[gpu] muon streams and graph")
+    cfg = pb.muon_config(0.01)
+
+    def handle(seed):
+        st = make([(200, 320, 320, 0), (320, 100, 100, 0)], seed)
+        part = [pb.muon_tensor(s["w"][1], s["g"][1], s["m"][1], s["copy"][1], s["wd"], s["scale"])
+                for s in st]
+        return st, part, torch.empty(pb.pblock_muon_workspace_bytes(cfg, part), dtype=torch.uint8,
+                                     device="cuda")
+
+    state = lambda st: [s[n][0].clone() for s in st for n in ("w", "m", "copy")]  # noqa: E731
+    alone = []
+    for seed in (1, 2):
+        st, part, ws = handle(seed)
+        for _ in range(3):
+            pb.pblock_muon_step(cfg, part, pb.PB_BF16, ws)
+        alone.append(state(st))
+    torch.cuda.synchronize()
+    sets, streams = [handle(1), handle(2)], [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for (st, part, ws), s in zip(sets, streams):
+            pb.pblock_muon_step(cfg, part, pb.PB_BF16, ws, s)
+    torch.cuda.synchronize()
+    for (st, _, _), want in zip(sets, alone):
+        assert all(torch.equal(a, b) for a, b in zip(state(st), want))
+    st, part, ws = handle(1)
+    first = [s[n][0].clone() for s in st for n in ("w", "m", "copy")]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pb.pblock_muon_step(cfg, part, pb.PB_BF16, ws)
+    for v, f in zip([s[n][0] for s in st for n in ("w", "m", "copy")], first):
+        v.copy_(f)
+    for r in range(3):
+        torch.cuda.synchronize()
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(state(st), alone[0]))

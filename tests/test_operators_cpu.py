@@ -1,0 +1,262 @@
+"""Refusals and sizes of the operators around the block, on a machine without a GPU:
+every call below fails a host check (or has nothing to launch), so its pointers are
+never read."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2402_15627_amd import pblock as pb
+
+FAKE = 1 << 40
+OK, BAD, UNSUPPORTED, SMALL = 0, 1, 2, 3
+
+
+def align(v):
+    return (v + 255) // 256 * 256
+
+
+# ------------------------------------------------------- rotary positions
+def rope(fn="pblock_rope_forward", n=None, tokens=4, seq=4, positions=None, tensors=None, **over):
+    cfg = pb.rope_config(64, scaling=over.pop("scaling", "by_parts"), factor=2.0, orig_len=64.0)
+    for k, v in over.items():
+        setattr(cfg, k, v)
+    x = tensors if tensors is not None else [pb.RopeTensor(FAKE, FAKE, 128, 128, 2)]
+    arr = (pb.RopeTensor * max(len(x), 1))(*x)
+    return getattr(pb.load_library(), fn)(ctypes.byref(cfg), len(x) if n is None else n, arr, tokens,
+                                          seq, positions, None)
+
+
+@pytest.mark.parametrize("fn", ["pblock_rope_forward", "pblock_rope_backward"])
+@pytest.mark.parametrize("over,status", [
+    (dict(head_dim=63), BAD), (dict(head_dim=0), BAD), (dict(head_dim=258), UNSUPPORTED),
+    (dict(rot_dim=0), BAD), (dict(rot_dim=7), BAD), (dict(rot_dim=66), BAD),
+    (dict(interleaved=2), BAD), (dict(base=0.0), BAD), (dict(base=float("inf")), BAD),
+    (dict(magnitude=0.0), BAD), (dict(magnitude=float("nan")), BAD), (dict(magnitude=1e300), BAD),
+    (dict(factor=0.0), BAD), (dict(orig_len=0.0), BAD), (dict(low_turns=-1.0), BAD),
+    (dict(high_turns=1.0), BAD), (dict(dtype=5), BAD), (dict(tokens=-1), BAD),
+    (dict(tokens=1 << 24), UNSUPPORTED), (dict(seq=0), BAD), (dict(positions=FAKE + 4), BAD),
+    (dict(n=0), BAD), (dict(n=5), BAD),
+    (dict(tensors=[pb.RopeTensor(None, FAKE, 128, 128, 2)]), BAD),
+    (dict(tensors=[pb.RopeTensor(FAKE, FAKE + 1, 128, 128, 2)]), BAD),
+    (dict(tensors=[pb.RopeTensor(FAKE, FAKE, 127, 128, 2)]), BAD),
+    (dict(tensors=[pb.RopeTensor(FAKE, FAKE, 128, 256, 2)]), BAD),
+    (dict(tensors=[pb.RopeTensor(FAKE, FAKE, 128, 128, 0)]), BAD),
+    (dict(tensors=[pb.RopeTensor(FAKE, FAKE, 1 << 20, 1 << 20, 8193)]), UNSUPPORTED),
+    (dict(tensors=[pb.RopeTensor(FAKE, FAKE, 1 << 32, 1 << 32, 2)]), UNSUPPORTED),
+])
+def test_rope_refusals(fn, over, status):
+    assert rope(fn, **over) == status
+    assert pb.pblock_last_error() != ""
+
+
+def test_rope_scaling_values_are_read_only_by_their_kind():
+    none = dict(tokens=0, factor=0.0, orig_len=-1.0, high_turns=0.0)
+    assert rope(scaling="plain", **none) == OK
+    assert rope(scaling="linear", **none) == BAD
+    assert rope(scaling="linear", **dict(none, factor=2.0)) == OK
+    cfg = pb.rope_config(64)
+    cfg.scaling = 3
+    arr = (pb.RopeTensor * 1)(pb.RopeTensor(FAKE, FAKE, 128, 128, 2))
+    assert pb.load_library().pblock_rope_forward(ctypes.byref(cfg), 1, arr, 0, 1, None, None) == BAD
+    assert pb.load_library().pblock_rope_forward(None, 1, arr, 0, 1, None, None) == BAD
+    cfg.scaling = 0
+    assert pb.load_library().pblock_rope_forward(ctypes.byref(cfg), 1, None, 0, 1, None, None) == BAD
+    # no tokens: nothing is launched, no pointer is needed
+    assert rope(tokens=0, tensors=[pb.RopeTensor(None, None, 128, 128, 2)]) == OK
+
+
+# ------------------------------------------------- root-mean-square norm
+def rms(**over):
+    cfg = pb.rmsnorm_config(4, 64)
+    a = dict(x=FAKE, resid=None, gamma=FAKE, sum=None, y=FAKE, q8=None, scales=None, rstd=None)
+    for k, v in over.items():
+        if k in a:
+            a[k] = v
+        else:
+            setattr(cfg, k, v)
+    return pb.load_library().pblock_rmsnorm_forward(ctypes.byref(cfg), *a.values(), None)
+
+
+def rms_back(nbytes=None, ws=FAKE, **over):
+    cfg = pb.rmsnorm_config(4, 64)
+    a = dict(s=FAKE, gamma=FAKE, rstd=FAKE, dy=FAKE, dsum=None, dx=FAKE, dgamma=FAKE)
+    for k, v in over.items():
+        if k in a:
+            a[k] = v
+        else:
+            setattr(cfg, k, v)
+    n = pb.pblock_rmsnorm_workspace_bytes(cfg) if nbytes is None else nbytes
+    return pb.load_library().pblock_rmsnorm_backward(ctypes.byref(cfg), *a.values(), ws, n, None)
+
+
+CONFIGS = [(dict(rows=-1), BAD), (dict(cols=0), BAD), (dict(cols=32769), UNSUPPORTED),
+           (dict(rows=1 << 31), UNSUPPORTED), (dict(group=16), BAD), (dict(group=256), BAD),
+           (dict(eps=-1e-5), BAD), (dict(eps=float("nan")), BAD), (dict(dtype=2), BAD),
+           (dict(gamma=None), BAD), (dict(gamma=FAKE + 1), BAD)]
+
+
+@pytest.mark.parametrize("over,status", CONFIGS + [
+    (dict(x=None), BAD), (dict(x=FAKE + 1), BAD), (dict(y=None), BAD), (dict(resid=FAKE + 1), BAD),
+    (dict(sum=FAKE + 256), BAD), (dict(resid=FAKE, sum=FAKE + 1), BAD),
+    (dict(resid=FAKE, sum=FAKE), BAD),  # sum and y in one buffer
+    (dict(q8=FAKE), BAD), (dict(scales=FAKE), BAD), (dict(q8=FAKE, scales=FAKE + 2), BAD),
+    (dict(rstd=FAKE + 2), BAD),
+])
+def test_rmsnorm_forward_refusals(over, status):
+    assert rms(**over) == status
+    assert pb.pblock_last_error() != ""
+
+
+@pytest.mark.parametrize("over,status", CONFIGS + [
+    (dict(s=None), BAD), (dict(rstd=None), BAD), (dict(rstd=FAKE + 2), BAD), (dict(dy=None), BAD),
+    (dict(dsum=FAKE + 1), BAD), (dict(dx=None), BAD), (dict(dgamma=None), BAD),
+    (dict(dgamma=FAKE + 2), BAD), (dict(ws=None), BAD), (dict(ws=FAKE + 16), BAD),
+    (dict(nbytes=0), SMALL), (dict(nbytes=4 * 64 * 1 - 1), SMALL),
+])
+def test_rmsnorm_backward_refusals(over, status):
+    assert rms_back(**over) == status
+    assert pb.pblock_last_error() != ""
+
+
+def test_rmsnorm_without_rows_and_its_workspace():
+    assert rms(rows=0, x=None, y=None) == OK
+    lib = pb.load_library()
+    assert lib.pblock_rmsnorm_forward(None, *[FAKE] * 8, None, None) == BAD
+    assert lib.pblock_rmsnorm_workspace_bytes(None) == 0
+    # a row of fp32 per workgroup
+    for rows in (1, 7, 100, 100000):
+        for cols in (1, 5, 128, 129, 1024, 5120, 32768):
+            n = pb.pblock_rmsnorm_workspace_bytes(pb.rmsnorm_config(rows, cols))
+            assert n % 256 == 0 and n >= 4 * cols
+            assert n <= align(4 * cols * min(rows, 1024))
+    assert pb.pblock_rmsnorm_workspace_bytes(pb.rmsnorm_config(0, 64)) == 0
+    assert pb.pblock_rmsnorm_workspace_bytes(pb.rmsnorm_config(4, 0)) == 0
+
+
+# ------------------------------------------------------------- Muon step
+def muon(ws=FAKE, nbytes=1 << 30, copy=pb.PB_BF16, n=None, tensors=None, cfg_null=False, **over):
+    cfg = pb.muon_config(1e-3)
+    x = dict(param=FAKE, grad=FAKE, momentum=FAKE, param_copy=None, rows=8, cols=16, ld=16,
+             weight_decay=0.1, scale=1.0)
+    own = dict(mom_ptr="momentum")
+    for k, v in over.items():
+        if k in own:
+            x[own[k]] = v
+        elif k in x and k != "momentum":
+            x[k] = v
+        else:
+            setattr(cfg, k, v)
+    ts = tensors if tensors is not None else [pb.MuonTensor(*x.values())]
+    arr = (pb.MuonTensor * max(len(ts), 1))(*ts)
+    return pb.load_library().pblock_muon_step(None if cfg_null else ctypes.byref(cfg),
+                                              len(ts) if n is None else n, arr, copy, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(lr=float("nan")), BAD), (dict(momentum=1.0), BAD), (dict(momentum=-0.1), BAD),
+    (dict(grad_scale=float("inf")), BAD), (dict(eps=0.0), BAD), (dict(nesterov=2), BAD),
+    (dict(steps=0), BAD), (dict(steps=17), BAD), (dict(products=4), BAD), (dict(copy=3), BAD),
+    (dict(n=0), BAD), (dict(n=17), BAD), (dict(param=None), BAD), (dict(grad=FAKE + 2), BAD),
+    (dict(mom_ptr=None), BAD), (dict(param_copy=FAKE + 1), BAD), (dict(rows=-1), BAD),
+    (dict(rows=65537, cols=65537, ld=65537), UNSUPPORTED),
+    (dict(rows=4, cols=(1 << 20) + 1, ld=1 << 21), UNSUPPORTED),
+    (dict(ld=15), BAD), (dict(ld=1 << 32), BAD), (dict(weight_decay=-1.0), BAD),
+    (dict(scale=float("nan")), BAD), (dict(ws=None), BAD), (dict(ws=FAKE + 16), BAD),
+    (dict(nbytes=1024), SMALL), (dict(cfg_null=True), BAD),
+])
+def test_muon_refusals(over, status):
+    assert muon(**over) == status
+    assert pb.pblock_last_error() != ""
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(dtype=7), BAD), (dict(steps=0), BAD), (dict(eps=-1.0), BAD), (dict(n=0), BAD),
+    (dict(x=pb.OrthoTensor(None, FAKE, 8, 16, 16, 16)), BAD),
+    (dict(x=pb.OrthoTensor(FAKE, FAKE + 1, 8, 16, 16, 16)), BAD),
+    (dict(x=pb.OrthoTensor(FAKE, FAKE, 8, 16, 15, 16)), BAD),
+    (dict(x=pb.OrthoTensor(FAKE, FAKE, 8, 16, 16, 24)), BAD),
+    (dict(x=pb.OrthoTensor(FAKE, FAKE, 8, -1, 16, 16)), BAD),
+    (dict(ws=None), BAD), (dict(nbytes=64), SMALL),
+])
+def test_orthogonalize_refusals(over, status):
+    a = dict(n=1, x=pb.OrthoTensor(FAKE, FAKE, 8, 16, 16, 16), dtype=pb.PB_BF16, steps=5, eps=1e-7,
+             ws=FAKE, nbytes=1 << 30)
+    a.update(over)
+    assert pb.load_library().pblock_orthogonalize(a["n"], (pb.OrthoTensor * 1)(a["x"]), a["dtype"],
+                                                  a["steps"], a["eps"], a["ws"], a["nbytes"],
+                                                  None) == status
+    assert pb.pblock_last_error() != ""
+
+
+def test_empty_matrices_and_workspaces():
+    empty = [pb.MuonTensor(None, None, None, None, 0, 16, 16, 0.0, 1.0),
+             pb.MuonTensor(None, None, None, None, 16, 0, 0, 0.0, 1.0)]
+    cfg = pb.muon_config(1e-3)
+    assert pb.pblock_muon_workspace_bytes(cfg, empty) == 0
+    assert muon(tensors=empty, ws=None, nbytes=0) == OK
+    # X twice, X X^T and its polynomial in planes of 2 bytes, padded to 64, at least
+    ts = [pb.MuonTensor(FAKE, FAKE, FAKE, None, 100, 1000, 1000, 0.0, 1.0)]
+    for products, planes in (("bf16", 1), ("f32", 2)):
+        need = pb.pblock_muon_workspace_bytes(pb.muon_config(1e-3, products=products), ts)
+        assert need >= planes * 2 * (2 * 128 * 1024 + 2 * 128 * 128)
+    assert pb.pblock_muon_workspace_bytes(cfg, []) == 0
+    assert pb.pblock_muon_workspace_bytes(cfg, ts * 17) == 0
+    o = [pb.OrthoTensor(FAKE, FAKE, 1000, 100, 100, 100)]
+    assert (pb.pblock_orthogonalize_workspace_bytes(o, "f32") >
+            pb.pblock_orthogonalize_workspace_bytes(o, "bf16") > 0)
+
+
+# ------------------------------------------------------------ the binding
+def test_binding_refuses_what_tensors_say_of_themselves():
+    bf, f32 = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(4, 64)
+    g = torch.ones(64, dtype=torch.bfloat16)
+    cfg = pb.rmsnorm_config(4, 64)
+    with pytest.raises(ValueError, match="not on a GPU"):
+        pb.pblock_rmsnorm_forward(cfg, bf, g, bf)
+    with pytest.raises(ValueError, match="x is torch.float32"):
+        pb.pblock_rmsnorm_forward(cfg, f32, g, bf)
+    with pytest.raises(ValueError, match="y has 128"):
+        pb.pblock_rmsnorm_forward(cfg, bf, g, bf[:2])
+    with pytest.raises(ValueError, match="not contiguous"):
+        pb.pblock_rmsnorm_forward(cfg, torch.zeros(64, 4, dtype=torch.bfloat16).t(), g, bf)
+    with pytest.raises(ValueError, match="q8 is"):
+        pb.pblock_rmsnorm_forward(cfg, bf, g, bf, q8=bf, scales=torch.zeros(4))
+    with pytest.raises(ValueError, match="dgamma"):
+        pb.pblock_rmsnorm_backward(cfg, bf, g, torch.zeros(4), bf, bf, g, None)
+    rc = pb.rope_config(32)
+    with pytest.raises(ValueError, match="short of 4 tokens"):
+        pb.pblock_rope_forward(rc, [pb.rope_tensor(bf[:, 8:], 64, 2)], 4)
+    with pytest.raises(ValueError, match="positions"):
+        pb.pblock_rope_forward(rc, [pb.rope_tensor(bf, 64, 2)], 4, positions=torch.zeros(4))
+    with pytest.raises(ValueError, match="not on a GPU"):
+        pb.pblock_rope_backward(rc, [pb.rope_tensor(bf, 64, 2)], 4)
+    with pytest.raises(ValueError, match="scaling"):
+        pb.rope_config(32, scaling="other")
+    with pytest.raises(ValueError, match="dtype"):
+        pb.rmsnorm_config(4, 64, dtype="fp8")
+    with pytest.raises(ValueError, match="another stride"):
+        pb.muon_tensor(f32, torch.zeros(4, 128)[:, :64], f32)
+    with pytest.raises(ValueError, match="rows are not contiguous"):
+        pb.muon_tensor(f32.t(), f32.t(), f32.t())
+    with pytest.raises(ValueError, match="grad is"):
+        pb.muon_tensor(f32, bf, f32)
+    with pytest.raises(ValueError, match="param_copy is"):
+        pb.pblock_muon_step(pb.muon_config(1e-3), [pb.muon_tensor(f32, f32, f32, f32)])
+    with pytest.raises(ValueError, match="dimensions"):
+        pb.ortho_tensor(torch.zeros(3), torch.zeros(3))
+    with pytest.raises(ValueError, match="x is"):
+        pb.pblock_orthogonalize([pb.ortho_tensor(f32, f32)], "bf16", None)
+
+
+class _Tensor:
+    def __init__(self, index):
+        self.device = torch.device("cuda", index)
+
+
+def test_binding_refuses_two_devices_and_a_stream_of_another():
+    with pytest.raises(ValueError, match="different devices"):
+        pb._On(dict(a=_Tensor(0), b=None, c=_Tensor(1)), None)
+    with pytest.raises(ValueError, match="stream is on device 1"):
+        pb._On(dict(a=_Tensor(0)), _Tensor(1))
+    assert pb._On(dict(a=_Tensor(1), b=FAKE), _Tensor(1)).index == 1
