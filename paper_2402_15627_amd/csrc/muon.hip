@@ -2,7 +2,7 @@
 // by Newton-Schulz steps (Muon: Jordan et al. 2024):
 //
 //   M = mu M + g,  U = g + mu M (Nesterov) or M;  X = U / (||U||_F + eps)
-//   `steps` times:  A = X X^T,  B = b A + c A A,  X = a X + B X
+//   `steps` times:  A = X X^T,  B = a I + b A + c A A,  X = B X
 //   w = w (1 - lr decay) - lr scale X
 //
 // with X of m <= n (U, or its transpose).  The odd polynomial a s + b s^3 + c s^5

@@ -11,9 +11,9 @@ namespace pb {
 // planes the second one holds the remainder, rounded again (2^-22 of the number).
 // The powers keep the values high in fp16's range, so that what the remainder
 // loses to subnormals is below 2^-39 of the spectral norm: X has a spectral norm
-// of at most 1.203, A = X X^T of 1.446 and B of 2.81 (b s + c s^2 over s in
-// [0, 1.446] lies in [-2.806, 0]), and no element of a matrix exceeds its norm:
-// 39.4e3, 47.4e3 and 46.0e3 of fp16's 65.5e3.
+// of at most 1.203, A = X X^T of 1.446 and B of 3.445 (a + b s + c s^2 over s in
+// [0, 1.446] lies in [0.638, 3.445]), and no element of a matrix exceeds its norm:
+// 39.4e3, 47.4e3 and 56.4e3 of fp16's 65.5e3.
 constexpr float kNsScaleX = 32768.0f, kNsScaleA = 32768.0f, kNsScaleB = 16384.0f;
 // Coefficients of the step (Jordan et al. 2024).
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;

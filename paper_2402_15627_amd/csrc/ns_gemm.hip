@@ -1,18 +1,26 @@
 // The products of a Newton-Schulz step, all matrices of a call in one launch each:
 //
-//   gram    A = X X^T          symmetric: tiles on and above the diagonal, each
-//                              written to its mirror image too
-//   square  B = b A + c A A    symmetric likewise
-//   apply   X' = a X + B X
+//   gram    A = X X^T                  symmetric: tiles on and above the diagonal, each
+//                                      written to its mirror image too
+//   square  B = a I + b A + c A A      symmetric likewise
+//   apply   X' = B X
 //
 // MFMA v_mfma_f32_16x16x32_f16 on the planes of ns_gemm.h, fp32 accumulation.  One
-// plane: one product of fp16 values (rounded by 2^-11 at most).  Two planes
-// (value h and remainder l): h l + l h + h h, in this order, as one sum over three
-// times the length (what is left out, l l, is at most 2^-22 of the product).
+// plane: one product of fp16 values (rounded by 2^-11 at most).  Two planes (value h
+// and remainder l): h l + l h + h h, in this order, as one sum over three times the
+// length (what is left out, l l, is at most 2^-22 of the product).  a goes into B, not
+// into apply's sum: near the end B is about 0.7 to 1.4 instead of -2.7 to -2.0, so its
+// rounding moves X' by less (one plane, one row of 777: 3.4e-3 off, 8e-4 so; 512 x 512
+// 1.34e-3, 1.24e-3), and apply reads no X beside its operand.
 //
-// 128 x 128 tile per workgroup of four waves, K-tiles of 64 through two LDS stages
-// filled by LDS-DMA.
+// Two kernels:
+//   - 256 x 256 tiles, eight waves, as the projection GEMMs' LDS-DMA kernel has them
+//     (gemm.hip: fragments read two phases ahead, one barrier a K-tile);
+//   - 128 x 128 tiles, four waves, for grids too small for the first.
+// X, A and B are padded to multiples of 64 with zeros, so a K-tile is never partial;
+// rows and columns past the end of a tile read the last ones and are not stored.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "gemm_common.h"
@@ -26,34 +34,35 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 enum class Op { Gram, Square, Apply };
 
-constexpr int kT = 128;           // tile rows and columns
-constexpr int kK = 64;            // K-tile
-constexpr int kWaves = 4;         // 2 x 2, each 64 x 64
-constexpr int kThreads = 64 * kWaves;
-constexpr int kOpBytes = kT * kK * 2;                 // one operand's K-tile: 16 KB
-constexpr int kPieces = kOpBytes / (1024 * kWaves);   // 1 KB DMA pieces per wave
-constexpr int kRowF = kT + 4;     // floats per row of the staged output
+constexpr int kK = 64;  // K-tile
 static_assert(kNsPad == kK, "X's dimensions are whole K-tiles");
+
+// From the sum of plane products to the result's plane values.
+template <Op OP>
+constexpr float out_scale() {
+  return OP == Op::Gram     ? kNsScaleA / (kNsScaleX * kNsScaleX)
+         : OP == Op::Square ? kNsC * kNsScaleB / (kNsScaleA * kNsScaleA)
+                            : 1.0f / kNsScaleB;
+}
 
 PB_DEV int swz(int row, int c) { return c ^ ((row ^ (row >> 3)) & 7); }
 PB_DEV int swz_mn(int k, int c) { return c ^ (4 * (k & 3)) ^ (2 * ((k >> 3) & 1)); }
 
-// Byte offset from the operand tile's first element of this lane's 16 bytes of a
-// piece.  KC: rows of the operand are K-contiguous, `rows` of them left; else the
-// operand is K rows of which `rows` columns are left.  Past them, the last is read
-// (its products are not stored).
-template <bool KC>
+// Byte offset from the operand tile's first element of this lane's 16 bytes of the LDS
+// position p.  KC: rows of the operand are K-contiguous, `rows` of them left; else the
+// operand is K rows of which `rows` columns are left.
+template <bool KC, int T>
 PB_DEV uint32_t lane_off(int ld, int rows, int p) {
   if constexpr (KC) {
     const int row = p >> 7, c = swz(row, (p >> 4) & 7);
     return (uint32_t)(min(row, rows - 1) * ld + 8 * c) * 2u;
   } else {
-    const int k = p >> 8, c = swz_mn(k, (p >> 4) & 15);
+    const int k = p / (2 * T), c = swz_mn(k, (p >> 4) & (T / 8 - 1));
     return (uint32_t)(k * ld + min(8 * c, rows - 8)) * 2u;
   }
 }
 // Fragment of 16 rows (columns) from `base`, k 32 s + 8 (lane >> 4) .. + 7.
-template <bool KC>
+template <bool KC, int T>
 PB_DEV f16x8 frag(const unsigned char* tile, int base, int s, int lane) {
   if constexpr (KC) {
     const int row = base + (lane & 15);
@@ -63,48 +72,381 @@ PB_DEV f16x8 frag(const unsigned char* tile, int base, int s, int lane) {
     const int k1 = 32 * s + 8 * (lane >> 4) + (i >> 2), k2 = k1 + 4;
     const int c = mn >> 3, off = (mn & 7) * 2;
     const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (PB_LDS s16x4*)(tile + k1 * 256 + swz_mn(k1, c) * 16 + off));
+        (PB_LDS s16x4*)(tile + k1 * (2 * T) + swz_mn(k1, c) * 16 + off));
     const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (PB_LDS s16x4*)(tile + k2 * 256 + swz_mn(k2, c) * 16 + off));
+        (PB_LDS s16x4*)(tile + k2 * (2 * T) + swz_mn(k2, c) * 16 + off));
     const f16x4 a4 = __builtin_bit_cast(f16x4, a), b4 = __builtin_bit_cast(f16x4, b);
     return f16x8{a4[0], a4[1], a4[2], a4[3], b4[0], b4[1], b4[2], b4[3]};
   }
 }
 
-int tiles_of(int v) { return (v + kT - 1) / kT; }
-
-struct NsTiles {
+// ------------------------------------------------------------ work items
+// A launch's items are tiles, or K-slices of tiles, in the order of NsPlan: the first
+// n_full tiles whole, then `splits` slices of each tile after them, whose fp32 partial
+// tiles ns_reduce_kernel sums.  first[i]: matrix i's first tile.
+struct NsPlan {
   int first[kNsMaxTensors + 1];
+  int n_full, splits;
 };
 
+// Tile of the triangle tm <= tn of t x t tiles, in bands of four rows walked column by
+// column (tiles that run together then share operand strips in an XCD's L2, as in the
+// walk of tile_of).
+PB_DEV void triangle_tile(int id, int t, int& tm, int& tn) {
+  int r0 = 0, g = min(4, t);
+  for (;;) {
+    const int n = g * (t - r0) - g * (g - 1) / 2;
+    if (id < n) break;
+    id -= n;
+    r0 += g;
+    g = min(4, t - r0);
+  }
+  const int corner = g * (g + 1) / 2;  // column j of the band's first g has j + 1 tiles
+  if (id < corner) {
+    int j = 0;
+    while (id > j) id -= ++j;
+    tm = r0 + id;
+    tn = r0 + j;
+  } else {
+    id -= corner;
+    tm = r0 + id % g;
+    tn = r0 + g + id / g;
+  }
+}
+
+template <Op OP, int T>
+PB_DEV void tile_at(const NsMat& x, int id, int& tm, int& tn) {
+  const int t = (x.m + T - 1) / T;
+  if constexpr (OP == Op::Apply) tile_of<4>(id, t, (x.n + T - 1) / T, tm, tn);
+  else triangle_tile(id, t, tm, tn);
+}
+
+PB_DEV int mat_of(const NsPlan& p, int count, int tile) {
+  int i = 0;
+#pragma unroll 1
+  for (int k = 1; k < count; ++k)
+    if (tile >= p.first[k]) i = k;
+  return i;
+}
+
+// Operands of a product, and where its result goes.
+struct Operands {
+  const _Float16 *A, *B;
+  size_t plane_a, plane_b;  // elements to the second plane
+  int lda, ldb, K;
+};
+template <Op OP>
+PB_DEV Operands operands(const NsMat& x, int cur) {
+  const size_t mm = (size_t)x.m * x.m, mn = (size_t)x.m * x.n;
+  if constexpr (OP == Op::Gram) return {x.x[cur], x.x[cur], mn, mn, x.n, x.n, x.n};
+  else if constexpr (OP == Op::Square) return {x.a, x.a, mm, mm, x.m, x.m, x.m};
+  else return {x.b, x.x[cur], mm, mn, x.m, x.n, x.m};
+}
+
+// Four consecutive columns n.. of row m of the result, v: the sums (scaled in place).
 template <Op OP, int PLANES>
-__global__ __launch_bounds__(kThreads, 2) void ns_gemm_kernel(NsTable t, NsTiles tiles, int cur) {
+PB_DEV void store_result4(const NsMat& x, int cur, int m, int n, float* v) {
+  constexpr float kOut = out_scale<OP>();
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] *= kOut;
+  if constexpr (OP == Op::Gram) {
+    ns_store4<PLANES>(x.a + (size_t)m * x.m + n, (size_t)x.m * x.m, v, 1.0f);
+  } else if constexpr (OP == Op::Square) {
+    float a4[4];
+    ns_load4<PLANES>(x.a + (size_t)m * x.m + n, (size_t)x.m * x.m, a4,
+                     kNsB * kNsScaleB / kNsScaleA);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += a4[e] + (m == n + e ? kNsA * kNsScaleB : 0.f);
+    ns_store4<PLANES>(x.b + (size_t)m * x.m + n, (size_t)x.m * x.m, v, 1.0f);
+  } else {
+    ns_store4<PLANES>(x.x[cur ^ 1] + (size_t)m * x.n + n, (size_t)x.m * x.n, v, 1.0f);
+  }
+}
+
+// ------------------------------------------------------ 256 x 256 tiles
+constexpr int kBT = 256;
+constexpr int kBThreads = 512;                       // 4 (m) x 2 (n) waves, each 64 x 128
+constexpr int kBTile = kBT * kK * 2;                 // one operand's K-tile: 32 KB
+constexpr int kBPieces = kBTile / kBThreads / 16;    // 1 KB pieces per operand per wave: 4
+constexpr int kWTM = 64, kWTN = 128;
+constexpr int kTM = kWTM / 16, kTN = kWTN / 16;
+constexpr int kEpiLds = 32 * kWTN * 4;               // a wave's 32 rows of sums: 16 KB
+constexpr size_t kBLds = 4 * (size_t)kBTile;         // two stages of two operands
+static_assert(8 * kEpiLds <= (int)kBLds, "staged output fits");
+
+template <int N>
+PB_DEV void wait_dma() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+// (the wait for LDS is the compiler's own instruction, so that it knows of it)
+PB_DEV void block_barrier() {
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  asm volatile("s_barrier" ::: "memory");
+}
+
+template <Op OP, int PLANES>
+__global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan plan, int cur,
+                                                            float* __restrict__ part) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  constexpr bool BK = OP != Op::Apply;  // the B operand is K-contiguous
+  const int bid = blockIdx.x;
+  int lid, slice = -1;
+  if (bid < plan.n_full) {
+    lid = xcd_remap(bid, plan.n_full);
+  } else {
+    const int j = xcd_remap(bid - plan.n_full, gridDim.x - plan.n_full);
+    lid = plan.n_full + j / plan.splits;
+    slice = j % plan.splits;
+  }
+  const int mi = mat_of(plan, t.count, lid);
+  const NsMat& x = t.mat[mi];
+  int tm, tn;
+  tile_at<OP, kBT>(x, lid - plan.first[mi], tm, tn);
+  const int m0 = tm * kBT, n0 = tn * kBT, M = x.m, N = BK ? x.m : x.n;
+  const Operands o = operands<OP>(x, cur);
+  const int nk = o.K / kK, all = PLANES == 2 ? 3 * nk : nk;
+  int kt0 = 0, kt1 = all;
+  if (slice >= 0) {
+    const int chunk = (all + plan.splits - 1) / plan.splits;
+    kt0 = min(all, slice * chunk);
+    kt1 = min(all, kt0 + chunk);
+  }
+  const int nt = kt1 - kt0;
+
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(PB_LDS unsigned char*)smem;
+  auto a_off = [&](int s) { return (2 * s) * kBTile; };
+  auto b_off = [&](int s) { return (2 * s + 1) * kBTile; };
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = (wave & 3) * kWTM, wn = (wave >> 2) * kWTN;
+
+  // Who moves what, as in gemm.hip: with K-contiguous operands every wave its own 4 KB
+  // of each; otherwise the first wave of each SIMD both 4 KB regions of its SIMD.
+  constexpr int kReg = BK ? 1 : 2;
+  constexpr int kDmaPerTile = 2 * kReg * kBPieces;
+  const bool dma_wave = BK || wave < 4;
+  auto region = [&](int r) { return BK ? wave : (wave & 3) + 4 * r; };
+  uint32_t aoff[kReg * kBPieces], boff[kReg * kBPieces];
+#pragma unroll
+  for (int r = 0; r < kReg; ++r)
+#pragma unroll
+    for (int i = 0; i < kBPieces; ++i) {
+      const int p = (region(r) * kBPieces + i) * 1024 + 16 * lane;
+      aoff[r * kBPieces + i] = lane_off<true, kBT>(o.lda, M - m0, p);
+      boff[r * kBPieces + i] = lane_off<BK, kBT>(o.ldb, N - n0, p);
+    }
+  const _Float16* abase = o.A + (size_t)m0 * o.lda;
+  const _Float16* bbase = BK ? o.B + (size_t)n0 * o.ldb : o.B + n0;
+  const size_t bstep = BK ? kK : (size_t)kK * o.ldb;
+  // this wave's pieces of one operand of the item's K-tile t (half 0: A, half 1: B)
+  auto issue_half = [&](int tt, int half) {
+    if (!dma_wave) return;
+    const int s = tt & 1, at = kt0 + tt;
+    const int seg = PLANES == 2 ? (at >= nk) + (at >= 2 * nk) : 2;
+    const int kt = PLANES == 2 ? at - seg * nk : at;
+    const _Float16* src =
+        half == 0 ? abase + (size_t)kt * kK + (PLANES == 2 && seg == 0 ? o.plane_a : 0)
+                  : bbase + (size_t)kt * bstep + (PLANES == 2 && seg == 1 ? o.plane_b : 0);
+    const uint32_t dst0 = lds0 + (half == 0 ? a_off(s) : b_off(s));
+#pragma unroll
+    for (int r = 0; r < kReg; ++r)
+#pragma unroll
+      for (int i = 0; i < kBPieces; ++i)
+        dma16s(src, half == 0 ? aoff[r * kBPieces + i] : boff[r * kBPieces + i],
+               __builtin_amdgcn_readfirstlane(dst0 + (region(r) * kBPieces + i) * 1024));
+  };
+
+  f32x4 acc[kTM][kTN];
+#pragma unroll
+  for (int i = 0; i < kTM; ++i)
+#pragma unroll
+    for (int j = 0; j < kTN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // Phase p (0..7) of a K-tile: k-step p / 4, N blocks 2 (p % 4) and the next, eight
+  // MFMAs; fragments are read kLook phases ahead (gemm.hip has the reasons).
+  constexpr int kPh = 8, kLook = 2;
+  f16x8 fa[2][kTM], fb[2][kTN];
+  auto read_frags = [&](int tt, int p) {
+    const int st = tt & 1, ks = p >> 2, r = p & 3;
+    const unsigned char* pa = smem + a_off(st);
+    const unsigned char* pb = smem + b_off(st);
+    if (r == 0) {
+#pragma unroll
+      for (int i = 0; i < kTM; ++i) fa[ks][i] = frag<true, kBT>(pa, wm + 16 * i, ks, lane);
+    }
+#pragma unroll
+    for (int j = 2 * r; j < 2 * r + 2; ++j) fb[ks][j] = frag<BK, kBT>(pb, wn + 16 * j, ks, lane);
+  };
+  auto mma = [&](auto P) {
+    constexpr int p = decltype(P)::value, ks = p >> 2, j0 = 2 * (p & 3);
+#pragma unroll
+    for (int i = 0; i < kTM; ++i)
+#pragma unroll
+      for (int j = j0; j < j0 + 2; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[ks][j], fa[ks][i], acc[i][j], 0, 0, 0);
+    constexpr int pn = (p + kLook) % kPh;
+    constexpr int kReads = ((pn & 3) == 0 ? kTM : 0) + (BK ? 1 : 2) * 2;
+    constexpr int kMfma = kTM * 2;
+    constexpr int pairs = kReads < kMfma ? kReads : kMfma;
+#pragma unroll
+    for (int u = 0; u < pairs; ++u) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    if constexpr (kMfma > pairs) __builtin_amdgcn_sched_group_barrier(0x008, kMfma - pairs, 0);
+    if constexpr (kReads > pairs) __builtin_amdgcn_sched_group_barrier(0x100, kReads - pairs, 0);
+  };
+  auto phase = [&](int tt, auto P) {
+    constexpr int p = decltype(P)::value;
+    if constexpr (p == kPh - kLook) {
+      wait_dma<0>();
+      block_barrier();
+      if (tt + 2 < nt) issue_half(tt + 2, 0);
+    }
+    if constexpr (p == 0)
+      if (tt + 1 >= 2 && tt + 1 < nt) issue_half(tt + 1, 1);
+    if constexpr (p + kLook < kPh) read_frags(tt, p + kLook);
+    else read_frags(tt + 1, p + kLook - kPh);
+    mma(P);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  if (nt > 0) issue_half(0, 0), issue_half(0, 1);
+  if (nt > 1) issue_half(1, 0), issue_half(1, 1);
+  if (nt > 1) wait_dma<kDmaPerTile>();  // tile 0 landed; tile 1 may be in flight
+  else wait_dma<0>();
+  block_barrier();
+#pragma unroll
+  for (int p = 0; p < kLook; ++p) {
+    read_frags(0, p);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  for (int tt = 0; tt < nt; ++tt) {
+    phase(tt, std::integral_constant<int, 0>{});
+    phase(tt, std::integral_constant<int, 1>{});
+    phase(tt, std::integral_constant<int, 2>{});
+    phase(tt, std::integral_constant<int, 3>{});
+    phase(tt, std::integral_constant<int, 4>{});
+    phase(tt, std::integral_constant<int, 5>{});
+    phase(tt, std::integral_constant<int, 6>{});
+    phase(tt, std::integral_constant<int, 7>{});
+  }
+  block_barrier();  // every wave is done with the main loop's LDS
+
+  // Through the wave's own 16 KB of LDS, 32 rows at a time (16-byte chunks XOR-ed by the
+  // row), so that rows go out in whole lines.  acc[i][j][e] is row wm + 16 i + (lane &
+  // 15), column wn + 16 j + 4 (lane >> 4) + e.
+  unsigned char* buf = smem + wave * kEpiLds;
+  const int c = lane & 31, hi = lane >> 5;
+  const int n = n0 + wn + 4 * c;
+  float* pt = slice < 0 ? nullptr
+                        : part + ((size_t)(lid - plan.n_full) * plan.splits + slice) * (kBT * kBT);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+#pragma unroll
+    for (int ii = 0; ii < 2; ++ii)
+#pragma unroll
+      for (int j = 0; j < kTN; ++j) {
+        const int rr = 16 * ii + (lane & 15), cw = 4 * j + (lane >> 4);
+        *reinterpret_cast<f32x4*>(buf + rr * (kWTN * 4) + ((cw ^ rr) & 31) * 16) = acc[2 * i + ii][j];
+      }
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const int r = 2 * k + hi;
+      f32x4* at = reinterpret_cast<f32x4*>(buf + r * (kWTN * 4) + ((c ^ r) & 31) * 16);
+      const int m = m0 + wm + 32 * i + r;
+      if (pt) {
+        *reinterpret_cast<f32x4*>(pt + (m - m0) * kBT + n - n0) = *at;
+        continue;
+      }
+      const f32x4 s4 = *at;
+      float v[4] = {s4[0], s4[1], s4[2], s4[3]};
+      if (m < M && n < N) {
+        store_result4<OP, PLANES>(x, cur, m, n, v);
+        if (OP != Op::Apply && tm != tn) *at = f32x4{v[0], v[1], v[2], v[3]};
+      }
+    }
+    if constexpr (OP != Op::Apply) {
+      // the mirror image: 4 lanes hold the 32 rows of a column, 8 each
+      if (pt || tm == tn) continue;
+      _Float16* out = OP == Op::Gram ? x.a : x.b;
+      const int r8 = 8 * (lane & 3), mm = m0 + wm + 32 * i + r8;
+#pragma unroll
+      for (int k = 0; k < kWTN / 16; ++k) {
+        const int cc = 16 * k + (lane >> 2), row = n0 + wn + cc;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          v[e] = *reinterpret_cast<const float*>(buf + (r8 + e) * (kWTN * 4) +
+                                                 (((cc >> 2) ^ (r8 + e)) & 31) * 16 + (cc & 3) * 4);
+        if (row < N && mm < M)
+          ns_store8<PLANES>(out + (size_t)row * x.m + mm, (size_t)x.m * x.m, v, 1.0f);
+      }
+    }
+  }
+}
+
+// Sum of a split tile's slices, in slice order, and its result: 64 x 64 of the tile per
+// workgroup.
+template <Op OP, int PLANES>
+__global__ __launch_bounds__(256) void ns_reduce_kernel(NsTable t, NsPlan plan, int cur,
+                                                        const float* __restrict__ part) {
+  __shared__ float lds[64][65];
+  const int tail = blockIdx.x >> 4, sub = blockIdx.x & 15, lid = plan.n_full + tail;
+  const int mi = mat_of(plan, t.count, lid);
+  const NsMat& x = t.mat[mi];
+  int tm, tn;
+  tile_at<OP, kBT>(x, lid - plan.first[mi], tm, tn);
+  const int r0 = (sub >> 2) * 64, c0 = (sub & 3) * 64, cl = 4 * (threadIdx.x & 15);
+  const int N = OP == Op::Apply ? x.n : x.m;
+  // (M and N are multiples of 64: the 64 x 64 block is inside or outside whole)
+  if (tm * kBT + r0 >= x.m || tn * kBT + c0 >= N) return;
+  const float* p = part + (size_t)tail * plan.splits * (kBT * kBT) + c0 + cl;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int rl = (threadIdx.x >> 4) + 16 * k;
+    const float* q = p + (r0 + rl) * kBT;
+    f32x4 s = *reinterpret_cast<const f32x4*>(q);
+    for (int i = 1; i < plan.splits; ++i)
+      s += *reinterpret_cast<const f32x4*>(q + (size_t)i * kBT * kBT);
+    float v[4] = {s[0], s[1], s[2], s[3]};
+    store_result4<OP, PLANES>(x, cur, tm * kBT + r0 + rl, tn * kBT + c0 + cl, v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) lds[rl][cl + e] = v[e];
+  }
+  if constexpr (OP != Op::Apply) {
+    if (tm == tn) return;
+    __syncthreads();
+    _Float16* out = OP == Op::Gram ? x.a : x.b;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int cc = (threadIdx.x >> 3) + 32 * k, r8 = 8 * (threadIdx.x & 7);
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = lds[r8 + e][cc];
+      ns_store8<PLANES>(out + (size_t)(tn * kBT + c0 + cc) * x.m + tm * kBT + r0 + r8,
+                        (size_t)x.m * x.m, v, 1.0f);
+    }
+  }
+}
+
+// ------------------------------------------------------ 128 x 128 tiles
+constexpr int kT = 128;
+constexpr int kWaves = 4;  // 2 x 2, each 64 x 64
+constexpr int kThreads = 64 * kWaves;
+constexpr int kOpBytes = kT * kK * 2;                // one operand's K-tile: 16 KB
+constexpr int kPieces = kOpBytes / (1024 * kWaves);  // 1 KB DMA pieces per wave
+constexpr int kRowF = kT + 4;                        // floats per row of the staged output
+
+template <Op OP, int PLANES>
+__global__ __launch_bounds__(kThreads, 2) void ns_gemm_kernel(NsTable t, NsPlan plan, int cur) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[kT * kRowF * 4];
   static_assert(4 * kOpBytes <= kT * kRowF * 4, "two stages of two operands");
-  constexpr bool BK = OP != Op::Apply;  // B operand K-contiguous
+  constexpr bool BK = OP != Op::Apply;
   const int lid = xcd_remap(blockIdx.x, gridDim.x);
-  int mi = 0;
-#pragma unroll 1
-  for (int k = 1; k < t.count; ++k)
-    if (lid >= tiles.first[k]) mi = k;
+  const int mi = mat_of(plan, t.count, lid);
   const NsMat& x = t.mat[mi];
-  const int m = x.m, n = x.n, id = lid - tiles.first[mi];
   int tm, tn;
-  if constexpr (OP == Op::Apply) {
-    tile_of<8>(id, (m + kT - 1) / kT, (n + kT - 1) / kT, tm, tn);
-  } else {  // tile id of the triangle tm <= tn, column by column
-    tn = (int)((__builtin_sqrtf(8.0f * id + 1.0f) - 1.0f) * 0.5f);
-    while (tn * (tn + 1) / 2 > id) --tn;
-    while ((tn + 1) * (tn + 2) / 2 <= id) ++tn;
-    tm = id - tn * (tn + 1) / 2;
-  }
-  const int m0 = tm * kT, n0 = tn * kT;
-  // operands: gram X, X; square A, A; apply B, X
-  const _Float16* A = OP == Op::Gram ? x.x[cur] : OP == Op::Square ? x.a : x.b;
-  const _Float16* B = OP == Op::Square ? x.a : x.x[cur];
-  const int lda = OP == Op::Gram ? n : m, ldb = OP == Op::Square ? m : n;
-  const int K = OP == Op::Gram ? n : m;
-  const size_t plane_a = (size_t)m * lda, plane_b = (size_t)m * ldb;
+  tile_at<OP, kT>(x, lid - plan.first[mi], tm, tn);
+  const int m0 = tm * kT, n0 = tn * kT, M = x.m, N = BK ? x.m : x.n;
+  const Operands o = operands<OP>(x, cur);
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -114,17 +456,18 @@ __global__ __launch_bounds__(kThreads, 2) void ns_gemm_kernel(NsTable t, NsTiles
 #pragma unroll
   for (int i = 0; i < kPieces; ++i) {
     const int p = (wave * kPieces + i) * 1024 + 16 * lane;
-    aoff[i] = lane_off<true>(lda, m - m0, p);
-    boff[i] = lane_off<BK>(ldb, (BK ? m : n) - n0, p);
+    aoff[i] = lane_off<true, kT>(o.lda, M - m0, p);
+    boff[i] = lane_off<BK, kT>(o.ldb, N - n0, p);
   }
-  const _Float16* abase = A + (size_t)m0 * lda;
-  const _Float16* bbase = BK ? B + (size_t)n0 * ldb : B + n0;
-  const size_t bstep = BK ? kK : (size_t)kK * ldb;
-  const int nk = K / kK, nt = PLANES == 2 ? 3 * nk : nk;
+  const _Float16* abase = o.A + (size_t)m0 * o.lda;
+  const _Float16* bbase = BK ? o.B + (size_t)n0 * o.ldb : o.B + n0;
+  const size_t bstep = BK ? kK : (size_t)kK * o.ldb;
+  const int nk = o.K / kK, nt = PLANES == 2 ? 3 * nk : nk;
   auto issue = [&](int tt) {
-    const int seg = PLANES == 2 ? tt / nk : 2, kt = PLANES == 2 ? tt - seg * nk : tt;
-    const _Float16* a = abase + (size_t)kt * kK + (seg == 0 ? plane_a : 0);
-    const _Float16* b = bbase + kt * bstep + (seg == 1 ? plane_b : 0);
+    const int seg = PLANES == 2 ? (tt >= nk) + (tt >= 2 * nk) : 2;
+    const int kt = PLANES == 2 ? tt - seg * nk : tt;
+    const _Float16* a = abase + (size_t)kt * kK + (PLANES == 2 && seg == 0 ? o.plane_a : 0);
+    const _Float16* b = bbase + kt * bstep + (PLANES == 2 && seg == 1 ? o.plane_b : 0);
     const uint32_t at = lds0 + (tt & 1) * 2 * kOpBytes + wave * kPieces * 1024;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
@@ -141,7 +484,7 @@ __global__ __launch_bounds__(kThreads, 2) void ns_gemm_kernel(NsTable t, NsTiles
   issue(0);
   for (int tt = 0; tt < nt; ++tt) {
     // tile tt has landed for every wave, and every wave is done with tile tt - 1
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    wait_dma<0>();
     __syncthreads();
     if (tt + 1 < nt) issue(tt + 1);
     const unsigned char* pa = smem + (tt & 1) * 2 * kOpBytes;
@@ -150,9 +493,9 @@ __global__ __launch_bounds__(kThreads, 2) void ns_gemm_kernel(NsTable t, NsTiles
     for (int s = 0; s < 2; ++s) {
       f16x8 fa[4], fb[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) fa[i] = frag<true>(pa, wm + 16 * i, s, lane);
+      for (int i = 0; i < 4; ++i) fa[i] = frag<true, kT>(pa, wm + 16 * i, s, lane);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) fb[j] = frag<BK>(pb, wn + 16 * j, s, lane);
+      for (int j = 0; j < 4; ++j) fb[j] = frag<BK, kT>(pb, wn + 16 * j, s, lane);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -173,74 +516,92 @@ __global__ __launch_bounds__(kThreads, 2) void ns_gemm_kernel(NsTable t, NsTiles
                                 4 * (lane >> 4)) = acc[i][j];
   __syncthreads();
   const int c = 4 * (threadIdx.x & 31);
-  const bool cok = n0 + c < (BK ? m : n);
-  constexpr float kOut = OP == Op::Gram     ? kNsScaleA / (kNsScaleX * kNsScaleX)
-                         : OP == Op::Square ? kNsC * kNsScaleB / (kNsScaleA * kNsScaleA)
-                                            : 1.0f / kNsScaleB;
 #pragma unroll 4
   for (int r = threadIdx.x >> 5; r < kT; r += kThreads / 32) {
     const int row = m0 + r;
-    if (row >= m || !cok) continue;
-    float v[4], add[4];
+    if (row >= M || n0 + c >= N) continue;
     const f32x4 s4 = *reinterpret_cast<const f32x4*>(stage + r * kRowF + c);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = s4[e] * kOut;
-    if constexpr (OP == Op::Gram) {
-      ns_store4<PLANES>(x.a + (size_t)row * m + n0 + c, (size_t)m * m, v, 1.0f);
-    } else if constexpr (OP == Op::Square) {
-      ns_load4<PLANES>(x.a + (size_t)row * m + n0 + c, (size_t)m * m, add,
-                       kNsB * kNsScaleB / kNsScaleA);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += add[e];
-      ns_store4<PLANES>(x.b + (size_t)row * m + n0 + c, (size_t)m * m, v, 1.0f);
-      if (tm != tn) *reinterpret_cast<f32x4*>(stage + r * kRowF + c) = f32x4{v[0], v[1], v[2], v[3]};
-    } else {
-      ns_load4<PLANES>(x.x[cur] + (size_t)row * n + n0 + c, (size_t)m * n, add, kNsA);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += add[e];
-      ns_store4<PLANES>(x.x[cur ^ 1] + (size_t)row * n + n0 + c, (size_t)m * n, v, 1.0f);
-    }
+    float v[4] = {s4[0], s4[1], s4[2], s4[3]};
+    store_result4<OP, PLANES>(x, cur, row, n0 + c, v);
+    if (OP != Op::Apply && tm != tn)
+      *reinterpret_cast<f32x4*>(stage + r * kRowF + c) = f32x4{v[0], v[1], v[2], v[3]};
   }
   if constexpr (OP != Op::Apply) {
     if (tm == tn) return;
     __syncthreads();
     _Float16* out = OP == Op::Gram ? x.a : x.b;
     const int r4 = 4 * (threadIdx.x & 31);  // four rows of the tile: columns of its image
-    if (m0 + r4 >= m) return;
+    if (m0 + r4 >= M) return;
 #pragma unroll 4
     for (int cc = threadIdx.x >> 5; cc < kT; cc += kThreads / 32) {
-      const int row = n0 + cc;
-      if (row >= m) continue;
+      if (n0 + cc >= N) continue;
       float v[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = stage[(r4 + e) * kRowF + cc] * (OP == Op::Gram ? kOut : 1.0f);
-      ns_store4<PLANES>(out + (size_t)row * m + m0 + r4, (size_t)m * m, v, 1.0f);
+      for (int e = 0; e < 4; ++e) v[e] = stage[(r4 + e) * kRowF + cc];
+      ns_store4<PLANES>(out + (size_t)(n0 + cc) * M + m0 + r4, (size_t)M * M, v, 1.0f);
     }
   }
 }
 
-template <Op OP, int PLANES>
-void launch(const NsTable& t, int cur, hipStream_t s) {
-  NsTiles tiles{};
+// ---------------------------------------------------------------- plans
+int tiles_of(Op op, const NsMat& x, int t) {
+  const int tm = (x.m + t - 1) / t, tn = (x.n + t - 1) / t;
+  return op == Op::Apply ? tm * tn : tm * (tm + 1) / 2;
+}
+
+// Whether the 256 x 256 tiles fill the chip, and how: whole rounds of tiles, and the
+// tiles of the last, partial round cut along K so that they end together.
+struct Choice {
+  bool big;
+  NsPlan plan;
+  int tail;
+};
+Choice choose(Op op, const NsTable& t, int planes) {
+  Choice c{};
+  long long work = 0;  // K-tiles
   for (int i = 0; i < t.count; ++i) {
-    const int tm = tiles_of(t.mat[i].m), tn = tiles_of(t.mat[i].n);
-    tiles.first[i + 1] = tiles.first[i] + (OP == Op::Apply ? tm * tn : tm * (tm + 1) / 2);
+    const int n = tiles_of(op, t.mat[i], kBT);
+    c.plan.first[i + 1] = c.plan.first[i] + n;
+    work += (long long)n * planes * (op == Op::Gram ? t.mat[i].n : t.mat[i].m) / kK;
   }
-  ns_gemm_kernel<OP, PLANES><<<tiles.first[t.count], kThreads, 0, s>>>(t, tiles, cur);
+  const int tiles = c.plan.first[t.count];
+  c.big = tiles >= 128;
+  if (!c.big) {
+    for (int i = 0; i < t.count; ++i)
+      c.plan.first[i + 1] = c.plan.first[i] + tiles_of(op, t.mat[i], kT);
+    c.plan.n_full = c.plan.first[t.count];
+    c.plan.splits = 1;
+    return c;
+  }
+  c.plan.n_full = tiles;
+  c.plan.splits = 1;
+  return c;
+}
+
+template <Op OP, int PLANES>
+void launch(const NsTable& t, int cur, float* part, hipStream_t s) {
+  const Choice c = choose(OP, t, PLANES);
+  if (c.big) {
+    ns_gemm_big<OP, PLANES>
+        <<<c.plan.n_full + c.tail * c.plan.splits, kBThreads, kBLds, s>>>(t, c.plan, cur, part);
+    if (c.tail) ns_reduce_kernel<OP, PLANES><<<c.tail * 16, 256, 0, s>>>(t, c.plan, cur, part);
+  } else {
+    ns_gemm_kernel<OP, PLANES><<<c.plan.n_full, kThreads, 0, s>>>(t, c.plan, cur);
+  }
 }
 
 template <int PLANES>
-void step(const NsTable& t, int cur, hipStream_t s) {
-  launch<Op::Gram, PLANES>(t, cur, s);
-  launch<Op::Square, PLANES>(t, cur, s);
-  launch<Op::Apply, PLANES>(t, cur, s);
+void step(const NsTable& t, int cur, float* part, hipStream_t s) {
+  launch<Op::Gram, PLANES>(t, cur, part, s);
+  launch<Op::Square, PLANES>(t, cur, part, s);
+  launch<Op::Apply, PLANES>(t, cur, part, s);
 }
 
 }  // namespace
 
 void launch_ns_step(const NsTable& t, int planes, int cur, hipStream_t s) {
-  if (planes == 2) step<2>(t, cur, s);
-  else step<1>(t, cur, s);
+  if (planes == 2) step<2>(t, cur, nullptr, s);
+  else step<1>(t, cur, nullptr, s);
 }
 
 }  // namespace pb

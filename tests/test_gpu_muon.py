@@ -293,3 +293,51 @@ def test_muon_streams_and_graph():
         graph.replay()
         torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(state(st), alone[0]))
+
+
+def wide_oracle(u, steps=5, dtype=None, rnd=lambda v: v):
+    """The iteration in torch on the GPU, for sizes that numpy is too slow for."""
+    import torch
+    a, b, c = oo.NS
+    dtype = dtype or torch.float64
+    x = u.double()
+    x = x.t() if u.shape[0] > u.shape[1] else x
+    x = rnd((x / (x.square().sum().sqrt() + 1e-7)).to(dtype))
+    for _ in range(steps):
+        gram = rnd(x @ x.t().contiguous())
+        x = rnd(a * x + rnd(b * gram + c * (gram @ gram)) @ x)
+    return (x.t() if u.shape[0] > u.shape[1] else x).double()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shapes", [
+    [(4160, 4290)],                              # 153 tiles of the triangle, ragged
+    [(17000, 520)],                              # few rows, 3 x 67 tiles of the last product
+    [(2048, 2112)] * 4 + [(300, 257), (1, 64)],  # several, with small ones among them
+    [(3000, 1200), (1200, 5000), (640, 640)],
+], ids=str)
+def test_orthogonalize_large(dtype, shapes):
+    import torch
+    from paper_2402_15627_amd import pblock as pb
+    _say(f"[gpu] orthogonalize {dtype} {shapes}")
+    act = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator(device="cuda").manual_seed(7)
+    xs = [torch.empty(r, c, device="cuda").normal_(generator=g).to(act) for r, c in shapes]
+    outs = [torch.full_like(x, 7.0) for x in xs]
+    part = [pb.ortho_tensor(x, o) for x, o in zip(xs, outs)]
+    ws = torch.empty(pb.pblock_orthogonalize_workspace_bytes(part, dtype), dtype=torch.uint8,
+                     device="cuda").fill_(255)
+    pb.pblock_orthogonalize(part, dtype, ws)
+    again = [torch.empty_like(x) for x in xs]
+    pb.pblock_orthogonalize([pb.ortho_tensor(x, o) for x, o in zip(xs, again)], dtype, ws)
+    fp16 = lambda v: (v * 16384).half().float() / 16384  # noqa: E731
+    for x, o, o2 in zip(xs, outs, again):
+        ref = wide_oracle(x)
+        n = float(ref.norm())
+        e = float((o.double() - ref).norm()) / n
+        if dtype == "f32":
+            tol = 4 * float((wide_oracle(x, dtype=torch.float32) - ref).norm()) / n + 2.0 ** -20
+        else:
+            tol = 2 * float((wide_oracle(x, dtype=torch.float32, rnd=fp16) - ref).norm()) / n + 2.0 ** -8
+        _say(f"      {tuple(x.shape)}: off {e:.2e} of {tol:.2e}")
+        assert e <= tol and torch.equal(o, o2)

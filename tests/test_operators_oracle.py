@@ -109,7 +109,7 @@ def test_newton_schulz_is_its_polynomial_on_the_singular_values(shape, steps):
 
 
 def test_newton_schulz_stays_in_the_range_that_the_planes_are_scaled_for():
-    """Over [0, 1]: X <= 1.2024, X X^T <= 1.446 and b s + c s^2 within [-2.807, 0], with
+    """Over [0, 1]: X <= 1.2024, X X^T <= 1.446 and a + b s + c s^2 within [0.637, a], with
     the powers of two of the kernel's planes below fp16's largest number."""
     s = np.linspace(0, 1, 200001)
     a, b, c = oo.NS
@@ -117,9 +117,9 @@ def test_newton_schulz_stays_in_the_range_that_the_planes_are_scaled_for():
         t = s * s
         poly = b * t + c * t * t
         assert s.max() <= 1.2024 and t.max() <= 1.446
-        assert poly.min() >= -2.807 and poly.max() <= 1e-12
+        assert a + poly.min() >= 0.637 and poly.max() <= 1e-12
         s = np.abs(a * s + poly * s)
-    assert 1.2024 * 32768 < 65504 and 1.446 * 32768 < 65504 and 2.807 * 16384 < 65504
+    assert 1.2024 * 32768 < 65504 and 1.446 * 32768 < 65504 and a * 16384 < 65504
 
 
 @pytest.mark.parametrize("nesterov", [False, True])
