@@ -124,8 +124,8 @@ void launch_rms_backward(Dt dt, const RmsBackward& a, hipStream_t s);
 // ------------------------------------- orthogonalised updates (Newton-Schulz)
 // One matrix of a call.  The iterate X is the update or, where it has more rows than
 // columns, its transpose: m x n with m <= n, both padded to multiples of 64 with
-// zeros.  x, a and b hold fp16 planes (one, or a value and its remainder): X twice
-// (in turn), X X^T, and the polynomial of it.
+// zeros.  x, a and b hold fp16 values (alone, or each with its remainder): X twice (in
+// turn), X X^T, and the polynomial of it.
 constexpr int kNsMaxTensors = 16;
 constexpr int kNsPad = 64;
 struct NsMat {
@@ -152,9 +152,11 @@ struct NsScalars {
 };
 // Where the updates come from and go to.
 enum class NsMode { Muon, Bf16, F32 };
-// partial: a double per tile; norm: one per matrix.
+// partial: a double per tile; norm: one per matrix; part: ns_partial_floats(t, planes)
+// floats, for the products' K-slices.
+size_t ns_partial_floats(const NsTable& t, int planes);
 void launch_newton_schulz(const NsTable& t, const NsScalars& sc, NsMode mode, Dt copy_dt,
-                          double* partial, double* norm, hipStream_t s);
+                          double* partial, double* norm, float* part, hipStream_t s);
 
 // ------------------------------------------------------ reduce-scatter sum
 // y = x + bias + sum over q < n of parts[q], row-major [rows, H] (H a

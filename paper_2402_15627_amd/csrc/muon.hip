@@ -175,7 +175,7 @@ __global__ __launch_bounds__(kThreads) void ns_init_kernel(NsTable t, NsScalars 
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = lds[i][j + e];
-    ns_store8<PLANES>(x.x[0] + (size_t)(i0 + i) * x.n + j0 + j, (size_t)x.m * x.n, v, kNsScaleX);
+    ns_store<PLANES, 8>(x.x[0] + ns_at<PLANES>(x.n, i0 + i, j0 + j), v, kNsScaleX);
   }
 }
 
@@ -192,8 +192,7 @@ __global__ __launch_bounds__(kThreads) void ns_apply_kernel(NsTable t, NsScalars
   for (int k = 0; k < 2; ++k) {
     const int i = (threadIdx.x >> 3) + 32 * k, j = 8 * (threadIdx.x & 7);
     float v[8];
-    ns_load8<PLANES>(x.x[last] + (size_t)(i0 + i) * x.n + j0 + j, (size_t)x.m * x.n, v,
-                     1.0f / kNsScaleX);
+    ns_load<PLANES, 8>(x.x[last] + ns_at<PLANES>(x.n, i0 + i, j0 + j), v, 1.0f / kNsScaleX);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       if (tall) lds[j + e][i] = v[e];
@@ -228,12 +227,12 @@ __global__ __launch_bounds__(kThreads) void ns_apply_kernel(NsTable t, NsScalars
 
 template <NsMode MODE, int PLANES>
 void run(const NsTable& t, const NsScalars& sc, Dt copy_dt, double* partial, double* norm,
-         hipStream_t s) {
+         float* part, hipStream_t s) {
   const int tiles = t.tile0[t.count];
   ns_update_kernel<MODE><<<tiles, kThreads, 0, s>>>(t, sc, partial);
   ns_norm_kernel<<<t.count, kThreads, 0, s>>>(t, sc.eps, partial, norm);
   ns_init_kernel<MODE, PLANES><<<tiles, kThreads, 0, s>>>(t, sc, norm);
-  for (int k = 0; k < sc.steps; ++k) launch_ns_step(t, PLANES, k & 1, s);
+  for (int k = 0; k < sc.steps; ++k) launch_ns_step(t, PLANES, k & 1, part, s);
   const int last = sc.steps & 1;
   if (MODE == NsMode::Bf16 || (MODE == NsMode::Muon && copy_dt == Dt::BF16))
     ns_apply_kernel<MODE, PLANES, bf16><<<tiles, kThreads, 0, s>>>(t, sc, last);
@@ -244,14 +243,14 @@ void run(const NsTable& t, const NsScalars& sc, Dt copy_dt, double* partial, dou
 }  // namespace
 
 void launch_newton_schulz(const NsTable& t, const NsScalars& sc, NsMode mode, Dt copy_dt,
-                          double* partial, double* norm, hipStream_t s) {
+                          double* partial, double* norm, float* part, hipStream_t s) {
   switch (mode) {
     case NsMode::Muon:
-      if (sc.planes == 2) run<NsMode::Muon, 2>(t, sc, copy_dt, partial, norm, s);
-      else run<NsMode::Muon, 1>(t, sc, copy_dt, partial, norm, s);
+      if (sc.planes == 2) run<NsMode::Muon, 2>(t, sc, copy_dt, partial, norm, part, s);
+      else run<NsMode::Muon, 1>(t, sc, copy_dt, partial, norm, part, s);
       break;
-    case NsMode::Bf16: run<NsMode::Bf16, 1>(t, sc, copy_dt, partial, norm, s); break;
-    case NsMode::F32: run<NsMode::F32, 2>(t, sc, copy_dt, partial, norm, s); break;
+    case NsMode::Bf16: run<NsMode::Bf16, 1>(t, sc, copy_dt, partial, norm, part, s); break;
+    case NsMode::F32: run<NsMode::F32, 2>(t, sc, copy_dt, partial, norm, part, s); break;
   }
 }
 

@@ -21,49 +21,41 @@ constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
-// Eight consecutive values to the planes `plane` elements apart, times scale.
+// Address of element (row, col) of a matrix with rows of ld: one plane is row-major;
+// with two, 32 values and their 32 remainders alternate along a row, so that 128 bytes
+// of a row hold both of 32 elements.  The remainder lies kNsRest after the value.
+constexpr int kNsRest = 32;
 template <int PLANES>
-PB_DEV void ns_store8(_Float16* p, size_t plane, const float* v, float scale) {
-  f16x8 hi, lo;
+PB_DEV size_t ns_at(int ld, int row, int col) {
+  if constexpr (PLANES == 1) return (size_t)row * ld + col;
+  else return (size_t)row * (2 * ld) + (col >> 5) * 64 + (col & 31);
+}
+// N (4 or 8) consecutive values from p on, times scale.
+template <int PLANES, int N>
+PB_DEV void ns_store(_Float16* p, const float* v, float scale) {
+  typedef _Float16 vec __attribute__((ext_vector_type(N)));
+  vec hi, lo;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+  for (int e = 0; e < N; ++e) {
     const float x = v[e] * scale;
     hi[e] = (_Float16)x;
     lo[e] = (_Float16)(x - (float)hi[e]);
   }
-  *reinterpret_cast<f16x8*>(p) = hi;
-  if constexpr (PLANES == 2) *reinterpret_cast<f16x8*>(p + plane) = lo;
+  *reinterpret_cast<vec*>(p) = hi;
+  if constexpr (PLANES == 2) *reinterpret_cast<vec*>(p + kNsRest) = lo;
 }
-template <int PLANES>
-PB_DEV void ns_store4(_Float16* p, size_t plane, const float* v, float scale) {
-  f16x4 hi, lo;
+template <int PLANES, int N>
+PB_DEV void ns_load(const _Float16* p, float* v, float scale) {
+  typedef _Float16 vec __attribute__((ext_vector_type(N)));
+  const vec hi = *reinterpret_cast<const vec*>(p);
+  vec lo = {};
+  if constexpr (PLANES == 2) lo = *reinterpret_cast<const vec*>(p + kNsRest);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float x = v[e] * scale;
-    hi[e] = (_Float16)x;
-    lo[e] = (_Float16)(x - (float)hi[e]);
-  }
-  *reinterpret_cast<f16x4*>(p) = hi;
-  if constexpr (PLANES == 2) *reinterpret_cast<f16x4*>(p + plane) = lo;
-}
-template <int PLANES>
-PB_DEV void ns_load8(const _Float16* p, size_t plane, float* v, float scale) {
-  const f16x8 hi = *reinterpret_cast<const f16x8*>(p);
-  f16x8 lo = {};
-  if constexpr (PLANES == 2) lo = *reinterpret_cast<const f16x8*>(p + plane);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = ((float)hi[e] + (float)lo[e]) * scale;
-}
-template <int PLANES>
-PB_DEV void ns_load4(const _Float16* p, size_t plane, float* v, float scale) {
-  const f16x4 hi = *reinterpret_cast<const f16x4*>(p);
-  f16x4 lo = {};
-  if constexpr (PLANES == 2) lo = *reinterpret_cast<const f16x4*>(p + plane);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = ((float)hi[e] + (float)lo[e]) * scale;
+  for (int e = 0; e < N; ++e) v[e] = ((float)hi[e] + (float)lo[e]) * scale;
 }
 
-// One Newton-Schulz step of every matrix: x[cur] -> x[cur ^ 1].
-void launch_ns_step(const NsTable& t, int planes, int cur, hipStream_t s);
+// One Newton-Schulz step of every matrix: x[cur] -> x[cur ^ 1].  part: room for
+// ns_partial_floats(t, planes) floats.
+void launch_ns_step(const NsTable& t, int planes, int cur, float* part, hipStream_t s);
 
 }  // namespace pb

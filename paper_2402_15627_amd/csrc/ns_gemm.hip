@@ -7,8 +7,9 @@
 //
 // MFMA v_mfma_f32_16x16x32_f16 on the planes of ns_gemm.h, fp32 accumulation.  One
 // plane: one product of fp16 values (rounded by 2^-11 at most).  Two planes (value h
-// and remainder l): h l + l h + h h, in this order, as one sum over three times the
-// length (what is left out, l l, is at most 2^-22 of the product).  a goes into B, not
+// and remainder l): l h + h h + h l (what is left out, l l, is at most 2^-22 of the
+// product).  A K-tile of 128-byte rows is 64 k of one plane or 32 k of both: two planes
+// move the same bytes for one and a half times the products.  a goes into B, not
 // into apply's sum: near the end B is about 0.7 to 1.4 instead of -2.7 to -2.0, so its
 // rounding moves X' by less (one plane, one row of 777: 3.4e-3 off, 8e-4 so; 512 x 512
 // 1.34e-3, 1.24e-3), and apply reads no X beside its operand.
@@ -34,8 +35,10 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 enum class Op { Gram, Square, Apply };
 
-constexpr int kK = 64;  // K-tile
-static_assert(kNsPad == kK, "X's dimensions are whole K-tiles");
+constexpr int kRow = 64;  // fp16 values of a K-contiguous row of a K-tile: 128 bytes
+template <int PLANES>
+constexpr int kK = kRow / PLANES;  // k of a K-tile
+static_assert(kNsPad == kRow, "X's dimensions are whole K-tiles");
 
 // From the sum of plane products to the result's plane values.
 template <Op OP>
@@ -49,43 +52,49 @@ PB_DEV int swz(int row, int c) { return c ^ ((row ^ (row >> 3)) & 7); }
 PB_DEV int swz_mn(int k, int c) { return c ^ (4 * (k & 3)) ^ (2 * ((k >> 3) & 1)); }
 
 // Byte offset from the operand tile's first element of this lane's 16 bytes of the LDS
-// position p.  KC: rows of the operand are K-contiguous, `rows` of them left; else the
-// operand is K rows of which `rows` columns are left.
-template <bool KC, int T>
+// position p, for rows of ld values (both planes counted).  KC: rows of the operand are
+// K-contiguous, `rows` of them left; else the operand is K rows of which `rows` columns
+// are left.
+template <bool KC, int T, int PLANES>
 PB_DEV uint32_t lane_off(int ld, int rows, int p) {
   if constexpr (KC) {
     const int row = p >> 7, c = swz(row, (p >> 4) & 7);
-    return (uint32_t)(min(row, rows - 1) * ld + 8 * c) * 2u;
+    return ((uint32_t)min(row, rows - 1) * (uint32_t)ld + 8 * c) * 2u;
   } else {
-    const int k = p / (2 * T), c = swz_mn(k, (p >> 4) & (T / 8 - 1));
-    return (uint32_t)(k * ld + min(8 * c, rows - 8)) * 2u;
+    constexpr int kChunks = T * PLANES / 8;  // 16-byte chunks of a k-row
+    const int k = p / (16 * kChunks), c = swz_mn(k, (p >> 4) & (kChunks - 1));
+    return ((uint32_t)k * (uint32_t)ld + min(8 * c, PLANES * rows - 8)) * 2u;
   }
 }
-// Fragment of 16 rows (columns) from `base`, k 32 s + 8 (lane >> 4) .. + 7.
-template <bool KC, int T>
-PB_DEV f16x8 frag(const unsigned char* tile, int base, int s, int lane) {
+// Fragment f of 16 rows (columns) from `base`: one plane, k 32 f + 8 (lane >> 4) .. + 7;
+// two planes, plane f (0 the values, 1 the remainders) of k 8 (lane >> 4) .. + 7.
+template <bool KC, int T, int PLANES>
+PB_DEV f16x8 frag(const unsigned char* tile, int base, int f, int lane) {
   if constexpr (KC) {
     const int row = base + (lane & 15);
-    return *reinterpret_cast<const f16x8*>(tile + row * 128 + swz(row, 4 * s + (lane >> 4)) * 16);
+    return *reinterpret_cast<const f16x8*>(tile + row * 128 + swz(row, 4 * f + (lane >> 4)) * 16);
   } else {
     const int i = lane & 15, mn = base + 4 * (i & 3);
-    const int k1 = 32 * s + 8 * (lane >> 4) + (i >> 2), k2 = k1 + 4;
-    const int c = mn >> 3, off = (mn & 7) * 2;
+    const int k1 = (PLANES == 1 ? 32 * f : 0) + 8 * (lane >> 4) + (i >> 2), k2 = k1 + 4;
+    const int c = PLANES == 1 ? mn >> 3 : 8 * (mn >> 5) + 4 * f + ((mn & 31) >> 3);
+    const int off = (mn & 7) * 2;
     const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (PB_LDS s16x4*)(tile + k1 * (2 * T) + swz_mn(k1, c) * 16 + off));
+        (PB_LDS s16x4*)(tile + k1 * (2 * T * PLANES) + swz_mn(k1, c) * 16 + off));
     const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (PB_LDS s16x4*)(tile + k2 * (2 * T) + swz_mn(k2, c) * 16 + off));
+        (PB_LDS s16x4*)(tile + k2 * (2 * T * PLANES) + swz_mn(k2, c) * 16 + off));
     const f16x4 a4 = __builtin_bit_cast(f16x4, a), b4 = __builtin_bit_cast(f16x4, b);
     return f16x8{a4[0], a4[1], a4[2], a4[3], b4[0], b4[1], b4[2], b4[3]};
   }
 }
 
 // ------------------------------------------------------------ work items
-// A launch's items are tiles, or K-slices of tiles, in the order of NsPlan: the first
-// n_full tiles whole, then `splits` slices of each tile after them, whose fp32 partial
-// tiles ns_reduce_kernel sums.  first[i]: matrix i's first tile.
+// A launch's items are tiles, or K-slices of tiles: tiles 0 .. n_full - 1 whole, then
+// `splits` slices of each tile after them, whose fp32 partial tiles ns_reduce_kernel
+// sums.  Tiles count through the matrices in the order of mat[] (longest K first):
+// first[i] is that of matrix mat[i].
 struct NsPlan {
   int first[kNsMaxTensors + 1];
+  int mat[kNsMaxTensors];
   int n_full, splits;
 };
 
@@ -121,7 +130,7 @@ PB_DEV void tile_at(const NsMat& x, int id, int& tm, int& tn) {
   else triangle_tile(id, t, tm, tn);
 }
 
-PB_DEV int mat_of(const NsPlan& p, int count, int tile) {
+PB_DEV int place_of(const NsPlan& p, int count, int tile) {
   int i = 0;
 #pragma unroll 1
   for (int k = 1; k < count; ++k)
@@ -129,18 +138,39 @@ PB_DEV int mat_of(const NsPlan& p, int count, int tile) {
   return i;
 }
 
-// Operands of a product, and where its result goes.
+// Workgroup b's item: tile (counted through the plan) and slice (-1: whole), and the
+// tile's place in mat[].  Workgroup b runs on XCD b % 8: the tiles of a matrix (and the
+// slices) are dealt out so that each XCD takes a contiguous run of each matrix.
+struct Item {
+  int tile, slice, place;
+};
+PB_DEV Item item_of(const NsPlan& p, int count, int b, int n) {
+  Item it{b, -1, 0};
+  if (b >= p.n_full) {
+    const int j = xcd_remap(b - p.n_full, n - p.n_full);
+    it.tile = p.n_full + j / p.splits;
+    it.slice = j % p.splits;
+    it.place = place_of(p, count, it.tile);
+  } else {
+    it.place = place_of(p, count, b);
+    const int f = p.first[it.place];
+    it.tile = f + xcd_remap(b - f, min(p.first[it.place + 1], p.n_full) - f);
+  }
+  return it;
+}
+
+// Operands of a product: A K-contiguous, B K-contiguous too but for apply's; leading
+// dimensions with both planes counted.
 struct Operands {
   const _Float16 *A, *B;
-  size_t plane_a, plane_b;  // elements to the second plane
   int lda, ldb, K;
 };
-template <Op OP>
+template <Op OP, int PLANES>
 PB_DEV Operands operands(const NsMat& x, int cur) {
-  const size_t mm = (size_t)x.m * x.m, mn = (size_t)x.m * x.n;
-  if constexpr (OP == Op::Gram) return {x.x[cur], x.x[cur], mn, mn, x.n, x.n, x.n};
-  else if constexpr (OP == Op::Square) return {x.a, x.a, mm, mm, x.m, x.m, x.m};
-  else return {x.b, x.x[cur], mm, mn, x.m, x.n, x.m};
+  const int m = PLANES * x.m, n = PLANES * x.n;
+  if constexpr (OP == Op::Gram) return {x.x[cur], x.x[cur], n, n, x.n};
+  else if constexpr (OP == Op::Square) return {x.a, x.a, m, m, x.m};
+  else return {x.b, x.x[cur], m, n, x.m};
 }
 
 // Four consecutive columns n.. of row m of the result, v: the sums (scaled in place).
@@ -150,23 +180,22 @@ PB_DEV void store_result4(const NsMat& x, int cur, int m, int n, float* v) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] *= kOut;
   if constexpr (OP == Op::Gram) {
-    ns_store4<PLANES>(x.a + (size_t)m * x.m + n, (size_t)x.m * x.m, v, 1.0f);
+    ns_store<PLANES, 4>(x.a + ns_at<PLANES>(x.m, m, n), v, 1.0f);
   } else if constexpr (OP == Op::Square) {
     float a4[4];
-    ns_load4<PLANES>(x.a + (size_t)m * x.m + n, (size_t)x.m * x.m, a4,
-                     kNsB * kNsScaleB / kNsScaleA);
+    ns_load<PLANES, 4>(x.a + ns_at<PLANES>(x.m, m, n), a4, kNsB * kNsScaleB / kNsScaleA);
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] += a4[e] + (m == n + e ? kNsA * kNsScaleB : 0.f);
-    ns_store4<PLANES>(x.b + (size_t)m * x.m + n, (size_t)x.m * x.m, v, 1.0f);
+    ns_store<PLANES, 4>(x.b + ns_at<PLANES>(x.m, m, n), v, 1.0f);
   } else {
-    ns_store4<PLANES>(x.x[cur ^ 1] + (size_t)m * x.n + n, (size_t)x.m * x.n, v, 1.0f);
+    ns_store<PLANES, 4>(x.x[cur ^ 1] + ns_at<PLANES>(x.n, m, n), v, 1.0f);
   }
 }
 
 // ------------------------------------------------------ 256 x 256 tiles
 constexpr int kBT = 256;
 constexpr int kBThreads = 512;                       // 4 (m) x 2 (n) waves, each 64 x 128
-constexpr int kBTile = kBT * kK * 2;                 // one operand's K-tile: 32 KB
+constexpr int kBTile = kBT * kRow * 2;                 // one operand's K-tile: 32 KB
 constexpr int kBPieces = kBTile / kBThreads / 16;    // 1 KB pieces per operand per wave: 4
 constexpr int kWTM = 64, kWTN = 128;
 constexpr int kTM = kWTM / 16, kTN = kWTN / 16;
@@ -187,27 +216,18 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
                                                             float* __restrict__ part) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   constexpr bool BK = OP != Op::Apply;  // the B operand is K-contiguous
-  const int bid = blockIdx.x;
-  int lid, slice = -1;
-  if (bid < plan.n_full) {
-    lid = xcd_remap(bid, plan.n_full);
-  } else {
-    const int j = xcd_remap(bid - plan.n_full, gridDim.x - plan.n_full);
-    lid = plan.n_full + j / plan.splits;
-    slice = j % plan.splits;
-  }
-  const int mi = mat_of(plan, t.count, lid);
-  const NsMat& x = t.mat[mi];
+  const Item it = item_of(plan, t.count, blockIdx.x, gridDim.x);
+  const NsMat& x = t.mat[plan.mat[it.place]];
   int tm, tn;
-  tile_at<OP, kBT>(x, lid - plan.first[mi], tm, tn);
+  tile_at<OP, kBT>(x, it.tile - plan.first[it.place], tm, tn);
   const int m0 = tm * kBT, n0 = tn * kBT, M = x.m, N = BK ? x.m : x.n;
-  const Operands o = operands<OP>(x, cur);
-  const int nk = o.K / kK, all = PLANES == 2 ? 3 * nk : nk;
-  int kt0 = 0, kt1 = all;
-  if (slice >= 0) {
-    const int chunk = (all + plan.splits - 1) / plan.splits;
-    kt0 = min(all, slice * chunk);
-    kt1 = min(all, kt0 + chunk);
+  const Operands o = operands<OP, PLANES>(x, cur);
+  const int nk = o.K / kK<PLANES>;
+  int kt0 = 0, kt1 = nk;
+  if (it.slice >= 0) {
+    const int chunk = (nk + plan.splits - 1) / plan.splits;
+    kt0 = min(nk, it.slice * chunk);
+    kt1 = min(nk, kt0 + chunk);
   }
   const int nt = kt1 - kt0;
 
@@ -230,21 +250,18 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
 #pragma unroll
     for (int i = 0; i < kBPieces; ++i) {
       const int p = (region(r) * kBPieces + i) * 1024 + 16 * lane;
-      aoff[r * kBPieces + i] = lane_off<true, kBT>(o.lda, M - m0, p);
-      boff[r * kBPieces + i] = lane_off<BK, kBT>(o.ldb, N - n0, p);
+      aoff[r * kBPieces + i] = lane_off<true, kBT, PLANES>(o.lda, M - m0, p);
+      boff[r * kBPieces + i] = lane_off<BK, kBT, PLANES>(o.ldb, N - n0, p);
     }
   const _Float16* abase = o.A + (size_t)m0 * o.lda;
-  const _Float16* bbase = BK ? o.B + (size_t)n0 * o.ldb : o.B + n0;
-  const size_t bstep = BK ? kK : (size_t)kK * o.ldb;
+  const _Float16* bbase = BK ? o.B + (size_t)n0 * o.ldb : o.B + (size_t)PLANES * n0;
+  const size_t bstep = BK ? kRow : (size_t)kK<PLANES> * o.ldb;  // values per K-tile
   // this wave's pieces of one operand of the item's K-tile t (half 0: A, half 1: B)
   auto issue_half = [&](int tt, int half) {
     if (!dma_wave) return;
-    const int s = tt & 1, at = kt0 + tt;
-    const int seg = PLANES == 2 ? (at >= nk) + (at >= 2 * nk) : 2;
-    const int kt = PLANES == 2 ? at - seg * nk : at;
-    const _Float16* src =
-        half == 0 ? abase + (size_t)kt * kK + (PLANES == 2 && seg == 0 ? o.plane_a : 0)
-                  : bbase + (size_t)kt * bstep + (PLANES == 2 && seg == 1 ? o.plane_b : 0);
+    const int s = tt & 1;
+    const _Float16* src = half == 0 ? abase + (size_t)(kt0 + tt) * kRow
+                                    : bbase + (size_t)(kt0 + tt) * bstep;
     const uint32_t dst0 = lds0 + (half == 0 ? a_off(s) : b_off(s));
 #pragma unroll
     for (int r = 0; r < kReg; ++r)
@@ -260,30 +277,57 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
 #pragma unroll
     for (int j = 0; j < kTN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  // Phase p (0..7) of a K-tile: k-step p / 4, N blocks 2 (p % 4) and the next, eight
-  // MFMAs; fragments are read kLook phases ahead (gemm.hip has the reasons).
-  constexpr int kPh = 8, kLook = 2;
+  // A K-tile is 8 (one plane) or 12 phases of eight MFMAs, a pair of N blocks times all
+  // M blocks of one fragment each; fragments are read kLook phases before the phase that
+  // first uses them (gemm.hip has the reasons).
+  //   one plane:  phase p takes k-step p / 4 and pair p % 4;
+  //   two planes: l h of pairs 0 and 1, h h of both, h l of both, then the same of
+  //               pairs 2 and 3: the values of A are first used in phase 2, so they
+  //               are read in phase 0, when the last K-tile's are dead.
+  constexpr int kPh = PLANES == 2 ? 12 : 8, kLook = 2;
   f16x8 fa[2][kTM], fb[2][kTN];
+  auto use = [](int p, int& af, int& bf, int& pair) {
+    if (PLANES == 1) {
+      af = bf = p >> 2;
+      pair = p & 3;
+    } else {
+      const int q = p % 6;
+      af = q < 2;
+      bf = q >= 4;
+      pair = 2 * (p / 6) + (p & 1);
+    }
+  };
+  // the reads for phase p, of the item's K-tile tt: what no earlier phase has read
+  auto reads_a = [](int p) { return PLANES == 1 ? (p & 3) == 0 : p == 0 || p == 2; };
+  auto reads_b = [](int p) { return PLANES == 1 || p % 6 < 2 || p % 6 >= 4; };
   auto read_frags = [&](int tt, int p) {
-    const int st = tt & 1, ks = p >> 2, r = p & 3;
+    const int st = tt & 1;
     const unsigned char* pa = smem + a_off(st);
     const unsigned char* pb = smem + b_off(st);
-    if (r == 0) {
+    int af, bf, pair;
+    use(p, af, bf, pair);
+    if (reads_a(p)) {
 #pragma unroll
-      for (int i = 0; i < kTM; ++i) fa[ks][i] = frag<true, kBT>(pa, wm + 16 * i, ks, lane);
+      for (int i = 0; i < kTM; ++i) fa[af][i] = frag<true, kBT, PLANES>(pa, wm + 16 * i, af, lane);
     }
+    if (reads_b(p)) {
 #pragma unroll
-    for (int j = 2 * r; j < 2 * r + 2; ++j) fb[ks][j] = frag<BK, kBT>(pb, wn + 16 * j, ks, lane);
+      for (int j = 2 * pair; j < 2 * pair + 2; ++j)
+        fb[bf][j] = frag<BK, kBT, PLANES>(pb, wn + 16 * j, bf, lane);
+    }
   };
   auto mma = [&](auto P) {
-    constexpr int p = decltype(P)::value, ks = p >> 2, j0 = 2 * (p & 3);
+    constexpr int p = decltype(P)::value;
+    int af, bf, pair;
+    use(p, af, bf, pair);
 #pragma unroll
     for (int i = 0; i < kTM; ++i)
 #pragma unroll
-      for (int j = j0; j < j0 + 2; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[ks][j], fa[ks][i], acc[i][j], 0, 0, 0);
+      for (int j = 2 * pair; j < 2 * pair + 2; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[bf][j], fa[af][i], acc[i][j], 0, 0, 0);
+    // one MFMA and one LDS read (a transposed fragment takes two) in turn
     constexpr int pn = (p + kLook) % kPh;
-    constexpr int kReads = ((pn & 3) == 0 ? kTM : 0) + (BK ? 1 : 2) * 2;
+    constexpr int kReads = (reads_a(pn) ? kTM : 0) + (reads_b(pn) ? (BK ? 1 : 2) * 2 : 0);
     constexpr int kMfma = kTM * 2;
     constexpr int pairs = kReads < kMfma ? kReads : kMfma;
 #pragma unroll
@@ -297,6 +341,7 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
   auto phase = [&](int tt, auto P) {
     constexpr int p = decltype(P)::value;
     if constexpr (p == kPh - kLook) {
+      // every wave has read K-tile tt, and tt + 1 has landed
       wait_dma<0>();
       block_barrier();
       if (tt + 2 < nt) issue_half(tt + 2, 0);
@@ -327,6 +372,12 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
     phase(tt, std::integral_constant<int, 5>{});
     phase(tt, std::integral_constant<int, 6>{});
     phase(tt, std::integral_constant<int, 7>{});
+    if constexpr (PLANES == 2) {
+      phase(tt, std::integral_constant<int, 8>{});
+      phase(tt, std::integral_constant<int, 9>{});
+      phase(tt, std::integral_constant<int, 10>{});
+      phase(tt, std::integral_constant<int, 11>{});
+    }
   }
   block_barrier();  // every wave is done with the main loop's LDS
 
@@ -336,8 +387,9 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
   unsigned char* buf = smem + wave * kEpiLds;
   const int c = lane & 31, hi = lane >> 5;
   const int n = n0 + wn + 4 * c;
-  float* pt = slice < 0 ? nullptr
-                        : part + ((size_t)(lid - plan.n_full) * plan.splits + slice) * (kBT * kBT);
+  float* pt = it.slice < 0 ? nullptr
+                           : part + ((size_t)(it.tile - plan.n_full) * plan.splits + it.slice) *
+                                        (kBT * kBT);
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
 #pragma unroll
@@ -377,7 +429,7 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
           v[e] = *reinterpret_cast<const float*>(buf + (r8 + e) * (kWTN * 4) +
                                                  (((cc >> 2) ^ (r8 + e)) & 31) * 16 + (cc & 3) * 4);
         if (row < N && mm < M)
-          ns_store8<PLANES>(out + (size_t)row * x.m + mm, (size_t)x.m * x.m, v, 1.0f);
+          ns_store<PLANES, 8>(out + ns_at<PLANES>(x.m, row, mm), v, 1.0f);
       }
     }
   }
@@ -390,10 +442,10 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(NsTable t, NsPlan plan, 
                                                         const float* __restrict__ part) {
   __shared__ float lds[64][65];
   const int tail = blockIdx.x >> 4, sub = blockIdx.x & 15, lid = plan.n_full + tail;
-  const int mi = mat_of(plan, t.count, lid);
-  const NsMat& x = t.mat[mi];
+  const int place = place_of(plan, t.count, lid);
+  const NsMat& x = t.mat[plan.mat[place]];
   int tm, tn;
-  tile_at<OP, kBT>(x, lid - plan.first[mi], tm, tn);
+  tile_at<OP, kBT>(x, lid - plan.first[place], tm, tn);
   const int r0 = (sub >> 2) * 64, c0 = (sub & 3) * 64, cl = 4 * (threadIdx.x & 15);
   const int N = OP == Op::Apply ? x.n : x.m;
   // (M and N are multiples of 64: the 64 x 64 block is inside or outside whole)
@@ -421,8 +473,7 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(NsTable t, NsPlan plan, 
       float v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = lds[r8 + e][cc];
-      ns_store8<PLANES>(out + (size_t)(tn * kBT + c0 + cc) * x.m + tm * kBT + r0 + r8,
-                        (size_t)x.m * x.m, v, 1.0f);
+      ns_store<PLANES, 8>(out + ns_at<PLANES>(x.m, tn * kBT + c0 + cc, tm * kBT + r0 + r8), v, 1.0f);
     }
   }
 }
@@ -431,7 +482,7 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(NsTable t, NsPlan plan, 
 constexpr int kT = 128;
 constexpr int kWaves = 4;  // 2 x 2, each 64 x 64
 constexpr int kThreads = 64 * kWaves;
-constexpr int kOpBytes = kT * kK * 2;                // one operand's K-tile: 16 KB
+constexpr int kOpBytes = kT * kRow * 2;                // one operand's K-tile: 16 KB
 constexpr int kPieces = kOpBytes / (1024 * kWaves);  // 1 KB DMA pieces per wave
 constexpr int kRowF = kT + 4;                        // floats per row of the staged output
 
@@ -440,13 +491,12 @@ __global__ __launch_bounds__(kThreads, 2) void ns_gemm_kernel(NsTable t, NsPlan 
   __shared__ __attribute__((aligned(1024))) unsigned char smem[kT * kRowF * 4];
   static_assert(4 * kOpBytes <= kT * kRowF * 4, "two stages of two operands");
   constexpr bool BK = OP != Op::Apply;
-  const int lid = xcd_remap(blockIdx.x, gridDim.x);
-  const int mi = mat_of(plan, t.count, lid);
-  const NsMat& x = t.mat[mi];
+  const Item it = item_of(plan, t.count, blockIdx.x, gridDim.x);
+  const NsMat& x = t.mat[plan.mat[it.place]];
   int tm, tn;
-  tile_at<OP, kT>(x, lid - plan.first[mi], tm, tn);
+  tile_at<OP, kT>(x, it.tile - plan.first[it.place], tm, tn);
   const int m0 = tm * kT, n0 = tn * kT, M = x.m, N = BK ? x.m : x.n;
-  const Operands o = operands<OP>(x, cur);
+  const Operands o = operands<OP, PLANES>(x, cur);
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -456,18 +506,16 @@ __global__ __launch_bounds__(kThreads, 2) void ns_gemm_kernel(NsTable t, NsPlan 
 #pragma unroll
   for (int i = 0; i < kPieces; ++i) {
     const int p = (wave * kPieces + i) * 1024 + 16 * lane;
-    aoff[i] = lane_off<true, kT>(o.lda, M - m0, p);
-    boff[i] = lane_off<BK, kT>(o.ldb, N - n0, p);
+    aoff[i] = lane_off<true, kT, PLANES>(o.lda, M - m0, p);
+    boff[i] = lane_off<BK, kT, PLANES>(o.ldb, N - n0, p);
   }
   const _Float16* abase = o.A + (size_t)m0 * o.lda;
-  const _Float16* bbase = BK ? o.B + (size_t)n0 * o.ldb : o.B + n0;
-  const size_t bstep = BK ? kK : (size_t)kK * o.ldb;
-  const int nk = o.K / kK, nt = PLANES == 2 ? 3 * nk : nk;
+  const _Float16* bbase = BK ? o.B + (size_t)n0 * o.ldb : o.B + (size_t)PLANES * n0;
+  const size_t bstep = BK ? kRow : (size_t)kK<PLANES> * o.ldb;  // values per K-tile
+  const int nt = o.K / kK<PLANES>;
   auto issue = [&](int tt) {
-    const int seg = PLANES == 2 ? (tt >= nk) + (tt >= 2 * nk) : 2;
-    const int kt = PLANES == 2 ? tt - seg * nk : tt;
-    const _Float16* a = abase + (size_t)kt * kK + (PLANES == 2 && seg == 0 ? o.plane_a : 0);
-    const _Float16* b = bbase + kt * bstep + (PLANES == 2 && seg == 1 ? o.plane_b : 0);
+    const _Float16* a = abase + (size_t)tt * kRow;
+    const _Float16* b = bbase + (size_t)tt * bstep;
     const uint32_t at = lds0 + (tt & 1) * 2 * kOpBytes + wave * kPieces * 1024;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
@@ -489,19 +537,24 @@ __global__ __launch_bounds__(kThreads, 2) void ns_gemm_kernel(NsTable t, NsPlan 
     if (tt + 1 < nt) issue(tt + 1);
     const unsigned char* pa = smem + (tt & 1) * 2 * kOpBytes;
     const unsigned char* pb = pa + kOpBytes;
+    f16x8 fa[2][4], fb[2][4];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      f16x8 fa[4], fb[4];
+    for (int f = 0; f < 2; ++f) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) fa[i] = frag<true, kT>(pa, wm + 16 * i, s, lane);
+      for (int i = 0; i < 4; ++i) fa[f][i] = frag<true, kT, PLANES>(pa, wm + 16 * i, f, lane);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) fb[j] = frag<BK, kT>(pb, wn + 16 * j, s, lane);
+      for (int j = 0; j < 4; ++j) fb[f][j] = frag<BK, kT, PLANES>(pb, wn + 16 * j, f, lane);
+    }
+    auto mma = [&](int af, int bf) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[j], fa[i], acc[i][j], 0, 0, 0);
-    }
+          acc[i][j] =
+              __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[bf][j], fa[af][i], acc[i][j], 0, 0, 0);
+    };
+    if constexpr (PLANES == 2) mma(1, 0), mma(0, 0), mma(0, 1);
+    else mma(0, 0), mma(1, 1);
   }
   __syncthreads();
 
@@ -538,7 +591,7 @@ __global__ __launch_bounds__(kThreads, 2) void ns_gemm_kernel(NsTable t, NsPlan 
       float v[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = stage[(r4 + e) * kRowF + cc];
-      ns_store4<PLANES>(out + (size_t)(n0 + cc) * M + m0 + r4, (size_t)M * M, v, 1.0f);
+      ns_store<PLANES, 4>(out + ns_at<PLANES>(M, n0 + cc, m0 + r4), v, 1.0f);
     }
   }
 }
@@ -549,38 +602,75 @@ int tiles_of(Op op, const NsMat& x, int t) {
   return op == Op::Apply ? tm * tn : tm * (tm + 1) / 2;
 }
 
-// Whether the 256 x 256 tiles fill the chip, and how: whole rounds of tiles, and the
-// tiles of the last, partial round cut along K so that they end together.
+// Time of a K-tile of a 256 x 256 tile with the chip full, and around a tile (launch,
+// prologue, epilogue), in us.
+template <int PLANES>
+constexpr double kStepUs = PLANES == 2 ? 1.9 : 1.65;
+constexpr double kTileUs = 12.0;
+
 struct Choice {
-  bool big;
+  bool big;  // 256 x 256 tiles
   NsPlan plan;
-  int tail;
+  int tail;  // tiles cut along K
 };
-Choice choose(Op op, const NsTable& t, int planes) {
+
+// Whole rounds of 256 x 256 tiles, and the tiles of the last, partial round (or of all,
+// where they do not fill one) cut along K where that is estimated to end sooner.
+template <int PLANES>
+Choice choose(Op op, const NsTable& t) {
   Choice c{};
-  long long work = 0;  // K-tiles
-  for (int i = 0; i < t.count; ++i) {
-    const int n = tiles_of(op, t.mat[i], kBT);
-    c.plan.first[i + 1] = c.plan.first[i] + n;
-    work += (long long)n * planes * (op == Op::Gram ? t.mat[i].n : t.mat[i].m) / kK;
+  auto len = [&](int i) { return (op == Op::Gram ? t.mat[i].n : t.mat[i].m) / kK<PLANES>; };
+  for (int i = 0; i < t.count; ++i) {  // the longest K first
+    int k = i;
+    for (; k > 0 && len(c.plan.mat[k - 1]) < len(i); --k) c.plan.mat[k] = c.plan.mat[k - 1];
+    c.plan.mat[k] = i;
   }
-  const int tiles = c.plan.first[t.count];
-  c.big = tiles >= 128;
-  if (!c.big) {
+  auto count = [&](int size) {
     for (int i = 0; i < t.count; ++i)
-      c.plan.first[i + 1] = c.plan.first[i] + tiles_of(op, t.mat[i], kT);
-    c.plan.n_full = c.plan.first[t.count];
-    c.plan.splits = 1;
-    return c;
-  }
+      c.plan.first[i + 1] = c.plan.first[i] + tiles_of(op, t.mat[c.plan.mat[i]], size);
+    return c.plan.first[t.count];
+  };
+  const int tiles = count(kBT);
+  // K-tiles until the last item ends, the items (longest first) taken in rounds of kCUs
+  auto rounds = [&](int n_full, int splits) {
+    long long steps = 0, next = 0, at = 0;
+    for (int i = 0; i < t.count; ++i) {
+      const int nk = len(c.plan.mat[i]), cut = (nk + splits - 1) / splits;
+      const int whole = std::max(0, std::min(c.plan.first[i + 1], n_full) - c.plan.first[i]);
+      const int rest = c.plan.first[i + 1] - c.plan.first[i] - whole;
+      for (const auto& [n, l] : {std::pair<long long, int>{whole, nk}, {(long long)rest * splits, cut}}) {
+        // items at .. at + n - 1; a round starts at each multiple of kCUs
+        if (n <= 0) continue;
+        const long long starts = next >= at + n ? 0 : (at + n - 1 - next) / kCUs + 1;
+        steps += starts * l;
+        next += starts * kCUs;
+        at += n;
+      }
+    }
+    return (double)steps;
+  };
+  double best = kTileUs + kStepUs<PLANES> * rounds(tiles, 1);
   c.plan.n_full = tiles;
   c.plan.splits = 1;
+  for (int keep = tiles / kCUs; keep >= std::max(0, tiles / kCUs - 1); --keep) {
+    const int tail = tiles - keep * kCUs;
+    for (int s = 2; tail > 0 && s <= 16 && (long long)tail * s <= 4 * kCUs; ++s) {
+      const double us = kTileUs + kStepUs<PLANES> * rounds(keep * kCUs, s) + 6.0 + 0.1 * tail * s;
+      if (us < best) best = us, c.plan.n_full = keep * kCUs, c.plan.splits = s, c.tail = tail;
+    }
+  }
+  c.big = tiles >= 64;
+  if (!c.big) {
+    c.plan.n_full = count(kT);
+    c.plan.splits = 1;
+    c.tail = 0;
+  }
   return c;
 }
 
 template <Op OP, int PLANES>
 void launch(const NsTable& t, int cur, float* part, hipStream_t s) {
-  const Choice c = choose(OP, t, PLANES);
+  const Choice c = choose<PLANES>(OP, t);
   if (c.big) {
     ns_gemm_big<OP, PLANES>
         <<<c.plan.n_full + c.tail * c.plan.splits, kBThreads, kBLds, s>>>(t, c.plan, cur, part);
@@ -597,11 +687,25 @@ void step(const NsTable& t, int cur, float* part, hipStream_t s) {
   launch<Op::Apply, PLANES>(t, cur, part, s);
 }
 
+template <int PLANES>
+size_t partial_tiles(const NsTable& t) {
+  size_t n = 0;
+  for (Op op : {Op::Gram, Op::Square, Op::Apply}) {
+    const Choice c = choose<PLANES>(op, t);
+    n = std::max(n, (size_t)c.tail * c.plan.splits);
+  }
+  return n;
+}
+
 }  // namespace
 
-void launch_ns_step(const NsTable& t, int planes, int cur, hipStream_t s) {
-  if (planes == 2) step<2>(t, cur, nullptr, s);
-  else step<1>(t, cur, nullptr, s);
+size_t ns_partial_floats(const NsTable& t, int planes) {
+  return (planes == 2 ? partial_tiles<2>(t) : partial_tiles<1>(t)) * (kBT * kBT);
+}
+
+void launch_ns_step(const NsTable& t, int planes, int cur, float* part, hipStream_t s) {
+  if (planes == 2) step<2>(t, cur, part, s);
+  else step<1>(t, cur, part, s);
 }
 
 }  // namespace pb

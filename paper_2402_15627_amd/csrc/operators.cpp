@@ -168,9 +168,9 @@ pb_status check_rms(const pb_rmsnorm_config* c) {
 // ------------------------------------------------------------- Muon step
 static_assert(PB_MUON_MAX_TENSORS == pb::kNsMaxTensors, "tensor limit");
 
-// Workspace: partial sums, norms, then each matrix's planes.
+// Workspace: partial sums, norms, each matrix's planes, the products' K-slices.
 struct NsLayout {
-  size_t partial, norm, planes;  // offsets; planes: of the first matrix
+  size_t partial, norm, part;  // offsets
   size_t total;
 };
 
@@ -201,8 +201,7 @@ bool ns_add(pb::NsTable& t, int rows, int cols) {
 NsLayout ns_layout(pb::NsTable& t, int planes, char* base) {
   NsLayout L{};
   L.norm = align256((size_t)t.tile0[t.count] * sizeof(double));
-  L.planes = L.norm + align256((size_t)t.count * sizeof(double));
-  size_t o = L.planes;
+  size_t o = L.norm + align256((size_t)t.count * sizeof(double));
   for (int i = 0; i < t.count; ++i) {
     pb::NsMat& x = t.mat[i];
     const size_t big = align256((size_t)planes * x.m * x.n * 2);
@@ -213,7 +212,8 @@ NsLayout ns_layout(pb::NsTable& t, int planes, char* base) {
     x.b = (_Float16*)(base + o + 2 * big + small);
     o += 2 * big + 2 * small;
   }
-  L.total = t.count ? o : 0;
+  L.part = o;
+  L.total = t.count ? o + align256(pb::ns_partial_floats(t, planes) * sizeof(float)) : 0;
   return L;
 }
 
@@ -248,7 +248,7 @@ void ns_launch(pb::NsTable& t, const pb::NsScalars& sc, pb::NsMode mode, pb::Dt 
                hipStream_t stream) {
   const NsLayout L = ns_layout(t, sc.planes, ws);
   pb::launch_newton_schulz(t, sc, mode, copy_dt, (double*)(ws + L.partial), (double*)(ws + L.norm),
-                           stream);
+                           (float*)(ws + L.part), stream);
 }
 
 }  // namespace
