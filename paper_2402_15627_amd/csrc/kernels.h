@@ -137,6 +137,7 @@ struct NsMat {
   long long ld_src, ld_out;
   _Float16 *x[2], *a, *b;
   int rows, cols, m, n;  // of the tensor; of X, padded
+  int ldm, ldn;          // values from row to row of a and b, and of x (one plane's)
   float decay, scale;
 };
 struct NsTable {

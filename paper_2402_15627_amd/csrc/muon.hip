@@ -12,7 +12,8 @@
 //   2. norm:   1 / (||U||_F + eps) of each matrix
 //   3. init:   X's fp16 planes, padded to multiples of 64 with zeros
 //   4. the products (ns_gemm.hip), three launches a step for all matrices at once
-//   5. apply:  w, and its copy; or the orthogonalised matrix itself
+//   5. finish: w and its copy, or the orthogonalised matrix itself; part of the last
+//      product where that runs in small tiles
 //
 // 1, 3 and 5 are HBM-bound: a 64 x 64 tile per workgroup, 256 contiguous bytes of
 // a row per 16 lanes; a tall matrix's tile is transposed through LDS.
@@ -116,19 +117,28 @@ __global__ __launch_bounds__(kThreads) void ns_update_kernel(NsTable t, NsScalar
 }
 
 // norm[i] = 1 / (||U|| + eps) of matrix i.
-__global__ __launch_bounds__(kThreads) void ns_norm_kernel(NsTable t, float eps,
-                                                           const double* __restrict__ partial,
-                                                           double* __restrict__ norm) {
-  __shared__ double red[kThreads / 64];
-  const int i = blockIdx.x;
-  double ss = 0.0;
-  for (int k = t.tile0[i] + threadIdx.x; k < t.tile0[i + 1]; k += kThreads) ss += partial[k];
+constexpr int kNormThreads = 1024;
+__global__ __launch_bounds__(kNormThreads) void ns_norm_kernel(NsTable t, float eps,
+                                                               const double* __restrict__ partial,
+                                                               double* __restrict__ norm) {
+  __shared__ double red[kNormThreads / 64];
+  const int i = blockIdx.x, end = t.tile0[i + 1];
+  double s[4] = {0.0, 0.0, 0.0, 0.0};  // (four loads in flight)
+  for (int k = t.tile0[i] + threadIdx.x; k < end; k += 4 * kNormThreads)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const double v = partial[min(k + e * kNormThreads, end - 1)];
+      s[e] += k + e * kNormThreads < end ? v : 0.0;
+    }
+  double ss = (s[0] + s[1]) + (s[2] + s[3]);
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) ss += __shfl_xor(ss, o, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
   __syncthreads();
-  if (threadIdx.x == 0)
-    norm[i] = 1.0 / (sqrt((red[0] + red[1]) + (red[2] + red[3])) + (double)eps);
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kNormThreads / 64; ++w) ss += red[w];
+    norm[i] = 1.0 / (sqrt(ss) + (double)eps);
+  }
 }
 
 // X's tile of 64 x 64 at (i0, j0) of its padded m x n from U's tile of the tensor.
@@ -175,14 +185,14 @@ __global__ __launch_bounds__(kThreads) void ns_init_kernel(NsTable t, NsScalars 
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = lds[i][j + e];
-    ns_store<PLANES, 8>(x.x[0] + ns_at<PLANES>(x.n, i0 + i, j0 + j), v, kNsScaleX);
+    ns_store<PLANES, 8>(x.x[0] + ns_at<PLANES>(x.ldn, i0 + i, j0 + j), v, kNsScaleX);
   }
 }
 
-// From the last iterate, in planes of x[last]: the weights' step and their copy, or
-// the matrix itself.
-template <NsMode MODE, int PLANES, typename CT>
-__global__ __launch_bounds__(kThreads) void ns_apply_kernel(NsTable t, NsScalars sc, int last) {
+// The tensors from the last iterate, in x[last], where the last product has not
+// written them.
+template <int PLANES>
+__global__ __launch_bounds__(kThreads) void ns_finish_kernel(NsTable t, NsFinish fin, int last) {
   __shared__ float lds[kTile][kTile + 1];
   const TileAt at = tile_at(t);
   const NsMat& x = t.mat[at.i];
@@ -192,7 +202,7 @@ __global__ __launch_bounds__(kThreads) void ns_apply_kernel(NsTable t, NsScalars
   for (int k = 0; k < 2; ++k) {
     const int i = (threadIdx.x >> 3) + 32 * k, j = 8 * (threadIdx.x & 7);
     float v[8];
-    ns_load<PLANES, 8>(x.x[last] + ns_at<PLANES>(x.n, i0 + i, j0 + j), v, 1.0f / kNsScaleX);
+    ns_load<PLANES, 8>(x.x[last] + ns_at<PLANES>(x.ldn, i0 + i, j0 + j), v, 1.0f / kNsScaleX);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       if (tall) lds[j + e][i] = v[e];
@@ -200,28 +210,14 @@ __global__ __launch_bounds__(kThreads) void ns_apply_kernel(NsTable t, NsScalars
     }
   }
   __syncthreads();
-  const int cl = 4 * (threadIdx.x & 15), c = at.c0 + cl, left = x.cols - c;
-  if (left <= 0) return;
+  const int cl = 4 * (threadIdx.x & 15);
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const int rl = (threadIdx.x >> 4) + 16 * k, r = at.r0 + rl;
-    if (r >= x.rows) continue;
+    const int rl = (threadIdx.x >> 4) + 16 * k;
     float v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = lds[rl][cl + e];
-    if constexpr (MODE == NsMode::Muon) {
-      const bool vec = rows_vec<float>(x.w, x.ld_src);
-      float w[4];
-      load4_cols(x.w + r * x.ld_src, c, left, vec, w);
-      const float keep = 1.0f - sc.lr * x.decay, step = sc.lr * x.scale;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = __builtin_fmaf(-step, v[e], w[e] * keep);
-      store4_cols(x.w + r * x.ld_src, c, left, vec, w);
-      if (x.copy)
-        store4_cols((CT*)x.copy + r * x.ld_src, c, left, rows_vec<CT>(x.copy, x.ld_src), w);
-    } else {
-      store4_cols((CT*)x.out + r * x.ld_out, c, left, rows_vec<CT>(x.out, x.ld_out), v);
-    }
+    finish<4>(x, fin, at.r0 + rl, at.c0 + cl, v);
   }
 }
 
@@ -230,14 +226,12 @@ void run(const NsTable& t, const NsScalars& sc, Dt copy_dt, double* partial, dou
          float* part, hipStream_t s) {
   const int tiles = t.tile0[t.count];
   ns_update_kernel<MODE><<<tiles, kThreads, 0, s>>>(t, sc, partial);
-  ns_norm_kernel<<<t.count, kThreads, 0, s>>>(t, sc.eps, partial, norm);
+  ns_norm_kernel<<<t.count, kNormThreads, 0, s>>>(t, sc.eps, partial, norm);
   ns_init_kernel<MODE, PLANES><<<tiles, kThreads, 0, s>>>(t, sc, norm);
-  for (int k = 0; k < sc.steps; ++k) launch_ns_step(t, PLANES, k & 1, part, s);
-  const int last = sc.steps & 1;
-  if (MODE == NsMode::Bf16 || (MODE == NsMode::Muon && copy_dt == Dt::BF16))
-    ns_apply_kernel<MODE, PLANES, bf16><<<tiles, kThreads, 0, s>>>(t, sc, last);
-  else
-    ns_apply_kernel<MODE, PLANES, float><<<tiles, kThreads, 0, s>>>(t, sc, last);
+  const bool bf16_out = MODE == NsMode::Bf16 || (MODE == NsMode::Muon && copy_dt == Dt::BF16);
+  const NsFinish fin{MODE, bf16_out, sc.lr};
+  if (!launch_ns_products(t, fin, PLANES, sc.steps, part, s))
+    ns_finish_kernel<PLANES><<<tiles, kThreads, 0, s>>>(t, fin, sc.steps & 1);
 }
 
 }  // namespace

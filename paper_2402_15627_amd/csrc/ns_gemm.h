@@ -54,8 +54,59 @@ PB_DEV void ns_load(const _Float16* p, float* v, float scale) {
   for (int e = 0; e < N; ++e) v[e] = ((float)hi[e] + (float)lo[e]) * scale;
 }
 
-// One Newton-Schulz step of every matrix: x[cur] -> x[cur ^ 1].  part: room for
-// ns_partial_floats(t, planes) floats.
-void launch_ns_step(const NsTable& t, int planes, int cur, float* part, hipStream_t s);
+// What becomes of the last X: the weights' step (Muon; bf16_out: the type of the
+// copies), or the matrix itself in its type.
+struct NsFinish {
+  NsMode mode;
+  bool bf16_out;
+  float lr;
+};
+// N elements of row r of a tensor from column c on, X's values there: the weights'
+// step and their copy, or the orthogonalised matrix.  Past the row's end, nothing.
+template <int N, typename T>
+PB_DEV void put(T* p, int left, const float* v) {
+  if (left >= N && (uintptr_t)p % (N * sizeof(T) < 16 ? N * sizeof(T) : 16) == 0) {
+#pragma unroll
+    for (int e = 0; e < N; e += 4) store4<T>(p + e, v + e);
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (e < left) p[e] = (T)v[e];
+  }
+}
+template <int N>
+PB_DEV void finish(const NsMat& x, const NsFinish& f, int r, int c, const float* v) {
+  const int left = x.cols - c;
+  if (r >= x.rows || left <= 0) return;
+  if (f.mode == NsMode::Muon) {
+    float* w = x.w + r * x.ld_src + c;
+    const float keep = 1.0f - f.lr * x.decay, step = f.lr * x.scale;
+    float u[N];
+    if (left >= N && (uintptr_t)w % 16 == 0) {
+#pragma unroll
+      for (int e = 0; e < N; e += 4) load4<float>(w + e, u + e);
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) u[e] = e < left ? w[e] : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) u[e] = __builtin_fmaf(-step, v[e], u[e] * keep);
+    put<N>(w, left, u);
+    if (x.copy) {
+      if (f.bf16_out) put<N>((bf16*)x.copy + r * x.ld_src + c, left, u);
+      else put<N>((float*)x.copy + r * x.ld_src + c, left, u);
+    }
+  } else if (f.bf16_out) {
+    put<N>((bf16*)x.out + r * x.ld_out + c, left, v);
+  } else {
+    put<N>((float*)x.out + r * x.ld_out + c, left, v);
+  }
+}
+
+// `steps` Newton-Schulz steps of every matrix from x[0] on.  part: room for
+// ns_partial_floats(t, planes) floats.  True where the last product has finished the
+// tensors; else X is in x[steps & 1].
+bool launch_ns_products(const NsTable& t, const NsFinish& fin, int planes, int steps, float* part,
+                        hipStream_t s);
 
 }  // namespace pb

@@ -4,6 +4,10 @@
 //                                      written to its mirror image too
 //   square  B = a I + b A + c A A      symmetric likewise
 //   apply   X' = B X
+//   last    the last step's apply in 64 x 64 tiles: its result goes to the weights (or
+//           to the caller's matrix) from the fp32 sums, which saves a launch.  (In the
+//           256 x 256 tiles, where all CUs then write at once, it took 0.9 ms of a 4.3
+//           ms launch over the 175B share, and the pass of its own takes 0.7.)
 //
 // MFMA v_mfma_f32_16x16x32_f16 on the planes of ns_gemm.h, fp32 accumulation.  One
 // plane: one product of fp16 values (rounded by 2^-11 at most).  Two planes (value h
@@ -17,7 +21,7 @@
 // Two kernels:
 //   - 256 x 256 tiles, eight waves, as the projection GEMMs' LDS-DMA kernel has them
 //     (gemm.hip: fragments read two phases ahead, one barrier a K-tile);
-//   - 128 x 128 tiles, four waves, for grids too small for the first.
+//   - 64 x 64 tiles with K split over the waves of a workgroup, for small grids.
 // X, A and B are padded to multiples of 64 with zeros, so a K-tile is never partial;
 // rows and columns past the end of a tile read the last ones and are not stored.
 #include <algorithm>
@@ -33,7 +37,8 @@ namespace {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 #define PB_LDS __attribute__((address_space(3)))
 
-enum class Op { Gram, Square, Apply };
+enum class Op { Gram, Square, Apply, Last };
+constexpr bool symmetric(Op op) { return op == Op::Gram || op == Op::Square; }
 
 constexpr int kRow = 64;  // fp16 values of a K-contiguous row of a K-tile: 128 bytes
 template <int PLANES>
@@ -45,11 +50,18 @@ template <Op OP>
 constexpr float out_scale() {
   return OP == Op::Gram     ? kNsScaleA / (kNsScaleX * kNsScaleX)
          : OP == Op::Square ? kNsC * kNsScaleB / (kNsScaleA * kNsScaleA)
-                            : 1.0f / kNsScaleB;
+         : OP == Op::Apply  ? 1.0f / kNsScaleB
+                            : 1.0f / (kNsScaleB * kNsScaleX);
 }
 
 PB_DEV int swz(int row, int c) { return c ^ ((row ^ (row >> 3)) & 7); }
-PB_DEV int swz_mn(int k, int c) { return c ^ (4 * (k & 3)) ^ (2 * ((k >> 3) & 1)); }
+// Rows of W bytes: the four rows of a transposing read, and row groups 8 apart, lie in
+// distinct parts of the 256-byte bank period.
+template <int W>
+PB_DEV int swz_mn(int k, int c) {
+  return W >= 256 ? c ^ (4 * (k & 3)) ^ (2 * ((k >> 3) & 1))
+                  : c ^ (4 * ((k >> 1) & 1)) ^ (2 * ((k >> 3) & 1));
+}
 
 // Byte offset from the operand tile's first element of this lane's 16 bytes of the LDS
 // position p, for rows of ld values (both planes counted).  KC: rows of the operand are
@@ -62,7 +74,7 @@ PB_DEV uint32_t lane_off(int ld, int rows, int p) {
     return ((uint32_t)min(row, rows - 1) * (uint32_t)ld + 8 * c) * 2u;
   } else {
     constexpr int kChunks = T * PLANES / 8;  // 16-byte chunks of a k-row
-    const int k = p / (16 * kChunks), c = swz_mn(k, (p >> 4) & (kChunks - 1));
+    const int k = p / (16 * kChunks), c = swz_mn<16 * kChunks>(k, (p >> 4) & (kChunks - 1));
     return ((uint32_t)k * (uint32_t)ld + min(8 * c, PLANES * rows - 8)) * 2u;
   }
 }
@@ -77,11 +89,12 @@ PB_DEV f16x8 frag(const unsigned char* tile, int base, int f, int lane) {
     const int i = lane & 15, mn = base + 4 * (i & 3);
     const int k1 = (PLANES == 1 ? 32 * f : 0) + 8 * (lane >> 4) + (i >> 2), k2 = k1 + 4;
     const int c = PLANES == 1 ? mn >> 3 : 8 * (mn >> 5) + 4 * f + ((mn & 31) >> 3);
+    constexpr int W = 2 * T * PLANES;  // bytes of a k-row
     const int off = (mn & 7) * 2;
     const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (PB_LDS s16x4*)(tile + k1 * (2 * T * PLANES) + swz_mn(k1, c) * 16 + off));
+        (PB_LDS s16x4*)(tile + k1 * W + swz_mn<W>(k1, c) * 16 + off));
     const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (PB_LDS s16x4*)(tile + k2 * (2 * T * PLANES) + swz_mn(k2, c) * 16 + off));
+        (PB_LDS s16x4*)(tile + k2 * W + swz_mn<W>(k2, c) * 16 + off));
     const f16x4 a4 = __builtin_bit_cast(f16x4, a), b4 = __builtin_bit_cast(f16x4, b);
     return f16x8{a4[0], a4[1], a4[2], a4[3], b4[0], b4[1], b4[2], b4[3]};
   }
@@ -126,8 +139,8 @@ PB_DEV void triangle_tile(int id, int t, int& tm, int& tn) {
 template <Op OP, int T>
 PB_DEV void tile_at(const NsMat& x, int id, int& tm, int& tn) {
   const int t = (x.m + T - 1) / T;
-  if constexpr (OP == Op::Apply) tile_of<4>(id, t, (x.n + T - 1) / T, tm, tn);
-  else triangle_tile(id, t, tm, tn);
+  if constexpr (symmetric(OP)) triangle_tile(id, t, tm, tn);
+  else tile_of<4>(id, t, (x.n + T - 1) / T, tm, tn);
 }
 
 PB_DEV int place_of(const NsPlan& p, int count, int tile) {
@@ -167,29 +180,35 @@ struct Operands {
 };
 template <Op OP, int PLANES>
 PB_DEV Operands operands(const NsMat& x, int cur) {
-  const int m = PLANES * x.m, n = PLANES * x.n;
+  const int m = PLANES * x.ldm, n = PLANES * x.ldn;
   if constexpr (OP == Op::Gram) return {x.x[cur], x.x[cur], n, n, x.n};
   else if constexpr (OP == Op::Square) return {x.a, x.a, m, m, x.m};
   else return {x.b, x.x[cur], m, n, x.m};
 }
 
-// Four consecutive columns n.. of row m of the result, v: the sums (scaled in place).
+// Four consecutive columns n.. of row m of a product, v: the sums (scaled in place).
 template <Op OP, int PLANES>
 PB_DEV void store_result4(const NsMat& x, int cur, int m, int n, float* v) {
   constexpr float kOut = out_scale<OP>();
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] *= kOut;
   if constexpr (OP == Op::Gram) {
-    ns_store<PLANES, 4>(x.a + ns_at<PLANES>(x.m, m, n), v, 1.0f);
+    ns_store<PLANES, 4>(x.a + ns_at<PLANES>(x.ldm, m, n), v, 1.0f);
   } else if constexpr (OP == Op::Square) {
     float a4[4];
-    ns_load<PLANES, 4>(x.a + ns_at<PLANES>(x.m, m, n), a4, kNsB * kNsScaleB / kNsScaleA);
+    ns_load<PLANES, 4>(x.a + ns_at<PLANES>(x.ldm, m, n), a4, kNsB * kNsScaleB / kNsScaleA);
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] += a4[e] + (m == n + e ? kNsA * kNsScaleB : 0.f);
-    ns_store<PLANES, 4>(x.b + ns_at<PLANES>(x.m, m, n), v, 1.0f);
-  } else {
-    ns_store<PLANES, 4>(x.x[cur ^ 1] + ns_at<PLANES>(x.n, m, n), v, 1.0f);
+    ns_store<PLANES, 4>(x.b + ns_at<PLANES>(x.ldm, m, n), v, 1.0f);
+  } else if constexpr (OP == Op::Apply) {
+    ns_store<PLANES, 4>(x.x[cur ^ 1] + ns_at<PLANES>(x.ldn, m, n), v, 1.0f);
   }
+}
+// Eight consecutive rows m.. of column n, v: scaled results.  Symmetric products: the
+// mirror image.
+template <Op OP, int PLANES>
+PB_DEV void store_mirror8(const NsMat& x, int m, int n, const float* v) {
+  ns_store<PLANES, 8>((OP == Op::Gram ? x.a : x.b) + ns_at<PLANES>(x.ldm, n, m), v, 1.0f);
 }
 
 // ------------------------------------------------------ 256 x 256 tiles
@@ -215,7 +234,7 @@ template <Op OP, int PLANES>
 __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan plan, int cur,
                                                             float* __restrict__ part) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  constexpr bool BK = OP != Op::Apply;  // the B operand is K-contiguous
+  constexpr bool BK = symmetric(OP);  // the B operand is K-contiguous
   const Item it = item_of(plan, t.count, blockIdx.x, gridDim.x);
   const NsMat& x = t.mat[plan.mat[it.place]];
   int tm, tn;
@@ -412,24 +431,22 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
       float v[4] = {s4[0], s4[1], s4[2], s4[3]};
       if (m < M && n < N) {
         store_result4<OP, PLANES>(x, cur, m, n, v);
-        if (OP != Op::Apply && tm != tn) *at = f32x4{v[0], v[1], v[2], v[3]};
+        if (symmetric(OP) && tm != tn) *at = f32x4{v[0], v[1], v[2], v[3]};
       }
     }
-    if constexpr (OP != Op::Apply) {
+    if constexpr (symmetric(OP)) {
       // the mirror image: 4 lanes hold the 32 rows of a column, 8 each
       if (pt || tm == tn) continue;
-      _Float16* out = OP == Op::Gram ? x.a : x.b;
       const int r8 = 8 * (lane & 3), mm = m0 + wm + 32 * i + r8;
 #pragma unroll
       for (int k = 0; k < kWTN / 16; ++k) {
-        const int cc = 16 * k + (lane >> 2), row = n0 + wn + cc;
+        const int cc = 16 * k + (lane >> 2), nn = n0 + wn + cc;
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           v[e] = *reinterpret_cast<const float*>(buf + (r8 + e) * (kWTN * 4) +
                                                  (((cc >> 2) ^ (r8 + e)) & 31) * 16 + (cc & 3) * 4);
-        if (row < N && mm < M)
-          ns_store<PLANES, 8>(out + ns_at<PLANES>(x.m, row, mm), v, 1.0f);
+        if (nn < N && mm < M) store_mirror8<OP, PLANES>(x, mm, nn, v);
       }
     }
   }
@@ -441,15 +458,15 @@ template <Op OP, int PLANES>
 __global__ __launch_bounds__(256) void ns_reduce_kernel(NsTable t, NsPlan plan, int cur,
                                                         const float* __restrict__ part) {
   __shared__ float lds[64][65];
-  const int tail = blockIdx.x >> 4, sub = blockIdx.x & 15, lid = plan.n_full + tail;
-  const int place = place_of(plan, t.count, lid);
+  const int tail = blockIdx.x >> 4, sub = blockIdx.x & 15, tile = plan.n_full + tail;
+  const int place = place_of(plan, t.count, tile);
   const NsMat& x = t.mat[plan.mat[place]];
   int tm, tn;
-  tile_at<OP, kBT>(x, lid - plan.first[place], tm, tn);
+  tile_at<OP, kBT>(x, tile - plan.first[place], tm, tn);
   const int r0 = (sub >> 2) * 64, c0 = (sub & 3) * 64, cl = 4 * (threadIdx.x & 15);
-  const int N = OP == Op::Apply ? x.n : x.m;
+  const int m0 = tm * kBT + r0, n0 = tn * kBT + c0, N = symmetric(OP) ? x.m : x.n;
   // (M and N are multiples of 64: the 64 x 64 block is inside or outside whole)
-  if (tm * kBT + r0 >= x.m || tn * kBT + c0 >= N) return;
+  if (m0 >= x.m || n0 >= N) return;
   const float* p = part + (size_t)tail * plan.splits * (kBT * kBT) + c0 + cl;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -459,147 +476,159 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(NsTable t, NsPlan plan, 
     for (int i = 1; i < plan.splits; ++i)
       s += *reinterpret_cast<const f32x4*>(q + (size_t)i * kBT * kBT);
     float v[4] = {s[0], s[1], s[2], s[3]};
-    store_result4<OP, PLANES>(x, cur, tm * kBT + r0 + rl, tn * kBT + c0 + cl, v);
+    store_result4<OP, PLANES>(x, cur, m0 + rl, n0 + cl, v);
 #pragma unroll
     for (int e = 0; e < 4; ++e) lds[rl][cl + e] = v[e];
   }
-  if constexpr (OP != Op::Apply) {
+  if constexpr (symmetric(OP)) {
     if (tm == tn) return;
     __syncthreads();
-    _Float16* out = OP == Op::Gram ? x.a : x.b;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const int cc = (threadIdx.x >> 3) + 32 * k, r8 = 8 * (threadIdx.x & 7);
       float v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = lds[r8 + e][cc];
-      ns_store<PLANES, 8>(out + ns_at<PLANES>(x.m, tn * kBT + c0 + cc, tm * kBT + r0 + r8), v, 1.0f);
+      store_mirror8<OP, PLANES>(x, m0 + r8, n0 + cc, v);
     }
   }
 }
 
-// ------------------------------------------------------ 128 x 128 tiles
-constexpr int kT = 128;
-constexpr int kWaves = 4;  // 2 x 2, each 64 x 64
-constexpr int kThreads = 64 * kWaves;
-constexpr int kOpBytes = kT * kRow * 2;                // one operand's K-tile: 16 KB
-constexpr int kPieces = kOpBytes / (1024 * kWaves);  // 1 KB DMA pieces per wave
-constexpr int kRowF = kT + 4;                        // floats per row of the staged output
+// -------------------------------------------------------- 64 x 64 tiles
+// Eight waves; wave w takes K-tiles w, w + 8, ... of the 64 x 64 tile, so the waves
+// share no operand values and the loop has no barrier.  Operands go through registers
+// and 16 KB of LDS of the wave's own: a fragment's quarter-wave lies in 16 rows, so
+// loading it straight from global memory takes 64 cache lookups an instruction (3.4 us
+// a K-tile of all waves), where eight lanes that share a row's 128 bytes take 8.  The
+// next K-tile's loads are in flight while one is multiplied.  The sums are added
+// through LDS in wave order.
+constexpr int kST = 64;
+constexpr int kSWaves = 8;
+constexpr int kSThreads = 64 * kSWaves;
+constexpr int kSWaveLds = kST * kST * 4;  // a wave's sums: 16 KB
+constexpr size_t kSLds = (size_t)kSWaves * kSWaveLds;
+
+// One operand of a wave.  (M, N and K are multiples of 64: a tile is whole.)
+template <bool KC, int PLANES>
+struct SmallSide {
+  const _Float16* p;  // wave-uniform
+  size_t step;
+  uint32_t off[8];    // bytes
+  PB_DEV void init(const _Float16* X, int ld, int R0, int kt, int lane) {
+    p = KC ? X + (size_t)R0 * ld + (size_t)kt * kRow
+           : X + (size_t)kt * kK<PLANES> * ld + (size_t)PLANES * R0;
+    step = (size_t)kSWaves * (KC ? kRow : kK<PLANES> * (size_t)ld);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) off[q] = lane_off<KC, kST, PLANES>(ld, kST, 1024 * q + 16 * lane);
+  }
+  // The next K-tile's 16 bytes of 1 KB piece q.
+  PB_DEV void load(u32x4 (&r)[8]) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      r[q] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(p) + off[q]);
+    p += step;
+  }
+  PB_DEV void frags(const u32x4 (&r)[8], unsigned char* lds, int lane, f16x8 (&f)[4][2]) const {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) *reinterpret_cast<u32x4*>(lds + 1024 * q + 16 * lane) = r[q];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) f[i][k] = frag<KC, kST, PLANES>(lds, 16 * i, k, lane);
+  }
+};
 
 template <Op OP, int PLANES>
-__global__ __launch_bounds__(kThreads, 2) void ns_gemm_kernel(NsTable t, NsPlan plan, int cur) {
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[kT * kRowF * 4];
-  static_assert(4 * kOpBytes <= kT * kRowF * 4, "two stages of two operands");
-  constexpr bool BK = OP != Op::Apply;
+__global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan plan, NsFinish fin,
+                                                              int cur) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  constexpr bool BK = symmetric(OP);
   const Item it = item_of(plan, t.count, blockIdx.x, gridDim.x);
   const NsMat& x = t.mat[plan.mat[it.place]];
   int tm, tn;
-  tile_at<OP, kT>(x, it.tile - plan.first[it.place], tm, tn);
-  const int m0 = tm * kT, n0 = tn * kT, M = x.m, N = BK ? x.m : x.n;
+  tile_at<OP, kST>(x, it.tile - plan.first[it.place], tm, tn);
+  const int m0 = tm * kST, n0 = tn * kST;
   const Operands o = operands<OP, PLANES>(x, cur);
-
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = (wave & 1) * 64, wn = (wave >> 1) * 64;
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(PB_LDS unsigned char*)smem;
-  uint32_t aoff[kPieces], boff[kPieces];
-#pragma unroll
-  for (int i = 0; i < kPieces; ++i) {
-    const int p = (wave * kPieces + i) * 1024 + 16 * lane;
-    aoff[i] = lane_off<true, kT, PLANES>(o.lda, M - m0, p);
-    boff[i] = lane_off<BK, kT, PLANES>(o.ldb, N - n0, p);
-  }
-  const _Float16* abase = o.A + (size_t)m0 * o.lda;
-  const _Float16* bbase = BK ? o.B + (size_t)n0 * o.ldb : o.B + (size_t)PLANES * n0;
-  const size_t bstep = BK ? kRow : (size_t)kK<PLANES> * o.ldb;  // values per K-tile
-  const int nt = o.K / kK<PLANES>;
-  auto issue = [&](int tt) {
-    const _Float16* a = abase + (size_t)tt * kRow;
-    const _Float16* b = bbase + (size_t)tt * bstep;
-    const uint32_t at = lds0 + (tt & 1) * 2 * kOpBytes + wave * kPieces * 1024;
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      dma16s(a, aoff[i], __builtin_amdgcn_readfirstlane(at + i * 1024));
-      dma16s(b, boff[i], __builtin_amdgcn_readfirstlane(at + kOpBytes + i * 1024));
-    }
-  };
+  const int nk = o.K / kK<PLANES>;
+  unsigned char* own = smem + wave * kSWaveLds;
 
   f32x4 acc[4][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  issue(0);
-  for (int tt = 0; tt < nt; ++tt) {
-    // tile tt has landed for every wave, and every wave is done with tile tt - 1
-    wait_dma<0>();
-    __syncthreads();
-    if (tt + 1 < nt) issue(tt + 1);
-    const unsigned char* pa = smem + (tt & 1) * 2 * kOpBytes;
-    const unsigned char* pb = pa + kOpBytes;
-    f16x8 fa[2][4], fb[2][4];
-#pragma unroll
-    for (int f = 0; f < 2; ++f) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) fa[f][i] = frag<true, kT, PLANES>(pa, wm + 16 * i, f, lane);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) fb[f][j] = frag<BK, kT, PLANES>(pb, wn + 16 * j, f, lane);
-    }
+  SmallSide<true, PLANES> sa;
+  SmallSide<BK, PLANES> sb;
+  sa.init(o.A, o.lda, m0, wave, lane);
+  sb.init(o.B, o.ldb, n0, wave, lane);
+  u32x4 ra[8], rb[8];
+  if (wave < nk) sa.load(ra), sb.load(rb);
+  for (int kt = wave; kt < nk; kt += kSWaves) {
+    f16x8 fa[4][2], fb[4][2];
+    sa.frags(ra, own, lane, fa);
+    sb.frags(rb, own + kSWaveLds / 2, lane, fb);
+    if (kt + kSWaves < nk) sa.load(ra), sb.load(rb);  // in flight while this one multiplies
     auto mma = [&](int af, int bf) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          acc[i][j] =
-              __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[bf][j], fa[af][i], acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[j][bf], fa[i][af], acc[i][j], 0, 0, 0);
     };
-    if constexpr (PLANES == 2) mma(1, 0), mma(0, 0), mma(0, 1);
+    if constexpr (PLANES == 2) mma(1, 0), mma(0, 1), mma(0, 0);
     else mma(0, 0), mma(1, 1);
   }
-  __syncthreads();
 
-  // Through LDS, so that rows (and the mirror image's rows) go out whole.
-  // acc[i][j][e] is row wm + 16 i + (lane & 15), column wn + 16 j + 4 (lane >> 4) + e.
-  float* stage = (float*)smem;
+  // acc[i][j][e] is row 16 i + (lane & 15), column 16 j + 4 (lane >> 4) + e; 16-byte
+  // chunks XOR-ed by the row
+  const int waves = min(kSWaves, nk);
+  if (wave < waves) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      *reinterpret_cast<f32x4*>(stage + (wm + 16 * i + (lane & 15)) * kRowF + wn + 16 * j +
-                                4 * (lane >> 4)) = acc[i][j];
+      for (int j = 0; j < 4; ++j) {
+        const int r = 16 * i + (lane & 15), c = 4 * j + (lane >> 4);
+        *reinterpret_cast<f32x4*>(own + r * (kST * 4) + ((c ^ r) & 15) * 16) = acc[i][j];
+      }
+  }
   __syncthreads();
-  const int c = 4 * (threadIdx.x & 31);
-#pragma unroll 4
-  for (int r = threadIdx.x >> 5; r < kT; r += kThreads / 32) {
-    const int row = m0 + r;
-    if (row >= M || n0 + c >= N) continue;
-    const f32x4 s4 = *reinterpret_cast<const f32x4*>(stage + r * kRowF + c);
-    float v[4] = {s4[0], s4[1], s4[2], s4[3]};
-    store_result4<OP, PLANES>(x, cur, row, n0 + c, v);
-    if (OP != Op::Apply && tm != tn)
-      *reinterpret_cast<f32x4*>(stage + r * kRowF + c) = f32x4{v[0], v[1], v[2], v[3]};
-  }
-  if constexpr (OP != Op::Apply) {
-    if (tm == tn) return;
-    __syncthreads();
-    _Float16* out = OP == Op::Gram ? x.a : x.b;
-    const int r4 = 4 * (threadIdx.x & 31);  // four rows of the tile: columns of its image
-    if (m0 + r4 >= M) return;
-#pragma unroll 4
-    for (int cc = threadIdx.x >> 5; cc < kT; cc += kThreads / 32) {
-      if (n0 + cc >= N) continue;
-      float v[4];
+  const int r = threadIdx.x >> 3, c8 = 8 * (threadIdx.x & 7);  // a row's eight columns
+  float v[8];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = stage[(r4 + e) * kRowF + cc];
-      ns_store<PLANES, 4>(out + ns_at<PLANES>(M, n0 + cc, m0 + r4), v, 1.0f);
-    }
+  for (int h = 0; h < 2; ++h) {
+    const int at = r * (kST * 4) + (((c8 >> 2) + h) ^ r & 15) * 16;
+    f32x4 s = *reinterpret_cast<const f32x4*>(smem + at);
+    for (int w = 1; w < waves; ++w) s += *reinterpret_cast<const f32x4*>(smem + w * kSWaveLds + at);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[4 * h + e] = s[e];
   }
+  const bool tall = x.rows > x.cols;
+  if constexpr (OP == Op::Last) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= out_scale<OP>();
+    if (!tall) finish<8>(x, fin, m0 + r, n0 + c8, v);
+  } else {
+    store_result4<OP, PLANES>(x, cur, m0 + r, n0 + c8, v);
+    store_result4<OP, PLANES>(x, cur, m0 + r, n0 + c8 + 4, v + 4);
+  }
+  if (OP == Op::Apply || (OP == Op::Last ? !tall : tm == tn)) return;
+  __syncthreads();
+  float* turned = (float*)smem;  // [64][65]
+#pragma unroll
+  for (int e = 0; e < 8; ++e) turned[(c8 + e) * 65 + r] = v[e];
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = turned[r * 65 + c8 + e];  // column r, eight rows
+  if constexpr (OP == Op::Last) finish<8>(x, fin, n0 + r, m0 + c8, v);
+  else store_mirror8<OP, PLANES>(x, m0 + c8, n0 + r, v);
 }
 
 // ---------------------------------------------------------------- plans
 int tiles_of(Op op, const NsMat& x, int t) {
   const int tm = (x.m + t - 1) / t, tn = (x.n + t - 1) / t;
-  return op == Op::Apply ? tm * tn : tm * (tm + 1) / 2;
+  return symmetric(op) ? tm * (tm + 1) / 2 : tm * tn;
 }
 
 // Time of a K-tile of a 256 x 256 tile with the chip full, and around a tile (launch,
@@ -607,6 +636,8 @@ int tiles_of(Op op, const NsMat& x, int t) {
 template <int PLANES>
 constexpr double kStepUs = PLANES == 2 ? 1.9 : 1.65;
 constexpr double kTileUs = 12.0;
+// Time of a K-tile of each wave of a 64 x 64 tile with the chip full.
+constexpr double kSmallUs = 1.2;
 
 struct Choice {
   bool big;  // 256 x 256 tiles
@@ -659,9 +690,18 @@ Choice choose(Op op, const NsTable& t) {
       if (us < best) best = us, c.plan.n_full = keep * kCUs, c.plan.splits = s, c.tail = tail;
     }
   }
-  c.big = tiles >= 64;
-  if (!c.big) {
-    c.plan.n_full = count(kT);
+  // 64 x 64 tiles: rounds of a workgroup a CU
+  const int small = count(kST);
+  long long waves = 0;
+  for (int i = 0; i < t.count; ++i)
+    waves += (long long)(c.plan.first[i + 1] - c.plan.first[i]) * ((len(c.plan.mat[i]) + 7) / 8);
+  const double est = 5.0 + 2.5 * ((small + kCUs - 1) / kCUs) +
+                     kSmallUs * std::max((double)waves / kCUs, (double)((len(c.plan.mat[0]) + 7) / 8));
+  c.big = best < est;
+  if (c.big) {
+    count(kBT);
+  } else {
+    c.plan.n_full = small;
     c.plan.splits = 1;
     c.tail = 0;
   }
@@ -669,22 +709,28 @@ Choice choose(Op op, const NsTable& t) {
 }
 
 template <Op OP, int PLANES>
-void launch(const NsTable& t, int cur, float* part, hipStream_t s) {
-  const Choice c = choose<PLANES>(OP, t);
-  if (c.big) {
-    ns_gemm_big<OP, PLANES>
-        <<<c.plan.n_full + c.tail * c.plan.splits, kBThreads, kBLds, s>>>(t, c.plan, cur, part);
+void launch(const NsTable& t, const NsFinish& fin, int cur, const Choice& c, float* part,
+            hipStream_t s) {
+  if (!c.big) {
+    ns_gemm_small<OP, PLANES><<<c.plan.n_full, kSThreads, kSLds, s>>>(t, c.plan, fin, cur);
+  } else if constexpr (OP != Op::Last) {
+    ns_gemm_big<OP, PLANES><<<c.plan.n_full + c.tail * c.plan.splits, kBThreads, kBLds, s>>>(
+        t, c.plan, cur, part);
     if (c.tail) ns_reduce_kernel<OP, PLANES><<<c.tail * 16, 256, 0, s>>>(t, c.plan, cur, part);
-  } else {
-    ns_gemm_kernel<OP, PLANES><<<c.plan.n_full, kThreads, 0, s>>>(t, c.plan, cur);
   }
 }
 
 template <int PLANES>
-void step(const NsTable& t, int cur, float* part, hipStream_t s) {
-  launch<Op::Gram, PLANES>(t, cur, part, s);
-  launch<Op::Square, PLANES>(t, cur, part, s);
-  launch<Op::Apply, PLANES>(t, cur, part, s);
+bool iterate(const NsTable& t, const NsFinish& fin, int steps, float* part, hipStream_t s) {
+  const Choice gram = choose<PLANES>(Op::Gram, t), square = choose<PLANES>(Op::Square, t),
+               apply = choose<PLANES>(Op::Apply, t);
+  for (int k = 0; k < steps; ++k) {
+    launch<Op::Gram, PLANES>(t, fin, k & 1, gram, part, s);
+    launch<Op::Square, PLANES>(t, fin, k & 1, square, part, s);
+    if (k + 1 == steps && !apply.big) launch<Op::Last, PLANES>(t, fin, k & 1, apply, part, s);
+    else launch<Op::Apply, PLANES>(t, fin, k & 1, apply, part, s);
+  }
+  return !apply.big;
 }
 
 template <int PLANES>
@@ -703,9 +749,9 @@ size_t ns_partial_floats(const NsTable& t, int planes) {
   return (planes == 2 ? partial_tiles<2>(t) : partial_tiles<1>(t)) * (kBT * kBT);
 }
 
-void launch_ns_step(const NsTable& t, int planes, int cur, float* part, hipStream_t s) {
-  if (planes == 2) step<2>(t, cur, part, s);
-  else step<1>(t, cur, part, s);
+bool launch_ns_products(const NsTable& t, const NsFinish& fin, int planes, int steps, float* part,
+                        hipStream_t s) {
+  return planes == 2 ? iterate<2>(t, fin, steps, part, s) : iterate<1>(t, fin, steps, part, s);
 }
 
 }  // namespace pb

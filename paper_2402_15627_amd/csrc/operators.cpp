@@ -191,6 +191,10 @@ bool ns_add(pb::NsTable& t, int rows, int cols) {
   x.cols = cols;
   x.m = pad(std::min(rows, cols));
   x.n = pad(std::max(rows, cols));
+  // rows an odd number of 64 values apart: rows a power of two apart lie in few of the
+  // L2's channels (256 x 1024, two planes: the first product 20 us, RESULT so)
+  x.ldm = x.m | pb::kNsPad;
+  x.ldn = x.n | pb::kNsPad;
   const long long tiles =
       t.tile0[t.count] + (long long)(pad(rows) / pb::kNsPad) * (pad(cols) / pb::kNsPad);
   t.tile0[++t.count] = (int)std::min(tiles, kMaxBlocks);
@@ -204,8 +208,8 @@ NsLayout ns_layout(pb::NsTable& t, int planes, char* base) {
   size_t o = L.norm + align256((size_t)t.count * sizeof(double));
   for (int i = 0; i < t.count; ++i) {
     pb::NsMat& x = t.mat[i];
-    const size_t big = align256((size_t)planes * x.m * x.n * 2);
-    const size_t small = align256((size_t)planes * x.m * x.m * 2);
+    const size_t big = align256((size_t)planes * x.m * x.ldn * 2);
+    const size_t small = align256((size_t)planes * x.m * x.ldm * 2);
     x.x[0] = (_Float16*)(base + o);
     x.x[1] = (_Float16*)(base + o + big);
     x.a = (_Float16*)(base + o + 2 * big);
