@@ -109,7 +109,8 @@ struct RmsForward {
   float eps;
 };
 void launch_rms_forward(Dt dt, const RmsForward& a, hipStream_t s);
-// part: rms_backward_parts(rows, cols) x cols floats.  dsum may be nullptr.
+// part: rms_backward_parts(rows, cols) rows of rms_part_ld(cols) floats, 16-byte aligned.
+// dsum may be nullptr.
 struct RmsBackward {
   const void *s, *gamma, *dy, *dsum;
   const float* rstd;
@@ -119,6 +120,7 @@ struct RmsBackward {
   int cols;
 };
 int rms_backward_parts(long long rows, int cols);
+__host__ __device__ inline size_t rms_part_ld(int cols) { return ((size_t)cols + 7) / 8 * 8; }
 void launch_rms_backward(Dt dt, const RmsBackward& a, hipStream_t s);
 
 // ------------------------------------- orthogonalised updates (Newton-Schulz)

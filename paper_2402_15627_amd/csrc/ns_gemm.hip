@@ -635,9 +635,11 @@ int tiles_of(Op op, const NsMat& x, int t) {
 // prologue, epilogue), in us.
 template <int PLANES>
 constexpr double kStepUs = PLANES == 2 ? 1.9 : 1.65;
-constexpr double kTileUs = 12.0;
-// Time of a K-tile of each wave of a 64 x 64 tile with the chip full.
-constexpr double kSmallUs = 1.2;
+constexpr double kTileUs = 16.0, kSplitUs = 9.0;
+// The same for the 64 x 64 tiles, a step being a K-tile of each of the eight waves.
+template <int PLANES>
+constexpr double kSmallStepUs = PLANES == 2 ? 2.05 : 1.9;
+constexpr double kSmallTileUs = 2.5, kSmallUs = 5.0;
 
 struct Choice {
   bool big;  // 256 x 256 tiles
@@ -662,41 +664,42 @@ Choice choose(Op op, const NsTable& t) {
     return c.plan.first[t.count];
   };
   const int tiles = count(kBT);
-  // K-tiles until the last item ends, the items (longest first) taken in rounds of kCUs
-  auto rounds = [&](int n_full, int splits) {
-    long long steps = 0, next = 0, at = 0;
+  // Steps until the last item ends, and rounds, the items (longest first) taken kCUs at
+  // a time; l(i): steps of a tile of matrix i, those past n_full in `splits` items
+  struct Rounds {
+    long long steps, count;
+  };
+  auto rounds = [&](auto l, int n_full, int splits) {
+    Rounds r{0, 0};
+    long long at = 0;  // items so far
     for (int i = 0; i < t.count; ++i) {
-      const int nk = len(c.plan.mat[i]), cut = (nk + splits - 1) / splits;
+      const int nk = l(c.plan.mat[i]), cut = (nk + splits - 1) / splits;
       const int whole = std::max(0, std::min(c.plan.first[i + 1], n_full) - c.plan.first[i]);
       const int rest = c.plan.first[i + 1] - c.plan.first[i] - whole;
-      for (const auto& [n, l] : {std::pair<long long, int>{whole, nk}, {(long long)rest * splits, cut}}) {
-        // items at .. at + n - 1; a round starts at each multiple of kCUs
-        if (n <= 0) continue;
-        const long long starts = next >= at + n ? 0 : (at + n - 1 - next) / kCUs + 1;
-        steps += starts * l;
-        next += starts * kCUs;
+      for (int part = 0; part < 2; ++part) {
+        const long long n = part ? (long long)rest * splits : whole;
+        const long long starts = (at + n + kCUs - 1) / kCUs - r.count;  // rounds that begin here
+        r.steps += starts * (part ? cut : nk);
+        r.count += starts;
         at += n;
       }
     }
-    return (double)steps;
+    return r;
   };
-  double best = kTileUs + kStepUs<PLANES> * rounds(tiles, 1);
+  double best = kTileUs + kStepUs<PLANES> * rounds(len, tiles, 1).steps;
   c.plan.n_full = tiles;
   c.plan.splits = 1;
   for (int keep = tiles / kCUs; keep >= std::max(0, tiles / kCUs - 1); --keep) {
     const int tail = tiles - keep * kCUs;
     for (int s = 2; tail > 0 && s <= 16 && (long long)tail * s <= 4 * kCUs; ++s) {
-      const double us = kTileUs + kStepUs<PLANES> * rounds(keep * kCUs, s) + 6.0 + 0.1 * tail * s;
+      const double us =
+          kTileUs + kStepUs<PLANES> * rounds(len, keep * kCUs, s).steps + kSplitUs + 0.1 * tail * s;
       if (us < best) best = us, c.plan.n_full = keep * kCUs, c.plan.splits = s, c.tail = tail;
     }
   }
-  // 64 x 64 tiles: rounds of a workgroup a CU
   const int small = count(kST);
-  long long waves = 0;
-  for (int i = 0; i < t.count; ++i)
-    waves += (long long)(c.plan.first[i + 1] - c.plan.first[i]) * ((len(c.plan.mat[i]) + 7) / 8);
-  const double est = 5.0 + 2.5 * ((small + kCUs - 1) / kCUs) +
-                     kSmallUs * std::max((double)waves / kCUs, (double)((len(c.plan.mat[0]) + 7) / 8));
+  const Rounds r = rounds([&](int i) { return (len(i) + kSWaves - 1) / kSWaves; }, small, 1);
+  const double est = kSmallUs + kSmallTileUs * r.count + kSmallStepUs<PLANES> * r.steps;
   c.big = best < est;
   if (c.big) {
     count(kBT);

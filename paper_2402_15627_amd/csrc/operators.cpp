@@ -309,7 +309,8 @@ pb_status pblock_rmsnorm_forward(const pb_rmsnorm_config* cfg, const void* x, co
 
 size_t pblock_rmsnorm_workspace_bytes(const pb_rmsnorm_config* cfg) {
   if (check_rms(cfg) != PB_OK) return 0;
-  return align256((size_t)pb::rms_backward_parts(cfg->rows, cfg->cols) * cfg->cols * 4);
+  return align256((size_t)pb::rms_backward_parts(cfg->rows, cfg->cols) *
+                  pb::rms_part_ld(cfg->cols) * sizeof(float));
 }
 
 pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s, const void* gamma,

@@ -27,21 +27,58 @@ namespace {
 constexpr float kE4m3Max = 448.0f;
 constexpr double kScaleMin = 0x1p-126;  // smallest scale: a group of zeros has this one
 
-// Eight columns from column c of a row of H, elementwise past 16-byte alignment or
-// the row's end (those columns read as zero).
+// Eight elements as they lie in memory, 16 bytes to a load.  AL: 16-byte aligned; the
+// hardware takes any alignment of the element, which rows of an odd width have.
+template <typename T>
+struct Piece {
+  static constexpr int kWords = sizeof(T) / 2;  // 16-byte words
+  u32x4 w[kWords];
+  PB_DEV float at(int e) const {
+    if constexpr (sizeof(T) == 2) return e & 1 ? hi_bf(w[0][e >> 1]) : lo_bf(w[0][e >> 1]);
+    else return __uint_as_float(w[e >> 2][e & 3]);
+  }
+};
+// Columns c .. c + 7 of a row of H (past the row's end zeros, where not AL).
 template <typename T, bool AL>
-PB_DEV void load_cols(const T* row, int c, int H, float* v) {
-  if constexpr (AL) {
-    load8<T>(row + c, v);
+PB_DEV Piece<T> load_piece(const T* row, int c, int H) {
+  Piece<T> p;
+  if (AL || c + 8 <= H) {
+#pragma unroll
+    for (int k = 0; k < Piece<T>::kWords; ++k) {
+      const T* at = row + c + 8 / Piece<T>::kWords * k;
+      if constexpr (AL) p.w[k] = *reinterpret_cast<const u32x4*>(at);
+      else __builtin_memcpy(&p.w[k], at, 16);
+    }
   } else {
+    float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = c + e < H ? load1<T>(row + c + e) : 0.f;
+#pragma unroll
+    for (int k = 0; k < 4 * Piece<T>::kWords; ++k)
+      p.w[k >> 2][k & 3] = sizeof(T) == 2 ? pack_bf2(v[2 * k], v[2 * k + 1]) : __float_as_uint(v[k]);
   }
+  return p;
+}
+template <typename T>
+PB_DEV Piece<T> zero_piece() {
+  Piece<T> p;
+#pragma unroll
+  for (int k = 0; k < Piece<T>::kWords; ++k) p.w[k] = u32x4{0, 0, 0, 0};
+  return p;
 }
 template <typename T, bool AL>
 PB_DEV void store_cols(T* row, int c, int H, const float* v) {
-  if constexpr (AL) {
-    store8<T>(row + c, v);
+  if (AL || c + 8 <= H) {
+#pragma unroll
+    for (int k = 0; k < Piece<T>::kWords; ++k) {
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        w[e] = sizeof(T) == 2 ? pack_bf2(v[2 * e], v[2 * e + 1]) : __float_as_uint(v[4 * k + e]);
+      T* at = row + c + 8 / Piece<T>::kWords * k;
+      if constexpr (AL) *reinterpret_cast<u32x4*>(at) = w;
+      else __builtin_memcpy(at, &w, 16);
+    }
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
@@ -50,19 +87,21 @@ PB_DEV void store_cols(T* row, int c, int H, const float* v) {
 }
 
 // Sum (or maximum) over the TPR threads that share a row; every one receives it.
-// red: one value per wave, used where a row spans waves.
+// red: a value per wave, where a row spans waves: its two halves are used in turn
+// (`turn`), so that one barrier a reduction is enough.
 template <int TPR, typename R, typename Op>
-PB_DEV R row_reduce(R v, R* red, Op op) {
+PB_DEV R row_reduce(R v, R* red, int& turn, Op op) {
 #pragma unroll
   for (int o = (TPR < 64 ? TPR : 64) / 2; o >= 1; o >>= 1) v = op(v, __shfl_xor(v, o, 64));
   if constexpr (TPR > 64) {
-    const int wave = threadIdx.x >> 6;
-    __syncthreads();  // red may still be read from an earlier reduction
-    if ((threadIdx.x & 63) == 0) red[wave] = v;
+    constexpr int kWaves = TPR / 64;
+    R* at = red + turn * kWaves;
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = red[0];
+    v = at[0];
 #pragma unroll
-    for (int i = 1; i < TPR / 64; ++i) v = op(v, red[i]);
+    for (int i = 1; i < kWaves; ++i) v = op(v, at[i]);
   }
   return v;
 }
@@ -71,83 +110,88 @@ template <typename T, int TPR, int NC, bool AL, bool Q8>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_fwd_kernel(RmsForward a) {
   using R = typename std::conditional<Q8, double, float>::type;
   constexpr int kThreads = TPR < 256 ? 256 : TPR, kRows = kThreads / TPR;
-  __shared__ R red[kThreads / 64];
+  __shared__ R red[2 * (kThreads / 64)];
   const int H = a.cols, l = threadIdx.x % TPR;
+  int turn = 0;
   for (long long r0 = (long long)blockIdx.x * kRows; r0 < a.rows;
        r0 += (long long)gridDim.x * kRows) {
     // (a row past the end, where rows share a workgroup, is zeros and stores nothing:
     // the lanes of a wave stay together)
     const long long row = r0 + threadIdx.x / TPR;
     const bool live = row < a.rows;
-    const long long rc = live ? row : a.rows - 1;
-    const T* x = (const T*)a.x + rc * H;
-    const T* res = a.resid ? (const T*)a.resid + rc * H : nullptr;
-    const T* gamma = (const T*)a.gamma;
-    R s[NC][8];
-    float xv[NC][8], rv[NC][8];
+    const long long at = (live ? row : a.rows - 1) * H;
+    // the row as it lies in memory: in fp64 its sums would take four times the registers
+    Piece<T> xp[NC], rp[NC];
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
       const int c = 8 * (l + j * TPR);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) xv[j][e] = rv[j][e] = 0.f;
+      xp[j] = rp[j] = zero_piece<T>();
       if (c < H && live) {
-        load_cols<T, AL>(x, c, H, xv[j]);
-        if (res) load_cols<T, AL>(res, c, H, rv[j]);
+        xp[j] = load_piece<T, AL>((const T*)a.x + at, c, H);
+        if (a.resid) rp[j] = load_piece<T, AL>((const T*)a.resid + at, c, H);
       }
     }
+    auto sum = [&](int j, int e) { return (R)xp[j].at(e) + (R)rp[j].at(e); };
     R ss = 0;
 #pragma unroll
-    for (int j = 0; j < NC; ++j)
+    for (int j = 0; j < NC; ++j) {
+      const int c = 8 * (l + j * TPR);
+      float o[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        s[j][e] = (R)xv[j][e] + (R)rv[j][e];
-        ss += s[j][e] * s[j][e];
+        const R s = sum(j, e);
+        o[e] = (float)s;
+        ss += s * s;
       }
-    if (a.sum && live)
-#pragma unroll
-      for (int j = 0; j < NC; ++j) {
-        const int c = 8 * (l + j * TPR);
-        float o[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = (float)s[j][e];
-        if (c < H) store_cols<T, AL>((T*)a.sum + rc * H, c, H, o);
-      }
-    ss = row_reduce<TPR>(ss, red, [](R p, R q) { return p + q; });
+      if (a.sum && live && c < H) store_cols<T, AL>((T*)a.sum + at, c, H, o);
+    }
+    ss = row_reduce<TPR>(ss, red, turn, [](R p, R q) { return p + q; });
     R r;
     if constexpr (Q8) r = 1.0 / sqrt(ss / H + (double)a.eps);
     else r = 1.0f / sqrtf(ss / H + a.eps);
     if (a.rstd && live && l == 0) a.rstd[row] = (float)r;
 
-    R most = 0;  // max |y| of the row
+    // columns c .. of y
+    auto values = [&](int j, int c, R (&y)[8]) {
+      Piece<T> g = zero_piece<T>();
+      if (c < H) g = load_piece<T, AL>((const T*)a.gamma, c, H);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = sum(j, e) * r * (R)g.at(e);
+    };
+    auto largest = [](const R (&y)[8]) {
+      R m = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) m = fmax(m, fabs(y[e]));
+      return m;
+    };
+    R most = 0;  // max |y| of the row, where it has one scale
+    if constexpr (Q8) {
+      if (!a.group) {
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+          R y[8];
+          values(j, 8 * (l + j * TPR), y);
+          most = fmax(most, largest(y));
+        }
+        most = row_reduce<TPR>(most, red, turn, [](R p, R q) { return fmax(p, q); });
+      }
+    }
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
       const int c = 8 * (l + j * TPR);
-      float g[8], o[8];
+      R y[8];
+      values(j, c, y);
+      if (a.y && live && c < H) {
+        float o[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) g[e] = 0.f;
-      if (c < H) load_cols<T, AL>(gamma, c, H, g);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        s[j][e] = s[j][e] * r * (R)g[e];
-        o[e] = (float)s[j][e];
+        for (int e = 0; e < 8; ++e) o[e] = (float)y[e];
+        store_cols<T, AL>((T*)a.y + at, c, H, o);
       }
-      if (a.y && live && c < H) store_cols<T, AL>((T*)a.y + rc * H, c, H, o);
-      if constexpr (Q8)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) most = fmax(most, fabs(s[j][e]));
-    }
-    if constexpr (Q8) {
-      const int G = a.group;
-      const int groups = G ? (H + G - 1) / G : 1;
-      if (!G) most = row_reduce<TPR>(most, red, [](R p, R q) { return fmax(p, q); });
-#pragma unroll
-      for (int j = 0; j < NC; ++j) {
-        const int c = 8 * (l + j * TPR);
+      if constexpr (Q8) {
+        const int G = a.group, groups = G ? (H + G - 1) / G : 1;
         R m = most;
         if (G) {  // the G / 8 neighbouring lanes of a group
-          m = 0;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) m = fmax(m, fabs(s[j][e]));
+          m = largest(y);
           for (int o = G / 16; o >= 1; o >>= 1) m = fmax(m, __shfl_xor(m, o, 64));
         }
         // the scale as it is kept, in fp32
@@ -156,92 +200,161 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_fwd_kernel(RmsForwa
         uint32_t w[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          int p = __builtin_amdgcn_cvt_pk_fp8_f32((float)(s[j][4 * h] * inv),
-                                                  (float)(s[j][4 * h + 1] * inv), 0, false);
-          p = __builtin_amdgcn_cvt_pk_fp8_f32((float)(s[j][4 * h + 2] * inv),
-                                              (float)(s[j][4 * h + 3] * inv), p, true);
+          int p = __builtin_amdgcn_cvt_pk_fp8_f32((float)(y[4 * h] * inv),
+                                                  (float)(y[4 * h + 1] * inv), 0, false);
+          p = __builtin_amdgcn_cvt_pk_fp8_f32((float)(y[4 * h + 2] * inv),
+                                              (float)(y[4 * h + 3] * inv), p, true);
           w[h] = (uint32_t)p;
         }
         if (live && c < H) {
-          uint8_t* q = a.q8 + rc * H + c;
-          if constexpr (AL) {
-            *reinterpret_cast<u32x2*>(q) = u32x2{w[0], w[1]};
+          uint8_t* q = a.q8 + at + c;
+          if (AL || c + 8 <= H) {
+            if constexpr (AL) *reinterpret_cast<u32x2*>(q) = u32x2{w[0], w[1]};
+            else __builtin_memcpy(q, w, 8);
           } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
               if (c + e < H) q[e] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
           }
-          if (G ? c % G == 0 : c == 0) a.scales[rc * groups + (G ? c / G : 0)] = scale;
+          if (G ? c % G == 0 : c == 0)
+            a.scales[(live ? row : 0) * groups + (G ? c / G : 0)] = scale;
         }
       }
     }
   }
 }
 
-// A workgroup takes every gridDim.x-th set of kRows rows and keeps its part of
-// dgamma in registers; the rows that share the workgroup add theirs up in LDS, in
-// turn, and the workgroup's sums go to part[workgroup][H].
+// A workgroup takes every gridDim.x-th set of kRows rows and keeps its part of dgamma
+// (and gamma) in registers; the next row's loads are issued before a row's reduction.
+// The rows that share a workgroup add theirs up in LDS, in turn; the workgroup's sums
+// go to part[workgroup][rms_part_ld(H)].
 template <typename T, int TPR, int NC, bool AL>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_bwd_kernel(RmsBackward a) {
   constexpr int kThreads = TPR < 256 ? 256 : TPR, kRows = kThreads / TPR;
-  __shared__ float red[kThreads / 64];
+  // Wider rows leave no registers for a second row, and the widest none for one: their
+  // second pass over the row reads it again, from the caches.
+  constexpr bool kAhead = sizeof(T) * NC <= 8 && TPR <= 256, kKeep = TPR <= 512;
+  __shared__ float red[2 * (kThreads / 64)];
   __shared__ float fold[kRows > 1 ? TPR * NC * 8 : 1];
   const int H = a.cols, l = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-  const T* gamma = (const T*)a.gamma;
+  int turn = 0;
   float acc[NC][8];
+  constexpr int kN = kKeep ? NC : 1;
+  Piece<T> gp[kN];
 #pragma unroll
-  for (int j = 0; j < NC; ++j)
+  for (int j = 0; j < NC; ++j) {
+    const int c = 8 * (l + j * TPR);
+    if constexpr (kKeep) {
+      gp[j] = zero_piece<T>();
+      if (c < H) gp[j] = load_piece<T, AL>((const T*)a.gamma, c, H);
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[j][e] = 0.f;
-  for (long long r0 = (long long)blockIdx.x * kRows; r0 < a.rows;
-       r0 += (long long)gridDim.x * kRows) {
-    const long long row = r0 + sub;
-    const bool live = row < a.rows;
-    const long long at = (live ? row : a.rows - 1) * H;
-    float s[NC][8], dy[NC][8], g[NC][8];
-#pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      const int c = 8 * (l + j * TPR);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s[j][e] = dy[j][e] = g[j][e] = 0.f;
-      if (c < H && live) {
-        load_cols<T, AL>((const T*)a.s + at, c, H, s[j]);
-        load_cols<T, AL>((const T*)a.dy + at, c, H, dy[j]);
-        load_cols<T, AL>(gamma, c, H, g[j]);
-      }
-    }
-    const float r = a.rstd[live ? row : a.rows - 1];
-    float k = 0.f;
-#pragma unroll
-    for (int j = 0; j < NC; ++j)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        g[j][e] *= dy[j][e];
-        s[j][e] *= r;
-        k += g[j][e] * s[j][e];
-        if (live) acc[j][e] += dy[j][e] * s[j][e];
-      }
-    k = row_reduce<TPR>(k, red, [](float p, float q) { return p + q; }) / H;
-    if (live)
+  }
+  float* part = a.part + (size_t)blockIdx.x * rms_part_ld(H);
+  if constexpr (!kKeep) {  // (a row a workgroup)
+    for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
+      const float r = a.rstd[row];
+      const T* sp = (const T*)a.s + row * H;
+      const T* dyp = (const T*)a.dy + row * H;
+      float k = 0.f;
 #pragma unroll
       for (int j = 0; j < NC; ++j) {
         const int c = 8 * (l + j * TPR);
-        if (c < H) {
-          float o[8];
+        if (c >= H) continue;
+        const Piece<T> s = load_piece<T, AL>(sp, c, H), dy = load_piece<T, AL>(dyp, c, H),
+                       g = load_piece<T, AL>((const T*)a.gamma, c, H);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] = 0.f;
-          if (a.dsum) load_cols<T, AL>((const T*)a.dsum + at, c, H, o);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] += r * (g[j][e] - s[j][e] * k);
-          store_cols<T, AL>((T*)a.dx + at, c, H, o);
+        for (int e = 0; e < 8; ++e) {
+          const float u = dy.at(e) * (s.at(e) * r);
+          k += g.at(e) * u;
+          acc[j][e] += u;
         }
       }
+      k = row_reduce<TPR>(k, red, turn, [](float p, float q) { return p + q; }) / H;
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+        const int c = 8 * (l + j * TPR);
+        if (c >= H) continue;
+        const Piece<T> s = load_piece<T, AL>(sp, c, H), dy = load_piece<T, AL>(dyp, c, H),
+                       g = load_piece<T, AL>((const T*)a.gamma, c, H);
+        Piece<T> ds = zero_piece<T>();
+        if (a.dsum) ds = load_piece<T, AL>((const T*)a.dsum + row * H, c, H);
+        float o[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          o[e] = ds.at(e) + r * (dy.at(e) * g.at(e) - s.at(e) * r * k);
+        store_cols<T, AL>((T*)a.dx + row * H, c, H, o);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      const int c = 8 * (l + j * TPR);  // (part's rows are padded to whole pieces)
+      if (c < H) store8<float>(part + c, acc[j]);
+    }
+    return;
+  }
+  struct Row {
+    Piece<T> s[kN], dy[kN], ds[kN];
+    float r;
+  };
+  // row `row` (past the last, the last again: loads are not behind a branch)
+  auto load = [&](long long row, Row& w) {
+    row = row < a.rows ? row : a.rows - 1;
+    const long long at = row * H;
+    w.r = a.rstd[row];
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      const int c = 8 * (l + j * TPR);
+      if (c < H) {
+        w.s[j] = load_piece<T, AL>((const T*)a.s + at, c, H);
+        w.dy[j] = load_piece<T, AL>((const T*)a.dy + at, c, H);
+        if (a.dsum) w.ds[j] = load_piece<T, AL>((const T*)a.dsum + at, c, H);
+      }
+    }
+  };
+  const long long step = (long long)gridDim.x * kRows;
+  Row cur, next;
+#pragma unroll
+  for (int j = 0; j < kN; ++j) {
+    cur.s[j] = cur.dy[j] = cur.ds[j] = zero_piece<T>();
+    next.s[j] = next.dy[j] = next.ds[j] = zero_piece<T>();
+  }
+  long long r0 = (long long)blockIdx.x * kRows;
+  load(r0 + sub, cur);
+  for (; r0 < a.rows; r0 += step) {
+    if constexpr (kAhead) load(r0 + step + sub, next);
+    const bool live = r0 + sub < a.rows;
+    const float r = cur.r;
+    float k = 0.f;
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float dy = cur.dy[j].at(e), s = cur.s[j].at(e) * r;
+        k += dy * gp[j].at(e) * s;
+        acc[j][e] += live ? dy * s : 0.f;
+      }
+    k = row_reduce<TPR>(k, red, turn, [](float p, float q) { return p + q; }) / H;
+    if (live)
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        const int c = 8 * (l + j * TPR);
+        if (c >= H) continue;
+        float o[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          o[e] = cur.ds[j].at(e) + r * (cur.dy[j].at(e) * gp[j].at(e) - cur.s[j].at(e) * r * k);
+        store_cols<T, AL>((T*)a.dx + (r0 + sub) * H, c, H, o);
+      }
+    if constexpr (kAhead) cur = next;
+    else if (r0 + step < a.rows) load(r0 + step + sub, cur);
   }
   if constexpr (kRows > 1) {
     for (int t = 0; t < kRows; ++t) {
       if (sub == t)
 #pragma unroll
-        for (int j = 0; j < NC; ++j)
+        for (int j = 0; j < kN; ++j)
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             float* f = fold + 8 * (l + j * TPR) + e;
@@ -249,33 +362,36 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_bwd_kernel(RmsBackw
           }
       __syncthreads();
     }
-    for (int c = threadIdx.x; c < H; c += kThreads) a.part[(size_t)blockIdx.x * H + c] = fold[c];
+    for (int c = threadIdx.x; c < H; c += kThreads) part[c] = fold[c];
   } else {
 #pragma unroll
-    for (int j = 0; j < NC; ++j)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int c = 8 * (l + j * TPR) + e;
-        if (c < H) a.part[(size_t)blockIdx.x * H + c] = acc[j][e];
-      }
+    for (int j = 0; j < kN; ++j) {
+      const int c = 8 * (l + j * TPR);  // (part's rows are padded to whole pieces)
+      if (c < H) store8<float>(part + c, acc[j]);
+    }
   }
 }
 
-// dgamma[c] = sum over n rows of part, 16 threads a column (n = 0: zeros).
-__global__ __launch_bounds__(256) void rms_fold_kernel(const float* __restrict__ part, int n, int H,
-                                                       float* __restrict__ dgamma) {
-  __shared__ float red[16][17];
-  const int cl = threadIdx.x & 15, rl = threadIdx.x >> 4, c = blockIdx.x * 16 + cl;
-  float v = 0.f;
+// dgamma[c] = sum over n rows of part: a thread four columns of every 64th row, then the
+// 64 threads of a column in LDS (n = 0: zeros).
+constexpr int kFoldThreads = 1024;
+__global__ __launch_bounds__(kFoldThreads) void rms_fold_kernel(const float* __restrict__ part,
+                                                                int n, int H,
+                                                                float* __restrict__ dgamma) {
+  __shared__ float red[64][64 + 4];
+  const int cl = 4 * (threadIdx.x & 15), rl = threadIdx.x >> 4, c = blockIdx.x * 64 + cl;
+  const size_t ld = rms_part_ld(H);
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
   if (c < H)
-    for (int i = rl; i < n; i += 16) v += part[(size_t)i * H + c];
-  red[rl][cl] = v;
+#pragma unroll 8
+    for (int i = rl; i < n; i += 64) v += *reinterpret_cast<const f32x4*>(part + i * ld + c);
+  *reinterpret_cast<f32x4*>(&red[rl][cl]) = v;
   __syncthreads();
-  if (rl == 0 && c < H) {
-#pragma unroll
-    for (int i = 1; i < 16; ++i) v += red[i][cl];
-    dgamma[c] = v;
-  }
+  // 16 neighbouring lanes sum a column, four rows each
+  const int col = threadIdx.x >> 4, q = threadIdx.x & 15;
+  float s = (red[4 * q][col] + red[4 * q + 1][col]) + (red[4 * q + 2][col] + red[4 * q + 3][col]);
+  s = row16_sum(s);
+  if (q == 0 && blockIdx.x * 64 + col < H) dgamma[blockIdx.x * 64 + col] = s;
 }
 
 // Threads a row and pieces of 8 columns a thread: rows of up to 128 columns take
@@ -332,7 +448,7 @@ void backward(const RmsBackward& a, hipStream_t s) {
       if (al) rms_bwd_kernel<T, TPR, NC, true><<<n, threads, 0, s>>>(a);
       else rms_bwd_kernel<T, TPR, NC, false><<<n, threads, 0, s>>>(a);
     });
-  rms_fold_kernel<<<(a.cols + 15) / 16, 256, 0, s>>>(a.part, n, a.cols, a.dgamma);
+  rms_fold_kernel<<<(a.cols + 63) / 64, kFoldThreads, 0, s>>>(a.part, n, a.cols, a.dgamma);
 }
 
 }  // namespace
