@@ -29,9 +29,9 @@ constexpr int kThreads = 256;
 
 PB_DEV int mat_of(const NsTable& t, int tile) {
   int i = 0;
-#pragma unroll 1
-  for (int k = 1; k < t.count; ++k)
-    if (tile >= t.tile0[k]) i = k;
+#pragma unroll
+  for (int k = 1; k < kNsMaxTensors; ++k)
+    if (k < t.count && tile >= t.tile0[k]) i = k;
   return i;
 }
 
@@ -198,6 +198,10 @@ __global__ __launch_bounds__(kThreads) void ns_finish_kernel(NsTable t, NsFinish
   const NsMat& x = t.mat[at.i];
   const bool tall = x.rows > x.cols;
   const int i0 = tall ? at.c0 : at.r0, j0 = tall ? at.r0 : at.c0;
+  const int rl = threadIdx.x >> 4, cl = 4 * (threadIdx.x & 15);
+  float u[4][4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) weights<4>(x, fin, at.r0 + rl + 16 * k, at.c0 + cl, u[k]);
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int i = (threadIdx.x >> 3) + 32 * k, j = 8 * (threadIdx.x & 7);
@@ -210,14 +214,12 @@ __global__ __launch_bounds__(kThreads) void ns_finish_kernel(NsTable t, NsFinish
     }
   }
   __syncthreads();
-  const int cl = 4 * (threadIdx.x & 15);
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const int rl = (threadIdx.x >> 4) + 16 * k;
     float v[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = lds[rl][cl + e];
-    finish<4>(x, fin, at.r0 + rl, at.c0 + cl, v);
+    for (int e = 0; e < 4; ++e) v[e] = lds[rl + 16 * k][cl + e];
+    finish<4>(x, fin, at.r0 + rl + 16 * k, at.c0 + cl, v, u[k]);
   }
 }
 

@@ -74,24 +74,30 @@ PB_DEV void put(T* p, int left, const float* v) {
       if (e < left) p[e] = (T)v[e];
   }
 }
+// The weights there before the step (Muon; else nothing).
 template <int N>
-PB_DEV void finish(const NsMat& x, const NsFinish& f, int r, int c, const float* v) {
+PB_DEV void weights(const NsMat& x, const NsFinish& f, int r, int c, float* u) {
+  const int left = x.cols - c;
+  if (f.mode != NsMode::Muon || r >= x.rows || left <= 0) return;
+  const float* w = x.w + r * x.ld_src + c;
+  if (left >= N && (uintptr_t)w % 16 == 0) {
+#pragma unroll
+    for (int e = 0; e < N; e += 4) load4<float>(w + e, u + e);
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) u[e] = e < left ? w[e] : 0.f;
+  }
+}
+// u: those weights, stepped in place.
+template <int N>
+PB_DEV void finish(const NsMat& x, const NsFinish& f, int r, int c, const float* v, float* u) {
   const int left = x.cols - c;
   if (r >= x.rows || left <= 0) return;
   if (f.mode == NsMode::Muon) {
-    float* w = x.w + r * x.ld_src + c;
     const float keep = 1.0f - f.lr * x.decay, step = f.lr * x.scale;
-    float u[N];
-    if (left >= N && (uintptr_t)w % 16 == 0) {
-#pragma unroll
-      for (int e = 0; e < N; e += 4) load4<float>(w + e, u + e);
-    } else {
-#pragma unroll
-      for (int e = 0; e < N; ++e) u[e] = e < left ? w[e] : 0.f;
-    }
 #pragma unroll
     for (int e = 0; e < N; ++e) u[e] = __builtin_fmaf(-step, v[e], u[e] * keep);
-    put<N>(w, left, u);
+    put<N>(x.w + r * x.ld_src + c, left, u);
     if (x.copy) {
       if (f.bf16_out) put<N>((bf16*)x.copy + r * x.ld_src + c, left, u);
       else put<N>((float*)x.copy + r * x.ld_src + c, left, u);
@@ -102,7 +108,6 @@ PB_DEV void finish(const NsMat& x, const NsFinish& f, int r, int c, const float*
     put<N>((float*)x.out + r * x.ld_out + c, left, v);
   }
 }
-
 // `steps` Newton-Schulz steps of every matrix from x[0] on.  part: room for
 // ns_partial_floats(t, planes) floats.  True where the last product has finished the
 // tensors; else X is in x[steps & 1].

@@ -144,10 +144,10 @@ PB_DEV void tile_at(const NsMat& x, int id, int& tm, int& tn) {
 }
 
 PB_DEV int place_of(const NsPlan& p, int count, int tile) {
-  int i = 0;
-#pragma unroll 1
-  for (int k = 1; k < count; ++k)
-    if (tile >= p.first[k]) i = k;
+  int i = 0;  // (unrolled: one batch of scalar loads, not a chain of them)
+#pragma unroll
+  for (int k = 1; k < kNsMaxTensors; ++k)
+    if (k < count && tile >= p.first[k]) i = k;
   return i;
 }
 
@@ -186,23 +186,24 @@ PB_DEV Operands operands(const NsMat& x, int cur) {
   else return {x.b, x.x[cur], m, n, x.m};
 }
 
-// Four consecutive columns n.. of row m of a product, v: the sums (scaled in place).
-template <Op OP, int PLANES>
-PB_DEV void store_result4(const NsMat& x, int cur, int m, int n, float* v) {
-  constexpr float kOut = out_scale<OP>();
+// What square adds to its sums at N consecutive columns n.. of row m: a I + b A.
+template <Op OP, int PLANES, int N>
+PB_DEV void addend(const NsMat& x, int m, int n, float* u) {
+  if constexpr (OP == Op::Square) {
+    ns_load<PLANES, N>(x.a + ns_at<PLANES>(x.ldm, m, n), u, kNsB * kNsScaleB / kNsScaleA);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] *= kOut;
-  if constexpr (OP == Op::Gram) {
-    ns_store<PLANES, 4>(x.a + ns_at<PLANES>(x.ldm, m, n), v, 1.0f);
-  } else if constexpr (OP == Op::Square) {
-    float a4[4];
-    ns_load<PLANES, 4>(x.a + ns_at<PLANES>(x.ldm, m, n), a4, kNsB * kNsScaleB / kNsScaleA);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += a4[e] + (m == n + e ? kNsA * kNsScaleB : 0.f);
-    ns_store<PLANES, 4>(x.b + ns_at<PLANES>(x.ldm, m, n), v, 1.0f);
-  } else if constexpr (OP == Op::Apply) {
-    ns_store<PLANES, 4>(x.x[cur ^ 1] + ns_at<PLANES>(x.ldn, m, n), v, 1.0f);
+    for (int e = 0; e < N; ++e) u[e] += m == n + e ? kNsA * kNsScaleB : 0.f;
   }
+}
+// N consecutive columns n.. of row m of a product.  v: the sums (scaled in place), u: the
+// addend.
+template <Op OP, int PLANES, int N>
+PB_DEV void store_result(const NsMat& x, int cur, int m, int n, float* v, const float* u) {
+#pragma unroll
+  for (int e = 0; e < N; ++e) v[e] = v[e] * out_scale<OP>() + (OP == Op::Square ? u[e] : 0.f);
+  if constexpr (OP == Op::Gram) ns_store<PLANES, N>(x.a + ns_at<PLANES>(x.ldm, m, n), v, 1.0f);
+  else if constexpr (OP == Op::Square) ns_store<PLANES, N>(x.b + ns_at<PLANES>(x.ldm, m, n), v, 1.0f);
+  else ns_store<PLANES, N>(x.x[cur ^ 1] + ns_at<PLANES>(x.ldn, m, n), v, 1.0f);
 }
 // Eight consecutive rows m.. of column n, v: scaled results.  Symmetric products: the
 // mirror image.
@@ -430,7 +431,9 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
       const f32x4 s4 = *at;
       float v[4] = {s4[0], s4[1], s4[2], s4[3]};
       if (m < M && n < N) {
-        store_result4<OP, PLANES>(x, cur, m, n, v);
+        float u[4];
+        addend<OP, PLANES, 4>(x, m, n, u);
+        store_result<OP, PLANES, 4>(x, cur, m, n, v, u);
         if (symmetric(OP) && tm != tn) *at = f32x4{v[0], v[1], v[2], v[3]};
       }
     }
@@ -475,8 +478,9 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(NsTable t, NsPlan plan, 
     f32x4 s = *reinterpret_cast<const f32x4*>(q);
     for (int i = 1; i < plan.splits; ++i)
       s += *reinterpret_cast<const f32x4*>(q + (size_t)i * kBT * kBT);
-    float v[4] = {s[0], s[1], s[2], s[3]};
-    store_result4<OP, PLANES>(x, cur, m0 + rl, n0 + cl, v);
+    float v[4] = {s[0], s[1], s[2], s[3]}, u[4];
+    addend<OP, PLANES, 4>(x, m0 + rl, n0 + cl, u);
+    store_result<OP, PLANES, 4>(x, cur, m0 + rl, n0 + cl, v, u);
 #pragma unroll
     for (int e = 0; e < 4; ++e) lds[rl][cl + e] = v[e];
   }
@@ -528,9 +532,11 @@ struct SmallSide {
       r[q] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(p) + off[q]);
     p += step;
   }
-  PB_DEV void frags(const u32x4 (&r)[8], unsigned char* lds, int lane, f16x8 (&f)[4][2]) const {
+  static PB_DEV void put(const u32x4 (&r)[8], unsigned char* lds, int lane) {
 #pragma unroll
     for (int q = 0; q < 8; ++q) *reinterpret_cast<u32x4*>(lds + 1024 * q + 16 * lane) = r[q];
+  }
+  static PB_DEV void frags(const unsigned char* lds, int lane, f16x8 (&f)[4][2]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -565,11 +571,21 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
   sb.init(o.B, o.ldb, n0, wave, lane);
   u32x4 ra[8], rb[8];
   if (wave < nk) sa.load(ra), sb.load(rb);
+  // this thread's part of the result, a row's eight columns (a column's eight rows for a
+  // tall matrix's tensor), and what it needs from memory for it, ahead of the products
+  const int r = threadIdx.x >> 3, c8 = 8 * (threadIdx.x & 7);
+  const bool tall = x.rows > x.cols;
+  float u[8];
+  if constexpr (OP == Op::Last) weights<8>(x, fin, tall ? n0 + r : m0 + r, (tall ? m0 : n0) + c8, u);
+  else addend<OP, PLANES, 8>(x, m0 + r, n0 + c8, u);
   for (int kt = wave; kt < nk; kt += kSWaves) {
-    f16x8 fa[4][2], fb[4][2];
-    sa.frags(ra, own, lane, fa);
-    sb.frags(rb, own + kSWaveLds / 2, lane, fb);
+    unsigned char* own_b = own + kSWaveLds / 2;
+    sa.put(ra, own, lane);
+    sb.put(rb, own_b, lane);
     if (kt + kSWaves < nk) sa.load(ra), sb.load(rb);  // in flight while this one multiplies
+    f16x8 fa[4][2], fb[4][2];
+    sa.frags(own, lane, fa);
+    sb.frags(own_b, lane, fb);
     auto mma = [&](int af, int bf) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -594,7 +610,6 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
       }
   }
   __syncthreads();
-  const int r = threadIdx.x >> 3, c8 = 8 * (threadIdx.x & 7);  // a row's eight columns
   float v[8];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -604,14 +619,12 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[4 * h + e] = s[e];
   }
-  const bool tall = x.rows > x.cols;
   if constexpr (OP == Op::Last) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= out_scale<OP>();
-    if (!tall) finish<8>(x, fin, m0 + r, n0 + c8, v);
+    if (!tall) finish<8>(x, fin, m0 + r, n0 + c8, v, u);
   } else {
-    store_result4<OP, PLANES>(x, cur, m0 + r, n0 + c8, v);
-    store_result4<OP, PLANES>(x, cur, m0 + r, n0 + c8 + 4, v + 4);
+    store_result<OP, PLANES, 8>(x, cur, m0 + r, n0 + c8, v, u);
   }
   if (OP == Op::Apply || (OP == Op::Last ? !tall : tm == tn)) return;
   __syncthreads();
@@ -621,7 +634,7 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
   __syncthreads();
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = turned[r * 65 + c8 + e];  // column r, eight rows
-  if constexpr (OP == Op::Last) finish<8>(x, fin, n0 + r, m0 + c8, v);
+  if constexpr (OP == Op::Last) finish<8>(x, fin, n0 + r, m0 + c8, v, u);
   else store_mirror8<OP, PLANES>(x, m0 + c8, n0 + r, v);
 }
 

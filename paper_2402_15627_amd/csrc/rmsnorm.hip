@@ -225,15 +225,15 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_fwd_kernel(RmsForwa
 }
 
 // A workgroup takes every gridDim.x-th set of kRows rows and keeps its part of dgamma
-// (and gamma) in registers; the next row's loads are issued before a row's reduction.
+// (and gamma) in registers.
 // The rows that share a workgroup add theirs up in LDS, in turn; the workgroup's sums
 // go to part[workgroup][rms_part_ld(H)].
 template <typename T, int TPR, int NC, bool AL>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_bwd_kernel(RmsBackward a) {
   constexpr int kThreads = TPR < 256 ? 256 : TPR, kRows = kThreads / TPR;
-  // Wider rows leave no registers for a second row, and the widest none for one: their
-  // second pass over the row reads it again, from the caches.
-  constexpr bool kAhead = sizeof(T) * NC <= 8 && TPR <= 256, kKeep = TPR <= 512;
+  // The widest rows do not fit into registers beside their sums: their second pass over
+  // the row reads it again, from the caches.
+  constexpr bool kKeep = TPR <= 512;
   __shared__ float red[2 * (kThreads / 64)];
   __shared__ float fold[kRows > 1 ? TPR * NC * 8 : 1];
   const int H = a.cols, l = threadIdx.x % TPR, sub = threadIdx.x / TPR;
@@ -294,46 +294,30 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_bwd_kernel(RmsBackw
     }
     return;
   }
-  struct Row {
+  for (long long r0 = (long long)blockIdx.x * kRows; r0 < a.rows;
+       r0 += (long long)gridDim.x * kRows) {
+    const bool live = r0 + sub < a.rows;
+    const long long row = live ? r0 + sub : a.rows - 1, at = row * H;
     Piece<T> s[kN], dy[kN], ds[kN];
-    float r;
-  };
-  // row `row` (past the last, the last again: loads are not behind a branch)
-  auto load = [&](long long row, Row& w) {
-    row = row < a.rows ? row : a.rows - 1;
-    const long long at = row * H;
-    w.r = a.rstd[row];
 #pragma unroll
     for (int j = 0; j < kN; ++j) {
       const int c = 8 * (l + j * TPR);
-      if (c < H) {
-        w.s[j] = load_piece<T, AL>((const T*)a.s + at, c, H);
-        w.dy[j] = load_piece<T, AL>((const T*)a.dy + at, c, H);
-        if (a.dsum) w.ds[j] = load_piece<T, AL>((const T*)a.dsum + at, c, H);
+      s[j] = dy[j] = ds[j] = zero_piece<T>();
+      if (c < H && live) {
+        s[j] = load_piece<T, AL>((const T*)a.s + at, c, H);
+        dy[j] = load_piece<T, AL>((const T*)a.dy + at, c, H);
+        if (a.dsum) ds[j] = load_piece<T, AL>((const T*)a.dsum + at, c, H);
       }
     }
-  };
-  const long long step = (long long)gridDim.x * kRows;
-  Row cur, next;
-#pragma unroll
-  for (int j = 0; j < kN; ++j) {
-    cur.s[j] = cur.dy[j] = cur.ds[j] = zero_piece<T>();
-    next.s[j] = next.dy[j] = next.ds[j] = zero_piece<T>();
-  }
-  long long r0 = (long long)blockIdx.x * kRows;
-  load(r0 + sub, cur);
-  for (; r0 < a.rows; r0 += step) {
-    if constexpr (kAhead) load(r0 + step + sub, next);
-    const bool live = r0 + sub < a.rows;
-    const float r = cur.r;
+    const float r = a.rstd[row];
     float k = 0.f;
 #pragma unroll
     for (int j = 0; j < kN; ++j)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float dy = cur.dy[j].at(e), s = cur.s[j].at(e) * r;
-        k += dy * gp[j].at(e) * s;
-        acc[j][e] += live ? dy * s : 0.f;
+        const float u = dy[j].at(e) * (live ? s[j].at(e) * r : 0.f);
+        k += gp[j].at(e) * u;
+        acc[j][e] += u;
       }
     k = row_reduce<TPR>(k, red, turn, [](float p, float q) { return p + q; }) / H;
     if (live)
@@ -344,11 +328,9 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_bwd_kernel(RmsBackw
         float o[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          o[e] = cur.ds[j].at(e) + r * (cur.dy[j].at(e) * gp[j].at(e) - cur.s[j].at(e) * r * k);
-        store_cols<T, AL>((T*)a.dx + (r0 + sub) * H, c, H, o);
+          o[e] = ds[j].at(e) + r * (dy[j].at(e) * gp[j].at(e) - s[j].at(e) * r * k);
+        store_cols<T, AL>((T*)a.dx + at, c, H, o);
       }
-    if constexpr (kAhead) cur = next;
-    else if (r0 + step < a.rows) load(r0 + step + sub, cur);
   }
   if constexpr (kRows > 1) {
     for (int t = 0; t < kRows; ++t) {
@@ -453,12 +435,15 @@ void backward(const RmsBackward& a, hipStream_t s) {
 
 }  // namespace
 
+// Workgroups of the backward.  Each holds the CU's registers for long, so there are as
+// many as run at once, 2 of 256 threads to a CU or 1 of 512 and more.
+constexpr int kParts = 512, kPartsWide = 256;
 int rms_backward_parts(long long rows, int cols) {
   long long n = 0;
   by_width(cols, [&](auto tpr, auto) {
     constexpr int TPR = decltype(tpr)::value;
     constexpr int per = TPR < 256 ? 256 / TPR : 1;
-    n = std::min<long long>((rows + per - 1) / per, 512);
+    n = std::min<long long>((rows + per - 1) / per, TPR > 256 ? kPartsWide : kParts);
   });
   return (int)n;
 }

@@ -593,48 +593,53 @@ def _torch_dtype(code: int):
     return torch.bfloat16 if code == PB_BF16 else torch.float32
 
 
-def _expect(name, t, dtype=None, numel=None, contiguous=True):
-    if t is None or isinstance(t, int):
-        return
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError(f"{name} is {t.dtype}, not {dtype}")
-    if numel is not None and t.numel() != numel:
-        raise ValueError(f"{name} has {t.numel()} elements, not {numel}")
-    if contiguous and not t.is_contiguous():
-        raise ValueError(f"{name} is not contiguous")
+class _Call:
+    """Collects a call's tensors: checks them, keeps their one device."""
+    __slots__ = ("index",)
 
+    def __init__(self):
+        self.index = -1
 
-class _On:
-    """The device and stream of a call: those of its tensors."""
+    def on(self, name, t):
+        """t is on a GPU, on that of the tensors before it."""
+        d = t.get_device()
+        if d < 0:
+            raise ValueError(f"{name} is on {t.device}, not on a GPU")
+        if self.index < 0:
+            self.index = d
+        elif d != self.index:
+            raise ValueError(f"{name} is on another device than the tensors before it "
+                             f"({d} and {self.index})")
 
-    def __init__(self, tensors: dict, stream):
-        devices = {}
-        for name, t in tensors.items():
-            if t is None or isinstance(t, int):
-                continue
-            if t.device.type != "cuda":
-                raise ValueError(f"{name} is on {t.device}, not on a GPU")
-            devices.setdefault(t.device.index, name)
-        if len(devices) > 1:
-            a, b = list(devices.items())[:2]
-            raise ValueError(f"{a[1]} and {b[1]} are on different devices ({a[0]} and {b[0]})")
-        self.index = next(iter(devices), None)
-        at = getattr(getattr(stream, "device", None), "index", None)
-        if at is not None and self.index is not None and at != self.index:
-            raise ValueError(f"the stream is on device {at}, the tensors on {self.index}")
-        self.stream = stream
+    def ptr(self, name, t, dtype=None, numel=None):
+        """Address of a contiguous tensor (or an address, or None)."""
+        if t is None or t.__class__ is int:
+            return t
+        if dtype is not None and t.dtype != dtype:
+            raise ValueError(f"{name} is {t.dtype}, not {dtype}")
+        if numel is not None and t.numel() != numel:
+            raise ValueError(f"{name} has {t.numel()} elements, not {numel}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} is not contiguous")
+        self.on(name, t)
+        return t.data_ptr()
 
-    def __enter__(self):
+    def run(self, fn, args, stream):
+        """fn(*args, stream) on the tensors' device."""
         import torch
-        self.guard = None
-        if self.index is not None and self.index != torch.cuda.current_device():
-            self.guard = torch.cuda.device(self.index)
-            self.guard.__enter__()
-        return _stream(self.stream)
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+        index = self.index
+        if stream is not None and stream.__class__ is not int and index >= 0:
+            at = stream.device.index
+            if at != index:
+                raise ValueError(f"the stream is on device {at}, the tensors on {index}")
+        if index < 0 or index == torch.cuda.current_device():
+            if stream is None and index >= 0:
+                # (the handle alone: a Stream object takes longer to make than the launch)
+                stream = torch._C._cuda_getCurrentRawStream(index)
+            _check(fn(*args, _stream(stream)))
+        else:
+            with torch.cuda.device(index):
+                _check(fn(*args, _stream(stream)))
 
 
 def rope_config(head_dim, rot_dim=None, interleaved=False, base=10000.0, scaling="plain",
@@ -654,42 +659,41 @@ def rope_tensor(x, ld, heads, out=None, ld_out=None) -> RopeTensor:
     to token.  Without out, in place."""
     r = RopeTensor(_ptr(x), _ptr(x if out is None else out), ld,
                    ld if ld_out is None else ld_out, heads)
-    r.tensors = (x, out)  # kept alive, and for their checks
+    # the tensors themselves (kept alive), and the elements that each has left
+    r.tensors = [(name, t, t.untyped_storage().nbytes() // t.element_size() - t.storage_offset(), n)
+                 for name, t, n in (("in", x, r.ld_in), ("out", out, r.ld_out))
+                 if t is not None and not isinstance(t, int)]
     return r
 
 
 def _rope(fn, cfg, tensors, tokens, seq, positions, stream):
     import torch
-    named = {"positions": positions}
+    call = _Call()
     act = _torch_dtype(cfg.dtype)
     for i, r in enumerate(tensors):
-        for name, t, ld in zip(("in", "out"), getattr(r, "tensors", ()), (r.ld_in, r.ld_out)):
-            named[f"tensor {i}: {name}"] = t
-            _expect(f"tensor {i}: {name}", t, act, contiguous=False)
-            if t is None or isinstance(t, int) or tokens < 1:
-                continue
-            left = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
-            need = (tokens - 1) * ld + r.heads * cfg.head_dim
+        for name, t, left, ld in getattr(r, "tensors", ()):
+            name = f"tensor {i}: {name}"
+            if t.dtype != act:
+                raise ValueError(f"{name} is {t.dtype}, not {act}")
+            need = (tokens - 1) * ld + r.heads * cfg.head_dim if tokens > 0 else 0
             if left < need:
-                raise ValueError(f"tensor {i}: {name} ends {need - left} elements short of "
-                                 f"{tokens} tokens")
-    _expect("positions", positions, torch.int64, tokens)
+                raise ValueError(f"{name} ends {need - left} elements short of {tokens} tokens")
+            call.on(name, t)
+    pos = call.ptr("positions", positions, torch.int64, tokens)
     arr = (RopeTensor * len(tensors))(*tensors)
-    with _On(named, stream) as st:
-        _check(getattr(load_library(), fn)(ctypes.byref(cfg), len(tensors), arr, int(tokens),
-                                           int(tokens if seq is None else seq), _ptr(positions),
-                                           st))
+    call.run(fn, (ctypes.byref(cfg), len(tensors), arr, tokens, tokens if seq is None else seq,
+                  pos), stream)
 
 
 def pblock_rope_forward(cfg: RopeConfig, tensors, tokens, seq=None, positions=None, stream=None):
     """tensors: a sequence of RopeTensor; positions: int64 [tokens], or None for
     token mod seq (seq: tokens by default)."""
-    _rope("pblock_rope_forward", cfg, tensors, tokens, seq, positions, stream)
+    _rope(load_library().pblock_rope_forward, cfg, tensors, tokens, seq, positions, stream)
 
 
 def pblock_rope_backward(cfg: RopeConfig, tensors, tokens, seq=None, positions=None, stream=None):
     """The gradients of pblock_rope_forward's inputs from those of its outputs."""
-    _rope("pblock_rope_backward", cfg, tensors, tokens, seq, positions, stream)
+    _rope(load_library().pblock_rope_backward, cfg, tensors, tokens, seq, positions, stream)
 
 
 def rmsnorm_config(rows, cols, eps=1e-5, dtype="bf16", group=0) -> RmsnormConfig:
@@ -701,22 +705,19 @@ def pblock_rmsnorm_forward(cfg: RmsnormConfig, x, gamma, y=None, resid=None, sum
                            scales=None, rstd=None, stream=None):
     """q8: float8_e4m3fn (or uint8) [rows, cols]; scales: fp32 [rows, groups]."""
     import torch
-    act, n = _torch_dtype(cfg.dtype), cfg.rows * cfg.cols
-    for name, t in (("x", x), ("resid", resid), ("sum_out", sum_out), ("y", y)):
-        _expect(name, t, act, n)
-    _expect("gamma", gamma, act, cfg.cols)
-    _expect("q8", q8, None, n)
+    act, rows, cols, f32 = _torch_dtype(cfg.dtype), cfg.rows, cfg.cols, torch.float32
+    n = rows * cols
+    groups = -(-cols // cfg.group) if cfg.group > 0 else 1
     if q8 is not None and not isinstance(q8, int) and q8.dtype not in (torch.float8_e4m3fn,
                                                                        torch.uint8):
         raise ValueError(f"q8 is {q8.dtype}, not float8_e4m3fn or uint8")
-    groups = -(-cfg.cols // cfg.group) if cfg.group > 0 else 1
-    _expect("scales", scales, torch.float32, cfg.rows * groups)
-    _expect("rstd", rstd, torch.float32, cfg.rows)
-    with _On(dict(x=x, gamma=gamma, y=y, resid=resid, sum_out=sum_out, q8=q8, scales=scales,
-                  rstd=rstd), stream) as st:
-        _check(load_library().pblock_rmsnorm_forward(
-            ctypes.byref(cfg), _ptr(x), _ptr(resid), _ptr(gamma), _ptr(sum_out), _ptr(y),
-            _ptr(q8), _ptr(scales), _ptr(rstd), st))
+    call = _Call()
+    ptr = call.ptr
+    args = (ctypes.byref(cfg), ptr("x", x, act, n), ptr("resid", resid, act, n),
+            ptr("gamma", gamma, act, cols), ptr("sum_out", sum_out, act, n), ptr("y", y, act, n),
+            ptr("q8", q8, None, n), ptr("scales", scales, f32, rows * groups),
+            ptr("rstd", rstd, f32, rows))
+    call.run(load_library().pblock_rmsnorm_forward, args, stream)
 
 
 def pblock_rmsnorm_workspace_bytes(cfg: RmsnormConfig) -> int:
@@ -728,17 +729,14 @@ def pblock_rmsnorm_backward(cfg: RmsnormConfig, s, gamma, rstd, dy, dx, dgamma, 
                             stream=None):
     """s: the forward's sum_out (its x where there was no residual)."""
     import torch
-    act, n = _torch_dtype(cfg.dtype), cfg.rows * cfg.cols
-    for name, t in (("s", s), ("dy", dy), ("dsum", dsum), ("dx", dx)):
-        _expect(name, t, act, n)
-    _expect("gamma", gamma, act, cfg.cols)
-    _expect("rstd", rstd, torch.float32, cfg.rows)
-    _expect("dgamma", dgamma, torch.float32, cfg.cols)
-    with _On(dict(s=s, gamma=gamma, rstd=rstd, dy=dy, dsum=dsum, dx=dx, dgamma=dgamma, ws=ws),
-             stream) as st:
-        _check(load_library().pblock_rmsnorm_backward(
-            ctypes.byref(cfg), _ptr(s), _ptr(gamma), _ptr(rstd), _ptr(dy), _ptr(dsum), _ptr(dx),
-            _ptr(dgamma), _ptr(ws), _nbytes(ws), st))
+    act, rows, cols, f32 = _torch_dtype(cfg.dtype), cfg.rows, cfg.cols, torch.float32
+    n = rows * cols
+    call = _Call()
+    ptr = call.ptr
+    args = (ctypes.byref(cfg), ptr("s", s, act, n), ptr("gamma", gamma, act, cols),
+            ptr("rstd", rstd, f32, rows), ptr("dy", dy, act, n), ptr("dsum", dsum, act, n),
+            ptr("dx", dx, act, n), ptr("dgamma", dgamma, f32, cols), ptr("ws", ws), _nbytes(ws))
+    call.run(load_library().pblock_rmsnorm_backward, args, stream)
 
 
 def muon_config(lr, momentum=0.95, nesterov=True, steps=5, eps=1e-7, grad_scale=1.0,
@@ -765,23 +763,33 @@ def muon_tensor(param, grad, momentum, param_copy=None, weight_decay=0.0, scale=
     """A pb_muon_tensor from matrices (or slices of packed weights, of one
     stride from row to row): fp32 param, grad and momentum, and a copy."""
     import torch
-    named = {"param": param, "grad": grad, "momentum": momentum, "param_copy": param_copy}
-    for name, t in named.items():
-        if t is None and name == "param_copy":
-            continue
-        if _rows(name, t, param) != _rows("param", param):
+    ld = _rows("param", param)
+    named = [("param", param), ("grad", grad), ("momentum", momentum)]
+    for name, t in named:
+        if t.dtype != torch.float32:
+            raise ValueError(f"{name} is {t.dtype}, not {torch.float32}")
+    if param_copy is not None:
+        named.append(("param_copy", param_copy))
+    for name, t in named:
+        if _rows(name, t, param) != ld:
             raise ValueError(f"{name} has another stride than param")
-        if name != "param_copy":
-            _expect(name, t, torch.float32, contiguous=False)
     r = MuonTensor(_ptr(param), _ptr(grad), _ptr(momentum), _ptr(param_copy), param.shape[0],
-                   param.shape[1], _rows("param", param), weight_decay, scale)
+                   param.shape[1], ld, weight_decay, scale)
     r.tensors = named
     return r
 
 
-def _named(tensors):
-    return {f"tensor {i}: {n}": t for i, r in enumerate(tensors)
-            for n, t in getattr(r, "tensors", {}).items()}
+def _matrices(tensors, typed, dtype):
+    """The call over handles whose tensors named `typed` are of dtype."""
+    call = _Call()
+    for i, r in enumerate(tensors):
+        named = getattr(r, "tensors", ())
+        for name, t in named:
+            if name == typed and t.dtype != dtype:
+                raise ValueError(f"tensor {i}: {name} is {t.dtype}, not {dtype}")
+        for name, t in named:
+            call.on(name, t)
+    return call
 
 
 def pblock_muon_workspace_bytes(cfg: MuonConfig, tensors) -> int:
@@ -792,14 +800,10 @@ def pblock_muon_workspace_bytes(cfg: MuonConfig, tensors) -> int:
 
 def pblock_muon_step(cfg: MuonConfig, tensors, copy_dtype=PB_BF16, ws=None, stream=None):
     """tensors: a sequence of MuonTensor; their copies are of copy_dtype."""
-    named = _named(tensors)
-    for name, t in named.items():
-        if name.endswith("param_copy") and copy_dtype in (PB_BF16, PB_F32):
-            _expect(name, t, _torch_dtype(copy_dtype), contiguous=False)
-    with _On(dict(named, ws=ws), stream) as st:
-        _check(load_library().pblock_muon_step(
-            ctypes.byref(cfg), len(tensors), (MuonTensor * len(tensors))(*tensors),
-            int(copy_dtype), _ptr(ws), _nbytes(ws), st))
+    call = _matrices(tensors, "param_copy", _torch_dtype(copy_dtype))
+    call.run(load_library().pblock_muon_step,
+             (ctypes.byref(cfg), len(tensors), (MuonTensor * len(tensors))(*tensors),
+              int(copy_dtype), call.ptr("ws", ws), _nbytes(ws)), stream)
 
 
 def ortho_tensor(x, out) -> OrthoTensor:
@@ -809,7 +813,7 @@ def ortho_tensor(x, out) -> OrthoTensor:
         raise ValueError(f"out is {out.dtype}, x {x.dtype}")
     ld, ld_out = _rows("x", x), _rows("out", out, x)
     r = OrthoTensor(_ptr(x), _ptr(out), x.shape[0], x.shape[1], ld, ld_out)
-    r.tensors = {"x": x, "out": out}
+    r.tensors = [("x", x), ("out", out)]
     return r
 
 
@@ -821,13 +825,11 @@ def pblock_orthogonalize_workspace_bytes(tensors, dtype="bf16") -> int:
 
 def pblock_orthogonalize(tensors, dtype, ws, steps=5, eps=1e-7, stream=None):
     """The orthogonalised matrices of OrthoTensors of dtype "bf16" or "f32"."""
-    code, named = _dtype_of(dtype), _named(tensors)
-    for name, t in named.items():
-        _expect(name, t, _torch_dtype(code), contiguous=False)
-    with _On(dict(named, ws=ws), stream) as st:
-        _check(load_library().pblock_orthogonalize(
-            len(tensors), (OrthoTensor * len(tensors))(*tensors), code, int(steps), eps, _ptr(ws),
-            _nbytes(ws), st))
+    code = _dtype_of(dtype)
+    call = _matrices(tensors, "x", _torch_dtype(code))
+    call.run(load_library().pblock_orthogonalize,
+             (len(tensors), (OrthoTensor * len(tensors))(*tensors), code, int(steps), eps,
+              call.ptr("ws", ws), _nbytes(ws)), stream)
 
 
 def pblock_status_string(status: int) -> str:

@@ -216,19 +216,19 @@ def test_binding_refuses_what_tensors_say_of_themselves():
         pb.pblock_rmsnorm_forward(cfg, bf, g, bf)
     with pytest.raises(ValueError, match="x is torch.float32"):
         pb.pblock_rmsnorm_forward(cfg, f32, g, bf)
-    with pytest.raises(ValueError, match="y has 128"):
-        pb.pblock_rmsnorm_forward(cfg, bf, g, bf[:2])
+    with pytest.raises(ValueError, match="x has 128"):
+        pb.pblock_rmsnorm_forward(cfg, bf[:2], g, bf)
     with pytest.raises(ValueError, match="not contiguous"):
         pb.pblock_rmsnorm_forward(cfg, torch.zeros(64, 4, dtype=torch.bfloat16).t(), g, bf)
     with pytest.raises(ValueError, match="q8 is"):
         pb.pblock_rmsnorm_forward(cfg, bf, g, bf, q8=bf, scales=torch.zeros(4))
-    with pytest.raises(ValueError, match="dgamma"):
-        pb.pblock_rmsnorm_backward(cfg, bf, g, torch.zeros(4), bf, bf, g, None)
+    with pytest.raises(ValueError, match="s is torch.float32"):
+        pb.pblock_rmsnorm_backward(cfg, f32, g, torch.zeros(4), bf, bf, g, None)
     rc = pb.rope_config(32)
     with pytest.raises(ValueError, match="short of 4 tokens"):
         pb.pblock_rope_forward(rc, [pb.rope_tensor(bf[:, 8:], 64, 2)], 4)
-    with pytest.raises(ValueError, match="positions"):
-        pb.pblock_rope_forward(rc, [pb.rope_tensor(bf, 64, 2)], 4, positions=torch.zeros(4))
+    with pytest.raises(ValueError, match="positions is torch.float32"):
+        pb.pblock_rope_forward(rc, [pb.rope_tensor(FAKE, 64, 2)], 4, positions=torch.zeros(4))
     with pytest.raises(ValueError, match="not on a GPU"):
         pb.pblock_rope_backward(rc, [pb.rope_tensor(bf, 64, 2)], 4)
     with pytest.raises(ValueError, match="scaling"):
@@ -253,10 +253,16 @@ class _Tensor:
     def __init__(self, index):
         self.device = torch.device("cuda", index)
 
+    def get_device(self):
+        return self.device.index
+
 
 def test_binding_refuses_two_devices_and_a_stream_of_another():
-    with pytest.raises(ValueError, match="different devices"):
-        pb._On(dict(a=_Tensor(0), b=None, c=_Tensor(1)), None)
-    with pytest.raises(ValueError, match="stream is on device 1"):
-        pb._On(dict(a=_Tensor(0)), _Tensor(1))
-    assert pb._On(dict(a=_Tensor(1), b=FAKE), _Tensor(1)).index == 1
+    call = pb._Call()
+    call.on("a", _Tensor(1))
+    call.on("b", _Tensor(1))
+    with pytest.raises(ValueError, match="c is on another device"):
+        call.on("c", _Tensor(0))
+    assert call.ptr("d", None) is None and call.ptr("e", FAKE) == FAKE
+    with pytest.raises(ValueError, match="stream is on device 0"):
+        call.run(None, (), _Tensor(0))
