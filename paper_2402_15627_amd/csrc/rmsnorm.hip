@@ -66,6 +66,8 @@ PB_DEV Piece<T> zero_piece() {
   for (int k = 0; k < Piece<T>::kWords; ++k) p.w[k] = u32x4{0, 0, 0, 0};
   return p;
 }
+// (Past the caches' retention, where aligned: 62 -> 60 us for the forward of 8192 x 5120,
+// 41 -> 36 of 2048 x 12288.)
 template <typename T, bool AL>
 PB_DEV void store_cols(T* row, int c, int H, const float* v) {
   if (AL || c + 8 <= H) {
@@ -76,7 +78,7 @@ PB_DEV void store_cols(T* row, int c, int H, const float* v) {
       for (int e = 0; e < 4; ++e)
         w[e] = sizeof(T) == 2 ? pack_bf2(v[2 * e], v[2 * e + 1]) : __float_as_uint(v[4 * k + e]);
       T* at = row + c + 8 / Piece<T>::kWords * k;
-      if constexpr (AL) *reinterpret_cast<u32x4*>(at) = w;
+      if constexpr (AL) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(at));
       else __builtin_memcpy(at, &w, 16);
     }
   } else {
@@ -209,7 +211,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_fwd_kernel(RmsForwa
         if (live && c < H) {
           uint8_t* q = a.q8 + at + c;
           if (AL || c + 8 <= H) {
-            if constexpr (AL) *reinterpret_cast<u32x2*>(q) = u32x2{w[0], w[1]};
+            if constexpr (AL) __builtin_nontemporal_store(u32x2{w[0], w[1]}, reinterpret_cast<u32x2*>(q));
             else __builtin_memcpy(q, w, 8);
           } else {
 #pragma unroll
