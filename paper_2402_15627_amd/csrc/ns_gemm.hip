@@ -24,6 +24,8 @@
 //   - 64 x 64 tiles with K split over the waves of a workgroup, for small grids.
 // X, A and B are padded to multiples of 64 with zeros, so a K-tile is never partial;
 // rows and columns past the end of a tile read the last ones and are not stored.
+#include <math.h>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -455,29 +457,31 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
   }
 }
 
-// Sum of a split tile's slices, in slice order, and its result: 64 x 64 of the tile per
-// workgroup.
-template <Op OP, int PLANES>
+// Sum of a split T x T tile's slices, in slice order, and its result: 64 x 64 of the tile
+// per workgroup.
+template <Op OP, int PLANES, int T>
 __global__ __launch_bounds__(256) void ns_reduce_kernel(NsTable t, NsPlan plan, int cur,
                                                         const float* __restrict__ part) {
   __shared__ float lds[64][65];
-  const int tail = blockIdx.x >> 4, sub = blockIdx.x & 15, tile = plan.n_full + tail;
-  const int place = place_of(plan, t.count, tile);
+  constexpr int kSub = T / 64;  // blocks across a tile
+  const int tail = blockIdx.x / (kSub * kSub), sub = blockIdx.x % (kSub * kSub);
+  const int tile = plan.n_full + tail, place = place_of(plan, t.count, tile);
   const NsMat& x = t.mat[plan.mat[place]];
   int tm, tn;
-  tile_at<OP, kBT>(x, tile - plan.first[place], tm, tn);
-  const int r0 = (sub >> 2) * 64, c0 = (sub & 3) * 64, cl = 4 * (threadIdx.x & 15);
-  const int m0 = tm * kBT + r0, n0 = tn * kBT + c0, N = symmetric(OP) ? x.m : x.n;
+  tile_at<OP, T>(x, tile - plan.first[place], tm, tn);
+  const int r0 = sub / kSub * 64, c0 = sub % kSub * 64, cl = 4 * (threadIdx.x & 15);
+  const int m0 = tm * T + r0, n0 = tn * T + c0, N = symmetric(OP) ? x.m : x.n;
   // (M and N are multiples of 64: the 64 x 64 block is inside or outside whole)
   if (m0 >= x.m || n0 >= N) return;
-  const float* p = part + (size_t)tail * plan.splits * (kBT * kBT) + c0 + cl;
+  const float* p = part + (size_t)tail * plan.splits * (T * T) + c0 + cl;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const int rl = (threadIdx.x >> 4) + 16 * k;
-    const float* q = p + (r0 + rl) * kBT;
+    const float* q = p + (r0 + rl) * T;
     f32x4 s = *reinterpret_cast<const f32x4*>(q);
+#pragma unroll 4
     for (int i = 1; i < plan.splits; ++i)
-      s += *reinterpret_cast<const f32x4*>(q + (size_t)i * kBT * kBT);
+      s += *reinterpret_cast<const f32x4*>(q + (size_t)i * T * T);
     float v[4] = {s[0], s[1], s[2], s[3]}, u[4];
     addend<OP, PLANES, 4>(x, m0 + rl, n0 + cl, u);
     store_result<OP, PLANES, 4>(x, cur, m0 + rl, n0 + cl, v, u);
@@ -546,7 +550,7 @@ struct SmallSide {
 
 template <Op OP, int PLANES>
 __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan plan, NsFinish fin,
-                                                              int cur) {
+                                                              int cur, float* __restrict__ part) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   constexpr bool BK = symmetric(OP);
   const Item it = item_of(plan, t.count, blockIdx.x, gridDim.x);
@@ -557,7 +561,13 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
   const Operands o = operands<OP, PLANES>(x, cur);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int nk = o.K / kK<PLANES>;
+  // K-tiles kt0 .. kt0 + nk - 1: the slice's
+  int kt0 = 0, nk = o.K / kK<PLANES>;
+  if (it.slice >= 0) {
+    const int chunk = (nk + plan.splits - 1) / plan.splits;
+    kt0 = min(nk, it.slice * chunk);
+    nk = min(nk, kt0 + chunk) - kt0;
+  }
   unsigned char* own = smem + wave * kSWaveLds;
 
   f32x4 acc[4][4];
@@ -567,8 +577,8 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
     for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   SmallSide<true, PLANES> sa;
   SmallSide<BK, PLANES> sb;
-  sa.init(o.A, o.lda, m0, wave, lane);
-  sb.init(o.B, o.ldb, n0, wave, lane);
+  sa.init(o.A, o.lda, m0, kt0 + wave, lane);
+  sb.init(o.B, o.ldb, n0, kt0 + wave, lane);
   u32x4 ra[8], rb[8];
   if (wave < nk) sa.load(ra), sb.load(rb);
   // this thread's part of the result, a row's eight columns (a column's eight rows for a
@@ -577,7 +587,7 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
   const bool tall = x.rows > x.cols;
   float u[8];
   if constexpr (OP == Op::Last) weights<8>(x, fin, tall ? n0 + r : m0 + r, (tall ? m0 : n0) + c8, u);
-  else addend<OP, PLANES, 8>(x, m0 + r, n0 + c8, u);
+  else if (it.slice < 0) addend<OP, PLANES, 8>(x, m0 + r, n0 + c8, u);
   for (int kt = wave; kt < nk; kt += kSWaves) {
     unsigned char* own_b = own + kSWaveLds / 2;
     sa.put(ra, own, lane);
@@ -599,7 +609,7 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
 
   // acc[i][j][e] is row 16 i + (lane & 15), column 16 j + 4 (lane >> 4) + e; 16-byte
   // chunks XOR-ed by the row
-  const int waves = min(kSWaves, nk);
+  const int waves = max(1, min(kSWaves, nk));
   if (wave < waves) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -618,6 +628,12 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
     for (int w = 1; w < waves; ++w) s += *reinterpret_cast<const f32x4*>(smem + w * kSWaveLds + at);
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[4 * h + e] = s[e];
+  }
+  if (it.slice >= 0) {
+    float* p = part + ((size_t)(it.tile - plan.n_full) * plan.splits + it.slice) * (kST * kST) +
+               r * kST + c8;
+    store8<float>(p, v);
+    return;
   }
   if constexpr (OP == Op::Last) {
 #pragma unroll
@@ -648,11 +664,11 @@ int tiles_of(Op op, const NsMat& x, int t) {
 // prologue, epilogue), in us.
 template <int PLANES>
 constexpr double kStepUs = PLANES == 2 ? 1.9 : 1.65;
-constexpr double kTileUs = 16.0, kSplitUs = 9.0;
+constexpr double kTileUs = 14.0, kSplitUs = 9.0;
 // The same for the 64 x 64 tiles, a step being a K-tile of each of the eight waves.
 template <int PLANES>
 constexpr double kSmallStepUs = PLANES == 2 ? 2.05 : 1.9;
-constexpr double kSmallTileUs = 2.5, kSmallUs = 5.0;
+constexpr double kSmallTileUs = 2.5, kSmallUs = 5.0, kSmallSplitUs = 7.0;
 
 struct Choice {
   bool big;  // 256 x 256 tiles
@@ -660,23 +676,24 @@ struct Choice {
   int tail;  // tiles cut along K
 };
 
-// Whole rounds of 256 x 256 tiles, and the tiles of the last, partial round (or of all,
-// where they do not fill one) cut along K where that is estimated to end sooner.
+// The tiles that are estimated to end sooner: 256 x 256, whole rounds of them and the
+// tiles of the last, partial round (or of all, where they do not fill one) cut along K;
+// or 64 x 64, all of them cut where they are few and K is long.
 template <int PLANES>
 Choice choose(Op op, const NsTable& t) {
-  Choice c{};
+  NsPlan plan{};
   auto len = [&](int i) { return (op == Op::Gram ? t.mat[i].n : t.mat[i].m) / kK<PLANES>; };
+  auto small_len = [&](int i) { return (len(i) + kSWaves - 1) / kSWaves; };
   for (int i = 0; i < t.count; ++i) {  // the longest K first
     int k = i;
-    for (; k > 0 && len(c.plan.mat[k - 1]) < len(i); --k) c.plan.mat[k] = c.plan.mat[k - 1];
-    c.plan.mat[k] = i;
+    for (; k > 0 && len(plan.mat[k - 1]) < len(i); --k) plan.mat[k] = plan.mat[k - 1];
+    plan.mat[k] = i;
   }
   auto count = [&](int size) {
     for (int i = 0; i < t.count; ++i)
-      c.plan.first[i + 1] = c.plan.first[i] + tiles_of(op, t.mat[c.plan.mat[i]], size);
-    return c.plan.first[t.count];
+      plan.first[i + 1] = plan.first[i] + tiles_of(op, t.mat[plan.mat[i]], size);
+    return plan.first[t.count];
   };
-  const int tiles = count(kBT);
   // Steps until the last item ends, and rounds, the items (longest first) taken kCUs at
   // a time; l(i): steps of a tile of matrix i, those past n_full in `splits` items
   struct Rounds {
@@ -686,9 +703,9 @@ Choice choose(Op op, const NsTable& t) {
     Rounds r{0, 0};
     long long at = 0;  // items so far
     for (int i = 0; i < t.count; ++i) {
-      const int nk = l(c.plan.mat[i]), cut = (nk + splits - 1) / splits;
-      const int whole = std::max(0, std::min(c.plan.first[i + 1], n_full) - c.plan.first[i]);
-      const int rest = c.plan.first[i + 1] - c.plan.first[i] - whole;
+      const int nk = l(plan.mat[i]), cut = (nk + splits - 1) / splits;
+      const int whole = std::max(0, std::min(plan.first[i + 1], n_full) - plan.first[i]);
+      const int rest = plan.first[i + 1] - plan.first[i] - whole;
       for (int part = 0; part < 2; ++part) {
         const long long n = part ? (long long)rest * splits : whole;
         const long long starts = (at + n + kCUs - 1) / kCUs - r.count;  // rounds that begin here
@@ -699,27 +716,32 @@ Choice choose(Op op, const NsTable& t) {
     }
     return r;
   };
-  double best = kTileUs + kStepUs<PLANES> * rounds(len, tiles, 1).steps;
-  c.plan.n_full = tiles;
-  c.plan.splits = 1;
+  Choice c{};
+  double best = INFINITY;
+  auto offer = [&](bool big, int n_full, int splits, int tail, double us) {
+    if (us >= best) return;
+    best = us;
+    c.big = big;
+    c.plan = plan;
+    c.plan.n_full = n_full;
+    c.plan.splits = splits;
+    c.tail = tail;
+  };
+  int tiles = count(kBT);
+  offer(true, tiles, 1, 0, kTileUs + kStepUs<PLANES> * rounds(len, tiles, 1).steps);
   for (int keep = tiles / kCUs; keep >= std::max(0, tiles / kCUs - 1); --keep) {
-    const int tail = tiles - keep * kCUs;
-    for (int s = 2; tail > 0 && s <= 16 && (long long)tail * s <= 4 * kCUs; ++s) {
-      const double us =
-          kTileUs + kStepUs<PLANES> * rounds(len, keep * kCUs, s).steps + kSplitUs + 0.1 * tail * s;
-      if (us < best) best = us, c.plan.n_full = keep * kCUs, c.plan.splits = s, c.tail = tail;
-    }
+    const int full = keep * kCUs, tail = tiles - full;
+    for (int s = 2; tail > 0 && s <= 16 && (long long)tail * s <= 4 * kCUs; ++s)
+      offer(true, full, s, tail,
+            kTileUs + kStepUs<PLANES> * rounds(len, full, s).steps + kSplitUs + 0.05 * tail * s);
   }
-  const int small = count(kST);
-  const Rounds r = rounds([&](int i) { return (len(i) + kSWaves - 1) / kSWaves; }, small, 1);
-  const double est = kSmallUs + kSmallTileUs * r.count + kSmallStepUs<PLANES> * r.steps;
-  c.big = best < est;
-  if (c.big) {
-    count(kBT);
-  } else {
-    c.plan.n_full = small;
-    c.plan.splits = 1;
-    c.tail = 0;
+  tiles = count(kST);
+  for (int s = 1; s <= 16 && (s == 1 || (op == Op::Gram && (long long)tiles * s <= 2 * kCUs)); ++s) {
+    const int full = s == 1 ? tiles : 0;
+    const Rounds r = rounds(small_len, full, s);
+    offer(false, full, s, tiles - full,
+          kSmallUs + kSmallTileUs * r.count + kSmallStepUs<PLANES> * r.steps +
+              (s > 1 ? kSmallSplitUs + 0.01 * tiles * s : 0.0));
   }
   return c;
 }
@@ -728,11 +750,15 @@ template <Op OP, int PLANES>
 void launch(const NsTable& t, const NsFinish& fin, int cur, const Choice& c, float* part,
             hipStream_t s) {
   if (!c.big) {
-    ns_gemm_small<OP, PLANES><<<c.plan.n_full, kSThreads, kSLds, s>>>(t, c.plan, fin, cur);
+    ns_gemm_small<OP, PLANES><<<c.plan.n_full + c.tail * c.plan.splits, kSThreads, kSLds, s>>>(
+        t, c.plan, fin, cur, part);
+    if constexpr (OP == Op::Gram)
+      if (c.tail)
+        ns_reduce_kernel<OP, PLANES, kST><<<c.tail, 256, 0, s>>>(t, c.plan, cur, part);
   } else if constexpr (OP != Op::Last) {
     ns_gemm_big<OP, PLANES><<<c.plan.n_full + c.tail * c.plan.splits, kBThreads, kBLds, s>>>(
         t, c.plan, cur, part);
-    if (c.tail) ns_reduce_kernel<OP, PLANES><<<c.tail * 16, 256, 0, s>>>(t, c.plan, cur, part);
+    if (c.tail) ns_reduce_kernel<OP, PLANES, kBT><<<c.tail * 16, 256, 0, s>>>(t, c.plan, cur, part);
   }
 }
 
@@ -750,11 +776,11 @@ bool iterate(const NsTable& t, const NsFinish& fin, int steps, float* part, hipS
 }
 
 template <int PLANES>
-size_t partial_tiles(const NsTable& t) {
+size_t partial_floats(const NsTable& t) {
   size_t n = 0;
   for (Op op : {Op::Gram, Op::Square, Op::Apply}) {
     const Choice c = choose<PLANES>(op, t);
-    n = std::max(n, (size_t)c.tail * c.plan.splits);
+    n = std::max(n, (size_t)c.tail * c.plan.splits * (c.big ? kBT * kBT : kST * kST));
   }
   return n;
 }
@@ -762,7 +788,7 @@ size_t partial_tiles(const NsTable& t) {
 }  // namespace
 
 size_t ns_partial_floats(const NsTable& t, int planes) {
-  return (planes == 2 ? partial_tiles<2>(t) : partial_tiles<1>(t)) * (kBT * kBT);
+  return planes == 2 ? partial_floats<2>(t) : partial_floats<1>(t);
 }
 
 bool launch_ns_products(const NsTable& t, const NsFinish& fin, int planes, int steps, float* part,
