@@ -608,7 +608,8 @@ pb_status pblock_lamb_step(const pb_lamb_config* cfg, int n_tensors,
  *   element (token, head, e) of in at in[token*ld_in + head*head_dim + e], ld_in in
  *   elements (>= heads*head_dim), out likewise.  out may be in with ld_out = ld_in
  *   (in place; elements past rot_dim are then left alone); otherwise no memory of
- *   any out may be in any other in or out.  Pointers are aligned to the element;
+ *   any out may be in any other in or out (refused, unless they interleave with two
+ *   leading dimensions, which is not seen).  Pointers are aligned to the element;
  *   16-byte aligned pieces (head_dim, ld and rot_dim, or rot_dim/2 when not
  *   interleaved, multiples of 16 bytes) run fastest.
  * positions: int64 per token, device memory, any value (negative ones turn the
@@ -672,7 +673,8 @@ pb_status pblock_rope_backward(const pb_rope_config* cfg, int n_tensors,
  * from elsewhere (the residual's other use).  With g = dy gamma,
  *   dx = dsum + r (g - s r^2 mean(g s))   act: the gradient of x, and of resid
  *   dgamma = sum over rows of dy s r      [cols] fp32, overwritten
- * dx may be dy, dsum or s.  ws: pblock_rmsnorm_workspace_bytes(cfg) bytes, 256-byte
+ * dx may be dy, dsum or s, as a whole (as above for sum and y: an output that shares
+ * part of an input's memory is refused).  ws: pblock_rmsnorm_workspace_bytes(cfg) bytes, 256-byte
  * aligned.  Results do not depend on timing (fixed order, no atomics).
  *
  * Pointers are aligned to their element; cols a multiple of 8 with 16-byte aligned
@@ -715,7 +717,9 @@ pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s,
  * copy_dtype.  Each is [rows, cols] with ld elements from row to row: a slice of a
  * packed weight (rows of w_in; columns of w_out, ld = K_out) is a matrix of its
  * own.  scale is the caller's rule for the shape (0.2 sqrt(max(rows, cols)), say).
- * Matrices with rows = 0 or cols = 0 are allowed (nothing is touched).
+ * Matrices with rows = 0 or cols = 0 are allowed (nothing is touched).  No param or
+ * momentum may share memory with another or with a grad (refused, unless they interleave
+ * with two lds, which is not seen).
  *
  * products: PB_F32 carries 22 bits of every factor (each fp16 value with its
  * remainder, three matrix products for one): the update is as exact as fp32

@@ -155,11 +155,30 @@ struct NsScalars {
 };
 // Where the updates come from and go to.
 enum class NsMode { Muon, Bf16, F32 };
-// partial: a double per tile; norm: one per matrix; part: ns_partial_floats(t, planes)
-// floats, for the products' K-slices.
-size_t ns_partial_floats(const NsTable& t, int planes);
+// How a product is launched.  Its items are tiles, or K-slices of tiles: tiles 0 ..
+// n_full - 1 whole, then `splits` slices of each of the `tail` tiles after them, whose
+// fp32 partial tiles another launch sums.  Tiles count through the matrices in the order
+// of mat[] (longest K first): first[i] is that of matrix mat[i].
+struct NsPlan {
+  int first[kNsMaxTensors + 1];
+  int mat[kNsMaxTensors];
+  int n_full, splits;
+};
+struct NsLaunch {
+  bool big;  // 256 x 256 tiles, else 64 x 64
+  NsPlan plan;
+  int tail;
+};
+struct NsProducts {
+  NsLaunch gram, square, apply;
+  size_t partial_floats;  // room for the partial tiles of one launch
+};
+// From the matrices' sizes alone (host only).
+void ns_plan(const NsTable& t, int planes, NsProducts* p);
+// partial: a double per tile; norm: one per matrix; part: p.partial_floats floats.
 void launch_newton_schulz(const NsTable& t, const NsScalars& sc, NsMode mode, Dt copy_dt,
-                          double* partial, double* norm, float* part, hipStream_t s);
+                          const NsProducts& p, double* partial, double* norm, float* part,
+                          hipStream_t s);
 
 // ------------------------------------------------------ reduce-scatter sum
 // y = x + bias + sum over q < n of parts[q], row-major [rows, H] (H a

@@ -224,29 +224,31 @@ __global__ __launch_bounds__(kThreads) void ns_finish_kernel(NsTable t, NsFinish
 }
 
 template <NsMode MODE, int PLANES>
-void run(const NsTable& t, const NsScalars& sc, Dt copy_dt, double* partial, double* norm,
-         float* part, hipStream_t s) {
+void run(const NsTable& t, const NsScalars& sc, Dt copy_dt, const NsProducts& p, double* partial,
+         double* norm, float* part, hipStream_t s) {
   const int tiles = t.tile0[t.count];
   ns_update_kernel<MODE><<<tiles, kThreads, 0, s>>>(t, sc, partial);
   ns_norm_kernel<<<t.count, kNormThreads, 0, s>>>(t, sc.eps, partial, norm);
   ns_init_kernel<MODE, PLANES><<<tiles, kThreads, 0, s>>>(t, sc, norm);
   const bool bf16_out = MODE == NsMode::Bf16 || (MODE == NsMode::Muon && copy_dt == Dt::BF16);
   const NsFinish fin{MODE, bf16_out, sc.lr};
-  if (!launch_ns_products(t, fin, PLANES, sc.steps, part, s))
+  launch_ns_products(t, fin, PLANES, sc.steps, p, part, s);
+  if (p.apply.big)
     ns_finish_kernel<PLANES><<<tiles, kThreads, 0, s>>>(t, fin, sc.steps & 1);
 }
 
 }  // namespace
 
 void launch_newton_schulz(const NsTable& t, const NsScalars& sc, NsMode mode, Dt copy_dt,
-                          double* partial, double* norm, float* part, hipStream_t s) {
+                          const NsProducts& p, double* partial, double* norm, float* part,
+                          hipStream_t s) {
   switch (mode) {
     case NsMode::Muon:
-      if (sc.planes == 2) run<NsMode::Muon, 2>(t, sc, copy_dt, partial, norm, part, s);
-      else run<NsMode::Muon, 1>(t, sc, copy_dt, partial, norm, part, s);
+      if (sc.planes == 2) run<NsMode::Muon, 2>(t, sc, copy_dt, p, partial, norm, part, s);
+      else run<NsMode::Muon, 1>(t, sc, copy_dt, p, partial, norm, part, s);
       break;
-    case NsMode::Bf16: run<NsMode::Bf16, 1>(t, sc, copy_dt, partial, norm, part, s); break;
-    case NsMode::F32: run<NsMode::F32, 2>(t, sc, copy_dt, partial, norm, part, s); break;
+    case NsMode::Bf16: run<NsMode::Bf16, 1>(t, sc, copy_dt, p, partial, norm, part, s); break;
+    case NsMode::F32: run<NsMode::F32, 2>(t, sc, copy_dt, p, partial, norm, part, s); break;
   }
 }
 

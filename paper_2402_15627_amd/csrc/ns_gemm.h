@@ -108,10 +108,9 @@ PB_DEV void finish(const NsMat& x, const NsFinish& f, int r, int c, const float*
     put<N>((float*)x.out + r * x.ld_out + c, left, v);
   }
 }
-// `steps` Newton-Schulz steps of every matrix from x[0] on.  part: room for
-// ns_partial_floats(t, planes) floats.  True where the last product has finished the
-// tensors; else X is in x[steps & 1].
-bool launch_ns_products(const NsTable& t, const NsFinish& fin, int planes, int steps, float* part,
-                        hipStream_t s);
+// `steps` Newton-Schulz steps of every matrix from x[0] on.  Where apply runs in small
+// tiles the last product finishes the tensors; else X is in x[steps & 1].
+void launch_ns_products(const NsTable& t, const NsFinish& fin, int planes, int steps,
+                        const NsProducts& p, float* part, hipStream_t s);
 
 }  // namespace pb

@@ -103,16 +103,6 @@ PB_DEV f16x8 frag(const unsigned char* tile, int base, int f, int lane) {
 }
 
 // ------------------------------------------------------------ work items
-// A launch's items are tiles, or K-slices of tiles: tiles 0 .. n_full - 1 whole, then
-// `splits` slices of each tile after them, whose fp32 partial tiles ns_reduce_kernel
-// sums.  Tiles count through the matrices in the order of mat[] (longest K first):
-// first[i] is that of matrix mat[i].
-struct NsPlan {
-  int first[kNsMaxTensors + 1];
-  int mat[kNsMaxTensors];
-  int n_full, splits;
-};
-
 // Tile of the triangle tm <= tn of t x t tiles, in bands of four rows walked column by
 // column (tiles that run together then share operand strips in an XCD's L2, as in the
 // walk of tile_of).
@@ -670,17 +660,11 @@ template <int PLANES>
 constexpr double kSmallStepUs = PLANES == 2 ? 2.05 : 1.9;
 constexpr double kSmallTileUs = 2.5, kSmallUs = 5.0, kSmallSplitUs = 7.0;
 
-struct Choice {
-  bool big;  // 256 x 256 tiles
-  NsPlan plan;
-  int tail;  // tiles cut along K
-};
-
 // The tiles that are estimated to end sooner: 256 x 256, whole rounds of them and the
 // tiles of the last, partial round (or of all, where they do not fill one) cut along K;
 // or 64 x 64, all of them cut where they are few and K is long.
 template <int PLANES>
-Choice choose(Op op, const NsTable& t) {
+NsLaunch choose(Op op, const NsTable& t) {
   NsPlan plan{};
   auto len = [&](int i) { return (op == Op::Gram ? t.mat[i].n : t.mat[i].m) / kK<PLANES>; };
   auto small_len = [&](int i) { return (len(i) + kSWaves - 1) / kSWaves; };
@@ -697,18 +681,18 @@ Choice choose(Op op, const NsTable& t) {
   // Steps until the last item ends, and rounds, the items (longest first) taken kCUs at
   // a time; l(i): steps of a tile of matrix i, those past n_full in `splits` items
   struct Rounds {
-    long long steps, count;
+    int steps, count;
   };
   auto rounds = [&](auto l, int n_full, int splits) {
     Rounds r{0, 0};
-    long long at = 0;  // items so far
+    int at = 0;  // items so far
     for (int i = 0; i < t.count; ++i) {
       const int nk = l(plan.mat[i]), cut = (nk + splits - 1) / splits;
       const int whole = std::max(0, std::min(plan.first[i + 1], n_full) - plan.first[i]);
       const int rest = plan.first[i + 1] - plan.first[i] - whole;
       for (int part = 0; part < 2; ++part) {
-        const long long n = part ? (long long)rest * splits : whole;
-        const long long starts = (at + n + kCUs - 1) / kCUs - r.count;  // rounds that begin here
+        const int n = part ? rest * splits : whole;
+        const int starts = (at + n + kCUs - 1) / kCUs - r.count;  // rounds that begin here
         r.steps += starts * (part ? cut : nk);
         r.count += starts;
         at += n;
@@ -716,7 +700,7 @@ Choice choose(Op op, const NsTable& t) {
     }
     return r;
   };
-  Choice c{};
+  NsLaunch c{};
   double best = INFINITY;
   auto offer = [&](bool big, int n_full, int splits, int tail, double us) {
     if (us >= best) return;
@@ -731,12 +715,12 @@ Choice choose(Op op, const NsTable& t) {
   offer(true, tiles, 1, 0, kTileUs + kStepUs<PLANES> * rounds(len, tiles, 1).steps);
   for (int keep = tiles / kCUs; keep >= std::max(0, tiles / kCUs - 1); --keep) {
     const int full = keep * kCUs, tail = tiles - full;
-    for (int s = 2; tail > 0 && s <= 16 && (long long)tail * s <= 4 * kCUs; ++s)
+    for (int s = 2; tail > 0 && s <= 16 && tail * s <= 4 * kCUs; ++s)
       offer(true, full, s, tail,
             kTileUs + kStepUs<PLANES> * rounds(len, full, s).steps + kSplitUs + 0.05 * tail * s);
   }
   tiles = count(kST);
-  for (int s = 1; s <= 16 && (s == 1 || (op == Op::Gram && (long long)tiles * s <= 2 * kCUs)); ++s) {
+  for (int s = 1; s <= 16 && (s == 1 || (op == Op::Gram && tiles <= 2 * kCUs / s)); ++s) {
     const int full = s == 1 ? tiles : 0;
     const Rounds r = rounds(small_len, full, s);
     offer(false, full, s, tiles - full,
@@ -747,53 +731,50 @@ Choice choose(Op op, const NsTable& t) {
 }
 
 template <Op OP, int PLANES>
-void launch(const NsTable& t, const NsFinish& fin, int cur, const Choice& c, float* part,
+void launch(const NsTable& t, const NsFinish& fin, int cur, const NsLaunch& c, float* part,
             hipStream_t s) {
+  const int items = c.plan.n_full + c.tail * c.plan.splits;
   if (!c.big) {
-    ns_gemm_small<OP, PLANES><<<c.plan.n_full + c.tail * c.plan.splits, kSThreads, kSLds, s>>>(
-        t, c.plan, fin, cur, part);
+    ns_gemm_small<OP, PLANES><<<items, kSThreads, kSLds, s>>>(t, c.plan, fin, cur, part);
     if constexpr (OP == Op::Gram)
       if (c.tail)
         ns_reduce_kernel<OP, PLANES, kST><<<c.tail, 256, 0, s>>>(t, c.plan, cur, part);
   } else if constexpr (OP != Op::Last) {
-    ns_gemm_big<OP, PLANES><<<c.plan.n_full + c.tail * c.plan.splits, kBThreads, kBLds, s>>>(
-        t, c.plan, cur, part);
-    if (c.tail) ns_reduce_kernel<OP, PLANES, kBT><<<c.tail * 16, 256, 0, s>>>(t, c.plan, cur, part);
+    ns_gemm_big<OP, PLANES><<<items, kBThreads, kBLds, s>>>(t, c.plan, cur, part);
+    if (c.tail)
+      ns_reduce_kernel<OP, PLANES, kBT><<<c.tail * 16, 256, 0, s>>>(t, c.plan, cur, part);
   }
 }
 
 template <int PLANES>
-bool iterate(const NsTable& t, const NsFinish& fin, int steps, float* part, hipStream_t s) {
-  const Choice gram = choose<PLANES>(Op::Gram, t), square = choose<PLANES>(Op::Square, t),
-               apply = choose<PLANES>(Op::Apply, t);
+void iterate(const NsTable& t, const NsFinish& fin, int steps, const NsProducts& p, float* part,
+             hipStream_t s) {
   for (int k = 0; k < steps; ++k) {
-    launch<Op::Gram, PLANES>(t, fin, k & 1, gram, part, s);
-    launch<Op::Square, PLANES>(t, fin, k & 1, square, part, s);
-    if (k + 1 == steps && !apply.big) launch<Op::Last, PLANES>(t, fin, k & 1, apply, part, s);
-    else launch<Op::Apply, PLANES>(t, fin, k & 1, apply, part, s);
+    launch<Op::Gram, PLANES>(t, fin, k & 1, p.gram, part, s);
+    launch<Op::Square, PLANES>(t, fin, k & 1, p.square, part, s);
+    if (k + 1 == steps && !p.apply.big) launch<Op::Last, PLANES>(t, fin, k & 1, p.apply, part, s);
+    else launch<Op::Apply, PLANES>(t, fin, k & 1, p.apply, part, s);
   }
-  return !apply.big;
-}
-
-template <int PLANES>
-size_t partial_floats(const NsTable& t) {
-  size_t n = 0;
-  for (Op op : {Op::Gram, Op::Square, Op::Apply}) {
-    const Choice c = choose<PLANES>(op, t);
-    n = std::max(n, (size_t)c.tail * c.plan.splits * (c.big ? kBT * kBT : kST * kST));
-  }
-  return n;
 }
 
 }  // namespace
 
-size_t ns_partial_floats(const NsTable& t, int planes) {
-  return planes == 2 ? partial_floats<2>(t) : partial_floats<1>(t);
+void ns_plan(const NsTable& t, int planes, NsProducts* p) {
+  auto of = [&](Op op) { return planes == 2 ? choose<2>(op, t) : choose<1>(op, t); };
+  p->gram = of(Op::Gram);
+  p->square = of(Op::Square);
+  p->apply = of(Op::Apply);
+  p->partial_floats = 0;
+  for (const NsLaunch* l : {&p->gram, &p->square, &p->apply})
+    p->partial_floats =
+        std::max(p->partial_floats,
+                 (size_t)l->tail * l->plan.splits * (l->big ? kBT * kBT : kST * kST));
 }
 
-bool launch_ns_products(const NsTable& t, const NsFinish& fin, int planes, int steps, float* part,
-                        hipStream_t s) {
-  return planes == 2 ? iterate<2>(t, fin, steps, part, s) : iterate<1>(t, fin, steps, part, s);
+void launch_ns_products(const NsTable& t, const NsFinish& fin, int planes, int steps,
+                        const NsProducts& p, float* part, hipStream_t s) {
+  if (planes == 2) iterate<2>(t, fin, steps, p, part, s);
+  else iterate<1>(t, fin, steps, p, part, s);
 }
 
 }  // namespace pb

@@ -42,6 +42,25 @@ pb_status check_ws(const void* ws, size_t bytes, size_t need) {
   return PB_OK;
 }
 
+// Rows of `width` elements of `e` bytes, ld elements apart.
+struct Span {
+  const void* p;
+  size_t ld, width;
+  int64_t rows;
+};
+// Whether two such are seen to share memory: apart as a whole they do not, and of one
+// leading dimension they may interleave.  (Of two leading dimensions, interleaved: not
+// seen.)
+bool overlap(const Span& a, const Span& b, size_t e) {
+  if (!a.rows || !b.rows || !a.p || !b.p) return false;
+  const Span &lo = (uintptr_t)a.p <= (uintptr_t)b.p ? a : b, &hi = &lo == &a ? b : a;
+  const size_t off = ((uintptr_t)hi.p - (uintptr_t)lo.p) / e;  // elements from lo to hi
+  if (off >= (size_t)(lo.rows - 1) * lo.ld + lo.width) return false;
+  if (lo.ld != hi.ld && lo.rows > 1 && hi.rows > 1) return false;
+  const size_t ld = lo.rows > 1 ? lo.ld : hi.ld, at = off % ld;
+  return at < lo.width || ld - at < hi.width;
+}
+
 // A call without any element: as finish_launches(), but no HIP call is made.
 pb_status nothing_to_do() {
   pb::clear_error();
@@ -124,6 +143,16 @@ pb_status rope(const pb_rope_config* c, int n, const pb_rope_tensor* x, int64_t 
     a.heads[i] = x[i].heads;
     a.copy_rest[i] = x[i].in != x[i].out;
   }
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; j < n; ++j) {
+      const Span out{x[i].out, x[i].ld_out, (size_t)x[i].heads * c->head_dim, tokens};
+      const Span in{x[j].in, x[j].ld_in, (size_t)x[j].heads * c->head_dim, tokens};
+      const Span out2{x[j].out, x[j].ld_out, (size_t)x[j].heads * c->head_dim, tokens};
+      if (i != j && overlap(out, out2, e))
+        return fail(PB_ERR_INVALID_ARG, "tensors %d and %d overlap in out", i, j);
+      if (!(i == j && x[i].in == x[i].out) && overlap(out, in, e))
+        return fail(PB_ERR_INVALID_ARG, "out of tensor %d overlaps in of tensor %d", i, j);
+    }
   a.n = n;
   a.head_dim = c->head_dim;
   a.rot_dim = c->rot_dim;
@@ -165,6 +194,10 @@ pb_status check_rms(const pb_rmsnorm_config* c) {
   return PB_OK;
 }
 
+Span dense(const pb_rmsnorm_config* c, const void* p) {
+  return {p, (size_t)c->cols, (size_t)c->cols, c->rows};
+}
+
 // ------------------------------------------------------------- Muon step
 static_assert(PB_MUON_MAX_TENSORS == pb::kNsMaxTensors, "tensor limit");
 
@@ -201,9 +234,12 @@ bool ns_add(pb::NsTable& t, int rows, int cols) {
   return tiles < kMaxBlocks;
 }
 
-// Places the planes of every matrix from base on (nullptr: sizes alone).
-NsLayout ns_layout(pb::NsTable& t, int planes, char* base) {
+// Plans the products, and places the planes of every matrix from base on (nullptr: sizes
+// alone).
+NsLayout ns_layout(pb::NsTable& t, int planes, char* base, pb::NsProducts* p) {
   NsLayout L{};
+  if (t.count == 0) return L;
+  pb::ns_plan(t, planes, p);
   L.norm = align256((size_t)t.tile0[t.count] * sizeof(double));
   size_t o = L.norm + align256((size_t)t.count * sizeof(double));
   for (int i = 0; i < t.count; ++i) {
@@ -217,7 +253,7 @@ NsLayout ns_layout(pb::NsTable& t, int planes, char* base) {
     o += 2 * big + 2 * small;
   }
   L.part = o;
-  L.total = t.count ? o + align256(pb::ns_partial_floats(t, planes) * sizeof(float)) : 0;
+  L.total = o + align256(p->partial_floats * sizeof(float));
   return L;
 }
 
@@ -248,11 +284,22 @@ pb_status check_steps(int steps, float eps) {
   return PB_OK;
 }
 
-void ns_launch(pb::NsTable& t, const pb::NsScalars& sc, pb::NsMode mode, pb::Dt copy_dt, char* ws,
-               hipStream_t stream) {
-  const NsLayout L = ns_layout(t, sc.planes, ws);
-  pb::launch_newton_schulz(t, sc, mode, copy_dt, (double*)(ws + L.partial), (double*)(ws + L.norm),
-                           (float*)(ws + L.part), stream);
+pb_status ns_launch(pb::NsTable& t, const pb::NsScalars& sc, pb::NsMode mode, pb::Dt copy_dt,
+                    void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (t.count == 0) return nothing_to_do();
+  pb::NsProducts p;
+  const NsLayout L = ns_layout(t, sc.planes, (char*)ws, &p);
+  PB_CHECK(check_ws(ws, ws_bytes, L.total));
+  char* w = (char*)ws;
+  pb::launch_newton_schulz(t, sc, mode, copy_dt, p, (double*)(w + L.partial),
+                           (double*)(w + L.norm), (float*)(w + L.part), stream);
+  return finish_launches();
+}
+
+// The bytes that the table's call needs.
+size_t ns_bytes(pb::NsTable& t, pb_dtype products) {
+  pb::NsProducts p;
+  return ns_layout(t, products == PB_F32 ? 2 : 1, nullptr, &p).total;
 }
 
 }  // namespace
@@ -286,7 +333,14 @@ pb_status pblock_rmsnorm_forward(const pb_rmsnorm_config* cfg, const void* x, co
     if (!y && !q8) return fail(PB_ERR_INVALID_ARG, "y and q8 are both NULL");
     if (!q8 != !scales) return fail(PB_ERR_INVALID_ARG, "q8 and scales come together");
     if (sum && !resid) return fail(PB_ERR_INVALID_ARG, "sum without resid");
-    if (sum && sum == y) return fail(PB_ERR_INVALID_ARG, "sum and y are the same buffer");
+    const void* outs[2] = {sum, y};
+    const void* ins[2] = {x, resid};
+    for (const void* o : outs)
+      for (const void* i : ins)
+        if (o != i && overlap(dense(cfg, o), dense(cfg, i), e))
+          return fail(PB_ERR_INVALID_ARG, "sum or y overlaps a part of x or resid");
+    if (overlap(dense(cfg, sum), dense(cfg, y), e))
+      return fail(PB_ERR_INVALID_ARG, "sum and y overlap");
   }
   PB_CHECK(check_ptr(gamma, e, "gamma"));
   if (cfg->rows == 0) return nothing_to_do();
@@ -324,6 +378,9 @@ pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s, c
     PB_CHECK(check_ptr(dy, e, "dy"));
     PB_CHECK(check_opt(dsum, e, "dsum"));
     PB_CHECK(check_ptr(dx, e, "dx"));
+    for (const void* i : {s, dy, dsum})
+      if (dx != i && overlap(dense(cfg, dx), dense(cfg, i), e))
+        return fail(PB_ERR_INVALID_ARG, "dx overlaps a part of s, dy or dsum");
   }
   PB_CHECK(check_ptr(gamma, e, "gamma"));
   PB_CHECK(check_ptr(dgamma, 4, "dgamma"));
@@ -347,7 +404,7 @@ size_t pblock_muon_workspace_bytes(const pb_muon_config* cfg, int n_tensors,
                                    const pb_muon_tensor* tensors) {
   pb::NsTable t{};
   if (!cfg || !known(cfg->products) || ns_table(n_tensors, tensors, t) != PB_OK) return 0;
-  return ns_layout(t, cfg->products == PB_F32 ? 2 : 1, nullptr).total;
+  return ns_bytes(t, cfg->products);
 }
 
 pb_status pblock_muon_step(const pb_muon_config* cfg, int n_tensors, const pb_muon_tensor* tensors,
@@ -390,8 +447,19 @@ pb_status pblock_muon_step(const pb_muon_config* cfg, int n_tensors, const pb_mu
     m.decay = x.weight_decay;
     m.scale = x.scale;
   }
-  PB_CHECK(check_ws(ws, ws_bytes, pblock_muon_workspace_bytes(cfg, n_tensors, tensors)));
-  if (t.count == 0) return nothing_to_do();
+  for (int i = 0; i < t.count; ++i)
+    for (int j = 0; j < t.count; ++j) {
+      const pb::NsMat &x = t.mat[i], &y = t.mat[j];
+      auto span = [](const pb::NsMat& v, const void* p) {
+        return Span{p, (size_t)v.ld_src, (size_t)v.cols, v.rows};
+      };
+      if (i < j && (overlap(span(x, x.w), span(y, y.w), 4) ||
+                    overlap(span(x, x.mom), span(y, y.mom), 4)))
+        return fail(PB_ERR_INVALID_ARG, "two tensors overlap in param or momentum");
+      if (overlap(span(x, x.w), span(y, y.mom), 4) || overlap(span(x, x.w), span(y, y.src), 4) ||
+          overlap(span(x, x.mom), span(y, y.src), 4))
+        return fail(PB_ERR_INVALID_ARG, "param, grad and momentum overlap");
+    }
   pb::NsScalars sc{};
   sc.lr = cfg->lr;
   sc.momentum = cfg->momentum;
@@ -400,15 +468,14 @@ pb_status pblock_muon_step(const pb_muon_config* cfg, int n_tensors, const pb_mu
   sc.nesterov = cfg->nesterov;
   sc.planes = cfg->products == PB_F32 ? 2 : 1;
   sc.steps = cfg->steps;
-  ns_launch(t, sc, pb::NsMode::Muon, dt_of(copy_dtype), (char*)ws, stream);
-  return finish_launches();
+  return ns_launch(t, sc, pb::NsMode::Muon, dt_of(copy_dtype), ws, ws_bytes, stream);
 }
 
 size_t pblock_orthogonalize_workspace_bytes(int n_tensors, const pb_ortho_tensor* tensors,
                                             pb_dtype dtype) {
   pb::NsTable t{};
   if (!known(dtype) || ns_table(n_tensors, tensors, t) != PB_OK) return 0;
-  return ns_layout(t, dtype == PB_F32 ? 2 : 1, nullptr).total;
+  return ns_bytes(t, dtype);
 }
 
 pb_status pblock_orthogonalize(int n_tensors, const pb_ortho_tensor* tensors, pb_dtype dtype,
@@ -438,15 +505,22 @@ pb_status pblock_orthogonalize(int n_tensors, const pb_ortho_tensor* tensors, pb
     m.ld_src = (long long)x.ld_in;
     m.ld_out = (long long)x.ld_out;
   }
-  PB_CHECK(check_ws(ws, ws_bytes, pblock_orthogonalize_workspace_bytes(n_tensors, tensors, dtype)));
-  if (t.count == 0) return nothing_to_do();
+  for (int i = 0; i < t.count; ++i)
+    for (int j = 0; j < t.count; ++j) {
+      const pb::NsMat &x = t.mat[i], &y = t.mat[j];
+      const Span out{x.out, (size_t)x.ld_out, (size_t)x.cols, x.rows};
+      if (i != j && overlap(out, Span{y.out, (size_t)y.ld_out, (size_t)y.cols, y.rows}, e))
+        return fail(PB_ERR_INVALID_ARG, "two tensors overlap in out");
+      if (!(i == j && x.src == x.out) &&
+          overlap(out, Span{y.src, (size_t)y.ld_src, (size_t)y.cols, y.rows}, e))
+        return fail(PB_ERR_INVALID_ARG, "an out overlaps an in");
+    }
   pb::NsScalars sc{};
   sc.eps = eps;
   sc.steps = steps;
   sc.planes = dtype == PB_F32 ? 2 : 1;
-  ns_launch(t, sc, dtype == PB_F32 ? pb::NsMode::F32 : pb::NsMode::Bf16, dt_of(dtype), (char*)ws,
-            stream);
-  return finish_launches();
+  return ns_launch(t, sc, dtype == PB_F32 ? pb::NsMode::F32 : pb::NsMode::Bf16, dt_of(dtype), ws,
+                   ws_bytes, stream);
 }
 
 }  // extern "C"

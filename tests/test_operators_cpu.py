@@ -100,6 +100,8 @@ CONFIGS = [(dict(rows=-1), BAD), (dict(cols=0), BAD), (dict(cols=32769), UNSUPPO
     (dict(x=None), BAD), (dict(x=FAKE + 1), BAD), (dict(y=None), BAD), (dict(resid=FAKE + 1), BAD),
     (dict(sum=FAKE + 256), BAD), (dict(resid=FAKE, sum=FAKE + 1), BAD),
     (dict(resid=FAKE, sum=FAKE), BAD),  # sum and y in one buffer
+    (dict(y=FAKE + 2), BAD), (dict(y=FAKE + 4 * 64 * 2 - 2), BAD),  # y over a part of x
+    (dict(resid=FAKE + 4096, sum=FAKE + 4096 - 2), BAD), (dict(resid=FAKE + 4096, sum=FAKE + 2), BAD),
     (dict(q8=FAKE), BAD), (dict(scales=FAKE), BAD), (dict(q8=FAKE, scales=FAKE + 2), BAD),
     (dict(rstd=FAKE + 2), BAD),
 ])
@@ -110,7 +112,8 @@ def test_rmsnorm_forward_refusals(over, status):
 
 @pytest.mark.parametrize("over,status", CONFIGS + [
     (dict(s=None), BAD), (dict(rstd=None), BAD), (dict(rstd=FAKE + 2), BAD), (dict(dy=None), BAD),
-    (dict(dsum=FAKE + 1), BAD), (dict(dx=None), BAD), (dict(dgamma=None), BAD),
+    (dict(dsum=FAKE + 1), BAD), (dict(dx=None), BAD), (dict(dx=FAKE + 2), BAD),
+    (dict(dsum=FAKE + 1024, dx=FAKE + 1022), BAD), (dict(dgamma=None), BAD),
     (dict(dgamma=FAKE + 2), BAD), (dict(ws=None), BAD), (dict(ws=FAKE + 16), BAD),
     (dict(nbytes=0), SMALL), (dict(nbytes=4 * 64 * 1 - 1), SMALL),
 ])
@@ -137,7 +140,7 @@ def test_rmsnorm_without_rows_and_its_workspace():
 # ------------------------------------------------------------- Muon step
 def muon(ws=FAKE, nbytes=1 << 30, copy=pb.PB_BF16, n=None, tensors=None, cfg_null=False, **over):
     cfg = pb.muon_config(1e-3)
-    x = dict(param=FAKE, grad=FAKE, momentum=FAKE, param_copy=None, rows=8, cols=16, ld=16,
+    x = dict(param=FAKE, grad=FAKE + (1 << 20), momentum=FAKE + (2 << 20), param_copy=None, rows=8, cols=16, ld=16,
              weight_decay=0.1, scale=1.0)
     own = dict(mom_ptr="momentum")
     for k, v in over.items():
@@ -187,6 +190,39 @@ def test_orthogonalize_refusals(over, status):
                                                   a["steps"], a["eps"], a["ws"], a["nbytes"],
                                                   None) == status
     assert pb.pblock_last_error() != ""
+
+
+def test_rope_refuses_tensors_that_overlap():
+    """Packed tensors interleave row by row: their columns decide.  The last calls pass
+    every check and fail for want of a GPU (or launch nothing)."""
+    R = pb.RopeTensor  # bf16, 2 heads of 64: 128 elements a row
+    at = lambda n: FAKE + 2 * n  # noqa: E731
+    assert rope(tensors=[R(FAKE, FAKE, 512, 512, 2), R(FAKE, FAKE, 512, 512, 2)]) == BAD
+    assert "overlap" in pb.pblock_last_error()
+    assert rope(tensors=[R(FAKE, FAKE, 512, 512, 2), R(at(127), at(127), 512, 512, 2)]) == BAD
+    assert rope(tensors=[R(FAKE, FAKE, 512, 512, 2), R(at(3 * 512 + 500), at(3 * 512 + 500), 512, 512, 2)]) != BAD
+    assert rope(tensors=[R(FAKE, FAKE, 512, 512, 2), R(at(2 * 512 + 500), at(2 * 512 + 500), 512, 512, 2)]) == BAD
+    assert rope(tensors=[R(FAKE, at(64), 512, 512, 2)]) == BAD  # out over the next head of in
+    assert rope(tensors=[R(FAKE, FAKE, 512, 512, 2), R(at(4096), at(128), 512, 512, 2)]) != BAD
+    assert rope(tensors=[R(FAKE, FAKE, 512, 512, 2), R(at(128), at(128), 512, 512, 2)]) != BAD
+    assert rope(tokens=0, tensors=[R(FAKE, FAKE, 512, 512, 2), R(FAKE, FAKE, 512, 512, 2)]) == OK
+
+
+def test_muon_and_orthogonalize_refuse_matrices_that_overlap():
+    M = lambda w, g, m: pb.MuonTensor(w, g, m, None, 8, 16, 64, 0.0, 1.0)  # noqa: E731
+    f = lambda n: FAKE + 4 * n  # noqa: E731
+    g, m = f(1 << 20), f(1 << 21)
+    for bad in ([M(FAKE, g, m)] * 2, [M(FAKE, g, m), M(f(15), f(1 << 22), f(1 << 23))],
+                [M(FAKE, FAKE, m)], [M(FAKE, g, f(64 + 8))], [M(FAKE, g, m), M(f(1 << 22), f(1 << 23), m)]):
+        assert muon(tensors=bad) == BAD and "overlap" in pb.pblock_last_error()
+    # columns of one weight side by side; a shared gradient is read alone
+    assert muon(tensors=[M(FAKE, g, m), M(f(16), g + 64, m + 64), M(f(32), g, m + 128)], nbytes=1) == SMALL
+    O = pb.OrthoTensor
+    call = lambda *x: pb.load_library().pblock_orthogonalize(  # noqa: E731
+        len(x), (O * len(x))(*x), pb.PB_F32, 5, 1e-7, FAKE, 1, None)
+    assert call(O(FAKE, f(8), 8, 16, 64, 64)) == BAD
+    assert call(O(FAKE, FAKE, 8, 16, 64, 64), O(f(32), f(4), 8, 16, 64, 64)) == BAD
+    assert call(O(FAKE, FAKE, 8, 16, 64, 64), O(f(16), f(32), 8, 16, 64, 64)) == SMALL
 
 
 def test_empty_matrices_and_workspaces():
