@@ -126,8 +126,8 @@ void launch_rms_backward(Dt dt, const RmsBackward& a, hipStream_t s);
 // ------------------------------------- orthogonalised updates (Newton-Schulz)
 // One matrix of a call.  The iterate X is the update or, where it has more rows than
 // columns, its transpose: m x n with m <= n, both padded to multiples of 64 with
-// zeros.  x, a and b hold fp16 values (alone, or each with its remainder): X twice (in
-// turn), X X^T, and the polynomial of it.
+// zeros.  x and s hold fp16 values (alone, or each with its remainder): X twice (in turn),
+// and the symmetric m x m matrices, X X^T and polynomials of it.
 constexpr int kNsMaxTensors = 16;
 constexpr int kNsPad = 64;
 struct NsMat {
@@ -137,9 +137,9 @@ struct NsMat {
   void* copy;       // nullptr: none
   void* out;        // orthogonalisation alone
   long long ld_src, ld_out;
-  _Float16 *x[2], *a, *b;
+  _Float16 *x[2], *s[3];
   int rows, cols, m, n;  // of the tensor; of X, padded
-  int ldm, ldn;          // values from row to row of a and b, and of x (one plane's)
+  int ldm, ldn;          // values from row to row of s, and of x (one plane's)
   float decay, scale;
 };
 struct NsTable {
@@ -168,11 +168,16 @@ struct NsLaunch {
   bool big;  // 256 x 256 tiles, else 64 x 64
   NsPlan plan;
   int tail;
+  double us;  // estimate
 };
 struct NsProducts {
-  NsLaunch gram, square, apply;
-  size_t partial_floats;  // room for the partial tiles of one launch
+  NsLaunch gram, square, apply;  // (square: every product of two symmetric matrices)
+  bool paired;                   // two steps to one gram and apply
+  size_t partial_floats;         // room for the partial tiles of one launch
 };
+inline int ns_symmetric(const NsProducts& p) { return p.paired ? 3 : 2; }  // s in use
+// Times that X is replaced: it is in x[ns_groups & 1] at the end.
+inline int ns_groups(const NsProducts& p, int steps) { return p.paired ? (steps + 1) / 2 : steps; }
 // From the matrices' sizes alone (host only).
 void ns_plan(const NsTable& t, int planes, NsProducts* p);
 // partial: a double per tile; norm: one per matrix; part: p.partial_floats floats.

@@ -11,7 +11,7 @@
 //   1. update: M in place, the sum of U^2 per 64 x 64 tile, in fp64
 //   2. norm:   1 / (||U||_F + eps) of each matrix
 //   3. init:   X's fp16 planes, padded to multiples of 64 with zeros
-//   4. the products (ns_gemm.hip), three launches a step for all matrices at once
+//   4. the products (ns_gemm.hip), each one launch for all matrices
 //   5. finish: w and its copy, or the orthogonalised matrix itself; part of the last
 //      product where that runs in small tiles
 //
@@ -234,7 +234,7 @@ void run(const NsTable& t, const NsScalars& sc, Dt copy_dt, const NsProducts& p,
   const NsFinish fin{MODE, bf16_out, sc.lr};
   launch_ns_products(t, fin, PLANES, sc.steps, p, part, s);
   if (p.apply.big)
-    ns_finish_kernel<PLANES><<<tiles, kThreads, 0, s>>>(t, fin, sc.steps & 1);
+    ns_finish_kernel<PLANES><<<tiles, kThreads, 0, s>>>(t, fin, ns_groups(p, sc.steps) & 1);
 }
 
 }  // namespace

@@ -7,14 +7,18 @@
 
 namespace pb {
 
-// A plane value is the number times a power of two, rounded to fp16; with two
-// planes the second one holds the remainder, rounded again (2^-22 of the number).
-// The powers keep the values high in fp16's range, so that what the remainder
-// loses to subnormals is below 2^-39 of the spectral norm: X has a spectral norm
-// of at most 1.203, A = X X^T of 1.446 and B of 3.445 (a + b s + c s^2 over s in
-// [0, 1.446] lies in [0.638, 3.445]), and no element of a matrix exceeds its norm:
-// 39.4e3, 47.4e3 and 56.4e3 of fp16's 65.5e3.
-constexpr float kNsScaleX = 32768.0f, kNsScaleA = 32768.0f, kNsScaleB = 16384.0f;
+// A plane value is the number times a power of two, rounded to fp16; with two planes the
+// second one holds the remainder, rounded again (2^-22 of the number).  The powers keep
+// the values high in fp16's range, so that what the remainder loses to subnormals is
+// below 2^-36 of the largest spectral norm: no element of a matrix exceeds its norm, and
+// with s the singular values of X, in [0, 1.203],
+//   X (1.203) and A = X X^T (1.446) times 2^15 stay below 39.4e3 and 47.4e3,
+//   B = a + b s^2 + c s^4, in [0.638, 3.445], times 2^14 below 56.4e3,
+//   B A (p(s) s: 1.446) times 2^15 below 47.4e3,
+//   Q = B' B, of two steps (11.87), times 2^12 below 48.6e3
+// of fp16's 65.5e3.
+constexpr float kNsScaleX = 32768.0f, kNsScaleA = 32768.0f, kNsScaleB = 16384.0f,
+                kNsScaleQ = 4096.0f;
 // Coefficients of the step (Jordan et al. 2024).
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 
@@ -109,7 +113,7 @@ PB_DEV void finish(const NsMat& x, const NsFinish& f, int r, int c, const float*
   }
 }
 // `steps` Newton-Schulz steps of every matrix from x[0] on.  Where apply runs in small
-// tiles the last product finishes the tensors; else X is in x[steps & 1].
+// tiles the last product finishes the tensors; else X is in x[ns_groups() & 1].
 void launch_ns_products(const NsTable& t, const NsFinish& fin, int planes, int steps,
                         const NsProducts& p, float* part, hipStream_t s);
 

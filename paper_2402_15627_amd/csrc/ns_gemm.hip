@@ -1,20 +1,35 @@
-// The products of a Newton-Schulz step, all matrices of a call in one launch each:
+// The products of the Newton-Schulz steps, all matrices of a call in one launch each.
+// A step is
 //
-//   gram    A = X X^T                  symmetric: tiles on and above the diagonal, each
-//                                      written to its mirror image too
-//   square  B = a I + b A + c A A      symmetric likewise
-//   apply   X' = B X
-//   last    the last step's apply in 64 x 64 tiles: its result goes to the weights (or
-//           to the caller's matrix) from the fp32 sums, which saves a launch.  (In the
-//           256 x 256 tiles, where all CUs then write at once, it took 0.9 ms of a 4.3
-//           ms launch over the 175B share, and the pass of its own takes 0.7.)
+//   A = X X^T,  B = a I + b A + c A A,  X' = B X
+//
+// and two steps need X but twice, since A' = X' X'^T = B A B and everything m x m
+// commutes:
+//
+//   A = X X^T,  B = f(A),  A' = (B A) B,  B' = f(A'),  X'' = (B' B) X
+//
+// m x m products for two of m x m x n: with half of each symmetric product computed,
+// 8 m^3 + 3 (n - m) m^2 operations for 8 m^3 + 6 (n - m) m^2.  (Over more steps the
+// spread of A's eigenvalues, the square of X's, costs accuracy: five steps from one A
+// lose two digits, a pair none: 256 x 1024, 16 directions in noise, 2.0e-6 off either
+// way, 8 in a tenth of the noise 5.0e-6 in pairs and 8.3e-6 step by step; fp32 2.1e-6 and
+// 4.6e-6.)
+//
+//   Sym     L R, L and R symmetric, or X X^T: tiles on and above the diagonal, each
+//           written to its mirror image too
+//   Square  f(L) likewise
+//   Apply   L X
+//   Last    the last Apply in 64 x 64 tiles: its result goes to the weights (or to the
+//           caller's matrix) from the fp32 sums, which saves a launch.  (In the 256 x 256
+//           tiles, where all CUs then write at once, it took 0.9 ms of a 4.3 ms launch
+//           over the 175B share, and the pass of its own takes 0.7.)
 //
 // MFMA v_mfma_f32_16x16x32_f16 on the planes of ns_gemm.h, fp32 accumulation.  One
 // plane: one product of fp16 values (rounded by 2^-11 at most).  Two planes (value h
 // and remainder l): l h + h h + h l (what is left out, l l, is at most 2^-22 of the
 // product).  A K-tile of 128-byte rows is 64 k of one plane or 32 k of both: two planes
-// move the same bytes for one and a half times the products.  a goes into B, not
-// into apply's sum: near the end B is about 0.7 to 1.4 instead of -2.7 to -2.0, so its
+// move the same bytes for one and a half times the products.  a goes into B, not into
+// Apply's sum: near the end B is about 0.7 to 1.4 instead of -2.7 to -2.0, so its
 // rounding moves X' by less (one plane, one row of 777: 3.4e-3 off, 8e-4 so; 512 x 512
 // 1.34e-3, 1.24e-3), and apply reads no X beside its operand.
 //
@@ -39,22 +54,22 @@ namespace {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 #define PB_LDS __attribute__((address_space(3)))
 
-enum class Op { Gram, Square, Apply, Last };
-constexpr bool symmetric(Op op) { return op == Op::Gram || op == Op::Square; }
+enum class Op { Sym, Square, Apply, Last };
+constexpr bool symmetric(Op op) { return op == Op::Sym || op == Op::Square; }
+
+// A product's matrices: of s, or kX for X; and the factor from the sum of its plane
+// products to its result's plane values (Last: to its values).
+constexpr int kX = -1;
+struct Product {
+  int left, right, dst;
+  float scale;
+};
+constexpr Product kGram{kX, kX, 0, kNsScaleA / (kNsScaleX * kNsScaleX)};
 
 constexpr int kRow = 64;  // fp16 values of a K-contiguous row of a K-tile: 128 bytes
 template <int PLANES>
 constexpr int kK = kRow / PLANES;  // k of a K-tile
 static_assert(kNsPad == kRow, "X's dimensions are whole K-tiles");
-
-// From the sum of plane products to the result's plane values.
-template <Op OP>
-constexpr float out_scale() {
-  return OP == Op::Gram     ? kNsScaleA / (kNsScaleX * kNsScaleX)
-         : OP == Op::Square ? kNsC * kNsScaleB / (kNsScaleA * kNsScaleA)
-         : OP == Op::Apply  ? 1.0f / kNsScaleB
-                            : 1.0f / (kNsScaleB * kNsScaleX);
-}
 
 PB_DEV int swz(int row, int c) { return c ^ ((row ^ (row >> 3)) & 7); }
 // Rows of W bytes: the four rows of a transposing read, and row groups 8 apart, lie in
@@ -171,18 +186,21 @@ struct Operands {
   int lda, ldb, K;
 };
 template <Op OP, int PLANES>
-PB_DEV Operands operands(const NsMat& x, int cur) {
+PB_DEV Operands operands(const NsMat& x, const Product& p, int cur) {
   const int m = PLANES * x.ldm, n = PLANES * x.ldn;
-  if constexpr (OP == Op::Gram) return {x.x[cur], x.x[cur], n, n, x.n};
-  else if constexpr (OP == Op::Square) return {x.a, x.a, m, m, x.m};
-  else return {x.b, x.x[cur], m, n, x.m};
+  if constexpr (symmetric(OP)) {
+    if (p.left == kX) return {x.x[cur], x.x[cur], n, n, x.n};
+    return {x.s[p.left], x.s[p.right], m, m, x.m};
+  } else {
+    return {x.s[p.left], x.x[cur], m, n, x.m};
+  }
 }
 
-// What square adds to its sums at N consecutive columns n.. of row m: a I + b A.
+// What Square adds to its sums at N consecutive columns n.. of row m: a I + b A.
 template <Op OP, int PLANES, int N>
-PB_DEV void addend(const NsMat& x, int m, int n, float* u) {
+PB_DEV void addend(const NsMat& x, const Product& p, int m, int n, float* u) {
   if constexpr (OP == Op::Square) {
-    ns_load<PLANES, N>(x.a + ns_at<PLANES>(x.ldm, m, n), u, kNsB * kNsScaleB / kNsScaleA);
+    ns_load<PLANES, N>(x.s[p.left] + ns_at<PLANES>(x.ldm, m, n), u, kNsB * kNsScaleB / kNsScaleA);
 #pragma unroll
     for (int e = 0; e < N; ++e) u[e] += m == n + e ? kNsA * kNsScaleB : 0.f;
   }
@@ -190,18 +208,19 @@ PB_DEV void addend(const NsMat& x, int m, int n, float* u) {
 // N consecutive columns n.. of row m of a product.  v: the sums (scaled in place), u: the
 // addend.
 template <Op OP, int PLANES, int N>
-PB_DEV void store_result(const NsMat& x, int cur, int m, int n, float* v, const float* u) {
+PB_DEV void store_result(const NsMat& x, const Product& p, int cur, int m, int n, float* v,
+                         const float* u) {
 #pragma unroll
-  for (int e = 0; e < N; ++e) v[e] = v[e] * out_scale<OP>() + (OP == Op::Square ? u[e] : 0.f);
-  if constexpr (OP == Op::Gram) ns_store<PLANES, N>(x.a + ns_at<PLANES>(x.ldm, m, n), v, 1.0f);
-  else if constexpr (OP == Op::Square) ns_store<PLANES, N>(x.b + ns_at<PLANES>(x.ldm, m, n), v, 1.0f);
+  for (int e = 0; e < N; ++e) v[e] = v[e] * p.scale + (OP == Op::Square ? u[e] : 0.f);
+  if constexpr (symmetric(OP))
+    ns_store<PLANES, N>(x.s[p.dst] + ns_at<PLANES>(x.ldm, m, n), v, 1.0f);
   else ns_store<PLANES, N>(x.x[cur ^ 1] + ns_at<PLANES>(x.ldn, m, n), v, 1.0f);
 }
 // Eight consecutive rows m.. of column n, v: scaled results.  Symmetric products: the
 // mirror image.
-template <Op OP, int PLANES>
-PB_DEV void store_mirror8(const NsMat& x, int m, int n, const float* v) {
-  ns_store<PLANES, 8>((OP == Op::Gram ? x.a : x.b) + ns_at<PLANES>(x.ldm, n, m), v, 1.0f);
+template <int PLANES>
+PB_DEV void store_mirror8(const NsMat& x, const Product& p, int m, int n, const float* v) {
+  ns_store<PLANES, 8>(x.s[p.dst] + ns_at<PLANES>(x.ldm, n, m), v, 1.0f);
 }
 
 // ------------------------------------------------------ 256 x 256 tiles
@@ -224,8 +243,8 @@ PB_DEV void block_barrier() {
 }
 
 template <Op OP, int PLANES>
-__global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan plan, int cur,
-                                                            float* __restrict__ part) {
+__global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan plan, Product prod,
+                                                            int cur, float* __restrict__ part) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   constexpr bool BK = symmetric(OP);  // the B operand is K-contiguous
   const Item it = item_of(plan, t.count, blockIdx.x, gridDim.x);
@@ -233,7 +252,7 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
   int tm, tn;
   tile_at<OP, kBT>(x, it.tile - plan.first[it.place], tm, tn);
   const int m0 = tm * kBT, n0 = tn * kBT, M = x.m, N = BK ? x.m : x.n;
-  const Operands o = operands<OP, PLANES>(x, cur);
+  const Operands o = operands<OP, PLANES>(x, prod, cur);
   const int nk = o.K / kK<PLANES>;
   int kt0 = 0, kt1 = nk;
   if (it.slice >= 0) {
@@ -250,12 +269,14 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = (wave & 3) * kWTM, wn = (wave >> 2) * kWTN;
 
-  // Who moves what, as in gemm.hip: with K-contiguous operands every wave its own 4 KB
-  // of each; otherwise the first wave of each SIMD both 4 KB regions of its SIMD.
-  constexpr int kReg = BK ? 1 : 2;
+  // Who moves what: every wave its own 4 KB of each operand; but Apply with two planes
+  // the first wave of each SIMD both 4 KB regions of its SIMD (two 6144 x 12288: 35.0 ms
+  // and 35.2; one plane, three of 5120 x 5120 and 20480: 12.3 and 12.2).
+  constexpr bool kOwn = BK || PLANES == 1;
+  constexpr int kReg = kOwn ? 1 : 2;
   constexpr int kDmaPerTile = 2 * kReg * kBPieces;
-  const bool dma_wave = BK || wave < 4;
-  auto region = [&](int r) { return BK ? wave : (wave & 3) + 4 * r; };
+  const bool dma_wave = kOwn || wave < 4;
+  auto region = [&](int r) { return kOwn ? wave : (wave & 3) + 4 * r; };
   uint32_t aoff[kReg * kBPieces], boff[kReg * kBPieces];
 #pragma unroll
   for (int r = 0; r < kReg; ++r)
@@ -424,8 +445,8 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
       float v[4] = {s4[0], s4[1], s4[2], s4[3]};
       if (m < M && n < N) {
         float u[4];
-        addend<OP, PLANES, 4>(x, m, n, u);
-        store_result<OP, PLANES, 4>(x, cur, m, n, v, u);
+        addend<OP, PLANES, 4>(x, prod, m, n, u);
+        store_result<OP, PLANES, 4>(x, prod, cur, m, n, v, u);
         if (symmetric(OP) && tm != tn) *at = f32x4{v[0], v[1], v[2], v[3]};
       }
     }
@@ -441,7 +462,7 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
         for (int e = 0; e < 8; ++e)
           v[e] = *reinterpret_cast<const float*>(buf + (r8 + e) * (kWTN * 4) +
                                                  (((cc >> 2) ^ (r8 + e)) & 31) * 16 + (cc & 3) * 4);
-        if (nn < N && mm < M) store_mirror8<OP, PLANES>(x, mm, nn, v);
+        if (nn < N && mm < M) store_mirror8<PLANES>(x, prod, mm, nn, v);
       }
     }
   }
@@ -450,8 +471,8 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
 // Sum of a split T x T tile's slices, in slice order, and its result: 64 x 64 of the tile
 // per workgroup.
 template <Op OP, int PLANES, int T>
-__global__ __launch_bounds__(256) void ns_reduce_kernel(NsTable t, NsPlan plan, int cur,
-                                                        const float* __restrict__ part) {
+__global__ __launch_bounds__(256) void ns_reduce_kernel(NsTable t, NsPlan plan, Product prod,
+                                                        int cur, const float* __restrict__ part) {
   __shared__ float lds[64][65];
   constexpr int kSub = T / 64;  // blocks across a tile
   const int tail = blockIdx.x / (kSub * kSub), sub = blockIdx.x % (kSub * kSub);
@@ -473,8 +494,8 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(NsTable t, NsPlan plan, 
     for (int i = 1; i < plan.splits; ++i)
       s += *reinterpret_cast<const f32x4*>(q + (size_t)i * T * T);
     float v[4] = {s[0], s[1], s[2], s[3]}, u[4];
-    addend<OP, PLANES, 4>(x, m0 + rl, n0 + cl, u);
-    store_result<OP, PLANES, 4>(x, cur, m0 + rl, n0 + cl, v, u);
+    addend<OP, PLANES, 4>(x, prod, m0 + rl, n0 + cl, u);
+    store_result<OP, PLANES, 4>(x, prod, cur, m0 + rl, n0 + cl, v, u);
 #pragma unroll
     for (int e = 0; e < 4; ++e) lds[rl][cl + e] = v[e];
   }
@@ -487,7 +508,7 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(NsTable t, NsPlan plan, 
       float v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = lds[r8 + e][cc];
-      store_mirror8<OP, PLANES>(x, m0 + r8, n0 + cc, v);
+      store_mirror8<PLANES>(x, prod, m0 + r8, n0 + cc, v);
     }
   }
 }
@@ -539,8 +560,9 @@ struct SmallSide {
 };
 
 template <Op OP, int PLANES>
-__global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan plan, NsFinish fin,
-                                                              int cur, float* __restrict__ part) {
+__global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan plan, Product prod,
+                                                              NsFinish fin, int cur,
+                                                              float* __restrict__ part) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   constexpr bool BK = symmetric(OP);
   const Item it = item_of(plan, t.count, blockIdx.x, gridDim.x);
@@ -548,7 +570,7 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
   int tm, tn;
   tile_at<OP, kST>(x, it.tile - plan.first[it.place], tm, tn);
   const int m0 = tm * kST, n0 = tn * kST;
-  const Operands o = operands<OP, PLANES>(x, cur);
+  const Operands o = operands<OP, PLANES>(x, prod, cur);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // K-tiles kt0 .. kt0 + nk - 1: the slice's
@@ -577,7 +599,7 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
   const bool tall = x.rows > x.cols;
   float u[8];
   if constexpr (OP == Op::Last) weights<8>(x, fin, tall ? n0 + r : m0 + r, (tall ? m0 : n0) + c8, u);
-  else if (it.slice < 0) addend<OP, PLANES, 8>(x, m0 + r, n0 + c8, u);
+  else if (it.slice < 0) addend<OP, PLANES, 8>(x, prod, m0 + r, n0 + c8, u);
   for (int kt = wave; kt < nk; kt += kSWaves) {
     unsigned char* own_b = own + kSWaveLds / 2;
     sa.put(ra, own, lane);
@@ -627,10 +649,10 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
   }
   if constexpr (OP == Op::Last) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= out_scale<OP>();
+    for (int e = 0; e < 8; ++e) v[e] *= prod.scale;
     if (!tall) finish<8>(x, fin, m0 + r, n0 + c8, v, u);
   } else {
-    store_result<OP, PLANES, 8>(x, cur, m0 + r, n0 + c8, v, u);
+    store_result<OP, PLANES, 8>(x, prod, cur, m0 + r, n0 + c8, v, u);
   }
   if (OP == Op::Apply || (OP == Op::Last ? !tall : tm == tn)) return;
   __syncthreads();
@@ -641,7 +663,7 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = turned[r * 65 + c8 + e];  // column r, eight rows
   if constexpr (OP == Op::Last) finish<8>(x, fin, n0 + r, m0 + c8, v, u);
-  else store_mirror8<OP, PLANES>(x, m0 + c8, n0 + r, v);
+  else store_mirror8<PLANES>(x, prod, m0 + c8, n0 + r, v);
 }
 
 // ---------------------------------------------------------------- plans
@@ -664,9 +686,9 @@ constexpr double kSmallTileUs = 2.5, kSmallUs = 5.0, kSmallSplitUs = 7.0;
 // tiles of the last, partial round (or of all, where they do not fill one) cut along K;
 // or 64 x 64, all of them cut where they are few and K is long.
 template <int PLANES>
-NsLaunch choose(Op op, const NsTable& t) {
+NsLaunch choose(Op op, bool gram, const NsTable& t) {
   NsPlan plan{};
-  auto len = [&](int i) { return (op == Op::Gram ? t.mat[i].n : t.mat[i].m) / kK<PLANES>; };
+  auto len = [&](int i) { return (gram ? t.mat[i].n : t.mat[i].m) / kK<PLANES>; };
   auto small_len = [&](int i) { return (len(i) + kSWaves - 1) / kSWaves; };
   for (int i = 0; i < t.count; ++i) {  // the longest K first
     int k = i;
@@ -710,6 +732,7 @@ NsLaunch choose(Op op, const NsTable& t) {
     c.plan.n_full = n_full;
     c.plan.splits = splits;
     c.tail = tail;
+    c.us = us;
   };
   int tiles = count(kBT);
   offer(true, tiles, 1, 0, kTileUs + kStepUs<PLANES> * rounds(len, tiles, 1).steps);
@@ -720,7 +743,7 @@ NsLaunch choose(Op op, const NsTable& t) {
             kTileUs + kStepUs<PLANES> * rounds(len, full, s).steps + kSplitUs + 0.05 * tail * s);
   }
   tiles = count(kST);
-  for (int s = 1; s <= 16 && (s == 1 || (op == Op::Gram && tiles <= 2 * kCUs / s)); ++s) {
+  for (int s = 1; s <= 16 && (s == 1 || (gram && tiles <= 2 * kCUs / s)); ++s) {
     const int full = s == 1 ? tiles : 0;
     const Rounds r = rounds(small_len, full, s);
     offer(false, full, s, tiles - full,
@@ -731,39 +754,66 @@ NsLaunch choose(Op op, const NsTable& t) {
 }
 
 template <Op OP, int PLANES>
-void launch(const NsTable& t, const NsFinish& fin, int cur, const NsLaunch& c, float* part,
-            hipStream_t s) {
+void launch(const NsTable& t, const NsLaunch& c, const Product& p, const NsFinish& fin, int cur,
+            float* part, hipStream_t s) {
   const int items = c.plan.n_full + c.tail * c.plan.splits;
   if (!c.big) {
-    ns_gemm_small<OP, PLANES><<<items, kSThreads, kSLds, s>>>(t, c.plan, fin, cur, part);
-    if constexpr (OP == Op::Gram)
+    ns_gemm_small<OP, PLANES><<<items, kSThreads, kSLds, s>>>(t, c.plan, p, fin, cur, part);
+    if constexpr (OP == Op::Sym)
       if (c.tail)
-        ns_reduce_kernel<OP, PLANES, kST><<<c.tail, 256, 0, s>>>(t, c.plan, cur, part);
+        ns_reduce_kernel<OP, PLANES, kST><<<c.tail, 256, 0, s>>>(t, c.plan, p, cur, part);
   } else if constexpr (OP != Op::Last) {
-    ns_gemm_big<OP, PLANES><<<items, kBThreads, kBLds, s>>>(t, c.plan, cur, part);
+    ns_gemm_big<OP, PLANES><<<items, kBThreads, kBLds, s>>>(t, c.plan, p, cur, part);
     if (c.tail)
-      ns_reduce_kernel<OP, PLANES, kBT><<<c.tail * 16, 256, 0, s>>>(t, c.plan, cur, part);
+      ns_reduce_kernel<OP, PLANES, kBT><<<c.tail * 16, 256, 0, s>>>(t, c.plan, p, cur, part);
   }
 }
 
 template <int PLANES>
 void iterate(const NsTable& t, const NsFinish& fin, int steps, const NsProducts& p, float* part,
              hipStream_t s) {
-  for (int k = 0; k < steps; ++k) {
-    launch<Op::Gram, PLANES>(t, fin, k & 1, p.gram, part, s);
-    launch<Op::Square, PLANES>(t, fin, k & 1, p.square, part, s);
-    if (k + 1 == steps && !p.apply.big) launch<Op::Last, PLANES>(t, fin, k & 1, p.apply, part, s);
-    else launch<Op::Apply, PLANES>(t, fin, k & 1, p.apply, part, s);
+  constexpr float kSquare = kNsC * kNsScaleB / (kNsScaleA * kNsScaleA);
+  int cur = 0;
+  auto sym = [&](const NsLaunch& c, const Product& q) {
+    launch<Op::Sym, PLANES>(t, c, q, fin, cur, part, s);
+  };
+  auto square = [&](int from, int to) {
+    launch<Op::Square, PLANES>(t, p.square, Product{from, from, to, kSquare}, fin, cur, part, s);
+  };
+  for (int left = steps; left > 0; cur ^= 1) {
+    sym(p.gram, kGram);  // A
+    square(0, 1);        // B
+    int by = 1;
+    float scale = kNsScaleB;  // of what X is multiplied by
+    if (p.paired && left > 1) {
+      sym(p.square, Product{1, 0, 2, 1.0f / kNsScaleB});  // B A
+      sym(p.square, Product{2, 1, 0, 1.0f / kNsScaleB});  // A' = B A B
+      square(0, 2);                                       // B'
+      sym(p.square, Product{2, 1, 0, kNsScaleQ / (kNsScaleB * kNsScaleB)});  // B' B
+      by = 0;
+      scale = kNsScaleQ;
+      --left;
+    }
+    --left;
+    if (left == 0 && !p.apply.big)
+      launch<Op::Last, PLANES>(t, p.apply, Product{by, kX, kX, 1.0f / (scale * kNsScaleX)}, fin,
+                               cur, part, s);
+    else
+      launch<Op::Apply, PLANES>(t, p.apply, Product{by, kX, kX, 1.0f / scale}, fin, cur, part, s);
   }
 }
 
 }  // namespace
 
 void ns_plan(const NsTable& t, int planes, NsProducts* p) {
-  auto of = [&](Op op) { return planes == 2 ? choose<2>(op, t) : choose<1>(op, t); };
-  p->gram = of(Op::Gram);
-  p->square = of(Op::Square);
-  p->apply = of(Op::Apply);
+  auto of = [&](Op op, bool gram) {
+    return planes == 2 ? choose<2>(op, gram, t) : choose<1>(op, gram, t);
+  };
+  p->gram = of(Op::Sym, true);
+  p->square = of(Op::Square, false);
+  p->apply = of(Op::Apply, false);
+  // a pair takes three symmetric products more, and a gram and an apply less
+  p->paired = 3 * p->square.us < 0.95 * (p->gram.us + p->apply.us);
   p->partial_floats = 0;
   for (const NsLaunch* l : {&p->gram, &p->square, &p->apply})
     p->partial_floats =

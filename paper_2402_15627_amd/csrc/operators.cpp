@@ -225,7 +225,8 @@ bool ns_add(pb::NsTable& t, int rows, int cols) {
   x.m = pad(std::min(rows, cols));
   x.n = pad(std::max(rows, cols));
   // rows an odd number of 64 values apart: rows a power of two apart lie in few of the
-  // L2's channels (256 x 1024, two planes: the first product 20 us, RESULT so)
+  // L2's channels (five steps of 2048 x 2048 in fp32 849 us, so 816; 2048 x 8192 in bf16
+  // 827 and 792; 256 x 1024 the same)
   x.ldm = x.m | pb::kNsPad;
   x.ldn = x.n | pb::kNsPad;
   const long long tiles =
@@ -248,9 +249,8 @@ NsLayout ns_layout(pb::NsTable& t, int planes, char* base, pb::NsProducts* p) {
     const size_t small = align256((size_t)planes * x.m * x.ldm * 2);
     x.x[0] = (_Float16*)(base + o);
     x.x[1] = (_Float16*)(base + o + big);
-    x.a = (_Float16*)(base + o + 2 * big);
-    x.b = (_Float16*)(base + o + 2 * big + small);
-    o += 2 * big + 2 * small;
+    o += 2 * big;
+    for (int k = 0; k < pb::ns_symmetric(*p); ++k, o += small) x.s[k] = (_Float16*)(base + o);
   }
   L.part = o;
   L.total = o + align256(p->partial_floats * sizeof(float));

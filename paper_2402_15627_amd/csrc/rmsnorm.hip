@@ -445,7 +445,9 @@ int rms_backward_parts(long long rows, int cols) {
   by_width(cols, [&](auto tpr, auto) {
     constexpr int TPR = decltype(tpr)::value;
     constexpr int per = TPR < 256 ? 256 / TPR : 1;
-    n = std::min<long long>((rows + per - 1) / per, TPR > 256 ? kPartsWide : kParts);
+    const long long sets = (rows + per - 1) / per, most = TPR > 256 ? kPartsWide : kParts;
+    const long long each = (sets + most - 1) / most;  // sets of rows a workgroup
+    n = sets ? (sets + each - 1) / each : 0;
   });
   return (int)n;
 }

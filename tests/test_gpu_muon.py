@@ -125,6 +125,35 @@ def test_orthogonalize_steps(steps):
     assert off(f64(out), ref) <= allowed(u, ref, "f32", steps)
 
 
+# Much wider than tall: two steps to one product with the matrix.  The emulation above
+# goes step by step, which is no more accurate; a pair rounds B A, A' and B' B more, by at
+# most 3 r each (as at COHERENT): 6 r in the singular values, under 30 r after five steps.
+@pytest.mark.parametrize("steps", [1, 2, 4, 5])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("r,c", [(1, 40000), (30000, 60), (64, 16384), (250, 20000), (9000, 500)],
+                         ids=lambda v: str(v))
+def test_orthogonalize_wide(dtype, r, c, steps):
+    import torch
+    from paper_2402_15627_amd import pblock as pb
+    _say(f"[gpu] orthogonalize wide {dtype} {r} x {c} steps={steps}")
+    act = torch.bfloat16 if dtype == "bf16" else torch.float32
+    rng = np.random.default_rng(r + c + steps)
+    for low in (False, True):
+        x = torch.from_numpy(matrix(rng, r, c, low)).to(act).cuda()
+        out = torch.empty_like(x)
+        part = [pb.ortho_tensor(x, out)]
+        ws = torch.empty(pb.pblock_orthogonalize_workspace_bytes(part, dtype), dtype=torch.uint8,
+                         device="cuda").fill_(255)
+        pb.pblock_orthogonalize(part, dtype, ws, steps)
+        u = f64(x)
+        ref = oo.newton_schulz(u, steps)
+        e, tol = off(f64(out), ref), allowed(u, ref, dtype, steps, out=dtype)
+        if dtype == "f32":
+            tol = max(tol, COHERENT) if min(r, c) == 1 else tol + 32 * 2.0 ** -22
+        _say(f"      off {e:.2e} of {tol:.2e}")
+        assert e <= tol
+
+
 def test_orthogonalize_extremes():
     """Zeros stay zeros; a matrix below eps shrinks towards them; one value alone, the
     largest of fp32, and a single NaN, which fills its matrix and no other."""

@@ -122,6 +122,27 @@ def test_newton_schulz_stays_in_the_range_that_the_planes_are_scaled_for():
     assert 1.2024 * 32768 < 65504 and 1.446 * 32768 < 65504 and a * 16384 < 65504
 
 
+def test_two_newton_schulz_steps_by_one_product_with_the_matrix():
+    """X'' = (B' B) X with A' = (B A) B for A = X X^T, what pairs of steps compute, and
+    the range of its further matrices: B A <= 1.446 and B' B <= 11.87."""
+    x = RNG(6).standard_normal((7, 31))
+    x /= np.linalg.norm(x) + 1e-7
+    a, b, c = oo.NS
+    poly = lambda t: a * np.eye(len(t)) + b * t + c * t @ t
+    g = x @ x.T
+    p = poly(g)
+    q = poly(p @ g @ p)
+    np.testing.assert_allclose(q @ p @ x, oo.newton_schulz(RNG(6).standard_normal((7, 31)), 2), atol=1e-12)
+    s = np.linspace(0, 1, 200001)
+    for _ in range(16):
+        f = a + b * s ** 2 + c * s ** 4
+        s1 = np.abs(f) * s
+        f1 = a + b * s1 ** 2 + c * s1 ** 4
+        assert (f * s * s).max() <= 1.446 and (f * f1).max() <= 11.87
+        s = s1
+    assert 1.446 * 32768 < 65504 and 11.87 * 4096 < 65504
+
+
 @pytest.mark.parametrize("nesterov", [False, True])
 def test_muon_step_by_hand(nesterov):
     """One row: the orthogonalised update is the unit row times the polynomial of 1."""
