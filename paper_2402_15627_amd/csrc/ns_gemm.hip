@@ -8,12 +8,12 @@
 //
 //   A = X X^T,  B = f(A),  A' = (B A) B,  B' = f(A'),  X'' = (B' B) X
 //
-// m x m products for two of m x m x n: with half of each symmetric product computed,
+// Three m x m products for two with X: with half of each symmetric product computed,
 // 8 m^3 + 3 (n - m) m^2 operations for 8 m^3 + 6 (n - m) m^2.  (Over more steps the
 // spread of A's eigenvalues, the square of X's, costs accuracy: five steps from one A
 // lose two digits, a pair none: 256 x 1024, 16 directions in noise, 2.0e-6 off either
-// way, 8 in a tenth of the noise 5.0e-6 in pairs and 8.3e-6 step by step; fp32 2.1e-6 and
-// 4.6e-6.)
+// way, 8 in a tenth of the noise 5.0e-6 in pairs and 8.3e-6 step by step, where fp32 is
+// 2.1e-6 and 4.6e-6 off.)
 //
 //   Sym     L R, L and R symmetric, or X X^T: tiles on and above the diagonal, each
 //           written to its mirror image too
@@ -270,8 +270,8 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
   const int wm = (wave & 3) * kWTM, wn = (wave >> 2) * kWTN;
 
   // Who moves what: every wave its own 4 KB of each operand; but Apply with two planes
-  // the first wave of each SIMD both 4 KB regions of its SIMD (two 6144 x 12288: 35.0 ms
-  // and 35.2; one plane, three of 5120 x 5120 and 20480: 12.3 and 12.2).
+  // the first wave of each SIMD both 4 KB regions of its SIMD (two 6144 x 12288: 29.2 ms
+  // and 29.3; one plane, 5120 x 5120 twice and 20480 x 5120: 10.56 and 10.51).
   constexpr bool kOwn = BK || PLANES == 1;
   constexpr int kReg = kOwn ? 1 : 2;
   constexpr int kDmaPerTile = 2 * kReg * kBPieces;
@@ -812,8 +812,13 @@ void ns_plan(const NsTable& t, int planes, NsProducts* p) {
   p->gram = of(Op::Sym, true);
   p->square = of(Op::Square, false);
   p->apply = of(Op::Apply, false);
-  // a pair takes three symmetric products more, and a gram and an apply less
-  p->paired = 3 * p->square.us < 0.95 * (p->gram.us + p->apply.us);
+  // A pair takes three symmetric products more, and a gram and an apply less: one launch
+  // more, which costs about kLaunchUs less here than estimated by itself.  Five steps, in
+  // pairs and step by step: fp32 64 x 1024 99 and 106 us, 256 x 1024 145 and 144, 2048 x
+  // 4096 1037 and 1085, 4096 x 5120 4556 and 4416; bf16 64 x 4096 98 and 111, 1024 x 4096
+  // 261 and 291 (chosen); 1024 x 2048, chosen too, 206 and 201.
+  constexpr double kLaunchUs = 5.0;
+  p->paired = 3 * p->square.us - kLaunchUs < 0.95 * (p->gram.us + p->apply.us);
   p->partial_floats = 0;
   for (const NsLaunch* l : {&p->gram, &p->square, &p->apply})
     p->partial_floats =
