@@ -673,9 +673,10 @@ pb_status pblock_rope_backward(const pb_rope_config* cfg, int n_tensors,
  * from elsewhere (the residual's other use).  With g = dy gamma,
  *   dx = dsum + r (g - s r^2 mean(g s))   act: the gradient of x, and of resid
  *   dgamma = sum over rows of dy s r      [cols] fp32, overwritten
- * dx may be dy, dsum or s, as a whole (as above for sum and y: an output that shares
- * part of an input's memory is refused).  ws: pblock_rmsnorm_workspace_bytes(cfg) bytes, 256-byte
- * aligned.  Results do not depend on timing (fixed order, no atomics).
+ * dx may be dy, dsum or s, as a whole.  Every other sharing of memory by an output
+ * and another tensor (or ws) is refused, in both calls.  ws:
+ * pblock_rmsnorm_workspace_bytes(cfg) bytes, 256-byte aligned, one for each call that
+ * may overlap another.  Results do not depend on timing (fixed order, no atomics).
  *
  * Pointers are aligned to their element; cols a multiple of 8 with 16-byte aligned
  * pointers (8 for q8) runs fastest.  rows may be 0 (the backward then writes zeros
@@ -717,9 +718,9 @@ pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s,
  * copy_dtype.  Each is [rows, cols] with ld elements from row to row: a slice of a
  * packed weight (rows of w_in; columns of w_out, ld = K_out) is a matrix of its
  * own.  scale is the caller's rule for the shape (0.2 sqrt(max(rows, cols)), say).
- * Matrices with rows = 0 or cols = 0 are allowed (nothing is touched).  No param or
- * momentum may share memory with another or with a grad (refused, unless they interleave
- * with two lds, which is not seen).
+ * Matrices with rows = 0 or cols = 0 are allowed (nothing is touched).  No param,
+ * momentum, param_copy or ws may share memory with another of them or with a grad
+ * (refused, unless they interleave with two lds, which is not always seen).
  *
  * products: PB_F32 carries 22 bits of every factor (each fp16 value with its
  * remainder, three matrix products for one): the update is as exact as fp32

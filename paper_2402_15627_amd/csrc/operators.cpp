@@ -49,16 +49,43 @@ struct Span {
   int64_t rows;
 };
 // Whether two such are seen to share memory: apart as a whole they do not, and of one
-// leading dimension they may interleave.  (Of two leading dimensions, interleaved: not
-// seen.)
+// leading dimension they may interleave.  (Of two leading dimensions: seen where the
+// first element of one lies in a row of the other.)
 bool overlap(const Span& a, const Span& b, size_t e) {
   if (!a.rows || !b.rows || !a.p || !b.p) return false;
   const Span &lo = (uintptr_t)a.p <= (uintptr_t)b.p ? a : b, &hi = &lo == &a ? b : a;
   const size_t off = ((uintptr_t)hi.p - (uintptr_t)lo.p) / e;  // elements from lo to hi
   if (off >= (size_t)(lo.rows - 1) * lo.ld + lo.width) return false;
+  if (lo.rows > 1 && off % lo.ld < lo.width) return true;
   if (lo.ld != hi.ld && lo.rows > 1 && hi.rows > 1) return false;
   const size_t ld = lo.rows > 1 ? lo.ld : hi.ld, at = off % ld;
   return at < lo.width || ld - at < hi.width;
+}
+// A workspace and the rows of an element of e bytes.
+bool overlap(const void* ws, size_t bytes, const Span& x, size_t e) {
+  return overlap(Span{ws, bytes, bytes, 1}, Span{x.p, x.ld * e, x.width * e, x.rows}, 1);
+}
+
+// A dense range of a call's memory.  An output may be an input where both are rows of
+// the same size that the call reads before it writes them.
+struct Range {
+  const char* name;
+  const void* p;
+  size_t bytes;
+  bool out, same;
+};
+template <size_t N>
+pb_status check_apart(const Range (&r)[N]) {
+  for (size_t i = 0; i < N; ++i)
+    for (size_t j = 0; j < i; ++j) {
+      const Range &a = r[i], &b = r[j];
+      if (!a.p || !b.p || !(a.out || b.out)) continue;
+      if (a.p == b.p && a.same && b.same && !(a.out && b.out)) continue;
+      const uintptr_t pa = (uintptr_t)a.p, pb = (uintptr_t)b.p;
+      if (pa < pb + b.bytes && pb < pa + a.bytes)
+        return fail(PB_ERR_INVALID_ARG, "%s and %s overlap", a.name, b.name);
+    }
+  return PB_OK;
 }
 
 // A call without any element: as finish_launches(), but no HIP call is made.
@@ -194,10 +221,6 @@ pb_status check_rms(const pb_rmsnorm_config* c) {
   return PB_OK;
 }
 
-Span dense(const pb_rmsnorm_config* c, const void* p) {
-  return {p, (size_t)c->cols, (size_t)c->cols, c->rows};
-}
-
 // ------------------------------------------------------------- Muon step
 static_assert(PB_MUON_MAX_TENSORS == pb::kNsMaxTensors, "tensor limit");
 
@@ -290,6 +313,19 @@ pb_status ns_launch(pb::NsTable& t, const pb::NsScalars& sc, pb::NsMode mode, pb
   pb::NsProducts p;
   const NsLayout L = ns_layout(t, sc.planes, (char*)ws, &p);
   PB_CHECK(check_ws(ws, ws_bytes, L.total));
+  for (int i = 0; i < t.count; ++i) {
+    const pb::NsMat& x = t.mat[i];
+    const size_t e = mode == pb::NsMode::Bf16 ? 2 : 4, e_copy = copy_dt == pb::Dt::BF16 ? 2 : 4;
+    auto span = [&](const void* p, long long ld) {
+      return Span{p, (size_t)ld, (size_t)x.cols, x.rows};
+    };
+    if (overlap(ws, L.total, span(x.src, x.ld_src), e) ||
+        overlap(ws, L.total, span(x.out, x.ld_out), e) ||
+        overlap(ws, L.total, span(x.w, x.ld_src), 4) ||
+        overlap(ws, L.total, span(x.mom, x.ld_src), 4) ||
+        overlap(ws, L.total, span(x.copy, x.ld_src), e_copy))
+      return fail(PB_ERR_INVALID_ARG, "ws overlaps tensor %d", i);
+  }
   char* w = (char*)ws;
   pb::launch_newton_schulz(t, sc, mode, copy_dt, p, (double*)(w + L.partial),
                            (double*)(w + L.norm), (float*)(w + L.part), stream);
@@ -333,17 +369,17 @@ pb_status pblock_rmsnorm_forward(const pb_rmsnorm_config* cfg, const void* x, co
     if (!y && !q8) return fail(PB_ERR_INVALID_ARG, "y and q8 are both NULL");
     if (!q8 != !scales) return fail(PB_ERR_INVALID_ARG, "q8 and scales come together");
     if (sum && !resid) return fail(PB_ERR_INVALID_ARG, "sum without resid");
-    const void* outs[2] = {sum, y};
-    const void* ins[2] = {x, resid};
-    for (const void* o : outs)
-      for (const void* i : ins)
-        if (o != i && overlap(dense(cfg, o), dense(cfg, i), e))
-          return fail(PB_ERR_INVALID_ARG, "sum or y overlaps a part of x or resid");
-    if (overlap(dense(cfg, sum), dense(cfg, y), e))
-      return fail(PB_ERR_INVALID_ARG, "sum and y overlap");
   }
   PB_CHECK(check_ptr(gamma, e, "gamma"));
   if (cfg->rows == 0) return nothing_to_do();
+  const size_t n = (size_t)cfg->rows * cfg->cols, rows = (size_t)cfg->rows * 4;
+  const int groups = cfg->group ? (cfg->cols + cfg->group - 1) / cfg->group : 1;
+  const Range ranges[] = {
+      {"x", x, n * e, false, true},     {"resid", resid, n * e, false, true},
+      {"sum", sum, n * e, true, true},  {"y", y, n * e, true, true},
+      {"q8", q8, n, true, false},       {"scales", scales, rows * groups, true, false},
+      {"rstd", rstd, rows, true, false}, {"gamma", gamma, cfg->cols * e, false, false}};
+  PB_CHECK(check_apart(ranges));
   pb::RmsForward a{};
   a.x = x;
   a.resid = resid;
@@ -378,13 +414,21 @@ pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s, c
     PB_CHECK(check_ptr(dy, e, "dy"));
     PB_CHECK(check_opt(dsum, e, "dsum"));
     PB_CHECK(check_ptr(dx, e, "dx"));
-    for (const void* i : {s, dy, dsum})
-      if (dx != i && overlap(dense(cfg, dx), dense(cfg, i), e))
-        return fail(PB_ERR_INVALID_ARG, "dx overlaps a part of s, dy or dsum");
   }
   PB_CHECK(check_ptr(gamma, e, "gamma"));
   PB_CHECK(check_ptr(dgamma, 4, "dgamma"));
-  PB_CHECK(check_ws(ws, ws_bytes, pblock_rmsnorm_workspace_bytes(cfg)));
+  const size_t need = pblock_rmsnorm_workspace_bytes(cfg);
+  PB_CHECK(check_ws(ws, ws_bytes, need));
+  const size_t n = (size_t)cfg->rows * cfg->cols;
+  const Range ranges[] = {{"s", s, n * e, false, true},
+                          {"dy", dy, n * e, false, true},
+                          {"dsum", dsum, n * e, false, true},
+                          {"dx", dx, n * e, true, true},
+                          {"gamma", gamma, cfg->cols * e, false, false},
+                          {"rstd", rstd, (size_t)cfg->rows * 4, false, false},
+                          {"dgamma", dgamma, (size_t)cfg->cols * 4, true, false},
+                          {"ws", ws, need, true, false}};
+  PB_CHECK(check_apart(ranges));
   pb::RmsBackward a{};
   a.s = s;
   a.gamma = gamma;
@@ -447,6 +491,7 @@ pb_status pblock_muon_step(const pb_muon_config* cfg, int n_tensors, const pb_mu
     m.decay = x.weight_decay;
     m.scale = x.scale;
   }
+  const size_t e_copy = size_of(copy_dtype);
   for (int i = 0; i < t.count; ++i)
     for (int j = 0; j < t.count; ++j) {
       const pb::NsMat &x = t.mat[i], &y = t.mat[j];
@@ -454,11 +499,16 @@ pb_status pblock_muon_step(const pb_muon_config* cfg, int n_tensors, const pb_mu
         return Span{p, (size_t)v.ld_src, (size_t)v.cols, v.rows};
       };
       if (i < j && (overlap(span(x, x.w), span(y, y.w), 4) ||
-                    overlap(span(x, x.mom), span(y, y.mom), 4)))
-        return fail(PB_ERR_INVALID_ARG, "two tensors overlap in param or momentum");
+                    overlap(span(x, x.mom), span(y, y.mom), 4) ||
+                    overlap(span(x, x.copy), span(y, y.copy), e_copy)))
+        return fail(PB_ERR_INVALID_ARG, "two tensors overlap in param, momentum or copy");
       if (overlap(span(x, x.w), span(y, y.mom), 4) || overlap(span(x, x.w), span(y, y.src), 4) ||
           overlap(span(x, x.mom), span(y, y.src), 4))
         return fail(PB_ERR_INVALID_ARG, "param, grad and momentum overlap");
+      auto bytes = [](Span v, size_t e) { return Span{v.p, v.ld * e, v.width * e, v.rows}; };
+      for (const void* p : {(const void*)y.w, (const void*)y.mom, y.src})
+        if (overlap(bytes(span(x, x.copy), e_copy), bytes(span(y, p), 4), 1))
+          return fail(PB_ERR_INVALID_ARG, "param_copy overlaps a param, grad or momentum");
     }
   pb::NsScalars sc{};
   sc.lr = cfg->lr;

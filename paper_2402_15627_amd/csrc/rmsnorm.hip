@@ -395,7 +395,7 @@ void by_width(int H, F f) {
   else if (pieces <= 1024) f(integral_constant<int, 256>{}, integral_constant<int, 4>{});
   else if (pieces <= 1536) f(integral_constant<int, 512>{}, integral_constant<int, 3>{});
   else if (pieces <= 2048) f(integral_constant<int, 512>{}, integral_constant<int, 4>{});
-  else if (pieces <= 3072) f(integral_constant<int, 1024>{}, integral_constant<int, 3>{});
+  else if (pieces <= 3 * 1024) f(integral_constant<int, 1024>{}, integral_constant<int, 3>{});
   else f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
 }
 

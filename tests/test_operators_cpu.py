@@ -69,7 +69,7 @@ def test_rope_scaling_values_are_read_only_by_their_kind():
 # ------------------------------------------------- root-mean-square norm
 def rms(**over):
     cfg = pb.rmsnorm_config(4, 64)
-    a = dict(x=FAKE, resid=None, gamma=FAKE, sum=None, y=FAKE, q8=None, scales=None, rstd=None)
+    a = dict(x=FAKE, resid=None, gamma=FAKE + (1 << 24), sum=None, y=FAKE, q8=None, scales=None, rstd=None)
     for k, v in over.items():
         if k in a:
             a[k] = v
@@ -78,9 +78,10 @@ def rms(**over):
     return pb.load_library().pblock_rmsnorm_forward(ctypes.byref(cfg), *a.values(), None)
 
 
-def rms_back(nbytes=None, ws=FAKE, **over):
+def rms_back(nbytes=None, ws=FAKE + (1 << 26), **over):
     cfg = pb.rmsnorm_config(4, 64)
-    a = dict(s=FAKE, gamma=FAKE, rstd=FAKE, dy=FAKE, dsum=None, dx=FAKE, dgamma=FAKE)
+    a = dict(s=FAKE, gamma=FAKE + (1 << 24), rstd=FAKE + (1 << 25), dy=FAKE, dsum=None, dx=FAKE,
+             dgamma=FAKE + (3 << 24))
     for k, v in over.items():
         if k in a:
             a[k] = v
@@ -138,7 +139,7 @@ def test_rmsnorm_without_rows_and_its_workspace():
 
 
 # ------------------------------------------------------------- Muon step
-def muon(ws=FAKE, nbytes=1 << 30, copy=pb.PB_BF16, n=None, tensors=None, cfg_null=False, **over):
+def muon(ws=FAKE + (1 << 32), nbytes=1 << 30, copy=pb.PB_BF16, n=None, tensors=None, cfg_null=False, **over):
     cfg = pb.muon_config(1e-3)
     x = dict(param=FAKE, grad=FAKE + (1 << 20), momentum=FAKE + (2 << 20), param_copy=None, rows=8, cols=16, ld=16,
              weight_decay=0.1, scale=1.0)
@@ -184,7 +185,7 @@ def test_muon_refusals(over, status):
 ])
 def test_orthogonalize_refusals(over, status):
     a = dict(n=1, x=pb.OrthoTensor(FAKE, FAKE, 8, 16, 16, 16), dtype=pb.PB_BF16, steps=5, eps=1e-7,
-             ws=FAKE, nbytes=1 << 30)
+             ws=FAKE + (1 << 32), nbytes=1 << 30)
     a.update(over)
     assert pb.load_library().pblock_orthogonalize(a["n"], (pb.OrthoTensor * 1)(a["x"]), a["dtype"],
                                                   a["steps"], a["eps"], a["ws"], a["nbytes"],
@@ -223,6 +224,38 @@ def test_muon_and_orthogonalize_refuse_matrices_that_overlap():
     assert call(O(FAKE, f(8), 8, 16, 64, 64)) == BAD
     assert call(O(FAKE, FAKE, 8, 16, 64, 64), O(f(32), f(4), 8, 16, 64, 64)) == BAD
     assert call(O(FAKE, FAKE, 8, 16, 64, 64), O(f(16), f(32), 8, 16, 64, 64)) == SMALL
+
+
+def test_muon_refuses_copies_and_workspaces_over_tensors():
+    f = lambda n: FAKE + 4 * n  # noqa: E731
+    g, m, w2, g2, m2 = (f(k << 20) for k in range(1, 6))
+    M = lambda copy, w=FAKE, gr=g, mo=m: pb.MuonTensor(w, gr, mo, copy, 8, 16, 64, 0.0, 1.0)  # noqa: E731
+    for copy in (FAKE, FAKE + 64 * 4, g + 32, m + 3 * 256):  # bf16, rows of 128 bytes; of 256
+        assert muon(tensors=[M(copy)]) == BAD and "copy" in pb.pblock_last_error()
+    c = FAKE + (1 << 28)
+    assert muon(tensors=[M(c), M(c + 30, w2, g2, m2)]) == BAD and "copy" in pb.pblock_last_error()
+    assert muon(tensors=[M(c), M(c + 32, w2, g2, m2)], nbytes=1) == SMALL
+    assert muon(tensors=[M(FAKE)], copy=pb.PB_F32) == BAD
+    need = pb.pblock_muon_workspace_bytes(pb.muon_config(1e-3), [M(c)])
+    for ws in (FAKE, FAKE - need + 256, m, c + 7 * 128, g - 256):
+        assert muon(tensors=[M(c)], ws=ws // 256 * 256) == BAD and "ws" in pb.pblock_last_error()
+    o = pb.OrthoTensor(FAKE, c, 8, 16, 64, 64)
+    for ws in (FAKE, c):
+        assert pb.load_library().pblock_orthogonalize(1, (pb.OrthoTensor * 1)(o), pb.PB_F32, 5, 1e-7, ws,
+                                                      1 << 30, None) == BAD
+        assert "ws" in pb.pblock_last_error()
+
+
+def test_rmsnorm_refuses_outputs_over_other_tensors():
+    """x is 512 bytes at FAKE, gamma 128 at FAKE + 2^24."""
+    gamma, far = FAKE + (1 << 24), FAKE + (1 << 27)
+    for over in (dict(q8=FAKE, scales=far), dict(q8=FAKE + 511, scales=far, y=far + 4096),
+                 dict(q8=far, scales=FAKE + 508), dict(q8=far, scales=far + 252), dict(rstd=FAKE),
+                 dict(rstd=gamma + 124), dict(y=gamma - 510), dict(resid=far, sum=gamma)):
+        assert rms(**over) == BAD and "overlap" in pb.pblock_last_error(), over
+    for over in (dict(dgamma=FAKE + 508), dict(dgamma=gamma), dict(dx=gamma), dict(ws=FAKE),
+                 dict(dx=FAKE + (1 << 25)), dict(dgamma=FAKE + (1 << 26))):
+        assert rms_back(**over) == BAD and "overlap" in pb.pblock_last_error(), over
 
 
 def test_empty_matrices_and_workspaces():
