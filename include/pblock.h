@@ -655,7 +655,8 @@ pb_status pblock_rope_backward(const pb_rope_config* cfg, int n_tensors,
  *   r = 1 / sqrt(mean(s^2) + eps)
  *   y = s r gamma
  *
- * y is formed from the unrounded s, in 32 bits (64 with q8), and rounded once.
+ * y is formed from the unrounded s, in 32 bits (64 with q8, and for the mean), and
+ * rounded once.
  * Outputs, each left out when NULL, but y or q8 must be there:
  *   sum  [rows, cols] act   s rounded, the next residual (NULL unless resid is
  *                           given; may be x or resid)

@@ -255,3 +255,22 @@ def test_rmsnorm_streams_and_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs(sets[0]), w)), r
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rmsnorm_of_rows_whose_squares_pass_fp32(dtype):
+    """Rows of 1e30 and 1e-30 beside ordinary ones, eps = 0: the squares do not fit into
+    fp32, the results do."""
+    import torch
+    from paper_2402_15627_amd import pblock as pb
+    _say(f"[gpu] rmsnorm range {dtype}")
+    for cols in (100, 1000, 5120):
+        t = make(dtype, 6, cols, seed=cols, resid=False)
+        scale = torch.tensor([1e30, 1.0, 1e-30, 1e19, 1e-19, 2e37], device="cuda")[:, None]
+        x = (t["x"].float().clamp(-8, 8) * scale).to(t["act"])
+        y, rstd = torch.empty_like(x), torch.empty(6, device="cuda")
+        cfg = pb.rmsnorm_config(6, cols, eps=0.0, dtype=dtype)
+        pb.pblock_rmsnorm_forward(cfg, x, t["gamma"], y, rstd=rstd)
+        _, rr, ry = oo.rmsnorm(f64(x), f64(t["gamma"]), 0.0)
+        assert np.all(np.abs(f64(y) - ry) <= (t["half"] + 2.0 ** -18) * np.abs(ry))
+        assert np.all(np.abs(f64(rstd) - rr) <= 2.0 ** -18 * rr)
