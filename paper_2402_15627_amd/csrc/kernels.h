@@ -155,19 +155,18 @@ struct NsScalars {
 };
 // Where the updates come from and go to.
 enum class NsMode { Muon, Bf16, F32 };
-// How a product is launched.  Its items are tiles, or K-slices of tiles: tiles 0 ..
-// n_full - 1 whole, then `splits` slices of each of the `tail` tiles after them, whose
-// fp32 partial tiles another launch sums.  Tiles count through the matrices in the order
-// of mat[] (longest K first): first[i] is that of matrix mat[i].
+// How a product is launched.  Its items are tiles, or K-slices of tiles: n_full whole
+// tiles, then `splits` slices of each of the next `tail` tiles, whose fp32 partial tiles
+// another launch sums, then whole tiles again.  Tiles count through the matrices in the
+// order of mat[] (longest K first): first[i] is that of matrix mat[i].
 struct NsPlan {
   int first[kNsMaxTensors + 1];
   int mat[kNsMaxTensors];
-  int n_full, splits;
+  int n_full, tail, splits;
 };
 struct NsLaunch {
   bool big;  // 256 x 256 tiles, else 64 x 64
   NsPlan plan;
-  int tail;
   double us;  // estimate
 };
 struct NsProducts {

@@ -164,17 +164,20 @@ PB_DEV int place_of(const NsPlan& p, int count, int tile) {
 struct Item {
   int tile, slice, place;
 };
-PB_DEV Item item_of(const NsPlan& p, int count, int b, int n) {
+PB_DEV Item item_of(const NsPlan& p, int count, int b) {
+  const int slices = p.tail * p.splits, j = b - p.n_full;
   Item it{b, -1, 0};
-  if (b >= p.n_full) {
-    const int j = xcd_remap(b - p.n_full, n - p.n_full);
-    it.tile = p.n_full + j / p.splits;
-    it.slice = j % p.splits;
+  if (j >= 0 && j < slices) {
+    const int k = xcd_remap(j, slices);
+    it.tile = p.n_full + k / p.splits;
+    it.slice = k % p.splits;
     it.place = place_of(p, count, it.tile);
   } else {
+    int lo = 0, hi = p.n_full;  // the whole tiles before the cut ones, or those after
+    if (j >= 0) lo = hi + p.tail, hi = 0x7fffffff, b -= slices - p.tail;
     it.place = place_of(p, count, b);
-    const int f = p.first[it.place];
-    it.tile = f + xcd_remap(b - f, min(p.first[it.place + 1], p.n_full) - f);
+    const int f = max(p.first[it.place], lo);
+    it.tile = f + xcd_remap(b - f, min(p.first[it.place + 1], hi) - f);
   }
   return it;
 }
@@ -247,7 +250,7 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
                                                             int cur, float* __restrict__ part) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   constexpr bool BK = symmetric(OP);  // the B operand is K-contiguous
-  const Item it = item_of(plan, t.count, blockIdx.x, gridDim.x);
+  const Item it = item_of(plan, t.count, blockIdx.x);
   const NsMat& x = t.mat[plan.mat[it.place]];
   int tm, tn;
   tile_at<OP, kBT>(x, it.tile - plan.first[it.place], tm, tn);
@@ -565,7 +568,7 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
                                                               float* __restrict__ part) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   constexpr bool BK = symmetric(OP);
-  const Item it = item_of(plan, t.count, blockIdx.x, gridDim.x);
+  const Item it = item_of(plan, t.count, blockIdx.x);
   const NsMat& x = t.mat[plan.mat[it.place]];
   int tm, tn;
   tile_at<OP, kST>(x, it.tile - plan.first[it.place], tm, tn);
@@ -682,14 +685,55 @@ template <int PLANES>
 constexpr double kSmallStepUs = PLANES == 2 ? 2.05 : 1.9;
 constexpr double kSmallTileUs = 2.5, kSmallUs = 5.0, kSmallSplitUs = 7.0;
 
-// The tiles that are estimated to end sooner: 256 x 256, whole rounds of them and the
-// tiles of the last, partial round (or of all, where they do not fill one) cut along K;
-// or 64 x 64, all of them cut where they are few and K is long.
+// When the last of kCUs CUs is done that take groups of equal items one after the other,
+// each CU the next item as it ends one.
+class Makespan {
+ public:
+  void take(int n, double us) {
+    if (n <= 0) return;
+    if (n > 4 * kCUs) {  // (whole rounds in one step)
+      const int r = n / kCUs - 2;
+      for (int i = 0; i < n_; ++i) c_[i].at += r * us;
+      n -= r * kCUs;
+    }
+    while (n > 0) {
+      int first = 0;
+      for (int i = 1; i < n_; ++i)
+        if (c_[i].at < c_[first].at) first = i;
+      const double at = c_[first].at + us;
+      int k = std::min(n, c_[first].cus), to = 0;
+      n -= k;
+      while (to < n_ && c_[to].at != at) ++to;
+      if (to == n_ && n_ == kMost) to = first;  // (never seen: an estimate all the same)
+      if (to == n_) c_[n_++] = {at, 0};
+      c_[to].cus += k;
+      if ((c_[first].cus -= k) == 0) c_[first] = c_[--n_];
+    }
+  }
+  double last() const {
+    double at = 0.0;
+    for (int i = 0; i < n_; ++i) at = std::max(at, c_[i].at);
+    return at;
+  }
+
+ private:
+  static constexpr int kMost = 64;
+  struct {
+    double at;
+    int cus;
+  } c_[kMost + 1] = {{0.0, kCUs}};
+  int n_ = 1;
+};
+
+// The tiles that are estimated to end sooner: 256 x 256, whole rounds of them and tiles
+// after those cut along K, all or the ones of the longest K among them; or 64 x 64, all of
+// them cut where they are few and K is long.  (The symmetric products of the 175B share,
+// 600 tiles of K = 6144 and 84 of 1536: 88 of the long ones cut in two 1.11 ms, those and
+// the short ones cut in five 1.26.)
 template <int PLANES>
 NsLaunch choose(Op op, bool gram, const NsTable& t) {
   NsPlan plan{};
   auto len = [&](int i) { return (gram ? t.mat[i].n : t.mat[i].m) / kK<PLANES>; };
-  auto small_len = [&](int i) { return (len(i) + kSWaves - 1) / kSWaves; };
   for (int i = 0; i < t.count; ++i) {  // the longest K first
     int k = i;
     for (; k > 0 && len(plan.mat[k - 1]) < len(i); --k) plan.mat[k] = plan.mat[k - 1];
@@ -700,54 +744,57 @@ NsLaunch choose(Op op, bool gram, const NsTable& t) {
       plan.first[i + 1] = plan.first[i] + tiles_of(op, t.mat[plan.mat[i]], size);
     return plan.first[t.count];
   };
-  // Steps until the last item ends, and rounds, the items (longest first) taken kCUs at
-  // a time; l(i): steps of a tile of matrix i, those past n_full in `splits` items
-  struct Rounds {
-    int steps, count;
-  };
-  auto rounds = [&](auto l, int n_full, int splits) {
-    Rounds r{0, 0};
-    int at = 0;  // items so far
-    for (int i = 0; i < t.count; ++i) {
-      const int nk = l(plan.mat[i]), cut = (nk + splits - 1) / splits;
-      const int whole = std::max(0, std::min(plan.first[i + 1], n_full) - plan.first[i]);
-      const int rest = plan.first[i + 1] - plan.first[i] - whole;
-      for (int part = 0; part < 2; ++part) {
-        const int n = part ? rest * splits : whole;
-        const int starts = (at + n + kCUs - 1) / kCUs - r.count;  // rounds that begin here
-        r.steps += starts * (part ? cut : nk);
-        r.count += starts;
-        at += n;
+  // The items' time, tiles n_full .. n_full + tail - 1 in `splits` slices; us(nk): of an
+  // item of nk K-tiles
+  auto items = [&](auto us, int n_full, int tail, int splits) {
+    Makespan m;
+    for (int part = 0; part < 3; ++part) {
+      const int lo = part == 0 ? 0 : part == 1 ? n_full : n_full + tail;
+      const int hi = part == 0 ? n_full : part == 1 ? n_full + tail : plan.first[t.count];
+      for (int i = 0; i < t.count; ++i) {
+        const int n = std::min(plan.first[i + 1], hi) - std::max(plan.first[i], lo);
+        const int nk = len(plan.mat[i]);
+        if (part == 1) m.take(n * splits, us((nk + splits - 1) / splits));
+        else m.take(n, us(nk));
       }
     }
-    return r;
+    return m.last();
   };
   NsLaunch c{};
   double best = INFINITY;
-  auto offer = [&](bool big, int n_full, int splits, int tail, double us) {
+  auto offer = [&](bool big, int n_full, int tail, int splits, double us) {
     if (us >= best) return;
     best = us;
     c.big = big;
     c.plan = plan;
     c.plan.n_full = n_full;
+    c.plan.tail = tail;
     c.plan.splits = splits;
-    c.tail = tail;
     c.us = us;
   };
+  auto big_us = [](int nk) { return kStepUs<PLANES> * nk; };
   int tiles = count(kBT);
-  offer(true, tiles, 1, 0, kTileUs + kStepUs<PLANES> * rounds(len, tiles, 1).steps);
+  offer(true, tiles, 0, 1, kTileUs + items(big_us, tiles, 0, 1));
   for (int keep = tiles / kCUs; keep >= std::max(0, tiles / kCUs - 1); --keep) {
-    const int full = keep * kCUs, tail = tiles - full;
-    for (int s = 2; tail > 0 && s <= 16 && tail * s <= 4 * kCUs; ++s)
-      offer(true, full, s, tail,
-            kTileUs + kStepUs<PLANES> * rounds(len, full, s).steps + kSplitUs + 0.05 * tail * s);
+    const int full = keep * kCUs;
+    int end = 0;  // of the matrices with the K of tile `full`
+    for (int i = 0; i < t.count && end <= full; ++i)
+      if (i + 1 == t.count || len(plan.mat[i]) != len(plan.mat[i + 1])) end = plan.first[i + 1];
+    for (int whole = 0; whole < (end < tiles ? 2 : 1); ++whole) {
+      const int tail = (whole ? tiles : end) - full;
+      for (int s = 2; tail > 0 && s <= 16 && tail * s <= 4 * kCUs; ++s)
+        offer(true, full, tail, s,
+              kTileUs + items(big_us, full, tail, s) + kSplitUs + 0.05 * tail * s);
+    }
   }
+  auto small_us = [](int nk) {
+    return kSmallTileUs + kSmallStepUs<PLANES> * ((nk + kSWaves - 1) / kSWaves);
+  };
   tiles = count(kST);
   for (int s = 1; s <= 16 && (s == 1 || (gram && tiles <= 2 * kCUs / s)); ++s) {
     const int full = s == 1 ? tiles : 0;
-    const Rounds r = rounds(small_len, full, s);
-    offer(false, full, s, tiles - full,
-          kSmallUs + kSmallTileUs * r.count + kSmallStepUs<PLANES> * r.steps +
+    offer(false, full, tiles - full, s,
+          kSmallUs + items(small_us, full, tiles - full, s) +
               (s > 1 ? kSmallSplitUs + 0.01 * tiles * s : 0.0));
   }
   return c;
@@ -756,16 +803,16 @@ NsLaunch choose(Op op, bool gram, const NsTable& t) {
 template <Op OP, int PLANES>
 void launch(const NsTable& t, const NsLaunch& c, const Product& p, const NsFinish& fin, int cur,
             float* part, hipStream_t s) {
-  const int items = c.plan.n_full + c.tail * c.plan.splits;
+  const int tail = c.plan.tail, items = c.plan.first[t.count] + tail * (c.plan.splits - 1);
   if (!c.big) {
     ns_gemm_small<OP, PLANES><<<items, kSThreads, kSLds, s>>>(t, c.plan, p, fin, cur, part);
     if constexpr (OP == Op::Sym)
-      if (c.tail)
-        ns_reduce_kernel<OP, PLANES, kST><<<c.tail, 256, 0, s>>>(t, c.plan, p, cur, part);
+      if (tail)
+        ns_reduce_kernel<OP, PLANES, kST><<<tail, 256, 0, s>>>(t, c.plan, p, cur, part);
   } else if constexpr (OP != Op::Last) {
     ns_gemm_big<OP, PLANES><<<items, kBThreads, kBLds, s>>>(t, c.plan, p, cur, part);
-    if (c.tail)
-      ns_reduce_kernel<OP, PLANES, kBT><<<c.tail * 16, 256, 0, s>>>(t, c.plan, p, cur, part);
+    if (tail)
+      ns_reduce_kernel<OP, PLANES, kBT><<<tail * 16, 256, 0, s>>>(t, c.plan, p, cur, part);
   }
 }
 
@@ -823,7 +870,7 @@ void ns_plan(const NsTable& t, int planes, NsProducts* p) {
   for (const NsLaunch* l : {&p->gram, &p->square, &p->apply})
     p->partial_floats =
         std::max(p->partial_floats,
-                 (size_t)l->tail * l->plan.splits * (l->big ? kBT * kBT : kST * kST));
+                 (size_t)l->plan.tail * l->plan.splits * (l->big ? kBT * kBT : kST * kST));
 }
 
 void launch_ns_products(const NsTable& t, const NsFinish& fin, int planes, int steps,
