@@ -172,16 +172,31 @@ struct NsLaunch {
 struct NsProducts {
   NsLaunch gram, square, apply;  // (square: every product of two symmetric matrices)
   bool paired;                   // two steps to one gram and apply
-  size_t partial_floats;         // room for the partial tiles of one launch
 };
 inline int ns_symmetric(const NsProducts& p) { return p.paired ? 3 : 2; }  // s in use
 // Times that X is replaced: it is in x[ns_groups & 1] at the end.
 inline int ns_groups(const NsProducts& p, int steps) { return p.paired ? (steps + 1) / 2 : steps; }
-// From the matrices' sizes alone (host only).
-void ns_plan(const NsTable& t, int planes, NsProducts* p);
-// partial: a double per tile; norm: one per matrix; part: p.partial_floats floats.
+// The chains of a call: matrices 0 .. end[0] - 1 of its table, then those up to end[1].
+struct NsChains {
+  int count;  // 1 or 2
+  int end[2];
+  NsProducts p[2];
+  size_t partial_floats;  // room for the partial tiles of one launch
+};
+// The matrices lo .. hi - 1 of a table as one of their own.
+inline NsTable ns_slice(const NsTable& t, int lo, int hi) {
+  NsTable u{};
+  for (u.count = 0; lo + u.count < hi; ++u.count) {
+    u.mat[u.count] = t.mat[lo + u.count];
+    u.tile0[u.count + 1] = t.tile0[lo + u.count + 1] - t.tile0[lo];
+  }
+  return u;
+}
+// From the matrices' sizes alone (host only); puts the table into the chains' order.
+void ns_plan(NsTable& t, int planes, NsChains* c);
+// partial: a double per tile; norm: one per matrix; part: c.partial_floats floats.
 void launch_newton_schulz(const NsTable& t, const NsScalars& sc, NsMode mode, Dt copy_dt,
-                          const NsProducts& p, double* partial, double* norm, float* part,
+                          const NsChains& c, double* partial, double* norm, float* part,
                           hipStream_t s);
 
 // ------------------------------------------------------ reduce-scatter sum

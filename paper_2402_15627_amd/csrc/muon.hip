@@ -11,7 +11,7 @@
 //   1. update: M in place, the sum of U^2 per 64 x 64 tile, in fp64
 //   2. norm:   1 / (||U||_F + eps) of each matrix
 //   3. init:   X's fp16 planes, padded to multiples of 64 with zeros
-//   4. the products (ns_gemm.hip), each one launch for all matrices
+//   4. the products (ns_gemm.hip), each one launch for all matrices of a chain
 //   5. finish: w and its copy, or the orthogonalised matrix itself; part of the last
 //      product where that runs in small tiles
 //
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(kThreads) void ns_finish_kernel(NsTable t, NsFinish
 }
 
 template <NsMode MODE, int PLANES>
-void run(const NsTable& t, const NsScalars& sc, Dt copy_dt, const NsProducts& p, double* partial,
+void run(const NsTable& t, const NsScalars& sc, Dt copy_dt, const NsChains& c, double* partial,
          double* norm, float* part, hipStream_t s) {
   const int tiles = t.tile0[t.count];
   ns_update_kernel<MODE><<<tiles, kThreads, 0, s>>>(t, sc, partial);
@@ -232,23 +232,31 @@ void run(const NsTable& t, const NsScalars& sc, Dt copy_dt, const NsProducts& p,
   ns_init_kernel<MODE, PLANES><<<tiles, kThreads, 0, s>>>(t, sc, norm);
   const bool bf16_out = MODE == NsMode::Bf16 || (MODE == NsMode::Muon && copy_dt == Dt::BF16);
   const NsFinish fin{MODE, bf16_out, sc.lr};
-  launch_ns_products(t, fin, PLANES, sc.steps, p, part, s);
-  if (p.apply.big)
-    ns_finish_kernel<PLANES><<<tiles, kThreads, 0, s>>>(t, fin, ns_groups(p, sc.steps) & 1);
+  for (int k = 0; k < c.count; ++k) {
+    const NsTable u = ns_slice(t, k ? c.end[k - 1] : 0, c.end[k]);
+    const NsProducts& p = c.p[k];
+    launch_ns_products(u, fin, PLANES, sc.steps, p, part, s);
+    if (p.apply.big)
+      ns_finish_kernel<PLANES><<<u.tile0[u.count], kThreads, 0, s>>>(u, fin,
+                                                                     ns_groups(p, sc.steps) & 1);
+  }
 }
 
 }  // namespace
 
 void launch_newton_schulz(const NsTable& t, const NsScalars& sc, NsMode mode, Dt copy_dt,
-                          const NsProducts& p, double* partial, double* norm, float* part,
+                          const NsChains& c, double* partial, double* norm, float* part,
                           hipStream_t s) {
   switch (mode) {
     case NsMode::Muon:
-      if (sc.planes == 2) run<NsMode::Muon, 2>(t, sc, copy_dt, p, partial, norm, part, s);
-      else run<NsMode::Muon, 1>(t, sc, copy_dt, p, partial, norm, part, s);
+      if (sc.planes == 2) run<NsMode::Muon, 2>(t, sc, copy_dt, c, partial, norm, part, s);
+      else run<NsMode::Muon, 1>(t, sc, copy_dt, c, partial, norm, part, s);
       break;
-    case NsMode::Bf16: run<NsMode::Bf16, 1>(t, sc, copy_dt, p, partial, norm, part, s); break;
-    case NsMode::F32: run<NsMode::F32, 2>(t, sc, copy_dt, p, partial, norm, part, s); break;
+    case NsMode::Bf16:
+      if (sc.planes == 2) run<NsMode::Bf16, 2>(t, sc, copy_dt, c, partial, norm, part, s);
+      else run<NsMode::Bf16, 1>(t, sc, copy_dt, c, partial, norm, part, s);
+      break;
+    case NsMode::F32: run<NsMode::F32, 2>(t, sc, copy_dt, c, partial, norm, part, s); break;
   }
 }
 

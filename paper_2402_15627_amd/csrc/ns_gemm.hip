@@ -1,4 +1,4 @@
-// The products of the Newton-Schulz steps, all matrices of a call in one launch each.
+// The products of the Newton-Schulz steps, all matrices of a chain in one launch each.
 // A step is
 //
 //   A = X X^T,  B = a I + b A + c A A,  X' = B X
@@ -852,25 +852,58 @@ void iterate(const NsTable& t, const NsFinish& fin, int steps, const NsProducts&
 
 }  // namespace
 
-void ns_plan(const NsTable& t, int planes, NsProducts* p) {
-  auto of = [&](Op op, bool gram) {
-    return planes == 2 ? choose<2>(op, gram, t) : choose<1>(op, gram, t);
+void ns_plan(NsTable& t, int planes, NsChains* c) {
+  auto plan = [&](const NsTable& u, bool paired) {
+    auto of = [&](Op op, bool gram) {
+      return planes == 2 ? choose<2>(op, gram, u) : choose<1>(op, gram, u);
+    };
+    return NsProducts{of(Op::Sym, true), of(Op::Square, false), of(Op::Apply, false), paired};
   };
-  p->gram = of(Op::Sym, true);
-  p->square = of(Op::Square, false);
-  p->apply = of(Op::Apply, false);
-  // A pair takes three symmetric products more, and a gram and an apply less: one launch
-  // more, which costs about kLaunchUs less here than estimated by itself.  Five steps, in
-  // pairs and step by step: fp32 64 x 1024 99 and 106 us, 256 x 1024 145 and 144, 2048 x
-  // 4096 1037 and 1085, 4096 x 5120 4556 and 4416; bf16 64 x 4096 98 and 111, 1024 x 4096
-  // 261 and 291 (chosen); 1024 x 2048, chosen too, 206 and 201.
+  // Estimate of two steps; a launch in a chain costs about kLaunchUs less than by itself.
   constexpr double kLaunchUs = 5.0;
-  p->paired = 3 * p->square.us - kLaunchUs < 0.95 * (p->gram.us + p->apply.us);
-  p->partial_floats = 0;
-  for (const NsLaunch* l : {&p->gram, &p->square, &p->apply})
-    p->partial_floats =
-        std::max(p->partial_floats,
-                 (size_t)l->plan.tail * l->plan.splits * (l->big ? kBT * kBT : kST * kST));
+  auto us = [](const NsProducts& p) {
+    return p.paired ? p.gram.us + 5 * p.square.us + p.apply.us - 7 * kLaunchUs
+                    : 2 * (p.gram.us + p.square.us + p.apply.us) - 6 * kLaunchUs;
+  };
+  // Pairs of steps only where X is at least twice as wide as tall: in a square one the
+  // roundings of A' show (300 x 300, fp32 2.7e-6 off in pairs, 1.8e-6 step by step; one
+  // plane 1.8e-3 and 1.3e-3; 128 x 256 1.3e-6 and 1.4e-6; 1.1e-3 either way).  And not
+  // under 16 rows, whose few elements' roundings do not average (fp32 1 x 777, off by
+  // 4.4e-7 in the median and 6.7e-7 at most step by step, 6.9e-7 and 1.3e-6 in pairs;
+  // 16 x 777 5.7e-7 and 7.7e-7, where fp32 products are off by 1.3e-6).
+  auto wide = [](const NsMat& x) {
+    const int m = std::min(x.rows, x.cols), n = std::max(x.rows, x.cols);
+    return m >= 16 && n >= 2 * m;
+  };
+  NsTable order{};  // the wide ones first
+  for (int k = 0; k < 2; ++k)
+    for (int i = 0; i < t.count; ++i)
+      if (wide(t.mat[i]) == (k == 0)) order.mat[order.count++] = t.mat[i];
+  for (int i = 0; i < t.count; ++i) {
+    auto tiles = [](int v) { return (v + kNsPad - 1) / kNsPad; };
+    order.tile0[i + 1] = order.tile0[i] + tiles(order.mat[i].rows) * tiles(order.mat[i].cols);
+  }
+  int n = 0;
+  while (n < t.count && wide(order.mat[n])) ++n;
+  *c = NsChains{1, {t.count, t.count}, {plan(t, false)}, 0};
+  // Five steps, in pairs and step by step: fp32 64 x 1024 99 and 106 us, 256 x 1024 145
+  // and 144, 2048 x 4096 1037 and 1085, 4096 x 8192 5670 and 6260; bf16 64 x 4096 98 and
+  // 111, 1024 x 4096 261 and 291 (chosen); 1024 x 2048, chosen too, 206 and 201.
+  if (n == t.count) {
+    NsProducts p = c->p[0];
+    p.paired = true;
+    if (us(p) < us(c->p[0]) - 0.05 * (p.gram.us + p.apply.us)) c->p[0] = p;
+  } else if (n > 0 && us(c->p[0]) > 3 * 7 * kLaunchUs) {
+    // two chains, where the seven launches more are repaid (pairs save a third at most)
+    NsChains d{2, {n, t.count}, {plan(ns_slice(order, 0, n), true),
+                                 plan(ns_slice(order, n, t.count), false)}, 0};
+    if (us(d.p[0]) + us(d.p[1]) < 0.95 * us(c->p[0])) *c = d, t = order;
+  }
+  for (int k = 0; k < c->count; ++k)
+    for (const NsLaunch* l : {&c->p[k].gram, &c->p[k].square, &c->p[k].apply})
+      c->partial_floats =
+          std::max(c->partial_floats, (size_t)l->plan.tail * l->plan.splits *
+                                          (l->big ? kBT * kBT : kST * kST));
 }
 
 void launch_ns_products(const NsTable& t, const NsFinish& fin, int planes, int steps,

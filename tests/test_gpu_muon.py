@@ -228,6 +228,32 @@ def test_muon_step_matches_oracle(products, nesterov, copy_dtype, gs):
         assert torch.equal(s["g"][0], b["g"])
 
 
+@pytest.mark.parametrize("steps", [4, 5])
+def test_muon_wide_and_square_matrices_in_one_call(steps):
+    """The wide ones' steps run in pairs, the square ones' by themselves."""
+    import torch
+    from paper_2402_15627_amd import pblock as pb
+    _say(f"[gpu] muon wide and square, steps={steps}")
+    st = make([(640, 640, 648, 0), (1200, 5000, 5000, 0), (0, 7, 7, 0), (700, 650, 650, 1), (3000, 1200, 1200, 0)], 21)
+    init = [{n: f64(s[n][1]) for n in ("w", "g", "m")} for s in st]
+    cfg = pb.muon_config(0.02, 0.9, steps=steps)
+    part = [pb.muon_tensor(s["w"][1], s["g"][1], s["m"][1], s["copy"][1], s["wd"], s["scale"]) for s in st]
+    ws = torch.empty(pb.pblock_muon_workspace_bytes(cfg, part), dtype=torch.uint8, device="cuda").fill_(255)
+    pb.pblock_muon_step(cfg, part, pb.PB_BF16, ws)
+    lr, mu = np.float64(np.float32(0.02)), np.float64(np.float32(0.9))
+    for s, x in zip(st, init):
+        if x["w"].size == 0:
+            continue
+        wd, scale = float(np.float32(s["wd"])), float(np.float32(s["scale"]))
+        w, m, o = oo.muon_step(x["w"], x["g"], x["m"], lr, mu, True, wd, scale, 1.0, steps)
+        e = np.linalg.norm(f64(s["w"][1]) - w)
+        tol = (allowed(x["g"] + mu * m, o, "f32", steps) + 32 * 2.0 ** -22) * lr * scale * np.linalg.norm(o)
+        tol += 2.0 ** -22 * np.linalg.norm(x["w"])
+        _say(f"      {x['w'].shape}: off {e:.2e} of {tol:.2e}")
+        assert e <= tol
+        assert torch.equal(s["copy"][1], s["w"][1].to(s["copy"][1].dtype))
+
+
 def test_muon_three_steps_and_split_calls():
     """Matrices are independent: one call over all gives the bits of a call each; three
     steps follow the oracle's."""
