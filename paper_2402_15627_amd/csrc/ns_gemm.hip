@@ -383,15 +383,18 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
       if (tt + 2 < nt) issue_half(tt + 2, 0);
     }
     if constexpr (p == 0)
-      if (tt + 1 >= 2 && tt + 1 < nt) issue_half(tt + 1, 1);
+      if (tt + 1 < nt) issue_half(tt + 1, 1);
     if constexpr (p + kLook < kPh) read_frags(tt, p + kLook);
     else read_frags(tt + 1, p + kLook - kPh);
     mma(P);
     __builtin_amdgcn_sched_barrier(0);
   };
   if (nt > 0) issue_half(0, 0), issue_half(0, 1);
-  if (nt > 1) issue_half(1, 0), issue_half(1, 1);
-  if (nt > 1) wait_dma<kDmaPerTile>();  // tile 0 landed; tile 1 may be in flight
+  // (its other half in phase 0, as in every K-tile: with a first K-tile of its own Square
+  // in one plane spilled a fragment, and every K-tile waited for the reload and with it for
+  // the DMA: 5120 x 5120 twice 293 us, 255 so)
+  if (nt > 1) issue_half(1, 0);
+  if (nt > 1) wait_dma<kDmaPerTile / 2>();  // tile 0 landed; tile 1 may be in flight
   else wait_dma<0>();
   block_barrier();
 #pragma unroll
@@ -421,7 +424,11 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
   // row), so that rows go out in whole lines.  acc[i][j][e] is row wm + 16 i + (lane &
   // 15), column wn + 16 j + 4 (lane >> 4) + e.
   unsigned char* buf = smem + wave * kEpiLds;
-  const int c = lane & 31, hi = lane >> 5;
+  // (opaque, or what is formed from it here would be formed before the main loop and cost
+  // it registers)
+  int el = lane;
+  asm volatile("" : "+v"(el));
+  const int c = el & 31, hi = el >> 5;
   const int n = n0 + wn + 4 * c;
   float* pt = it.slice < 0 ? nullptr
                            : part + ((size_t)(it.tile - plan.n_full) * plan.splits + it.slice) *
@@ -432,7 +439,7 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
     for (int ii = 0; ii < 2; ++ii)
 #pragma unroll
       for (int j = 0; j < kTN; ++j) {
-        const int rr = 16 * ii + (lane & 15), cw = 4 * j + (lane >> 4);
+        const int rr = 16 * ii + (el & 15), cw = 4 * j + (el >> 4);
         *reinterpret_cast<f32x4*>(buf + rr * (kWTN * 4) + ((cw ^ rr) & 31) * 16) = acc[2 * i + ii][j];
       }
 #pragma unroll
@@ -456,10 +463,10 @@ __global__ __launch_bounds__(kBThreads, 1) void ns_gemm_big(NsTable t, NsPlan pl
     if constexpr (symmetric(OP)) {
       // the mirror image: 4 lanes hold the 32 rows of a column, 8 each
       if (pt || tm == tn) continue;
-      const int r8 = 8 * (lane & 3), mm = m0 + wm + 32 * i + r8;
+      const int r8 = 8 * (el & 3), mm = m0 + wm + 32 * i + r8;
 #pragma unroll
       for (int k = 0; k < kWTN / 16; ++k) {
-        const int cc = 16 * k + (lane >> 2), nn = n0 + wn + cc;
+        const int cc = 16 * k + (el >> 2), nn = n0 + wn + cc;
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e)
