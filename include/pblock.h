@@ -727,8 +727,8 @@ pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s,
  * remainder, three matrix products for one): the update is as exact as fp32
  * products make it.  PB_BF16 rounds the factors to fp16 (11 bits), one product, a
  * third of the time: the update is off by 1e-3 to 8e-3 of its norm, the more the
- * fewer directions hold most of it (fp32 sums, norms, M and w either way); a call of
- * matrices with fewer than 64 rows or columns each runs as with PB_F32.
+ * fewer directions hold most of it (fp32 sums, norms, M and w either way); matrices
+ * with fewer than 64 rows or columns have PB_F32's products.
  *
  * pblock_orthogonalize: X alone, from in to out (may be the same memory with the
  * same ld, else apart), both in dtype; PB_F32 products for PB_F32, PB_BF16 products

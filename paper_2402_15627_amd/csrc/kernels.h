@@ -150,7 +150,6 @@ struct NsTable {
 struct NsScalars {
   float lr, momentum, grad_scale, eps;
   int nesterov;
-  int planes;  // 1: one fp16 product; 2: a value and its remainder, three products
   int steps;
 };
 // Where the updates come from and go to.
@@ -176,12 +175,14 @@ struct NsProducts {
 inline int ns_symmetric(const NsProducts& p) { return p.paired ? 3 : 2; }  // s in use
 // Times that X is replaced: it is in x[ns_groups & 1] at the end.
 inline int ns_groups(const NsProducts& p, int steps) { return p.paired ? (steps + 1) / 2 : steps; }
-// The chains of a call: matrices 0 .. end[0] - 1 of its table, then those up to end[1].
+// The chains of a call: chain k has the matrices end[k - 1] .. end[k] - 1 of its table.
+constexpr int kNsMaxChains = 4;
 struct NsChains {
-  int count;  // 1 or 2
-  int end[2];
-  NsProducts p[2];
-  size_t partial_floats;  // room for the partial tiles of one launch
+  int count;
+  int end[kNsMaxChains];
+  int planes[kNsMaxChains];  // 1: an fp16 product; 2: values and remainders, three products
+  NsProducts p[kNsMaxChains];
+  size_t partial_floats;     // room for the partial tiles of one launch
 };
 // The matrices lo .. hi - 1 of a table as one of their own.
 inline NsTable ns_slice(const NsTable& t, int lo, int hi) {
@@ -193,7 +194,7 @@ inline NsTable ns_slice(const NsTable& t, int lo, int hi) {
   return u;
 }
 // From the matrices' sizes alone (host only); puts the table into the chains' order.
-void ns_plan(NsTable& t, int planes, NsChains* c);
+void ns_plan(NsTable& t, bool f32_products, NsChains* c);
 // partial: a double per tile; norm: one per matrix; part: c.partial_floats floats.
 void launch_newton_schulz(const NsTable& t, const NsScalars& sc, NsMode mode, Dt copy_dt,
                           const NsChains& c, double* partial, double* norm, float* part,

@@ -16,7 +16,10 @@
 //      product where that runs in small tiles
 //
 // 1, 3 and 5 are HBM-bound: a 64 x 64 tile per workgroup, 256 contiguous bytes of
-// a row per 16 lanes; a tall matrix's tile is transposed through LDS.
+// a row per 16 lanes; a tall matrix's tile is transposed through LDS (226 M elements of
+// the 175B share: 0.54, 0.53 and 0.61 ms, 5.0, 5.1 and 5.2 TB/s).  A step of those takes
+// 33.7 ms, 32 of them products at the matrix cores' power limit; one of six matrices of
+// 256 x 256 and 1024 x 256 0.16 ms, 18 launches of about 8 us each in a row.
 #include "common.h"
 #include "kernels.h"
 #include "ns_gemm.h"
@@ -223,22 +226,29 @@ __global__ __launch_bounds__(kThreads) void ns_finish_kernel(NsTable t, NsFinish
   }
 }
 
+// A chain: X's planes, products, the tensors.
 template <NsMode MODE, int PLANES>
+void run_chain(const NsTable& t, const NsScalars& sc, const NsFinish& fin, const NsProducts& p,
+               const double* norm, float* part, hipStream_t s) {
+  const int tiles = t.tile0[t.count];
+  ns_init_kernel<MODE, PLANES><<<tiles, kThreads, 0, s>>>(t, sc, norm);
+  launch_ns_products(t, fin, PLANES, sc.steps, p, part, s);
+  if (p.apply.big)
+    ns_finish_kernel<PLANES><<<tiles, kThreads, 0, s>>>(t, fin, ns_groups(p, sc.steps) & 1);
+}
+
+template <NsMode MODE>
 void run(const NsTable& t, const NsScalars& sc, Dt copy_dt, const NsChains& c, double* partial,
          double* norm, float* part, hipStream_t s) {
-  const int tiles = t.tile0[t.count];
-  ns_update_kernel<MODE><<<tiles, kThreads, 0, s>>>(t, sc, partial);
+  ns_update_kernel<MODE><<<t.tile0[t.count], kThreads, 0, s>>>(t, sc, partial);
   ns_norm_kernel<<<t.count, kNormThreads, 0, s>>>(t, sc.eps, partial, norm);
-  ns_init_kernel<MODE, PLANES><<<tiles, kThreads, 0, s>>>(t, sc, norm);
   const bool bf16_out = MODE == NsMode::Bf16 || (MODE == NsMode::Muon && copy_dt == Dt::BF16);
   const NsFinish fin{MODE, bf16_out, sc.lr};
-  for (int k = 0; k < c.count; ++k) {
-    const NsTable u = ns_slice(t, k ? c.end[k - 1] : 0, c.end[k]);
-    const NsProducts& p = c.p[k];
-    launch_ns_products(u, fin, PLANES, sc.steps, p, part, s);
-    if (p.apply.big)
-      ns_finish_kernel<PLANES><<<u.tile0[u.count], kThreads, 0, s>>>(u, fin,
-                                                                     ns_groups(p, sc.steps) & 1);
+  for (int k = 0, lo = 0; k < c.count; lo = c.end[k++]) {
+    const NsTable u = ns_slice(t, lo, c.end[k]);
+    if (c.planes[k] == 2) run_chain<MODE, 2>(u, sc, fin, c.p[k], norm + lo, part, s);
+    else if constexpr (MODE != NsMode::F32)
+      run_chain<MODE, 1>(u, sc, fin, c.p[k], norm + lo, part, s);
   }
 }
 
@@ -248,15 +258,9 @@ void launch_newton_schulz(const NsTable& t, const NsScalars& sc, NsMode mode, Dt
                           const NsChains& c, double* partial, double* norm, float* part,
                           hipStream_t s) {
   switch (mode) {
-    case NsMode::Muon:
-      if (sc.planes == 2) run<NsMode::Muon, 2>(t, sc, copy_dt, c, partial, norm, part, s);
-      else run<NsMode::Muon, 1>(t, sc, copy_dt, c, partial, norm, part, s);
-      break;
-    case NsMode::Bf16:
-      if (sc.planes == 2) run<NsMode::Bf16, 2>(t, sc, copy_dt, c, partial, norm, part, s);
-      else run<NsMode::Bf16, 1>(t, sc, copy_dt, c, partial, norm, part, s);
-      break;
-    case NsMode::F32: run<NsMode::F32, 2>(t, sc, copy_dt, c, partial, norm, part, s); break;
+    case NsMode::Muon: run<NsMode::Muon>(t, sc, copy_dt, c, partial, norm, part, s); break;
+    case NsMode::Bf16: run<NsMode::Bf16>(t, sc, copy_dt, c, partial, norm, part, s); break;
+    case NsMode::F32: run<NsMode::F32>(t, sc, copy_dt, c, partial, norm, part, s); break;
   }
 }
 

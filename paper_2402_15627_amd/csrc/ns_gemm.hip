@@ -33,6 +33,11 @@
 // rounding moves X' by less (one plane, one row of 777: 3.4e-3 off, 8e-4 so; 512 x 512
 // 1.34e-3, 1.24e-3), and apply reads no X beside its operand.
 //
+// MFMA-bound: the 175B share's products in two planes (44e12 operations a step of five)
+// run at 1.38 PFLOP/s, matrix cores busy 72 to 84% at the 1.7 to 1.8 GHz that their power
+// allows; in one plane (5120 x 5120 twice, 20480 x 5120) at 1.1, busy 57 to 71%, the
+// operands' way through LDS being longer than the products.
+//
 // Two kernels:
 //   - 256 x 256 tiles, eight waves, as the projection GEMMs' LDS-DMA kernel has them
 //     (gemm.hip: fragments read two phases ahead, one barrier a K-tile);
@@ -859,18 +864,42 @@ void iterate(const NsTable& t, const NsFinish& fin, int steps, const NsProducts&
 
 }  // namespace
 
-void ns_plan(NsTable& t, int planes, NsChains* c) {
+namespace {
+
+// Estimate of two steps; a launch in a chain costs about kLaunchUs less than by itself.
+constexpr double kLaunchUs = 5.0;
+double two_steps(const NsProducts& p) {
+  return p.paired ? p.gram.us + 5 * p.square.us + p.apply.us - 7 * kLaunchUs
+                  : 2 * (p.gram.us + p.square.us + p.apply.us) - 6 * kLaunchUs;
+}
+double two_steps(const NsChains& c) {
+  double us = 0.0;
+  for (int k = 0; k < c.count; ++k) us += two_steps(c.p[k]);
+  return us;
+}
+
+// The table with the matrices for which f holds first; n: their number.
+template <typename F>
+NsTable ordered(const NsTable& t, F f, int& n) {
+  NsTable u{};
+  for (int k = 0; k < 2; ++k) {
+    for (int i = 0; i < t.count; ++i)
+      if (f(t.mat[i]) == (k == 0)) u.mat[u.count++] = t.mat[i];
+    if (k == 0) n = u.count;
+  }
+  auto tiles = [](int v) { return (v + kNsPad - 1) / kNsPad; };
+  for (int i = 0; i < u.count; ++i)
+    u.tile0[i + 1] = u.tile0[i] + tiles(u.mat[i].rows) * tiles(u.mat[i].cols);
+  return u;
+}
+
+// One chain, or one of the wide matrices in pairs of steps and one of the others.
+NsChains pair_chains(NsTable& t, int planes) {
   auto plan = [&](const NsTable& u, bool paired) {
     auto of = [&](Op op, bool gram) {
       return planes == 2 ? choose<2>(op, gram, u) : choose<1>(op, gram, u);
     };
     return NsProducts{of(Op::Sym, true), of(Op::Square, false), of(Op::Apply, false), paired};
-  };
-  // Estimate of two steps; a launch in a chain costs about kLaunchUs less than by itself.
-  constexpr double kLaunchUs = 5.0;
-  auto us = [](const NsProducts& p) {
-    return p.paired ? p.gram.us + 5 * p.square.us + p.apply.us - 7 * kLaunchUs
-                    : 2 * (p.gram.us + p.square.us + p.apply.us) - 6 * kLaunchUs;
   };
   // Pairs of steps only where X is at least twice as wide as tall: in a square one the
   // roundings of A' show (300 x 300, fp32 2.7e-6 off in pairs, 1.8e-6 step by step; one
@@ -878,34 +907,59 @@ void ns_plan(NsTable& t, int planes, NsChains* c) {
   // under 16 rows, whose few elements' roundings do not average (fp32 1 x 777, off by
   // 4.4e-7 in the median and 6.7e-7 at most step by step, 6.9e-7 and 1.3e-6 in pairs;
   // 16 x 777 5.7e-7 and 7.7e-7, where fp32 products are off by 1.3e-6).
-  auto wide = [](const NsMat& x) {
-    const int m = std::min(x.rows, x.cols), n = std::max(x.rows, x.cols);
-    return m >= 16 && n >= 2 * m;
-  };
-  NsTable order{};  // the wide ones first
-  for (int k = 0; k < 2; ++k)
-    for (int i = 0; i < t.count; ++i)
-      if (wide(t.mat[i]) == (k == 0)) order.mat[order.count++] = t.mat[i];
-  for (int i = 0; i < t.count; ++i) {
-    auto tiles = [](int v) { return (v + kNsPad - 1) / kNsPad; };
-    order.tile0[i + 1] = order.tile0[i] + tiles(order.mat[i].rows) * tiles(order.mat[i].cols);
-  }
   int n = 0;
-  while (n < t.count && wide(order.mat[n])) ++n;
-  *c = NsChains{1, {t.count, t.count}, {plan(t, false)}, 0};
+  const NsTable order = ordered(t, [](const NsMat& x) {
+    const int m = std::min(x.rows, x.cols);
+    return m >= 16 && std::max(x.rows, x.cols) >= 2 * m;
+  }, n);
+  NsChains c{1, {t.count}, {planes}, {plan(t, false)}, 0};
   // Five steps, in pairs and step by step: fp32 64 x 1024 99 and 106 us, 256 x 1024 145
   // and 144, 2048 x 4096 1037 and 1085, 4096 x 8192 5670 and 6260; bf16 64 x 4096 98 and
   // 111, 1024 x 4096 261 and 291 (chosen); 1024 x 2048, chosen too, 206 and 201.
   if (n == t.count) {
-    NsProducts p = c->p[0];
+    NsProducts p = c.p[0];
     p.paired = true;
-    if (us(p) < us(c->p[0]) - 0.05 * (p.gram.us + p.apply.us)) c->p[0] = p;
-  } else if (n > 0 && us(c->p[0]) > 3 * 7 * kLaunchUs) {
+    if (two_steps(p) < two_steps(c) - 0.05 * (p.gram.us + p.apply.us)) c.p[0] = p;
+  } else if (n > 0 && two_steps(c) > 3 * 7 * kLaunchUs) {
     // two chains, where the seven launches more are repaid (pairs save a third at most)
-    NsChains d{2, {n, t.count}, {plan(ns_slice(order, 0, n), true),
-                                 plan(ns_slice(order, n, t.count), false)}, 0};
-    if (us(d.p[0]) + us(d.p[1]) < 0.95 * us(c->p[0])) *c = d, t = order;
+    const NsChains d{2, {n, t.count}, {planes, planes},
+                     {plan(ns_slice(order, 0, n), true), plan(ns_slice(order, n, t.count), false)}, 0};
+    if (two_steps(d) < 0.95 * two_steps(c)) {
+      t = order;
+      return d;
+    }
   }
+  return c;
+}
+
+}  // namespace
+
+// One plane serves bf16 from 64 rows and columns on.  Under that the roundings of few
+// elements show (16 x 16 off by up to 2.6e-3, 64 x 64 by 1.5e-3) and a step is latency:
+// five steps of 64 x 256 take 70 us in one plane, of 60 x 256 82 in two.  Beside larger
+// matrices the small ones have a chain of their own, or all of a call take two planes,
+// whichever is estimated to end sooner.
+void ns_plan(NsTable& t, bool f32_products, NsChains* c) {
+  int n = 0;
+  NsTable order = ordered(t, [](const NsMat& x) { return std::min(x.rows, x.cols) < 64; }, n);
+  if (f32_products || n == 0 || n == t.count) {
+    *c = pair_chains(t, f32_products || n ? 2 : 1);
+  } else {
+    NsTable small = ns_slice(order, 0, n), rest = ns_slice(order, n, t.count);
+    const NsChains a = pair_chains(small, 2), b = pair_chains(rest, 1);
+    *c = pair_chains(t, 2);
+    if (two_steps(a) + two_steps(b) < two_steps(*c)) {
+      *c = a;
+      for (int k = 0; k < b.count; ++k) {
+        c->end[c->count] = n + b.end[k];
+        c->planes[c->count] = b.planes[k];
+        c->p[c->count++] = b.p[k];
+      }
+      for (int i = 0; i < t.count; ++i) order.mat[i] = i < n ? small.mat[i] : rest.mat[i - n];
+      t = ordered(order, [](const NsMat&) { return true; }, n);
+    }
+  }
+  c->partial_floats = 0;
   for (int k = 0; k < c->count; ++k)
     for (const NsLaunch* l : {&c->p[k].gram, &c->p[k].square, &c->p[k].apply})
       c->partial_floats =

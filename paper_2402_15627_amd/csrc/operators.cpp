@@ -260,20 +260,22 @@ bool ns_add(pb::NsTable& t, int rows, int cols) {
 
 // Plans the products, and places the planes of every matrix from base on (nullptr: sizes
 // alone).
-NsLayout ns_layout(pb::NsTable& t, int planes, char* base, pb::NsChains* c) {
+NsLayout ns_layout(pb::NsTable& t, bool f32_products, char* base, pb::NsChains* c) {
   NsLayout L{};
   if (t.count == 0) return L;
-  pb::ns_plan(t, planes, c);
+  pb::ns_plan(t, f32_products, c);
   L.norm = align256((size_t)t.tile0[t.count] * sizeof(double));
   size_t o = L.norm + align256((size_t)t.count * sizeof(double));
-  for (int i = 0; i < t.count; ++i) {
+  for (int i = 0, chain = 0; i < t.count; ++i) {
     pb::NsMat& x = t.mat[i];
+    while (i >= c->end[chain]) ++chain;
+    const int planes = c->planes[chain];
     const size_t big = align256((size_t)planes * x.m * x.ldn * 2);
     const size_t small = align256((size_t)planes * x.m * x.ldm * 2);
     x.x[0] = (_Float16*)(base + o);
     x.x[1] = (_Float16*)(base + o + big);
     o += 2 * big;
-    const int n = pb::ns_symmetric(c->p[i < c->end[0] ? 0 : 1]);
+    const int n = pb::ns_symmetric(c->p[chain]);
     for (int k = 0; k < n; ++k, o += small) x.s[k] = (_Float16*)(base + o);
   }
   L.part = o;
@@ -308,11 +310,11 @@ pb_status check_steps(int steps, float eps) {
   return PB_OK;
 }
 
-pb_status ns_launch(pb::NsTable& t, const pb::NsScalars& sc, pb::NsMode mode, pb::Dt copy_dt,
-                    void* ws, size_t ws_bytes, hipStream_t stream) {
+pb_status ns_launch(pb::NsTable& t, const pb::NsScalars& sc, pb::NsMode mode,
+                    bool f32_products, pb::Dt copy_dt, void* ws, size_t ws_bytes, hipStream_t stream) {
   if (t.count == 0) return nothing_to_do();
   pb::NsChains c;
-  const NsLayout L = ns_layout(t, sc.planes, (char*)ws, &c);
+  const NsLayout L = ns_layout(t, f32_products, (char*)ws, &c);
   PB_CHECK(check_ws(ws, ws_bytes, L.total));
   for (int i = 0; i < t.count; ++i) {
     const pb::NsMat& x = t.mat[i];
@@ -333,20 +335,10 @@ pb_status ns_launch(pb::NsTable& t, const pb::NsScalars& sc, pb::NsMode mode, pb
   return finish_launches();
 }
 
-// fp16 planes of a call's products.  Under 64 rows or columns a step is latency alone, and
-// few elements' roundings do not average: 16 x 16 in one plane is off by up to 2.6e-3, 64
-// x 64 by 1.5e-3, and five steps of 60 x 256 take 70 us in one plane, 82 in two.
-int planes_of(pb_dtype products, const pb::NsTable& t) {
-  bool small = true;
-  for (int i = 0; i < t.count; ++i)
-    small = small && std::min(t.mat[i].rows, t.mat[i].cols) < 64;
-  return products == PB_F32 || small ? 2 : 1;
-}
-
 // The bytes that the table's call needs.
 size_t ns_bytes(pb::NsTable& t, pb_dtype products) {
   pb::NsChains c;
-  return ns_layout(t, planes_of(products, t), nullptr, &c).total;
+  return ns_layout(t, products == PB_F32, nullptr, &c).total;
 }
 
 }  // namespace
@@ -527,9 +519,9 @@ pb_status pblock_muon_step(const pb_muon_config* cfg, int n_tensors, const pb_mu
   sc.grad_scale = cfg->grad_scale;
   sc.eps = cfg->eps;
   sc.nesterov = cfg->nesterov;
-  sc.planes = planes_of(cfg->products, t);
   sc.steps = cfg->steps;
-  return ns_launch(t, sc, pb::NsMode::Muon, dt_of(copy_dtype), ws, ws_bytes, stream);
+  return ns_launch(t, sc, pb::NsMode::Muon, cfg->products == PB_F32, dt_of(copy_dtype), ws,
+                   ws_bytes, stream);
 }
 
 size_t pblock_orthogonalize_workspace_bytes(int n_tensors, const pb_ortho_tensor* tensors,
@@ -579,9 +571,8 @@ pb_status pblock_orthogonalize(int n_tensors, const pb_ortho_tensor* tensors, pb
   pb::NsScalars sc{};
   sc.eps = eps;
   sc.steps = steps;
-  sc.planes = planes_of(dtype, t);
-  return ns_launch(t, sc, dtype == PB_F32 ? pb::NsMode::F32 : pb::NsMode::Bf16, dt_of(dtype), ws,
-                   ws_bytes, stream);
+  return ns_launch(t, sc, dtype == PB_F32 ? pb::NsMode::F32 : pb::NsMode::Bf16,
+                   dtype == PB_F32, dt_of(dtype), ws, ws_bytes, stream);
 }
 
 }  // extern "C"

@@ -12,7 +12,9 @@
 // reduced to [-1/2, 1/2] before it is rounded to fp32 (error of the rounded
 // angle 2^-25 turns; of the fp64 product 2^-53 of all turns, 1e-10 at a million).
 //
-// HBM-bound: every element is read and written once (2 e bytes) for 3 operations.
+// HBM-bound: every element is read and written once (2 e bytes) for 3 operations: 8192
+// tokens x 80 heads x 128 in bf16 61.5 us, 5.5 TB/s; below a megabyte or two a launch's
+// latency (four tokens x 80 heads 4 us, 8 a call back to back).
 // A workgroup takes some tokens by some heads of one tensor, up to kItems 16-byte
 // pieces a thread (a pair of pieces r/2 apart in the half layout).  It first
 // issues all its loads, then forms the cosines and sines of its tokens into LDS

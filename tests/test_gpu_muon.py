@@ -254,6 +254,31 @@ def test_muon_wide_and_square_matrices_in_one_call(steps):
         assert torch.equal(s["copy"][1], s["w"][1].to(s["copy"][1].dtype))
 
 
+@pytest.mark.parametrize("shapes", [[(20, 300), (130, 100), (48, 48)],
+                                    [(1500, 1400), (50, 3000), (16, 16), (1200, 5000), (7, 9)]], ids=len)
+def test_small_matrices_beside_larger_ones_keep_their_precision(shapes):
+    """Under 64 rows or columns products="bf16" has the products of "f32"."""
+    import torch
+    from paper_2402_15627_amd import pblock as pb
+    _say(f"[gpu] muon bf16 products, small beside larger: {shapes}")
+    st = make([(r, c, c, 0) for r, c in shapes], 33)
+    init = [{n: f64(s[n][1]) for n in ("w", "g", "m")} for s in st]
+    cfg = pb.muon_config(0.02, 0.9, products="bf16")
+    part = [pb.muon_tensor(s["w"][1], s["g"][1], s["m"][1], s["copy"][1], s["wd"], s["scale"]) for s in st]
+    ws = torch.empty(pb.pblock_muon_workspace_bytes(cfg, part), dtype=torch.uint8, device="cuda").fill_(255)
+    pb.pblock_muon_step(cfg, part, pb.PB_BF16, ws)
+    lr, mu = np.float64(np.float32(0.02)), np.float64(np.float32(0.9))
+    for s, x in zip(st, init):
+        wd, scale = float(np.float32(s["wd"])), float(np.float32(s["scale"]))
+        w, m, o = oo.muon_step(x["w"], x["g"], x["m"], lr, mu, True, wd, scale)
+        e = np.linalg.norm(f64(s["w"][1]) - w)
+        products = "f32" if min(w.shape) < 64 else "bf16"
+        tol = (allowed(x["g"] + mu * m, o, products) + 32 * 2.0 ** -22) * lr * scale * np.linalg.norm(o)
+        tol += 2.0 ** -22 * np.linalg.norm(x["w"])
+        _say(f"      {w.shape}: off {e:.2e} of {tol:.2e}")
+        assert e <= tol
+
+
 def test_muon_three_steps_and_split_calls():
     """Matrices are independent: one call over all gives the bits of a call each; three
     steps follow the oracle's."""
