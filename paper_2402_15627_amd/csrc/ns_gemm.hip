@@ -34,8 +34,8 @@
 // 1.34e-3, 1.24e-3), and apply reads no X beside its operand.
 //
 // MFMA-bound: the 175B share's products in two planes (44e12 operations a step of five)
-// run at 1.38 PFLOP/s, matrix cores busy 72 to 84% at the 1.7 to 1.8 GHz that their power
-// allows; in one plane (5120 x 5120 twice, 20480 x 5120) at 1.1, busy 57 to 71%, the
+// run at 1.38 PFLOP/s, matrix cores busy 72 to 83% at the 1.7 to 1.8 GHz that their power
+// allows; in one plane (5120 x 5120 twice, 20480 x 5120) at 1.2, busy 49 to 69%, the
 // operands' way through LDS being longer than the products.
 //
 // Two kernels:
