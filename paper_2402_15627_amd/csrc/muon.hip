@@ -9,7 +9,7 @@
 // moves every singular value of X in [0, 1] towards 1 and stays in [0, 1.203].
 //
 //   1. update: M in place, the sum of U^2 per 64 x 64 tile, in fp64
-//   2. norm:   1 / (||U||_F + eps) of each matrix
+//   2. norm:   1 / (||U||_F + eps) of each matrix (few tiles: part of 3)
 //   3. init:   X's fp16 planes, padded to multiples of 64 with zeros
 //   4. the products (ns_gemm.hip), each one launch for all matrices of a chain
 //   5. finish: w and its copy, or the orthogonalised matrix itself; part of the last
@@ -19,7 +19,7 @@
 // a row per 16 lanes; a tall matrix's tile is transposed through LDS (226 M elements of
 // the 175B share: 0.54, 0.53 and 0.61 ms, 5.0, 5.1 and 5.2 TB/s).  A step of those takes
 // 33.5 ms, 32 of them products at the matrix cores' power limit; one of six matrices of
-// 256 x 256 and 1024 x 256 0.16 ms, 18 launches of about 8 us each in a row.
+// 256 x 256 and 1024 x 256 0.16 ms, 17 launches of about 8 us each in a row.
 #include "common.h"
 #include "kernels.h"
 #include "ns_gemm.h"
@@ -144,10 +144,14 @@ __global__ __launch_bounds__(kNormThreads) void ns_norm_kernel(NsTable t, float 
   }
 }
 
-// X's tile of 64 x 64 at (i0, j0) of its padded m x n from U's tile of the tensor.
-template <NsMode MODE, int PLANES>
+// X's tile of 64 x 64 at (i0, j0) of its padded m x n from U's tile of the tensor.  sums:
+// ns_norm_kernel's factors; or (FOLD) the tiles' sums, kThreads to a matrix at most, that
+// every workgroup then adds up itself, in the order of that kernel: a launch less for a
+// longer start here (five steps of 256 x 256 in fp32 113.7 us with the launch, 112.1
+// without; 64 x 256 80.9 and 79.4).
+template <NsMode MODE, int PLANES, bool FOLD>
 __global__ __launch_bounds__(kThreads) void ns_init_kernel(NsTable t, NsScalars sc,
-                                                           const double* __restrict__ norm) {
+                                                           const double* __restrict__ sums) {
   using T = typename std::conditional<MODE == NsMode::Bf16, bf16, float>::type;
   __shared__ float lds[kTile][kTile + 1];
   const TileAt at = tile_at(t);
@@ -155,7 +159,19 @@ __global__ __launch_bounds__(kThreads) void ns_init_kernel(NsTable t, NsScalars 
   const bool tall = x.rows > x.cols;
   const bool vec = rows_vec<T>(x.src, x.ld_src) &&
                    (MODE != NsMode::Muon || rows_vec<float>(x.mom, x.ld_src));
-  const double f = norm[at.i];  // (in fp32 that of a norm past 1e38 has lost its bits)
+  double f;  // (in fp32 that of a norm past 1e38 has lost its bits)
+  if constexpr (FOLD) {
+    __shared__ double red[kThreads / 64];
+    const int k0 = t.tile0[at.i], n = t.tile0[at.i + 1] - k0;
+    double ss = (int)threadIdx.x < n ? sums[k0 + threadIdx.x] : 0.0;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) ss += __shfl_xor(ss, o, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
+    __syncthreads();
+    f = 1.0 / (sqrt(((red[0] + red[1]) + red[2]) + red[3]) + (double)sc.eps);
+  } else {
+    f = sums[at.i];
+  }
   const int cl = 4 * (threadIdx.x & 15), c = at.c0 + cl, left = x.cols - c;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -229,9 +245,10 @@ __global__ __launch_bounds__(kThreads) void ns_finish_kernel(NsTable t, NsFinish
 // A chain: X's planes, products, the tensors.
 template <NsMode MODE, int PLANES>
 void run_chain(const NsTable& t, const NsScalars& sc, const NsFinish& fin, const NsProducts& p,
-               const double* norm, float* part, hipStream_t s) {
+               const double* sums, bool fold, float* part, hipStream_t s) {
   const int tiles = t.tile0[t.count];
-  ns_init_kernel<MODE, PLANES><<<tiles, kThreads, 0, s>>>(t, sc, norm);
+  if (fold) ns_init_kernel<MODE, PLANES, true><<<tiles, kThreads, 0, s>>>(t, sc, sums);
+  else ns_init_kernel<MODE, PLANES, false><<<tiles, kThreads, 0, s>>>(t, sc, sums);
   launch_ns_products(t, fin, PLANES, sc.steps, p, part, s);
   if (p.apply.big)
     ns_finish_kernel<PLANES><<<tiles, kThreads, 0, s>>>(t, fin, ns_groups(p, sc.steps) & 1);
@@ -241,14 +258,17 @@ template <NsMode MODE>
 void run(const NsTable& t, const NsScalars& sc, Dt copy_dt, const NsChains& c, double* partial,
          double* norm, float* part, hipStream_t s) {
   ns_update_kernel<MODE><<<t.tile0[t.count], kThreads, 0, s>>>(t, sc, partial);
-  ns_norm_kernel<<<t.count, kNormThreads, 0, s>>>(t, sc.eps, partial, norm);
+  bool fold = true;
+  for (int i = 0; i < t.count; ++i) fold = fold && t.tile0[i + 1] - t.tile0[i] <= kThreads;
+  if (!fold) ns_norm_kernel<<<t.count, kNormThreads, 0, s>>>(t, sc.eps, partial, norm);
   const bool bf16_out = MODE == NsMode::Bf16 || (MODE == NsMode::Muon && copy_dt == Dt::BF16);
   const NsFinish fin{MODE, bf16_out, sc.lr};
   for (int k = 0, lo = 0; k < c.count; lo = c.end[k++]) {
     const NsTable u = ns_slice(t, lo, c.end[k]);
-    if (c.planes[k] == 2) run_chain<MODE, 2>(u, sc, fin, c.p[k], norm + lo, part, s);
+    const double* sums = fold ? partial + t.tile0[lo] : norm + lo;
+    if (c.planes[k] == 2) run_chain<MODE, 2>(u, sc, fin, c.p[k], sums, fold, part, s);
     else if constexpr (MODE != NsMode::F32)
-      run_chain<MODE, 1>(u, sc, fin, c.p[k], norm + lo, part, s);
+      run_chain<MODE, 1>(u, sc, fin, c.p[k], sums, fold, part, s);
   }
 }
 

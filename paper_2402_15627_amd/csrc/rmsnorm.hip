@@ -7,11 +7,10 @@
 //             dgamma = sum over rows of dy s r
 //
 // HBM-bound, one pass each (bf16, 8192 x 5120: forward 60 us and 5.6 TB/s, backward 61 and
-// 5.5 with 5 more for dgamma; 2048 x 12288 in 8 bits 42 us): a row stays in the registers of the TPR threads that
-// share it (NC pieces of 8 columns a thread), so it is read once.  Narrow rows
-// share a workgroup.  s is stored rounded to the activation type, while y is
-// formed from the unrounded sum; the backward takes the stored s and the
-// forward's r.
+// 5.5 with 5 more for dgamma; 2048 x 12288 in 8 bits 42 us): a row stays in the registers
+// of the TPR threads that share it (NC pieces of 8 columns a thread), so it is read once.
+// Narrow rows share a workgroup.  s is stored rounded to the activation type, while y is
+// formed from the unrounded sum; the backward takes the stored s and the forward's r.
 //
 // The sum of squares is formed in fp64: in fp32 it overflows from elements of 1e19 on and
 // vanishes below 1e-23 (8192 x 5120: 60.1 us in fp32, 60.6 so).
