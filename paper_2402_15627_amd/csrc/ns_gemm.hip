@@ -648,14 +648,34 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
   }
   __syncthreads();
   float v[8];
+  auto sum_at = [&](int w, int h) {
+    return *reinterpret_cast<const f32x4*>(smem + w * kSWaveLds + r * (kST * 4) +
+                                           ((((c8 >> 2) + h) ^ r) & 15) * 16);
+  };
+  f32x4 sum[2];
+  if (waves == kSWaves) {
+    // all the reads at once: five steps of 256 x 256 in fp32 112.3 us one after the other,
+    // 108.1 so (for fewer waves so many reads take longer: 64 x 256 78.4 and 82.1)
+    f32x4 q[2][kSWaves];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int at = r * (kST * 4) + (((c8 >> 2) + h) ^ r & 15) * 16;
-    f32x4 s = *reinterpret_cast<const f32x4*>(smem + at);
-    for (int w = 1; w < waves; ++w) s += *reinterpret_cast<const f32x4*>(smem + w * kSWaveLds + at);
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[4 * h + e] = s[e];
+      for (int w = 0; w < kSWaves; ++w) q[h][w] = sum_at(w, h);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      sum[h] = q[h][0];
+#pragma unroll
+      for (int w = 1; w < kSWaves; ++w) sum[h] += q[h][w];
+    }
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      sum[h] = sum_at(0, h);
+      for (int w = 1; w < waves; ++w) sum[h] += sum_at(w, h);
+    }
   }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = sum[e >> 2][e & 3];
   if (it.slice >= 0) {
     float* p = part + ((size_t)(it.tile - plan.n_full) * plan.splits + it.slice) * (kST * kST) +
                r * kST + c8;
