@@ -19,7 +19,7 @@
 // a row per 16 lanes; a tall matrix's tile is transposed through LDS (226 M elements of
 // the 175B share: 0.54, 0.53 and 0.61 ms, 5.0, 5.1 and 5.2 TB/s).  A step of those takes
 // 33.5 ms, 32 of them products at the matrix cores' power limit; one of six matrices of
-// 256 x 256 and 1024 x 256 0.16 ms, 17 launches of about 8 us each in a row.
+// 256 x 256 and 1024 x 256 0.15 ms, 17 launches of about 8 us each in a row.
 #include "common.h"
 #include "kernels.h"
 #include "ns_gemm.h"
