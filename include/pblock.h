@@ -731,8 +731,8 @@ pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s,
  * with fewer than 64 rows or columns have PB_F32's products.
  *
  * pblock_orthogonalize: X alone, from in to out (may be the same memory with the
- * same ld, else apart), both in dtype; PB_F32 products for PB_F32, PB_BF16 products
- * for PB_BF16 (whose own rounding of the input moves the result by more).
+ * same ld, else apart), both in dtype; PB_F32's products for either type, and the
+ * result rounded once.
  *
  * ws: the *_workspace_bytes, 256-byte aligned; nothing in it outlives the call, and
  * calls that may overlap need one each (so do two captured graphs that may).

@@ -173,6 +173,9 @@ struct NsProducts {
   bool paired;                   // two steps to one gram and apply
 };
 inline int ns_symmetric(const NsProducts& p) { return p.paired ? 3 : 2; }  // s in use
+// The one of them that is dead before X is replaced: without memory of its own (nullptr) it
+// takes that of the X that replaces it (of at least its size).
+inline int ns_lent(const NsProducts& p) { return p.paired ? 2 : 0; }
 // Times that X is replaced: it is in x[ns_groups & 1] at the end.
 inline int ns_groups(const NsProducts& p, int steps) { return p.paired ? (steps + 1) / 2 : steps; }
 // The chains of a call: chain k has the matrices end[k - 1] .. end[k] - 1 of its table.

@@ -267,7 +267,7 @@ void run(const NsTable& t, const NsScalars& sc, Dt copy_dt, const NsChains& c, d
     const NsTable u = ns_slice(t, lo, c.end[k]);
     const double* sums = fold ? partial + t.tile0[lo] : norm + lo;
     if (c.planes[k] == 2) run_chain<MODE, 2>(u, sc, fin, c.p[k], sums, fold, part, s);
-    else if constexpr (MODE != NsMode::F32)
+    else if constexpr (MODE == NsMode::Muon)
       run_chain<MODE, 1>(u, sc, fin, c.p[k], sums, fold, part, s);
   }
 }

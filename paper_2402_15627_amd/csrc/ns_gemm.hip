@@ -849,9 +849,10 @@ void launch(const NsTable& t, const NsLaunch& c, const Product& p, const NsFinis
 }
 
 template <int PLANES>
-void iterate(const NsTable& t, const NsFinish& fin, int steps, const NsProducts& p, float* part,
-             hipStream_t s) {
+void iterate(const NsTable& matrices, const NsFinish& fin, int steps, const NsProducts& p,
+             float* part, hipStream_t s) {
   constexpr float kSquare = kNsC * kNsScaleB / (kNsScaleA * kNsScaleA);
+  NsTable t = matrices;
   int cur = 0;
   auto sym = [&](const NsLaunch& c, const Product& q) {
     launch<Op::Sym, PLANES>(t, c, q, fin, cur, part, s);
@@ -860,6 +861,9 @@ void iterate(const NsTable& t, const NsFinish& fin, int steps, const NsProducts&
     launch<Op::Square, PLANES>(t, p.square, Product{from, from, to, kSquare}, fin, cur, part, s);
   };
   for (int left = steps; left > 0; cur ^= 1) {
+    const int lent = ns_lent(p);  // (A; in pairs B A and B')
+    for (int i = 0; i < t.count; ++i)
+      if (!matrices.mat[i].s[lent]) t.mat[i].s[lent] = t.mat[i].x[cur ^ 1];
     sym(p.gram, kGram);  // A
     square(0, 1);        // B
     int by = 1;
@@ -954,8 +958,9 @@ NsChains pair_chains(NsTable& t, int planes) {
 
 }  // namespace
 
-// One plane serves bf16 from 64 rows and columns on.  Under that the roundings of few
-// elements show (16 x 16 off by up to 2.6e-3, 64 x 64 by 1.5e-3) and a step is latency:
+// One plane serves the Muon step's bf16 products from 64 rows and columns on.  Under that
+// the roundings of few elements show (16 x 16 off by up to 2.6e-3, 64 x 64 by 1.5e-3) and a
+// step is latency:
 // five steps of 64 x 256 take 70 us in one plane, of 60 x 256 82 in two.  Beside larger
 // matrices the small ones have a chain of their own, or all of a call take two planes,
 // whichever is estimated to end sooner.

@@ -259,8 +259,10 @@ bool ns_add(pb::NsTable& t, int rows, int cols) {
 }
 
 // Plans the products, and places the planes of every matrix from base on (nullptr: sizes
-// alone).
-NsLayout ns_layout(pb::NsTable& t, bool f32_products, char* base, pb::NsChains* c) {
+// alone).  lend: the symmetric matrix that is dead before X is replaced lies in the X that
+// replaces it (for matrices held in bf16, whose workspace is then 6 values an element of a
+// square matrix instead of 8; fp32 calls keep it apart).
+NsLayout ns_layout(pb::NsTable& t, bool f32_products, bool lend, char* base, pb::NsChains* c) {
   NsLayout L{};
   if (t.count == 0) return L;
   pb::ns_plan(t, f32_products, c);
@@ -275,8 +277,11 @@ NsLayout ns_layout(pb::NsTable& t, bool f32_products, char* base, pb::NsChains* 
     x.x[0] = (_Float16*)(base + o);
     x.x[1] = (_Float16*)(base + o + big);
     o += 2 * big;
-    const int n = pb::ns_symmetric(c->p[chain]);
-    for (int k = 0; k < n; ++k, o += small) x.s[k] = (_Float16*)(base + o);
+    const int n = pb::ns_symmetric(c->p[chain]), lent = lend ? pb::ns_lent(c->p[chain]) : -1;
+    for (int k = 0; k < n; ++k) {
+      x.s[k] = k == lent ? nullptr : (_Float16*)(base + o);
+      if (k != lent) o += small;
+    }
   }
   L.part = o;
   L.total = o + align256(c->partial_floats * sizeof(float));
@@ -314,7 +319,7 @@ pb_status ns_launch(pb::NsTable& t, const pb::NsScalars& sc, pb::NsMode mode,
                     bool f32_products, pb::Dt copy_dt, void* ws, size_t ws_bytes, hipStream_t stream) {
   if (t.count == 0) return nothing_to_do();
   pb::NsChains c;
-  const NsLayout L = ns_layout(t, f32_products, (char*)ws, &c);
+  const NsLayout L = ns_layout(t, f32_products, mode == pb::NsMode::Bf16, (char*)ws, &c);
   PB_CHECK(check_ws(ws, ws_bytes, L.total));
   for (int i = 0; i < t.count; ++i) {
     const pb::NsMat& x = t.mat[i];
@@ -336,9 +341,9 @@ pb_status ns_launch(pb::NsTable& t, const pb::NsScalars& sc, pb::NsMode mode,
 }
 
 // The bytes that the table's call needs.
-size_t ns_bytes(pb::NsTable& t, pb_dtype products) {
+size_t ns_bytes(pb::NsTable& t, bool f32_products, bool lend) {
   pb::NsChains c;
-  return ns_layout(t, products == PB_F32, nullptr, &c).total;
+  return ns_layout(t, f32_products, lend, nullptr, &c).total;
 }
 
 }  // namespace
@@ -451,7 +456,7 @@ size_t pblock_muon_workspace_bytes(const pb_muon_config* cfg, int n_tensors,
                                    const pb_muon_tensor* tensors) {
   pb::NsTable t{};
   if (!cfg || !known(cfg->products) || ns_table(n_tensors, tensors, t) != PB_OK) return 0;
-  return ns_bytes(t, cfg->products);
+  return ns_bytes(t, cfg->products == PB_F32, false);
 }
 
 pb_status pblock_muon_step(const pb_muon_config* cfg, int n_tensors, const pb_muon_tensor* tensors,
@@ -528,7 +533,7 @@ size_t pblock_orthogonalize_workspace_bytes(int n_tensors, const pb_ortho_tensor
                                             pb_dtype dtype) {
   pb::NsTable t{};
   if (!known(dtype) || ns_table(n_tensors, tensors, t) != PB_OK) return 0;
-  return ns_bytes(t, dtype);
+  return ns_bytes(t, true, dtype == PB_BF16);
 }
 
 pb_status pblock_orthogonalize(int n_tensors, const pb_ortho_tensor* tensors, pb_dtype dtype,
@@ -572,7 +577,7 @@ pb_status pblock_orthogonalize(int n_tensors, const pb_ortho_tensor* tensors, pb
   sc.eps = eps;
   sc.steps = steps;
   return ns_launch(t, sc, dtype == PB_F32 ? pb::NsMode::F32 : pb::NsMode::Bf16,
-                   dtype == PB_F32, dt_of(dtype), ws, ws_bytes, stream);
+                   true, dt_of(dtype), ws, ws_bytes, stream);
 }
 
 }  // extern "C"

@@ -824,7 +824,8 @@ def pblock_orthogonalize_workspace_bytes(tensors, dtype="bf16") -> int:
 
 
 def pblock_orthogonalize(tensors, dtype, ws, steps=5, eps=1e-7, stream=None):
-    """The orthogonalised matrices of OrthoTensors of dtype "bf16" or "f32"."""
+    """The orthogonalised matrices of OrthoTensors of dtype "bf16" or "f32" (how
+    they are held: products carry 22 bits of each factor either way)."""
     code = _dtype_of(dtype)
     call = _matrices(tensors, "x", _torch_dtype(code))
     call.run(load_library().pblock_orthogonalize,
