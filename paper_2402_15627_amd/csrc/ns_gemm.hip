@@ -11,9 +11,10 @@
 // Three m x m products for two with X: with half of each symmetric product computed,
 // 8 m^3 + 3 (n - m) m^2 operations for 8 m^3 + 6 (n - m) m^2.  (Over more steps the
 // spread of A's eigenvalues, the square of X's, costs accuracy: five steps from one A
-// lose two digits, a pair none: 256 x 1024, 16 directions in noise, 2.0e-6 off either
-// way, 8 in a tenth of the noise 5.0e-6 in pairs and 8.3e-6 step by step, where fp32 is
-// 2.1e-6 and 4.6e-6 off.)
+// lose two digits, pairs between nothing and a factor of 2.5.  256 x 1024: noise alone
+// 2.0e-6 off either way; 16 directions beside noise of their elements' size 4.2e-6 in
+// pairs and 2.1e-6 step by step, of a hundredth of it 2.7e-5 and 4.5e-5; one plane 3.5e-3
+// and 1.7e-3, 3.0e-2 and 3.9e-2.  fp32 is 1.9e-6 and 2.2e-5 off.)
 //
 //   Sym     L R, L and R symmetric, or X X^T: tiles on and above the diagonal, each
 //           written to its mirror image too

@@ -81,3 +81,63 @@ def test_orthogonalize_bf16_steps_in_both_tiles(steps):
         pb.pblock_orthogonalize([pb.ortho_tensor(x, x) for x in xs], "bf16", ws, steps)
         assert all(torch.equal(x, o) for x, o in zip(xs, outs))
         assert not any(torch.equal(x, k) for x, k in zip(xs, keep))
+
+
+def exact(u, steps=5):
+    """The iteration in float64, on the GPU."""
+    import torch
+    a, b, c = oo.NS
+    x = u.double()
+    x = x.t() if u.shape[0] > u.shape[1] else x
+    x = (x / (x.square().sum().sqrt() + float(np.float32(1e-7)))).contiguous()
+    for _ in range(steps):
+        gram = x @ x.t().contiguous()
+        x = a * x + (b * gram + c * (gram @ gram)) @ x
+    return x.t() if u.shape[0] > u.shape[1] else x
+
+
+# What include/pblock.h states, by the noise beside the strong directions (as a share of
+# their elements): for products of 22 and of 11 bits.
+STATED = {1.0: (5e-6, 5e-3), 0.1: (5e-5, 3e-2), 1e-2: (5e-4, 2e-1), 1e-3: (5e-4, 2e-1), 0.0: (5e-4, 2e-1)}
+
+
+@pytest.mark.parametrize("r,c", [(512, 512), (256, 1024), (1024, 64), (1100, 1100), (2048, 4096)],
+                         ids=lambda v: str(v))
+def test_muon_products_are_as_exact_as_stated(r, c):
+    """From zero weights and momentum a step of length one leaves the update itself."""
+    import torch
+    from paper_2402_15627_amd import pblock as pb
+    g = torch.Generator(device="cuda").manual_seed(r + c)
+    new = lambda *s: torch.empty(s, device="cuda").normal_(generator=g)  # noqa: E731
+    for noise, stated in STATED.items():
+        for rank in (1, 4, 16, 48) if noise < 1.0 else (0, 1, 16):
+            u = noise * new(r, c)
+            if rank:
+                u += new(r, rank) @ new(rank, c)
+            ref, off_by = exact(u), []
+            for products, tol in zip(("f32", "bf16"), stated):
+                w, m = torch.zeros_like(u), torch.zeros_like(u)
+                cfg = pb.muon_config(-1.0, 0.0, nesterov=False, products=products)
+                part = [pb.muon_tensor(w, u, m)]
+                pb.pblock_muon_step(cfg, part, ws=workspace(pb.pblock_muon_workspace_bytes(cfg, part)))
+                off_by.append(float((w.double() - ref).norm() / ref.norm()))
+            _say(f"[gpu] muon {r} x {c} rank={rank} noise={noise:g}: f32 {off_by[0]:.1e} bf16 {off_by[1]:.1e}")
+            assert off_by[0] <= stated[0] and off_by[1] <= stated[1]
+
+
+@pytest.mark.parametrize("size", [1e-9, 1e-13, 1e-18, 1e-30])
+def test_updates_far_below_eps(size):
+    """X is U / eps there and each step multiplies it by 3.4445.  Its elements are kept to
+    2^-40 in each of five steps, which the later ones raise by 485, 141, 41, 12 and 3.4:
+    2^-40 times 682 is below 2^-30; beside that the fp32 figure."""
+    import torch
+    from paper_2402_15627_amd import pblock as pb
+    _say(f"[gpu] orthogonalize, norm {size:g}")
+    g = torch.Generator(device="cuda").manual_seed(11)
+    u = torch.empty(200, 300, device="cuda").normal_(generator=g)
+    u *= size / float(u.norm())
+    out = torch.empty_like(u)
+    part = [pb.ortho_tensor(u, out)]
+    pb.pblock_orthogonalize(part, "f32", workspace(pb.pblock_orthogonalize_workspace_bytes(part, "f32")))
+    ref = exact(u)
+    assert bool(((out.double() - ref).abs() <= 2.0 ** -30 + 2.0 ** -20 * ref.abs().max()).all())
