@@ -608,8 +608,8 @@ pb_status pblock_lamb_step(const pb_lamb_config* cfg, int n_tensors,
  *   element (token, head, e) of in at in[token*ld_in + head*head_dim + e], ld_in in
  *   elements (>= heads*head_dim), out likewise.  out may be in with ld_out = ld_in
  *   (in place; elements past rot_dim are then left alone); otherwise no memory of
- *   any out may be in any other in or out (refused, unless they interleave with two
- *   leading dimensions, which is not seen).  Pointers are aligned to the element;
+ *   any out may be in any other in or out or in positions (refused, unless tensors
+ *   interleave with two leading dimensions, which is not seen).  Pointers are aligned to the element;
  *   16-byte aligned pieces (head_dim, ld and rot_dim, or rot_dim/2 when not
  *   interleaved, multiples of 16 bytes) run fastest.
  * positions: int64 per token, device memory, any value (negative ones turn the
@@ -737,8 +737,9 @@ pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s,
  *   a tenth                    5e-5      3e-2      3e-5
  *   a hundredth and less       5e-4      2e-1      6e-4      (U nearly of low rank)
  *
- * measured at 64 to 5120 rows, beside the same steps by fp32 library products.  Elements of X are kept to 2^-40: an update whose norm is far below eps, which
- * stays far from orthogonal, is good to 2^-30 absolute.
+ * measured at 64 to 5120 rows, beside the same steps by fp32 library products.  Elements
+ * of X are kept to 2^-40: an update whose norm is far below eps, which stays far from
+ * orthogonal, is good to 2^-30 absolute.
  * Sizes and company decide tiles, cuts along K and whether steps go in pairs (which
  * moves X by up to 2.5 times the error of single ones): a matrix's last bits, with
  * PB_BF16 those within the table, may differ with the other matrices of the call.  The

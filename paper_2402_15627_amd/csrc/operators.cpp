@@ -61,7 +61,7 @@ bool overlap(const Span& a, const Span& b, size_t e) {
   const size_t ld = lo.rows > 1 ? lo.ld : hi.ld, at = off % ld;
   return at < lo.width || ld - at < hi.width;
 }
-// A workspace and the rows of an element of e bytes.
+// A workspace (or other dense range) and the rows of an element of e bytes.
 bool overlap(const void* ws, size_t bytes, const Span& x, size_t e) {
   return overlap(Span{ws, bytes, bytes, 1}, Span{x.p, x.ld * e, x.width * e, x.rows}, 1);
 }
@@ -170,9 +170,11 @@ pb_status rope(const pb_rope_config* c, int n, const pb_rope_tensor* x, int64_t 
     a.heads[i] = x[i].heads;
     a.copy_rest[i] = x[i].in != x[i].out;
   }
-  for (int i = 0; i < n; ++i)
+  for (int i = 0; i < n; ++i) {
+    const Span out{x[i].out, x[i].ld_out, (size_t)x[i].heads * c->head_dim, tokens};
+    if (overlap(positions, (size_t)tokens * 8, out, e))
+      return fail(PB_ERR_INVALID_ARG, "out of tensor %d overlaps positions", i);
     for (int j = 0; j < n; ++j) {
-      const Span out{x[i].out, x[i].ld_out, (size_t)x[i].heads * c->head_dim, tokens};
       const Span in{x[j].in, x[j].ld_in, (size_t)x[j].heads * c->head_dim, tokens};
       const Span out2{x[j].out, x[j].ld_out, (size_t)x[j].heads * c->head_dim, tokens};
       if (i != j && overlap(out, out2, e))
@@ -180,6 +182,7 @@ pb_status rope(const pb_rope_config* c, int n, const pb_rope_tensor* x, int64_t 
       if (!(i == j && x[i].in == x[i].out) && overlap(out, in, e))
         return fail(PB_ERR_INVALID_ARG, "out of tensor %d overlaps in of tensor %d", i, j);
     }
+  }
   a.n = n;
   a.head_dim = c->head_dim;
   a.rot_dim = c->rot_dim;
