@@ -608,8 +608,8 @@ pb_status pblock_lamb_step(const pb_lamb_config* cfg, int n_tensors,
  *   element (token, head, e) of in at in[token*ld_in + head*head_dim + e], ld_in in
  *   elements (>= heads*head_dim), out likewise.  out may be in with ld_out = ld_in
  *   (in place; elements past rot_dim are then left alone); otherwise no memory of
- *   any out may be in any other in or out or in positions (refused, unless tensors
- *   interleave with two leading dimensions, which is not seen).  Pointers are aligned to the element;
+ *   any out may be in any other in or out or in positions (refused; tensors may
+ *   interleave row by row).  Pointers are aligned to the element;
  *   16-byte aligned pieces (head_dim, ld and rot_dim, or rot_dim/2 when not
  *   interleaved, multiples of 16 bytes) run fastest.
  * positions: int64 per token, device memory, any value (negative ones turn the
@@ -721,7 +721,7 @@ pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s,
  * own.  scale is the caller's rule for the shape (0.2 sqrt(max(rows, cols)), say).
  * Matrices with rows = 0 or cols = 0 are allowed (nothing is touched).  No param,
  * momentum, param_copy or ws may share memory with another of them or with a grad
- * (refused, unless they interleave with two lds, which is not always seen).
+ * (refused; they may interleave row by row).
  *
  * products: PB_F32 carries 22 bits of every factor (each fp16 value with its
  * remainder, three matrix products for one).  PB_BF16 rounds the factors to fp16 (11

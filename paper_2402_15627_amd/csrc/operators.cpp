@@ -48,18 +48,31 @@ struct Span {
   size_t ld, width;
   int64_t rows;
 };
-// Whether two such are seen to share memory: apart as a whole they do not, and of one
-// leading dimension they may interleave.  (Of two leading dimensions: seen where the
-// first element of one lies in a row of the other.)
+// Whether two such share memory.  Tensors apart as a whole, or of one leading dimension
+// (whose rows may interleave), are told at once; else the rows of one are looked up among
+// the other's, a few ns each.
 bool overlap(const Span& a, const Span& b, size_t e) {
   if (!a.rows || !b.rows || !a.p || !b.p) return false;
   const Span &lo = (uintptr_t)a.p <= (uintptr_t)b.p ? a : b, &hi = &lo == &a ? b : a;
   const size_t off = ((uintptr_t)hi.p - (uintptr_t)lo.p) / e;  // elements from lo to hi
   if (off >= (size_t)(lo.rows - 1) * lo.ld + lo.width) return false;
   if (lo.rows > 1 && off % lo.ld < lo.width) return true;
-  if (lo.ld != hi.ld && lo.rows > 1 && hi.rows > 1) return false;
-  const size_t ld = lo.rows > 1 ? lo.ld : hi.ld, at = off % ld;
-  return at < lo.width || ld - at < hi.width;
+  if (lo.ld == hi.ld || lo.rows == 1 || hi.rows == 1) {
+    const size_t ld = lo.rows > 1 ? lo.ld : hi.ld, at = off % ld;
+    return at < lo.width || ld - at < hi.width;
+  }
+  const Span &few = lo.rows < hi.rows ? lo : hi, &many = &few == &lo ? hi : lo;
+  const int64_t first = &few == &hi ? (int64_t)off : -(int64_t)off;  // of few, from many's
+  const int64_t ld = (int64_t)few.ld, width = (int64_t)few.width, ld2 = (int64_t)many.ld;
+  const int64_t end = (many.rows - 1) * ld2 + (int64_t)many.width;
+  for (int64_t r = first < 0 ? -first / ld : 0; r < few.rows && first + r * ld < end; ++r) {
+    const int64_t at = first + r * ld;
+    if (at + width <= 0) continue;
+    // many's last row that begins before this one ends
+    const int64_t k = std::min((at + width - 1) / ld2, many.rows - 1);
+    if (k * ld2 + (int64_t)many.width > at) return true;
+  }
+  return false;
 }
 // A workspace (or other dense range) and the rows of an element of e bytes.
 bool overlap(const void* ws, size_t bytes, const Span& x, size_t e) {
