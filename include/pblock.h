@@ -615,7 +615,7 @@ pb_status pblock_lamb_step(const pb_lamb_config* cfg, int n_tensors,
  * positions: int64 per token, device memory, any value (negative ones turn the
  *   other way; beyond 2^31 the angles lose accuracy).  NULL: token t is at position
  *   t mod seq.  seq is read only then.
- * tokens may be 0 (nothing is launched).
+ * tokens may be 0 (nothing is launched, and no pointer, position or seq is needed).
  * Errors: PB_ERR_INVALID_ARG for a bad config or pointer, PB_ERR_UNSUPPORTED for
  * head_dim > 256, or too many tokens or heads. */
 #define PB_ROPE_MAX_TENSORS 4

@@ -152,7 +152,7 @@ pb_status rope(const pb_rope_config* c, int n, const pb_rope_tensor* x, int64_t 
   if (tokens < 0) return fail(PB_ERR_INVALID_ARG, "tokens=%lld", (long long)tokens);
   if (tokens >= kMaxBlocks)
     return fail(PB_ERR_UNSUPPORTED, "tokens=%lld >= 2^24", (long long)tokens);
-  if (!positions && seq < 1) return fail(PB_ERR_INVALID_ARG, "seq must be >= 1");
+  if (!positions && tokens > 0 && seq < 1) return fail(PB_ERR_INVALID_ARG, "seq must be >= 1");
   PB_CHECK(check_opt(positions, 8, "positions"));
   static_assert(PB_ROPE_MAX_TENSORS == pb::kRopeMaxTensors, "tensor limit");
   static_assert(sizeof(int64_t) == sizeof(long long), "positions");
