@@ -616,8 +616,8 @@ pb_status pblock_lamb_step(const pb_lamb_config* cfg, int n_tensors,
  *   other way; beyond 2^31 the angles lose accuracy).  NULL: token t is at position
  *   t mod seq.  seq is read only then.
  * tokens may be 0 (nothing is launched, and no pointer, position or seq is needed).
- * Errors: PB_ERR_INVALID_ARG for a bad config or pointer, PB_ERR_UNSUPPORTED for
- * head_dim > 256, or too many tokens or heads. */
+ * Errors: PB_ERR_INVALID_ARG for a bad config (a frequency that is not finite among
+ * them) or pointer, PB_ERR_UNSUPPORTED for head_dim > 256, or too many tokens or heads. */
 #define PB_ROPE_MAX_TENSORS 4
 typedef enum { PB_ROPE_PLAIN = 0, PB_ROPE_LINEAR = 1, PB_ROPE_BY_PARTS = 2 } pb_rope_scaling;
 typedef struct {
@@ -630,7 +630,7 @@ typedef struct {
   double orig_len;   /* > 0; this and the next two by PB_ROPE_BY_PARTS only   */
   double low_turns;  /* 0 <= low_turns < high_turns                           */
   double high_turns;
-  double magnitude;  /* > 0, finite                                           */
+  double magnitude;  /* > 0, finite, in fp32                                  */
   pb_dtype dtype;
 } pb_rope_config;
 typedef struct {

@@ -128,8 +128,8 @@ pb_status check_rope(const pb_rope_config* c) {
     return fail(PB_ERR_INVALID_ARG, "interleaved must be 0 or 1");
   if (!(c->base > 0.0) || !std::isfinite(c->base))
     return fail(PB_ERR_INVALID_ARG, "base must be finite and > 0");
-  if (!(c->magnitude > 0.0) || !std::isfinite((float)c->magnitude))
-    return fail(PB_ERR_INVALID_ARG, "magnitude must be finite and > 0");
+  if (!((float)c->magnitude > 0.f) || !std::isfinite((float)c->magnitude))
+    return fail(PB_ERR_INVALID_ARG, "magnitude must be finite and > 0 in fp32");
   if (c->scaling < PB_ROPE_PLAIN || c->scaling > PB_ROPE_BY_PARTS)
     return fail(PB_ERR_INVALID_ARG, "scaling=%d", c->scaling);
   if (c->scaling != PB_ROPE_PLAIN && (!(c->factor > 0.0) || !std::isfinite(c->factor)))
@@ -213,6 +213,8 @@ pb_status rope(const pb_rope_config* c, int n, const pb_rope_tensor* x, int64_t 
                                                        (c->high_turns - c->low_turns)));
       f *= g + (1.0 - g) / c->factor;
     }
+    if (!std::isfinite(f))
+      return fail(PB_ERR_INVALID_ARG, "the frequency of pair %d is not finite", i);
     a.turns[i] = f / two_pi;
   }
   if (tokens == 0) return nothing_to_do();
