@@ -601,8 +601,8 @@ pb_status pblock_lamb_step(const pb_lamb_config* cfg, int n_tensors,
  * By parts: pairs that turn often within the trained length orig_len keep their
  * frequency, the slow ones are interpolated (Peng et al. 2023); magnitude is the
  * attention's rescaling that goes with it (1 for none).  The other elements of a
- * head are passed through.  Angles are formed in 64 bits, the rotation in 32,
- * rounded once.
+ * head are passed through.  Angles are formed in 64 bits; sine, cosine (good to 1.5
+ * 2^-24) and the rotation in 32, rounded once.
  *
  * tensors[k] (1 to PB_ROPE_MAX_TENSORS, e.g. Q and K, of their own head counts):
  *   element (token, head, e) of in at in[token*ld_in + head*head_dim + e], ld_in in
