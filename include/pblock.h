@@ -661,13 +661,18 @@ pb_status pblock_rope_backward(const pb_rope_config* cfg, int n_tensors,
  *   sum  [rows, cols] act   s rounded, the next residual (NULL unless resid is
  *                           given; may be x or resid)
  *   y    [rows, cols] act   (may be x or resid, whichever sum is not)
- *   q8   [rows, cols] OCP e4m3, with scales: q8 = y / scale rounded to nearest
- *        even, scale = max(max|y| / 448, 2^-126) in fp32 over each group of
+ *   q8   [rows, cols] OCP e4m3, with scales: q8 = y / scale rounded to fp32 and
+ *        that to e4m3, each to nearest even (as a cast does),
+ *        scale = max(max|y| / 448, 2^-126) in fp32 over each group of
  *        `group` columns of a row (32, 64 or 128; the last group of a row may be
  *        short) or over the row (0).  scales [rows, ceil(cols / group)] (or
- *        [rows]).  A row with a NaN or an infinity has NaN codes where y is NaN.
+ *        [rows]).  A NaN in y has a NaN code and is passed over by its scale; an
+ *        infinite y (of an infinite gamma) makes its scale infinite, its own code
+ *        NaN and the others of its group 0.
  *   rstd [rows] fp32        r, for the backward
- * gamma [cols] act.
+ * gamma [cols] act.  A NaN in a row of s makes the row of y NaN, an infinity makes r 0:
+ * y is NaN there and 0 beside it.  (eps 0: a row whose root mean square is under 3e-39,
+ * past which r leaves fp32, is infinite or NaN; in q8 a row of zeros alone.)
  *
  * pblock_rmsnorm_backward: s [rows, cols] act is the forward's sum (x without a
  * residual), dy the gradient of y, dsum (may be NULL) the gradient that reaches s
