@@ -141,3 +141,29 @@ def test_updates_far_below_eps(size):
     pb.pblock_orthogonalize(part, "f32", workspace(pb.pblock_orthogonalize_workspace_bytes(part, "f32")))
     ref = exact(u)
     assert bool(((out.double() - ref).abs() <= 2.0 ** -30 + 2.0 ** -20 * ref.abs().max()).all())
+
+
+@pytest.mark.parametrize("products", ["f32", "bf16"])
+def test_a_matrix_alone_and_among_others(products):
+    """Tiles, cuts and pairs of a matrix may change with its company; the result stays
+    within the stated distance of the exact one, and a call repeated gives its bits."""
+    import torch
+    from paper_2402_15627_amd import pblock as pb
+    _say(f"[gpu] muon alone and among others, {products}")
+    g = torch.Generator(device="cuda").manual_seed(5)
+    shapes = [(300, 900), (640, 640), (1200, 5000), (40, 70), (2100, 512), (64, 256)]
+    us = [torch.empty(s, device="cuda").normal_(generator=g) for s in shapes]
+
+    def call(us):
+        ws_, ms = [torch.zeros_like(u) for u in us], [torch.zeros_like(u) for u in us]
+        cfg = pb.muon_config(-1.0, 0.0, nesterov=False, products=products)
+        part = [pb.muon_tensor(w, u, m) for w, u, m in zip(ws_, us, ms)]
+        pb.pblock_muon_step(cfg, part, ws=workspace(pb.pblock_muon_workspace_bytes(cfg, part)))
+        return ws_
+
+    together, again = call(us), call(us)
+    for u, t, a in zip(us, together, again):
+        ref, alone = exact(u), call([u])[0]
+        assert torch.equal(t, a)
+        for v in (t, alone):
+            assert float((v.double() - ref).norm() / ref.norm()) <= STATED[1.0][products == "bf16"]
