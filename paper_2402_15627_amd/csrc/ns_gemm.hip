@@ -205,22 +205,43 @@ PB_DEV Operands operands(const NsMat& x, const Product& p, int cur) {
   }
 }
 
-// What Square adds to its sums at N consecutive columns n.. of row m: a I + b A.
+// Matrices of fewer than 16 rows or columns, whose few elements' roundings do not average:
+// their steps are not paired (pair_chains), and in 64 x 64 tiles (a call of large matrices
+// takes 256 x 256 for all) two planes' products are whole, l l too, and Square's sum is
+// fp64.  Off in the median over 30 inputs, so, without either and in fp32: 1 x 777 2.1e-7,
+// 8.1e-7 and 5.4e-7; 1 x 64 2.1e-7, 5.4e-7 and 4.0e-7; from 16 rows on fp32 is the
+// farthest without.  (For all matrices they would take 4% of a step of small ones.)
+__host__ __device__ inline bool few_rows(const NsMat& x) {
+  return (x.rows < x.cols ? x.rows : x.cols) < 16;
+}
+
+// A's plane values at N consecutive columns n.. of row m, for what Square adds to its
+// sums there: a I + b A.
 template <Op OP, int PLANES, int N>
 PB_DEV void addend(const NsMat& x, const Product& p, int m, int n, float* u) {
-  if constexpr (OP == Op::Square) {
-    ns_load<PLANES, N>(x.s[p.left] + ns_at<PLANES>(x.ldm, m, n), u, kNsB * kNsScaleB / kNsScaleA);
-#pragma unroll
-    for (int e = 0; e < N; ++e) u[e] += m == n + e ? kNsA * kNsScaleB : 0.f;
-  }
+  if constexpr (OP == Op::Square)
+    ns_load<PLANES, N>(x.s[p.left] + ns_at<PLANES>(x.ldm, m, n), u, 1.0f);
 }
-// N consecutive columns n.. of row m of a product.  v: the sums (scaled in place), u: the
-// addend.
+// N consecutive columns n.. of row m of a product.  v: the sums (scaled in place), u: those
+// of addend().  wide: Square's sum in fp64, rounded once.
 template <Op OP, int PLANES, int N>
 PB_DEV void store_result(const NsMat& x, const Product& p, int cur, int m, int n, float* v,
-                         const float* u) {
+                         const float* u, bool wide = false) {
+  auto sum = [&](auto zero) {
+    using R = decltype(zero);
 #pragma unroll
-  for (int e = 0; e < N; ++e) v[e] = v[e] * p.scale + (OP == Op::Square ? u[e] : 0.f);
+    for (int e = 0; e < N; ++e) {
+      const R add = (R)u[e] * (R)(kNsB * kNsScaleB / kNsScaleA) + (m == n + e ? kNsA * kNsScaleB : 0.f);
+      v[e] = (float)((R)v[e] * (R)p.scale + add);
+    }
+  };
+  if constexpr (OP == Op::Square) {
+    if (wide) sum(0.0);
+    else sum(0.f);
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] *= p.scale;
+  }
   if constexpr (symmetric(OP))
     ns_store<PLANES, N>(x.s[p.dst] + ns_at<PLANES>(x.ldm, m, n), v, 1.0f);
   else ns_store<PLANES, N>(x.x[cur ^ 1] + ns_at<PLANES>(x.ldn, m, n), v, 1.0f);
@@ -597,6 +618,7 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
     nk = min(nk, kt0 + chunk) - kt0;
   }
   unsigned char* own = smem + wave * kSWaveLds;
+  const bool few = PLANES == 2 && few_rows(x);
 
   f32x4 acc[4][4];
 #pragma unroll
@@ -631,7 +653,10 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
         for (int j = 0; j < 4; ++j)
           acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[j][bf], fa[i][af], acc[i][j], 0, 0, 0);
     };
-    if constexpr (PLANES == 2) mma(1, 0), mma(0, 1), mma(0, 0);
+    if constexpr (PLANES == 2) {
+      if (few) mma(1, 1);
+      mma(1, 0), mma(0, 1), mma(0, 0);
+    }
     else mma(0, 0), mma(1, 1);
   }
 
@@ -688,7 +713,7 @@ __global__ __launch_bounds__(kSThreads, 1) void ns_gemm_small(NsTable t, NsPlan 
     for (int e = 0; e < 8; ++e) v[e] *= prod.scale;
     if (!tall) finish<8>(x, fin, m0 + r, n0 + c8, v, u);
   } else {
-    store_result<OP, PLANES, 8>(x, prod, cur, m0 + r, n0 + c8, v, u);
+    store_result<OP, PLANES, 8>(x, prod, cur, m0 + r, n0 + c8, v, u, few);
   }
   if (OP == Op::Apply || (OP == Op::Last ? !tall : tm == tn)) return;
   __syncthreads();
@@ -929,13 +954,11 @@ NsChains pair_chains(NsTable& t, int planes) {
   // Pairs of steps only where X is at least twice as wide as tall: in a square one the
   // roundings of A' show (300 x 300, fp32 2.7e-6 off in pairs, 1.8e-6 step by step; one
   // plane 1.8e-3 and 1.3e-3; 128 x 256 1.3e-6 and 1.4e-6; 1.1e-3 either way).  And not
-  // under 16 rows, whose few elements' roundings do not average (fp32 1 x 777, off by
-  // 4.4e-7 in the median and 6.7e-7 at most step by step, 6.9e-7 and 1.3e-6 in pairs;
-  // 16 x 777 5.7e-7 and 7.7e-7, where fp32 products are off by 1.3e-6).
+  // under 16 rows (1 x 777 in pairs 1.6 times as far off; 16 x 777 5.7e-7 step by step and
+  // 7.7e-7, where fp32 products are off by 1.3e-6).
   int n = 0;
   const NsTable order = ordered(t, [](const NsMat& x) {
-    const int m = std::min(x.rows, x.cols);
-    return m >= 16 && std::max(x.rows, x.cols) >= 2 * m;
+    return !few_rows(x) && std::max(x.rows, x.cols) >= 2 * std::min(x.rows, x.cols);
   }, n);
   NsChains c{1, {t.count}, {planes}, {plan(t, false)}, 0};
   // Five steps, in pairs and step by step: fp32 64 x 1024 99 and 106 us, 256 x 1024 145

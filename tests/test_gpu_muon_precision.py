@@ -167,3 +167,24 @@ def test_a_matrix_alone_and_among_others(products):
         assert torch.equal(t, a)
         for v in (t, alone):
             assert float((v.double() - ref).norm() / ref.norm()) <= STATED[1.0][products == "bf16"]
+
+
+@pytest.mark.parametrize("r,c", [(1, 777), (1, 64), (3, 900), (777, 2)], ids=lambda v: str(v))
+def test_few_rows_are_no_farther_off_than_in_fp32(r, c):
+    """A few rows' roundings do not average.  In fp32 a step rounds X, A and B by 2^-24; an
+    fp16 value with its remainder is rounded by 2^-23 at most, so the products have to be
+    whole.  Over 30 inputs: the median within that of the iteration in fp32."""
+    import torch
+    from paper_2402_15627_amd import pblock as pb
+    ours, fp32 = [], []
+    for seed in range(30):
+        u = np.float32(np.random.default_rng(seed).standard_normal((r, c))).astype(np.float64)
+        x = torch.from_numpy(u).float().cuda()
+        part = [pb.ortho_tensor(x, x)]
+        pb.pblock_orthogonalize(part, "f32", workspace(pb.pblock_orthogonalize_workspace_bytes(part, "f32")))
+        ref = oo.newton_schulz(u, eps=np.float64(np.float32(1e-7)))
+        ours.append(off(f64(x), ref))
+        fp32.append(off(oo.newton_schulz(u, dtype=np.float32).astype(np.float64), ref))
+    _say(f"[gpu] orthogonalize f32 {r} x {c}: median {np.median(ours):.1e}, most {max(ours):.1e}; "
+         f"in fp32 {np.median(fp32):.1e}, {max(fp32):.1e}")
+    assert np.median(ours) <= np.median(fp32)
