@@ -581,10 +581,15 @@ pb_status pblock_lamb_step(const pb_lamb_config* cfg, int n_tensors,
                            hipStream_t stream);
 
 /* ------------------------------------------------------- rotary positions
- * The block has no positional terms of its own; these calls rotate Q and K
- * between the in-projection and the attention, and their gradients after the
- * attention backward (the stash and dZ then hold the rotated Q and K and, after
- * pblock_rope_backward, the gradients of the unrotated ones).
+ * The block has no positional terms of its own, and pblock_forward and
+ * pblock_backward run from their inputs to their outputs, with no place for another
+ * operator between their steps.  A block with rotated Q and K is put together from the
+ * calls of its parts (with tp = 1 on one GPU): pblock_ag_in_proj, pblock_rope_forward on
+ * Q and K of the packed Z, pblock_swattn_forward, pblock_rs_out_proj, pblock_rs_reduce;
+ * and pblock_ag_dc, pblock_swattn_backward, pblock_rope_backward on dQ and dK of the
+ * packed dZ, pblock_rs_dh.  Z then holds the rotated Q and K, and dZ the gradients of
+ * the unrotated ones; the weights' gradients, dZ^T h and dy^T C, are the caller's.  (A
+ * root-mean-square norm, below, takes its place before and after these in the same way.)
  *
  * The leading rot_dim elements of each head turn in pairs, i = 0 .. rot_dim/2 - 1:
  * elements (2i, 2i + 1) when interleaved, else (i, i + rot_dim/2), with
@@ -678,7 +683,8 @@ pb_status pblock_rope_backward(const pb_rope_config* cfg, int n_tensors,
  * residual), dy the gradient of y, dsum (may be NULL) the gradient that reaches s
  * from elsewhere (the residual's other use).  With g = dy gamma,
  *   dx = dsum + r (g - s r^2 mean(g s))   act: the gradient of x, and of resid
- *   dgamma = sum over rows of dy s r      [cols] fp32, overwritten
+ *   dgamma = sum over rows of dy s r      [cols] fp32, overwritten; summed in fp32
+ *            (off by 1e-7 of its norm at 8192 rows, 4e-7 at 10^6)
  * dx may be dy, dsum or s, as a whole.  Every other sharing of memory by an output
  * and another tensor (or ws) is refused, in both calls.  ws:
  * pblock_rmsnorm_workspace_bytes(cfg) bytes, 256-byte aligned, one for each call that

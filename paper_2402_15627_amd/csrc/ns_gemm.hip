@@ -36,8 +36,9 @@
 //
 // MFMA-bound: the 175B share's products in two planes (44e12 operations a step of five)
 // run at 1.38 PFLOP/s, matrix cores busy 72 to 83% at the 1.7 to 1.8 GHz that their power
-// allows; in one plane (5120 x 5120 twice, 20480 x 5120) at 1.2, busy 49 to 69%, the
-// operands' way through LDS being longer than the products.
+// allows; in one plane, which the Muon step's bf16 products alone have (5120 x 5120 twice,
+// 20480 x 5120), at 1.2, busy 49 to 69%, the operands' way through LDS being longer than
+// the products.
 //
 // Two kernels:
 //   - 256 x 256 tiles, eight waves, as the projection GEMMs' LDS-DMA kernel has them
@@ -962,8 +963,8 @@ NsChains pair_chains(NsTable& t, int planes) {
   }, n);
   NsChains c{1, {t.count}, {planes}, {plan(t, false)}, 0};
   // Five steps, in pairs and step by step: fp32 64 x 1024 99 and 106 us, 256 x 1024 145
-  // and 144, 2048 x 4096 1037 and 1085, 4096 x 8192 5670 and 6260; bf16 64 x 4096 98 and
-  // 111, 1024 x 4096 261 and 291 (chosen); 1024 x 2048, chosen too, 206 and 201.
+  // and 144, 2048 x 4096 1037 and 1085, 4096 x 8192 5670 and 6260; one plane 64 x 4096 98
+  // and 111, 1024 x 4096 261 and 291 (chosen); 1024 x 2048, chosen too, 206 and 201.
   if (n == t.count) {
     NsProducts p = c.p[0];
     p.paired = true;

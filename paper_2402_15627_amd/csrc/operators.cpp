@@ -266,8 +266,8 @@ bool ns_add(pb::NsTable& t, int rows, int cols) {
   x.m = pad(std::min(rows, cols));
   x.n = pad(std::max(rows, cols));
   // rows an odd number of 64 values apart: rows a power of two apart lie in few of the
-  // L2's channels (five steps of 2048 x 2048 in fp32 849 us, so 816; 2048 x 8192 in bf16
-  // 827 and 792; 256 x 1024 the same)
+  // L2's channels (five steps of 2048 x 2048 in fp32 849 us, so 816; 2048 x 8192 in one
+  // plane 827 and 792; 256 x 1024 the same)
   x.ldm = x.m | pb::kNsPad;
   x.ldn = x.n | pb::kNsPad;
   const long long tiles =
