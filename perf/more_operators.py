@@ -233,11 +233,12 @@ def _handles(s):
     from paper_2402_15627_amd import pblock as pb
     if s["kind"] == "adamw":
         s["cfg"] = pb.adamw_config(**ADAMW)
-        s["parts"] = [pb.adamw_tensor(t["w"], t["g"], t["m"], t["v"], t["copy"], t["decay"])
-                      if s["state"] == "f32" else
-                      pb.adamw_tensor(t["w"], t["g"], t["m"], t["r"], t["copy"], t["decay"],
-                                      t["m_scale"], t["r_scale"], t["seed"])
-                      for t in s["tensors"]]
+        s["parts"] = pb.AdamwTensors(
+            pb.adamw_tensor(t["w"], t["g"], t["m"], t["v"], t["copy"], t["decay"])
+            if s["state"] == "f32" else
+            pb.adamw_tensor(t["w"], t["g"], t["m"], t["r"], t["copy"], t["decay"], t["m_scale"],
+                            t["r_scale"], t["seed"])
+            for t in s["tensors"])
         return s
     s["cfg"] = pb.score_attn_config(s["batch"], s["seq_q"], s["seq"], s["heads"], s["kv_heads"],
                                     s["head_dim"], causal=s["causal"], window=s["window"],
