@@ -712,6 +712,109 @@ pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s,
                                   float* dgamma, void* ws, size_t ws_bytes,
                                   hipStream_t stream);
 
+/* ------------------------------- attention with terms in its scores
+ * Attention as a block with position biases, capped scores, packed documents or shared
+ * key heads has it, next to pblock_swattn_forward / _backward (plain scores, causal
+ * window, equal heads), whose place it takes among the calls of a block's parts.
+ *
+ * The seq_q queries of a batch row are the last of its seq_k positions: query i is at
+ * p = i + seq_k - seq_q (seq_q = seq_k in training; 1 for a new token over kept keys).
+ * Query head h reads key head h / (heads / kv_heads).
+ *
+ *   u = scale q.k
+ *   c = cap tanh(u / cap)                           (cap 0: c = u)
+ *   s = c - slopes[h] |p - j|                       with slopes
+ *   s = c + table[bucket(p - j)][h]                 with a table
+ *   P = softmax of s over the visible keys,  o = P v,  lse = log sum e^s
+ *
+ * Key j of the row is visible to query p when both are in one document and
+ *   0 <= p - j < window (causal), or |p - j| < window (not causal),
+ *   or j is in the document's prefix.
+ * docs: n_docs + 1 ascending offsets into the batch * seq_k tokens; document d is
+ *   tokens docs[d] .. docs[d + 1] - 1 (empty ones allowed), cut where a batch row ends.
+ *   NULL: each batch row is a document, and n_docs is ignored.  Tokens before the first
+ *   and behind the last document see nothing and are seen by none.
+ * prefix: the leading tokens of each document ([n_docs], or [batch] without docs) that
+ *   all its queries see, ahead of them or outside their window too.
+ * Both are read on the device; offsets out of range are clamped (nothing outside the
+ * tensors is touched).  What a mask hides does not enter any result, whatever it holds
+ * (infinities and NaN too).  A query that sees nothing has o = 0, lse = -infinity and
+ * no part in any gradient; so has one whose every score is -infinity.
+ *
+ * bucket(n), of n = p - j: the first half of the buckets is of one distance each, the
+ * others grow in the logarithm up to max_distance, from which on all is the last
+ * bucket.  Causal: of max(n, 0), all buckets.  Not causal: of |n| among the first half
+ * of the buckets where n >= 0, else among the second half.  With N buckets (of a side)
+ * and E = N / 2, distance d >= E is in bucket
+ *   E + floor((N - E) log(d / E) / log(max_distance / E)), at most N - 1,
+ * in exact arithmetic: pblock_score_attn_borders gives the first distance of each
+ * bucket (of a side; a bucket that no distance falls into has that of the next).
+ *
+ * Element (b, t, head, e) of a tensor is at ptr[(b*seq + t)*ld + head*head_dim + e],
+ * in cfg->dtype, 16-byte aligned, ld in elements (>= its heads*head_dim, a multiple of
+ * 16 bytes, < 2^24): q, o, d_o, dq with heads and seq_q; k, v, dk, dv with kv_heads and
+ * seq_k.  lse [batch, heads, seq_q] fp32; slopes [heads], table and dtable [buckets,
+ * heads] fp32.
+ *
+ * The backward gives the gradients of sum(o d_o): dq, dk, dv (dk and dv summed over the
+ * heads that share a key head) and, when dtable is not NULL, dtable (fp32); all are
+ * overwritten.  The softmax's row term is formed from o as it is kept for dq and dk, and
+ * from unrounded values for dtable.
+ *
+ * ws, 256-byte aligned, pblock_score_attn_workspace_bytes(cfg, mode): the PB_ATTN_WS_*
+ * modes.  PB_ATTN_WS_FORWARD is optional as for pblock_swattn_forward (less runs
+ * unsplit, the same result up to fp32 rounding), PB_ATTN_WS_BACKWARD_MIN is needed,
+ * PB_ATTN_WS_BACKWARD for full speed.  Nothing in it outlives the call; calls that may
+ * overlap (two captured graphs too) need one each.  Outputs may share no memory with any
+ * other tensor of the call (refused).  Results do not depend on timing (fixed order, no
+ * atomics between waves).
+ *
+ * Errors: PB_ERR_INVALID_ARG for a bad config, pointer or ld, PB_ERR_UNSUPPORTED for
+ * sizes past the kernels' (batch*seq_k and batch*seq_q*heads < 2^31), PB_ERR_WORKSPACE
+ * for a small ws. */
+#define PB_SCORE_MAX_BUCKETS 64
+typedef struct {
+  int batch;         /* >= 1                                                  */
+  int seq_q, seq_k;  /* 1 <= seq_q <= seq_k                                   */
+  int heads;         /* a multiple of kv_heads                                */
+  int kv_heads;      /* >= 1                                                  */
+  int head_dim;      /* 64, 96 or 128                                         */
+  int causal;        /* 0 or 1                                                */
+  int window;        /* >= 1                                                  */
+  float scale;       /* > 0, finite                                           */
+  float cap;         /* 0, or > 0 and finite                                  */
+  int buckets;       /* 0 without a table; else 2 .. 64, or even, 4 .. 64,
+                        when not causal                                       */
+  int max_distance;  /* > half the buckets (of a side), <= 2^20               */
+  pb_dtype dtype;
+} pb_score_attn_config;
+/* What enters the scores beside q and k, in device memory; NULL where there is none.
+ * At most one of slopes and table, which goes with cfg->buckets. */
+typedef struct {
+  const int32_t* docs;    /* [n_docs + 1]                                     */
+  int n_docs;             /* >= 0                                             */
+  const int32_t* prefix;  /* [n_docs], or [batch] without docs                */
+  const float* slopes;    /* [heads]                                          */
+  const float* table;     /* [buckets, heads]                                 */
+} pb_score_terms;
+/* first: an entry for each bucket (of a side, when not causal).  Host only. */
+pb_status pblock_score_attn_borders(const pb_score_attn_config* cfg, int* first);
+size_t pblock_score_attn_workspace_bytes(const pb_score_attn_config* cfg, int mode);
+/* terms may be NULL (none). */
+pb_status pblock_score_attn_forward(const pb_score_attn_config* cfg,
+                                    const pb_score_terms* terms, const void* q,
+                                    size_t ld_q, const void* k, const void* v,
+                                    size_t ld_kv, void* o, size_t ld_o, float* lse,
+                                    void* ws, size_t ws_bytes, hipStream_t stream);
+pb_status pblock_score_attn_backward(const pb_score_attn_config* cfg,
+                                     const pb_score_terms* terms, const void* q,
+                                     size_t ld_q, const void* k, const void* v,
+                                     size_t ld_kv, const void* o, size_t ld_o,
+                                     const void* d_o, size_t ld_do, const float* lse,
+                                     void* dq, size_t ld_dq, void* dk, void* dv,
+                                     size_t ld_dkv, float* dtable, void* ws,
+                                     size_t ws_bytes, hipStream_t stream);
+
 /* ------------------------------------------------------------- Muon step
  * An optimizer step that treats each weight as a matrix (Jordan et al. 2024), next
  * to pblock_lamb_step: the momentum's update, made nearly orthogonal by `steps`
@@ -802,6 +905,70 @@ size_t pblock_orthogonalize_workspace_bytes(int n_tensors,
 pb_status pblock_orthogonalize(int n_tensors, const pb_ortho_tensor* tensors,
                                pb_dtype dtype, int steps, float eps, void* ws,
                                size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------ AdamW step
+ * One step of Adam with decoupled weight decay (Loshchilov and Hutter 2019) over many
+ * tensors at once, next to pblock_lamb_step and pblock_muon_step (whose matrices leave
+ * the biases, norm gains and bias tables to a step like this one).  Per element, with
+ * t = cfg->step:
+ *
+ *   g = grad_scale grad
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *   w = w (1 - lr weight_decay) - lr (m c1) / (sqrt(v c2) + eps)
+ *       c1 = 1 / (1 - beta1^t), c2 = 1 / (1 - beta2^t) (1 and 1 without bias_correction)
+ *
+ * in fp32, each operation rounded by itself.  param and grad are fp32, param updated in
+ * place; param_copy, when not NULL, receives the updated weights in copy_dtype (bf16:
+ * round to nearest even).  state:
+ *
+ *   PB_ADAMW_F32   exp_avg is m and exp_avg_sq v, fp32.
+ *   PB_ADAMW_E4M3  exp_avg holds m and exp_avg_sq sqrt(v) as OCP e4m3 codes, one byte
+ *       an element, with fp32 scales for each PB_ADAMW_BLOCK elements (the last block may
+ *       be short): value = code scale.  scale = max(largest magnitude / 448, 2^-126) of
+ *       the block's updated values; a code is one of the two neighbours of the quotient,
+ *       the upper as often as it is near (a moving average that moves by less than half
+ *       a code's step would stand still under rounding to nearest).  sqrt(v) above 0
+ *       keeps a code above 0.  Which one is taken follows from 16 bits of a hash of
+ *       (seed, number of the element), the upper half of 32 for m and the lower for
+ *       sqrt(v): the same seed gives the same codes, so give each tensor and step its
+ *       own.  The step itself uses the updated values before they are rounded.  All
+ *       zeros (codes and scales) are states of zero.  A value that is not finite makes
+ *       its block's scale infinite or NaN, and the block's states with it.
+ *
+ * A captured step replays with the lr, step and seeds that it was captured with.
+ * Pointers are aligned to their element.  numel may be 0 (nothing is touched).  No
+ * array that is written may share memory with another array of the call (refused).
+ * Any number of tensors from 1 to PB_ADAMW_MAX_TENSORS, 48 in a launch; results do not
+ * depend on how tensors are divided over calls.  No workspace.
+ * Errors: PB_ERR_INVALID_ARG for a bad config, pointer or decay, PB_ERR_UNSUPPORTED for
+ * a tensor of 2^34 elements or more. */
+#define PB_ADAMW_MAX_TENSORS 1024
+#define PB_ADAMW_BLOCK 256
+typedef enum { PB_ADAMW_F32 = 0, PB_ADAMW_E4M3 = 1 } pb_adamw_state;
+typedef struct {
+  float lr;            /* finite                                              */
+  float beta1, beta2;  /* 0 <= beta < 1                                       */
+  float eps;           /* > 0, finite                                         */
+  float grad_scale;    /* finite                                              */
+  int step;            /* t >= 1                                              */
+  int bias_correction; /* 0 or 1                                              */
+  int state;           /* pb_adamw_state                                      */
+} pb_adamw_config;
+typedef struct {
+  float* param;        /* [numel] fp32                                        */
+  const float* grad;   /* [numel] fp32                                        */
+  void* exp_avg;       /* [numel] fp32, or e4m3 codes                         */
+  void* exp_avg_sq;    /* [numel] fp32, or e4m3 codes of the root             */
+  float* avg_scale;    /* [ceil(numel / PB_ADAMW_BLOCK)], PB_ADAMW_E4M3 only  */
+  float* sq_scale;     /* the same                                            */
+  void* param_copy;    /* NULL or [numel] in copy_dtype                       */
+  size_t numel;
+  uint64_t seed;       /* of the codes' rounding, PB_ADAMW_E4M3 only          */
+  float weight_decay;  /* >= 0, finite                                        */
+} pb_adamw_tensor;
+pb_status pblock_adamw_step(const pb_adamw_config* cfg, int n_tensors,
+                            const pb_adamw_tensor* tensors, pb_dtype copy_dtype,
+                            hipStream_t stream);
 
 /* Human-readable name of a status, and a description of the most recent
  * failed check on the calling thread ("" if none). */

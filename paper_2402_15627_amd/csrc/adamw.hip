@@ -1,0 +1,223 @@
+// One AdamW step over many fp32 tensors at once, states in 32 bits or in 8.
+//
+//   g = grad_scale grad,  m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2
+//   w = w (1 - lr decay) - lr (m c1) / (sqrt(v c2) + eps)
+//
+// Bound by HBM: each element of w, g and the states is read once and written
+// once (30 bytes with a bf16 copy of w, 18 with states of 8 bits), so the
+// arithmetic is free as long as it stays under about a hundred instructions an
+// element.  A launch takes up to kAdamMax tensors, cut into chunks of 1024
+// elements, a workgroup each; a thread has four elements, a wave the 256 that
+// share the scales of an 8-bit state.
+//
+// Every operation is rounded by itself (no contraction into fused products): a
+// value that decides an 8-bit code is then the one that elementary operations
+// give, and codes do not depend on how a compiler groups them.
+#include "common.h"
+#include "kernels.h"
+
+namespace pb {
+namespace {
+
+// Tensors need the alignment of their elements only: gfx950 loads and stores
+// vectors at any address.
+typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32_a1 __attribute__((aligned(1)));
+
+PB_DEV f32x4 load_stream(const float* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const f32x4_a4*>(p));
+}
+PB_DEV void store_stream(float* p, const f32x4& v) {
+  __builtin_nontemporal_store((f32x4_a4)v, reinterpret_cast<f32x4_a4*>(p));
+}
+
+// 32 random bits of element e: two rounds of shift and product.
+PB_DEV uint32_t random_bits(uint64_t seed, uint64_t e) {
+  uint32_t x = (uint32_t)e * 0x9E3779B1u + (uint32_t)seed;
+  x = (x ^ (x >> 16)) * 0x6A09E667u;
+  x += (uint32_t)(e >> 32) * 0x9E3779B1u + (uint32_t)(seed >> 32);
+  x = (x ^ (x >> 15)) * 0xBB67AE85u;
+  return x ^ (x >> 16);
+}
+
+// Largest of the wave's 64 unsigned words, in every lane.
+PB_DEV uint32_t wave_umax(uint32_t v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
+  return v;
+}
+
+// e4m3 code of |y| <= 448 rounded up or down as `rnd` (16 bits) says: to a
+// neighbour as often as y is near it.  Bits of the fp32 value below the code's
+// last place meet the random ones in an integer sum; below 2^-6, where codes
+// are multiples of 2^-9, the value itself takes the place of its bits.
+PB_DEV uint32_t code_e4m3(float a, uint32_t rnd) {
+  const uint32_t bits = a < 0x1p-6f ? (uint32_t)(a * 0x1p29f)
+                                    : __float_as_uint(a) - (120u << 23);
+  return min((bits + (rnd << 4)) >> 20, 0x7eu);
+}
+
+// Four elements' updated state x (lane's part of its wave's 256) as codes; their
+// scale is the largest magnitude over 448, at least 2^-126.  A value that is not
+// finite makes the scale so (magnitudes are compared as words, where NaN is above
+// all).  KEEP (x >= 0): what is above zero keeps a code above zero.
+template <bool KEEP>
+PB_DEV uint32_t quantise(const float (&x)[4], const uint32_t (&rnd)[4], float& scale) {
+#pragma clang fp contract(off)
+  uint32_t top = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) top = max(top, __float_as_uint(fabsf(x[k])));
+  const float s = __uint_as_float(wave_umax(top)) / 448.0f;
+  scale = s < 0x1p-126f ? 0x1p-126f : s;
+  const float inv = 1.0f / scale;
+  uint32_t word = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float y = x[k] * inv;
+    uint32_t c = code_e4m3(fabsf(y), rnd[k]);
+    if (KEEP) c = c == 0 && x[k] > 0.f ? 1u : c;
+    else c |= (__float_as_uint(y) >> 24) & 0x80u;
+    word |= c << (8 * k);
+  }
+  return word;
+}
+PB_DEV void dequantise(uint32_t word, float scale, float (&x)[4]) {
+#pragma clang fp contract(off)
+  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(word, false);
+  const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(word, true);
+  x[0] = lo[0] * scale, x[1] = lo[1] * scale, x[2] = hi[0] * scale, x[3] = hi[1] * scale;
+}
+
+PB_DEV void update(const AdamScalars& c, float decay, float grad, float& w, float& m, float& v) {
+#pragma clang fp contract(off)
+  const float g = grad * c.grad_scale;
+  m = m * c.beta1 + g * c.rest1;
+  v = v * c.beta2 + (g * g) * c.rest2;
+  const float u = (m * c.c1) / (__builtin_sqrtf(v * c.c2) + c.eps);
+  w = w * decay - u * c.lr;
+}
+
+template <typename CT>
+PB_DEV void store_copy(void* copy, long long e, int n, const f32x4& w) {
+  CT* p = (CT*)copy + e;
+  if (n == 4) {
+    if constexpr (sizeof(CT) == 2)
+      __builtin_nontemporal_store((u32x2_a2)u32x2{pack_bf2(w[0], w[1]), pack_bf2(w[2], w[3])},
+                                  reinterpret_cast<u32x2_a2*>(p));
+    else
+      store_stream((float*)p, w);
+  } else {
+    for (int k = 0; k < n; ++k) p[k] = (CT)w[k];
+  }
+}
+// n of four values (the tensor's end may be in between)
+PB_DEV f32x4 load_some(const float* p, int n) {
+  if (n == 4) return load_stream(p);
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+    if (k < n) v[k] = p[k];
+  return v;
+}
+PB_DEV void store_some(float* p, int n, const f32x4& v) {
+  if (n == 4) return store_stream(p, v);
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+    if (k < n) p[k] = v[k];
+}
+PB_DEV uint32_t load_codes(const uint8_t* p, int n) {
+  if (n == 4) return *reinterpret_cast<const u32_a1*>(p);
+  uint32_t v = 0;
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+    if (k < n) v |= (uint32_t)p[k] << (8 * k);
+  return v;
+}
+PB_DEV void store_codes(uint8_t* p, int n, uint32_t v) {
+  if (n == 4) {
+    *reinterpret_cast<u32_a1*>(p) = v;
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+    if (k < n) p[k] = (uint8_t)(v >> (8 * k));
+}
+
+// The tensor of a chunk: the last whose chunks begin at or before it.
+PB_DEV int tensor_of(const AdamTable& t, int chunk) {
+  int lo = 0, hi = t.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (chunk >= t.chunk0[mid]) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+template <bool E4M3, typename CT>
+__global__ __launch_bounds__(256) void adamw_kernel(AdamTable t, AdamScalars c) {
+  const int chunk = blockIdx.x, i = tensor_of(t, chunk);
+  const long long e = (long long)(chunk - t.chunk0[i]) * kAdamChunk + 4 * threadIdx.x;
+  const int n = (int)max(0LL, min(4LL, t.numel[i] - e));
+  // (a wave stays whole for its scales, whichever lanes have elements)
+  if (!E4M3 && n == 0) return;
+  f32x4 w = load_some(t.w[i] + e, n);
+  const f32x4 g = load_some(t.g[i] + e, n);
+  if constexpr (!E4M3) {
+    f32x4 m = load_some((const float*)t.m[i] + e, n), v = load_some((const float*)t.v[i] + e, n);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float wk = w[k], mk = m[k], vk = v[k];
+      update(c, t.decay[i], g[k], wk, mk, vk);
+      w[k] = wk, m[k] = mk, v[k] = vk;
+    }
+    store_some((float*)t.m[i] + e, n, m);
+    store_some((float*)t.v[i] + e, n, v);
+  } else {
+    const long long block = e / kAdamBlock;
+    const bool any = block * kAdamBlock < t.numel[i];  // wave-uniform
+    if (!any) return;
+    float m[4], r[4];
+    dequantise(load_codes((const uint8_t*)t.m[i] + e, n), t.m_scale[i][block], m);
+    dequantise(load_codes((const uint8_t*)t.v[i] + e, n), t.v_scale[i][block], r);
+    uint32_t rm[4], rr[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+#pragma clang fp contract(off)
+      float wk = w[k], vk = r[k] * r[k];
+      update(c, t.decay[i], g[k], wk, m[k], vk);
+      w[k] = wk;
+      r[k] = __builtin_sqrtf(vk);
+      const uint32_t bits = random_bits(t.seed[i], (uint64_t)(e + k));
+      rm[k] = bits >> 16, rr[k] = bits & 0xffffu;
+      if (k >= n) m[k] = r[k] = 0.f;
+    }
+    float ms, rs;
+    store_codes((uint8_t*)t.m[i] + e, n, quantise<false>(m, rm, ms));
+    store_codes((uint8_t*)t.v[i] + e, n, quantise<true>(r, rr, rs));
+    if ((threadIdx.x & 63) == 0) {
+      t.m_scale[i][block] = ms;
+      t.v_scale[i][block] = rs;
+    }
+  }
+  if (n == 0) return;
+  store_some(t.w[i] + e, n, w);
+  if (t.copy[i]) store_copy<CT>(t.copy[i], e, n, w);
+}
+
+}  // namespace
+
+void launch_adamw(const AdamTable& t, const AdamScalars& c, bool e4m3, Dt copy_dt, hipStream_t s) {
+  static_assert(kAdamChunk == 1024 && kAdamBlock == 256, "four elements a thread, a wave a block");
+  const int n = t.chunk0[t.n];
+  if (e4m3) {
+    if (copy_dt == Dt::BF16) adamw_kernel<true, bf16><<<n, 256, 0, s>>>(t, c);
+    else adamw_kernel<true, float><<<n, 256, 0, s>>>(t, c);
+  } else {
+    if (copy_dt == Dt::BF16) adamw_kernel<false, bf16><<<n, 256, 0, s>>>(t, c);
+    else adamw_kernel<false, float><<<n, 256, 0, s>>>(t, c);
+  }
+}
+
+}  // namespace pb

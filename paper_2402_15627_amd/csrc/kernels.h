@@ -73,6 +73,34 @@ int lamb_padded_chunks(long long numel);  // rounded up to a multiple of kLambGr
 void launch_lamb(const LambTable& t, const LambScalars& sc, Dt copy_dt, float2* partial,
                  double2* group, float* ratio, float* ratio_out, hipStream_t s);
 
+// ------------------------------------------------------------- AdamW step
+// Up to kAdamMax tensors of a launch (their descriptors fill the 4 KB of a kernel's
+// arguments), each cut into chunks of kAdamChunk elements, a workgroup each, from
+// chunk0[i] on.  States m and v: fp32, or e4m3 codes of m and of sqrt(v) with a scale
+// for each kAdamBlock elements.
+constexpr int kAdamMax = 48;
+constexpr int kAdamChunk = 1024, kAdamBlock = 256;
+struct AdamTable {
+  float* w[kAdamMax];
+  const float* g[kAdamMax];
+  void* m[kAdamMax];
+  void* v[kAdamMax];
+  float* m_scale[kAdamMax];  // 8-bit states only
+  float* v_scale[kAdamMax];
+  void* copy[kAdamMax];      // nullptr: no copy of this tensor
+  long long numel[kAdamMax];
+  uint64_t seed[kAdamMax];   // of the codes' rounding
+  float decay[kAdamMax];     // 1 - lr weight_decay
+  int chunk0[kAdamMax + 1];
+  int n;
+};
+static_assert(sizeof(AdamTable) <= 4000, "kernel arguments");
+struct AdamScalars {
+  float lr, beta1, rest1, beta2, rest2, eps, grad_scale;  // rest: 1 - beta
+  float c1, c2;  // 1 / (1 - beta^t), or 1 without bias correction
+};
+void launch_adamw(const AdamTable& t, const AdamScalars& c, bool e4m3, Dt copy_dt, hipStream_t s);
+
 // ------------------------------------------------------- rotary positions
 // Up to kRopeMaxTensors tensors of `tokens` rows, each of its own number of heads of
 // head_dim elements, head h of token t at in + t ld_in + h head_dim.  turns[i] is
@@ -411,5 +439,11 @@ void launch_attn_backward_f32(const AttnShape& a, const float* q, const float* k
                               int ld_qkv, const float* o, int ld_o, const float* d_o, int ld_do,
                               const float* lse, float* delta, float* dq, float* dk, float* dv,
                               int ld_d, hipStream_t s);
+
+// ----------------------------------- attention with terms in its scores
+// (ScoreArgs: score_attn.h)
+struct ScoreArgs;
+void launch_score_forward(Dt dt, int head_dim, const ScoreArgs& a, hipStream_t s);
+void launch_score_backward(Dt dt, int head_dim, const ScoreArgs& a, hipStream_t s);
 
 }  // namespace pb

@@ -11,7 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_double, c_float, c_int, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, c_double, c_float, c_int, c_int64, c_size_t, c_uint64, c_void_p
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libpblock.so")
@@ -48,11 +48,17 @@ EXPORTS = (
     "pblock_rmsnorm_forward", "pblock_rmsnorm_workspace_bytes", "pblock_rmsnorm_backward",
     "pblock_muon_workspace_bytes", "pblock_muon_step",
     "pblock_orthogonalize_workspace_bytes", "pblock_orthogonalize",
+    "pblock_adamw_step",
+    "pblock_score_attn_borders", "pblock_score_attn_workspace_bytes",
+    "pblock_score_attn_forward", "pblock_score_attn_backward",
 )
 NOALLOC_SCRATCH_BYTES = 32 << 20  # PB_NOALLOC_SCRATCH_BYTES
 LAMB_MAX_TENSORS = 16
 ROPE_MAX_TENSORS = 4
 MUON_MAX_TENSORS = 16
+ADAMW_MAX_TENSORS = 1024
+ADAMW_BLOCK = 256  # PB_ADAMW_BLOCK: elements of an 8-bit state that share a scale
+ADAMW_F32, ADAMW_E4M3 = 0, 1  # pb_adamw_state
 ROPE_SCALING = ("plain", "linear", "by_parts")  # pb_rope_scaling
 
 # pb_step order of include/pblock.h
@@ -115,6 +121,20 @@ class RmsnormConfig(ctypes.Structure):
                 ("dtype", c_int)]
 
 
+class ScoreAttnConfig(ctypes.Structure):
+    """pb_score_attn_config."""
+    _fields_ = [("batch", c_int), ("seq_q", c_int), ("seq_k", c_int), ("heads", c_int),
+                ("kv_heads", c_int), ("head_dim", c_int), ("causal", c_int), ("window", c_int),
+                ("scale", c_float), ("cap", c_float), ("buckets", c_int), ("max_distance", c_int),
+                ("dtype", c_int)]
+
+
+class ScoreTerms(ctypes.Structure):
+    """pb_score_terms (device addresses as integers)."""
+    _fields_ = [("docs", c_void_p), ("n_docs", c_int), ("prefix", c_void_p),
+                ("slopes", c_void_p), ("table", c_void_p)]
+
+
 class MuonConfig(ctypes.Structure):
     """pb_muon_config."""
     _fields_ = [("lr", c_float), ("momentum", c_float), ("grad_scale", c_float), ("eps", c_float),
@@ -132,6 +152,21 @@ class OrthoTensor(ctypes.Structure):
     """pb_ortho_tensor (device addresses as integers)."""
     _fields_ = [("in_", c_void_p), ("out", c_void_p), ("rows", c_int), ("cols", c_int),
                 ("ld_in", c_size_t), ("ld_out", c_size_t)]
+
+
+class AdamwConfig(ctypes.Structure):
+    """pb_adamw_config."""
+    _fields_ = [("lr", c_float), ("beta1", c_float), ("beta2", c_float), ("eps", c_float),
+                ("grad_scale", c_float), ("step", c_int), ("bias_correction", c_int),
+                ("state", c_int)]
+
+
+class AdamwTensor(ctypes.Structure):
+    """pb_adamw_tensor (device addresses as integers)."""
+    _fields_ = [("param", c_void_p), ("grad", c_void_p), ("exp_avg", c_void_p),
+                ("exp_avg_sq", c_void_p), ("avg_scale", c_void_p), ("sq_scale", c_void_p),
+                ("param_copy", c_void_p), ("numel", c_size_t), ("seed", c_uint64),
+                ("weight_decay", c_float)]
 
 
 class PblockError(RuntimeError):
@@ -223,6 +258,16 @@ def load_library(path: str = LIB_PATH):
         "pblock_orthogonalize_workspace_bytes": (c_size_t, [c_int, POINTER(OrthoTensor), c_int]),
         "pblock_orthogonalize": (c_int, [c_int, POINTER(OrthoTensor), c_int, c_int, c_float, P,
                                          c_size_t, P]),
+        "pblock_score_attn_borders": (c_int, [POINTER(ScoreAttnConfig), POINTER(c_int)]),
+        "pblock_score_attn_workspace_bytes": (c_size_t, [POINTER(ScoreAttnConfig), c_int]),
+        "pblock_score_attn_forward": (c_int, [POINTER(ScoreAttnConfig), POINTER(ScoreTerms), P,
+                                              c_size_t, P, P, c_size_t, P, c_size_t, P, P,
+                                              c_size_t, P]),
+        "pblock_score_attn_backward": (c_int, [POINTER(ScoreAttnConfig), POINTER(ScoreTerms), P,
+                                               c_size_t, P, P, c_size_t, P, c_size_t, P, c_size_t,
+                                               P, P, c_size_t, P, P, c_size_t, P, P, c_size_t, P]),
+        "pblock_adamw_step": (c_int, [POINTER(AdamwConfig), c_int, POINTER(AdamwTensor), c_int,
+                                      P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -739,6 +784,112 @@ def pblock_rmsnorm_backward(cfg: RmsnormConfig, s, gamma, rstd, dy, dx, dgamma, 
     call.run(load_library().pblock_rmsnorm_backward, args, stream)
 
 
+def score_attn_config(batch, seq_q, seq_k, heads, kv_heads, head_dim, causal=True, window=None,
+                      scale=None, cap=0.0, buckets=0, max_distance=0,
+                      dtype="bf16") -> ScoreAttnConfig:
+    """window: no limit by default; scale: 1 / sqrt(head_dim) by default; buckets and
+    max_distance go with a table."""
+    return ScoreAttnConfig(batch, seq_q, seq_k, heads, kv_heads, head_dim, int(bool(causal)),
+                           seq_k if window is None else window,
+                           head_dim ** -0.5 if scale is None else scale, cap, buckets,
+                           max_distance, _dtype_of(dtype))
+
+
+def pblock_score_attn_borders(cfg: ScoreAttnConfig) -> list:
+    """The first distance of each bucket (of a side, when not causal)."""
+    arr = (c_int * max(cfg.buckets, 1))()
+    _check(load_library().pblock_score_attn_borders(ctypes.byref(cfg), arr))
+    return list(arr)[:cfg.buckets if cfg.causal else cfg.buckets // 2]
+
+
+def pblock_score_attn_workspace_bytes(cfg: ScoreAttnConfig, mode: int) -> int:
+    """mode: ATTN_WS_FORWARD, ATTN_WS_BACKWARD_MIN or ATTN_WS_BACKWARD."""
+    return load_library().pblock_score_attn_workspace_bytes(ctypes.byref(cfg), int(mode))
+
+
+class _ScoreCall(_Call):
+    """A call of attention with terms in its scores: its tensors' sizes."""
+    __slots__ = ("cfg", "act")
+
+    def __init__(self, cfg):
+        super().__init__()
+        self.cfg, self.act = cfg, _torch_dtype(cfg.dtype)
+
+    def rows(self, name, t, kv):
+        """Address and leading dimension of a matrix [batch*seq, heads*head_dim]."""
+        c = self.cfg
+        shape = (c.batch * (c.seq_k if kv else c.seq_q),
+                 (c.kv_heads if kv else c.heads) * c.head_dim)
+        if t.dtype != self.act:
+            raise ValueError(f"{name} is {t.dtype}, not {self.act}")
+        if t.shape != shape:
+            raise ValueError(f"{name} is {tuple(t.shape)}, not {shape}")
+        ld = _rows(name, t)
+        self.on(name, t)
+        return t.data_ptr(), ld
+
+    def terms(self, docs, prefix, slopes, table):
+        import torch
+        c, i32, f32 = self.cfg, torch.int32, torch.float32
+        if docs is not None and docs.numel() < 1:
+            raise ValueError("docs is empty: it holds one offset more than there are documents")
+        n = c.batch if docs is None else docs.numel() - 1
+        return ScoreTerms(self.ptr("docs", docs, i32), n, self.ptr("prefix", prefix, i32, n),
+                          self.ptr("slopes", slopes, f32, c.heads),
+                          self.ptr("table", table, f32, c.buckets * c.heads))
+
+
+def _same_ld(a, ld_a, b, ld_b):
+    if ld_a != ld_b:
+        raise ValueError(f"{a} and {b} have different strides ({ld_a} and {ld_b})")
+
+
+def pblock_score_attn_forward(cfg: ScoreAttnConfig, q, k, v, o, lse, docs=None, prefix=None,
+                              slopes=None, table=None, ws=None, stream=None):
+    """q, o: [batch*seq_q, heads*head_dim]; k, v: [batch*seq_k, kv_heads*head_dim], of one
+    stride (columns of a wider matrix, say); lse: fp32 [batch, heads, seq_q].
+    docs: int32 offsets of the documents, one more than there are; prefix: int32 per
+    document (or batch row); slopes: fp32 [heads]; table: fp32 [buckets, heads]."""
+    import torch
+    call = _ScoreCall(cfg)
+    qp, ld_q = call.rows("q", q, False)
+    kp, ld_k = call.rows("k", k, True)
+    vp, ld_v = call.rows("v", v, True)
+    _same_ld("k", ld_k, "v", ld_v)
+    op, ld_o = call.rows("o", o, False)
+    lp = call.ptr("lse", lse, torch.float32, cfg.batch * cfg.heads * cfg.seq_q)
+    terms = call.terms(docs, prefix, slopes, table)
+    call.run(load_library().pblock_score_attn_forward,
+             (ctypes.byref(cfg), ctypes.byref(terms), qp, ld_q, kp, vp, ld_k, op, ld_o, lp,
+              call.ptr("ws", ws), _nbytes(ws)), stream)
+
+
+def pblock_score_attn_backward(cfg: ScoreAttnConfig, q, k, v, o, d_o, lse, dq, dk, dv, ws,
+                               docs=None, prefix=None, slopes=None, table=None, dtable=None,
+                               stream=None):
+    """The gradients of sum(o d_o): dq like q, dk and dv like k (of one stride), dtable
+    like table (or None)."""
+    import torch
+    call = _ScoreCall(cfg)
+    qp, ld_q = call.rows("q", q, False)
+    kp, ld_k = call.rows("k", k, True)
+    vp, ld_v = call.rows("v", v, True)
+    _same_ld("k", ld_k, "v", ld_v)
+    op, ld_o = call.rows("o", o, False)
+    gp, ld_do = call.rows("d_o", d_o, False)
+    lp = call.ptr("lse", lse, torch.float32, cfg.batch * cfg.heads * cfg.seq_q)
+    dqp, ld_dq = call.rows("dq", dq, False)
+    dkp, ld_dk = call.rows("dk", dk, True)
+    dvp, ld_dv = call.rows("dv", dv, True)
+    _same_ld("dk", ld_dk, "dv", ld_dv)
+    terms = call.terms(docs, prefix, slopes, table)
+    call.run(load_library().pblock_score_attn_backward,
+             (ctypes.byref(cfg), ctypes.byref(terms), qp, ld_q, kp, vp, ld_k, op, ld_o, gp, ld_do,
+              lp, dqp, ld_dq, dkp, dvp, ld_dk,
+              call.ptr("dtable", dtable, torch.float32, cfg.buckets * cfg.heads),
+              call.ptr("ws", ws), _nbytes(ws)), stream)
+
+
 def muon_config(lr, momentum=0.95, nesterov=True, steps=5, eps=1e-7, grad_scale=1.0,
                 products="f32") -> MuonConfig:
     """products: "f32" (22 bits of each factor) or "bf16" (11 bits: 0.41 of the
@@ -832,6 +983,86 @@ def pblock_orthogonalize(tensors, dtype, ws, steps=5, eps=1e-7, stream=None):
     call.run(load_library().pblock_orthogonalize,
              (len(tensors), (OrthoTensor * len(tensors))(*tensors), code, int(steps), eps,
               call.ptr("ws", ws), _nbytes(ws)), stream)
+
+
+def adamw_config(lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, bias_correction=True,
+                 grad_scale=1.0) -> AdamwConfig:
+    """The state's type is that of the tensors of the call."""
+    return AdamwConfig(lr, beta1, beta2, eps, grad_scale, int(step), int(bool(bias_correction)),
+                       ADAMW_F32)
+
+
+def adamw_tensor(param, grad, exp_avg, exp_avg_sq, param_copy=None, weight_decay=0.0,
+                 avg_scale=None, sq_scale=None, seed=0) -> AdamwTensor:
+    """A pb_adamw_tensor from contiguous tensors. exp_avg and exp_avg_sq: fp32, or
+    float8_e4m3fn (or uint8) codes of m and of sqrt(v) with their fp32 scales and
+    the seed of their rounding."""
+    import torch
+    f32, n = torch.float32, param.numel()
+    e4m3 = exp_avg.dtype != f32
+    if e4m3 and (avg_scale is None or sq_scale is None):
+        raise ValueError("states of 8 bits need avg_scale and sq_scale")
+    if not e4m3 and (avg_scale is not None or sq_scale is not None):
+        raise ValueError("states of 32 bits have no scales")
+    state = (torch.float8_e4m3fn, torch.uint8) if e4m3 else (f32,)
+    scales = -(-n // ADAMW_BLOCK)
+    call, ptrs = _Call(), []
+    for name, t, types, numel in (
+            ("param", param, (f32,), n), ("grad", grad, (f32,), n), ("exp_avg", exp_avg, state, n),
+            ("exp_avg_sq", exp_avg_sq, state, n), ("avg_scale", avg_scale, (f32,), scales),
+            ("sq_scale", sq_scale, (f32,), scales),
+            ("param_copy", param_copy, (f32, torch.bfloat16), n)):
+        if t is not None and t.dtype not in types:
+            raise ValueError(f"{name} is {t.dtype}, not {types[0]}")
+        ptrs.append(call.ptr(name, t, None, numel))
+    r = AdamwTensor(*ptrs, n, int(seed) & 0xffffffffffffffff, weight_decay)
+    r.index, r.e4m3 = call.index, e4m3
+    r.copy_dtype = None if param_copy is None else param_copy.dtype
+    # (kept alive)
+    r.tensors = (param, grad, exp_avg, exp_avg_sq, avg_scale, sq_scale, param_copy)
+    return r
+
+
+class AdamwTensors:
+    """AdamwTensor of one device and one type of state, laid out once for many
+    steps. (seeds(...) gives each the seed of a new step.)"""
+
+    def __init__(self, tensors):
+        self.parts = list(tensors)
+        if not self.parts:
+            raise ValueError("no tensors")
+        first = self.parts[0]
+        for i, r in enumerate(self.parts):
+            if r.index != first.index:
+                raise ValueError(f"tensor {i} is on another device than the first "
+                                 f"({r.index} and {first.index})")
+            if r.e4m3 != first.e4m3:
+                raise ValueError(f"tensor {i} has states of another type than the first")
+        copies = {r.copy_dtype for r in self.parts if r.copy_dtype is not None}
+        if len(copies) > 1:
+            raise ValueError(f"copies of more than one type: {sorted(map(str, copies))}")
+        self.copy_dtype = copies.pop() if copies else None
+        self.index, self.e4m3 = first.index, first.e4m3
+        self.array = (AdamwTensor * len(self.parts))(*self.parts)
+
+    def seeds(self, seeds):
+        for r, seed in zip(self.array, seeds, strict=True):
+            r.seed = int(seed) & 0xffffffffffffffff
+
+
+def pblock_adamw_step(cfg: AdamwConfig, tensors, copy_dtype=PB_BF16, stream=None):
+    """tensors: an AdamwTensors, or a sequence of AdamwTensor; their copies are of
+    copy_dtype."""
+    if not isinstance(tensors, AdamwTensors):
+        tensors = AdamwTensors(tensors)
+    if tensors.copy_dtype not in (None, _torch_dtype(copy_dtype)):
+        raise ValueError(f"param_copy is {tensors.copy_dtype}, not {_torch_dtype(copy_dtype)}")
+    call = _Call()
+    call.index = tensors.index
+    c = AdamwConfig.from_buffer_copy(cfg)
+    c.state = ADAMW_E4M3 if tensors.e4m3 else ADAMW_F32
+    call.run(load_library().pblock_adamw_step,
+             (ctypes.byref(c), len(tensors.array), tensors.array, int(copy_dtype)), stream)
 
 
 def pblock_status_string(status: int) -> str:
