@@ -59,16 +59,16 @@ PB_DEV uint32_t code_e4m3(float a, uint32_t rnd) {
 }
 
 // Four elements' updated state x (lane's part of its wave's 256) as codes; their
-// scale is the largest magnitude over 448, at least 2^-126.  A value that is not
-// finite makes the scale so (magnitudes are compared as words, where NaN is above
-// all).  KEEP (x >= 0): what is above zero keeps a code above zero.
+// scale is the largest magnitude over 448 (its product with the rounded 1/448),
+// at least 2^-126.  A value that is not finite makes the scale so (magnitudes are
+// compared as words, where NaN is above all).  KEEP (x >= 0): what is above zero keeps a code above zero.
 template <bool KEEP>
 PB_DEV uint32_t quantise(const float (&x)[4], const uint32_t (&rnd)[4], float& scale) {
 #pragma clang fp contract(off)
   uint32_t top = 0;
 #pragma unroll
   for (int k = 0; k < 4; ++k) top = max(top, __float_as_uint(fabsf(x[k])));
-  const float s = __uint_as_float(wave_umax(top)) / 448.0f;
+  const float s = __uint_as_float(wave_umax(top)) * (1.0f / 448.0f);
   scale = s < 0x1p-126f ? 0x1p-126f : s;
   const float inv = 1.0f / scale;
   uint32_t word = 0;

@@ -443,6 +443,13 @@ void launch_attn_backward_f32(const AttnShape& a, const float* q, const float* k
 // ----------------------------------- attention with terms in its scores
 // (ScoreArgs: score_attn.h)
 struct ScoreArgs;
+struct ScorePlan;
+// How the bf16 forward is split over workgroups, and the bytes of its partial results (0:
+// not split).
+ScorePlan score_fwd_plan(int head_dim, const ScoreArgs& a);
+size_t score_fwd_part_bytes(int head_dim, const ScoreArgs& a, const ScorePlan& p);
+void launch_score_forward_bf16(int head_dim, const ScoreArgs& a, const ScorePlan& p, void* part,
+                               hipStream_t s);
 void launch_score_forward(Dt dt, int head_dim, const ScoreArgs& a, hipStream_t s);
 void launch_score_backward(Dt dt, int head_dim, const ScoreArgs& a, hipStream_t s);
 

@@ -24,8 +24,8 @@ pb_status check_config(const pb_score_attn_config* c) {
   if (c->window < 1) return fail(PB_ERR_INVALID_ARG, "window=%d must be >= 1", c->window);
   if (!(c->scale > 0.f) || !std::isfinite(c->scale))
     return fail(PB_ERR_INVALID_ARG, "scale must be finite and > 0");
-  if (!(c->cap >= 0.f) || !std::isfinite(c->cap))
-    return fail(PB_ERR_INVALID_ARG, "cap must be finite and >= 0");
+  if (c->cap != 0.f && !(c->cap >= c->scale / 32768.f && c->cap <= 0x1p100f))
+    return fail(PB_ERR_INVALID_ARG, "cap must be 0, or in scale / 2^15 .. 2^100");
   if (c->buckets != 0) {
     const int side = c->causal ? c->buckets : c->buckets / 2;
     if (c->buckets > PB_SCORE_MAX_BUCKETS || side < 2 || (!c->causal && c->buckets % 2))
@@ -119,6 +119,9 @@ size_t prefix_bytes(const pb_score_attn_config* c, const pb_score_terms* t) {
   return 4 * (size_t)(t->docs ? t->n_docs : c->batch);
 }
 
+const pb_score_terms kNoTerms{};
+constexpr int kMaxPack = 8;  // heads of a block of rows
+
 pb::ScoreArgs args_of(const pb_score_attn_config* c, const pb_score_terms* t) {
   pb::ScoreArgs a{};
   a.batch = c->batch, a.seq_q = c->seq_q, a.seq_k = c->seq_k;
@@ -129,10 +132,24 @@ pb::ScoreArgs args_of(const pb_score_attn_config* c, const pb_score_terms* t) {
   a.slopes = t->slopes, a.table = t->table;
   a.buckets = c->buckets, a.side = c->causal ? c->buckets : c->buckets / 2;
   if (c->buckets) borders_of(c, a.first);
+  a.pack = 1;
+  for (int n = 2; n <= kMaxPack; ++n)
+    if (a.group % n == 0) a.pack = n;
   return a;
 }
-
-const pb_score_terms kNoTerms{};
+// What a call's plans depend on beside the config: the workspace's sizes are for any
+// terms.
+size_t fwd_bytes(const pb_score_attn_config* c) {
+  if (c->dtype != PB_BF16) return 0;
+  size_t most = 0;
+  for (int prefix = 0; prefix < 2; ++prefix) {
+    pb::ScoreArgs a = args_of(c, &kNoTerms);
+    static const int some = 0;
+    a.prefix = prefix ? &some : nullptr;
+    most = std::max(most, pb::score_fwd_part_bytes(c->head_dim, a, pb::score_fwd_plan(c->head_dim, a)));
+  }
+  return align256(most);
+}
 
 }  // namespace
 
@@ -148,7 +165,7 @@ pb_status pblock_score_attn_borders(const pb_score_attn_config* cfg, int* first)
 
 size_t pblock_score_attn_workspace_bytes(const pb_score_attn_config* cfg, int mode) {
   if (check_config(cfg) != PB_OK) return 0;
-  if (mode == PB_ATTN_WS_FORWARD) return 0;
+  if (mode == PB_ATTN_WS_FORWARD) return fwd_bytes(cfg);
   return bias_bytes(cfg);
 }
 
@@ -180,7 +197,13 @@ pb_status pblock_score_attn_forward(const pb_score_attn_config* cfg, const pb_sc
   pb::ScoreArgs a = args_of(cfg, t);
   a.q = q, a.k = k, a.v = v, a.ld_q = (int)ld_q, a.ld_kv = (int)ld_kv;
   a.o = o, a.ld_o = (int)ld_o, a.lse = lse;
-  pb::launch_score_forward(dt_of(cfg->dtype), cfg->head_dim, a, stream);
+  if (cfg->dtype == PB_BF16) {
+    pb::ScorePlan p = pb::score_fwd_plan(cfg->head_dim, a);
+    if (!ws || ws_bytes < pb::score_fwd_part_bytes(cfg->head_dim, a, p)) p = {1 << 30, 1};
+    pb::launch_score_forward_bf16(cfg->head_dim, a, p, ws, stream);
+  } else {
+    pb::launch_score_forward(dt_of(cfg->dtype), cfg->head_dim, a, stream);
+  }
   return finish_launches();
 }
 

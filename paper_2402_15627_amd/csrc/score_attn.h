@@ -3,6 +3,8 @@
 // one row a wave.
 #pragma once
 
+#include <algorithm>
+
 #include "common.h"
 
 namespace pb {
@@ -30,7 +32,22 @@ struct ScoreArgs {
   int first[kScoreMaxBuckets];  // first distance of each bucket of a side
   float* dtable;
   float* bias_part;             // [batch * row blocks][heads][buckets]
+  int pack;                     // heads of one key head that a block of rows holds
 };
+
+// How a block's tiles are divided: `chunks` workgroups of at most `chunk` tiles each.
+struct ScorePlan {
+  int chunk, chunks;
+};
+// The most tiles (of `keys`) that a block of `rows` rows may visit, whatever the
+// documents.
+inline int score_most_tiles(const ScoreArgs& a, int rows, int keys) {
+  const long long all = (a.seq_k + keys - 1) / keys;
+  if (a.prefix) return (int)all;
+  const long long span = (rows + a.pack - 1) / a.pack + 1;
+  const long long reach = (long long)(a.causal ? 1 : 2) * a.window + span;
+  return (int)std::min(all, reach / keys + 2);
+}
 
 namespace score {
 

@@ -1,0 +1,230 @@
+// What the bf16 kernels of attention with terms in its scores share beside
+// score_attn.h: rows of several heads in a tile, the key tiles that a block of rows
+// visits, the cap on scores in base 2, the biases of a tile.
+#pragma once
+
+#include "attn_tiles.h"
+#include "score_attn.h"
+
+namespace pb {
+namespace {
+
+using score::Bounds;
+using score::bounds_of;
+using score::window_first;
+using score::window_last;
+
+// A block's rows are (position, head) pairs of the `pack` heads that share a key head
+// (a part of them where there are more than eight): row r is query r / pack of head
+// r mod pack.  Keys and values are then read once for all of them, and the gradients of
+// shared heads are sums within a workgroup.
+struct Packed {
+  int pack;       // heads of a block
+  uint32_t magic; // ceil(2^32 / pack): rows below 2^29 divide by a high product
+  PB_DEV explicit Packed(int n) : pack(n), magic((uint32_t)((0x100000000ull + n - 1) / n)) {}
+  PB_DEV int pos(int r) const { return pack == 1 ? r : (int)__umulhi((uint32_t)r, magic); }
+};
+
+PB_DEV int wave_imin(int v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+PB_DEV int wave_imax(int v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+
+// Keys of one row: first .. first + len - 1 by the window, pfirst .. pfirst + plen - 1 by
+// the prefix.
+struct RowKeys {
+  int first, len, pfirst, plen;
+  // bit k: whether key k0 + k is seen
+  static PB_DEV uint64_t below(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0 : (1ull << n) - 1; }
+  PB_DEV uint64_t bits(int k0) const {
+    return (below(first - k0 + len) & ~below(first - k0)) |
+           (below(pfirst - k0 + plen) & ~below(pfirst - k0));
+  }
+};
+PB_DEV RowKeys row_keys(const ScoreArgs& a, int b, int p) {
+  const Bounds d = bounds_of(a, b, p);
+  const int first = window_first(a, d, p);
+  return RowKeys{first, d.de > d.ds ? window_last(a, d, p) - first + 1 : 0, d.ds, d.pe - d.ds};
+}
+
+// The key tiles (of TL) that positions p0 .. p1 of a batch row visit: up to two runs,
+// the prefixes' and the windows', in ascending order.  lo .. hi: the keys that any of
+// them sees, and all between.
+struct KeyTiles {
+  int t0, n0, t1, n;  // tile i is t0 + i below n0, then t1 + i - n0; n in all
+  int lo, hi;
+  PB_DEV int tile(int i) const { return i < n0 ? t0 + i : t1 + i - n0; }
+};
+template <int TL>
+PB_DEV KeyTiles key_tiles(const ScoreArgs& a, int b, int p0, int p1, int lane) {
+  int w0 = 0x7fffffff, w1 = -1, x0 = 0x7fffffff, x1 = -1;
+  if (!a.docs && !a.prefix) {
+    const Bounds d{0, a.seq_k, 0};
+    w0 = window_first(a, d, p0), w1 = window_last(a, d, p1);
+  } else {
+    for (int p = p0 + lane; p <= p1; p += 64) {
+      const RowKeys k = row_keys(a, b, p);
+      if (k.len > 0) w0 = min(w0, k.first), w1 = max(w1, k.first + k.len - 1);
+      if (k.plen > 0) x0 = min(x0, k.pfirst), x1 = max(x1, k.pfirst + k.plen - 1);
+    }
+    w0 = wave_imin(w0), w1 = wave_imax(w1), x0 = wave_imin(x0), x1 = wave_imax(x1);
+  }
+  KeyTiles k{0, 0, 0, 0, min(w0, x0), max(w1, x1)};
+  int wa = w0 / TL, wb = w1 < 0 ? -1 : w1 / TL, xa = x0 / TL, xb = x1 < 0 ? -1 : x1 / TL;
+  if (wb < 0 || (xb >= 0 && xa < wa)) {  // the run that begins first comes first
+    const int ta = wa, tb = wb;
+    wa = xa, wb = xb, xa = ta, xb = tb;
+  }
+  if (wb < 0) return k;
+  k.t0 = wa;
+  if (xb < 0 || xa <= wb + 1) {
+    k.n0 = max(wb, xb) - wa + 1;
+    k.n = k.n0;
+  } else {
+    k.n0 = wb - wa + 1;
+    k.t1 = xa;
+    k.n = k.n0 + xb - xa + 1;
+  }
+  return k;
+}
+
+// cap tanh(scale u / cap) log2 e.  Tiles differ in how far their scores go, so a wave
+// looks at its largest |scale u / cap| first: to 1/8 three terms in x^2 are good to
+// 2^-24, to 1/2 five, beyond 1 - 2 / (1 + e^(2|x|)) takes over from 1/2 on.  (An
+// exponential and a reciprocal take eight instructions' time each.)
+struct Cap {
+  float small, mid;      // bounds of |u|
+  float a0, a1, a2;      // x <= 1/8: z = u (a0 + a1 u^2 + a2 u^4)
+  float b0, b1, b2, b3, b4;
+  float two, top;        // 2 scale / cap log2 e, cap log2 e
+  PB_DEV Cap(float scale, float cap) {
+    const float k = scale / cap, k2 = k * k, s = scale * kLog2e;
+    small = 0.125f / k, mid = 0.5f / k;
+    a0 = s * kA0, a1 = s * kA1 * k2, a2 = s * kA2 * k2 * k2;
+    b0 = s * kB0, b1 = s * kB1 * k2, b2 = s * kB2 * (k2 * k2), b3 = s * kB3 * (k2 * k2 * k2),
+    b4 = s * kB4 * (k2 * k2) * (k2 * k2);
+    two = 2.f * k * kLog2e, top = cap * kLog2e;
+  }
+  // tanh(x) / x in x^2 of least largest relative error (by Remez exchange): 7e-9 to 1/8,
+  // 1.4e-8 to 1/2; in fp32 4.3e-8 and 6.5e-8
+  static constexpr float kA0 = 1.0f, kA1 = -0.33332599f, kA2 = 0.13207752f;
+  static constexpr float kB0 = 1.0f, kB1 = -0.33333069f, kB2 = 0.13324779f, kB3 = -0.052986075f,
+                         kB4 = 0.017135007f;
+  PB_DEV float near(float u) const {
+    const float w = u * u;
+    return u * fmaf(fmaf(a2, w, a1), w, a0);
+  }
+  PB_DEV float half(float u) const {
+    const float w = u * u;
+    return u * fmaf(fmaf(fmaf(fmaf(b4, w, b3), w, b2), w, b1), w, b0);
+  }
+  PB_DEV float any(float u) const {
+    const float e = __builtin_amdgcn_exp2f(two * fabsf(u));
+    const float t = fmaf(-2.f * top, __builtin_amdgcn_rcpf(1.f + e), top);
+    return fabsf(u) <= mid ? half(u) : __builtin_copysignf(t, u);
+  }
+  // of some of a wave's scores, by the largest of them in any lane
+  template <typename V, int N>
+  PB_DEV void apply(V (&s)[N]) const {
+    constexpr int W = sizeof(V) / 4;
+    float largest = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < W; ++e) largest = fmaxf(largest, fabsf(s[i][e]));
+    if (!__builtin_amdgcn_ballot_w64(largest > small)) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < W; ++e) s[i][e] = near(s[i][e]);
+    } else if (!__builtin_amdgcn_ballot_w64(largest > mid)) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < W; ++e) s[i][e] = half(s[i][e]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < W; ++e) s[i][e] = any(s[i][e]);
+    }
+  }
+};
+
+// Biases of learned buckets in base 2.  A tile of NP positions and NK keys has NP + NK -
+// 1 distances: where they span buckets, the workgroup writes the bias of each (for each
+// of the block's heads) into LDS a tile ahead, key after key in ascending order, so that
+// a lane reads runs of neighbours; beyond the last bucket's first distance one value
+// does for a tile.  Bytes: the table of the block's heads, the first distances, the
+// buckets of distances below kMap, two tiles' biases.
+struct BiasLds {
+  static constexpr int kMap = 512;
+  int stride;  // floats of a head's biases in a tile
+  int tab, first, map, tile[2], bytes;
+  __host__ __device__ BiasLds(int at, int buckets, int pack, int positions, int keys) {
+    stride = positions + keys;  // (one spare: an odd stride for even sizes)
+    tab = at;
+    first = tab + 4 * buckets * pack;
+    map = first + 4 * kScoreMaxBuckets;
+    tile[0] = map + kMap;
+    tile[1] = tile[0] + 4 * stride * pack;
+    bytes = tile[1] + 4 * stride * pack;
+  }
+};
+// Tables of a workgroup (its first barrier comes after): heads h0 .. h0 + pack - 1.
+PB_DEV void bias_prologue(const ScoreArgs& a, const BiasLds& l, unsigned char* smem, int h0,
+                          int pack, int tid, int threads) {
+  float* tab = (float*)(smem + l.tab);
+  for (int x = tid; x < a.buckets * pack; x += threads) {
+    // (a bias of the type's lowest value stays finite in base 2)
+    const float v = a.table[(size_t)(x / pack) * a.heads + h0 + x % pack];
+    tab[x] = v < -2.3e38f && v > score::kNegInf ? -3.4e38f : v * kLog2e;
+  }
+  int* first = (int*)(smem + l.first);
+  if (tid < a.side) first[tid] = a.first[tid];
+}
+PB_DEV int bias_search(const int* first, int side, int d) {
+  int lo = 0, hi = side - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (first[mid] <= d) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+PB_DEV void bias_map(const ScoreArgs& a, const BiasLds& l, unsigned char* smem, int tid,
+                     int threads) {
+  for (int d = tid; d < BiasLds::kMap; d += threads)
+    smem[l.map + d] = (uint8_t)bias_search((const int*)(smem + l.first), a.side, d);
+}
+PB_DEV int bias_bucket(const ScoreArgs& a, const BiasLds& l, const unsigned char* smem, int n) {
+  const int d = a.causal ? max(n, 0) : abs(n);
+  const int k = d < BiasLds::kMap ? smem[l.map + d]
+                                  : bias_search((const int*)(smem + l.first), a.side, d);
+  return k + (!a.causal && n < 0 ? a.side : 0);
+}
+// The bucket of every distance n0 .. n1, or -1 where it is not known to be one.
+PB_DEV int bias_uniform(const ScoreArgs& a, int last, int n0, int n1) {
+  if (n0 >= last) return a.side - 1;
+  if (a.causal) return n1 <= 0 ? 0 : -1;
+  return n1 <= -last ? 2 * a.side - 1 : -1;
+}
+// Biases of a tile: entry x of a head is of distance top - x.
+PB_DEV void bias_tile(const ScoreArgs& a, const BiasLds& l, unsigned char* smem, int buf, int pack,
+                      int top, int tid, int threads) {
+  float* out = (float*)(smem + l.tile[buf]);
+  const float* tab = (const float*)(smem + l.tab);
+  for (int x = tid; x < l.stride; x += threads) {
+    const int k = bias_bucket(a, l, smem, top - x);
+    for (int h = 0; h < pack; ++h) out[h * l.stride + x] = tab[k * pack + h];
+  }
+}
+
+}  // namespace
+}  // namespace pb
