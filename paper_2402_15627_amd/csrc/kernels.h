@@ -450,6 +450,14 @@ ScorePlan score_fwd_plan(int head_dim, const ScoreArgs& a);
 size_t score_fwd_part_bytes(int head_dim, const ScoreArgs& a, const ScorePlan& p);
 void launch_score_forward_bf16(int head_dim, const ScoreArgs& a, const ScorePlan& p, void* part,
                                hipStream_t s);
+struct ScoreBwdPlan;
+ScoreBwdPlan score_bwd_plan(int head_dim, const ScoreArgs& a);
+ScoreBwdPlan score_bwd_whole(const ScoreArgs& a);  // not split but where it has to be
+size_t score_bwd_bytes(int head_dim, const ScoreArgs& a, const ScoreBwdPlan& p);
+void launch_score_backward_bf16(int head_dim, const ScoreArgs& a, const ScoreBwdPlan& p, void* ws,
+                                hipStream_t s);
+// dtable from a.bias_part, [parts][heads][buckets]
+void launch_score_dtable_sum(const ScoreArgs& a, int parts, hipStream_t s);
 void launch_score_forward(Dt dt, int head_dim, const ScoreArgs& a, hipStream_t s);
 void launch_score_backward(Dt dt, int head_dim, const ScoreArgs& a, hipStream_t s);
 

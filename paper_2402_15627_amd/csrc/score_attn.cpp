@@ -151,6 +151,20 @@ size_t fwd_bytes(const pb_score_attn_config* c) {
   return align256(most);
 }
 
+// min: without room for partial results.
+size_t bwd_bytes(const pb_score_attn_config* c, bool min) {
+  if (c->dtype != PB_BF16) return bias_bytes(c);
+  size_t most = 0;
+  for (int prefix = 0; prefix < 2; ++prefix) {
+    pb::ScoreArgs a = args_of(c, &kNoTerms);
+    static const int some = 0;
+    a.prefix = prefix ? &some : nullptr;
+    const pb::ScoreBwdPlan p = min ? pb::score_bwd_whole(a) : pb::score_bwd_plan(c->head_dim, a);
+    most = std::max(most, pb::score_bwd_bytes(c->head_dim, a, p));
+  }
+  return align256(most);
+}
+
 }  // namespace
 
 extern "C" {
@@ -166,7 +180,7 @@ pb_status pblock_score_attn_borders(const pb_score_attn_config* cfg, int* first)
 size_t pblock_score_attn_workspace_bytes(const pb_score_attn_config* cfg, int mode) {
   if (check_config(cfg) != PB_OK) return 0;
   if (mode == PB_ATTN_WS_FORWARD) return fwd_bytes(cfg);
-  return bias_bytes(cfg);
+  return bwd_bytes(cfg, mode == PB_ATTN_WS_BACKWARD_MIN);
 }
 
 pb_status pblock_score_attn_forward(const pb_score_attn_config* cfg, const pb_score_terms* terms,
@@ -253,7 +267,13 @@ pb_status pblock_score_attn_backward(const pb_score_attn_config* cfg, const pb_s
   a.d_o = d_o, a.ld_do = (int)ld_do;
   a.dq = dq, a.ld_dq = (int)ld_dq, a.dk = dk, a.dv = dv, a.ld_dkv = (int)ld_dkv;
   a.dtable = dtable, a.bias_part = (float*)ws;
-  pb::launch_score_backward(dt_of(cfg->dtype), cfg->head_dim, a, stream);
+  if (cfg->dtype == PB_BF16) {
+    pb::ScoreBwdPlan p = pb::score_bwd_plan(cfg->head_dim, a);
+    if (ws_bytes < pb::score_bwd_bytes(cfg->head_dim, a, p)) p = pb::score_bwd_whole(a);
+    pb::launch_score_backward_bf16(cfg->head_dim, a, p, ws, stream);
+  } else {
+    pb::launch_score_backward(dt_of(cfg->dtype), cfg->head_dim, a, stream);
+  }
   return finish_launches();
 }
 

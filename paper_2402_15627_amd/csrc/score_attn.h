@@ -39,6 +39,9 @@ struct ScoreArgs {
 struct ScorePlan {
   int chunk, chunks;
 };
+struct ScoreBwdPlan {
+  ScorePlan kv, q;  // dK and dV by tiles of rows, dQ by tiles of keys
+};
 // The most tiles (of `keys`) that a block of `rows` rows may visit, whatever the
 // documents.
 inline int score_most_tiles(const ScoreArgs& a, int rows, int keys) {

@@ -1,0 +1,901 @@
+// Gradients of attention with terms in its scores, bf16, on v_mfma_f32_32x32x16_bf16.
+//
+// Row terms (lse in base 2, delta = sum of dO O) come from a pass of their own, laid out
+// in the order of the blocks' rows.  Then one launch has two roles, as in attn.hip:
+//   dK, dV: 64 keys, a "P" and a "dS" wave for 32 each, over 32-row tiles of the heads
+//     that share the key head, so that the gradients of shared heads are one sum (of
+//     more than eight heads several, merged in order);
+//   dQ: 128 rows over 64-key tiles.
+// P = 2^(s - lse) with the scores' terms as in the forward; with a cap the P wave hands
+// P (1 - tanh^2) on, which is what dS = P (dP - delta) needs for dQ and dK.
+//
+// The table's gradient sums dz = P (dP - delta) by bucket, and there delta has to be
+// better than sum of dO O, whose O is rounded: dQ's rows also give e = the sum of their
+// dz, by which delta is off (the exact ones sum to zero), and the sums of dz and of P
+// over the tiles beyond the last bucket's first distance.  A last launch goes over the
+// other tiles again, with the row terms put right.
+//
+// Non-finite values behind the mask are met as in the forward.
+#include "kernels.h"
+#include "score_attn_tiles.h"
+
+namespace pb {
+namespace {
+
+#define PB_INLINE __attribute__((always_inline))
+
+constexpr int kNoBias = 0, kSlopes = 1, kTable = 2;
+constexpr int kBlockK = 64, kTileQ = 32;   // dK, dV: keys of a workgroup, rows of a tile
+constexpr int kBlockQ = 128, kTileK = 64;  // dQ: rows of a workgroup, keys of a tile
+constexpr int kSums = 5;  // of a row: e; dz and P beyond the last bucket, of either side
+
+// (By value: a choice of two members would be one of their addresses, and keep the whole
+// of the kernel's arguments in memory.)
+template <typename T>
+PB_DEV T pick(bool first, T x, T y) {
+  return first ? x : y;
+}
+
+// Rows of all blocks: [batch][head / pack][position][head mod pack].
+PB_DEV size_t packed_row(const ScoreArgs& a, int hb, int r) {
+  return (size_t)hb * a.seq_q * a.pack + r;
+}
+
+// ------------------------------------------------------------- row terms
+// Both operands read once, D / 8 lanes a row (four for head_dim 96).
+template <int D>
+__global__ __launch_bounds__(256) void score_terms(ScoreArgs a, float* __restrict__ L2,
+                                                   float* __restrict__ delta) {
+  constexpr int kLanes = D == 96 ? 4 : D / 8, kChunks = D / 8 / kLanes;
+  const size_t at = ((size_t)blockIdx.x * 256 + threadIdx.x) / kLanes;
+  const size_t all = (size_t)a.batch * a.seq_q * a.heads;
+  const int l = threadIdx.x % kLanes;
+  // heads fastest: neighbouring rows of memory
+  const size_t x = min(at, all - 1);
+  const int h = (int)(x % a.heads), i = (int)(x / a.heads % a.seq_q);
+  const int b = (int)(x / a.heads / a.seq_q);
+  const bf16 *o = score::o_row<bf16, D>(a, b, i, h), *g = score::do_row<bf16, D>(a, b, i, h);
+  float acc = 0.f;
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    float u[8], v[8];
+    load8(o + 8 * (l + c * kLanes), u);
+    load8(g + 8 * (l + c * kLanes), v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc = fmaf(u[e], v[e], acc);
+  }
+#pragma unroll
+  for (int s = 1; s < kLanes; s <<= 1) acc += __shfl_xor(acc, s, 64);
+  if (l != 0 || at >= all) return;
+  const float L = a.lse[score::lse_at(a, b, h, i)];
+  const size_t to = packed_row(a, b * (a.heads / a.pack) + h / a.pack, i * a.pack + h % a.pack);
+  // a row that sees nothing: probabilities of 2^-inf
+  L2[to] = L == kNegInf ? -kNegInf : L * kLog2e;
+  delta[to] = L == kNegInf ? 0.f : acc;
+}
+
+// A TL-row tile in the layout of dma_tile (attn_tiles.h), its rows' addresses from
+// row(0 .. TL - 1).
+template <int D, int TL, int NW, typename Row>
+PB_DEV void dma_rows(Row row, uint32_t lds_tile, int wave, int lane) {
+  constexpr int RB = 2 * D, NP = TL * RB / 1024;
+#pragma unroll
+  for (int i = 0; i < (NP + NW - 1) / NW; ++i) {
+    const int pc = NP % NW == 0 ? wave * (NP / NW) + i : i * NW + wave;
+    if (NP % NW != 0 && pc >= NP) break;  // wave-uniform
+    const int p = pc * 1024 + 16 * lane;
+    const int r = p / RB, slot = (p / 16) % (RB / 16);
+    dma16(row(r) + 8 * chunk_at<D>(r, slot),
+          __builtin_amdgcn_readfirstlane(lds_tile + pc * 1024));
+  }
+}
+
+// Scores to base 2, with the cap.
+template <bool CAP, int N>
+PB_DEV void to_base2(const Cap& cap, float c2, f32x16 (&s)[N]) {
+  if constexpr (CAP) {
+    cap.apply(s);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[i][e] *= c2;
+  }
+}
+// 1 - tanh^2 of a capped score, it = 1 / cap.top.
+PB_DEV float cap_slope(float z, float it) {
+  const float t = z * it;
+  return fmaf(-t, t, 1.f);
+}
+
+struct BwdWork {
+  float *L2, *delta;           // row terms, in the blocks' order
+  float *pdk, *pdv, *pdq;      // partial results of split blocks
+  float* sums;                 // [chunk][kSums][rows] (with dtable)
+  int kv_cs, kv_nc, q_cs, q_nc;
+};
+
+// ------------------------------------------------------------------ dK, dV
+template <int D, int BIAS>
+struct KvLds {
+  static constexpr int kStages = D == 128 && BIAS == kTable ? 3 : 4;
+  static constexpr int kTile = kTileQ * 2 * D;
+  // Q, dO, then of each row: lse, delta, position, and its bias (slope, place or value)
+  static constexpr int kStage = 2 * kTile + 4 * kTileQ * 4;
+  static constexpr int kP = 64 * 16 * 4;  // one wave's P
+  static constexpr int kBytes = kStages * kStage + 2 * kP;
+  static __host__ __device__ BiasLds bias(const ScoreArgs& a) {
+    return BiasLds(kBytes, a.buckets, a.pack, (kTileQ + a.pack - 1) / a.pack + 1, kBlockK);
+  }
+};
+
+template <int D, bool CAP, int BIAS>
+PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
+  constexpr int TL = kTileQ, NB = kBlockK, TB = TL * 2 * D;
+  using L = KvLds<D, BIAS>;
+  constexpr int NS = L::kStages, STAGE = L::kStage;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(PB_LDS unsigned char*)smem;
+  const int b = hb / a.kv_heads, kvh = hb % a.kv_heads;
+  // chunk: a set of heads, and a run of its row tiles
+  const int parts = a.group / a.pack, subs = w.kv_nc / parts;
+  const int chunk = bx % w.kv_nc, k0 = bx / w.kv_nc * NB;
+  const int h0 = kvh * a.group + chunk / subs * a.pack;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int grp = wave & 1;
+  const bool pside = wave < 2;
+  const int fr = lane & 31, fh = lane >> 5;
+  const int off = a.seq_k - a.seq_q, rows = a.seq_q * a.pack;
+  const Packed pk(a.pack);
+  const int key = k0 + 32 * grp + fr, key_c = min(key, a.seq_k - 1);
+
+  // queries that see the lane's key: positions sf .. sf + sn - 1; all keys' together
+  int sf = 0, sn = 0, lo = 0x7fffffff, hi = -1;
+  {
+    const int j = k0 + lane;  // (64 keys, a lane each)
+    int f = 0, n = 0;
+    if (j < a.seq_k) {
+      const Bounds d = bounds_of(a, b, j);
+      if (d.de > d.ds) {
+        f = max(score::seen_first(a, d, j), off);
+        n = max(score::seen_last(a, d, j) - f + 1, 0);
+      }
+    }
+    if (n > 0) lo = f, hi = f + n - 1;
+    lo = wave_imin(lo), hi = wave_imax(hi);
+    sf = __shfl(f, 32 * grp + fr, 64);
+    sn = __shfl(n, 32 * grp + fr, 64);
+  }
+  const int r_lo = hi < 0 ? 0 : (lo - off) * a.pack, r_hi = hi < 0 ? -1 : (hi - off + 1) * a.pack - 1;
+  const int t_lo = r_lo / TL, per = hi < 0 ? 0 : r_hi / TL - t_lo + 1;
+  const int t_begin = chunk % subs * w.kv_cs, nt = min(per - t_begin, w.kv_cs);
+  const bool split = w.kv_nc > 1;
+  const size_t keys = (size_t)a.batch * a.kv_heads * a.seq_k;
+  if (nt <= 0) {  // nobody sees these keys (the merge counts a split block's chunks itself)
+    bf16* out = (bf16*)pick(pside, a.dv, a.dk) + ((size_t)b * a.seq_k + key) * a.ld_dkv + kvh * D;
+    if (!split && key < a.seq_k)
+      for (int e = 8 * fh; e < D; e += 16) *reinterpret_cast<u32x4*>(out + e) = u32x4{0, 0, 0, 0};
+    if (split && key < a.seq_k) {
+      float* prow = pick(pside, w.pdv, w.pdk) +
+                    ((size_t)chunk * keys + (size_t)hb * a.seq_k + key) * D;
+      for (int e = 4 * fh; e < D; e += 8) *reinterpret_cast<f32x4*>(prow + e) = zero4();
+    }
+    return;
+  }
+  // keys that every query of a tile has to lie between for the wave's tile to be whole
+  int full_lo = sn > 0 ? sf : 0x7fffffff, full_hi = sf + sn - 1;
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) {
+    full_lo = max(full_lo, __shfl_xor(full_lo, o, 64));
+    full_hi = min(full_hi, __shfl_xor(full_hi, o, 64));
+  }
+  full_lo = __builtin_amdgcn_readfirstlane(full_lo);
+  full_hi = __builtin_amdgcn_readfirstlane(full_hi);
+
+  const bf16* kvr = score::kv_row<bf16, D>(a, pick(pside, a.k, a.v), b, key_c, kvh);
+  bf16x8 kvf[D / 16];
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks)
+    kvf[ks] = load_row_frag(kvr + 16 * ks + 8 * fh, key < a.seq_k);
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) acc[i] = zero16();
+  const float c2 = a.scale * kLog2e;
+  const Cap cap(a.scale, CAP ? a.cap : 1.f);
+  const BiasLds bl = L::bias(a);
+  const int bias_last = BIAS == kTable ? a.first[a.side - 1] : 0;
+
+  float* pbuf = (float*)(smem + NS * STAGE + grp * L::kP);
+  auto tile_row = [&](int i) PB_INLINE { return (t_lo + t_begin + i) * TL; };
+  auto tile_span = [&](int i, int& p0, int& p1) PB_INLINE {  // positions of tile i
+    const int r = tile_row(i);
+    p0 = off + pk.pos(r);
+    p1 = off + pk.pos(r + TL - 1);
+  };
+  auto uniform = [&](int i) PB_INLINE {
+    int p0, p1;
+    tile_span(i, p0, p1);
+    return bias_uniform(a, bias_last, p0 - k0 - NB + 1, p1 - k0);
+  };
+  const int per_stage = 2 * dma_pieces<D, TL, 4>(wave) + (wave == 0 ? 1 : 0);
+  auto issue_stage = [&](int i) PB_INLINE {
+    const int s = i % NS, r0 = tile_row(i);
+    const uint32_t at = lds0 + s * STAGE;
+    const bf16* q = score::q_row<bf16, D>(a, b, 0, h0);
+    const bf16* g = score::do_row<bf16, D>(a, b, 0, h0);
+    auto row_of = [&](int r) { return max(r_lo, min(r0 + r, r_hi)); };
+    dma_rows<D, TL, 4>([&](int r) {
+      const int x = row_of(r), y = pk.pos(x);
+      return q + (size_t)y * a.ld_q + (x - y * a.pack) * D;
+    }, at, wave, lane);
+    dma_rows<D, TL, 4>([&](int r) {
+      const int x = row_of(r), y = pk.pos(x);
+      return g + (size_t)y * a.ld_do + (x - y * a.pack) * D;
+    }, at + TB, wave, lane);
+    const size_t row0 = packed_row(a, b * (a.heads / a.pack) + h0 / a.pack, 0);
+    if (wave == 0)
+      dma4(pick(lane < 32, w.L2, w.delta) + row0 + row_of(lane & 31),
+           __builtin_amdgcn_readfirstlane(at + 2 * TB));
+    if (wave == 1 && lane < TL) {
+      const int r = r0 + lane, y = pk.pos(r), hh = r - y * a.pack;
+      int* rows_of = (int*)(smem + s * STAGE + 2 * TB + 2 * TL * 4);
+      rows_of[lane] = y + off;
+      if constexpr (BIAS == kSlopes) ((float*)rows_of)[TL + lane] = -a.slopes[h0 + hh] * kLog2e;
+      if constexpr (BIAS == kTable) {
+        const int u = uniform(i);
+        if (u < 0) rows_of[TL + lane] = hh * bl.stride + off + pk.pos(r0 + TL - 1) - (y + off);
+        else ((float*)rows_of)[TL + lane] = ((const float*)(smem + bl.tab))[u * a.pack + hh];
+      }
+    }
+  };
+  auto build = [&](int i) PB_INLINE {
+    int p0, p1;
+    tile_span(i, p0, p1);
+    if (uniform(i) < 0) bias_tile(a, bl, smem, i & 1, a.pack, p1 - k0, tid, 256);
+  };
+  if constexpr (BIAS == kTable) {
+    bias_prologue(a, bl, smem, h0, a.pack, tid, 256);
+    __syncthreads();
+    bias_map(a, bl, smem, tid, 256);
+    __syncthreads();
+    build(0);
+  }
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i)
+    if (i < nt) issue_stage(i);
+
+  for (int i = 0; i < nt; ++i) {
+    const int cur = i % NS;
+    wait_dma_upto(min(nt - 1 - i, NS - 2) * per_stage);
+    block_barrier();  // ... for every wave; and every wave is done with tile i - 1
+    if (i + NS - 1 < nt) issue_stage(i + NS - 1);
+    if constexpr (BIAS == kTable)
+      if (i + 1 < nt) build(i + 1);
+    const unsigned char* qt = smem + cur * STAGE;
+    const unsigned char* gt = qt + TB;
+    const float* ls = (const float*)(qt + 2 * TB);
+    // Lane holds key `key` and rows r0 + 8 j + 4 fh + i of element 4 j + i.
+    f32x16 sc[1] = {zero16()};  // S (P side) or dP (dS side)
+    const unsigned char* nt_ = pside ? qt : gt;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+      sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_row<D>(nt_, fr, ks, fh), kvf[ks], sc[0],
+                                                      0, 0, 0);
+    if (pside) {
+      f32x16 slope;
+      const float it = 1.f / cap.top;
+      if constexpr (CAP || BIAS != kNoBias) to_base2<CAP>(cap, c2, sc);
+      if constexpr (CAP)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) slope[e] = cap_slope(sc[0][e], it);
+      const int* row_pos = (const int*)(ls + 2 * TL);
+      int p0, p1;
+      tile_span(i, p0, p1);
+      const bool full = p0 >= full_lo && p1 <= full_hi;
+      int u = 0;
+      if constexpr (BIAS == kTable) u = uniform(i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = 8 * j + 4 * fh;
+        const f32x4 L4 = *reinterpret_cast<const f32x4*>(ls + at);
+        const u32x4 P4 = *reinterpret_cast<const u32x4*>(row_pos + at);
+        const u32x4 X4 = *reinterpret_cast<const u32x4*>(row_pos + TL + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float v = sc[0][4 * j + e];
+          if constexpr (BIAS == kSlopes)
+            v = fmaf(__uint_as_float(X4[e]), fabsf((float)((int)P4[e] - key)), v);
+          if constexpr (BIAS == kTable)
+            v += u < 0 ? ((const float*)(smem + bl.tile(i & 1, a.pack)))[(int)X4[e] + key - k0]
+                       : __uint_as_float(X4[e]);
+          if (!full) v = (unsigned)((int)P4[e] - sf) < (unsigned)sn ? v : kNegInf;
+          const float p = exp2_hw(CAP || BIAS != kNoBias ? v - L4[e] : fmaf(v, c2, -L4[e]));
+          sc[0][4 * j + e] = p;
+        }
+        f32x4 out;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          out[e] = CAP ? sc[0][4 * j + e] * slope[4 * j + e] : sc[0][4 * j + e];
+        *reinterpret_cast<f32x4*>(pbuf + (j * 64 + lane) * 4) = out;
+      }
+    }
+    block_barrier();  // P of this tile is visible to the dS side
+    if (!pside) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x4 P4 = *reinterpret_cast<const f32x4*>(pbuf + (j * 64 + lane) * 4);
+        const f32x4 D4 = *reinterpret_cast<const f32x4*>(ls + TL + 8 * j + 4 * fh);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[0][4 * j + e] = P4[e] * (sc[0][4 * j + e] - D4[e]);
+      }
+    }
+    const unsigned char* tt = pside ? gt : qt;  // dO^T with P, Q^T with dS
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int s2 = 0; s2 < TL / 16; ++s2)
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            frag_tr<D>(tt, 32 * db + fr, s2, fh, lane), probs_frag(sc, s2), acc[db], 0, 0, 0);
+  }
+
+  const float mul = pside ? 1.f : a.scale;
+  if (split) {
+    if (key >= a.seq_k) return;
+    float* prow = pick(pside, w.pdv, w.pdk) + ((size_t)chunk * keys + (size_t)hb * a.seq_k + key) * D;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<f32x4*>(prow + 32 * db + 8 * j + 4 * fh) =
+            f32x4{acc[db][4 * j] * mul, acc[db][4 * j + 1] * mul, acc[db][4 * j + 2] * mul,
+                  acc[db][4 * j + 3] * mul};
+    return;
+  }
+  float bad = 0.f;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) bad = fmaf(acc[db][e], 0.f, bad);
+  if (__syncthreads_or(key < a.seq_k && bad != 0.f)) {
+    for (int j = k0 + wave; j < min(k0 + NB, a.seq_k); j += 4)
+      score::dkdv_row<bf16, D>(a, b, kvh, j, lane);
+    return;
+  }
+  if (key >= a.seq_k) return;
+  bf16* orow = (bf16*)pick(pside, a.dv, a.dk) + ((size_t)b * a.seq_k + key) * a.ld_dkv + kvh * D;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = acc[db][4 * j + e] * mul;
+      store4(orow + 32 * db + 8 * j + 4 * fh, v);
+    }
+}
+
+// --------------------------------------------------------- rows over key tiles
+// What dQ and the table's gradient share: 128 rows, a lane's row and its P and dz of a
+// 64-key tile.
+template <int D, bool CAP, int BIAS>
+struct RowTiles {
+  const ScoreArgs& a;
+  const BwdWork& w;
+  unsigned char* smem;
+  int b, h0, kvh, r0, rows, off, lane, wave, fr, fh, r, i, h, p, p_first, p_last;
+  float L2, dl, slope2;
+  int bias_at, bias_last;
+  RowKeys keys;
+  bf16x8 qf[D / 16], gf[D / 16];
+  Cap cap;
+  BiasLds bl;
+  Packed pk;
+
+  PB_DEV RowTiles(const ScoreArgs& a_, const BwdWork& w_, unsigned char* s, int lds_at, int blk,
+                  int hb)
+      : a(a_), w(w_), smem(s), cap(a_.scale, CAP ? a_.cap : 1.f),
+        bl(lds_at, a_.buckets, a_.pack, (kBlockQ + a_.pack - 1) / a_.pack + 1, kTileK),
+        pk(a_.pack) {
+    const int sets = a.heads / a.pack;
+    b = hb / sets, h0 = hb % sets * a.pack, kvh = h0 / a.group;
+    rows = a.seq_q * a.pack, off = a.seq_k - a.seq_q, r0 = blk * kBlockQ;
+    lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    fr = lane & 31, fh = lane >> 5;
+    r = r0 + 32 * wave + fr;
+    const int rc = min(r, rows - 1);
+    i = pk.pos(rc), h = h0 + rc - i * a.pack, p = i + off;
+    p_first = off + pk.pos(r0), p_last = off + pk.pos(min(r0 + kBlockQ, rows) - 1);
+    const bf16 *q = score::q_row<bf16, D>(a, b, i, h), *g = score::do_row<bf16, D>(a, b, i, h);
+    keys = row_keys(a, b, p);
+    if (r >= rows) keys = RowKeys{0, 0, 0, 0};
+    // (a row that sees nothing may hold anything)
+    const bool any = keys.len > 0 || keys.plen > 0;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+      qf[ks] = load_row_frag(q + 16 * ks + 8 * fh, any);
+      gf[ks] = load_row_frag(g + 16 * ks + 8 * fh, any);
+    }
+    const size_t at = packed_row(a, hb, rc);
+    L2 = w.L2[at];
+    dl = w.delta[at];
+    slope2 = BIAS == kSlopes ? -a.slopes[h] * kLog2e : 0.f;
+    bias_last = BIAS == kTable ? a.first[a.side - 1] : 0;
+    bias_at = BIAS == kTable ? (h - h0) * bl.stride + (p_last - p) + 4 * fh : 0;
+  }
+  PB_DEV void tables() {
+    bias_prologue(a, bl, smem, h0, a.pack, threadIdx.x, 256);
+    __syncthreads();
+    bias_map(a, bl, smem, threadIdx.x, 256);
+    __syncthreads();
+  }
+  PB_DEV int uniform(int kv0) const {
+    return bias_uniform(a, bias_last, p_first - kv0 - kTileK + 1, p_last - kv0);
+  }
+  PB_DEV void build(int kv0, int buf) {
+    if (uniform(kv0) < 0) bias_tile(a, bl, smem, buf, a.pack, p_last - kv0, threadIdx.x, 256);
+  }
+  PB_DEV void request(const KeyTiles& kt, int kv0, uint32_t lds_k, uint32_t lds_v) const {
+    const int lo = max(kt.lo - kv0, 0), hi = min(kt.hi - kv0, kTileK - 1);
+    const bf16 *k = score::kv_row<bf16, D>(a, a.k, b, kv0, kvh),
+               *v = score::kv_row<bf16, D>(a, a.v, b, kv0, kvh);
+    dma_rows<D, kTileK, 4>([&](int x) { return k + (size_t)max(lo, min(x, hi)) * a.ld_kv; }, lds_k,
+                           wave, lane);
+    dma_rows<D, kTileK, 4>([&](int x) { return v + (size_t)max(lo, min(x, hi)) * a.ld_kv; }, lds_v,
+                           wave, lane);
+  }
+  // P and dz of the lane's row and keys kv0 + 32 h2 + 8 j + 4 fh + e (element 4 j + e of
+  // h2).  see: the row's keys of the tile.  SLOPE: 0, dz as it is; 1, times what the cap
+  // leaves; 2, that apart, in slope.
+  template <int SLOPE>
+  PB_DEV void pair(int kv0, int buf, const unsigned char* kt, const unsigned char* vt,
+                   uint64_t see, f32x16 (&pr)[2], f32x16 (&dz)[2], f32x16 (&slope)[2]) {
+    const float c2 = a.scale * kLog2e;
+#pragma unroll
+    for (int h2 = 0; h2 < 2; ++h2) {
+      pr[h2] = zero16();
+      dz[h2] = zero16();
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) {
+        pr[h2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_row<D>(kt, 32 * h2 + fr, ks, fh),
+                                                         qf[ks], pr[h2], 0, 0, 0);
+        dz[h2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_row<D>(vt, 32 * h2 + fr, ks, fh),
+                                                         gf[ks], dz[h2], 0, 0, 0);
+      }
+    }
+    if constexpr (CAP || BIAS != kNoBias) to_base2<CAP>(cap, c2, pr);
+    const float it = 1.f / cap.top;
+#pragma unroll
+    for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        dz[h2][x] -= dl;
+        if constexpr (CAP && SLOPE == 1) dz[h2][x] *= cap_slope(pr[h2][x], it);
+        if constexpr (CAP && SLOPE == 2) slope[h2][x] = cap_slope(pr[h2][x], it);
+      }
+    if constexpr (BIAS == kSlopes) {
+      const float d0 = (float)(p - kv0 - 4 * fh);
+#pragma unroll
+      for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+        for (int x = 0; x < 16; ++x)
+          pr[h2][x] = fmaf(slope2, fabsf(d0 - (float)(32 * h2 + 8 * (x >> 2) + (x & 3))), pr[h2][x]);
+    }
+    if constexpr (BIAS == kTable) {
+      const int u = uniform(kv0);
+      const float* bt = (const float*)(smem + bl.tile(buf, a.pack)) + bias_at;
+      const float f =
+          u < 0 ? 0.f : ((const float*)(smem + bl.tab))[u * a.pack + h - h0];
+      if (u < 0) {
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) pr[h2][x] += bt[32 * h2 + 8 * (x >> 2) + (x & 3)];
+      } else {
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) pr[h2][x] += f;
+      }
+    }
+    if (__builtin_amdgcn_ballot_w64(see != ~0ull)) {
+      const uint64_t mine = see >> (4 * fh);
+      const uint32_t half[2] = {(uint32_t)mine, (uint32_t)(mine >> 32)};
+#pragma unroll
+      for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+        for (int x = 0; x < 16; ++x)
+          pr[h2][x] = half[h2] & (1u << (8 * (x >> 2) + (x & 3))) ? pr[h2][x] : kNegInf;
+    }
+#pragma unroll
+    for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        pr[h2][x] = exp2_hw(CAP || BIAS != kNoBias ? pr[h2][x] - L2 : fmaf(pr[h2][x], c2, -L2));
+        dz[h2][x] *= pr[h2][x];
+      }
+  }
+};
+
+template <int D, bool CAP, int BIAS>
+PB_DEV void dq_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
+  constexpr int TB = kTileK * 2 * D;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(PB_LDS unsigned char*)smem;
+  const int nblk = (a.seq_q * a.pack + kBlockQ - 1) / kBlockQ;
+  const int chunk = bx % w.q_nc;
+  RowTiles<D, CAP, BIAS> t(a, w, smem, 4 * TB, nblk - 1 - bx / w.q_nc, hb);
+  const KeyTiles kt = key_tiles<kTileK>(a, t.b, t.p_first, t.p_last, t.lane);
+  const int t_begin = chunk * w.q_cs, n = min(kt.n - t_begin, w.q_cs);
+  const bool split = w.q_nc > 1;
+  const size_t all = (size_t)a.batch * a.heads * a.seq_q;
+  const size_t row = (size_t)chunk * all + packed_row(a, hb, min(t.r, t.rows - 1));
+
+  f32x16 dq[D / 32];
+#pragma unroll
+  for (int x = 0; x < D / 32; ++x) dq[x] = zero16();
+  float sums[kSums] = {0.f, 0.f, 0.f, 0.f, 0.f};
+  if (n > 0) {
+    auto kv_of = [&](int i) { return kt.tile(t_begin + i) * kTileK; };
+    auto k_off = [&](int s) { return lds0 + (2 * s) * TB; };
+    auto v_off = [&](int s) { return lds0 + (2 * s + 1) * TB; };
+    if constexpr (BIAS == kTable) {
+      t.tables();
+      t.build(kv_of(0), 0);
+    }
+    t.request(kt, kv_of(0), k_off(0), v_off(0));
+    for (int i = 0; i < n; ++i) {
+      const int cur = i & 1, kv0 = kv_of(i);
+      wait_dma_all();
+      block_barrier();
+      if (i + 1 < n) {
+        t.request(kt, kv_of(i + 1), k_off(cur ^ 1), v_off(cur ^ 1));
+        if constexpr (BIAS == kTable) t.build(kv_of(i + 1), cur ^ 1);
+      }
+      const uint64_t see = t.keys.bits(kv0);
+      if (!__builtin_amdgcn_ballot_w64(see != 0)) continue;
+      const unsigned char *kl = smem + (2 * cur) * TB, *vl = kl + TB;
+      f32x16 pr[2], dz[2], slope[2];
+      t.template pair<BIAS == kTable ? 2 : 1>(kv0, cur, kl, vl, see, pr, dz, slope);
+      if constexpr (BIAS == kTable) {
+        if (a.dtable) {
+          float s = 0.f, sp = 0.f;
+#pragma unroll
+          for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) s += dz[h2][x];
+          sums[0] += s;
+          const int u = t.uniform(kv0);
+          if (u >= 0) {
+#pragma unroll
+            for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+              for (int x = 0; x < 16; ++x) sp += pr[h2][x];
+            if (u == a.side - 1) sums[1] += s, sums[2] += sp;
+            else sums[3] += s, sums[4] += sp;
+          }
+        }
+      }
+      if constexpr (CAP && BIAS == kTable) {
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) dz[h2][x] *= slope[h2][x];
+      }
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int s2 = 0; s2 < kTileK / 16; ++s2)
+          dq[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              frag_tr<D>(kl, 32 * db + t.fr, s2, t.fh, t.lane), probs_frag(dz, s2), dq[db], 0, 0,
+              0);
+    }
+  }
+  if constexpr (BIAS == kTable) {
+    if (a.dtable) {
+#pragma unroll
+      for (int x = 0; x < kSums; ++x) {
+        const float s = sums[x] + __shfl_xor(sums[x], 32, 64);
+        if (t.r < t.rows && t.fh == 0)
+          w.sums[((size_t)chunk * kSums + x) * all + packed_row(a, hb, t.r)] = s;
+      }
+    }
+  }
+  if (split) {
+    if (t.r >= t.rows) return;
+    float* prow = w.pdq + row * D;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<f32x4*>(prow + 32 * db + 8 * j + 4 * t.fh) =
+            f32x4{dq[db][4 * j] * a.scale, dq[db][4 * j + 1] * a.scale, dq[db][4 * j + 2] * a.scale,
+                  dq[db][4 * j + 3] * a.scale};
+    return;
+  }
+  float bad = 0.f;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) bad = fmaf(dq[db][e], 0.f, bad);
+  if (__builtin_amdgcn_ballot_w64(t.r < t.rows && bad != 0.f)) {
+    const int w0 = t.r0 + 32 * t.wave;
+    for (int r = w0; r < min(w0 + 32, t.rows); ++r) {
+      const int i = t.pk.pos(r);
+      score::dq_row<bf16, D>(a, t.b, t.h0 + r - i * a.pack, i, t.lane);
+    }
+    return;
+  }
+  if (t.r >= t.rows) return;
+  bf16* out = (bf16*)a.dq + ((size_t)t.b * a.seq_q + t.i) * a.ld_dq + t.h * D;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = dq[db][4 * j + e] * a.scale;
+      store4(out + 32 * db + 8 * j + 4 * t.fh, v);
+    }
+}
+
+// Both roles in one launch, in turn, each with its (under a causal mask) longest blocks
+// first, all heads' before the next.
+template <int D, bool CAP, int BIAS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void score_bwd_bf16(
+    ScoreArgs a, BwdWork w, int nk, int nq) {
+  const int id = blockIdx.x, mn = min(nk, nq);
+  const bool kv = id < 2 * mn ? !(id & 1) : nk > nq;
+  const int x = id < 2 * mn ? id >> 1 : id - mn;
+  if (kv) {
+    const int n = a.batch * a.kv_heads;
+    dkdv_block<D, CAP, BIAS>(a, w, x / n, x % n);
+  } else {
+    const int n = a.batch * (a.heads / a.pack);
+    dq_block<D, CAP, BIAS>(a, w, x / n, x % n);
+  }
+}
+
+// ----------------------------------------------------- the table's gradient
+// Sums by bucket of 128 rows' dz over the tiles whose distances span buckets, with delta
+// put right by e; those beyond come from dQ's sums: dz less e P.  A lane adds to places
+// of its own in LDS.
+template <int D, bool CAP>
+__global__ __launch_bounds__(256) void score_dtable_bf16(ScoreArgs a, BwdWork w, int nblk) {
+  constexpr int TB = kTileK * 2 * D, kPad = 65;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(PB_LDS unsigned char*)smem;
+  const int hb_n = a.batch * (a.heads / a.pack);
+  const int hb = blockIdx.x % hb_n, blk = nblk - 1 - blockIdx.x / hb_n;
+  RowTiles<D, CAP, kTable> t(a, w, smem, 2 * TB, blk, hb);
+  float* acc = (float*)(smem + t.bl.bytes);
+  unsigned char* ids = smem + t.bl.bytes + 4 * a.buckets * kPad * 4;
+  float* mine = acc + (size_t)t.wave * a.buckets * kPad + t.lane;
+  for (int n = 0; n < a.buckets; ++n) mine[n * kPad] = 0.f;
+  t.tables();
+  const size_t all = (size_t)a.batch * a.heads * a.seq_q;
+  float sums[kSums] = {0.f, 0.f, 0.f, 0.f, 0.f};
+  if (t.r < t.rows)
+    for (int c = 0; c < w.q_nc; ++c)
+#pragma unroll
+      for (int x = 0; x < kSums; ++x)
+        sums[x] += w.sums[((size_t)c * kSums + x) * all + packed_row(a, hb, t.r)];
+  t.dl += sums[0];
+  if (t.fh == 0) {
+    mine[(a.side - 1) * kPad] += fmaf(-sums[0], sums[2], sums[1]);
+    mine[(a.causal ? 0 : 2 * a.side - 1) * kPad] += fmaf(-sums[0], sums[4], sums[3]);
+  }
+  const KeyTiles kt = key_tiles<kTileK>(a, t.b, t.p_first, t.p_last, t.lane);
+  for (int i = 0; i < kt.n; ++i) {
+    const int kv0 = kt.tile(i) * kTileK;
+    if (t.uniform(kv0) >= 0) continue;
+    block_barrier();  // the tile before has been read by all
+    t.request(kt, kv0, lds0, lds0 + TB);
+    t.build(kv0, 0);
+    for (int x = threadIdx.x; x < t.bl.stride; x += 256)
+      ids[x] = (unsigned char)bias_bucket(a, t.bl, smem, t.p_last - kv0 - x);
+    wait_dma_all();
+    block_barrier();
+    const uint64_t see = t.keys.bits(kv0);
+    if (!__builtin_amdgcn_ballot_w64(see != 0)) continue;
+    f32x16 pr[2], dz[2], slope[2];
+    t.template pair<0>(kv0, 0, smem, smem + TB, see, pr, dz, slope);
+    const int at = t.p_last - t.p + 4 * t.fh;
+#pragma unroll
+    for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+      for (int x = 0; x < 16; ++x)
+        unsafeAtomicAdd(&mine[ids[at + 32 * h2 + 8 * (x >> 2) + (x & 3)] * kPad], dz[h2][x]);
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < a.buckets * a.pack; x += 256) {
+    const int n = x % a.buckets, hh = x / a.buckets;
+    float s = 0.f;
+    for (int wv = 0; wv < 4; ++wv)
+      for (int l = 0; l < 32; ++l) {
+        const int r = t.r0 + 32 * wv + l;
+        if (r - t.pk.pos(r) * a.pack != hh) continue;
+        const float* from = acc + ((size_t)wv * a.buckets + n) * kPad + l;
+        s += from[0] + from[32];
+      }
+    a.bias_part[(((size_t)t.b * nblk + blk) * a.heads + t.h0 + hh) * a.buckets + n] = s;
+  }
+}
+
+// ----------------------------------------------------------------- merges
+// Sums of a split block's parts, in chunk order; a thread has 8 features of a row.  A row
+// with a non-finite part is computed again by the definition.
+template <int D, bool KEYS>
+__global__ __launch_bounds__(256) void score_bwd_merge(ScoreArgs a, BwdWork w) {
+  const int H = KEYS ? a.kv_heads : a.heads, S = KEYS ? a.seq_k : a.seq_q;
+  const int nc = KEYS ? w.kv_nc : w.q_nc;
+  const size_t all = (size_t)a.batch * H * S;
+  const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
+  const int g = (int)(at % (D / 8)), lane = threadIdx.x & 63;
+  const size_t row = min(at / (D / 8), all - 1);
+  int b, h, i;
+  if (KEYS) {
+    i = (int)(row % S), h = (int)(row / S % H), b = (int)(row / S / H);
+  } else {
+    const int r = (int)(row % ((size_t)S * a.pack)), hb = (int)(row / ((size_t)S * a.pack));
+    i = r / a.pack, h = hb % (H / a.pack) * a.pack + r % a.pack, b = hb / (H / a.pack);
+  }
+  float acc[2][8] = {}, bad = 0.f;
+#pragma unroll
+  for (int k = 0; k < (KEYS ? 2 : 1); ++k) {
+    const float* from = (KEYS ? (k ? w.pdv : w.pdk) : w.pdq) + row * D + 8 * g;
+    for (int c = 0; c < nc; ++c) {
+      float v[8];
+      load8(from + (size_t)c * all * D, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[k][e] += v[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bad = fmaf(acc[k][e], 0.f, bad);
+  }
+  unsigned long long rows = __builtin_amdgcn_ballot_w64(bad != 0.f);
+  if (at / (D / 8) < all && bad == 0.f) {
+    if (KEYS) {
+      const size_t to = ((size_t)b * S + i) * a.ld_dkv + h * D + 8 * g;
+      store8((bf16*)a.dk + to, acc[0]);
+      store8((bf16*)a.dv + to, acc[1]);
+    } else {
+      store8((bf16*)a.dq + ((size_t)b * S + i) * a.ld_dq + h * D + 8 * g, acc[0]);
+    }
+  }
+  while (rows) {
+    const int first = __builtin_ctzll(rows);
+    const int i2 = __builtin_amdgcn_readlane(i, first), h2 = __builtin_amdgcn_readlane(h, first);
+    const int b2 = __builtin_amdgcn_readlane(b, first);
+    rows &= ~__builtin_amdgcn_ballot_w64(i == i2 && h == h2 && b == b2);
+    if (KEYS) score::dkdv_row<bf16, D>(a, b2, h2, i2, lane);
+    else score::dq_row<bf16, D>(a, b2, h2, i2, lane);
+  }
+}
+
+int row_blocks(const ScoreArgs& a) { return (a.seq_q * a.pack + kBlockQ - 1) / kBlockQ; }
+int key_blocks(const ScoreArgs& a) { return (a.seq_k + kBlockK - 1) / kBlockK; }
+size_t round64(size_t floats) { return (floats + 63) & ~(size_t)63; }
+
+// The workspace's parts, in floats from its start.
+struct BwdLayout {
+  size_t L2, delta, bias, sums, pdk, pdv, pdq, min, total;
+};
+BwdLayout bwd_layout(int D, const ScoreArgs& a, const ScoreBwdPlan& p) {
+  const size_t rows = (size_t)a.batch * a.heads * a.seq_q;
+  const size_t keys = (size_t)a.batch * a.kv_heads * a.seq_k;
+  BwdLayout l{};
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    const size_t from = at;
+    at += round64(n);
+    return from;
+  };
+  l.L2 = take(rows), l.delta = take(rows);
+  l.bias = take(a.buckets ? (size_t)a.batch * row_blocks(a) * a.heads * a.buckets : 0);
+  l.sums = take(a.buckets ? (size_t)p.q.chunks * kSums * rows : 0);
+  l.pdk = take(p.kv.chunks > 1 ? (size_t)p.kv.chunks * keys * D : 0);
+  l.pdv = take(p.kv.chunks > 1 ? (size_t)p.kv.chunks * keys * D : 0);
+  l.pdq = take(p.q.chunks > 1 ? (size_t)p.q.chunks * rows * D : 0);
+  l.total = at;
+  return l;
+}
+
+template <int D>
+void bwd_d(const ScoreArgs& a, const ScoreBwdPlan& p, float* ws, hipStream_t s) {
+  const BwdLayout l = bwd_layout(D, a, p);
+  BwdWork w{ws + l.L2, ws + l.delta, ws + l.pdk, ws + l.pdv, ws + l.pdq, ws + l.sums,
+            p.kv.chunk, p.kv.chunks, p.q.chunk, p.q.chunks};
+  ScoreArgs x = a;
+  x.bias_part = ws + l.bias;
+  const size_t rows = (size_t)a.batch * a.heads * a.seq_q;
+  const size_t keys = (size_t)a.batch * a.kv_heads * a.seq_k;
+  constexpr int kLanes = D == 96 ? 4 : D / 8;
+  score_terms<D><<<(unsigned)((rows * kLanes + 255) / 256), 256, 0, s>>>(x, w.L2, w.delta);
+  const int nk = key_blocks(a) * a.batch * a.kv_heads * p.kv.chunks;
+  const int nq = row_blocks(a) * a.batch * (a.heads / a.pack) * p.q.chunks;
+  const size_t q_tiles = 4 * (size_t)kTileK * 2 * D;
+  const bool cap = a.cap > 0.f;
+#define PB_BWD(C, B)                                                                              \
+  do {                                                                                            \
+    size_t lds = std::max((size_t)KvLds<D, B>::kBytes, q_tiles);                                  \
+    if (B == kTable)                                                                              \
+      lds = std::max((size_t)KvLds<D, B>::bias(a).bytes,                                          \
+                     (size_t)BiasLds((int)q_tiles, a.buckets, a.pack,                             \
+                                     (kBlockQ + a.pack - 1) / a.pack + 1, kTileK).bytes);         \
+    score_bwd_bf16<D, C, B><<<(unsigned)(nk + nq), 256, lds, s>>>(x, w, nk, nq);                  \
+  } while (0)
+  const int bias = a.slopes ? kSlopes : a.table ? kTable : kNoBias;
+  if (cap) {
+    if (bias == kTable) PB_BWD(true, kTable);
+    else if (bias == kSlopes) PB_BWD(true, kSlopes);
+    else PB_BWD(true, kNoBias);
+  } else {
+    if (bias == kTable) PB_BWD(false, kTable);
+    else if (bias == kSlopes) PB_BWD(false, kSlopes);
+    else PB_BWD(false, kNoBias);
+  }
+#undef PB_BWD
+  if (p.kv.chunks > 1)
+    score_bwd_merge<D, true><<<(unsigned)((keys * (D / 8) + 255) / 256), 256, 0, s>>>(x, w);
+  if (p.q.chunks > 1)
+    score_bwd_merge<D, false><<<(unsigned)((rows * (D / 8) + 255) / 256), 256, 0, s>>>(x, w);
+  if (!a.dtable) return;
+  const int nblk = row_blocks(a);
+  const unsigned grid = (unsigned)(nblk * a.batch * (a.heads / a.pack));
+  const BiasLds bl(2 * kTileK * 2 * D, a.buckets, a.pack, (kBlockQ + a.pack - 1) / a.pack + 1,
+                   kTileK);
+  const size_t lds = bl.bytes + (size_t)4 * a.buckets * 65 * 4 + bl.stride;
+  if (cap) score_dtable_bf16<D, true><<<grid, 256, lds, s>>>(x, w, nblk);
+  else score_dtable_bf16<D, false><<<grid, 256, lds, s>>>(x, w, nblk);
+  launch_score_dtable_sum(x, nblk * a.batch, s);
+}
+
+}  // namespace
+
+size_t score_bwd_bytes(int head_dim, const ScoreArgs& a, const ScoreBwdPlan& p) {
+  return bwd_layout(head_dim, a, p).total * sizeof(float);
+}
+
+// Row tiles of a key block and a set of heads.
+static int most_row_tiles(const ScoreArgs& a) {
+  const long long all = ((long long)a.seq_q * a.pack + kTileQ - 1) / kTileQ;
+  const long long reach = (long long)(a.causal ? 1 : 2) * a.window + kBlockK;
+  return (int)(a.prefix ? all : std::min(all, reach * a.pack / kTileQ + 2));
+}
+
+ScoreBwdPlan score_bwd_whole(const ScoreArgs& a) {
+  return ScoreBwdPlan{{1 << 30, a.group / a.pack}, {1 << 30, 1}};
+}
+ScoreBwdPlan score_bwd_plan(int head_dim, const ScoreArgs& a) {
+  ScoreBwdPlan p = score_bwd_whole(a);
+  const int sets = p.kv.chunks;
+  const long long nk = (long long)key_blocks(a) * a.batch * a.kv_heads * sets;
+  const long long nq = (long long)row_blocks(a) * a.batch * (a.heads / a.pack);
+  const int kv = most_row_tiles(a), q = score_most_tiles(a, kBlockQ, kTileK);
+  // Times of a tile, and of all workgroups over the chip's 512 places (under a causal
+  // mask blocks have half the longest one's tiles, on average).
+  const double kv_us = 1.3, q_us = 2.6;
+  const double half = a.causal && !a.prefix && a.window >= a.seq_k ? 0.5 : 1.0;
+  const double all = half * (nk * kv_us * kv + nq * q_us * q) / 512;
+  const double target = std::max(0.6 * all, 25.0);
+  auto cut = [&](ScorePlan& s, int tiles, double us) {
+    const int want = (int)std::ceil(tiles * us / target);
+    const int m = std::min(want, (tiles + 3) / 4);
+    if (m < 2) return;
+    const int chunk = (tiles + m - 1) / m, chunks = (tiles + chunk - 1) / chunk;
+    if (chunks > 1) s.chunk = chunk, s.chunks *= chunks;
+  };
+  cut(p.kv, kv, kv_us);
+  cut(p.q, q, q_us);
+  return p;
+}
+
+void launch_score_backward_bf16(int head_dim, const ScoreArgs& a, const ScoreBwdPlan& p, void* ws,
+                                hipStream_t s) {
+  if (head_dim == 64) bwd_d<64>(a, p, (float*)ws, s);
+  else if (head_dim == 96) bwd_d<96>(a, p, (float*)ws, s);
+  else bwd_d<128>(a, p, (float*)ws, s);
+}
+
+}  // namespace pb

@@ -290,7 +290,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
     }
     if constexpr (BIAS == kTable) {
       const int u = bias_uniform(a, bias_last, p_first - kv0 - TL + 1, p_last - kv0);
-      const float* bt = (const float*)(smem + bl.tile[i & 1]);
+      const float* bt = (const float*)(smem + bl.tile(i & 1, a.pack));
       if (u < 0) {
 #pragma unroll
         for (int j = 0; j < 2; ++j)

@@ -87,7 +87,7 @@ void bwd_td(const ScoreArgs& a, hipStream_t s) {
   const int blocks = (a.seq_q + kScoreBiasRows - 1) / kScoreBiasRows;
   score_dtable<T, D><<<(unsigned)(blocks * a.heads * a.batch), 256,
                        (size_t)4 * a.buckets * 64 * 4, s>>>(a, blocks);
-  score_dtable_sum<<<(unsigned)(a.heads * a.buckets), 64, 0, s>>>(a, blocks * a.batch);
+  launch_score_dtable_sum(a, blocks * a.batch, s);
 }
 #define PB_BY_TYPE(fn, ...)                                   \
   do {                                                        \
@@ -108,6 +108,9 @@ void fwd_td(const ScoreArgs& a, hipStream_t s) {
 
 }  // namespace
 
+void launch_score_dtable_sum(const ScoreArgs& a, int parts, hipStream_t s) {
+  score_dtable_sum<<<(unsigned)(a.heads * a.buckets), 64, 0, s>>>(a, parts);
+}
 void launch_score_forward(Dt dt, int head_dim, const ScoreArgs& a, hipStream_t s) {
   PB_BY_TYPE(fwd_td, a, s);
 }

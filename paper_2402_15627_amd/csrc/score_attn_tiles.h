@@ -166,16 +166,16 @@ struct Cap {
 struct BiasLds {
   static constexpr int kMap = 512;
   int stride;  // floats of a head's biases in a tile
-  int tab, first, map, tile[2], bytes;
+  int tab, first, map, tile0, bytes;
   __host__ __device__ BiasLds(int at, int buckets, int pack, int positions, int keys) {
     stride = positions + keys;  // (one spare: an odd stride for even sizes)
     tab = at;
     first = tab + 4 * buckets * pack;
     map = first + 4 * kScoreMaxBuckets;
-    tile[0] = map + kMap;
-    tile[1] = tile[0] + 4 * stride * pack;
-    bytes = tile[1] + 4 * stride * pack;
+    tile0 = map + kMap;
+    bytes = tile0 + 8 * stride * pack;
   }
+  PB_DEV int tile(int buf, int pack) const { return tile0 + buf * 4 * stride * pack; }
 };
 // Tables of a workgroup (its first barrier comes after): heads h0 .. h0 + pack - 1.
 PB_DEV void bias_prologue(const ScoreArgs& a, const BiasLds& l, unsigned char* smem, int h0,
@@ -218,7 +218,7 @@ PB_DEV int bias_uniform(const ScoreArgs& a, int last, int n0, int n1) {
 // Biases of a tile: entry x of a head is of distance top - x.
 PB_DEV void bias_tile(const ScoreArgs& a, const BiasLds& l, unsigned char* smem, int buf, int pack,
                       int top, int tid, int threads) {
-  float* out = (float*)(smem + l.tile[buf]);
+  float* out = (float*)(smem + l.tile(buf, pack));
   const float* tab = (const float*)(smem + l.tab);
   for (int x = tid; x < l.stride; x += threads) {
     const int k = bias_bucket(a, l, smem, top - x);
