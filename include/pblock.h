@@ -739,7 +739,8 @@ pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s,
  * Both are read on the device; offsets out of range are clamped (nothing outside the
  * tensors is touched).  What a mask hides does not enter any result, whatever it holds
  * (infinities and NaN too).  A query that sees nothing has o = 0, lse = -infinity and
- * no part in any gradient; so has one whose every score is -infinity.
+ * no part in any gradient; so has one whose every score is -infinity.  A table entry
+ * below -1e38 (the lowest value, as some programs mask with) counts as -infinity.
  *
  * bucket(n), of n = p - j: the first half of the buckets is of one distance each, the
  * others grow in the logarithm up to max_distance, from which on all is the last

@@ -33,6 +33,7 @@ EXTRA = {
     "attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-mllvm", "-disable-lsr"],
     "score_attn_fwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-mllvm", "-disable-lsr"],
     "score_attn_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "score_attn_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "attn_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 

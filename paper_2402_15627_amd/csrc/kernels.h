@@ -458,7 +458,9 @@ void launch_score_backward_bf16(int head_dim, const ScoreArgs& a, const ScoreBwd
                                 hipStream_t s);
 // dtable from a.bias_part, [parts][heads][buckets]
 void launch_score_dtable_sum(const ScoreArgs& a, int parts, hipStream_t s);
-void launch_score_forward(Dt dt, int head_dim, const ScoreArgs& a, hipStream_t s);
-void launch_score_backward(Dt dt, int head_dim, const ScoreArgs& a, hipStream_t s);
+// The fp32 forms, never split; a.bias_part has this many floats.
+size_t score_bias_part_floats_f32(const ScoreArgs& a);
+void launch_score_forward_f32(int head_dim, const ScoreArgs& a, hipStream_t s);
+void launch_score_backward_f32(int head_dim, const ScoreArgs& a, hipStream_t s);
 
 }  // namespace pb

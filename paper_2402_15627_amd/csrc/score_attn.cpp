@@ -62,13 +62,6 @@ void borders_of(const pb_score_attn_config* c, int* first) {
   }
 }
 
-int bias_blocks(const pb_score_attn_config* c) {
-  return (c->seq_q + pb::kScoreBiasRows - 1) / pb::kScoreBiasRows;
-}
-size_t bias_bytes(const pb_score_attn_config* c) {
-  return align256((size_t)c->batch * bias_blocks(c) * c->heads * c->buckets * 4);
-}
-
 // A tensor's rows (in bytes), by name.
 struct Named {
   const char* name;
@@ -153,7 +146,7 @@ size_t fwd_bytes(const pb_score_attn_config* c) {
 
 // min: without room for partial results.
 size_t bwd_bytes(const pb_score_attn_config* c, bool min) {
-  if (c->dtype != PB_BF16) return bias_bytes(c);
+  if (c->dtype != PB_BF16) return align256(4 * pb::score_bias_part_floats_f32(args_of(c, &kNoTerms)));
   size_t most = 0;
   for (int prefix = 0; prefix < 2; ++prefix) {
     pb::ScoreArgs a = args_of(c, &kNoTerms);
@@ -216,7 +209,7 @@ pb_status pblock_score_attn_forward(const pb_score_attn_config* cfg, const pb_sc
     if (!ws || ws_bytes < pb::score_fwd_part_bytes(cfg->head_dim, a, p)) p = {1 << 30, 1};
     pb::launch_score_forward_bf16(cfg->head_dim, a, p, ws, stream);
   } else {
-    pb::launch_score_forward(dt_of(cfg->dtype), cfg->head_dim, a, stream);
+    pb::launch_score_forward_f32(cfg->head_dim, a, stream);
   }
   return finish_launches();
 }
@@ -272,7 +265,7 @@ pb_status pblock_score_attn_backward(const pb_score_attn_config* cfg, const pb_s
     if (ws_bytes < pb::score_bwd_bytes(cfg->head_dim, a, p)) p = pb::score_bwd_whole(a);
     pb::launch_score_backward_bf16(cfg->head_dim, a, p, ws, stream);
   } else {
-    pb::launch_score_backward(dt_of(cfg->dtype), cfg->head_dim, a, stream);
+    pb::launch_score_backward_f32(cfg->head_dim, a, stream);
   }
   return finish_launches();
 }

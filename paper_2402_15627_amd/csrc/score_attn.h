@@ -10,7 +10,6 @@
 namespace pb {
 
 constexpr int kScoreMaxBuckets = 64;
-constexpr int kScoreBiasRows = 64;  // rows of a workgroup of the table's gradient
 
 struct ScoreArgs {
   const void *q, *k, *v;
@@ -31,7 +30,7 @@ struct ScoreArgs {
   int buckets, side;            // side: buckets of one sign of the distance
   int first[kScoreMaxBuckets];  // first distance of each bucket of a side
   float* dtable;
-  float* bias_part;             // [batch * row blocks][heads][buckets]
+  float* bias_part;             // sums of the table's gradient, [batch * row blocks][heads][buckets]
   int pack;                     // heads of one key head that a block of rows holds
 };
 
@@ -109,6 +108,11 @@ PB_DEV int bucket_of(const ScoreArgs& a, int n) {
   return lo + (!a.causal && n < 0 ? a.side : 0);
 }
 
+// A bias of the type's lowest value masks, as -infinity does (sums with it would lose
+// the score, and the softmax's base 2 has no room for it).
+constexpr float kMasks = -1e38f;
+PB_DEV float bias_value(float v) { return v < kMasks ? kNegInf : v; }
+
 // ---------------------------------------------------- rows by the definition
 // One wave a row, 64 keys (or queries) at a time, a lane each; the products with rows
 // of V, K, Q or dO then take features e = lane + 64 n, one visible row after another.
@@ -136,7 +140,7 @@ PB_DEV float score_of(const ScoreArgs& a, float dot, int h, int n, float& slope)
     slope = (1.f - t) * (1.f + t);
   }
   if (a.slopes) s = fmaf(-a.slopes[h], (float)abs(n), s);
-  if (a.table) s += a.table[(size_t)bucket_of(a, n) * a.heads + h];
+  if (a.table) s += bias_value(a.table[(size_t)bucket_of(a, n) * a.heads + h]);
   return s;
 }
 PB_DEV float lane_value(float v, int lane) {

@@ -94,7 +94,7 @@ PB_DEV KeyTiles key_tiles(const ScoreArgs& a, int b, int p0, int p1, int lane) {
   return k;
 }
 
-// cap tanh(scale u / cap) log2 e.  Tiles differ in how far their scores go, so a wave
+// cap tanh(scale u / cap) times a unit (log2 e for base 2).  Tiles differ in how far their scores go, so a wave
 // looks at its largest |scale u / cap| first: to 1/8 three terms in x^2 are good to
 // 2^-24, to 1/2 five, beyond 1 - 2 / (1 + e^(2|x|)) takes over from 1/2 on.  (An
 // exponential and a reciprocal take eight instructions' time each.)
@@ -102,14 +102,14 @@ struct Cap {
   float small, mid;      // bounds of |u|
   float a0, a1, a2;      // x <= 1/8: z = u (a0 + a1 u^2 + a2 u^4)
   float b0, b1, b2, b3, b4;
-  float two, top;        // 2 scale / cap log2 e, cap log2 e
-  PB_DEV Cap(float scale, float cap) {
-    const float k = scale / cap, k2 = k * k, s = scale * kLog2e;
+  float two, top;        // 2 scale / cap log2 e, cap
+  PB_DEV Cap(float scale, float cap, float unit = kLog2e) {
+    const float k = scale / cap, k2 = k * k, s = scale * unit;
     small = 0.125f / k, mid = 0.5f / k;
     a0 = s * kA0, a1 = s * kA1 * k2, a2 = s * kA2 * k2 * k2;
     b0 = s * kB0, b1 = s * kB1 * k2, b2 = s * kB2 * (k2 * k2), b3 = s * kB3 * (k2 * k2 * k2),
     b4 = s * kB4 * (k2 * k2) * (k2 * k2);
-    two = 2.f * k * kLog2e, top = cap * kLog2e;
+    two = 2.f * k * kLog2e, top = cap * unit;
   }
   // tanh(x) / x in x^2 of least largest relative error (by Remez exchange): 7e-9 to 1/8,
   // 1.4e-8 to 1/2; in fp32 4.3e-8 and 6.5e-8
@@ -157,7 +157,7 @@ struct Cap {
   }
 };
 
-// Biases of learned buckets in base 2.  A tile of NP positions and NK keys has NP + NK -
+// Biases of learned buckets.  A tile of NP positions and NK keys has NP + NK -
 // 1 distances: where they span buckets, the workgroup writes the bias of each (for each
 // of the block's heads) into LDS a tile ahead, key after key in ascending order, so that
 // a lane reads runs of neighbours; beyond the last bucket's first distance one value
@@ -177,14 +177,13 @@ struct BiasLds {
   }
   PB_DEV int tile(int buf, int pack) const { return tile0 + buf * 4 * stride * pack; }
 };
-// Tables of a workgroup (its first barrier comes after): heads h0 .. h0 + pack - 1.
+// Tables of a workgroup (its first barrier comes after): heads h0 .. h0 + pack - 1, times a
+// unit.
 PB_DEV void bias_prologue(const ScoreArgs& a, const BiasLds& l, unsigned char* smem, int h0,
-                          int pack, int tid, int threads) {
+                          int pack, int tid, int threads, float unit = kLog2e) {
   float* tab = (float*)(smem + l.tab);
   for (int x = tid; x < a.buckets * pack; x += threads) {
-    // (a bias of the type's lowest value stays finite in base 2)
-    const float v = a.table[(size_t)(x / pack) * a.heads + h0 + x % pack];
-    tab[x] = v < -2.3e38f && v > score::kNegInf ? -3.4e38f : v * kLog2e;
+    tab[x] = score::bias_value(a.table[(size_t)(x / pack) * a.heads + h0 + x % pack]) * unit;
   }
   int* first = (int*)(smem + l.first);
   if (tid < a.side) first[tid] = a.first[tid];
