@@ -206,7 +206,7 @@ pb_status pblock_score_attn_forward(const pb_score_attn_config* cfg, const pb_sc
   a.o = o, a.ld_o = (int)ld_o, a.lse = lse;
   if (cfg->dtype == PB_BF16) {
     pb::ScorePlan p = pb::score_fwd_plan(cfg->head_dim, a);
-    if (!ws || ws_bytes < pb::score_fwd_part_bytes(cfg->head_dim, a, p)) p = {1 << 30, 1};
+    if (!ws || ws_bytes < pb::score_fwd_part_bytes(cfg->head_dim, a, p)) p = {1};
     pb::launch_score_forward_bf16(cfg->head_dim, a, p, ws, stream);
   } else {
     pb::launch_score_forward_f32(cfg->head_dim, a, stream);

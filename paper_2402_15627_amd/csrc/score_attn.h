@@ -34,9 +34,9 @@ struct ScoreArgs {
   int pack;                     // heads of one key head that a block of rows holds
 };
 
-// How a block's tiles are divided: `chunks` workgroups of at most `chunk` tiles each.
+// How many workgroups may share a block's tiles.
 struct ScorePlan {
-  int chunk, chunks;
+  int chunks;
 };
 struct ScoreBwdPlan {
   ScorePlan kv, q;  // dK and dV by tiles of rows, dQ by tiles of keys

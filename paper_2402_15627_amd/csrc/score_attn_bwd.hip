@@ -2,12 +2,13 @@
 //
 // Row terms (lse in base 2, delta = sum of dO O) come from a pass of their own, laid out
 // in the order of the blocks' rows.  Then one launch has two roles, as in attn.hip:
-//   dK, dV: 64 keys, a "P" and a "dS" wave for 32 each, over 32-row tiles of the heads
-//     that share the key head, so that the gradients of shared heads are one sum (of
-//     more than eight heads several, merged in order);
+//   dK, dV: 128 keys over 32-row tiles of the heads that share the key head, so that the
+//     gradients of shared heads are one sum (of more than eight heads several, merged in
+//     order);
 //   dQ: 128 rows over 64-key tiles.
-// P = 2^(s - lse) with the scores' terms as in the forward; with a cap the P wave hands
-// P (1 - tanh^2) on, which is what dS = P (dP - delta) needs for dQ and dK.
+// P = 2^(s - lse) with the scores' terms as in the forward, dS = P (dP - delta), times
+// 1 - tanh^2 with a cap for dQ and dK.  How many tiles a block has depends on documents
+// that only the device knows, so a block that the plan cuts shares its own tiles out.
 //
 // The table's gradient sums dz = P (dP - delta) by bucket, and there delta has to be
 // better than sum of dO O, whose O is rounded: dQ's rows also give e = the sum of their
@@ -25,7 +26,7 @@ namespace {
 #define PB_INLINE __attribute__((always_inline))
 
 constexpr int kNoBias = 0, kSlopes = 1, kTable = 2;
-constexpr int kBlockK = 64, kTileQ = 32;   // dK, dV: keys of a workgroup, rows of a tile
+constexpr int kBlockK = 128, kTileQ = 32;  // dK, dV: keys of a workgroup, rows of a tile
 constexpr int kBlockQ = 128, kTileK = 64;  // dQ: rows of a workgroup, keys of a tile
 constexpr int kSums = 5;  // of a row: e; dz and P beyond the last bucket, of either side
 
@@ -74,21 +75,74 @@ __global__ __launch_bounds__(256) void score_terms(ScoreArgs a, float* __restric
   delta[to] = L == kNegInf ? 0.f : acc;
 }
 
-// A TL-row tile in the layout of dma_tile (attn_tiles.h), its rows' addresses from
-// row(0 .. TL - 1).
-template <int D, int TL, int NW, typename Row>
-PB_DEV void dma_rows(Row row, uint32_t lds_tile, int wave, int lane) {
+// A TL-row tile in the layout of dma_tile (attn_tiles.h): offset(0 .. TL - 1) is that of a
+// row from base, in bytes.
+template <int D, int TL, int NW, typename Offset>
+PB_DEV void dma_rows(const bf16* base, Offset offset, uint32_t lds_tile, int wave, int lane) {
   constexpr int RB = 2 * D, NP = TL * RB / 1024;
+  asm("" : "+v"(lane));  // (nothing derived from it is kept over a loop)
 #pragma unroll
   for (int i = 0; i < (NP + NW - 1) / NW; ++i) {
     const int pc = NP % NW == 0 ? wave * (NP / NW) + i : i * NW + wave;
     if (NP % NW != 0 && pc >= NP) break;  // wave-uniform
     const int p = pc * 1024 + 16 * lane;
     const int r = p / RB, slot = (p / 16) % (RB / 16);
-    dma16(row(r) + 8 * chunk_at<D>(r, slot),
-          __builtin_amdgcn_readfirstlane(lds_tile + pc * 1024));
+    dma16s(base, offset(r) + 16 * chunk_at<D>(r, slot),
+           __builtin_amdgcn_readfirstlane(lds_tile + pc * 1024));
   }
 }
+
+// A lane's places in a tile of dma_rows: its reads' addresses follow from three of them by
+// an exclusive or or an addition each (frag_row and frag_tr would keep one for each step
+// over the loop, some fifty registers).  Tiles begin at multiples of 256 bytes.
+template <int D>
+struct LaneReads {
+  uint32_t row[D == 96 ? 2 : 1];  // features 8 fh .. + 7 of row fr
+  uint32_t tr[2];                 // rows 4 fh + j and 8 more, features (fr & 16) + 4 q
+  PB_DEV explicit LaneReads(int lane) {
+    const int fr = lane & 31, fh = lane >> 5, i = lane & 15, j = i >> 2, q = i & 3;
+    row[0] = fr * 2 * D + 16 * chunk_at<D>(fr, fh);
+    if constexpr (D == 96) row[1] = fr * 2 * D + 16 * (chunk_at<D>(fr, fh) ^ 2);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int t = 4 * fh + j + 8 * k;
+      tr[k] = t * 2 * D + 16 * chunk_at<D>(t, 2 * (fr >> 4) + (q >> 1)) + 8 * (q & 1);
+    }
+  }
+  // the places in the tile at lds (a fresh copy: nothing derived is kept over a loop)
+  PB_DEV LaneReads at(uint32_t lds) const {
+    LaneReads x = *this;
+    x.row[0] += lds;
+    asm volatile("" : "+v"(x.row[0]));
+    if constexpr (D == 96) {
+      x.row[1] += lds;
+      asm volatile("" : "+v"(x.row[1]));
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      x.tr[k] += lds;
+      asm volatile("" : "+v"(x.tr[k]));
+    }
+    return x;
+  }
+  // 8 features of step ks, `bytes` further on
+  PB_DEV bf16x8 rows(int ks, int bytes) const {
+    if constexpr (D == 96) return lds_b128(row[ks & 1] + 64 * (ks >> 1) + bytes);
+    else return lds_b128((row[0] ^ (32 * ks)) + bytes);
+  }
+  // 8 rows (as frag_tr) of features 32 db + fr, k-step s
+  PB_DEV bf16x8 cols(int db, int s, int bytes) const {
+    const int more = s * 16 * 2 * D + bytes;
+    if constexpr (D == 96) return lds_tr_pair(tr[0] + 64 * db + more, tr[1] + 64 * db + more);
+    else return lds_tr_pair((tr[0] ^ (64 * db)) + more, (tr[1] ^ (64 * db)) + more);
+  }
+  static PB_DEV bf16x8 lds_tr_pair(uint32_t x, uint32_t y) {
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PB_LDS s16x4*)x);
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PB_LDS s16x4*)y);
+    const bf16x4 a4 = __builtin_bit_cast(bf16x4, a), b4 = __builtin_bit_cast(bf16x4, b);
+    return bf16x8{a4[0], a4[1], a4[2], a4[3], b4[0], b4[1], b4[2], b4[3]};
+  }
+};
 
 // Scores to base 2, with the cap.
 template <bool CAP, int N>
@@ -109,21 +163,35 @@ PB_DEV float cap_slope(float z, float it) {
 }
 
 struct BwdWork {
-  float *L2, *delta;           // row terms, in the blocks' order
-  float *pdk, *pdv, *pdq;      // partial results of split blocks
-  float* sums;                 // [chunk][kSums][rows] (with dtable)
-  int kv_cs, kv_nc, q_cs, q_nc;
+  float *L2, *delta;        // row terms, in the blocks' order
+  float *pdk, *pdv, *pdq;   // partial results of split blocks, [chunk][row][D]
+  float* sums;              // [chunk][kSums][rows] (with dtable)
+  int *kv_used, *q_used;    // chunks of each block, [set][batch, head][block]
+  int kv_nc, q_nc;          // at most
 };
+constexpr int kMinTilesKv = 12, kMinTilesQ = 4;  // of a chunk
+__host__ __device__ inline int row_blocks(const ScoreArgs& a) {
+  return (a.seq_q * a.pack + kBlockQ - 1) / kBlockQ;
+}
+__host__ __device__ inline int key_blocks(const ScoreArgs& a) {
+  return (a.seq_k + kBlockK - 1) / kBlockK;
+}
 
 // ------------------------------------------------------------------ dK, dV
-template <int D, int BIAS>
+// A wave has 32 keys: K and both accumulators in registers, V in LDS beside the row
+// tiles (each with its row terms, positions and biases), which all four waves share.
+// S = Q K^T and dP = dO V^T come out with a key a lane and four rows an element group;
+// P and dS go from there into dV^T += dO^T P and dK^T += Q^T dS.
+// (A "P" and a "dS" wave for each 32 keys, as in attn.hip, take 24 registers less but
+// hand P over through LDS: the wave with the scores' terms has twice the other's work,
+// and each waits for the other once a tile.)
+template <int D>
 struct KvLds {
-  static constexpr int kStages = D == 128 && BIAS == kTable ? 3 : 4;
+  static constexpr int kV = kBlockK * 2 * D;
   static constexpr int kTile = kTileQ * 2 * D;
   // Q, dO, then of each row: lse, delta, position, and its bias (slope, place or value)
   static constexpr int kStage = 2 * kTile + 4 * kTileQ * 4;
-  static constexpr int kP = 64 * 16 * 4;  // one wave's P
-  static constexpr int kBytes = kStages * kStage + 2 * kP;
+  static constexpr int kBytes = kV + 2 * kStage;
   static __host__ __device__ BiasLds bias(const ScoreArgs& a) {
     return BiasLds(kBytes, a.buckets, a.pack, (kTileQ + a.pack - 1) / a.pack + 1, kBlockK);
   }
@@ -132,28 +200,27 @@ struct KvLds {
 template <int D, bool CAP, int BIAS>
 PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
   constexpr int TL = kTileQ, NB = kBlockK, TB = TL * 2 * D;
-  using L = KvLds<D, BIAS>;
-  constexpr int NS = L::kStages, STAGE = L::kStage;
+  using L = KvLds<D>;
+  constexpr int STAGE = L::kStage;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(PB_LDS unsigned char*)smem;
   const int b = hb / a.kv_heads, kvh = hb % a.kv_heads;
   // chunk: a set of heads, and a run of its row tiles
   const int parts = a.group / a.pack, subs = w.kv_nc / parts;
-  const int chunk = bx % w.kv_nc, k0 = bx / w.kv_nc * NB;
-  const int h0 = kvh * a.group + chunk / subs * a.pack;
+  const int chunk = bx % w.kv_nc, kblk = bx / w.kv_nc, k0 = kblk * NB;
+  const int set = chunk / subs, h0 = kvh * a.group + set * a.pack;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int grp = wave & 1;
-  const bool pside = wave < 2;
   const int fr = lane & 31, fh = lane >> 5;
-  const int off = a.seq_k - a.seq_q, rows = a.seq_q * a.pack;
+  const int off = a.seq_k - a.seq_q;
   const Packed pk(a.pack);
-  const int key = k0 + 32 * grp + fr, key_c = min(key, a.seq_k - 1);
+  const int key = k0 + 32 * wave + fr, key_c = min(key, a.seq_k - 1);
 
-  // queries that see the lane's key: positions sf .. sf + sn - 1; all keys' together
+  // queries that see the lane's key: positions sf .. sf + sn - 1; all keys' together, and
+  // the wave's: any of them, and all
   int sf = 0, sn = 0, lo = 0x7fffffff, hi = -1;
-  {
-    const int j = k0 + lane;  // (64 keys, a lane each)
+  for (int x = 0; x < NB / 64; ++x) {
+    const int j = k0 + 64 * x + lane;
     int f = 0, n = 0;
     if (j < a.seq_k) {
       const Bounds d = bounds_of(a, b, j);
@@ -162,84 +229,70 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
         n = max(score::seen_last(a, d, j) - f + 1, 0);
       }
     }
-    if (n > 0) lo = f, hi = f + n - 1;
-    lo = wave_imin(lo), hi = wave_imax(hi);
-    sf = __shfl(f, 32 * grp + fr, 64);
-    sn = __shfl(n, 32 * grp + fr, 64);
+    if (n > 0) lo = min(lo, f), hi = max(hi, f + n - 1);
+    if (wave / 2 == x) {
+      sf = __shfl(f, 32 * (wave & 1) + fr, 64);
+      sn = __shfl(n, 32 * (wave & 1) + fr, 64);
+    }
   }
+  lo = wave_imin(lo), hi = wave_imax(hi);
+  const int any_lo = wave_imin(sn > 0 ? sf : 0x7fffffff), any_hi = wave_imax(sf + sn - 1);
+  const int all_lo = wave_imax(sn > 0 ? sf : 0x7fffffff), all_hi = wave_imin(sf + sn - 1);
   const int r_lo = hi < 0 ? 0 : (lo - off) * a.pack, r_hi = hi < 0 ? -1 : (hi - off + 1) * a.pack - 1;
-  const int t_lo = r_lo / TL, per = hi < 0 ? 0 : r_hi / TL - t_lo + 1;
-  const int t_begin = chunk % subs * w.kv_cs, nt = min(per - t_begin, w.kv_cs);
-  const bool split = w.kv_nc > 1;
-  const size_t keys = (size_t)a.batch * a.kv_heads * a.seq_k;
-  if (nt <= 0) {  // nobody sees these keys (the merge counts a split block's chunks itself)
-    bf16* out = (bf16*)pick(pside, a.dv, a.dk) + ((size_t)b * a.seq_k + key) * a.ld_dkv + kvh * D;
-    if (!split && key < a.seq_k)
-      for (int e = 8 * fh; e < D; e += 16) *reinterpret_cast<u32x4*>(out + e) = u32x4{0, 0, 0, 0};
-    if (split && key < a.seq_k) {
-      float* prow = pick(pside, w.pdv, w.pdk) +
-                    ((size_t)chunk * keys + (size_t)hb * a.seq_k + key) * D;
-      for (int e = 4 * fh; e < D; e += 8) *reinterpret_cast<f32x4*>(prow + e) = zero4();
+  const int t_lo = r_lo / TL, tiles = hi < 0 ? 0 : r_hi / TL - t_lo + 1;
+  const Share share(tiles, subs, kMinTilesKv);
+  const int t_begin = chunk % subs * share.size, nt = min(tiles - t_begin, share.size);
+  const bool split = parts > 1 || share.used > 1;
+  if (w.kv_nc > 1 && tid == 0 && chunk % subs == 0)
+    w.kv_used[((size_t)set * a.batch * a.kv_heads + hb) * key_blocks(a) + kblk] = share.used;
+  if (nt <= 0) {
+    if (chunk % subs || split) return;  // fewer chunks than there may be
+    for (int x = tid; x < NB * (D / 8); x += 256) {  // nobody sees these keys
+      const int j = k0 + x / (D / 8);
+      if (j >= a.seq_k) break;
+      const size_t at = ((size_t)b * a.seq_k + j) * a.ld_dkv + kvh * D + 8 * (x % (D / 8));
+      *reinterpret_cast<u32x4*>((bf16*)a.dk + at) = u32x4{0, 0, 0, 0};
+      *reinterpret_cast<u32x4*>((bf16*)a.dv + at) = u32x4{0, 0, 0, 0};
     }
     return;
   }
-  // keys that every query of a tile has to lie between for the wave's tile to be whole
-  int full_lo = sn > 0 ? sf : 0x7fffffff, full_hi = sf + sn - 1;
-#pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) {
-    full_lo = max(full_lo, __shfl_xor(full_lo, o, 64));
-    full_hi = min(full_hi, __shfl_xor(full_hi, o, 64));
-  }
-  full_lo = __builtin_amdgcn_readfirstlane(full_lo);
-  full_hi = __builtin_amdgcn_readfirstlane(full_hi);
 
-  const bf16* kvr = score::kv_row<bf16, D>(a, pick(pside, a.k, a.v), b, key_c, kvh);
-  bf16x8 kvf[D / 16];
-#pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks)
-    kvf[ks] = load_row_frag(kvr + 16 * ks + 8 * fh, key < a.seq_k);
-  f32x16 acc[D / 32];
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i) acc[i] = zero16();
-  const float c2 = a.scale * kLog2e;
-  const Cap cap(a.scale, CAP ? a.cap : 1.f);
-  const BiasLds bl = L::bias(a);
-  const int bias_last = BIAS == kTable ? a.first[a.side - 1] : 0;
-
-  float* pbuf = (float*)(smem + NS * STAGE + grp * L::kP);
   auto tile_row = [&](int i) PB_INLINE { return (t_lo + t_begin + i) * TL; };
   auto tile_span = [&](int i, int& p0, int& p1) PB_INLINE {  // positions of tile i
     const int r = tile_row(i);
     p0 = off + pk.pos(r);
     p1 = off + pk.pos(r + TL - 1);
   };
+  const BiasLds bl = L::bias(a);
+  const int bias_last = BIAS == kTable ? a.first[a.side - 1] : 0;
   auto uniform = [&](int i) PB_INLINE {
     int p0, p1;
     tile_span(i, p0, p1);
     return bias_uniform(a, bias_last, p0 - k0 - NB + 1, p1 - k0);
   };
-  const int per_stage = 2 * dma_pieces<D, TL, 4>(wave) + (wave == 0 ? 1 : 0);
+  const bf16* q0 = score::q_row<bf16, D>(a, b, 0, h0);
+  const bf16* g0 = score::do_row<bf16, D>(a, b, 0, h0);
+  const size_t row0 = packed_row(a, b * (a.heads / a.pack) + h0 / a.pack, 0);
   auto issue_stage = [&](int i) PB_INLINE {
-    const int s = i % NS, r0 = tile_row(i);
-    const uint32_t at = lds0 + s * STAGE;
-    const bf16* q = score::q_row<bf16, D>(a, b, 0, h0);
-    const bf16* g = score::do_row<bf16, D>(a, b, 0, h0);
-    auto row_of = [&](int r) { return max(r_lo, min(r0 + r, r_hi)); };
-    dma_rows<D, TL, 4>([&](int r) {
+    const int r0 = tile_row(i);
+    const uint32_t at = lds0 + L::kV + (i & 1) * STAGE;
+    // rows beyond those that see any of the keys are read from the nearest that do
+    auto row_of = [&](int r) PB_INLINE { return max(r_lo, min(r0 + r, r_hi)); };
+    const int y0 = pk.pos(max(r_lo, r0));  // (of the tile's first row that is read)
+    auto offset = [&](int r, int ld) PB_INLINE {
       const int x = row_of(r), y = pk.pos(x);
-      return q + (size_t)y * a.ld_q + (x - y * a.pack) * D;
-    }, at, wave, lane);
-    dma_rows<D, TL, 4>([&](int r) {
-      const int x = row_of(r), y = pk.pos(x);
-      return g + (size_t)y * a.ld_do + (x - y * a.pack) * D;
-    }, at + TB, wave, lane);
-    const size_t row0 = packed_row(a, b * (a.heads / a.pack) + h0 / a.pack, 0);
+      return (uint32_t)(y - y0) * (uint32_t)(2 * ld) + (uint32_t)(x - y * a.pack) * (2 * D);
+    };
+    dma_rows<D, TL, 4>(q0 + (size_t)y0 * a.ld_q,
+                       [&](int r) PB_INLINE { return offset(r, a.ld_q); }, at, wave, lane);
+    dma_rows<D, TL, 4>(g0 + (size_t)y0 * a.ld_do,
+                       [&](int r) PB_INLINE { return offset(r, a.ld_do); }, at + TB, wave, lane);
     if (wave == 0)
       dma4(pick(lane < 32, w.L2, w.delta) + row0 + row_of(lane & 31),
            __builtin_amdgcn_readfirstlane(at + 2 * TB));
     if (wave == 1 && lane < TL) {
       const int r = r0 + lane, y = pk.pos(r), hh = r - y * a.pack;
-      int* rows_of = (int*)(smem + s * STAGE + 2 * TB + 2 * TL * 4);
+      int* rows_of = (int*)(smem + L::kV + (i & 1) * STAGE + 2 * TB + 2 * TL * 4);
       rows_of[lane] = y + off;
       if constexpr (BIAS == kSlopes) ((float*)rows_of)[TL + lane] = -a.slopes[h0 + hh] * kLog2e;
       if constexpr (BIAS == kTable) {
@@ -254,6 +307,9 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
     tile_span(i, p0, p1);
     if (uniform(i) < 0) bias_tile(a, bl, smem, i & 1, a.pack, p1 - k0, tid, 256);
   };
+  dma_rows<D, NB, 4>(score::kv_row<bf16, D>(a, a.v, b, k0, kvh), [&](int r) PB_INLINE {
+    return (uint32_t)min(r, a.seq_k - 1 - k0) * (uint32_t)(2 * a.ld_kv);
+  }, lds0, wave, lane);
   if constexpr (BIAS == kTable) {
     bias_prologue(a, bl, smem, h0, a.pack, tid, 256);
     __syncthreads();
@@ -261,117 +317,152 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
     __syncthreads();
     build(0);
   }
+  issue_stage(0);
+  const bf16* kr = score::kv_row<bf16, D>(a, a.k, b, key_c, kvh);
+  bf16x8 kf[D / 16];
 #pragma unroll
-  for (int i = 0; i < NS - 1; ++i)
-    if (i < nt) issue_stage(i);
+  for (int ks = 0; ks < D / 16; ++ks) kf[ks] = load_row_frag(kr + 16 * ks + 8 * fh, key < a.seq_k);
+  f32x16 dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = zero16();
+  const float c2 = a.scale * kLog2e;
+  const Cap cap(a.scale, CAP ? a.cap : 1.f);
+  const float it = 1.f / cap.top;
+  const LaneReads<D> places(lane);
 
   for (int i = 0; i < nt; ++i) {
-    const int cur = i % NS;
-    wait_dma_upto(min(nt - 1 - i, NS - 2) * per_stage);
+    wait_dma_all();   // tile i, requested an iteration ago
     block_barrier();  // ... for every wave; and every wave is done with tile i - 1
-    if (i + NS - 1 < nt) issue_stage(i + NS - 1);
-    if constexpr (BIAS == kTable)
-      if (i + 1 < nt) build(i + 1);
-    const unsigned char* qt = smem + cur * STAGE;
-    const unsigned char* gt = qt + TB;
-    const float* ls = (const float*)(qt + 2 * TB);
-    // Lane holds key `key` and rows r0 + 8 j + 4 fh + i of element 4 j + i.
-    f32x16 sc[1] = {zero16()};  // S (P side) or dP (dS side)
-    const unsigned char* nt_ = pside ? qt : gt;
+    if (i + 1 < nt) {
+      issue_stage(i + 1);
+      if constexpr (BIAS == kTable) build(i + 1);
+    }
+    int p0, p1;
+    tile_span(i, p0, p1);
+    if (p1 < any_lo || p0 > any_hi) continue;
+    const uint32_t stage = L::kV + (i & 1) * STAGE;
+    const LaneReads<D> qr = places.at(lds0 + stage), vr = places.at(lds0 + 32 * wave * 2 * D);
+    const float* ls = (const float*)(smem + stage + 2 * TB);
+    const int* row_pos = (const int*)(ls + 2 * TL);
+    // Lane holds key `key` and rows r0 + 8 j + 4 fh + e of element 4 j + e.
+    f32x16 sc[1] = {zero16()}, dp = zero16();
+    // (fragments one step ahead of their products, and no further: registers)
+    bf16x8 fq[2], fg[2], fv[2];
+    auto read = [&](int ks) PB_INLINE {
+      fq[ks & 1] = qr.rows(ks, 0);
+      fg[ks & 1] = qr.rows(ks, TB);
+      fv[ks & 1] = vr.rows(ks, 0);
+    };
+    read(0);
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks)
-      sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_row<D>(nt_, fr, ks, fh), kvf[ks], sc[0],
-                                                      0, 0, 0);
-    if (pside) {
-      f32x16 slope;
-      const float it = 1.f / cap.top;
-      if constexpr (CAP || BIAS != kNoBias) to_base2<CAP>(cap, c2, sc);
-      if constexpr (CAP)
+    for (int ks = 0; ks < D / 16; ++ks) {
+      if (ks + 1 < D / 16) read(ks + 1);
+      sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[ks & 1], kf[ks], sc[0], 0, 0, 0);
+      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fg[ks & 1], fv[ks & 1], dp, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (CAP || BIAS != kNoBias) to_base2<CAP>(cap, c2, sc);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) slope[e] = cap_slope(sc[0][e], it);
-      const int* row_pos = (const int*)(ls + 2 * TL);
-      int p0, p1;
-      tile_span(i, p0, p1);
-      const bool full = p0 >= full_lo && p1 <= full_hi;
-      int u = 0;
-      if constexpr (BIAS == kTable) u = uniform(i);
+    for (int j = 0; j < 4; ++j) {
+      const f32x4 D4 = *reinterpret_cast<const f32x4*>(ls + TL + 8 * j + 4 * fh);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        dp[4 * j + e] -= D4[e];
+        if constexpr (CAP) dp[4 * j + e] *= cap_slope(sc[0][4 * j + e], it);
+      }
+    }
+    if constexpr (BIAS == kSlopes) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int at = 8 * j + 4 * fh;
-        const f32x4 L4 = *reinterpret_cast<const f32x4*>(ls + at);
-        const u32x4 P4 = *reinterpret_cast<const u32x4*>(row_pos + at);
-        const u32x4 X4 = *reinterpret_cast<const u32x4*>(row_pos + TL + at);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float v = sc[0][4 * j + e];
-          if constexpr (BIAS == kSlopes)
-            v = fmaf(__uint_as_float(X4[e]), fabsf((float)((int)P4[e] - key)), v);
-          if constexpr (BIAS == kTable)
-            v += u < 0 ? ((const float*)(smem + bl.tile(i & 1, a.pack)))[(int)X4[e] + key - k0]
-                       : __uint_as_float(X4[e]);
-          if (!full) v = (unsigned)((int)P4[e] - sf) < (unsigned)sn ? v : kNegInf;
-          const float p = exp2_hw(CAP || BIAS != kNoBias ? v - L4[e] : fmaf(v, c2, -L4[e]));
-          sc[0][4 * j + e] = p;
-        }
-        f32x4 out;
+        const u32x4 P4 = *reinterpret_cast<const u32x4*>(row_pos + 8 * j + 4 * fh);
+        const f32x4 X4 = *reinterpret_cast<const f32x4*>(row_pos + TL + 8 * j + 4 * fh);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          out[e] = CAP ? sc[0][4 * j + e] * slope[4 * j + e] : sc[0][4 * j + e];
-        *reinterpret_cast<f32x4*>(pbuf + (j * 64 + lane) * 4) = out;
+          sc[0][4 * j + e] = fmaf(X4[e], fabsf((float)((int)P4[e] - key)), sc[0][4 * j + e]);
       }
     }
-    block_barrier();  // P of this tile is visible to the dS side
-    if (!pside) {
+    if constexpr (BIAS == kTable) {
+      const bool near = uniform(i) < 0;
+      const float* bt = (const float*)(smem + bl.tile(i & 1, a.pack)) + (key - k0);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const f32x4 P4 = *reinterpret_cast<const f32x4*>(pbuf + (j * 64 + lane) * 4);
-        const f32x4 D4 = *reinterpret_cast<const f32x4*>(ls + TL + 8 * j + 4 * fh);
+        u32x4 X4 = *reinterpret_cast<const u32x4*>(row_pos + TL + 8 * j + 4 * fh);
+        if (near)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[0][4 * j + e] = P4[e] * (sc[0][4 * j + e] - D4[e]);
+          for (int e = 0; e < 4; ++e) X4[e] = __float_as_uint(bt[(int)X4[e]]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[0][4 * j + e] += __uint_as_float(X4[e]);
       }
     }
-    const unsigned char* tt = pside ? gt : qt;  // dO^T with P, Q^T with dS
+    if (!(p0 >= all_lo && p1 <= all_hi)) {
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
+      for (int j = 0; j < 4; ++j) {
+        const u32x4 P4 = *reinterpret_cast<const u32x4*>(row_pos + 8 * j + 4 * fh);
 #pragma unroll
-      for (int s2 = 0; s2 < TL / 16; ++s2)
-        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            frag_tr<D>(tt, 32 * db + fr, s2, fh, lane), probs_frag(sc, s2), acc[db], 0, 0, 0);
+        for (int e = 0; e < 4; ++e)
+          sc[0][4 * j + e] =
+              (unsigned)((int)P4[e] - sf) < (unsigned)sn ? sc[0][4 * j + e] : kNegInf;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const f32x4 L4 = *reinterpret_cast<const f32x4*>(ls + 8 * j + 4 * fh);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float z = sc[0][4 * j + e];
+        sc[0][4 * j + e] = exp2_hw(CAP || BIAS != kNoBias ? z - L4[e] : fmaf(z, c2, -L4[e]));
+        dp[4 * j + e] *= sc[0][4 * j + e];
+      }
+    }
+#pragma unroll
+    for (int s2 = 0; s2 < TL / 16; ++s2) {
+      const bf16x8 pf = probs_frag(sc, s2), df = probs_frag(&dp, s2);
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qr.cols(db, s2, TB), pf, dv[db], 0, 0, 0);
+        dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qr.cols(db, s2, 0), df, dk[db], 0, 0, 0);
+      }
+    }
   }
 
-  const float mul = pside ? 1.f : a.scale;
   if (split) {
     if (key >= a.seq_k) return;
-    float* prow = pick(pside, w.pdv, w.pdk) + ((size_t)chunk * keys + (size_t)hb * a.seq_k + key) * D;
+    const size_t keys = (size_t)a.batch * a.kv_heads * a.seq_k;
+    const size_t at = ((size_t)chunk * keys + (size_t)hb * a.seq_k + key) * D + 4 * fh;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<f32x4*>(prow + 32 * db + 8 * j + 4 * fh) =
-            f32x4{acc[db][4 * j] * mul, acc[db][4 * j + 1] * mul, acc[db][4 * j + 2] * mul,
-                  acc[db][4 * j + 3] * mul};
+      for (int j = 0; j < 4; ++j) {
+        f32x4 x, y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = dk[db][4 * j + e] * a.scale, y[e] = dv[db][4 * j + e];
+        *reinterpret_cast<f32x4*>(w.pdk + at + 32 * db + 8 * j) = x;
+        *reinterpret_cast<f32x4*>(w.pdv + at + 32 * db + 8 * j) = y;
+      }
     return;
   }
   float bad = 0.f;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) bad = fmaf(acc[db][e], 0.f, bad);
-  if (__syncthreads_or(key < a.seq_k && bad != 0.f)) {
-    for (int j = k0 + wave; j < min(k0 + NB, a.seq_k); j += 4)
+    for (int e = 0; e < 16; ++e) bad = fmaf(dk[db][e], 0.f, fmaf(dv[db][e], 0.f, bad));
+  if (__builtin_amdgcn_ballot_w64(key < a.seq_k && bad != 0.f)) {
+    const int j0 = k0 + 32 * wave;
+    for (int j = j0; j < min(j0 + 32, a.seq_k); ++j)
       score::dkdv_row<bf16, D>(a, b, kvh, j, lane);
     return;
   }
   if (key >= a.seq_k) return;
-  bf16* orow = (bf16*)pick(pside, a.dv, a.dk) + ((size_t)b * a.seq_k + key) * a.ld_dkv + kvh * D;
+  const size_t at = ((size_t)b * a.seq_k + key) * a.ld_dkv + kvh * D + 4 * fh;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      float v[4];
+      float x[4], y[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = acc[db][4 * j + e] * mul;
-      store4(orow + 32 * db + 8 * j + 4 * fh, v);
+      for (int e = 0; e < 4; ++e) x[e] = dk[db][4 * j + e] * a.scale, y[e] = dv[db][4 * j + e];
+      store4((bf16*)a.dk + at + 32 * db + 8 * j, x);
+      store4((bf16*)a.dv + at + 32 * db + 8 * j, y);
     }
 }
 
@@ -439,81 +530,67 @@ struct RowTiles {
     const int lo = max(kt.lo - kv0, 0), hi = min(kt.hi - kv0, kTileK - 1);
     const bf16 *k = score::kv_row<bf16, D>(a, a.k, b, kv0, kvh),
                *v = score::kv_row<bf16, D>(a, a.v, b, kv0, kvh);
-    dma_rows<D, kTileK, 4>([&](int x) { return k + (size_t)max(lo, min(x, hi)) * a.ld_kv; }, lds_k,
-                           wave, lane);
-    dma_rows<D, kTileK, 4>([&](int x) { return v + (size_t)max(lo, min(x, hi)) * a.ld_kv; }, lds_v,
-                           wave, lane);
+    auto offset = [&](int x) PB_INLINE {
+      return (uint32_t)max(lo, min(x, hi)) * (uint32_t)(2 * a.ld_kv);
+    };
+    dma_rows<D, kTileK, 4>(k, offset, lds_k, wave, lane);
+    dma_rows<D, kTileK, 4>(v, offset, lds_v, wave, lane);
   }
-  // P and dz of the lane's row and keys kv0 + 32 h2 + 8 j + 4 fh + e (element 4 j + e of
-  // h2).  see: the row's keys of the tile.  SLOPE: 0, dz as it is; 1, times what the cap
-  // leaves; 2, that apart, in slope.
+  // P and dz of the lane's row and keys kv0 + 32 h2 + 8 j + 4 fh + e (element 4 j + e).
+  // see: the row's keys of the tile.  SLOPE: 0, dz as it is; 1, times what the cap leaves;
+  // 2, that apart, in slope.
+  // kr: the lane's places in the K tile; V's is kTileK rows further on.
   template <int SLOPE>
-  PB_DEV void pair(int kv0, int buf, const unsigned char* kt, const unsigned char* vt,
-                   uint64_t see, f32x16 (&pr)[2], f32x16 (&dz)[2], f32x16 (&slope)[2]) {
+  PB_DEV void pair(int kv0, int h2, int buf, const LaneReads<D>& kr, uint64_t see,
+                    f32x16 (&pr)[1], f32x16 (&dz)[1], f32x16& slope) {
     const float c2 = a.scale * kLog2e;
+    pr[0] = zero16();
+    dz[0] = zero16();
 #pragma unroll
-    for (int h2 = 0; h2 < 2; ++h2) {
-      pr[h2] = zero16();
-      dz[h2] = zero16();
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {
-        pr[h2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_row<D>(kt, 32 * h2 + fr, ks, fh),
-                                                         qf[ks], pr[h2], 0, 0, 0);
-        dz[h2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_row<D>(vt, 32 * h2 + fr, ks, fh),
-                                                         gf[ks], dz[h2], 0, 0, 0);
-      }
+    for (int ks = 0; ks < D / 16; ++ks) {
+      pr[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr.rows(ks, 32 * h2 * 2 * D), qf[ks], pr[0], 0,
+                                                      0, 0);
+      dz[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr.rows(ks, (kTileK + 32 * h2) * 2 * D),
+                                                      gf[ks], dz[0], 0, 0, 0);
     }
     if constexpr (CAP || BIAS != kNoBias) to_base2<CAP>(cap, c2, pr);
     const float it = 1.f / cap.top;
 #pragma unroll
-    for (int h2 = 0; h2 < 2; ++h2)
-#pragma unroll
-      for (int x = 0; x < 16; ++x) {
-        dz[h2][x] -= dl;
-        if constexpr (CAP && SLOPE == 1) dz[h2][x] *= cap_slope(pr[h2][x], it);
-        if constexpr (CAP && SLOPE == 2) slope[h2][x] = cap_slope(pr[h2][x], it);
-      }
+    for (int x = 0; x < 16; ++x) {
+      dz[0][x] -= dl;
+      if constexpr (CAP && SLOPE == 1) dz[0][x] *= cap_slope(pr[0][x], it);
+      if constexpr (CAP && SLOPE == 2) slope[x] = cap_slope(pr[0][x], it);
+    }
     if constexpr (BIAS == kSlopes) {
-      const float d0 = (float)(p - kv0 - 4 * fh);
+      const float d0 = (float)(p - kv0 - 32 * h2 - 4 * fh);
 #pragma unroll
-      for (int h2 = 0; h2 < 2; ++h2)
-#pragma unroll
-        for (int x = 0; x < 16; ++x)
-          pr[h2][x] = fmaf(slope2, fabsf(d0 - (float)(32 * h2 + 8 * (x >> 2) + (x & 3))), pr[h2][x]);
+      for (int x = 0; x < 16; ++x)
+        pr[0][x] = fmaf(slope2, fabsf(d0 - (float)(8 * (x >> 2) + (x & 3))), pr[0][x]);
     }
     if constexpr (BIAS == kTable) {
       const int u = uniform(kv0);
-      const float* bt = (const float*)(smem + bl.tile(buf, a.pack)) + bias_at;
-      const float f =
-          u < 0 ? 0.f : ((const float*)(smem + bl.tab))[u * a.pack + h - h0];
       if (u < 0) {
+        const float* bt = (const float*)(smem + bl.tile(buf, a.pack)) + bias_at + 32 * h2;
 #pragma unroll
-        for (int h2 = 0; h2 < 2; ++h2)
-#pragma unroll
-          for (int x = 0; x < 16; ++x) pr[h2][x] += bt[32 * h2 + 8 * (x >> 2) + (x & 3)];
+        for (int x = 0; x < 16; ++x) pr[0][x] += bt[8 * (x >> 2) + (x & 3)];
       } else {
+        const float f = ((const float*)(smem + bl.tab))[u * a.pack + h - h0];
 #pragma unroll
-        for (int h2 = 0; h2 < 2; ++h2)
-#pragma unroll
-          for (int x = 0; x < 16; ++x) pr[h2][x] += f;
+        for (int x = 0; x < 16; ++x) pr[0][x] += f;
       }
     }
-    if (__builtin_amdgcn_ballot_w64(see != ~0ull)) {
-      const uint64_t mine = see >> (4 * fh);
-      const uint32_t half[2] = {(uint32_t)mine, (uint32_t)(mine >> 32)};
+    const uint32_t mine = (uint32_t)(see >> (32 * h2));
+    if (__builtin_amdgcn_ballot_w64(mine != ~0u)) {
+      const uint32_t bits = mine >> (4 * fh);
 #pragma unroll
-      for (int h2 = 0; h2 < 2; ++h2)
-#pragma unroll
-        for (int x = 0; x < 16; ++x)
-          pr[h2][x] = half[h2] & (1u << (8 * (x >> 2) + (x & 3))) ? pr[h2][x] : kNegInf;
+      for (int x = 0; x < 16; ++x)
+        pr[0][x] = bits & (1u << (8 * (x >> 2) + (x & 3))) ? pr[0][x] : kNegInf;
     }
 #pragma unroll
-    for (int h2 = 0; h2 < 2; ++h2)
-#pragma unroll
-      for (int x = 0; x < 16; ++x) {
-        pr[h2][x] = exp2_hw(CAP || BIAS != kNoBias ? pr[h2][x] - L2 : fmaf(pr[h2][x], c2, -L2));
-        dz[h2][x] *= pr[h2][x];
-      }
+    for (int x = 0; x < 16; ++x) {
+      pr[0][x] = exp2_hw(CAP || BIAS != kNoBias ? pr[0][x] - L2 : fmaf(pr[0][x], c2, -L2));
+      dz[0][x] *= pr[0][x];
+    }
   }
 };
 
@@ -526,8 +603,12 @@ PB_DEV void dq_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
   const int chunk = bx % w.q_nc;
   RowTiles<D, CAP, BIAS> t(a, w, smem, 4 * TB, nblk - 1 - bx / w.q_nc, hb);
   const KeyTiles kt = key_tiles<kTileK>(a, t.b, t.p_first, t.p_last, t.lane);
-  const int t_begin = chunk * w.q_cs, n = min(kt.n - t_begin, w.q_cs);
-  const bool split = w.q_nc > 1;
+  const Share share(kt.n, w.q_nc, kMinTilesQ);
+  const int t_begin = chunk * share.size, n = min(kt.n - t_begin, share.size);
+  const bool split = share.used > 1;
+  if (chunk >= max(share.used, 1)) return;
+  if (w.q_nc > 1 && threadIdx.x == 0 && chunk == 0)
+    w.q_used[(size_t)hb * nblk + nblk - 1 - bx / w.q_nc] = share.used;
   const size_t all = (size_t)a.batch * a.heads * a.seq_q;
   const size_t row = (size_t)chunk * all + packed_row(a, hb, min(t.r, t.rows - 1));
 
@@ -544,6 +625,7 @@ PB_DEV void dq_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
       t.build(kv_of(0), 0);
     }
     t.request(kt, kv_of(0), k_off(0), v_off(0));
+    const LaneReads<D> places(t.lane);
     for (int i = 0; i < n; ++i) {
       const int cur = i & 1, kv0 = kv_of(i);
       wait_dma_all();
@@ -554,41 +636,36 @@ PB_DEV void dq_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
       }
       const uint64_t see = t.keys.bits(kv0);
       if (!__builtin_amdgcn_ballot_w64(see != 0)) continue;
-      const unsigned char *kl = smem + (2 * cur) * TB, *vl = kl + TB;
-      f32x16 pr[2], dz[2], slope[2];
-      t.template pair<BIAS == kTable ? 2 : 1>(kv0, cur, kl, vl, see, pr, dz, slope);
-      if constexpr (BIAS == kTable) {
-        if (a.dtable) {
-          float s = 0.f, sp = 0.f;
+      const LaneReads<D> kr = places.at(lds0 + (2 * cur) * TB);
 #pragma unroll
-          for (int h2 = 0; h2 < 2; ++h2)
+      for (int h2 = 0; h2 < 2; ++h2) {
+        f32x16 pr[1], dz[1], slope;
+        t.template pair<BIAS == kTable ? 2 : 1>(kv0, h2, cur, kr, see, pr, dz, slope);
+        if constexpr (BIAS == kTable) {
+          if (a.dtable) {
+            float s = 0.f, sp = 0.f;
 #pragma unroll
-            for (int x = 0; x < 16; ++x) s += dz[h2][x];
-          sums[0] += s;
-          const int u = t.uniform(kv0);
-          if (u >= 0) {
+            for (int x = 0; x < 16; ++x) s += dz[0][x];
+            sums[0] += s;
+            const int u = t.uniform(kv0);
+            if (u >= 0) {
 #pragma unroll
-            for (int h2 = 0; h2 < 2; ++h2)
-#pragma unroll
-              for (int x = 0; x < 16; ++x) sp += pr[h2][x];
-            if (u == a.side - 1) sums[1] += s, sums[2] += sp;
-            else sums[3] += s, sums[4] += sp;
+              for (int x = 0; x < 16; ++x) sp += pr[0][x];
+              if (u == a.side - 1) sums[1] += s, sums[2] += sp;
+              else sums[3] += s, sums[4] += sp;
+            }
           }
+          if constexpr (CAP)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) dz[0][x] *= slope[x];
         }
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+          for (int s2 = 0; s2 < 2; ++s2)
+            dq[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                kr.cols(db, 2 * h2 + s2, 0), probs_frag(dz, s2), dq[db], 0, 0, 0);
       }
-      if constexpr (CAP && BIAS == kTable) {
-#pragma unroll
-        for (int h2 = 0; h2 < 2; ++h2)
-#pragma unroll
-          for (int x = 0; x < 16; ++x) dz[h2][x] *= slope[h2][x];
-      }
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int s2 = 0; s2 < kTileK / 16; ++s2)
-          dq[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              frag_tr<D>(kl, 32 * db + t.fr, s2, t.fh, t.lane), probs_frag(dz, s2), dq[db], 0, 0,
-              0);
     }
   }
   if constexpr (BIAS == kTable) {
@@ -676,7 +753,7 @@ __global__ __launch_bounds__(256) void score_dtable_bf16(ScoreArgs a, BwdWork w,
   const size_t all = (size_t)a.batch * a.heads * a.seq_q;
   float sums[kSums] = {0.f, 0.f, 0.f, 0.f, 0.f};
   if (t.r < t.rows)
-    for (int c = 0; c < w.q_nc; ++c)
+    for (int c = 0; c < (w.q_nc > 1 ? max(w.q_used[(size_t)hb * nblk + blk], 1) : 1); ++c)
 #pragma unroll
       for (int x = 0; x < kSums; ++x)
         sums[x] += w.sums[((size_t)c * kSums + x) * all + packed_row(a, hb, t.r)];
@@ -686,6 +763,7 @@ __global__ __launch_bounds__(256) void score_dtable_bf16(ScoreArgs a, BwdWork w,
     mine[(a.causal ? 0 : 2 * a.side - 1) * kPad] += fmaf(-sums[0], sums[4], sums[3]);
   }
   const KeyTiles kt = key_tiles<kTileK>(a, t.b, t.p_first, t.p_last, t.lane);
+  const LaneReads<D> places(t.lane);
   for (int i = 0; i < kt.n; ++i) {
     const int kv0 = kt.tile(i) * kTileK;
     if (t.uniform(kv0) >= 0) continue;
@@ -698,14 +776,16 @@ __global__ __launch_bounds__(256) void score_dtable_bf16(ScoreArgs a, BwdWork w,
     block_barrier();
     const uint64_t see = t.keys.bits(kv0);
     if (!__builtin_amdgcn_ballot_w64(see != 0)) continue;
-    f32x16 pr[2], dz[2], slope[2];
-    t.template pair<0>(kv0, 0, smem, smem + TB, see, pr, dz, slope);
+    const LaneReads<D> kr = places.at(lds0);
     const int at = t.p_last - t.p + 4 * t.fh;
 #pragma unroll
-    for (int h2 = 0; h2 < 2; ++h2)
+    for (int h2 = 0; h2 < 2; ++h2) {
+      f32x16 pr[1], dz[1], slope;
+      t.template pair<0>(kv0, h2, 0, kr, see, pr, dz, slope);
 #pragma unroll
       for (int x = 0; x < 16; ++x)
-        unsafeAtomicAdd(&mine[ids[at + 32 * h2 + 8 * (x >> 2) + (x & 3)] * kPad], dz[h2][x]);
+        unsafeAtomicAdd(&mine[ids[at + 32 * h2 + 8 * (x >> 2) + (x & 3)] * kPad], dz[0][x]);
+    }
   }
   __syncthreads();
   for (int x = threadIdx.x; x < a.buckets * a.pack; x += 256) {
@@ -728,33 +808,40 @@ __global__ __launch_bounds__(256) void score_dtable_bf16(ScoreArgs a, BwdWork w,
 template <int D, bool KEYS>
 __global__ __launch_bounds__(256) void score_bwd_merge(ScoreArgs a, BwdWork w) {
   const int H = KEYS ? a.kv_heads : a.heads, S = KEYS ? a.seq_k : a.seq_q;
-  const int nc = KEYS ? w.kv_nc : w.q_nc;
   const size_t all = (size_t)a.batch * H * S;
   const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
   const int g = (int)(at % (D / 8)), lane = threadIdx.x & 63;
   const size_t row = min(at / (D / 8), all - 1);
   int b, h, i;
+  const int* used;  // of set 0
   if (KEYS) {
     i = (int)(row % S), h = (int)(row / S % H), b = (int)(row / S / H);
+    used = w.kv_used + ((size_t)b * H + h) * key_blocks(a) + i / kBlockK;
   } else {
     const int r = (int)(row % ((size_t)S * a.pack)), hb = (int)(row / ((size_t)S * a.pack));
     i = r / a.pack, h = hb % (H / a.pack) * a.pack + r % a.pack, b = hb / (H / a.pack);
+    used = w.q_used + (size_t)hb * row_blocks(a) + r / kBlockQ;
   }
+  const int sets = KEYS ? a.group / a.pack : 1, subs = (KEYS ? w.kv_nc : w.q_nc) / sets;
+  const bool whole = sets == 1 && *used <= 1;  // written by its workgroup
   float acc[2][8] = {}, bad = 0.f;
+  if (!whole) {
 #pragma unroll
-  for (int k = 0; k < (KEYS ? 2 : 1); ++k) {
-    const float* from = (KEYS ? (k ? w.pdv : w.pdk) : w.pdq) + row * D + 8 * g;
-    for (int c = 0; c < nc; ++c) {
-      float v[8];
-      load8(from + (size_t)c * all * D, v);
+    for (int k = 0; k < (KEYS ? 2 : 1); ++k) {
+      const float* from = pick(KEYS, pick(k != 0, w.pdv, w.pdk), w.pdq) + row * D + 8 * g;
+      for (int s = 0; s < sets; ++s)
+        for (int c = 0; c < used[(size_t)s * a.batch * H * key_blocks(a)]; ++c) {
+          float v[8];
+          load8(from + (size_t)(s * subs + c) * all * D, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[k][e] += v[e];
+          for (int e = 0; e < 8; ++e) acc[k][e] += v[e];
+        }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) bad = fmaf(acc[k][e], 0.f, bad);
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) bad = fmaf(acc[k][e], 0.f, bad);
   }
   unsigned long long rows = __builtin_amdgcn_ballot_w64(bad != 0.f);
-  if (at / (D / 8) < all && bad == 0.f) {
+  if (at / (D / 8) < all && bad == 0.f && !whole) {
     if (KEYS) {
       const size_t to = ((size_t)b * S + i) * a.ld_dkv + h * D + 8 * g;
       store8((bf16*)a.dk + to, acc[0]);
@@ -773,13 +860,11 @@ __global__ __launch_bounds__(256) void score_bwd_merge(ScoreArgs a, BwdWork w) {
   }
 }
 
-int row_blocks(const ScoreArgs& a) { return (a.seq_q * a.pack + kBlockQ - 1) / kBlockQ; }
-int key_blocks(const ScoreArgs& a) { return (a.seq_k + kBlockK - 1) / kBlockK; }
 size_t round64(size_t floats) { return (floats + 63) & ~(size_t)63; }
 
 // The workspace's parts, in floats from its start.
 struct BwdLayout {
-  size_t L2, delta, bias, sums, pdk, pdv, pdq, min, total;
+  size_t L2, delta, bias, sums, pdk, pdv, pdq, kv_used, q_used, total;
 };
 BwdLayout bwd_layout(int D, const ScoreArgs& a, const ScoreBwdPlan& p) {
   const size_t rows = (size_t)a.batch * a.heads * a.seq_q;
@@ -797,6 +882,8 @@ BwdLayout bwd_layout(int D, const ScoreArgs& a, const ScoreBwdPlan& p) {
   l.pdk = take(p.kv.chunks > 1 ? (size_t)p.kv.chunks * keys * D : 0);
   l.pdv = take(p.kv.chunks > 1 ? (size_t)p.kv.chunks * keys * D : 0);
   l.pdq = take(p.q.chunks > 1 ? (size_t)p.q.chunks * rows * D : 0);
+  l.kv_used = take(p.kv.chunks > 1 ? (size_t)a.batch * a.heads / a.pack * key_blocks(a) : 0);
+  l.q_used = take(p.q.chunks > 1 ? (size_t)a.batch * a.heads / a.pack * row_blocks(a) : 0);
   l.total = at;
   return l;
 }
@@ -805,7 +892,7 @@ template <int D>
 void bwd_d(const ScoreArgs& a, const ScoreBwdPlan& p, float* ws, hipStream_t s) {
   const BwdLayout l = bwd_layout(D, a, p);
   BwdWork w{ws + l.L2, ws + l.delta, ws + l.pdk, ws + l.pdv, ws + l.pdq, ws + l.sums,
-            p.kv.chunk, p.kv.chunks, p.q.chunk, p.q.chunks};
+            (int*)(ws + l.kv_used), (int*)(ws + l.q_used), p.kv.chunks, p.q.chunks};
   ScoreArgs x = a;
   x.bias_part = ws + l.bias;
   const size_t rows = (size_t)a.batch * a.heads * a.seq_q;
@@ -818,9 +905,9 @@ void bwd_d(const ScoreArgs& a, const ScoreBwdPlan& p, float* ws, hipStream_t s) 
   const bool cap = a.cap > 0.f;
 #define PB_BWD(C, B)                                                                              \
   do {                                                                                            \
-    size_t lds = std::max((size_t)KvLds<D, B>::kBytes, q_tiles);                                  \
+    size_t lds = std::max((size_t)KvLds<D>::kBytes, q_tiles);                                  \
     if (B == kTable)                                                                              \
-      lds = std::max((size_t)KvLds<D, B>::bias(a).bytes,                                          \
+      lds = std::max((size_t)KvLds<D>::bias(a).bytes,                                          \
                      (size_t)BiasLds((int)q_tiles, a.buckets, a.pack,                             \
                                      (kBlockQ + a.pack - 1) / a.pack + 1, kTileK).bytes);         \
     score_bwd_bf16<D, C, B><<<(unsigned)(nk + nq), 256, lds, s>>>(x, w, nk, nq);                  \
@@ -864,30 +951,26 @@ static int most_row_tiles(const ScoreArgs& a) {
   return (int)(a.prefix ? all : std::min(all, reach * a.pack / kTileQ + 2));
 }
 
-ScoreBwdPlan score_bwd_whole(const ScoreArgs& a) {
-  return ScoreBwdPlan{{1 << 30, a.group / a.pack}, {1 << 30, 1}};
-}
+ScoreBwdPlan score_bwd_whole(const ScoreArgs& a) { return ScoreBwdPlan{{a.group / a.pack}, {1}}; }
+
+// Chunks enough that the longest is about a fifth of the launch (of 512 workgroups at a
+// time), and half as long where that is short; not shorter than a tile's worth of merge.
 ScoreBwdPlan score_bwd_plan(int head_dim, const ScoreArgs& a) {
   ScoreBwdPlan p = score_bwd_whole(a);
   const int sets = p.kv.chunks;
   const long long nk = (long long)key_blocks(a) * a.batch * a.kv_heads * sets;
   const long long nq = (long long)row_blocks(a) * a.batch * (a.heads / a.pack);
   const int kv = most_row_tiles(a), q = score_most_tiles(a, kBlockQ, kTileK);
-  // Times of a tile, and of all workgroups over the chip's 512 places (under a causal
-  // mask blocks have half the longest one's tiles, on average).
-  const double kv_us = 1.3, q_us = 2.6;
+  const double kv_us = 1.5, q_us = 2.4;
   const double half = a.causal && !a.prefix && a.window >= a.seq_k ? 0.5 : 1.0;
   const double all = half * (nk * kv_us * kv + nq * q_us * q) / 512;
-  const double target = std::max(0.6 * all, 25.0);
-  auto cut = [&](ScorePlan& s, int tiles, double us) {
-    const int want = (int)std::ceil(tiles * us / target);
-    const int m = std::min(want, (tiles + 3) / 4);
-    if (m < 2) return;
-    const int chunk = (tiles + m - 1) / m, chunks = (tiles + chunk - 1) / chunk;
-    if (chunks > 1) s.chunk = chunk, s.chunks *= chunks;
+  const double target = std::max(0.25 * all, 30.0);
+  auto cut = [&](ScorePlan& s, int tiles, double us, int least) {
+    const int m = std::min((int)std::ceil(tiles * us / target), tiles / least);
+    if (m > 1) s.chunks *= m;
   };
-  cut(p.kv, kv, kv_us);
-  cut(p.q, q, q_us);
+  cut(p.kv, kv, kv_us, kMinTilesKv);
+  cut(p.q, q, q_us, kMinTilesQ);
   return p;
 }
 

@@ -28,6 +28,7 @@ struct Type {
 };
 constexpr int kRows = 128;  // rows of a workgroup
 constexpr int kTL = 64;     // keys of a tile
+constexpr int kMinTiles = 2;  // of a chunk
 constexpr int kNoBias = 0, kSlopes = 1, kTable = 2;
 
 template <int D>
@@ -42,7 +43,8 @@ BiasLds bias_lds(const ScoreArgs& a) {
 
 template <int D, bool CAP, int BIAS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void score_fwd_bf16(
-    ScoreArgs a, int cs, int nc, float* __restrict__ po, float* __restrict__ plse) {
+    ScoreArgs a, int nc, float* __restrict__ po, float* __restrict__ plse,
+    int* __restrict__ used) {
   constexpr int TL = kTL, TB = TL * 2 * D, KS = D / 32, DB = D / 16;
   constexpr bool kZ = CAP || BIAS != kNoBias;  // scores are turned to base 2 with their terms
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
@@ -66,20 +68,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
   const int p_first = off + pk.pos(r0), p_last = off + pk.pos(min(r0 + kRows, rows) - 1);
 
   const KeyTiles kt = key_tiles<TL>(a, b, p_first, p_last, lane);
-  const int t_begin = chunk * cs, n = min(kt.n - t_begin, cs);
+  const Share share(kt.n, nc, kMinTiles);
+  const int t_begin = chunk * share.size, n = min(kt.n - t_begin, share.size);
   const int qw0 = r0 + 32 * wave;
-  const bool split = nc > 1;
+  const bool split = share.used > 1;
+  if (chunk >= max(share.used, 1)) return;
+  if (nc > 1 && chunk == 0 && tid == 0) used[(size_t)hb * nblk + r0 / kRows] = share.used;
   const size_t part0 = (size_t)chunk * a.batch * a.heads * a.seq_q;
   auto row_at = [&](int r) {  // of lse, and of the partial results
     const int i = pk.pos(r);
     return score::lse_at(a, b, h0 + r - i * a.pack, i);
   };
-  if (n <= 0) {  // nothing is seen, or the block has fewer chunks
-    if (split) {
-      const int r = r0 + tid;
-      if (tid < kRows && r < rows) plse[part0 + row_at(r)] = kNegInf;
-      return;
-    }
+  if (n <= 0) {  // nothing is seen
     for (int x = tid; x < kRows * (D / 8); x += 256) {
       const int r = r0 + x / (D / 8);
       if (r >= rows) break;
@@ -502,17 +502,22 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
 }
 
 // Merge of a split forward, in chunk order: the chunks' outputs weighted by 2^(lse_c -
-// lse).  A thread has 8 features of a row; chunks without a visible key are not read.
+// lse).  A thread has 8 features of a row.
 template <int D>
-__global__ __launch_bounds__(256) void score_fwd_merge(ScoreArgs a, int nc,
-                                                       const float* __restrict__ po,
-                                                       const float* __restrict__ plse) {
+__global__ __launch_bounds__(256) void score_fwd_merge(ScoreArgs a, const float* __restrict__ po,
+                                                       const float* __restrict__ plse,
+                                                       const int* __restrict__ used) {
   const size_t all = (size_t)a.batch * a.heads * a.seq_q;
   const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
   const int g = (int)(at % (D / 8)), lane = threadIdx.x & 63;
-  const size_t row = at / (D / 8);
+  const size_t row = min(at / (D / 8), all - 1);
+  const int i = (int)(row % a.seq_q), bh = (int)(row / a.seq_q);
+  const int sets = a.heads / a.pack, b = bh / a.heads, h = bh % a.heads;
+  const int blocks = (a.seq_q * a.pack + kRows - 1) / kRows;
+  const int nc = used[((size_t)b * sets + h / a.pack) * blocks + (i * a.pack + h % a.pack) / kRows];
+  const bool mine = at / (D / 8) < all && nc > 1;  // (else its workgroup wrote it)
   float m = kNegInf, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, bad = 0.f;
-  if (row < all) {
+  if (mine) {
     for (int c = 0; c < nc; ++c) m = fmaxf(m, plse[c * all + row]);
     for (int c = 0; c < nc; ++c) {
       const float lc = plse[c * all + row];
@@ -529,9 +534,8 @@ __global__ __launch_bounds__(256) void score_fwd_merge(ScoreArgs a, int nc,
     }
     bad = fmaf(l, 0.f, bad);
   }
-  const int i = row < all ? (int)(row % a.seq_q) : 0, bh = row < all ? (int)(row / a.seq_q) : 0;
   unsigned long long rows = __builtin_amdgcn_ballot_w64(bad != 0.f);
-  if (row < all && bad == 0.f) {
+  if (mine && bad == 0.f) {
     const float inv = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] *= inv;
@@ -551,13 +555,14 @@ void fwd_d(const ScoreArgs& a, const ScorePlan& p, void* part, hipStream_t s) {
   float* po = (float*)part;
   const size_t all = (size_t)a.batch * a.heads * a.seq_q;
   float* plse = po ? po + (size_t)p.chunks * all * D : nullptr;
+  int* used = po ? (int*)(plse + (size_t)p.chunks * all) : nullptr;
   const unsigned grid = (unsigned)((size_t)a.batch * (a.heads / a.pack) * p.chunks *
                                    ((a.seq_q * a.pack + kRows - 1) / kRows));
   const bool cap = a.cap > 0.f;
   const int bias = a.slopes ? kSlopes : a.table ? kTable : kNoBias;
   const size_t lds = a.table ? bias_lds<D>(a).bytes
                              : tiles_bytes<D>() + kRows * sizeof(RowKeys);
-#define PB_FWD(C, B) score_fwd_bf16<D, C, B><<<grid, 256, lds, s>>>(a, p.chunk, p.chunks, po, plse)
+#define PB_FWD(C, B) score_fwd_bf16<D, C, B><<<grid, 256, lds, s>>>(a, p.chunks, po, plse, used)
   if (cap) {
     if (bias == kTable) PB_FWD(true, kTable);
     else if (bias == kSlopes) PB_FWD(true, kSlopes);
@@ -569,33 +574,32 @@ void fwd_d(const ScoreArgs& a, const ScorePlan& p, void* part, hipStream_t s) {
   }
 #undef PB_FWD
   if (p.chunks > 1)
-    score_fwd_merge<D><<<(unsigned)((all * (D / 8) + 255) / 256), 256, 0, s>>>(a, p.chunks, po, plse);
+    score_fwd_merge<D><<<(unsigned)((all * (D / 8) + 255) / 256), 256, 0, s>>>(a, po, plse, used);
 }
 
 }  // namespace
 
 size_t score_fwd_part_bytes(int head_dim, const ScoreArgs& a, const ScorePlan& p) {
   if (p.chunks < 2) return 0;
-  return (size_t)p.chunks * a.batch * a.heads * a.seq_q * (head_dim + 1) * 4;
+  const size_t blocks = (size_t)(a.seq_q * a.pack + kRows - 1) / kRows;
+  return ((size_t)p.chunks * a.batch * a.heads * a.seq_q * (head_dim + 1) +
+          (size_t)a.batch * (a.heads / a.pack) * blocks) * 4;
 }
 
 // Split as in attn.hip: where the grid has fewer than 2048 waves, into as many chunks as
 // bring it to 1536, of two tiles at least; a tile takes about 1.4 us, the merge 3.5 us
 // and its traffic.
 ScorePlan score_fwd_plan(int head_dim, const ScoreArgs& a) {
-  ScorePlan p{1 << 30, 1};
   const long long blocks = (long long)a.batch * (a.heads / a.pack) *
                            ((a.seq_q * a.pack + kRows - 1) / kRows);
   const int most = score_most_tiles(a, kRows, kTL);
-  if (blocks * 4 >= 2048) return p;
+  if (blocks * 4 >= 2048) return ScorePlan{1};
   const int want = (int)((1536 + blocks * 4 - 1) / (blocks * 4));
-  const int m = std::min(want, (most + 1) / 2);
-  if (m < 2) return p;
-  ScorePlan q{(most + m - 1) / m, 0};
-  q.chunks = (most + q.chunk - 1) / q.chunk;
-  if (q.chunks < 2) return p;
+  const int m = std::min(want, most / kMinTiles);
+  if (m < 2) return ScorePlan{1};
+  const ScorePlan q{m};
   const double merge_us = 3.5 + 2.0 * (double)score_fwd_part_bytes(head_dim, a, q) / 8e6;
-  return 1.4 * (most - q.chunk) < merge_us ? p : q;
+  return 1.4 * (most - (most + m - 1) / m) < merge_us ? ScorePlan{1} : q;
 }
 
 void launch_score_forward_bf16(int head_dim, const ScoreArgs& a, const ScorePlan& p, void* part,

@@ -53,6 +53,13 @@ PB_DEV RowKeys row_keys(const ScoreArgs& a, int b, int p) {
   return RowKeys{first, d.de > d.ds ? window_last(a, d, p) - first + 1 : 0, d.ds, d.pe - d.ds};
 }
 
+// A block's n tiles shared out over at most `most` chunks of `least` tiles or more.
+struct Share {
+  int size, used;  // tiles of a chunk, chunks
+  PB_DEV Share(int n, int most, int least)
+      : size(max((n + most - 1) / most, most > 1 ? least : 1)), used((n + size - 1) / size) {}
+};
+
 // The key tiles (of TL) that positions p0 .. p1 of a batch row visit: up to two runs,
 // the prefixes' and the windows', in ascending order.  lo .. hi: the keys that any of
 // them sees, and all between.
