@@ -126,8 +126,9 @@ pb::ScoreArgs args_of(const pb_score_attn_config* c, const pb_score_terms* t) {
   a.buckets = c->buckets, a.side = c->causal ? c->buckets : c->buckets / 2;
   if (c->buckets) borders_of(c, a.first);
   a.pack = 1;
+  // (with a table a power of two: lanes of the table's gradient have one head each)
   for (int n = 2; n <= kMaxPack; ++n)
-    if (a.group % n == 0) a.pack = n;
+    if (a.group % n == 0 && (!c->buckets || (n & (n - 1)) == 0)) a.pack = n;
   return a;
 }
 // What a call's plans depend on beside the config: the workspace's sizes are for any

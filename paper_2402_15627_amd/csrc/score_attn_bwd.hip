@@ -590,6 +590,8 @@ struct RowTiles {
     for (int x = 0; x < 16; ++x) {
       pr[0][x] = exp2_hw(CAP || BIAS != kNoBias ? pr[0][x] - L2 : fmaf(pr[0][x], c2, -L2));
       dz[0][x] *= pr[0][x];
+      // (behind the mask dP may be anything: the table's sums take none of it)
+      if constexpr (BIAS == kTable) dz[0][x] = pr[0][x] == 0.f ? 0.f : dz[0][x];
     }
   }
 };
@@ -735,20 +737,38 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
 
 // ----------------------------------------------------- the table's gradient
 // Sums by bucket of 128 rows' dz over the tiles whose distances span buckets, with delta
-// put right by e; those beyond come from dQ's sums: dz less e P.  A lane adds to places
-// of its own in LDS.
+// put right by e; those beyond come from dQ's sums: dz less e P.
+//
+// Keys of one distance from their rows lie on a diagonal of a wave's 32 x 64 tile: the
+// wave writes its dz to LDS (over K and V, once all waves are done with them) and reads
+// diagonals back, 32 values a lane in all, each lane those of one head, and adds the sum
+// of each to its own place for the distance's bucket.  (An LDS atomic for each dz, the
+// direct way, takes about 130 cycles a wave and CU: 8192 tokens, 40 heads, window 1024
+// 470 us against XXX.)
+template <int D>
+struct DtableLds {
+  static constexpr int kRow = kTileK + 4;  // floats of a row of dz
+  static constexpr int kTiles = 2 * kTileK * 2 * D;
+  static constexpr int kStaged = 4 * 32 * kRow * 4;
+  static constexpr int kBytes = kTiles > kStaged ? kTiles : kStaged;
+  static __host__ __device__ BiasLds bias(const ScoreArgs& a) {
+    return BiasLds(kBytes, a.buckets, a.pack, (kBlockQ + a.pack - 1) / a.pack + 1, kTileK);
+  }
+};
 template <int D, bool CAP>
-__global__ __launch_bounds__(256) void score_dtable_bf16(ScoreArgs a, BwdWork w, int nblk) {
-  constexpr int TB = kTileK * 2 * D, kPad = 65;
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void score_dtable_bf16(
+    ScoreArgs a, BwdWork w, int nblk) {
+  constexpr int TB = kTileK * 2 * D, kRow = DtableLds<D>::kRow;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(PB_LDS unsigned char*)smem;
   const int hb_n = a.batch * (a.heads / a.pack);
   const int hb = blockIdx.x % hb_n, blk = nblk - 1 - blockIdx.x / hb_n;
-  RowTiles<D, CAP, kTable> t(a, w, smem, 2 * TB, blk, hb);
+  RowTiles<D, CAP, kTable> t(a, w, smem, DtableLds<D>::kBytes, blk, hb);
+  // a place for each bucket and lane, then the bucket of each distance of a tile
   float* acc = (float*)(smem + t.bl.bytes);
-  unsigned char* ids = smem + t.bl.bytes + 4 * a.buckets * kPad * 4;
-  float* mine = acc + (size_t)t.wave * a.buckets * kPad + t.lane;
-  for (int n = 0; n < a.buckets; ++n) mine[n * kPad] = 0.f;
+  unsigned char* ids = smem + t.bl.bytes + 4 * a.buckets * 64 * 4;
+  float* mine = acc + (size_t)t.wave * a.buckets * 64 + t.lane;
+  for (int n = 0; n < a.buckets; ++n) mine[n * 64] = 0.f;
   t.tables();
   const size_t all = (size_t)a.batch * a.heads * a.seq_q;
   float sums[kSums] = {0.f, 0.f, 0.f, 0.f, 0.f};
@@ -758,12 +778,17 @@ __global__ __launch_bounds__(256) void score_dtable_bf16(ScoreArgs a, BwdWork w,
       for (int x = 0; x < kSums; ++x)
         sums[x] += w.sums[((size_t)c * kSums + x) * all + packed_row(a, hb, t.r)];
   t.dl += sums[0];
+  // (pack is a power of two here: lane and row have one head, and blocks begin with head 0)
+  const int span = 32 / a.pack, hh = t.lane % a.pack, y = t.lane / a.pack, step = 64 / a.pack;
   if (t.fh == 0) {
-    mine[(a.side - 1) * kPad] += fmaf(-sums[0], sums[2], sums[1]);
-    mine[(a.causal ? 0 : 2 * a.side - 1) * kPad] += fmaf(-sums[0], sums[4], sums[3]);
+    mine[(a.side - 1) * 64] += fmaf(-sums[0], sums[2], sums[1]);
+    mine[(a.causal ? 0 : 2 * a.side - 1) * 64] += fmaf(-sums[0], sums[4], sums[3]);
   }
   const KeyTiles kt = key_tiles<kTileK>(a, t.b, t.p_first, t.p_last, t.lane);
   const LaneReads<D> places(t.lane);
+  float* staged = (float*)smem + t.wave * 32 * kRow;
+  // from the block's last position to the wave's
+  const int after = t.p_last - (t.off + t.pk.pos(t.r0 + 32 * t.wave + 31));
   for (int i = 0; i < kt.n; ++i) {
     const int kv0 = kt.tile(i) * kTileK;
     if (t.uniform(kv0) >= 0) continue;
@@ -775,30 +800,50 @@ __global__ __launch_bounds__(256) void score_dtable_bf16(ScoreArgs a, BwdWork w,
     wait_dma_all();
     block_barrier();
     const uint64_t see = t.keys.bits(kv0);
-    if (!__builtin_amdgcn_ballot_w64(see != 0)) continue;
-    const LaneReads<D> kr = places.at(lds0);
-    const int at = t.p_last - t.p + 4 * t.fh;
+    const bool any = __builtin_amdgcn_ballot_w64(see != 0);
+    f32x16 dz[2][1];
+    if (any) {
+      const LaneReads<D> kr = places.at(lds0);
 #pragma unroll
-    for (int h2 = 0; h2 < 2; ++h2) {
-      f32x16 pr[1], dz[1], slope;
-      t.template pair<0>(kv0, h2, 0, kr, see, pr, dz, slope);
+      for (int h2 = 0; h2 < 2; ++h2) {
+        f32x16 pr[1], slope;
+        t.template pair<0>(kv0, h2, 0, kr, see, pr, dz[h2], slope);
+      }
+    }
+    block_barrier();  // every wave is done with K and V
+    if (!any) continue;
 #pragma unroll
-      for (int x = 0; x < 16; ++x)
-        unsafeAtomicAdd(&mine[ids[at + 32 * h2 + 8 * (x >> 2) + (x & 3)] * kPad], dz[0][x]);
+    for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<f32x4*>(staged + t.fr * kRow + 32 * h2 + 8 * j + 4 * t.fh) =
+            f32x4{dz[h2][0][4 * j], dz[h2][0][4 * j + 1], dz[h2][0][4 * j + 2], dz[h2][0][4 * j + 3]};
+    // Entry x (as in bias_tile, from the wave's last position on) of position q is key x -
+    // (span - 1) + q; where that is below 0, key + 64 is on diagonal x + 64.
+    for (int m = 0; m < a.pack; ++m) {
+      const int x = y + step * m;
+      float lo = 0.f, hi = 0.f;
+#pragma unroll 8
+      for (int q = 0; q < span; ++q) {
+        const int key = x - (span - 1) + q;
+        const float v = staged[(q * a.pack + hh) * kRow + (key & 63)];
+        lo += key >= 0 ? v : 0.f;
+        hi += key >= 0 ? 0.f : v;
+      }
+      const int at = x + after;  // (rows past the end lie beyond the block's last position)
+      if (at >= 0) mine[ids[at] * 64] += lo;
+      if (x < span - 1 && at + 64 >= 0) mine[ids[at + 64] * 64] += hi;
     }
   }
   __syncthreads();
-  for (int x = threadIdx.x; x < a.buckets * a.pack; x += 256) {
-    const int n = x % a.buckets, hh = x / a.buckets;
+  // a wave a bucket: sums over the waves, then over the lanes of a head
+  for (int n = t.wave; n < a.buckets; n += 4) {
     float s = 0.f;
-    for (int wv = 0; wv < 4; ++wv)
-      for (int l = 0; l < 32; ++l) {
-        const int r = t.r0 + 32 * wv + l;
-        if (r - t.pk.pos(r) * a.pack != hh) continue;
-        const float* from = acc + ((size_t)wv * a.buckets + n) * kPad + l;
-        s += from[0] + from[32];
-      }
-    a.bias_part[(((size_t)t.b * nblk + blk) * a.heads + t.h0 + hh) * a.buckets + n] = s;
+#pragma unroll
+    for (int wv = 0; wv < 4; ++wv) s += acc[(wv * a.buckets + n) * 64 + t.lane];
+    for (int o = 32; o >= a.pack; o >>= 1) s += __shfl_xor(s, o, 64);
+    if (t.lane < a.pack)
+      a.bias_part[(((size_t)t.b * nblk + blk) * a.heads + t.h0 + t.lane) * a.buckets + n] = s;
   }
 }
 
@@ -930,9 +975,8 @@ void bwd_d(const ScoreArgs& a, const ScoreBwdPlan& p, float* ws, hipStream_t s) 
   if (!a.dtable) return;
   const int nblk = row_blocks(a);
   const unsigned grid = (unsigned)(nblk * a.batch * (a.heads / a.pack));
-  const BiasLds bl(2 * kTileK * 2 * D, a.buckets, a.pack, (kBlockQ + a.pack - 1) / a.pack + 1,
-                   kTileK);
-  const size_t lds = bl.bytes + (size_t)4 * a.buckets * 65 * 4 + bl.stride;
+  const BiasLds bl = DtableLds<D>::bias(a);
+  const size_t lds = bl.bytes + (size_t)4 * a.buckets * 64 * 4 + bl.stride;
   if (cap) score_dtable_bf16<D, true><<<grid, 256, lds, s>>>(x, w, nblk);
   else score_dtable_bf16<D, false><<<grid, 256, lds, s>>>(x, w, nblk);
   launch_score_dtable_sum(x, nblk * a.batch, s);
