@@ -331,6 +331,7 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
   const LaneReads<D> places(lane);
 
   for (int i = 0; i < nt; ++i) {
+    __builtin_amdgcn_s_setprio(0);
     wait_dma_all();   // tile i, requested an iteration ago
     block_barrier();  // ... for every wave; and every wave is done with tile i - 1
     if (i + 1 < nt) {
@@ -346,13 +347,15 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
     const int* row_pos = (const int*)(ls + 2 * TL);
     // Lane holds key `key` and rows r0 + 8 j + 4 fh + e of element 4 j + e.
     f32x16 sc[1] = {zero16()}, dp = zero16();
-    // (fragments one step ahead of their products, and no further: registers)
+    // (fragments one step ahead of their products, and no further: registers; a wave at
+    // its products goes before the SIMD's other one: capped scores 3%)
     bf16x8 fq[2], fg[2], fv[2];
     auto read = [&](int ks) PB_INLINE {
       fq[ks & 1] = qr.rows(ks, 0);
       fg[ks & 1] = qr.rows(ks, TB);
       fv[ks & 1] = vr.rows(ks, 0);
     };
+    __builtin_amdgcn_s_setprio(1);
     read(0);
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
@@ -361,6 +364,7 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
       dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fg[ks & 1], fv[ks & 1], dp, 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
     if constexpr (CAP || BIAS != kNoBias) to_base2<CAP>(cap, c2, sc);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -414,6 +418,7 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
         dp[4 * j + e] *= sc[0][4 * j + e];
       }
     }
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int s2 = 0; s2 < TL / 16; ++s2) {
       const bf16x8 pf = probs_frag(sc, s2), df = probs_frag(&dp, s2);
@@ -474,7 +479,8 @@ struct RowTiles {
   const ScoreArgs& a;
   const BwdWork& w;
   unsigned char* smem;
-  int b, h0, kvh, r0, rows, off, lane, wave, fr, fh, r, i, h, p, p_first, p_last;
+  int b, h0, kvh, r0, rows, off, lane, wave, fr, fh, r, i, h, p;
+  int p_first, p_last, w_first, w_last;  // positions of the block, and of the wave
   float L2, dl, slope2;
   int bias_at, bias_last;
   RowKeys keys;
@@ -497,6 +503,8 @@ struct RowTiles {
     const int rc = min(r, rows - 1);
     i = pk.pos(rc), h = h0 + rc - i * a.pack, p = i + off;
     p_first = off + pk.pos(r0), p_last = off + pk.pos(min(r0 + kBlockQ, rows) - 1);
+    w_first = off + pk.pos(min(r0 + 32 * wave, rows - 1));
+    w_last = off + pk.pos(min(r0 + 32 * wave + 31, rows - 1));
     const bf16 *q = score::q_row<bf16, D>(a, b, i, h), *g = score::do_row<bf16, D>(a, b, i, h);
     keys = row_keys(a, b, p);
     if (r >= rows) keys = RowKeys{0, 0, 0, 0};
@@ -523,6 +531,9 @@ struct RowTiles {
   PB_DEV int uniform(int kv0) const {
     return bias_uniform(a, bias_last, p_first - kv0 - kTileK + 1, p_last - kv0);
   }
+  PB_DEV int wave_uniform(int kv0) const {
+    return bias_uniform(a, bias_last, w_first - kv0 - kTileK + 1, w_last - kv0);
+  }
   PB_DEV void build(int kv0, int buf) {
     if (uniform(kv0) < 0) bias_tile(a, bl, smem, buf, a.pack, p_last - kv0, threadIdx.x, 256);
   }
@@ -546,12 +557,18 @@ struct RowTiles {
     const float c2 = a.scale * kLog2e;
     pr[0] = zero16();
     dz[0] = zero16();
+    bf16x8 fk[2], fv[2];
+    auto read = [&](int ks) PB_INLINE {
+      fk[ks & 1] = kr.rows(ks, 32 * h2 * 2 * D);
+      fv[ks & 1] = kr.rows(ks, (kTileK + 32 * h2) * 2 * D);
+    };
+    read(0);
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
-      pr[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr.rows(ks, 32 * h2 * 2 * D), qf[ks], pr[0], 0,
-                                                      0, 0);
-      dz[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr.rows(ks, (kTileK + 32 * h2) * 2 * D),
-                                                      gf[ks], dz[0], 0, 0, 0);
+      if (ks + 1 < D / 16) read(ks + 1);
+      pr[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[ks & 1], qf[ks], pr[0], 0, 0, 0);
+      dz[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv[ks & 1], gf[ks], dz[0], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (CAP || BIAS != kNoBias) to_base2<CAP>(cap, c2, pr);
     const float it = 1.f / cap.top;
@@ -649,7 +666,7 @@ PB_DEV void dq_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
 #pragma unroll
             for (int x = 0; x < 16; ++x) s += dz[0][x];
             sums[0] += s;
-            const int u = t.uniform(kv0);
+            const int u = t.wave_uniform(kv0);
             if (u >= 0) {
 #pragma unroll
               for (int x = 0; x < 16; ++x) sp += pr[0][x];
@@ -800,7 +817,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
     wait_dma_all();
     block_barrier();
     const uint64_t see = t.keys.bits(kv0);
-    const bool any = __builtin_amdgcn_ballot_w64(see != 0);
+    // (where the wave's rows are all beyond, dQ has summed)
+    const bool any = t.wave_uniform(kv0) < 0 && __builtin_amdgcn_ballot_w64(see != 0);
     f32x16 dz[2][1];
     if (any) {
       const LaneReads<D> kr = places.at(lds0);
@@ -875,11 +893,15 @@ __global__ __launch_bounds__(256) void score_bwd_merge(ScoreArgs a, BwdWork w) {
     for (int k = 0; k < (KEYS ? 2 : 1); ++k) {
       const float* from = pick(KEYS, pick(k != 0, w.pdv, w.pdk), w.pdq) + row * D + 8 * g;
       for (int s = 0; s < sets; ++s)
-        for (int c = 0; c < used[(size_t)s * a.batch * H * key_blocks(a)]; ++c) {
-          float v[8];
-          load8(from + (size_t)(s * subs + c) * all * D, v);
+        for (int c0 = 0, n = used[(size_t)s * a.batch * H * key_blocks(a)]; c0 < n; c0 += 4) {
+          float v[4][8];  // (four loads in flight)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) acc[k][e] += v[e];
+          for (int c = 0; c < 4; ++c)
+            load8(from + (size_t)(s * subs + min(c0 + c, n - 1)) * all * D, v[c]);
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[k][e] += c0 + c < n ? v[c][e] : 0.f;
         }
 #pragma unroll
       for (int e = 0; e < 8; ++e) bad = fmaf(acc[k][e], 0.f, bad);
@@ -997,24 +1019,34 @@ static int most_row_tiles(const ScoreArgs& a) {
 
 ScoreBwdPlan score_bwd_whole(const ScoreArgs& a) { return ScoreBwdPlan{{a.group / a.pack}, {1}}; }
 
-// Chunks enough that the longest is about a fifth of the launch (of 512 workgroups at a
-// time), and half as long where that is short; not shorter than a tile's worth of merge.
+// A key block has as many row tiles as all heads that share it bring, a row block few key
+// tiles, and splitting costs a merge and its traffic (fp32 parts, written and read).  So
+// keys are cut down to what the launch takes as a whole (over 512 workgroups at a time;
+// half the longest block's tiles on average under a causal mask) or the longest row block
+// takes, whichever is more; rows only where few of them see many keys.  Found by timing
+// 21 plans each for 12 shapes (us; keys' chunks 1, 2, 4, 8):
+//   4096 tokens, 16 heads over 4, 128        687 412 295 295
+//   the same, capped, three documents        632 361 278 266
+//   2048, 12 x 128                           113  88  95 115
+//   8192, 4 over 1 x 128                    1297 685 401 302
+//   4 x 2048, 16 over 2 x 96                 632 357 270 277
+//   2048, 40 x 128, window 512               136 158 184 203
+//   4096, 8 x 128, window 1024                91 111 126 131
 ScoreBwdPlan score_bwd_plan(int head_dim, const ScoreArgs& a) {
   ScoreBwdPlan p = score_bwd_whole(a);
   const int sets = p.kv.chunks;
   const long long nk = (long long)key_blocks(a) * a.batch * a.kv_heads * sets;
   const long long nq = (long long)row_blocks(a) * a.batch * (a.heads / a.pack);
   const int kv = most_row_tiles(a), q = score_most_tiles(a, kBlockQ, kTileK);
-  const double kv_us = 1.5, q_us = 2.4;
-  const double half = a.causal && !a.prefix && a.window >= a.seq_k ? 0.5 : 1.0;
-  const double all = half * (nk * kv_us * kv + nq * q_us * q) / 512;
-  const double target = std::max(0.25 * all, 30.0);
-  auto cut = [&](ScorePlan& s, int tiles, double us, int least) {
-    const int m = std::min((int)std::ceil(tiles * us / target), tiles / least);
+  const double kv_us = 1.5 * kv, q_us = 2.4 * q;
+  const double half = a.causal && a.window >= a.seq_k ? 0.5 : 1.0;
+  const double all = half * (nk * kv_us + nq * q_us) / 512;
+  auto cut = [&](ScorePlan& s, double us, double target, int most) {
+    const int m = std::min((int)std::ceil(us / target - 0.25), most);
     if (m > 1) s.chunks *= m;
   };
-  cut(p.kv, kv, kv_us, kMinTilesKv);
-  cut(p.q, q, q_us, kMinTilesQ);
+  cut(p.kv, kv_us, std::max(all, 0.8 * q_us), kv / kMinTilesKv);
+  cut(p.q, q_us, std::max(all, 100.0), q / kMinTilesQ);
   return p;
 }
 

@@ -28,7 +28,7 @@ struct Type {
 };
 constexpr int kRows = 128;  // rows of a workgroup
 constexpr int kTL = 64;     // keys of a tile
-constexpr int kMinTiles = 2;  // of a chunk
+constexpr int kMinTiles = 4;  // of a chunk
 constexpr int kNoBias = 0, kSlopes = 1, kTable = 2;
 
 template <int D>
@@ -424,6 +424,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
   // prologue: tile 0's scores, terms and maximum
   wait_dma_all();
   block_barrier();
+  if (qw0 >= rows) {  // a wave without rows only loads for the others
+    for (int i = 0; i < n; ++i) {
+      wait_dma_all();
+      block_barrier();
+      if (i + 2 < n) {
+        issue_k(i + 2);
+        if constexpr (BIAS == kTable) build(i + 2);
+      }
+      if (i + 1 < n) issue_v(i + 1);
+    }
+    return;
+  }
   read_k(lds0 + k_off(0), 0);
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -518,18 +530,26 @@ __global__ __launch_bounds__(256) void score_fwd_merge(ScoreArgs a, const float*
   const bool mine = at / (D / 8) < all && nc > 1;  // (else its workgroup wrote it)
   float m = kNegInf, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, bad = 0.f;
   if (mine) {
+#pragma unroll 4
     for (int c = 0; c < nc; ++c) m = fmaxf(m, plse[c * all + row]);
-    for (int c = 0; c < nc; ++c) {
-      const float lc = plse[c * all + row];
-      if (lc == kNegInf) continue;
-      const float w = exp2_hw(lc - m);
-      float v[8];
-      load8(po + (c * all + row) * D + 8 * g, v);
-      l += w;
+    for (int c0 = 0; c0 < nc; c0 += 4) {
+      float v[4][8], w[4];  // (four loads in flight)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        acc[e] = fmaf(w, v[e], acc[e]);
-        bad = fmaf(v[e], 0.f, bad);
+      for (int c = 0; c < 4; ++c) {
+        const size_t from = min(c0 + c, nc - 1) * all + row;
+        load8(po + from * D + 8 * g, v[c]);
+        w[c] = plse[from];
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        if (c0 + c >= nc || w[c] == kNegInf) continue;
+        w[c] = exp2_hw(w[c] - m);
+        l += w[c];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          acc[e] = fmaf(w[c], v[c][e], acc[e]);
+          bad = fmaf(v[c][e], 0.f, bad);
+        }
       }
     }
     bad = fmaf(l, 0.f, bad);
@@ -587,8 +607,14 @@ size_t score_fwd_part_bytes(int head_dim, const ScoreArgs& a, const ScorePlan& p
 }
 
 // Split as in attn.hip: where the grid has fewer than 2048 waves, into as many chunks as
-// bring it to 1536, of two tiles at least; a tile takes about 1.4 us, the merge 3.5 us
-// and its traffic.
+// bring it to 1536, of four tiles at least; a tile takes about 1.4 us, the merge 3.5 us
+// and its traffic.  Timed (us, 1, 2, 4, 8, 12, 16 chunks):
+//   4 x 1 token over 8192, 40 heads over 8 x 128   232 123  68  42  35  36
+//   1 token over 1000, 8 x 64                       24  18  14  14  14  14
+//   2048, 12 x 128, capped                          60  49  50  64  72  81
+//   4096, 4 x 128, capped                          105  70  51  56  68  78
+//   128 over 4096, 16 over 4 x 128                  77  47  31  25  26  27
+//   1024, 8 x 128                                   26  24  23  26  27  27
 ScorePlan score_fwd_plan(int head_dim, const ScoreArgs& a) {
   const long long blocks = (long long)a.batch * (a.heads / a.pack) *
                            ((a.seq_q * a.pack + kRows - 1) / kRows);
