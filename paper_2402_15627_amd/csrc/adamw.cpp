@@ -103,6 +103,7 @@ pb_status pblock_adamw_step(const pb_adamw_config* cfg, int n_tensors,
   c.beta2 = cfg->beta2, c.rest2 = 1.0f - cfg->beta2;
   c.c1 = cfg->bias_correction ? (float)(1.0 / (1.0 - pow((double)cfg->beta1, cfg->step))) : 1.f;
   c.c2 = cfg->bias_correction ? (float)(1.0 / (1.0 - pow((double)cfg->beta2, cfg->step))) : 1.f;
+  c.eps_in_range = cfg->eps >= 0x1p-90f && cfg->eps <= 0x1p40f;
   pb::AdamTable t{};
   long long chunks = 0;
   auto launch = [&] {

@@ -42,28 +42,38 @@ PB_DEV uint32_t random_bits(uint64_t seed, uint64_t e) {
 }
 
 // Largest of the wave's 64 unsigned words, in every lane.
+template <int CTRL>
+PB_DEV uint32_t umax_dpp(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true));
+}
 PB_DEV uint32_t wave_umax(uint32_t v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
-  return v;
+  v = umax_dpp<0x128>(v);  // rotations within 16 lanes
+  v = umax_dpp<0x124>(v);
+  v = umax_dpp<0x122>(v);
+  v = umax_dpp<0x121>(v);
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max(b[0], b[1]);
 }
 
-// e4m3 code of |y| <= 448 rounded up or down as `rnd` (16 bits) says: to a
+// e4m3 code of |y| <= 448 rounded up or down as `rnd` (16 bits, and 4 zeros) says: to a
 // neighbour as often as y is near it.  Bits of the fp32 value below the code's
 // last place meet the random ones in an integer sum; below 2^-6, where codes
 // are multiples of 2^-9, the value itself takes the place of its bits.
 PB_DEV uint32_t code_e4m3(float a, uint32_t rnd) {
   const uint32_t bits = a < 0x1p-6f ? (uint32_t)(a * 0x1p29f)
                                     : __float_as_uint(a) - (120u << 23);
-  return min((bits + (rnd << 4)) >> 20, 0x7eu);
+  return min((bits + rnd) >> 20, 0x7eu);
 }
 
 // Four elements' updated state x (lane's part of its wave's 256) as codes; their
 // scale is the largest magnitude over 448 (its product with the rounded 1/448),
 // at least 2^-126.  A value that is not finite makes the scale so (magnitudes are
-// compared as words, where NaN is above all).  KEEP (x >= 0): what is above zero keeps a code above zero.
+// compared as words, where NaN is above all).  bits: of each, random; the upper half, or with KEEP the lower.  KEEP (x >= 0):
+// what is above zero keeps a code above zero.
 template <bool KEEP>
-PB_DEV uint32_t quantise(const float (&x)[4], const uint32_t (&rnd)[4], float& scale) {
+PB_DEV uint32_t quantise(const f32x4& x, const uint32_t (&bits)[4], float& scale) {
 #pragma clang fp contract(off)
   uint32_t top = 0;
 #pragma unroll
@@ -75,67 +85,108 @@ PB_DEV uint32_t quantise(const float (&x)[4], const uint32_t (&rnd)[4], float& s
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const float y = x[k] * inv;
-    uint32_t c = code_e4m3(fabsf(y), rnd[k]);
+    uint32_t c = code_e4m3(fabsf(y), KEEP ? (bits[k] & 0xffffu) << 4 : bits[k] >> 16 << 4);
     if (KEEP) c = c == 0 && x[k] > 0.f ? 1u : c;
     else c |= (__float_as_uint(y) >> 24) & 0x80u;
     word |= c << (8 * k);
   }
   return word;
 }
-PB_DEV void dequantise(uint32_t word, float scale, float (&x)[4]) {
+PB_DEV void dequantise(uint32_t word, float scale, f32x4& x) {
 #pragma clang fp contract(off)
   const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(word, false);
   const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(word, true);
   x[0] = lo[0] * scale, x[1] = lo[1] * scale, x[2] = hi[0] * scale, x[3] = hi[1] * scale;
 }
 
-PB_DEV void update(const AdamScalars& c, float decay, float grad, float& w, float& m, float& v) {
+// Square root and quotient as correctly rounded ones (but for about one in 2^22, off by a
+// step), from the hardware's approximations and an exact remainder each: half the
+// instructions of the general ones, which also take care of values whose squares or
+// reciprocals leave fp32.  x: 0, or 2^-90 .. 2^90; d: 2^-90 .. 2^90.
+PB_DEV float sqrt_near(float x) {
+  const float y = __builtin_amdgcn_rsqf(fmaxf(x, 0x1p-90f)), s = x * y;
+  return __builtin_fmaf(__builtin_fmaf(-s, s, x), 0.5f * y, s);
+}
+PB_DEV float div_near(float n, float d) {
+  const float y = __builtin_amdgcn_rcpf(d), q = n * y;
+  return __builtin_fmaf(__builtin_fmaf(-d, q, n), y, q);
+}
+PB_DEV bool in_range(float x) { return x >= 0x1p-90f && x <= 0x1p90f; }
+
+// One step of four elements; r: the root of the new v, where ROOT.
+template <bool ROOT>
+PB_DEV void update(const AdamScalars& c, float decay, const f32x4& grad, f32x4& w, f32x4& m,
+                   f32x4& v, f32x4& r) {
 #pragma clang fp contract(off)
-  const float g = grad * c.grad_scale;
-  m = m * c.beta1 + g * c.rest1;
-  v = v * c.beta2 + (g * g) * c.rest2;
-  const float u = (m * c.c1) / (__builtin_sqrtf(v * c.c2) + c.eps);
-  w = w * decay - u * c.lr;
+  f32x4 vh;
+  bool plain = true;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float g = grad[k] * c.grad_scale;
+    m[k] = m[k] * c.beta1 + g * c.rest1;
+    v[k] = v[k] * c.beta2 + (g * g) * c.rest2;
+    vh[k] = v[k] * c.c2;
+    plain = plain && (v[k] == 0.f || (in_range(v[k]) && in_range(vh[k])));
+  }
+  f32x4 u;
+  if (c.eps_in_range && __builtin_amdgcn_ballot_w64(!plain) == 0) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      u[k] = div_near(m[k] * c.c1, sqrt_near(vh[k]) + c.eps);
+      if (ROOT) r[k] = sqrt_near(v[k]);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      u[k] = (m[k] * c.c1) / (__builtin_sqrtf(vh[k]) + c.eps);
+      if (ROOT) r[k] = __builtin_sqrtf(v[k]);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) w[k] = w[k] * decay - u[k] * c.lr;
 }
 
-template <typename CT>
-PB_DEV void store_copy(void* copy, long long e, int n, const f32x4& w) {
-  CT* p = (CT*)copy + e;
-  if (n == 4) {
-    if constexpr (sizeof(CT) == 2)
-      __builtin_nontemporal_store((u32x2_a2)u32x2{pack_bf2(w[0], w[1]), pack_bf2(w[2], w[3])},
-                                  reinterpret_cast<u32x2_a2*>(p));
-    else
-      store_stream((float*)p, w);
-  } else {
-    for (int k = 0; k < n; ++k) p[k] = (CT)w[k];
-  }
-}
-// n of four values (the tensor's end may be in between)
+// n of four values (the tensor's end may be in between); WHOLE: all four.
+template <bool WHOLE>
 PB_DEV f32x4 load_some(const float* p, int n) {
-  if (n == 4) return load_stream(p);
+  if (WHOLE || n == 4) return load_stream(p);
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int k = 0; k < 3; ++k)
     if (k < n) v[k] = p[k];
   return v;
 }
+template <bool WHOLE>
 PB_DEV void store_some(float* p, int n, const f32x4& v) {
-  if (n == 4) return store_stream(p, v);
+  if (WHOLE || n == 4) return store_stream(p, v);
 #pragma unroll
   for (int k = 0; k < 3; ++k)
     if (k < n) p[k] = v[k];
 }
+template <bool WHOLE>
+PB_DEV void store_copy(bf16* p, int n, const f32x4& w) {
+  if (WHOLE || n == 4)
+    __builtin_nontemporal_store((u32x2_a2)u32x2{pack_bf2(w[0], w[1]), pack_bf2(w[2], w[3])},
+                                reinterpret_cast<u32x2_a2*>(p));
+  else
+    for (int k = 0; k < n; ++k) p[k] = (bf16)w[k];
+}
+template <bool WHOLE>
+PB_DEV void store_copy(float* p, int n, const f32x4& w) {
+  store_some<WHOLE>(p, n, w);
+}
+template <bool WHOLE>
 PB_DEV uint32_t load_codes(const uint8_t* p, int n) {
-  if (n == 4) return *reinterpret_cast<const u32_a1*>(p);
+  if (WHOLE || n == 4) return *reinterpret_cast<const u32_a1*>(p);
   uint32_t v = 0;
 #pragma unroll
   for (int k = 0; k < 3; ++k)
     if (k < n) v |= (uint32_t)p[k] << (8 * k);
   return v;
 }
+template <bool WHOLE>
 PB_DEV void store_codes(uint8_t* p, int n, uint32_t v) {
-  if (n == 4) {
+  if (WHOLE || n == 4) {
     *reinterpret_cast<u32_a1*>(p) = v;
     return;
   }
@@ -155,55 +206,54 @@ PB_DEV int tensor_of(const AdamTable& t, int chunk) {
   return lo;
 }
 
+// Elements e .. e + n - 1 of tensor i (n <= 4, a wave's lanes side by side).
+template <bool E4M3, typename CT, bool WHOLE>
+PB_DEV void step(const AdamTable& t, const AdamScalars& c, int i, long long e, int n) {
+  f32x4 w = load_some<WHOLE>(t.w[i] + e, n), r;
+  const f32x4 g = load_some<WHOLE>(t.g[i] + e, n);
+  if constexpr (!E4M3) {
+    float *mp = (float*)t.m[i] + e, *vp = (float*)t.v[i] + e;
+    f32x4 m = load_some<WHOLE>(mp, n), v = load_some<WHOLE>(vp, n);
+    update<false>(c, t.decay[i], g, w, m, v, r);
+    store_some<WHOLE>(mp, n, m);
+    store_some<WHOLE>(vp, n, v);
+  } else {
+#pragma clang fp contract(off)
+    uint8_t *mp = (uint8_t*)t.m[i] + e, *vp = (uint8_t*)t.v[i] + e;
+    float *ms = t.m_scale[i] + e / kAdamBlock, *vs = t.v_scale[i] + e / kAdamBlock;
+    const uint32_t cm = load_codes<WHOLE>(mp, n), cv = load_codes<WHOLE>(vp, n);
+    f32x4 m, v;
+    dequantise(cm, *ms, m);
+    dequantise(cv, *vs, v);
+    v *= v;
+    update<true>(c, t.decay[i], g, w, m, v, r);
+    uint32_t bits[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      bits[k] = random_bits(t.seed[i], (uint64_t)(e + k));
+      if (!WHOLE && k >= n) m[k] = r[k] = 0.f;
+    }
+    float s;
+    store_codes<WHOLE>(mp, n, quantise<false>(m, bits, s));
+    if ((threadIdx.x & 63) == 0) *ms = s;
+    store_codes<WHOLE>(vp, n, quantise<true>(r, bits, s));
+    if ((threadIdx.x & 63) == 0) *vs = s;
+  }
+  store_some<WHOLE>(t.w[i] + e, n, w);
+  if (t.copy[i]) store_copy<WHOLE>((CT*)t.copy[i] + e, n, w);
+}
+
 template <bool E4M3, typename CT>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamTable t, AdamScalars c) {
   const int chunk = blockIdx.x, i = tensor_of(t, chunk);
-  const long long e = (long long)(chunk - t.chunk0[i]) * kAdamChunk + 4 * threadIdx.x;
-  const int n = (int)max(0LL, min(4LL, t.numel[i] - e));
-  // (a wave stays whole for its scales, whichever lanes have elements)
-  if (!E4M3 && n == 0) return;
-  f32x4 w = load_some(t.w[i] + e, n);
-  const f32x4 g = load_some(t.g[i] + e, n);
-  if constexpr (!E4M3) {
-    f32x4 m = load_some((const float*)t.m[i] + e, n), v = load_some((const float*)t.v[i] + e, n);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      float wk = w[k], mk = m[k], vk = v[k];
-      update(c, t.decay[i], g[k], wk, mk, vk);
-      w[k] = wk, m[k] = mk, v[k] = vk;
-    }
-    store_some((float*)t.m[i] + e, n, m);
-    store_some((float*)t.v[i] + e, n, v);
+  const long long e0 = (long long)(chunk - t.chunk0[i]) * kAdamChunk, e = e0 + 4 * threadIdx.x;
+  if (e0 + kAdamChunk <= t.numel[i]) {
+    step<E4M3, CT, true>(t, c, i, e, 4);
   } else {
-    const long long block = e / kAdamBlock;
-    const bool any = block * kAdamBlock < t.numel[i];  // wave-uniform
-    if (!any) return;
-    float m[4], r[4];
-    dequantise(load_codes((const uint8_t*)t.m[i] + e, n), t.m_scale[i][block], m);
-    dequantise(load_codes((const uint8_t*)t.v[i] + e, n), t.v_scale[i][block], r);
-    uint32_t rm[4], rr[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-#pragma clang fp contract(off)
-      float wk = w[k], vk = r[k] * r[k];
-      update(c, t.decay[i], g[k], wk, m[k], vk);
-      w[k] = wk;
-      r[k] = __builtin_sqrtf(vk);
-      const uint32_t bits = random_bits(t.seed[i], (uint64_t)(e + k));
-      rm[k] = bits >> 16, rr[k] = bits & 0xffffu;
-      if (k >= n) m[k] = r[k] = 0.f;
-    }
-    float ms, rs;
-    store_codes((uint8_t*)t.m[i] + e, n, quantise<false>(m, rm, ms));
-    store_codes((uint8_t*)t.v[i] + e, n, quantise<true>(r, rr, rs));
-    if ((threadIdx.x & 63) == 0) {
-      t.m_scale[i][block] = ms;
-      t.v_scale[i][block] = rs;
-    }
+    const int n = (int)max(0LL, min(4LL, t.numel[i] - e));
+    // (a wave with any element stays whole, for its scales)
+    if (e / kAdamBlock * kAdamBlock < t.numel[i]) step<E4M3, CT, false>(t, c, i, e, n);
   }
-  if (n == 0) return;
-  store_some(t.w[i] + e, n, w);
-  if (t.copy[i]) store_copy<CT>(t.copy[i], e, n, w);
 }
 
 }  // namespace

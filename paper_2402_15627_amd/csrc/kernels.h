@@ -98,6 +98,7 @@ static_assert(sizeof(AdamTable) <= 4000, "kernel arguments");
 struct AdamScalars {
   float lr, beta1, rest1, beta2, rest2, eps, grad_scale;  // rest: 1 - beta
   float c1, c2;  // 1 / (1 - beta^t), or 1 without bias correction
+  int eps_in_range;  // 2^-90 <= eps <= 2^40
 };
 void launch_adamw(const AdamTable& t, const AdamScalars& c, bool e4m3, Dt copy_dt, hipStream_t s);
 
