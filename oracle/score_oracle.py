@@ -113,7 +113,8 @@ def attention(q, k, v, see, scale, d_o=None, **terms):
             with np.errstate(divide="ignore"):
                 r["lse"][b, h] = top + np.log(total)
             mag = scale * (np.abs(qq) @ np.abs(kk).T)  # of the products' own sums
-            r["a_s"][b, h] = np.where(m, mag + np.abs(np.where(m, s, 0.0)), 0.0).max(1)
+            finite = np.abs(np.where(np.isfinite(s), s, 0.0))  # (a bias of -inf masks)
+            r["a_s"][b, h] = np.where(m, mag + finite, 0.0).max(1)
             if d_o is None:
                 continue
             gg = np.where(any_[:, None], d_o[b, :, h], 0.0)
@@ -135,7 +136,7 @@ def attention(q, k, v, see, scale, d_o=None, **terms):
             if terms.get("table") is not None:
                 # errors of the scores, of dP and of the row term, relative to 1
                 a_dp = np.abs(gg) @ np.abs(vv).T
-                a = p * ((mag + np.abs(np.where(m, s, 0.0)) + 4) * (np.abs(dp) + np.abs(delta)) + a_dp
+                a = p * ((mag + finite + 4) * (np.abs(dp) + np.abs(delta)) + a_dp
                          + (p * a_dp).sum(1, keepdims=True))
                 for n in range(len(terms["table"])):
                     at = ids == n
