@@ -771,8 +771,8 @@ pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s,
  * atomics between waves).
  *
  * Errors: PB_ERR_INVALID_ARG for a bad config, pointer or ld, PB_ERR_UNSUPPORTED for
- * sizes past the kernels' (batch*seq_k and batch*seq_q*heads < 2^31), PB_ERR_WORKSPACE
- * for a small ws. */
+ * another head_dim and for sizes past the kernels' (batch*seq_q*heads and
+ * batch*seq_k*kv_heads <= 2^26, batch*heads <= 2^21), PB_ERR_WORKSPACE for a small ws. */
 #define PB_SCORE_MAX_BUCKETS 64
 typedef struct {
   int batch;         /* >= 1                                                  */
@@ -925,15 +925,15 @@ pb_status pblock_orthogonalize(int n_tensors, const pb_ortho_tensor* tensors,
  *   PB_ADAMW_F32   exp_avg is m and exp_avg_sq v, fp32.
  *   PB_ADAMW_E4M3  exp_avg holds m and exp_avg_sq sqrt(v) as OCP e4m3 codes, one byte
  *       an element, with fp32 scales for each PB_ADAMW_BLOCK elements (the last block may
- *       be short): value = code scale.  scale = max(largest magnitude / 448, 2^-126) of
- *       the block's updated values; a code is one of the two neighbours of the quotient,
- *       the upper as often as it is near (a moving average that moves by less than half
- *       a code's step would stand still under rounding to nearest).  sqrt(v) above 0
- *       keeps a code above 0.  Which one is taken follows from 16 bits of a hash of
- *       (seed, number of the element), the upper half of 32 for m and the lower for
- *       sqrt(v): the same seed gives the same codes, so give each tensor and step its
- *       own.  The step itself uses the updated values before they are rounded.  All
- *       zeros (codes and scales) are states of zero.  A value that is not finite makes
+ *       be short): value = code scale.  scale = max(largest magnitude (1 / 448), 2^-126)
+ *       of the block's updated values, 1 / 448 rounded to fp32.  A code is one of the two
+ *       neighbours of value / scale, the upper as often as it is near (a moving average
+ *       that moves by less than half a code's step would stand still under rounding to
+ *       nearest).  sqrt(v) above 0 keeps a code above 0.  Which one is taken follows from
+ *       16 bits of a hash of (seed, number of the element), the upper half of 32 for m and
+ *       the lower for sqrt(v): the same seed gives the same codes, so give each tensor and
+ *       step its own.  The step itself uses the updated values before they are rounded.
+ *       All zeros (codes and scales) are states of zero.  A value that is not finite makes
  *       its block's scale infinite or NaN, and the block's states with it.
  *
  * A captured step replays with the lr, step and seeds that it was captured with.
@@ -942,7 +942,7 @@ pb_status pblock_orthogonalize(int n_tensors, const pb_ortho_tensor* tensors,
  * Any number of tensors from 1 to PB_ADAMW_MAX_TENSORS, 48 in a launch; results do not
  * depend on how tensors are divided over calls.  No workspace.
  * Errors: PB_ERR_INVALID_ARG for a bad config, pointer or decay, PB_ERR_UNSUPPORTED for
- * a tensor of 2^34 elements or more. */
+ * a tensor of more than 2^34 - 2^10 elements. */
 #define PB_ADAMW_MAX_TENSORS 1024
 #define PB_ADAMW_BLOCK 256
 typedef enum { PB_ADAMW_F32 = 0, PB_ADAMW_E4M3 = 1 } pb_adamw_state;

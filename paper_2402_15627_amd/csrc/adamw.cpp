@@ -66,8 +66,8 @@ pb_status pblock_adamw_step(const pb_adamw_config* cfg, int n_tensors,
     const pb_adamw_tensor& x = tensors[i];
     if (!(x.weight_decay >= 0.f) || !std::isfinite(x.weight_decay))
       return fail(PB_ERR_INVALID_ARG, "tensor %d: weight_decay=%g", i, (double)x.weight_decay);
-    if (x.numel >= (size_t)kMaxBlocks * pb::kAdamChunk)
-      return fail(PB_ERR_UNSUPPORTED, "tensor %d: %zu elements, 2^34 or more", i, x.numel);
+    if (x.numel > (size_t)(kMaxBlocks - 1) * pb::kAdamChunk)
+      return fail(PB_ERR_UNSUPPORTED, "tensor %d: %zu elements, over 2^34 - 2^10", i, x.numel);
     if (x.numel == 0) continue;
     const size_t s = e4m3 ? 1 : 4, scales = 4 * ((x.numel + PB_ADAMW_BLOCK - 1) / PB_ADAMW_BLOCK);
     const struct {

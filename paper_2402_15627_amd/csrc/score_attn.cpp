@@ -7,6 +7,8 @@
 namespace {
 
 constexpr size_t kMaxLd = (size_t)1 << 24;
+constexpr long long kMaxRows = 1LL << 26, kMaxHeads = 1LL << 21;
+static_assert(2 * (kMaxRows / 16 + kMaxHeads) < kMaxBlocks, "workgroups of a launch");
 
 pb_status check_config(const pb_score_attn_config* c) {
   if (!c) return fail(PB_ERR_INVALID_ARG, "cfg is NULL");
@@ -35,13 +37,13 @@ pb_status check_config(const pb_score_attn_config* c) {
       return fail(PB_ERR_INVALID_ARG, "max_distance=%d must be in %d..2^20", c->max_distance,
                   side / 2 + 1);
   }
-  if ((long long)c->batch * c->seq_k > kMaxInt ||
-      (long long)c->batch * c->seq_q > kMaxInt / c->heads)
-    return fail(PB_ERR_UNSUPPORTED, "batch*seq_k or batch*seq_q*heads is 2^31 or more");
-  // workgroups: four rows each at least, of keys and of queries
-  if ((long long)c->batch * c->seq_q * c->heads > 4 * kMaxBlocks ||
-      (long long)c->batch * c->seq_k > 4 * kMaxBlocks / c->kv_heads)
-    return fail(PB_ERR_UNSUPPORTED, "over 2^26 rows of a head");
+  // A launch has workgroups for 16 rows at least of each head's queries and keys: fewer
+  // than kMaxBlocks, also where a head has one row.
+  if ((long long)c->batch * c->seq_q > kMaxRows / c->heads ||
+      (long long)c->batch * c->seq_k > kMaxRows / c->kv_heads)
+    return fail(PB_ERR_UNSUPPORTED, "over 2^26 rows of queries' or of keys' heads");
+  if ((long long)c->batch * c->heads > kMaxHeads)
+    return fail(PB_ERR_UNSUPPORTED, "batch*heads is over 2^21");
   return PB_OK;
 }
 
@@ -173,8 +175,12 @@ pb_status pblock_score_attn_borders(const pb_score_attn_config* cfg, int* first)
 
 size_t pblock_score_attn_workspace_bytes(const pb_score_attn_config* cfg, int mode) {
   if (check_config(cfg) != PB_OK) return 0;
-  if (mode == PB_ATTN_WS_FORWARD) return fwd_bytes(cfg);
-  return bwd_bytes(cfg, mode == PB_ATTN_WS_BACKWARD_MIN);
+  switch (mode) {
+    case PB_ATTN_WS_FORWARD: return fwd_bytes(cfg);
+    case PB_ATTN_WS_BACKWARD_MIN: return bwd_bytes(cfg, true);
+    case PB_ATTN_WS_BACKWARD: return bwd_bytes(cfg, false);
+    default: return 0;
+  }
 }
 
 pb_status pblock_score_attn_forward(const pb_score_attn_config* cfg, const pb_score_terms* terms,

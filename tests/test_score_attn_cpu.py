@@ -56,6 +56,7 @@ BUCKETS = dict(buckets=8, max_distance=20)
     (dict(buckets=8, max_distance=20, causal=0), BAD),  # buckets without a table
     (dict(batch=1 << 20, seq_k=1 << 12, seq_q=1), UNSUPPORTED),
     (dict(batch=1 << 14, seq_k=1 << 13, seq_q=1 << 13), UNSUPPORTED),
+    (dict(batch=1 << 22, seq_k=1, seq_q=1, heads=1, kv_heads=1), UNSUPPORTED),
     (dict(q=None), BAD), (dict(q=FAKE + 8), BAD), (dict(k=None), BAD), (dict(v=FAKE + 2), BAD),
     (dict(o=None), BAD), (dict(lse=None), BAD), (dict(lse=FAKE + 2), BAD),
     (dict(ld_q=255), BAD), (dict(ld_q=260), BAD), (dict(ld_kv=127), BAD), (dict(ld_o=256 + 4), BAD),
@@ -138,6 +139,7 @@ def test_workspaces():
     for cfg in (few, many, pb.score_attn_config(1, 300, 300, 22, 2, 64, buckets=32, max_distance=99)):
         small, full = size(cfg, pb.ATTN_WS_BACKWARD_MIN), size(cfg, pb.ATTN_WS_BACKWARD)
         assert 0 < small <= full and small % 256 == 0
+        assert size(cfg, 9) == 0
     assert size(pb.score_attn_config(0, 1, 1, 1, 1, 64), pb.ATTN_WS_BACKWARD) == 0
     assert size(pb.score_attn_config(1, 9, 9, 2, 2, 64, dtype="f32"), pb.ATTN_WS_FORWARD) == 0
 
@@ -192,6 +194,7 @@ def test_adamw_refusals(state, over, status):
     (dict(param=None), BAD), (dict(grad=None), BAD), (dict(exp_avg=None), BAD), (dict(exp_avg_sq=None), BAD),
     (dict(param=FAKE + 2), BAD), (dict(grad=FAKE + GAP + 1), BAD), (dict(param_copy=FAKE + 9 * GAP + 1), BAD),
     (dict(weight_decay=-1.0), BAD), (dict(weight_decay=NAN), BAD), (dict(numel=1 << 34), UNSUPPORTED),
+    (dict(numel=(1 << 34) - 1023), UNSUPPORTED),
     # shared memory: with another array, and by the end of one
     (dict(grad=FAKE), BAD), (dict(exp_avg=FAKE), BAD), (dict(param_copy=FAKE), BAD),
     (dict(param=FAKE + GAP - 4), BAD), (dict(exp_avg_sq=FAKE + 2 * GAP), BAD)])
