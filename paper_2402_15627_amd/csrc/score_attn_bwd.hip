@@ -46,7 +46,7 @@ PB_DEV size_t packed_row(const ScoreArgs& a, int hb, int r) {
 // Both operands read once, D / 8 lanes a row (four for head_dim 96).
 template <int D>
 __global__ __launch_bounds__(256) void score_terms(ScoreArgs a, float* __restrict__ L2,
-                                                   float* __restrict__ delta) {
+                                                   float* __restrict__ minus_delta) {
   constexpr int kLanes = D == 96 ? 4 : D / 8, kChunks = D / 8 / kLanes;
   const size_t at = ((size_t)blockIdx.x * 256 + threadIdx.x) / kLanes;
   const size_t all = (size_t)a.batch * a.seq_q * a.heads;
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256) void score_terms(ScoreArgs a, float* __restric
   const size_t to = packed_row(a, b * (a.heads / a.pack) + h / a.pack, i * a.pack + h % a.pack);
   // a row that sees nothing: probabilities of 2^-inf
   L2[to] = L == kNegInf ? -kNegInf : L * kLog2e;
-  delta[to] = L == kNegInf ? 0.f : acc;
+  minus_delta[to] = L == kNegInf ? 0.f : -acc;
 }
 
 // A TL-row tile in the layout of dma_tile (attn_tiles.h): offset(0 .. TL - 1) is that of a
@@ -144,26 +144,8 @@ struct LaneReads {
   }
 };
 
-// Scores to base 2, with the cap.
-template <bool CAP, int N>
-PB_DEV void to_base2(const Cap& cap, float c2, f32x16 (&s)[N]) {
-  if constexpr (CAP) {
-    cap.apply(s);
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[i][e] *= c2;
-  }
-}
-// 1 - tanh^2 of a capped score, it = 1 / cap.top.
-PB_DEV float cap_slope(float z, float it) {
-  const float t = z * it;
-  return fmaf(-t, t, 1.f);
-}
-
 struct BwdWork {
-  float *L2, *delta;        // row terms, in the blocks' order
+  float *L2, *minus_delta;  // row terms, in the blocks' order
   float *pdk, *pdv, *pdq;   // partial results of split blocks, [chunk][row][D]
   float* sums;              // [chunk][kSums][rows] (with dtable)
   int *kv_used, *q_used;    // chunks of each block, [set][batch, head][block]
@@ -189,7 +171,7 @@ template <int D>
 struct KvLds {
   static constexpr int kV = kBlockK * 2 * D;
   static constexpr int kTile = kTileQ * 2 * D;
-  // Q, dO, then of each row: lse, delta, position, and its bias (slope, place or value)
+  // Q, dO, then of each row: lse, -delta, position, and its bias (slope, place or value)
   static constexpr int kStage = 2 * kTile + 4 * kTileQ * 4;
   static constexpr int kBytes = kV + 2 * kStage;
   static __host__ __device__ BiasLds bias(const ScoreArgs& a) {
@@ -288,7 +270,7 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
     dma_rows<D, TL, 4>(g0 + (size_t)y0 * a.ld_do,
                        [&](int r) PB_INLINE { return offset(r, a.ld_do); }, at + TB, wave, lane);
     if (wave == 0)
-      dma4(pick(lane < 32, w.L2, w.delta) + row0 + row_of(lane & 31),
+      dma4(pick(lane < 32, w.L2, w.minus_delta) + row0 + row_of(lane & 31),
            __builtin_amdgcn_readfirstlane(at + 2 * TB));
     if (wave == 1 && lane < TL) {
       const int r = r0 + lane, y = pk.pos(r), hh = r - y * a.pack;
@@ -325,9 +307,8 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
   f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = zero16();
-  const float c2 = a.scale * kLog2e;
   const Cap cap(a.scale, CAP ? a.cap : 1.f);
-  const float it = 1.f / cap.top;
+  const float c2 = CAP ? cap.top : a.scale * kLog2e;  // (of tanh, with a cap)
   const LaneReads<D> places(lane);
 
   for (int i = 0; i < nt; ++i) {
@@ -346,7 +327,13 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
     const float* ls = (const float*)(smem + stage + 2 * TB);
     const int* row_pos = (const int*)(ls + 2 * TL);
     // Lane holds key `key` and rows r0 + 8 j + 4 fh + e of element 4 j + e.
-    f32x16 sc[1] = {zero16()}, dp = zero16();
+    f32x16 sc[1] = {zero16()}, dp;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {  // dP - delta
+      const f32x4 D4 = *reinterpret_cast<const f32x4*>(ls + TL + 8 * j + 4 * fh);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dp[4 * j + e] = D4[e];
+    }
     // (fragments one step ahead of their products, and no further: registers; a wave at
     // its products goes before the SIMD's other one: capped scores 3%)
     bf16x8 fq[2], fg[2], fv[2];
@@ -365,15 +352,10 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
       __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_s_setprio(0);
-    if constexpr (CAP || BIAS != kNoBias) to_base2<CAP>(cap, c2, sc);
+    if constexpr (CAP) {
+      cap.apply(sc);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const f32x4 D4 = *reinterpret_cast<const f32x4*>(ls + TL + 8 * j + 4 * fh);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        dp[4 * j + e] -= D4[e];
-        if constexpr (CAP) dp[4 * j + e] *= cap_slope(sc[0][4 * j + e], it);
-      }
+      for (int e = 0; e < 16; ++e) dp[e] *= fmaf(-sc[0][e], sc[0][e], 1.f);
     }
     if constexpr (BIAS == kSlopes) {
 #pragma unroll
@@ -382,7 +364,7 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
         const f32x4 X4 = *reinterpret_cast<const f32x4*>(row_pos + TL + 8 * j + 4 * fh);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          sc[0][4 * j + e] = fmaf(X4[e], fabsf((float)((int)P4[e] - key)), sc[0][4 * j + e]);
+          sc[0][4 * j + e] = fmaf(X4[e], fabsf((float)((int)P4[e] - key)), sc[0][4 * j + e] * c2);
       }
     }
     if constexpr (BIAS == kTable) {
@@ -395,7 +377,8 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) X4[e] = __float_as_uint(bt[(int)X4[e]]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[0][4 * j + e] += __uint_as_float(X4[e]);
+        for (int e = 0; e < 4; ++e)
+          sc[0][4 * j + e] = fmaf(sc[0][4 * j + e], c2, __uint_as_float(X4[e]));
       }
     }
     if (!(p0 >= all_lo && p1 <= all_hi)) {
@@ -414,7 +397,7 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float z = sc[0][4 * j + e];
-        sc[0][4 * j + e] = exp2_hw(CAP || BIAS != kNoBias ? z - L4[e] : fmaf(z, c2, -L4[e]));
+        sc[0][4 * j + e] = exp2_hw(BIAS != kNoBias ? z - L4[e] : fmaf(z, c2, -L4[e]));
         dp[4 * j + e] *= sc[0][4 * j + e];
       }
     }
@@ -517,7 +500,7 @@ struct RowTiles {
     }
     const size_t at = packed_row(a, hb, rc);
     L2 = w.L2[at];
-    dl = w.delta[at];
+    dl = -w.minus_delta[at];
     slope2 = BIAS == kSlopes ? -a.slopes[h] * kLog2e : 0.f;
     bias_last = BIAS == kTable ? a.first[a.side - 1] : 0;
     bias_at = BIAS == kTable ? (h - h0) * bl.stride + (p_last - p) + 4 * fh : 0;
@@ -554,7 +537,7 @@ struct RowTiles {
   template <int SLOPE>
   PB_DEV void pair(int kv0, int h2, int buf, const LaneReads<D>& kr, uint64_t see,
                     f32x16 (&pr)[1], f32x16 (&dz)[1], f32x16& slope) {
-    const float c2 = a.scale * kLog2e;
+    const float c2 = CAP ? cap.top : a.scale * kLog2e;  // (of tanh, with a cap)
     pr[0] = zero16();
     dz[0] = zero16();
     bf16x8 fk[2], fv[2];
@@ -570,30 +553,29 @@ struct RowTiles {
       dz[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv[ks & 1], gf[ks], dz[0], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (CAP || BIAS != kNoBias) to_base2<CAP>(cap, c2, pr);
-    const float it = 1.f / cap.top;
+    if constexpr (CAP) cap.apply(pr);
 #pragma unroll
     for (int x = 0; x < 16; ++x) {
       dz[0][x] -= dl;
-      if constexpr (CAP && SLOPE == 1) dz[0][x] *= cap_slope(pr[0][x], it);
-      if constexpr (CAP && SLOPE == 2) slope[x] = cap_slope(pr[0][x], it);
+      if constexpr (CAP && SLOPE == 1) dz[0][x] *= fmaf(-pr[0][x], pr[0][x], 1.f);
+      if constexpr (CAP && SLOPE == 2) slope[x] = fmaf(-pr[0][x], pr[0][x], 1.f);
     }
     if constexpr (BIAS == kSlopes) {
       const float d0 = (float)(p - kv0 - 32 * h2 - 4 * fh);
 #pragma unroll
       for (int x = 0; x < 16; ++x)
-        pr[0][x] = fmaf(slope2, fabsf(d0 - (float)(8 * (x >> 2) + (x & 3))), pr[0][x]);
+        pr[0][x] = fmaf(slope2, fabsf(d0 - (float)(8 * (x >> 2) + (x & 3))), pr[0][x] * c2);
     }
     if constexpr (BIAS == kTable) {
       const int u = uniform(kv0);
       if (u < 0) {
         const float* bt = (const float*)(smem + bl.tile(buf, a.pack)) + bias_at + 32 * h2;
 #pragma unroll
-        for (int x = 0; x < 16; ++x) pr[0][x] += bt[8 * (x >> 2) + (x & 3)];
+        for (int x = 0; x < 16; ++x) pr[0][x] = fmaf(pr[0][x], c2, bt[8 * (x >> 2) + (x & 3)]);
       } else {
         const float f = ((const float*)(smem + bl.tab))[u * a.pack + h - h0];
 #pragma unroll
-        for (int x = 0; x < 16; ++x) pr[0][x] += f;
+        for (int x = 0; x < 16; ++x) pr[0][x] = fmaf(pr[0][x], c2, f);
       }
     }
     const uint32_t mine = (uint32_t)(see >> (32 * h2));
@@ -605,7 +587,7 @@ struct RowTiles {
     }
 #pragma unroll
     for (int x = 0; x < 16; ++x) {
-      pr[0][x] = exp2_hw(CAP || BIAS != kNoBias ? pr[0][x] - L2 : fmaf(pr[0][x], c2, -L2));
+      pr[0][x] = exp2_hw(BIAS != kNoBias ? pr[0][x] - L2 : fmaf(pr[0][x], c2, -L2));
       dz[0][x] *= pr[0][x];
       // (behind the mask dP may be anything: the table's sums take none of it)
       if constexpr (BIAS == kTable) dz[0][x] = pr[0][x] == 0.f ? 0.f : dz[0][x];
@@ -965,7 +947,7 @@ void bwd_d(const ScoreArgs& a, const ScoreBwdPlan& p, float* ws, hipStream_t s) 
   const size_t rows = (size_t)a.batch * a.heads * a.seq_q;
   const size_t keys = (size_t)a.batch * a.kv_heads * a.seq_k;
   constexpr int kLanes = D == 96 ? 4 : D / 8;
-  score_terms<D><<<(unsigned)((rows * kLanes + 255) / 256), 256, 0, s>>>(x, w.L2, w.delta);
+  score_terms<D><<<(unsigned)((rows * kLanes + 255) / 256), 256, 0, s>>>(x, w.L2, w.minus_delta);
   const int nk = key_blocks(a) * a.batch * a.kv_heads * p.kv.chunks;
   const int nq = row_blocks(a) * a.batch * (a.heads / a.pack) * p.q.chunks;
   const size_t q_tiles = 4 * (size_t)kTileK * 2 * D;

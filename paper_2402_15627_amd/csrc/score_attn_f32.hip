@@ -115,7 +115,7 @@ struct Terms {
     if constexpr (CAP) {
       f32x4 x[1] = {s};
       cap.apply(x);
-      return x[0];
+      return x[0] * a.cap;
     }
     return s * a.scale;
   }

@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
     ScoreArgs a, int nc, float* __restrict__ po, float* __restrict__ plse,
     int* __restrict__ used) {
   constexpr int TL = kTL, TB = TL * 2 * D, KS = D / 32, DB = D / 16;
-  constexpr bool kZ = CAP || BIAS != kNoBias;  // scores are turned to base 2 with their terms
+  constexpr bool kZ = BIAS != kNoBias;  // scores are turned to base 2 with their bias
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(PB_LDS unsigned char*)smem;
   auto k_off = [](int s) { return (uint32_t)(s * TB); };
@@ -201,9 +201,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
       far[j][1] = tab[(a.causal ? 0 : 2 * a.side - 1) * a.pack + h];
     }
   }
-  Cap cap(a.scale, CAP ? a.cap : 1.f);
+  const Cap cap(a.scale, CAP ? a.cap : 1.f);
 
-  const float c2 = a.scale * kLog2e;
+  const float c2 = CAP ? cap.top : a.scale * kLog2e;  // (of tanh, with a cap)
   float m_run[2] = {kNegInf, kNegInf}, l_run[2] = {0.f, 0.f};
   f32x4 o[DB][2];
 #pragma unroll
@@ -266,16 +266,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
   // the terms of tile i's scores, and its mask where the wave does not see all of it
   auto terms = [&](f32x4 (&sc)[4][2], int i) {
     const int kv0 = kt.tile(t_begin + i) * TL;
-    if constexpr (CAP) {
-      cap.apply(reinterpret_cast<f32x4(&)[8]>(sc));
-    } else if constexpr (kZ) {
-#pragma unroll
-      for (int k4 = 0; k4 < 4; ++k4)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sc[k4][j][e] *= c2;
-    }
+    if constexpr (CAP) cap.apply(reinterpret_cast<f32x4(&)[8]>(sc));
     if constexpr (BIAS == kSlopes) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -285,7 +276,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             sc[k4][j][e] =
-                fmaf(slope2[j], fabsf(d0 - (float)(score_row_off(k4) + e)), sc[k4][j][e]);
+                fmaf(slope2[j], fabsf(d0 - (float)(score_row_off(k4) + e)), sc[k4][j][e] * c2);
       }
     }
     if constexpr (BIAS == kTable) {
@@ -298,7 +289,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
           for (int k4 = 0; k4 < 4; ++k4)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              sc[k4][j][e] += bt[bias_at[j] + score_row_off(k4) + e];
+              sc[k4][j][e] = fmaf(sc[k4][j][e], c2, bt[bias_at[j] + score_row_off(k4) + e]);
       } else {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -306,7 +297,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
 #pragma unroll
           for (int k4 = 0; k4 < 4; ++k4)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sc[k4][j][e] += f;
+            for (int e = 0; e < 4; ++e) sc[k4][j][e] = fmaf(sc[k4][j][e], c2, f);
         }
       }
     }

@@ -101,42 +101,45 @@ PB_DEV KeyTiles key_tiles(const ScoreArgs& a, int b, int p0, int p1, int lane) {
   return k;
 }
 
-// cap tanh(scale u / cap) times a unit (log2 e for base 2).  Tiles differ in how far their scores go, so a wave
-// looks at its largest |scale u / cap| first: to 1/8 three terms in x^2 are good to
-// 2^-24, to 1/2 five, beyond 1 - 2 / (1 + e^(2|x|)) takes over from 1/2 on.  (An
-// exponential and a reciprocal take eight instructions' time each.)
+// t = tanh(scale u / cap); the score is cap t, what the cap leaves of its gradient 1 - t^2.
+// Tiles differ in how far their scores go, so a wave looks at its largest |x| = |scale u /
+// cap| first: to 1/8 three terms in x^2 are good to 2^-24, to 1/2 five, beyond 1 - 2 / (1 +
+// e^(2|x|)) takes over from 1/2 on.  (An exponential and a reciprocal take eight
+// instructions' time each.)  What follows takes t: the product with cap is part of the
+// exponential's or of the bias's fused multiply.
 struct Cap {
-  float small, mid;      // bounds of |u|
-  float a0, a1, a2;      // x <= 1/8: z = u (a0 + a1 u^2 + a2 u^4)
-  float b0, b1, b2, b3, b4;
-  float two, top;        // 2 scale / cap log2 e, cap
+  float k, small;  // scale / cap, and |u| of x = 1/8
+  float a1, a2, b1, b2, b3, b4;  // (k: the first coefficient of either)
+  float top;       // cap times a unit (log2 e for base 2)
   PB_DEV Cap(float scale, float cap, float unit = kLog2e) {
-    const float k = scale / cap, k2 = k * k, s = scale * unit;
-    small = 0.125f / k, mid = 0.5f / k;
-    a0 = s * kA0, a1 = s * kA1 * k2, a2 = s * kA2 * k2 * k2;
-    b0 = s * kB0, b1 = s * kB1 * k2, b2 = s * kB2 * (k2 * k2), b3 = s * kB3 * (k2 * k2 * k2),
-    b4 = s * kB4 * (k2 * k2) * (k2 * k2);
-    two = 2.f * k * kLog2e, top = cap * unit;
+    k = scale / cap, small = 0.125f / k;
+    a1 = kA1 * k * (k * k), a2 = kA2 * k * (k * k) * (k * k);
+    top = cap * unit;
+    const float k3 = k * (k * k), k5 = k3 * (k * k), k7 = k5 * (k * k), k9 = k7 * (k * k);
+    b1 = kB1 * k3, b2 = kB2 * k5, b3 = kB3 * k7, b4 = kB4 * k9;
+    for (float* x : {&k, &small, &a1, &a2, &b1, &b2, &b3, &b4, &top})  // scalar registers
+      *x = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(*x)));
   }
   // tanh(x) / x in x^2 of least largest relative error (by Remez exchange): 7e-9 to 1/8,
   // 1.4e-8 to 1/2; in fp32 4.3e-8 and 6.5e-8
-  static constexpr float kA0 = 1.0f, kA1 = -0.33332599f, kA2 = 0.13207752f;
-  static constexpr float kB0 = 1.0f, kB1 = -0.33333069f, kB2 = 0.13324779f, kB3 = -0.052986075f,
+  static constexpr float kA1 = -0.33332599f, kA2 = 0.13207752f;  // (1 + ..)
+  static constexpr float kB1 = -0.33333069f, kB2 = 0.13324779f, kB3 = -0.052986075f,
                          kB4 = 0.017135007f;
   PB_DEV float near(float u) const {
     const float w = u * u;
-    return u * fmaf(fmaf(a2, w, a1), w, a0);
+    return u * fmaf(fmaf(a2, w, a1), w, k);
   }
   PB_DEV float half(float u) const {
     const float w = u * u;
-    return u * fmaf(fmaf(fmaf(fmaf(b4, w, b3), w, b2), w, b1), w, b0);
+    return u * fmaf(fmaf(fmaf(fmaf(b4, w, b3), w, b2), w, b1), w, k);
   }
   PB_DEV float any(float u) const {
-    const float e = __builtin_amdgcn_exp2f(two * fabsf(u));
-    const float t = fmaf(-2.f * top, __builtin_amdgcn_rcpf(1.f + e), top);
-    return fabsf(u) <= mid ? half(u) : __builtin_copysignf(t, u);
+    const float x = u * k;
+    const float e = __builtin_amdgcn_exp2f(2.f * kLog2e * fabsf(x));
+    const float t = fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + e), 1.f);
+    return fabsf(x) <= 0.5f ? half(u) : __builtin_copysignf(t, x);
   }
-  // of some of a wave's scores, by the largest of them in any lane
+  // of some of a wave's products, by the largest of them in any lane
   template <typename V, int N>
   PB_DEV void apply(V (&s)[N]) const {
     constexpr int W = sizeof(V) / 4;
@@ -150,7 +153,7 @@ struct Cap {
       for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int e = 0; e < W; ++e) s[i][e] = near(s[i][e]);
-    } else if (!__builtin_amdgcn_ballot_w64(largest > mid)) {
+    } else if (!__builtin_amdgcn_ballot_w64(largest > 4.f * small)) {
 #pragma unroll
       for (int i = 0; i < N; ++i)
 #pragma unroll
