@@ -162,7 +162,15 @@ struct RowBlock {
 };
 
 // ---------------------------------------------------------------- forward
-template <int D, bool CAP, int BIAS>
+// EARLY: V is requested ahead of the scores' products and the next K right behind them.
+// That takes 20 to 60 registers more, which pay where a CU has one workgroup (us, without
+// and with; the last with 512 workgroups):
+//   1 token over 4096, 32 heads over 8 x 128   150  99
+//   4 x 7 over 2048, 16 over 4 x 96             89  54
+//   256, 8 x 128                              13.5 12.2
+//   1000, 4 x 96                              28.4 25.8
+//   1024, 8 x 128                             49.5 55.6
+template <int D, bool CAP, int BIAS, bool EARLY>
 __global__ __launch_bounds__(64 * kW) void score_fwd_f32(ScoreArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   __shared__ float ml[2][kW][kR];
@@ -179,16 +187,33 @@ __global__ __launch_bounds__(64 * kW) void score_fwd_f32(ScoreArgs a) {
 #pragma unroll
   for (int db = 0; db < D / 16; ++db) acc[db] = zero4();
   float m = kNegInf, l = 0.f;
+  auto key_row = [&](int k) { return max(t.kt.lo, min(k, t.kt.hi)); };
+  f32x4 kf[D / 16];
+  auto load_k = [&](int n) {
+    row_frag<D>(score::kv_row<float, D>(a, a.k, t.b, key_row(t.kt.tile(n) * kR + i), t.kvh), g, kf);
+  };
+  if (EARLY && wave < t.kt.n) load_k(wave);
   for (int n = wave; n < t.kt.n; n += kW) {
     const int k0 = t.kt.tile(n) * kR;
-    auto key_row = [&](int k) { return max(t.kt.lo, min(k, t.kt.hi)); };
-    f32x4 kf[D / 16];
-    row_frag<D>(score::kv_row<float, D>(a, a.k, t.b, key_row(k0 + i), t.kvh), g, kf);
+    if constexpr (!EARLY) load_k(n);
     const float* vr[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       vr[j] = score::kv_row<float, D>(a, a.v, t.b, key_row(k0 + 4 * g + j), t.kvh) + i;
+    f32x4 vf[D / 16];
+    if constexpr (EARLY) {
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) vf[db][j] = vr[j][16 * db];
+      __builtin_amdgcn_sched_barrier(0);
+    }
     f32x4 s = terms.base(dot_rows<D>(kf, qf));
+    if constexpr (EARLY) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (n + kW < t.kt.n) load_k(n + kW);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     const uint32_t see = (uint32_t)(t.keys.bits(k0) >> (4 * g));
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -204,7 +229,15 @@ __global__ __launch_bounds__(64 * kW) void score_fwd_f32(ScoreArgs a) {
     m = mn;
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) acc[db] *= f;
-    add_rows<D>(vr, s, acc);
+    if constexpr (EARLY) {
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc[db] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[db][j], s[j], acc[db], 0, 0, 0);
+    } else {
+      add_rows<D>(vr, s, acc);
+    }
   }
   l = sum_groups(l);
   if (g == 0) ml[0][wave][i] = m, ml[1][wave][i] = l;
@@ -471,7 +504,12 @@ unsigned row_blocks(const ScoreArgs& a) {
 template <int D>
 void fwd_d(const ScoreArgs& a, hipStream_t s) {
   const size_t lds = a.table ? bias_of<D>(a).bytes : Merge<D>::kFloats * 4;
-#define PB_FWD(C, B) score_fwd_f32<D, C, B><<<row_blocks(a), 64 * kW, lds, s>>>(a)
+  const unsigned grid = row_blocks(a);
+#define PB_FWD(C, B)                                                       \
+  do {                                                                     \
+    if (grid <= 256) score_fwd_f32<D, C, B, true><<<grid, 64 * kW, lds, s>>>(a); \
+    else score_fwd_f32<D, C, B, false><<<grid, 64 * kW, lds, s>>>(a);      \
+  } while (0)
   PB_BY_TERMS(PB_FWD);
 #undef PB_FWD
 }
