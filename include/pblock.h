@@ -783,7 +783,7 @@ typedef struct {
   int causal;        /* 0 or 1                                                */
   int window;        /* >= 1                                                  */
   float scale;       /* > 0, finite                                           */
-  float cap;         /* 0 (none), or scale / 2^15 .. 2^100                    */
+  float cap;         /* 0 (none), or scale / 2^12 .. scale 2^120, <= 2^100    */
   int buckets;       /* 0 without a table; else 2 .. 64, or even, 4 .. 64,
                         when not causal                                       */
   int max_distance;  /* > half the buckets (of a side), <= 2^20               */

@@ -26,8 +26,11 @@ pb_status check_config(const pb_score_attn_config* c) {
   if (c->window < 1) return fail(PB_ERR_INVALID_ARG, "window=%d must be >= 1", c->window);
   if (!(c->scale > 0.f) || !std::isfinite(c->scale))
     return fail(PB_ERR_INVALID_ARG, "scale must be finite and > 0");
-  if (c->cap != 0.f && !(c->cap >= c->scale / 32768.f && c->cap <= 0x1p100f))
-    return fail(PB_ERR_INVALID_ARG, "cap must be 0, or in scale / 2^15 .. 2^100");
+  // (the coefficients of tanh hold powers of scale / cap up to the ninth)
+  if (c->cap != 0.f && !(c->cap >= c->scale / 4096.f && c->cap <= 0x1p100f &&
+                         c->cap <= c->scale * 0x1p120f))
+    return fail(PB_ERR_INVALID_ARG, "cap must be 0, or in scale / 2^12 .. scale 2^120, and at most "
+                "2^100");
   if (c->buckets != 0) {
     const int side = c->causal ? c->buckets : c->buckets / 2;
     if (c->buckets > PB_SCORE_MAX_BUCKETS || side < 2 || (!c->causal && c->buckets % 2))

@@ -283,3 +283,22 @@ def test_unsorted_offsets_touch_nothing_outside():
     for n, x in c.full.items():
         assert bool((x[:, -c.pad:] == 7.0).all()), n
     assert torch.isfinite(c.o.float()).all() and torch.isfinite(c.dk.float()).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bias", [dict(), dict(slopes=True), dict(buckets=8, max_distance=20)])
+@pytest.mark.parametrize("cap", [2.0 ** -12, 2.0 ** -6, 1.0, 2.0 ** 99])
+def test_caps_to_the_bounds(dtype, bias, cap):
+    """From scores that are all at the cap to those far below it.  (Where 1 - tanh^2 is
+    next to nothing, its rounding, 2^-24 of 1, is all there is of dq and dk: they are only
+    finite there.)"""
+    import torch
+    print(dtype, bias, cap, flush=True)
+    c = Case(dtype=dtype, seq=100, heads=2, kv_heads=1, cap=cap * 64 ** -0.5, **bias)
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    r = c.oracle()
+    c.check(r, ("o", "lse"))
+    c.check(r, ("dv", "dtable") + (("dq", "dk") if cap > 1 else ()))
+    assert bool(torch.isfinite(c.dq).all()) and bool(torch.isfinite(c.dk).all())

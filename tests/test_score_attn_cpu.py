@@ -50,7 +50,8 @@ BUCKETS = dict(buckets=8, max_distance=20)
     (dict(heads=0), BAD), (dict(kv_heads=0), BAD), (dict(kv_heads=3), BAD), (dict(head_dim=80), UNSUPPORTED),
     (dict(causal=2), BAD), (dict(window=0), BAD), (dict(scale=0.0), BAD), (dict(scale=NAN), BAD),
     (dict(scale=INF), BAD), (dict(cap=-1.0), BAD), (dict(cap=NAN), BAD), (dict(cap=INF), BAD),
-    (dict(cap=1e-9), BAD), (dict(dtype=7), BAD),
+    (dict(cap=1e-9), BAD), (dict(dtype=7), BAD), (dict(cap=0.125 / 4100), BAD), (dict(cap=2.0 ** 101), BAD),
+    (dict(cap=1.0, scale=2.0 ** -121), BAD),
     (dict(buckets=8, max_distance=4), BAD), (dict(buckets=1, max_distance=9), BAD),
     (dict(buckets=65, max_distance=99), BAD), (dict(buckets=8, max_distance=1 << 21), BAD),
     (dict(buckets=8, max_distance=20, causal=0), BAD),  # buckets without a table
