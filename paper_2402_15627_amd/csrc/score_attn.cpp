@@ -129,7 +129,14 @@ pb::ScoreArgs args_of(const pb_score_attn_config* c, const pb_score_terms* t) {
   a.docs = t->docs, a.prefix = t->prefix, a.n_docs = t->n_docs;
   a.slopes = t->slopes, a.table = t->table;
   a.buckets = c->buckets, a.side = c->causal ? c->buckets : c->buckets / 2;
-  if (c->buckets) borders_of(c, a.first);
+  if (c->buckets) {
+    borders_of(c, a.first);
+    unsigned char* map = reinterpret_cast<unsigned char*>(a.map);
+    for (int d = 0, k = 0; d < pb::kScoreMap; ++d) {
+      while (k + 1 < a.side && a.first[k + 1] <= d) ++k;
+      map[d] = (unsigned char)k;
+    }
+  }
   a.pack = 1;
   // (with a table a power of two: lanes of the table's gradient have one head each)
   for (int n = 2; n <= kMaxPack; ++n)

@@ -10,6 +10,7 @@
 namespace pb {
 
 constexpr int kScoreMaxBuckets = 64;
+constexpr int kScoreMap = 512;
 
 struct ScoreArgs {
   const void *q, *k, *v;
@@ -29,6 +30,7 @@ struct ScoreArgs {
   const float *slopes, *table;
   int buckets, side;            // side: buckets of one sign of the distance
   int first[kScoreMaxBuckets];  // first distance of each bucket of a side
+  uint32_t map[kScoreMap / 4];  // a byte each: bucket of the distances below kScoreMap
   float* dtable;
   float* bias_part;             // sums of the table's gradient, [batch * row blocks][heads][buckets]
   int pack;                     // heads of one key head that a block of rows holds

@@ -347,8 +347,6 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
   if constexpr (BIAS == kTable) {
     bias_prologue(a, bl, smem, h0, a.pack, tid, 256);
     __syncthreads();
-    bias_map(a, bl, smem, tid, 256);
-    __syncthreads();
     build(0);
   }
   issue_stage(0);
@@ -542,8 +540,6 @@ struct RowTiles {
   }
   PB_DEV void tables() {
     bias_prologue(a, bl, smem, h0, a.pack, threadIdx.x, 256);
-    __syncthreads();
-    bias_map(a, bl, smem, threadIdx.x, 256);
     __syncthreads();
   }
   PB_DEV int uniform(int kv0) const {

@@ -134,8 +134,6 @@ struct Terms {
 PB_DEV void bias_tables(const ScoreArgs& a, const BiasLds& bl, unsigned char* smem, int h0) {
   bias_prologue(a, bl, smem, h0, a.pack, threadIdx.x, 256, 1.f);
   __syncthreads();
-  bias_map(a, bl, smem, threadIdx.x, 256);
-  __syncthreads();
 }
 
 // A block of 16 packed rows: what forward and dQ share.

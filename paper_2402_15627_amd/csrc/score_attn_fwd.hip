@@ -189,8 +189,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
     bias_last = a.first[a.side - 1];
     bias_prologue(a, bl, smem, h0, a.pack, tid, 256);
     __syncthreads();
-    bias_map(a, bl, smem, tid, 256);
-    __syncthreads();
     build(0);
     if (n > 1) build(1);
     const float* tab = (const float*)(smem + bl.tab);

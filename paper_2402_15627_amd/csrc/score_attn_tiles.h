@@ -174,7 +174,7 @@ struct Cap {
 // does for a tile.  Bytes: the table of the block's heads, the first distances, the
 // buckets of distances below kMap, two tiles' biases.
 struct BiasLds {
-  static constexpr int kMap = 512;
+  static constexpr int kMap = kScoreMap;
   int stride;  // floats of a head's biases in a tile
   int tab, first, map, tile0, bytes;
   __host__ __device__ BiasLds(int at, int buckets, int pack, int positions, int keys) {
@@ -197,6 +197,7 @@ PB_DEV void bias_prologue(const ScoreArgs& a, const BiasLds& l, unsigned char* s
   }
   int* first = (int*)(smem + l.first);
   if (tid < a.side) first[tid] = a.first[tid];
+  for (int x = tid; x < kScoreMap / 4; x += threads) ((uint32_t*)(smem + l.map))[x] = a.map[x];
 }
 PB_DEV int bias_search(const int* first, int side, int d) {
   int lo = 0, hi = side - 1;
@@ -206,11 +207,6 @@ PB_DEV int bias_search(const int* first, int side, int d) {
     else hi = mid - 1;
   }
   return lo;
-}
-PB_DEV void bias_map(const ScoreArgs& a, const BiasLds& l, unsigned char* smem, int tid,
-                     int threads) {
-  for (int d = tid; d < BiasLds::kMap; d += threads)
-    smem[l.map + d] = (uint8_t)bias_search((const int*)(smem + l.first), a.side, d);
 }
 PB_DEV int bias_bucket(const ScoreArgs& a, const BiasLds& l, const unsigned char* smem, int n) {
   const int d = a.causal ? max(n, 0) : abs(n);
