@@ -1,8 +1,8 @@
 // Attention with terms in its scores in fp32, forward and backward, on
 // v_mfma_f32_16x16x4_f32.  The layout is that of attn_f32.hip: a workgroup of four waves
-// has 16 rows (queries of the heads that share a key head, see Packed; or keys) and
-// walks tiles of 16 of the other side, tile t on wave t mod 4; everything is computed
-// transposed, so that a lane owns one row and the probabilities leave the score
+// (eight in a backward of long rows and few workgroups) has 16 rows (queries of the heads
+// that share a key head, see Packed; or keys) and walks tiles of 16 of the other side, its
+// waves in turn; everything is computed transposed, so that a lane owns one row and the probabilities leave the score
 // accumulators in the order in which the next product contracts them; fragments go from
 // global memory to registers, and the waves' parts are merged through LDS.
 //
@@ -12,8 +12,9 @@
 // the dQ role: each lane adds dz to a place of its own for each bucket.
 //
 // A workgroup with a non-finite result computes its rows again by the definition, which
-// reads visible rows alone.  Bound by latency at the sizes that fp32 runs at, by the
-// matrix cores in long rows.
+// reads visible rows alone.  Bound by the chain of loads, products and exponentials in each
+// wave: 2 x 333 tokens, 16 heads over 4 x 96, forward 22.5 us with the matrix cores busy
+// 18% (30 TFLOP/s), backward 89.
 #include "kernels.h"
 #include "score_attn_tiles.h"
 
@@ -21,8 +22,8 @@ namespace pb {
 namespace {
 
 constexpr int kNoBias = 0, kSlopes = 1, kTable = 2;
-constexpr int kW = 4;   // waves
-constexpr int kR = 16;  // rows of a block and of a tile
+constexpr int kR = 16;   // rows of a block and of a tile
+constexpr int kFwd = 4;  // waves of a workgroup of the forward
 
 // 2^(s log2 e - ref), and e^(s - L), each with what the products with log2 e lose.
 constexpr float kLog2eRest = 1.9259630e-8f;  // log2 e - kLog2e
@@ -74,13 +75,13 @@ PB_DEV void add_rows(const float* const (&x)[4], const f32x4& p, f32x4 (&out)[D 
 }
 
 // Sum of the waves' [16][D] parts; each thread's float4 number n is row(n), col(n).
-template <int D>
+template <int D, int W>
 struct Merge {
-  static constexpr int kVec = (kR * D / 4 + 255) / 256;
-  static constexpr int kFloats = kW * kR * (D + 4);
-  static PB_DEV bool has(int n) { return (int)threadIdx.x + 256 * n < kR * D / 4; }
-  static PB_DEV int row(int n) { return ((int)threadIdx.x + 256 * n) / (D / 4); }
-  static PB_DEV int col(int n) { return 4 * (((int)threadIdx.x + 256 * n) % (D / 4)); }
+  static constexpr int kVec = (kR * D / 4 + 64 * W - 1) / (64 * W);
+  static constexpr int kFloats = W * kR * (D + 4);
+  static PB_DEV bool has(int n) { return (int)threadIdx.x + 64 * W * n < kR * D / 4; }
+  static PB_DEV int row(int n) { return ((int)threadIdx.x + 64 * W * n) / (D / 4); }
+  static PB_DEV int col(int n) { return 4 * (((int)threadIdx.x + 64 * W * n) % (D / 4)); }
   static PB_DEV void run(float* __restrict__ buf, const f32x4 (&part)[D / 16], float f, int wave,
                          int i, int g, f32x4 (&sum)[kVec]) {
 #pragma unroll
@@ -92,14 +93,14 @@ struct Merge {
       sum[n] = zero4();
       if (!has(n)) continue;
 #pragma unroll
-      for (int w = 0; w < kW; ++w)
+      for (int w = 0; w < W; ++w)
         sum[n] += *reinterpret_cast<const f32x4*>(buf + (w * kR + row(n)) * (D + 4) + col(n));
     }
   }
 };
-template <int D>
+template <int D, int W>
 __host__ __device__ BiasLds bias_of(const ScoreArgs& a) {
-  return BiasLds(Merge<D>::kFloats * 4, a.buckets, a.pack, 0, 0);
+  return BiasLds(Merge<D, W>::kFloats * 4, a.buckets, a.pack, 0, 0);
 }
 
 // Scores of a tile with their terms, natural; z0: the capped ones before their bias.
@@ -131,8 +132,9 @@ struct Terms {
     return fmaf(-t, t, 1.f);
   }
 };
-PB_DEV void bias_tables(const ScoreArgs& a, const BiasLds& bl, unsigned char* smem, int h0) {
-  bias_prologue(a, bl, smem, h0, a.pack, threadIdx.x, 256, 1.f);
+PB_DEV void bias_tables(const ScoreArgs& a, const BiasLds& bl, unsigned char* smem, int h0,
+                        int threads) {
+  bias_prologue(a, bl, smem, h0, a.pack, threadIdx.x, threads, 1.f);
   __syncthreads();
 }
 
@@ -169,16 +171,17 @@ struct RowBlock {
 //   1000, 4 x 96                              28.4 25.8
 //   1024, 8 x 128                             49.5 55.6
 template <int D, bool CAP, int BIAS, bool EARLY>
-__global__ __launch_bounds__(64 * kW) void score_fwd_f32(ScoreArgs a) {
+__global__ __launch_bounds__(64 * kFwd) void score_fwd_f32(ScoreArgs a) {
+  constexpr int W = kFwd;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  __shared__ float ml[2][kW][kR];
+  __shared__ float ml[2][W][kR];
   float* buf = (float*)smem;
-  const BiasLds bl = bias_of<D>(a);
+  const BiasLds bl = bias_of<D, W>(a);
   const int hb_n = a.batch * (a.heads / a.pack), nblk = gridDim.x / hb_n;
   const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const RowBlock t(a, nblk - 1 - blockIdx.x / hb_n, blockIdx.x % hb_n, lane);
-  if constexpr (BIAS == kTable) bias_tables(a, bl, smem, t.h0);
+  if constexpr (BIAS == kTable) bias_tables(a, bl, smem, t.h0, 64 * W);
   const Terms<CAP, BIAS> terms(a, bl, smem);
   f32x4 qf[D / 16], acc[D / 16];
   row_frag<D>(score::q_row<float, D>(a, t.b, t.i, t.h0 + t.hh), g, qf);
@@ -191,7 +194,7 @@ __global__ __launch_bounds__(64 * kW) void score_fwd_f32(ScoreArgs a) {
     row_frag<D>(score::kv_row<float, D>(a, a.k, t.b, key_row(t.kt.tile(n) * kR + i), t.kvh), g, kf);
   };
   if (EARLY && wave < t.kt.n) load_k(wave);
-  for (int n = wave; n < t.kt.n; n += kW) {
+  for (int n = wave; n < t.kt.n; n += W) {
     const int k0 = t.kt.tile(n) * kR;
     if constexpr (!EARLY) load_k(n);
     const float* vr[4];
@@ -209,7 +212,7 @@ __global__ __launch_bounds__(64 * kW) void score_fwd_f32(ScoreArgs a) {
     f32x4 s = terms.base(dot_rows<D>(kf, qf));
     if constexpr (EARLY) {
       __builtin_amdgcn_sched_barrier(0);
-      if (n + kW < t.kt.n) load_k(n + kW);
+      if (n + W < t.kt.n) load_k(n + W);
       __builtin_amdgcn_sched_barrier(0);
     }
     const uint32_t see = (uint32_t)(t.keys.bits(k0) >> (4 * g));
@@ -242,19 +245,19 @@ __global__ __launch_bounds__(64 * kW) void score_fwd_f32(ScoreArgs a) {
   __syncthreads();
   float M = kNegInf, L = 0.f;
 #pragma unroll
-  for (int w = 0; w < kW; ++w) M = fmaxf(M, ml[0][w][i]);
+  for (int w = 0; w < W; ++w) M = fmaxf(M, ml[0][w][i]);
   const float mu = M == kNegInf ? 0.f : M;
 #pragma unroll
-  for (int w = 0; w < kW; ++w) L += ml[1][w][i] * exp2_hw(ml[0][w][i] - mu);
-  f32x4 o[Merge<D>::kVec];
-  Merge<D>::run(buf, acc, L == 0.f ? 0.f : exp2_hw(m - mu) / L, wave, i, g, o);
+  for (int w = 0; w < W; ++w) L += ml[1][w][i] * exp2_hw(ml[0][w][i] - mu);
+  f32x4 o[Merge<D, W>::kVec];
+  Merge<D, W>::run(buf, acc, L == 0.f ? 0.f : exp2_hw(m - mu) / L, wave, i, g, o);
   const float ls = L == 0.f ? kNegInf : fmaf(M, kLn2, logf(L));
   bool bad = wave == 0 && g == 0 && t.r < t.rows && !(L - L == 0.f);
 #pragma unroll
-  for (int n = 0; n < Merge<D>::kVec; ++n)
-    bad |= Merge<D>::has(n) && t.r0 + Merge<D>::row(n) < t.rows && !finite4(o[n]);
+  for (int n = 0; n < Merge<D, W>::kVec; ++n)
+    bad |= Merge<D, W>::has(n) && t.r0 + Merge<D, W>::row(n) < t.rows && !finite4(o[n]);
   if (__syncthreads_or(bad)) {
-    for (int r = t.r0 + wave; r < min(t.r0 + kR, t.rows); r += kW) {
+    for (int r = t.r0 + wave; r < min(t.r0 + kR, t.rows); r += W) {
       int pos;
       const int h = t.head_of(r, pos);
       score::fwd_row<float, D>(a, t.b, h, pos, lane);
@@ -262,30 +265,30 @@ __global__ __launch_bounds__(64 * kW) void score_fwd_f32(ScoreArgs a) {
     return;
   }
 #pragma unroll
-  for (int n = 0; n < Merge<D>::kVec; ++n) {
-    const int r = t.r0 + Merge<D>::row(n);
-    if (!Merge<D>::has(n) || r >= t.rows) continue;
+  for (int n = 0; n < Merge<D, W>::kVec; ++n) {
+    const int r = t.r0 + Merge<D, W>::row(n);
+    if (!Merge<D, W>::has(n) || r >= t.rows) continue;
     int pos;
     const int h = t.head_of(r, pos);
-    *reinterpret_cast<f32x4*>(score::o_row<float, D>(a, t.b, pos, h) + Merge<D>::col(n)) = o[n];
+    *reinterpret_cast<f32x4*>(score::o_row<float, D>(a, t.b, pos, h) + Merge<D, W>::col(n)) = o[n];
   }
   if (wave == 0 && g == 0 && t.r < t.rows) a.lse[score::lse_at(a, t.b, t.h0 + t.hh, t.i)] = ls;
 }
 
 // --------------------------------------------------------------- backward
-template <int D, bool CAP, int BIAS>
+template <int D, bool CAP, int BIAS, int W>
 PB_DEV void dq_block(const ScoreArgs& a, int blk, int nblk, int hb) {
   constexpr int kPad = 65;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   float* buf = (float*)smem;
-  const BiasLds bl = bias_of<D>(a);
+  const BiasLds bl = bias_of<D, W>(a);
   const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const RowBlock t(a, blk, hb, lane);
   float* slots = (float*)(smem + bl.bytes);
   float* mine = slots + wave * a.buckets * kPad + lane;
   if constexpr (BIAS == kTable) {
-    bias_tables(a, bl, smem, t.h0);
+    bias_tables(a, bl, smem, t.h0, 64 * W);
     if (a.dtable)
       for (int n = 0; n < a.buckets; ++n) mine[n * kPad] = 0.f;
   }
@@ -306,7 +309,7 @@ PB_DEV void dq_block(const ScoreArgs& a, int blk, int nblk, int hb) {
   }
   float dl = sum_groups((x[0] + x[1]) + (x[2] + x[3]));
   if (!live) dl = 0.f;
-  for (int n = wave; n < t.kt.n; n += kW) {
+  for (int n = wave; n < t.kt.n; n += W) {
     const int k0 = t.kt.tile(n) * kR;
     auto key_row = [&](int k) { return max(t.kt.lo, min(k, t.kt.hi)); };
     f32x4 kf[D / 16], vf[D / 16];
@@ -331,17 +334,17 @@ PB_DEV void dq_block(const ScoreArgs& a, int blk, int nblk, int hb) {
     }
     add_rows<D>(kr, ds, dq);
   }
-  f32x4 o[Merge<D>::kVec];
-  Merge<D>::run(buf, dq, a.scale, wave, i, g, o);  // (its barrier: every wave's sums are there)
+  f32x4 o[Merge<D, W>::kVec];
+  Merge<D, W>::run(buf, dq, a.scale, wave, i, g, o);  // (its barrier: every wave's sums are there)
   if constexpr (BIAS == kTable) {
     if (a.dtable)
-      for (int y = threadIdx.x; y < a.buckets * a.pack; y += 256) {
+      for (int y = threadIdx.x; y < a.buckets * a.pack; y += 64 * W) {
         const int n = y % a.buckets, hh = y / a.buckets;
         float s = 0.f;
         for (int q = 0; q < kR; ++q) {
           int pos;
           if (t.head_of(t.r0 + q, pos) != t.h0 + hh) continue;
-          for (int w = 0; w < kW; ++w)
+          for (int w = 0; w < W; ++w)
 #pragma unroll
             for (int k = 0; k < 4; ++k) s += slots[(w * a.buckets + n) * kPad + q + 16 * k];
         }
@@ -350,10 +353,10 @@ PB_DEV void dq_block(const ScoreArgs& a, int blk, int nblk, int hb) {
   }
   bool bad = false;
 #pragma unroll
-  for (int n = 0; n < Merge<D>::kVec; ++n)
-    bad |= Merge<D>::has(n) && t.r0 + Merge<D>::row(n) < t.rows && !finite4(o[n]);
+  for (int n = 0; n < Merge<D, W>::kVec; ++n)
+    bad |= Merge<D, W>::has(n) && t.r0 + Merge<D, W>::row(n) < t.rows && !finite4(o[n]);
   if (__syncthreads_or(bad)) {
-    for (int r = t.r0 + wave; r < min(t.r0 + kR, t.rows); r += kW) {
+    for (int r = t.r0 + wave; r < min(t.r0 + kR, t.rows); r += W) {
       int pos;
       const int hr = t.head_of(r, pos);
       score::dq_row<float, D>(a, t.b, hr, pos, lane);
@@ -361,21 +364,21 @@ PB_DEV void dq_block(const ScoreArgs& a, int blk, int nblk, int hb) {
     return;
   }
 #pragma unroll
-  for (int n = 0; n < Merge<D>::kVec; ++n) {
-    const int r = t.r0 + Merge<D>::row(n);
-    if (!Merge<D>::has(n) || r >= t.rows) continue;
+  for (int n = 0; n < Merge<D, W>::kVec; ++n) {
+    const int r = t.r0 + Merge<D, W>::row(n);
+    if (!Merge<D, W>::has(n) || r >= t.rows) continue;
     int pos;
     const int hr = t.head_of(r, pos);
     *reinterpret_cast<f32x4*>((float*)a.dq + ((size_t)t.b * a.seq_q + pos) * a.ld_dq + hr * D +
-                              Merge<D>::col(n)) = o[n];
+                              Merge<D, W>::col(n)) = o[n];
   }
 }
 
-template <int D, bool CAP, int BIAS>
+template <int D, bool CAP, int BIAS, int W>
 PB_DEV void dkdv_block(const ScoreArgs& a, int blk, int hb) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   float* buf = (float*)smem;
-  const BiasLds bl = bias_of<D>(a);
+  const BiasLds bl = bias_of<D, W>(a);
   const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int b = hb / a.kv_heads, kvh = hb % a.kv_heads, j0 = blk * kR, key = j0 + i;
@@ -400,9 +403,9 @@ PB_DEV void dkdv_block(const ScoreArgs& a, int blk, int hb) {
   for (int h0 = kvh * a.group; h0 < (kvh + 1) * a.group; h0 += a.pack) {
     if constexpr (BIAS == kTable) {
       __syncthreads();  // (every wave is done with the last heads' table)
-      bias_tables(a, bl, smem, h0);
+      bias_tables(a, bl, smem, h0, 64 * W);
     }
-    for (int r0 = r_lo / kR * kR + kR * wave; r0 <= r_hi; r0 += kR * kW) {
+    for (int r0 = r_lo / kR * kR + kR * wave; r0 <= r_hi; r0 += kR * W) {
       auto row_of = [&](int r, int& h) {
         const int x = max(r_lo, min(r, r_hi)), pos = pk.pos(x);
         h = h0 + x - pos * a.pack;
@@ -445,41 +448,41 @@ PB_DEV void dkdv_block(const ScoreArgs& a, int blk, int hb) {
       add_rows<D>(qr, ds, dk);
     }
   }
-  f32x4 ov[Merge<D>::kVec], ok[Merge<D>::kVec];
-  Merge<D>::run(buf, dv, 1.f, wave, i, g, ov);
+  f32x4 ov[Merge<D, W>::kVec], ok[Merge<D, W>::kVec];
+  Merge<D, W>::run(buf, dv, 1.f, wave, i, g, ov);
   __syncthreads();
-  Merge<D>::run(buf, dk, a.scale, wave, i, g, ok);
+  Merge<D, W>::run(buf, dk, a.scale, wave, i, g, ok);
   bool bad = false;
 #pragma unroll
-  for (int n = 0; n < Merge<D>::kVec; ++n)
-    bad |= Merge<D>::has(n) && j0 + Merge<D>::row(n) < a.seq_k && !(finite4(ov[n]) && finite4(ok[n]));
+  for (int n = 0; n < Merge<D, W>::kVec; ++n)
+    bad |= Merge<D, W>::has(n) && j0 + Merge<D, W>::row(n) < a.seq_k && !(finite4(ov[n]) && finite4(ok[n]));
   if (__syncthreads_or(bad)) {
-    for (int r = j0 + wave; r < min(j0 + kR, a.seq_k); r += kW)
+    for (int r = j0 + wave; r < min(j0 + kR, a.seq_k); r += W)
       score::dkdv_row<float, D>(a, b, kvh, r, lane);
     return;
   }
 #pragma unroll
-  for (int n = 0; n < Merge<D>::kVec; ++n)
-    if (Merge<D>::has(n) && j0 + Merge<D>::row(n) < a.seq_k) {
-      const size_t at = ((size_t)b * a.seq_k + j0 + Merge<D>::row(n)) * a.ld_dkv + kvh * D +
-                        Merge<D>::col(n);
+  for (int n = 0; n < Merge<D, W>::kVec; ++n)
+    if (Merge<D, W>::has(n) && j0 + Merge<D, W>::row(n) < a.seq_k) {
+      const size_t at = ((size_t)b * a.seq_k + j0 + Merge<D, W>::row(n)) * a.ld_dkv + kvh * D +
+                        Merge<D, W>::col(n);
       *reinterpret_cast<f32x4*>((float*)a.dk + at) = ok[n];
       *reinterpret_cast<f32x4*>((float*)a.dv + at) = ov[n];
     }
 }
 
 // Both roles in one launch, in turn, each longest first.
-template <int D, bool CAP, int BIAS>
-__global__ __launch_bounds__(64 * kW) void score_bwd_f32(ScoreArgs a, int nk, int nq) {
+template <int D, bool CAP, int BIAS, int W>
+__global__ __launch_bounds__(64 * W) void score_bwd_f32(ScoreArgs a, int nk, int nq) {
   const int id = blockIdx.x, mn = min(nk, nq);
   const bool kv = id < 2 * mn ? !(id & 1) : nk > nq;
   const int x = id < 2 * mn ? id >> 1 : id - mn;
   if (kv) {
     const int n = a.batch * a.kv_heads;
-    dkdv_block<D, CAP, BIAS>(a, x / n, x % n);
+    dkdv_block<D, CAP, BIAS, W>(a, x / n, x % n);
   } else {
     const int n = a.batch * (a.heads / a.pack), nblk = nq / n;
-    dq_block<D, CAP, BIAS>(a, nblk - 1 - x / n, nblk, x % n);
+    dq_block<D, CAP, BIAS, W>(a, nblk - 1 - x / n, nblk, x % n);
   }
 }
 
@@ -501,24 +504,52 @@ unsigned row_blocks(const ScoreArgs& a) {
 
 template <int D>
 void fwd_d(const ScoreArgs& a, hipStream_t s) {
-  const size_t lds = a.table ? bias_of<D>(a).bytes : Merge<D>::kFloats * 4;
+  const size_t lds = a.table ? bias_of<D, kFwd>(a).bytes : Merge<D, kFwd>::kFloats * 4;
   const unsigned grid = row_blocks(a);
-#define PB_FWD(C, B)                                                       \
-  do {                                                                     \
-    if (grid <= 256) score_fwd_f32<D, C, B, true><<<grid, 64 * kW, lds, s>>>(a); \
-    else score_fwd_f32<D, C, B, false><<<grid, 64 * kW, lds, s>>>(a);      \
+#define PB_FWD(C, B)                                                                   \
+  do {                                                                                 \
+    if (grid <= 256) score_fwd_f32<D, C, B, true><<<grid, 64 * kFwd, lds, s>>>(a);     \
+    else score_fwd_f32<D, C, B, false><<<grid, 64 * kFwd, lds, s>>>(a);                \
   } while (0)
   PB_BY_TERMS(PB_FWD);
 #undef PB_FWD
 }
+
+// Waves of a backward workgroup: eight where the longest row of tiles, shared by four,
+// would take half as long again as all tiles over the card's waves (two a SIMD), and has
+// 32 tiles; else four.  Timed (us, four and eight waves):
+//   333 x 2, 16 over 4 x 96          99.6  88.6     1024, 8 x 128                173 179
+//   1000, 4 x 96                       84    69     900 x 2, 8 over 4 x 64       130 152
+//   2048, 2 x 128                     213   164     4096, 4 x 64                 541 575
+//   700 x 2, 8 over 2 x 64, a table   156   127     2048, 16 x 96, window 256    239 316
+//   1 over 4096, 32 over 8 x 128      253   186     256, 4 x 128                25.8 26.8
+int bwd_waves(const ScoreArgs& a, int nk, int nq) {
+  const long long rows = ((long long)a.seq_q * a.pack + kR - 1) / kR, sets = a.group / a.pack;
+  const long long reach = (long long)(a.causal ? 1 : 2) * a.window + kR;
+  const double kv = (double)sets * (a.prefix ? rows : std::min(rows, reach * a.pack / kR + 2));
+  const double q = score_most_tiles(a, kR, kR);
+  const double half = a.causal && a.window >= a.seq_k ? 0.5 : 1.0;
+  const double all = half * (nk * kv + nq * q) / 2048, longest = std::max(kv, q);
+  return longest >= 32 && longest / 4 >= 1.5 * all ? 8 : 4;
+}
+template <int D, int W>
+size_t bwd_lds(const ScoreArgs& a) {
+  return (a.table ? bias_of<D, W>(a).bytes : Merge<D, W>::kFloats * 4) +
+         (a.dtable ? (size_t)W * a.buckets * 65 * 4 : 0);
+}
+template <int D, int W>
+void bwd_w(const ScoreArgs& a, int nk, int nq, hipStream_t s) {
+  const size_t lds = bwd_lds<D, W>(a);
+#define PB_BWD(C, B) score_bwd_f32<D, C, B, W><<<nk + nq, 64 * W, lds, s>>>(a, nk, nq)
+  PB_BY_TERMS(PB_BWD);
+#undef PB_BWD
+}
 template <int D>
 void bwd_d(const ScoreArgs& a, hipStream_t s) {
   const int nq = (int)row_blocks(a), nk = (a.seq_k + kR - 1) / kR * a.batch * a.kv_heads;
-  size_t lds = a.table ? bias_of<D>(a).bytes : Merge<D>::kFloats * 4;
-  if (a.dtable) lds += (size_t)kW * a.buckets * 65 * 4;
-#define PB_BWD(C, B) score_bwd_f32<D, C, B><<<nk + nq, 64 * kW, lds, s>>>(a, nk, nq)
-  PB_BY_TERMS(PB_BWD);
-#undef PB_BWD
+  // (a table of many buckets leaves room for four waves' sums)
+  if (bwd_waves(a, nk, nq) == 8 && bwd_lds<D, 8>(a) <= 152 * 1024) bwd_w<D, 8>(a, nk, nq, s);
+  else bwd_w<D, 4>(a, nk, nq, s);
   if (a.dtable)
     launch_score_dtable_sum(a, (a.seq_q * a.pack + kR - 1) / kR * a.batch, s);
 }

@@ -302,3 +302,15 @@ def test_caps_to_the_bounds(dtype, bias, cap):
     c.check(r, ("o", "lse"))
     c.check(r, ("dv", "dtable") + (("dq", "dk") if cap > 1 else ()))
     assert bool(torch.isfinite(c.dq).all()) and bool(torch.isfinite(c.dk).all())
+
+
+@pytest.mark.parametrize("what", [
+    dict(seq=600, heads=4, kv_heads=1, docs=[0, 250, 251, 599], prefix=[40, 0, 300], cap=5.0),
+    dict(seq=530, heads=2, kv_heads=1, d=96, buckets=32, max_distance=200),
+    dict(seq=530, heads=2, kv_heads=1, buckets=64, max_distance=200, d=128),
+    dict(seq=900, seq_q=3, heads=4, kv_heads=2, slopes=True, causal=False)])
+def test_long_rows_in_fp32(what):
+    """Rows of 32 tiles and more: backward workgroups of eight waves (with 64 buckets, of
+    four)."""
+    print(what, flush=True)
+    Case(dtype="f32", **what).run()
