@@ -6,9 +6,10 @@
 // Bound by HBM: each element of w, g and the states is read once and written
 // once (30 bytes with a bf16 copy of w, 18 with states of 8 bits), so the
 // arithmetic is free as long as it stays under about a hundred instructions an
-// element.  A launch takes up to kAdamMax tensors, cut into chunks of 1024
-// elements, a workgroup each; a thread has four elements, a wave the 256 that
-// share the scales of an 8-bit state.
+// element: 226.5 M parameters 1165 us (5.8 TB/s), in 8 bits 664 (6.1).  A launch
+// takes up to kAdamMax tensors, cut into chunks of 1024 elements, a workgroup
+// each (2048: 1191 us, 4096: 1195); a thread has four elements, a wave the 256
+// that share the scales of an 8-bit state.
 //
 // Every operation is rounded by itself (no contraction into fused products): a
 // value that decides an 8-bit code is then the one that elementary operations
@@ -70,8 +71,8 @@ PB_DEV uint32_t code_e4m3(float a, uint32_t rnd) {
 // Four elements' updated state x (lane's part of its wave's 256) as codes; their
 // scale is the largest magnitude over 448 (its product with the rounded 1/448),
 // at least 2^-126.  A value that is not finite makes the scale so (magnitudes are
-// compared as words, where NaN is above all).  bits: of each, random; the upper half, or with KEEP the lower.  KEEP (x >= 0):
-// what is above zero keeps a code above zero.
+// compared as words, where NaN is above all).  bits: random, of each element; the upper
+// half, or with KEEP the lower.  KEEP (x >= 0): what is above zero keeps a code above zero.
 template <bool KEEP>
 PB_DEV uint32_t quantise(const f32x4& x, const uint32_t (&bits)[4], float& scale) {
 #pragma clang fp contract(off)

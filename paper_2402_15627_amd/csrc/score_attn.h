@@ -32,7 +32,7 @@ struct ScoreArgs {
   int first[kScoreMaxBuckets];  // first distance of each bucket of a side
   uint32_t map[kScoreMap / 4];  // a byte each: bucket of the distances below kScoreMap
   float* dtable;
-  float* bias_part;             // sums of the table's gradient, [batch * row blocks][heads][buckets]
+  float* bias_part;  // sums of the table's gradient, [batch * row blocks][heads][buckets]
   int pack;                     // heads of one key head that a block of rows holds
 };
 

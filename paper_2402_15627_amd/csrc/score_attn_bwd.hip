@@ -16,6 +16,11 @@
 // over the tiles beyond the last bucket's first distance.  A last launch goes over the
 // other tiles again, with the row terms put right.
 //
+// Bound by the vector instructions of the terms beside the products, at two waves a SIMD
+// (registers): 4096 tokens of packed documents, 16 heads over 4 x 128, capped 234 us, 424
+// TFLOP/s, matrix cores busy 26%, vector instructions 45%; 8192 x 40 heads, window 1024,
+// without terms 820 us (attn.hip 855), capped 890, with a table 840 and its gradient 970.
+//
 // Non-finite values behind the mask are met as in the forward.
 #include "kernels.h"
 #include "score_attn_tiles.h"

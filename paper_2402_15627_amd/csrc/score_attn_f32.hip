@@ -2,9 +2,10 @@
 // v_mfma_f32_16x16x4_f32.  The layout is that of attn_f32.hip: a workgroup of four waves
 // (eight in a backward of long rows and few workgroups) has 16 rows (queries of the heads
 // that share a key head, see Packed; or keys) and walks tiles of 16 of the other side, its
-// waves in turn; everything is computed transposed, so that a lane owns one row and the probabilities leave the score
-// accumulators in the order in which the next product contracts them; fragments go from
-// global memory to registers, and the waves' parts are merged through LDS.
+// waves in turn; everything is computed transposed, so that a lane owns one row and the
+// probabilities leave the score accumulators in the order in which the next product
+// contracts them; fragments go from global memory to registers, and the waves' parts are
+// merged through LDS.
 //
 // Scores, with their terms, are natural logarithms here and turn to base 2 in the
 // exponential, with the roundings of the products with log2 e added back.  The row term
@@ -455,7 +456,8 @@ PB_DEV void dkdv_block(const ScoreArgs& a, int blk, int hb) {
   bool bad = false;
 #pragma unroll
   for (int n = 0; n < Merge<D, W>::kVec; ++n)
-    bad |= Merge<D, W>::has(n) && j0 + Merge<D, W>::row(n) < a.seq_k && !(finite4(ov[n]) && finite4(ok[n]));
+    bad |= Merge<D, W>::has(n) && j0 + Merge<D, W>::row(n) < a.seq_k &&
+           !(finite4(ov[n]) && finite4(ok[n]));
   if (__syncthreads_or(bad)) {
     for (int r = j0 + wave; r < min(j0 + kR, a.seq_k); r += W)
       score::dkdv_row<float, D>(a, b, kvh, r, lane);

