@@ -241,6 +241,7 @@ template <int D, int TL, int NW, bool VSWZ = false>
 struct DmaRows {
   static constexpr int NP = TL * 2 * D / 1024;
   static constexpr int NPW = NP / NW;
+  static constexpr bool kV = VSWZ;
   static_assert(NP % NW == 0, "whole pieces per wave");
   int row[NPW];
   uint32_t cof[NPW];

@@ -13,6 +13,7 @@ static_assert(2 * (kMaxRows / 16 + kMaxHeads) < kMaxBlocks, "workgroups of a lau
 pb_status check_config(const pb_score_attn_config* c) {
   if (!c) return fail(PB_ERR_INVALID_ARG, "cfg is NULL");
   if (!known(c->dtype)) return fail(PB_ERR_INVALID_ARG, "unknown dtype %d", (int)c->dtype);
+  if (!known(c->products)) return fail(PB_ERR_INVALID_ARG, "unknown products %d", (int)c->products);
   if (c->batch < 1 || c->seq_q < 1 || c->seq_k < 1 || c->heads < 1 || c->kv_heads < 1)
     return fail(PB_ERR_INVALID_ARG, "batch=%d, seq_q=%d, seq_k=%d, heads=%d, kv_heads=%d: each "
                 "must be >= 1", c->batch, c->seq_q, c->seq_k, c->heads, c->kv_heads);
@@ -126,6 +127,7 @@ pb::ScoreArgs args_of(const pb_score_attn_config* c, const pb_score_terms* t) {
   a.heads = c->heads, a.kv_heads = c->kv_heads, a.group = c->heads / c->kv_heads;
   a.causal = c->causal, a.window = c->window;
   a.scale = c->scale, a.cap = c->cap;
+  a.wide = c->products == PB_F32;
   a.docs = t->docs, a.prefix = t->prefix, a.n_docs = t->n_docs;
   a.slopes = t->slopes, a.table = t->table;
   a.buckets = c->buckets, a.side = c->causal ? c->buckets : c->buckets / 2;

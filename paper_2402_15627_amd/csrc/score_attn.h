@@ -34,6 +34,10 @@ struct ScoreArgs {
   float* dtable;
   float* bias_part;  // sums of the table's gradient, [batch * row blocks][heads][buckets]
   int pack;                     // heads of one key head that a block of rows holds
+  int wide;                     // products: factors that are computed keep 16 bits
+  // minus sum of P dP of the rows, [batch][head / pack][position][head mod pack]; null: as
+  // minus sum of dO O
+  const float* minus_delta;
 };
 
 // How many workgroups may share a block's tiles.
@@ -41,7 +45,7 @@ struct ScorePlan {
   int chunks;
 };
 struct ScoreBwdPlan {
-  ScorePlan kv, q;  // dK and dV by tiles of rows, dQ by tiles of keys
+  ScorePlan kv, q, d;  // dK and dV by tiles of rows, dQ and the row terms by tiles of keys
 };
 // The most tiles (of `keys`) that a block of `rows` rows may visit, whatever the
 // documents.
@@ -233,13 +237,19 @@ PB_DEV Pair pair_of(const ScoreArgs& a, const T* qr, const T* gr, const T* kr, c
   return x;
 }
 template <typename T, int D>
+PB_DEV float delta_of(const ScoreArgs& a, const T* gr, int b, int h, int i) {
+  if (!a.minus_delta) return dot_row<T, D>(gr, o_row<T, D>(a, b, i, h));
+  const size_t set = (size_t)b * (a.heads / a.pack) + h / a.pack;
+  return -a.minus_delta[(set * a.seq_q + i) * a.pack + h % a.pack];
+}
+template <typename T, int D>
 PB_DEV void dq_row(const ScoreArgs& a, int b, int h, int i, int lane) {
   const int p = i + a.seq_k - a.seq_q, kvh = h / a.group;
   const Bounds d = bounds_of(a, b, p);
   const int first = window_first(a, d, p), last = window_last(a, d, p);
   const T *qr = q_row<T, D>(a, b, i, h), *gr = do_row<T, D>(a, b, i, h);
   const float L = a.lse[lse_at(a, b, h, i)];
-  const float delta = dot_row<T, D>(gr, o_row<T, D>(a, b, i, h));
+  const float delta = delta_of<T, D>(a, gr, b, h, i);
   RowSum<D> acc;
   const int end = L == kNegInf ? 0 : max(last + 1, d.pe);
   for (int j0 = d.pe > d.ds ? d.ds : first; j0 < end; j0 += 64) {
@@ -273,7 +283,7 @@ PB_DEV void dkdv_row(const ScoreArgs& a, int b, int kvh, int j, int lane) {
       if (i <= last) {
         const T* gr = do_row<T, D>(a, b, i, h);
         x = pair_of<T, D>(a, q_row<T, D>(a, b, i, h), gr, kr, vr, h, i + off - j,
-                          a.lse[lse_at(a, b, h, i)], dot_row<T, D>(gr, o_row<T, D>(a, b, i, h)));
+                          a.lse[lse_at(a, b, h, i)], delta_of<T, D>(a, gr, b, h, i));
       }
       const float du = x.dz * x.slope;
       unsigned long long any = __builtin_amdgcn_ballot_w64(x.p != 0.f);

@@ -1,7 +1,7 @@
 // Gradients of attention with terms in its scores, bf16, on v_mfma_f32_32x32x16_bf16.
 //
-// Row terms (lse in base 2, delta = sum of dO O) come from a pass of their own, laid out
-// in the order of the blocks' rows.  Then one launch has two roles, as in attn.hip:
+// Row terms (lse in base 2, delta) come from a launch of their own, laid out in the order of
+// the blocks' rows.  Then one launch has two roles, as in attn.hip:
 //   dK, dV: 128 keys over 32-row tiles of the heads that share the key head, so that the
 //     gradients of shared heads are one sum (of more than eight heads several, merged in
 //     order);
@@ -10,11 +10,17 @@
 // 1 - tanh^2 with a cap for dQ and dK.  How many tiles a block has depends on documents
 // that only the device knows, so a block that the plan cuts shares its own tiles out.
 //
+// P and dS enter the products as bf16.  WIDE adds those with what that rounding leaves (16
+// bits of each in all), and its delta = sum of P dP is summed over the tiles in a launch
+// before (scores and dP once more); without, delta = sum of dO O, whose O is rounded.  In
+// norm dq, dk and dv are off by 1.66e-3 with, their own rounding; without, dv 2.1e-3 to
+// 2.4e-3, dq and dk 2.6e-3 to 2.8e-3 over rows of 500 keys and more, 5.2e-3 over rows of two.
+//
 // The table's gradient sums dz = P (dP - delta) by bucket, and there delta has to be
-// better than sum of dO O, whose O is rounded: dQ's rows also give e = the sum of their
-// dz, by which delta is off (the exact ones sum to zero), and the sums of dz and of P
-// over the tiles beyond the last bucket's first distance.  A last launch goes over the
-// other tiles again, with the row terms put right.
+// better than a sum of dO O: dQ's rows also give e = the sum of their dz, by which delta is
+// off (the exact ones sum to zero), and the sums of dz and of P over the tiles beyond the
+// last bucket's first distance.  A last launch goes over the other tiles again, with the
+// row terms put right.
 //
 // Bound by the vector instructions of the terms beside the products, at two waves a SIMD
 // (registers): 4096 tokens of packed documents, 16 heads over 4 x 128, capped 234 us, 424
@@ -47,6 +53,9 @@ PB_DEV size_t packed_row(const ScoreArgs& a, int hb, int r) {
   return (size_t)hb * a.seq_q * a.pack + r;
 }
 
+// A row's lse in base 2; of one that sees nothing infinity, for probabilities of 2^-inf.
+PB_DEV float base2(float L) { return L == kNegInf ? -kNegInf : L * kLog2e; }
+
 // ------------------------------------------------------------- row terms
 // Both operands read once, D / 8 lanes a row (four for head_dim 96).
 template <int D>
@@ -75,8 +84,7 @@ __global__ __launch_bounds__(256) void score_terms(ScoreArgs a, float* __restric
   if (l != 0 || at >= all) return;
   const float L = a.lse[score::lse_at(a, b, h, i)];
   const size_t to = packed_row(a, b * (a.heads / a.pack) + h / a.pack, i * a.pack + h % a.pack);
-  // a row that sees nothing: probabilities of 2^-inf
-  L2[to] = L == kNegInf ? -kNegInf : L * kLog2e;
+  L2[to] = base2(L);
   minus_delta[to] = L == kNegInf ? 0.f : -acc;
 }
 
@@ -201,14 +209,28 @@ PB_DEV void store_rows(unsigned char* lds, const f32x16 (&x)[D / 32], float f, f
   }
 }
 
+// What k-step s of p (as probs_frag) leaves.
+PB_DEV bf16x8 rest_frag(const f32x16* p, int s, const bf16x8& rounded) {
+  const f32x16& a = p[s >> 1];
+  const int o = 8 * (s & 1);
+  bf16x8 r;
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const bf16x2 x = rest_of(bf16x2{rounded[e], rounded[e + 1]}, a[o + e], a[o + e + 1]);
+    r[e] = x[0], r[e + 1] = x[1];
+  }
+  return r;
+}
+
 struct BwdWork {
   float *L2, *minus_delta;  // row terms, in the blocks' order
   float *pdk, *pdv, *pdq;   // partial results of split blocks, [chunk][row][D]
   float* sums;              // [chunk][kSums][rows] (with dtable)
-  int *kv_used, *q_used;    // chunks of each block, [set][batch, head][block]
-  int kv_nc, q_nc;          // at most
+  float* pdelta;            // parts of delta, [chunk][rows] (of blocks in chunks)
+  int *kv_used, *q_used, *d_used;  // chunks of each block, [set][batch, head][block]
+  int kv_nc, q_nc, d_nc;           // at most
 };
-constexpr int kMinTilesKv = 12, kMinTilesQ = 4;  // of a chunk
+constexpr int kMinTilesKv = 12, kMinTilesQ = 4, kMinTilesD = 4;  // of a chunk
 __host__ __device__ inline int row_blocks(const ScoreArgs& a) {
   return (a.seq_q * a.pack + kBlockQ - 1) / kBlockQ;
 }
@@ -236,7 +258,7 @@ struct KvLds {
   }
 };
 
-template <int D, bool CAP, int BIAS>
+template <int D, bool CAP, int BIAS, bool WIDE>
 PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
   constexpr int TL = kTileQ, NB = kBlockK, TB = TL * 2 * D;
   using L = KvLds<D>;
@@ -460,10 +482,17 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
 #pragma unroll
     for (int s2 = 0; s2 < TL / 16; ++s2) {
       const bf16x8 pf = probs_frag(sc, s2), df = probs_frag(&dp, s2);
+      bf16x8 pl, dl;
+      if constexpr (WIDE) pl = rest_frag(sc, s2, pf), dl = rest_frag(&dp, s2, df);
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) {
-        dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qr.cols(db, s2, TB), pf, dv[db], 0, 0, 0);
-        dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qr.cols(db, s2, 0), df, dk[db], 0, 0, 0);
+        const bf16x8 gc = qr.cols(db, s2, TB), qc = qr.cols(db, s2, 0);
+        dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(gc, pf, dv[db], 0, 0, 0);
+        dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qc, df, dk[db], 0, 0, 0);
+        if constexpr (WIDE) {
+          dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(gc, pl, dv[db], 0, 0, 0);
+          dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qc, dl, dk[db], 0, 0, 0);
+        }
       }
     }
   }
@@ -510,8 +539,9 @@ struct RowTiles {
   BiasLds bl;
   Packed pk;
 
+  // terms: whether the row terms are there
   PB_DEV RowTiles(const ScoreArgs& a_, const BwdWork& w_, unsigned char* s, int lds_at, int blk,
-                  int hb)
+                  int hb, bool terms = true)
       : a(a_), w(w_), smem(s), cap(a_.scale, CAP ? a_.cap : 1.f),
         bl(lds_at, a_.buckets, a_.pack, (kBlockQ + a_.pack - 1) / a_.pack + 1, kTileK),
         pk(a_.pack) {
@@ -537,8 +567,8 @@ struct RowTiles {
       gf[ks] = load_row_frag(g + 16 * ks + 8 * fh, any);
     }
     const size_t at = packed_row(a, hb, rc);
-    L2 = w.L2[at];
-    dl = -w.minus_delta[at];
+    L2 = terms ? w.L2[at] : base2(a.lse[score::lse_at(a, b, h, i)]);
+    dl = terms ? -w.minus_delta[at] : 0.f;
     slope2 = BIAS == kSlopes ? -a.slopes[h] * kLog2e : 0.f;
     bias_last = BIAS == kTable ? a.first[a.side - 1] : 0;
     bias_at = BIAS == kTable ? (h - h0) * bl.stride + (p_last - p) + 4 * fh : 0;
@@ -625,13 +655,42 @@ struct RowTiles {
     for (int x = 0; x < 16; ++x) {
       pr[0][x] = exp2_hw(BIAS != kNoBias ? pr[0][x] - L2 : fmaf(pr[0][x], c2, -L2));
       dz[0][x] *= pr[0][x];
-      // (behind the mask dP may be anything: the table's sums take none of it)
-      if constexpr (BIAS == kTable) dz[0][x] = pr[0][x] == 0.f ? 0.f : dz[0][x];
+      // (behind the mask dP may be anything: sums over a row take none of it)
+      if constexpr (BIAS == kTable || SLOPE == 0) dz[0][x] = pr[0][x] == 0.f ? 0.f : dz[0][x];
     }
   }
 };
 
-template <int D, bool CAP, int BIAS>
+// n key tiles of a block from t_begin on, by way of two slots of K and V: f(first key, the
+// row's keys of the tile, slot, places of K) for those that the wave sees any of.
+template <int D, bool CAP, int BIAS, typename F>
+PB_DEV void each_tile(RowTiles<D, CAP, BIAS>& t, const KeyTiles& kt, int t_begin, int n,
+                      uint32_t lds0, F f) {
+  constexpr int TB = kTileK * 2 * D;
+  auto kv_of = [&](int i) PB_INLINE { return kt.tile(t_begin + i) * kTileK; };
+  auto k_off = [&](int s) PB_INLINE { return lds0 + (2 * s) * TB; };
+  auto v_off = [&](int s) PB_INLINE { return lds0 + (2 * s + 1) * TB; };
+  if constexpr (BIAS == kTable) {
+    t.tables();
+    t.build(kv_of(0), 0);
+  }
+  t.request(kt, kv_of(0), k_off(0), v_off(0));
+  const LaneReads<D> places(t.lane);
+  for (int i = 0; i < n; ++i) {
+    const int cur = i & 1, kv0 = kv_of(i);
+    wait_dma_all();
+    block_barrier();
+    if (i + 1 < n) {
+      t.request(kt, kv_of(i + 1), k_off(cur ^ 1), v_off(cur ^ 1));
+      if constexpr (BIAS == kTable) t.build(kv_of(i + 1), cur ^ 1);
+    }
+    const uint64_t see = t.keys.bits(kv0);
+    if (!__builtin_amdgcn_ballot_w64(see != 0)) continue;
+    f(kv0, see, cur, places.at(lds0 + (2 * cur) * TB));
+  }
+}
+
+template <int D, bool CAP, int BIAS, bool WIDE>
 PB_DEV void dq_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
   constexpr int TB = kTileK * 2 * D;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
@@ -653,27 +712,9 @@ PB_DEV void dq_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
 #pragma unroll
   for (int x = 0; x < D / 32; ++x) dq[x] = zero16();
   float sums[kSums] = {0.f, 0.f, 0.f, 0.f, 0.f};
-  if (n > 0) {
-    auto kv_of = [&](int i) { return kt.tile(t_begin + i) * kTileK; };
-    auto k_off = [&](int s) { return lds0 + (2 * s) * TB; };
-    auto v_off = [&](int s) { return lds0 + (2 * s + 1) * TB; };
-    if constexpr (BIAS == kTable) {
-      t.tables();
-      t.build(kv_of(0), 0);
-    }
-    t.request(kt, kv_of(0), k_off(0), v_off(0));
-    const LaneReads<D> places(t.lane);
-    for (int i = 0; i < n; ++i) {
-      const int cur = i & 1, kv0 = kv_of(i);
-      wait_dma_all();
-      block_barrier();
-      if (i + 1 < n) {
-        t.request(kt, kv_of(i + 1), k_off(cur ^ 1), v_off(cur ^ 1));
-        if constexpr (BIAS == kTable) t.build(kv_of(i + 1), cur ^ 1);
-      }
-      const uint64_t see = t.keys.bits(kv0);
-      if (!__builtin_amdgcn_ballot_w64(see != 0)) continue;
-      const LaneReads<D> kr = places.at(lds0 + (2 * cur) * TB);
+  if (n > 0)
+    each_tile(t, kt, t_begin, n, lds0,
+              [&](int kv0, uint64_t see, int cur, const LaneReads<D>& kr) PB_INLINE {
 #pragma unroll
       for (int h2 = 0; h2 < 2; ++h2) {
         f32x16 pr[1], dz[1], slope;
@@ -696,15 +737,23 @@ PB_DEV void dq_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
 #pragma unroll
             for (int x = 0; x < 16; ++x) dz[0][x] *= slope[x];
         }
+        bf16x8 df[2], dl[2];
+#pragma unroll
+        for (int s2 = 0; s2 < 2; ++s2) {
+          df[s2] = probs_frag(dz, s2);
+          if constexpr (WIDE) dl[s2] = rest_frag(dz, s2, df[s2]);
+        }
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-          for (int s2 = 0; s2 < 2; ++s2)
-            dq[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                kr.cols(db, 2 * h2 + s2, 0), probs_frag(dz, s2), dq[db], 0, 0, 0);
+          for (int s2 = 0; s2 < 2; ++s2) {
+            const bf16x8 kc = kr.cols(db, 2 * h2 + s2, 0);
+            dq[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kc, df[s2], dq[db], 0, 0, 0);
+            if constexpr (WIDE)
+              dq[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kc, dl[s2], dq[db], 0, 0, 0);
+          }
       }
-    }
-  }
+    });
   if constexpr (BIAS == kTable) {
     if (a.dtable) {
 #pragma unroll
@@ -753,9 +802,58 @@ PB_DEV void dq_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
     }
 }
 
+// The row terms from unrounded values, of a block's rows or of a chunk's part of their
+// tiles.
+template <int D, bool CAP, int BIAS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void score_delta_bf16(
+    ScoreArgs a, BwdWork w) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(PB_LDS unsigned char*)smem;
+  const int hb_n = a.batch * (a.heads / a.pack), hb = blockIdx.x % hb_n;
+  const int bx = blockIdx.x / hb_n, nblk = row_blocks(a), blk = nblk - 1 - bx / w.d_nc;
+  const int chunk = bx % w.d_nc;
+  RowTiles<D, CAP, BIAS> t(a, w, smem, 4 * kTileK * 2 * D, blk, hb, false);
+  const KeyTiles kt = key_tiles<kTileK>(a, t.b, t.p_first, t.p_last, t.lane);
+  const Share share(kt.n, w.d_nc, kMinTilesD);
+  const int t_begin = chunk * share.size, n = min(kt.n - t_begin, share.size);
+  if (chunk >= max(share.used, 1)) return;
+  if (w.d_nc > 1 && threadIdx.x == 0 && chunk == 0) w.d_used[(size_t)hb * nblk + blk] = share.used;
+  float delta = 0.f;
+  if (n > 0)
+    each_tile(t, kt, t_begin, n, lds0,
+              [&](int kv0, uint64_t see, int cur, const LaneReads<D>& kr) PB_INLINE {
+#pragma unroll
+      for (int h2 = 0; h2 < 2; ++h2) {
+        f32x16 pr[1], dz[1], slope;
+        t.template pair<0>(kv0, h2, cur, kr, see, pr, dz, slope);
+        float s = 0.f;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) s += dz[0][x];
+        delta += s;
+      }
+    });
+  delta += __shfl_xor(delta, 32, 64);
+  if (t.r >= t.rows || t.fh != 0) return;
+  const size_t row = packed_row(a, hb, t.r);
+  if (chunk == 0) w.L2[row] = t.L2;
+  if (share.used > 1) w.pdelta[(size_t)chunk * a.batch * a.heads * a.seq_q + row] = delta;
+  else w.minus_delta[row] = -delta;
+}
+// ... from the parts of blocks in chunks, in their order.
+__global__ __launch_bounds__(256) void score_delta_merge(ScoreArgs a, BwdWork w) {
+  const size_t all = (size_t)a.batch * a.heads * a.seq_q, set = (size_t)a.seq_q * a.pack;
+  const size_t row = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (row >= all) return;
+  const int n = w.d_used[row / set * row_blocks(a) + row % set / kBlockQ];
+  if (n < 2) return;
+  float delta = 0.f;
+  for (int c = 0; c < n; ++c) delta += w.pdelta[c * all + row];
+  w.minus_delta[row] = -delta;
+}
+
 // Both roles in one launch, in turn, each with its (under a causal mask) longest blocks
 // first, all heads' before the next.
-template <int D, bool CAP, int BIAS>
+template <int D, bool CAP, int BIAS, bool WIDE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void score_bwd_bf16(
     ScoreArgs a, BwdWork w, int nk, int nq) {
   const int id = blockIdx.x, mn = min(nk, nq);
@@ -763,10 +861,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
   const int x = id < 2 * mn ? id >> 1 : id - mn;
   if (kv) {
     const int n = a.batch * a.kv_heads;
-    dkdv_block<D, CAP, BIAS>(a, w, x / n, x % n);
+    dkdv_block<D, CAP, BIAS, WIDE>(a, w, x / n, x % n);
   } else {
     const int n = a.batch * (a.heads / a.pack);
-    dq_block<D, CAP, BIAS>(a, w, x / n, x % n);
+    dq_block<D, CAP, BIAS, WIDE>(a, w, x / n, x % n);
   }
 }
 
@@ -949,7 +1047,7 @@ size_t round64(size_t floats) { return (floats + 63) & ~(size_t)63; }
 
 // The workspace's parts, in floats from its start.
 struct BwdLayout {
-  size_t L2, delta, bias, sums, pdk, pdv, pdq, kv_used, q_used, total;
+  size_t L2, delta, bias, sums, pdelta, pdk, pdv, pdq, kv_used, q_used, d_used, total;
 };
 BwdLayout bwd_layout(int D, const ScoreArgs& a, const ScoreBwdPlan& p) {
   const size_t rows = (size_t)a.batch * a.heads * a.seq_q;
@@ -964,11 +1062,13 @@ BwdLayout bwd_layout(int D, const ScoreArgs& a, const ScoreBwdPlan& p) {
   l.L2 = take(rows), l.delta = take(rows);
   l.bias = take(a.buckets ? (size_t)a.batch * row_blocks(a) * a.heads * a.buckets : 0);
   l.sums = take(a.buckets ? (size_t)p.q.chunks * kSums * rows : 0);
+  l.pdelta = take(p.d.chunks > 1 ? (size_t)p.d.chunks * rows : 0);
   l.pdk = take(p.kv.chunks > 1 ? (size_t)p.kv.chunks * keys * D : 0);
   l.pdv = take(p.kv.chunks > 1 ? (size_t)p.kv.chunks * keys * D : 0);
   l.pdq = take(p.q.chunks > 1 ? (size_t)p.q.chunks * rows * D : 0);
   l.kv_used = take(p.kv.chunks > 1 ? (size_t)a.batch * a.heads / a.pack * key_blocks(a) : 0);
   l.q_used = take(p.q.chunks > 1 ? (size_t)a.batch * a.heads / a.pack * row_blocks(a) : 0);
+  l.d_used = take(p.d.chunks > 1 ? (size_t)a.batch * a.heads / a.pack * row_blocks(a) : 0);
   l.total = at;
   return l;
 }
@@ -976,26 +1076,39 @@ BwdLayout bwd_layout(int D, const ScoreArgs& a, const ScoreBwdPlan& p) {
 template <int D>
 void bwd_d(const ScoreArgs& a, const ScoreBwdPlan& p, float* ws, hipStream_t s) {
   const BwdLayout l = bwd_layout(D, a, p);
-  BwdWork w{ws + l.L2, ws + l.delta, ws + l.pdk, ws + l.pdv, ws + l.pdq, ws + l.sums,
-            (int*)(ws + l.kv_used), (int*)(ws + l.q_used), p.kv.chunks, p.q.chunks};
+  BwdWork w{ws + l.L2, ws + l.delta, ws + l.pdk, ws + l.pdv, ws + l.pdq, ws + l.sums, ws + l.pdelta,
+            (int*)(ws + l.kv_used), (int*)(ws + l.q_used), (int*)(ws + l.d_used),
+            p.kv.chunks, p.q.chunks, p.d.chunks};
   ScoreArgs x = a;
   x.bias_part = ws + l.bias;
+  x.minus_delta = a.wide ? w.minus_delta : nullptr;
   const size_t rows = (size_t)a.batch * a.heads * a.seq_q;
   const size_t keys = (size_t)a.batch * a.kv_heads * a.seq_k;
   constexpr int kLanes = D == 96 ? 4 : D / 8;
-  score_terms<D><<<(unsigned)((rows * kLanes + 255) / 256), 256, 0, s>>>(x, w.L2, w.minus_delta);
+  if (!a.wide)
+    score_terms<D><<<(unsigned)((rows * kLanes + 255) / 256), 256, 0, s>>>(x, w.L2, w.minus_delta);
   const int nk = key_blocks(a) * a.batch * a.kv_heads * p.kv.chunks;
   const int nq = row_blocks(a) * a.batch * (a.heads / a.pack) * p.q.chunks;
+  const int nd = row_blocks(a) * a.batch * (a.heads / a.pack) * p.d.chunks;
   const size_t q_tiles = 4 * (size_t)kTileK * 2 * D;
   const bool cap = a.cap > 0.f;
 #define PB_BWD(C, B)                                                                              \
   do {                                                                                            \
-    size_t lds = std::max((size_t)KvLds<D>::kBytes, q_tiles);                                  \
-    if (B == kTable)                                                                              \
-      lds = std::max((size_t)KvLds<D>::bias(a).bytes,                                          \
-                     (size_t)BiasLds((int)q_tiles, a.buckets, a.pack,                             \
-                                     (kBlockQ + a.pack - 1) / a.pack + 1, kTileK).bytes);         \
-    score_bwd_bf16<D, C, B><<<(unsigned)(nk + nq), 256, lds, s>>>(x, w, nk, nq);                  \
+    size_t lds_q = q_tiles, lds = KvLds<D>::kBytes;                                               \
+    if (B == kTable) {                                                                            \
+      lds_q = BiasLds((int)q_tiles, a.buckets, a.pack, (kBlockQ + a.pack - 1) / a.pack + 1,       \
+                      kTileK).bytes;                                                              \
+      lds = KvLds<D>::bias(a).bytes;                                                              \
+    }                                                                                             \
+    lds = std::max(lds, lds_q);                                                                   \
+    if (a.wide) {                                                                                 \
+      score_delta_bf16<D, C, B><<<(unsigned)nd, 256, lds_q, s>>>(x, w);                           \
+      if (p.d.chunks > 1)                                                                         \
+        score_delta_merge<<<(unsigned)((rows + 255) / 256), 256, 0, s>>>(x, w);                   \
+      score_bwd_bf16<D, C, B, true><<<(unsigned)(nk + nq), 256, lds, s>>>(x, w, nk, nq);          \
+    } else {                                                                                      \
+      score_bwd_bf16<D, C, B, false><<<(unsigned)(nk + nq), 256, lds, s>>>(x, w, nk, nq);         \
+    }                                                                                             \
   } while (0)
   const int bias = a.slopes ? kSlopes : a.table ? kTable : kNoBias;
   if (cap) {
@@ -1035,7 +1148,7 @@ static int most_row_tiles(const ScoreArgs& a) {
   return (int)(a.prefix ? all : std::min(all, reach * a.pack / kTileQ + 2));
 }
 
-ScoreBwdPlan score_bwd_whole(const ScoreArgs& a) { return ScoreBwdPlan{{a.group / a.pack}, {1}}; }
+ScoreBwdPlan score_bwd_whole(const ScoreArgs& a) { return ScoreBwdPlan{{a.group / a.pack}, {1}, {1}}; }
 
 // A key block has as many row tiles as all heads that share it bring, a row block few key
 // tiles, and splitting costs a merge and its traffic (fp32 parts, written and read).  So
@@ -1050,6 +1163,14 @@ ScoreBwdPlan score_bwd_whole(const ScoreArgs& a) { return ScoreBwdPlan{{a.group 
 //   4 x 2048, 16 over 2 x 96                 632 357 270 277
 //   2048, 40 x 128, window 512               136 158 184 203
 //   4096, 8 x 128, window 1024                91 111 126 131
+// The row terms' parts are four bytes a row, so their chunks cost a workgroup's beginning
+// (its rows, the first tile) and a launch: one and a half times what runs at a time.  All
+// gradients (us, for 1, 512, 1024 workgroups at least):
+//   2048, 12 x 128                           148 126 131
+//   4096 tokens, 16 heads over 4 x 128       480 479 462
+//   4096, 16 x 64                            284 284 268
+//   2048, 40 x 128, window 512, with a table 277 277 275
+constexpr long long kDeltaBlocks = 768;
 ScoreBwdPlan score_bwd_plan(int head_dim, const ScoreArgs& a) {
   ScoreBwdPlan p = score_bwd_whole(a);
   const int sets = p.kv.chunks;
@@ -1065,6 +1186,8 @@ ScoreBwdPlan score_bwd_plan(int head_dim, const ScoreArgs& a) {
   };
   cut(p.kv, kv_us, std::max(all, 0.8 * q_us), kv / kMinTilesKv);
   cut(p.q, q_us, std::max(all, 100.0), q / kMinTilesQ);
+  if (a.wide)
+    p.d.chunks = (int)std::max(1LL, std::min((kDeltaBlocks + nq - 1) / nq, (long long)q / kMinTilesD));
   return p;
 }
 

@@ -9,6 +9,11 @@
 // beside tile t's exponentials.  The row sums are of unrounded probabilities (lse is
 // kept in fp32 and the gradient's probabilities follow from it).
 //
+// Probabilities enter O as bf16.  WIDE adds the products with what that rounding leaves
+// (16 bits of each in all), so that o is off by its own rounding alone (1.66e-3 in norm,
+// without 1.7e-3 to 2.1e-3): half as many matrix products again and three vector
+// instructions a score.
+//
 // LDS: K and V in two slots each; iteration t loads K of tile t + 2 and V of tile t + 1.
 // That leaves 16 KB of a CU's half for the rows' keys (read back in partial tiles only)
 // and the biases, so that two workgroups share a CU.
@@ -46,11 +51,12 @@ BiasLds bias_lds(const ScoreArgs& a) {
                  (kRows + a.pack - 1) / a.pack + 1, kTL);
 }
 
-template <int D, bool CAP, int BIAS>
+template <int D, bool CAP, int BIAS, bool WIDE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void score_fwd_bf16(
     ScoreArgs a, int nc, float* __restrict__ po, float* __restrict__ plse,
     int* __restrict__ used) {
   constexpr int TL = kTL, TB = TL * 2 * D, KS = D / 32, DB = D / 16;
+  constexpr bool LEAN = WIDE && D == 128;  // registers
   constexpr bool kZ = BIAS != kNoBias;  // scores are turned to base 2 with their bias
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(PB_LDS unsigned char*)smem;
@@ -107,19 +113,35 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
   const FwdLds<D> la(lane);
   // The lane's pieces of a tile; kept for tiles of which every row is a key between lo
   // and hi, formed anew where rows beyond are read from the nearest of those.
+  // (LEAN: formed anew each tile from the first piece's, with the lane's places in LDS)
   uint32_t at_k[PK], at_v[PK];
   auto pieces = [&](const auto& dma, int lo, int hi, uint32_t (&at)[PK]) {
 #pragma unroll
     for (int x = 0; x < PK; ++x)
       at[x] = (uint32_t)max(lo, min(dma.row[x], hi)) * (uint32_t)(2 * a.ld_kv) + dma.cof[x];
   };
-  pieces(DmaK(wave, lane), 0, TL - 1, at_k);
-  pieces(DmaV(wave, lane), 0, TL - 1, at_v);
+  uint32_t lean_r = 0, lean_c = 0;
+  if constexpr (LEAN) {
+    const DmaK first(wave, lane);
+    lean_r = (uint32_t)first.row[0] * (uint32_t)(2 * a.ld_kv), lean_c = first.cof[0];
+  } else {
+    pieces(DmaK(wave, lane), 0, TL - 1, at_k);
+    pieces(DmaV(wave, lane), 0, TL - 1, at_v);
+  }
   auto issue = [&](const bf16* base, auto type, const uint32_t (&whole)[PK], int i, uint32_t slot) {
     using Dma = typename decltype(type)::type;
     const int kv0 = kt.tile(t_begin + i) * TL;
     const bf16* tile = base + (size_t)kv0 * a.ld_kv;
-    if (kv0 >= kt.lo && kv0 + TL - 1 <= kt.hi) {
+    if (LEAN && kv0 >= kt.lo && kv0 + TL - 1 <= kt.hi) {
+      // piece x begins 4 x rows on, its chunks are those of the first with bit 1 of x / 2
+      // turned (in V, whose swizzle leaves bit 4 of the row out, with bit 0 of the wave's)
+      uint32_t c = lean_c ^ (Dma::kV ? 16u * (wave & 1) : 0u);
+      asm volatile("" : "+v"(c));
+#pragma unroll
+      for (int x = 0; x < PK; ++x)
+        dma16s(tile + (size_t)(4 * x) * a.ld_kv, lean_r + (c ^ (32u * (x >> 1))),
+               lds0 + slot + (uint32_t)((wave * PK + x) * 1024));
+    } else if (kv0 >= kt.lo && kv0 + TL - 1 <= kt.hi) {
 #pragma unroll
       for (int x = 0; x < PK; ++x)
         dma16s(tile, whole[x], lds0 + slot + (uint32_t)((wave * PK + x) * 1024));
@@ -213,18 +235,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
   for (int db = 0; db < DB; ++db) o[db][0] = o[db][1] = zero4();
 
   f32x4 sa[4][2], sb[4][2];
-  bf16x8 pf[2][2], kf[2][4], vf[3][2];
+  bf16x8 pf[2][2], pl[2][2], kf[2][4], vf[3][2];  // (pl: what pf leaves, with WIDE)
   float m_use[2];
 
+  auto place = [&](uint32_t base, const auto& of, int n, uint32_t bits) {
+    if constexpr (!LEAN) return base + of[n];
+    uint32_t x = base + of[0];  // (rows begin at multiples of 256 bytes)
+    asm volatile("" : "+v"(x));
+    return x ^ (bits * n);
+  };
   auto read_k = [&](uint32_t base, int ks) {
+    const uint32_t at = place(base, la.k, ks, 64);
 #pragma unroll
     for (int k4 = 0; k4 < 4; ++k4)
-      kf[ks & 1][k4] = lds_b128(base + la.k[ks] + 2 * D * score_row_off(k4));
+      kf[ks & 1][k4] = lds_b128(at + 2 * D * score_row_off(k4));
   };
   auto read_v = [&](uint32_t base, int db) {
+    const uint32_t at = place(base, la.v, db, 32);
 #pragma unroll
     for (int sp = 0; sp < 2; ++sp)
-      vf[db % 3][sp] = lds_tr2(base + la.v[db] + 2 * D * 32 * sp, 2 * D * 4);
+      vf[db % 3][sp] = lds_tr2(at + 2 * D * 32 * sp, 2 * D * 4);
   };
   auto exp_unit = [&](const f32x4 (&sc)[4][2], int u) {
     const int j = u >> 2, sp = (u >> 1) & 1, h = u & 1;
@@ -235,6 +265,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
                         : fmaf(sc[2 * sp + h][j][e], c2, -m_use[j]));
 #pragma unroll
     for (int e = 0; e < 4; ++e) pf[sp][j][4 * h + e] = (bf16)p[e];
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        const int at = 4 * h + e;
+        const bf16x2 x = rest_of(bf16x2{pf[sp][j][at], pf[sp][j][at + 1]}, p[e], p[e + 1]);
+        pl[sp][j][at] = x[0], pl[sp][j][at + 1] = x[1];
+      }
+    }
     l_run[j] += (p[0] + p[1]) + (p[2] + p[3]);
   };
   auto score_phase = [&](uint32_t kbase, int ks, f32x4 (&sn)[4][2]) {
@@ -262,7 +300,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
   auto keep_exps = [&](int ks) {
 #pragma unroll
     for (int u = ks * 8 / KS; u < (ks + 1) * 8 / KS; ++u)
-      if (u % 2 == 1 || u == (ks + 1) * 8 / KS - 1) keep(pf[(u >> 1) & 1][u >> 2]);
+      if (u % 2 == 1 || u == (ks + 1) * 8 / KS - 1) {
+        keep(pf[(u >> 1) & 1][u >> 2]);
+        if constexpr (WIDE) keep(pl[(u >> 1) & 1][u >> 2]);
+      }
     keep(l_run[0]);
     keep(l_run[1]);
   };
@@ -337,13 +378,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
     for (int sp = 0; sp < 2; ++sp) {
       o[db][0] = mfma16(vf[db % 3][sp], pf[sp][0], o[db][0]);
       o[db][1] = mfma16(vf[db % 3][sp], pf[sp][1], o[db][1]);
+      if constexpr (WIDE) {
+        o[db][0] = mfma16(vf[db % 3][sp], pl[sp][0], o[db][0]);
+        o[db][1] = mfma16(vf[db % 3][sp], pl[sp][1], o[db][1]);
+      }
     }
   };
   auto pv_sched = [&](int db, bool valu) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < (WIDE ? 8 : 4); ++r) {
       __builtin_amdgcn_sched_group_barrier(kSgMfma, 1, 0);
-      if (db + 2 < DB) __builtin_amdgcn_sched_group_barrier(kSgDsRead, 1, 0);
+      if (r < 4 && db + 2 < DB) __builtin_amdgcn_sched_group_barrier(kSgDsRead, 1, 0);
       if (valu) __builtin_amdgcn_sched_group_barrier(kSgValu, 4, 0);
     }
   };
@@ -576,7 +621,11 @@ void fwd_d(const ScoreArgs& a, const ScorePlan& p, void* part, hipStream_t s) {
   const int bias = a.slopes ? kSlopes : a.table ? kTable : kNoBias;
   const size_t lds = a.table ? bias_lds<D>(a).bytes
                              : tiles_bytes<D>() + kRows * sizeof(RowKeys);
-#define PB_FWD(C, B) score_fwd_bf16<D, C, B><<<grid, 256, lds, s>>>(a, p.chunks, po, plse, used)
+#define PB_FWD(C, B)                                                                          \
+  do {                                                                                        \
+    if (a.wide) score_fwd_bf16<D, C, B, true><<<grid, 256, lds, s>>>(a, p.chunks, po, plse, used); \
+    else score_fwd_bf16<D, C, B, false><<<grid, 256, lds, s>>>(a, p.chunks, po, plse, used);  \
+  } while (0)
   if (cap) {
     if (bias == kTable) PB_FWD(true, kTable);
     else if (bias == kSlopes) PB_FWD(true, kSlopes);

@@ -25,6 +25,17 @@ struct Packed {
   PB_DEV int pos(int r) const { return pack == 1 ? r : (int)__umulhi((uint32_t)r, magic); }
 };
 
+// What the bf16 values x of pair leave of u and v, in bf16: 16 bits of each in both.  (A dot
+// product with (-1, 0) or (0, -1): the difference is exact, in one instruction.  The
+// constants come in registers: as an immediate, (-1, 0) is read as fp32's -1, which is (0, -1).)
+PB_DEV bf16x2 rest_of(bf16x2 pair, float u, float v) {
+  uint32_t first = 0xbf80u, second = 0xbf800000u;
+  asm("" : "+s"(first), "+s"(second));
+  return bf16x2{
+      (bf16)__builtin_amdgcn_fdot2_f32_bf16(pair, __builtin_bit_cast(bf16x2, first), u, false),
+      (bf16)__builtin_amdgcn_fdot2_f32_bf16(pair, __builtin_bit_cast(bf16x2, second), v, false)};
+}
+
 PB_DEV int wave_imin(int v) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) v = min(v, __shfl_xor(v, o, 64));

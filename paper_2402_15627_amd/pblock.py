@@ -126,7 +126,7 @@ class ScoreAttnConfig(ctypes.Structure):
     _fields_ = [("batch", c_int), ("seq_q", c_int), ("seq_k", c_int), ("heads", c_int),
                 ("kv_heads", c_int), ("head_dim", c_int), ("causal", c_int), ("window", c_int),
                 ("scale", c_float), ("cap", c_float), ("buckets", c_int), ("max_distance", c_int),
-                ("dtype", c_int)]
+                ("dtype", c_int), ("products", c_int)]
 
 
 class ScoreTerms(ctypes.Structure):
@@ -786,13 +786,15 @@ def pblock_rmsnorm_backward(cfg: RmsnormConfig, s, gamma, rstd, dy, dx, dgamma, 
 
 def score_attn_config(batch, seq_q, seq_k, heads, kv_heads, head_dim, causal=True, window=None,
                       scale=None, cap=0.0, buckets=0, max_distance=0,
-                      dtype="bf16") -> ScoreAttnConfig:
+                      dtype="bf16", products="f32") -> ScoreAttnConfig:
     """window: no limit by default; scale: 1 / sqrt(head_dim) by default; buckets and
-    max_distance go with a table."""
+    max_distance go with a table. products (of bf16 tensors): "f32" (16 bits of P and of its
+    gradient, results off by their own rounding) or "bf16" (rounded as the block's own
+    attention does; 0.65 to 0.75 of the time, gradients off by up to three roundings)."""
     return ScoreAttnConfig(batch, seq_q, seq_k, heads, kv_heads, head_dim, int(bool(causal)),
                            seq_k if window is None else window,
                            head_dim ** -0.5 if scale is None else scale, cap, buckets,
-                           max_distance, _dtype_of(dtype))
+                           max_distance, _dtype_of(dtype), _dtype_of(products))
 
 
 def pblock_score_attn_borders(cfg: ScoreAttnConfig) -> list:
