@@ -982,15 +982,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
 }
 
 // ----------------------------------------------------------------- merges
-// Sums of a split block's parts, in chunk order; a thread has 8 features of a row.  A row
-// with a non-finite part is computed again by the definition.
+// Sums of a split block's parts, in chunk order.  A row with a non-finite part is computed
+// again by the definition.
 template <int D, bool KEYS>
 __global__ __launch_bounds__(256) void score_bwd_merge(ScoreArgs a, BwdWork w) {
   const int H = KEYS ? a.kv_heads : a.heads, S = KEYS ? a.seq_k : a.seq_q;
   const size_t all = (size_t)a.batch * H * S;
-  const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
-  const int g = (int)(at % (D / 8)), lane = threadIdx.x & 63;
-  const size_t row = min(at / (D / 8), all - 1);
+  using ML = MergeLanes<D>;
+  const size_t at = ((size_t)blockIdx.x * 256 + threadIdx.x) / ML::kLanes;
+  const int g = threadIdx.x % ML::kLanes, lane = threadIdx.x & 63;
+  const size_t row = min(at, all - 1);
   int b, h, i;
   const int* used;  // of set 0
   if (KEYS) {
@@ -1003,34 +1004,44 @@ __global__ __launch_bounds__(256) void score_bwd_merge(ScoreArgs a, BwdWork w) {
   }
   const int sets = KEYS ? a.group / a.pack : 1, subs = (KEYS ? w.kv_nc : w.q_nc) / sets;
   const bool whole = sets == 1 && *used <= 1;  // written by its workgroup
-  float acc[2][8] = {}, bad = 0.f;
+  float acc[2][ML::kChunks][8] = {}, bad = 0.f;
   if (!whole) {
 #pragma unroll
     for (int k = 0; k < (KEYS ? 2 : 1); ++k) {
-      const float* from = pick(KEYS, pick(k != 0, w.pdv, w.pdk), w.pdq) + row * D + 8 * g;
+      const float* from = pick(KEYS, pick(k != 0, w.pdv, w.pdk), w.pdq) + row * D;
       for (int s = 0; s < sets; ++s)
         for (int c0 = 0, n = used[(size_t)s * a.batch * H * key_blocks(a)]; c0 < n; c0 += 4) {
-          float v[4][8];  // (four loads in flight)
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            load8(from + (size_t)(s * subs + min(c0 + c, n - 1)) * all * D, v[c]);
+          float v[4][ML::kChunks][8];  // (four loads in flight)
 #pragma unroll
           for (int c = 0; c < 4; ++c)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[k][e] += c0 + c < n ? v[c][e] : 0.f;
+            for (int x = 0; x < ML::kChunks; ++x)
+              load8(from + (size_t)(s * subs + min(c0 + c, n - 1)) * all * D + ML::at(g, x), v[c][x]);
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int x = 0; x < ML::kChunks; ++x)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) acc[k][x][e] += c0 + c < n ? v[c][x][e] : 0.f;
         }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) bad = fmaf(acc[k][e], 0.f, bad);
+      for (int x = 0; x < ML::kChunks; ++x)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) bad = fmaf(acc[k][x][e], 0.f, bad);
     }
   }
-  unsigned long long rows = __builtin_amdgcn_ballot_w64(bad != 0.f);
-  if (at / (D / 8) < all && bad == 0.f && !whole) {
-    if (KEYS) {
-      const size_t to = ((size_t)b * S + i) * a.ld_dkv + h * D + 8 * g;
-      store8((bf16*)a.dk + to, acc[0]);
-      store8((bf16*)a.dv + to, acc[1]);
-    } else {
-      store8((bf16*)a.dq + ((size_t)b * S + i) * a.ld_dq + h * D + 8 * g, acc[0]);
+  const bool again = ML::any(at < all && bad != 0.f);
+  unsigned long long rows = __builtin_amdgcn_ballot_w64(again);
+  if (at < all && !again && !whole) {
+#pragma unroll
+    for (int x = 0; x < ML::kChunks; ++x) {
+      if (KEYS) {
+        const size_t to = ((size_t)b * S + i) * a.ld_dkv + h * D + ML::at(g, x);
+        store8((bf16*)a.dk + to, acc[0][x]);
+        store8((bf16*)a.dv + to, acc[1][x]);
+      } else {
+        store8((bf16*)a.dq + ((size_t)b * S + i) * a.ld_dq + h * D + ML::at(g, x), acc[0][x]);
+      }
     }
   }
   while (rows) {
@@ -1122,9 +1133,9 @@ void bwd_d(const ScoreArgs& a, const ScoreBwdPlan& p, float* ws, hipStream_t s) 
   }
 #undef PB_BWD
   if (p.kv.chunks > 1)
-    score_bwd_merge<D, true><<<(unsigned)((keys * (D / 8) + 255) / 256), 256, 0, s>>>(x, w);
+    score_bwd_merge<D, true><<<(unsigned)((keys * MergeLanes<D>::kLanes + 255) / 256), 256, 0, s>>>(x, w);
   if (p.q.chunks > 1)
-    score_bwd_merge<D, false><<<(unsigned)((rows * (D / 8) + 255) / 256), 256, 0, s>>>(x, w);
+    score_bwd_merge<D, false><<<(unsigned)((rows * MergeLanes<D>::kLanes + 255) / 256), 256, 0, s>>>(x, w);
   if (!a.dtable) return;
   const int nblk = row_blocks(a);
   const unsigned grid = (unsigned)(nblk * a.batch * (a.heads / a.pack));

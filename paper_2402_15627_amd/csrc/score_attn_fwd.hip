@@ -553,30 +553,32 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
 }
 
 // Merge of a split forward, in chunk order: the chunks' outputs weighted by 2^(lse_c -
-// lse).  A thread has 8 features of a row.
+// lse).
 template <int D>
 __global__ __launch_bounds__(256) void score_fwd_merge(ScoreArgs a, const float* __restrict__ po,
                                                        const float* __restrict__ plse,
                                                        const int* __restrict__ used) {
   const size_t all = (size_t)a.batch * a.heads * a.seq_q;
-  const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
-  const int g = (int)(at % (D / 8)), lane = threadIdx.x & 63;
-  const size_t row = min(at / (D / 8), all - 1);
+  using ML = MergeLanes<D>;
+  const size_t at = ((size_t)blockIdx.x * 256 + threadIdx.x) / ML::kLanes;
+  const int g = threadIdx.x % ML::kLanes, lane = threadIdx.x & 63;
+  const size_t row = min(at, all - 1);
   const int i = (int)(row % a.seq_q), bh = (int)(row / a.seq_q);
   const int sets = a.heads / a.pack, b = bh / a.heads, h = bh % a.heads;
   const int blocks = (a.seq_q * a.pack + kRows - 1) / kRows;
   const int nc = used[((size_t)b * sets + h / a.pack) * blocks + (i * a.pack + h % a.pack) / kRows];
-  const bool mine = at / (D / 8) < all && nc > 1;  // (else its workgroup wrote it)
-  float m = kNegInf, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, bad = 0.f;
+  const bool mine = at < all && nc > 1;  // (else its workgroup wrote it)
+  float m = kNegInf, l = 0.f, acc[ML::kChunks][8] = {}, bad = 0.f;
   if (mine) {
 #pragma unroll 4
     for (int c = 0; c < nc; ++c) m = fmaxf(m, plse[c * all + row]);
     for (int c0 = 0; c0 < nc; c0 += 4) {
-      float v[4][8], w[4];  // (four loads in flight)
+      float v[4][ML::kChunks][8], w[4];  // (four loads in flight)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         const size_t from = min(c0 + c, nc - 1) * all + row;
-        load8(po + from * D + 8 * g, v[c]);
+#pragma unroll
+        for (int x = 0; x < ML::kChunks; ++x) load8(po + from * D + ML::at(g, x), v[c][x]);
         w[c] = plse[from];
       }
 #pragma unroll
@@ -585,20 +587,26 @@ __global__ __launch_bounds__(256) void score_fwd_merge(ScoreArgs a, const float*
         w[c] = exp2_hw(w[c] - m);
         l += w[c];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          acc[e] = fmaf(w[c], v[c][e], acc[e]);
-          bad = fmaf(v[c][e], 0.f, bad);
-        }
+        for (int x = 0; x < ML::kChunks; ++x)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            acc[x][e] = fmaf(w[c], v[c][x][e], acc[x][e]);
+            bad = fmaf(v[c][x][e], 0.f, bad);
+          }
       }
     }
     bad = fmaf(l, 0.f, bad);
   }
-  unsigned long long rows = __builtin_amdgcn_ballot_w64(bad != 0.f);
-  if (mine && bad == 0.f) {
+  const bool again = ML::any(bad != 0.f);
+  unsigned long long rows = __builtin_amdgcn_ballot_w64(again);
+  if (mine && !again) {
     const float inv = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] *= inv;
-    store8(score::o_row<bf16, D>(a, bh / a.heads, i, bh % a.heads) + 8 * g, acc);
+    for (int x = 0; x < ML::kChunks; ++x) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[x][e] *= inv;
+      store8(score::o_row<bf16, D>(a, bh / a.heads, i, bh % a.heads) + ML::at(g, x), acc[x]);
+    }
     if (g == 0) a.lse[row] = l == 0.f ? kNegInf : (m + log2f(l)) * kLn2;
   }
   while (rows) {  // rows with a non-finite part, again by the definition
@@ -637,7 +645,8 @@ void fwd_d(const ScoreArgs& a, const ScorePlan& p, void* part, hipStream_t s) {
   }
 #undef PB_FWD
   if (p.chunks > 1)
-    score_fwd_merge<D><<<(unsigned)((all * (D / 8) + 255) / 256), 256, 0, s>>>(a, po, plse, used);
+    score_fwd_merge<D><<<(unsigned)((all * MergeLanes<D>::kLanes + 255) / 256), 256, 0, s>>>(a, po, plse,
+                                                                                      used);
 }
 
 }  // namespace

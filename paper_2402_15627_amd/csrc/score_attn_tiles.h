@@ -36,6 +36,20 @@ PB_DEV bf16x2 rest_of(bf16x2 pair, float u, float v) {
       (bf16)__builtin_amdgcn_fdot2_f32_bf16(pair, __builtin_bit_cast(bf16x2, second), v, false)};
 }
 
+// A row of D features in the merges: kLanes lanes with kChunks times 8 features each, chunk
+// c of lane l from 8 (l + c kLanes) on.  The lanes divide a wave's, so a row lies in one
+// wave, which alone writes it: merged, or where any of it is not finite, by the definition.
+template <int D>
+struct MergeLanes {
+  static constexpr int kLanes = D == 96 ? 4 : D / 8, kChunks = D / 8 / kLanes;
+  static PB_DEV int at(int l, int c) { return 8 * (l + c * kLanes); }
+  static PB_DEV bool any(bool x) {  // of the row's lanes
+    const unsigned long long all = __builtin_amdgcn_ballot_w64(x);
+    const int first = (int)(threadIdx.x & 63) / kLanes * kLanes;
+    return (all >> first) & ((1ull << kLanes) - 1);
+  }
+};
+
 PB_DEV int wave_imin(int v) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
