@@ -141,9 +141,9 @@ PB_DEV float score_of(const ScoreArgs& a, float dot, int h, int n, float& slope)
   float s = dot * a.scale;
   slope = 1.f;
   if (a.cap > 0.f) {
-    const float t = tanhf(s / a.cap);
-    s = a.cap * t;
-    slope = (1.f - t) * (1.f + t);
+    const float x = s / a.cap, e = expf(-2.f * fabsf(x)), r = 1.f / (1.f + e);
+    s = a.cap * tanhf(x);
+    slope = 4.f * e * r * r;  // 1 - tanh^2, to the last of it
   }
   if (a.slopes) s = fmaf(-a.slopes[h], (float)abs(n), s);
   if (a.table) s += bias_value(a.table[(size_t)bucket_of(a, n) * a.heads + h]);

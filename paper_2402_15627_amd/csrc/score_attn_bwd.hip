@@ -430,9 +430,7 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
     }
     __builtin_amdgcn_s_setprio(0);
     if constexpr (CAP) {
-      cap.apply(sc);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) dp[e] *= fmaf(-sc[0][e], sc[0][e], 1.f);
+      cap.apply(sc, [&](int, int e, float d) PB_INLINE { dp[e] *= d; });
     }
     if constexpr (BIAS == kSlopes) {
 #pragma unroll
@@ -619,13 +617,13 @@ struct RowTiles {
       dz[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv[ks & 1], gf[ks], dz[0], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (CAP) cap.apply(pr);
 #pragma unroll
-    for (int x = 0; x < 16; ++x) {
-      dz[0][x] -= dl;
-      if constexpr (CAP && SLOPE == 1) dz[0][x] *= fmaf(-pr[0][x], pr[0][x], 1.f);
-      if constexpr (CAP && SLOPE == 2) slope[x] = fmaf(-pr[0][x], pr[0][x], 1.f);
-    }
+    for (int x = 0; x < 16; ++x) dz[0][x] -= dl;
+    if constexpr (CAP)
+      cap.apply(pr, [&](int, int x, float d) PB_INLINE {
+        if constexpr (SLOPE == 1) dz[0][x] *= d;
+        if constexpr (SLOPE == 2) slope[x] = d;
+      });
     if constexpr (BIAS == kSlopes) {
       const float d0 = (float)(p - kv0 - 32 * h2 - 4 * fh);
 #pragma unroll

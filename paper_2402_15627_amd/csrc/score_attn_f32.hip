@@ -114,9 +114,14 @@ struct Terms {
   PB_DEV Terms(const ScoreArgs& a_, const BiasLds& b_, const unsigned char* s)
       : a(a_), bl(b_), smem(s), cap(a_.scale, CAP ? a_.cap : 1.f, 1.f) {}
   PB_DEV f32x4 base(f32x4 s) const {
+    f32x4 slope;
+    return base(s, slope);
+  }
+  // slope: what the cap leaves of their gradients
+  PB_DEV f32x4 base(f32x4 s, f32x4& slope) const {
     if constexpr (CAP) {
       f32x4 x[1] = {s};
-      cap.apply(x);
+      cap.apply(x, [&](int, int e, float d) { slope[e] = d; });
       return x[0] * a.cap;
     }
     return s * a.scale;
@@ -127,10 +132,6 @@ struct Terms {
     if constexpr (BIAS == kTable)
       return ((const float*)(smem + bl.tab))[bias_bucket(a, bl, smem, n) * a.pack + hh];
     return 0.f;
-  }
-  PB_DEV float slope(float z) const {
-    const float t = z * (1.f / cap.top);
-    return fmaf(-t, t, 1.f);
   }
 };
 PB_DEV void bias_tables(const ScoreArgs& a, const BiasLds& bl, unsigned char* smem, int h0,
@@ -320,7 +321,8 @@ PB_DEV void dq_block(const ScoreArgs& a, int blk, int nblk, int hb) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       kr[j] = score::kv_row<float, D>(a, a.k, t.b, key_row(k0 + 4 * g + j), t.kvh) + i;
-    const f32x4 z = terms.base(dot_rows<D>(kf, qf));
+    f32x4 slope;
+    const f32x4 z = terms.base(dot_rows<D>(kf, qf), slope);
     f32x4 ds = dot_rows<D>(vf, gf);
     const uint32_t see = live ? (uint32_t)(t.keys.bits(k0) >> (4 * g)) : 0;
 #pragma unroll
@@ -331,7 +333,7 @@ PB_DEV void dq_block(const ScoreArgs& a, int blk, int nblk, int hb) {
       if constexpr (BIAS == kTable)
         if (a.dtable && (see & (1u << e)))
           unsafeAtomicAdd(&mine[bias_bucket(a, bl, smem, n_) * kPad], ds[e]);
-      if constexpr (CAP) ds[e] *= terms.slope(z[e]);
+      if constexpr (CAP) ds[e] *= slope[e];
     }
     add_rows<D>(kr, ds, dq);
   }
@@ -434,7 +436,8 @@ PB_DEV void dkdv_block(const ScoreArgs& a, int blk, int hb) {
         const int r = r0 + 4 * g + j;
         pos[j] = r >= r_lo && r <= r_hi ? y + off : -1;
       }
-      const f32x4 z = terms.base(dot_rows<D>(qf, kf));
+      f32x4 slope;
+      const f32x4 z = terms.base(dot_rows<D>(qf, kf), slope);
       f32x4 pr, ds = dot_rows<D>(gf, vf);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -443,7 +446,7 @@ PB_DEV void dkdv_block(const ScoreArgs& a, int blk, int hb) {
         const float s = z[e] + terms.bias(h0, hh[e], pos[e] - key);
         pr[e] = see && s != kNegInf ? exp_less(s, L) : 0.f;
         ds[e] = pr[e] == 0.f ? 0.f : pr[e] * (ds[e] - dl);
-        if constexpr (CAP) ds[e] *= terms.slope(z[e]);
+        if constexpr (CAP) ds[e] *= slope[e];
       }
       add_rows<D>(gr, pr, dv);
       add_rows<D>(qr, ds, dk);

@@ -126,7 +126,9 @@ PB_DEV KeyTiles key_tiles(const ScoreArgs& a, int b, int p0, int p1, int lane) {
   return k;
 }
 
-// t = tanh(scale u / cap); the score is cap t, what the cap leaves of its gradient 1 - t^2.
+// t = tanh(scale u / cap); the score is cap t, what the cap leaves of its gradient 1 - t^2, or
+// 4 w (1 - w) with w = 1 / (1 + e^(2|x|)) beyond 1/2, where 1 - t^2 would lose what t is
+// rounded to (a tenth of itself at |x| = 7.5).
 // Tiles differ in how far their scores go, so a wave looks at its largest |x| = |scale u /
 // cap| first: to 1/8 three terms in x^2 are good to 2^-24, to 1/2 five, beyond 1 - 2 / (1 +
 // e^(2|x|)) takes over from 1/2 on.  (An exponential and a reciprocal take eight
@@ -158,15 +160,24 @@ struct Cap {
     const float w = u * u;
     return u * fmaf(fmaf(fmaf(fmaf(b4, w, b3), w, b2), w, b1), w, k);
   }
-  PB_DEV float any(float u) const {
+  static PB_DEV float slope(float t) { return fmaf(-t, t, 1.f); }
+  // d: the slope
+  PB_DEV float any(float u, float& d) const {
     const float x = u * k;
     const float e = __builtin_amdgcn_exp2f(2.f * kLog2e * fabsf(x));
-    const float t = fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + e), 1.f);
-    return fabsf(x) <= 0.5f ? half(u) : __builtin_copysignf(t, x);
+    const float w = __builtin_amdgcn_rcpf(1.f + e), t = fmaf(-2.f, w, 1.f), y = half(u);
+    const bool in = fabsf(x) <= 0.5f;
+    d = in ? slope(y) : 4.f * fmaf(-w, w, w);
+    return in ? y : __builtin_copysignf(t, x);
   }
-  // of some of a wave's products, by the largest of them in any lane
+  // of some of a wave's products, by the largest of them in any lane; slopes: f(i, e, slope
+  // of s[i][e])
   template <typename V, int N>
   PB_DEV void apply(V (&s)[N]) const {
+    apply(s, [](int, int, float) {});
+  }
+  template <typename V, int N, typename F>
+  PB_DEV void apply(V (&s)[N], F f) const {
     constexpr int W = sizeof(V) / 4;
     float largest = 0.f;
 #pragma unroll
@@ -177,17 +188,21 @@ struct Cap {
 #pragma unroll
       for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int e = 0; e < W; ++e) s[i][e] = near(s[i][e]);
+        for (int e = 0; e < W; ++e) s[i][e] = near(s[i][e]), f(i, e, slope(s[i][e]));
     } else if (!__builtin_amdgcn_ballot_w64(largest > 4.f * small)) {
 #pragma unroll
       for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int e = 0; e < W; ++e) s[i][e] = half(s[i][e]);
+        for (int e = 0; e < W; ++e) s[i][e] = half(s[i][e]), f(i, e, slope(s[i][e]));
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int e = 0; e < W; ++e) s[i][e] = any(s[i][e]);
+        for (int e = 0; e < W; ++e) {
+          float d;
+          s[i][e] = any(s[i][e], d);
+          f(i, e, d);
+        }
     }
   }
 };
