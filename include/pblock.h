@@ -782,7 +782,7 @@ pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s,
  *
  * Errors: PB_ERR_INVALID_ARG for a bad config, pointer or ld, PB_ERR_UNSUPPORTED for
  * another head_dim and for sizes past the kernels' (batch*seq_q*heads and
- * batch*seq_k*kv_heads <= 2^26, batch*heads <= 2^21), PB_ERR_WORKSPACE for a small ws. */
+ * batch*seq_k*kv_heads <= 2^26, batch*heads <= 2^21, buckets*heads < 2^26), PB_ERR_WORKSPACE for a small ws. */
 #define PB_SCORE_MAX_BUCKETS 64
 typedef struct {
   int batch;         /* >= 1                                                  */

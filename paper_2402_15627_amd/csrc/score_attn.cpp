@@ -7,8 +7,9 @@
 namespace {
 
 constexpr size_t kMaxLd = (size_t)1 << 24;
-constexpr long long kMaxRows = 1LL << 26, kMaxHeads = 1LL << 21;
+constexpr long long kMaxRows = 1LL << 26, kMaxHeads = 1LL << 21, kMaxEntries = 1LL << 26;
 static_assert(2 * (kMaxRows / 16 + kMaxHeads) < kMaxBlocks, "workgroups of a launch");
+static_assert(kMaxEntries * 64 <= kMaxBlocks * 256, "threads of the table's sums");
 
 pb_status check_config(const pb_score_attn_config* c) {
   if (!c) return fail(PB_ERR_INVALID_ARG, "cfg is NULL");
@@ -48,6 +49,9 @@ pb_status check_config(const pb_score_attn_config* c) {
     return fail(PB_ERR_UNSUPPORTED, "over 2^26 rows of queries' or of keys' heads");
   if ((long long)c->batch * c->heads > kMaxHeads)
     return fail(PB_ERR_UNSUPPORTED, "batch*heads is over 2^21");
+  // The table's gradient is summed by a wave an entry.
+  if ((long long)c->buckets * c->heads >= kMaxEntries)
+    return fail(PB_ERR_UNSUPPORTED, "a table of 2^26 entries or more");
   return PB_OK;
 }
 
