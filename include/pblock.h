@@ -759,7 +759,8 @@ pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s,
  *
  * The backward gives the gradients of sum(o d_o): dq, dk, dv (dk and dv summed over the
  * heads that share a key head) and, when dtable is not NULL, dtable (fp32); all are
- * overwritten.
+ * overwritten.  Where no query sees two keys (seq_k 1; window 1 without prefixes) dq, dk
+ * and dtable are 0 to the bit.
  *
  * products, of PB_BF16 tensors (PB_F32 ones have fp32 products either way): the factors
  * that a call computes, P and its gradient, are not values of the type.  PB_F32 keeps 16

@@ -132,6 +132,7 @@ pb::ScoreArgs args_of(const pb_score_attn_config* c, const pb_score_terms* t) {
   a.causal = c->causal, a.window = c->window;
   a.scale = c->scale, a.cap = c->cap;
   a.wide = c->products == PB_F32;
+  a.dscale = c->seq_k == 1 || (c->window == 1 && !t->prefix) ? 0.f : c->scale;
   a.docs = t->docs, a.prefix = t->prefix, a.n_docs = t->n_docs;
   a.slopes = t->slopes, a.table = t->table;
   a.buckets = c->buckets, a.side = c->causal ? c->buckets : c->buckets / 2;

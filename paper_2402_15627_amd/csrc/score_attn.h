@@ -25,6 +25,7 @@ struct ScoreArgs {
   int batch, seq_q, seq_k, heads, kv_heads, group;  // group: heads / kv_heads
   int causal, window;
   float scale, cap;
+  float dscale;  // scale; 0 where no query sees two keys (P is 1 and its gradient 0)
   const int *docs, *prefix;
   int n_docs;
   const float *slopes, *table;
@@ -266,7 +267,7 @@ PB_DEV void dq_row(const ScoreArgs& a, int b, int h, int i, int lane) {
       acc.add(kv_row<T, D>(a, a.k, b, j0 + jj, kvh), lane_value(du, jj), lane);
     }
   }
-  acc.store((T*)a.dq + ((size_t)b * a.seq_q + i) * a.ld_dq + (size_t)h * D, a.scale, lane);
+  acc.store((T*)a.dq + ((size_t)b * a.seq_q + i) * a.ld_dq + (size_t)h * D, a.dscale, lane);
 }
 template <typename T, int D>
 PB_DEV void dkdv_row(const ScoreArgs& a, int b, int kvh, int j, int lane) {
@@ -295,7 +296,7 @@ PB_DEV void dkdv_row(const ScoreArgs& a, int b, int kvh, int j, int lane) {
       }
     }
   const size_t at = ((size_t)b * a.seq_k + j) * a.ld_dkv + (size_t)kvh * D;
-  dk.store((T*)a.dk + at, a.scale, lane);
+  dk.store((T*)a.dk + at, a.dscale, lane);
   dv.store((T*)a.dv + at, 1.f, lane);
 }
 

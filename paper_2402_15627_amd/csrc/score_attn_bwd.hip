@@ -500,7 +500,7 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
   if (split) {
     const size_t keys = (size_t)a.batch * a.kv_heads * a.seq_k;
     const size_t at = ((size_t)chunk * keys + (size_t)hb * a.seq_k + j0) * D;
-    store_rows<D>(mine, dk, a.scale, w.pdk + at, a.seq_k - j0, lane);
+    store_rows<D>(mine, dk, a.dscale, w.pdk + at, a.seq_k - j0, lane);
     store_rows<D>(mine, dv, 1.f, w.pdv + at, a.seq_k - j0, lane);
     return;
   }
@@ -515,7 +515,7 @@ PB_DEV void dkdv_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
     return;
   }
   const size_t at = ((size_t)b * a.seq_k + j0) * a.ld_dkv + kvh * D;
-  store_rows<D>(mine, dk, a.scale, (bf16*)a.dk + at, a.ld_dkv, a.seq_k - j0, lane);
+  store_rows<D>(mine, dk, a.dscale, (bf16*)a.dk + at, a.ld_dkv, a.seq_k - j0, lane);
   store_rows<D>(mine, dv, 1.f, (bf16*)a.dv + at, a.ld_dkv, a.seq_k - j0, lane);
 }
 
@@ -770,8 +770,8 @@ PB_DEV void dq_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         *reinterpret_cast<f32x4*>(prow + 32 * db + 8 * j + 4 * t.fh) =
-            f32x4{dq[db][4 * j] * a.scale, dq[db][4 * j + 1] * a.scale, dq[db][4 * j + 2] * a.scale,
-                  dq[db][4 * j + 3] * a.scale};
+            f32x4{dq[db][4 * j] * a.dscale, dq[db][4 * j + 1] * a.dscale,
+                  dq[db][4 * j + 2] * a.dscale, dq[db][4 * j + 3] * a.dscale};
     return;
   }
   float bad = 0.f;
@@ -795,7 +795,7 @@ PB_DEV void dq_block(const ScoreArgs& a, const BwdWork& w, int bx, int hb) {
     for (int j = 0; j < 4; ++j) {
       float v[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = dq[db][4 * j + e] * a.scale;
+      for (int e = 0; e < 4; ++e) v[e] = dq[db][4 * j + e] * a.dscale;
       store4(out + 32 * db + 8 * j + 4 * t.fh, v);
     }
 }

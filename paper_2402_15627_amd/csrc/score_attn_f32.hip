@@ -338,7 +338,7 @@ PB_DEV void dq_block(const ScoreArgs& a, int blk, int nblk, int hb) {
     add_rows<D>(kr, ds, dq);
   }
   f32x4 o[Merge<D, W>::kVec];
-  Merge<D, W>::run(buf, dq, a.scale, wave, i, g, o);  // (its barrier: every wave's sums are there)
+  Merge<D, W>::run(buf, dq, a.dscale, wave, i, g, o);  // (its barrier: every wave's sums are there)
   if constexpr (BIAS == kTable) {
     if (a.dtable)
       for (int y = threadIdx.x; y < a.buckets * a.pack; y += 64 * W) {
@@ -455,7 +455,7 @@ PB_DEV void dkdv_block(const ScoreArgs& a, int blk, int hb) {
   f32x4 ov[Merge<D, W>::kVec], ok[Merge<D, W>::kVec];
   Merge<D, W>::run(buf, dv, 1.f, wave, i, g, ov);
   __syncthreads();
-  Merge<D, W>::run(buf, dk, a.scale, wave, i, g, ok);
+  Merge<D, W>::run(buf, dk, a.dscale, wave, i, g, ok);
   bool bad = false;
 #pragma unroll
   for (int n = 0; n < Merge<D, W>::kVec; ++n)

@@ -13,7 +13,7 @@ __global__ __launch_bounds__(64) void score_dtable_sum(ScoreArgs a, int parts) {
     s += (double)a.bias_part[((size_t)i * a.heads + h) * a.buckets + n];
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
-  if (threadIdx.x == 0) a.dtable[n * a.heads + h] = (float)s;
+  if (threadIdx.x == 0) a.dtable[n * a.heads + h] = (float)s * (a.dscale == 0.f ? 0.f : 1.f);
 }
 
 }  // namespace
