@@ -932,9 +932,9 @@ pb_status pblock_orthogonalize(int n_tensors, const pb_ortho_tensor* tensors,
  *   w = w (1 - lr weight_decay) - lr (m c1) / (sqrt(v c2) + eps)
  *       c1 = 1 / (1 - beta1^t), c2 = 1 / (1 - beta2^t) (1 and 1 without bias_correction)
  *
- * in fp32, each operation rounded by itself.  param and grad are fp32, param updated in
- * place; param_copy, when not NULL, receives the updated weights in copy_dtype (bf16:
- * round to nearest even).  state:
+ * in fp32, each operation rounded by itself (one quotient in 2^32 to the next to
+ * nearest).  param and grad are fp32, param updated in place; param_copy, when not NULL,
+ * receives the updated weights in copy_dtype (bf16: round to nearest even).  state:
  *
  *   PB_ADAMW_F32   exp_avg is m and exp_avg_sq v, fp32.
  *   PB_ADAMW_E4M3  exp_avg holds m and exp_avg_sq sqrt(v) as OCP e4m3 codes, one byte

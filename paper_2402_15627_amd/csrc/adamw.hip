@@ -11,9 +11,10 @@
 // each (2048: 1191 us, 4096: 1195); a thread has four elements, a wave the 256
 // that share the scales of an 8-bit state.
 //
-// Every operation is rounded by itself (no contraction into fused products): a
-// value that decides an 8-bit code is then the one that elementary operations
-// give, and codes do not depend on how a compiler groups them.
+// Every operation is rounded by itself (no contraction into fused products; a quotient
+// in 2^32 is off by a step, see sqrt_near): a value that decides an 8-bit code is then the
+// one that elementary operations give, codes do not depend on how a compiler groups
+// them, and an element's result on no other element but by its block's scales.
 #include "common.h"
 #include "kernels.h"
 
@@ -100,8 +101,9 @@ PB_DEV void dequantise(uint32_t word, float scale, f32x4& x) {
   x[0] = lo[0] * scale, x[1] = lo[1] * scale, x[2] = hi[0] * scale, x[3] = hi[1] * scale;
 }
 
-// Square root and quotient as correctly rounded ones (but for about one in 2^22, off by a
-// step), from the hardware's approximations and an exact remainder each: half the
+// Square root and quotient from the hardware's approximations and an exact remainder each.
+// Beside the correctly rounded ones: roots the same for all 2^24 values of 1 .. 4 (other
+// powers of four scale them), quotients but for one of 2^32, off by a step.  Half the
 // instructions of the general ones, which also take care of values whose squares or
 // reciprocals leave fp32.  x: 0, or 2^-90 .. 2^90; d: 2^-90 .. 2^90.
 PB_DEV float sqrt_near(float x) {
@@ -120,17 +122,18 @@ PB_DEV void update(const AdamScalars& c, float decay, const f32x4& grad, f32x4& 
                    f32x4& v, f32x4& r) {
 #pragma clang fp contract(off)
   f32x4 vh;
-  bool plain = true;
+  bool plain[4], all = true;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const float g = grad[k] * c.grad_scale;
     m[k] = m[k] * c.beta1 + g * c.rest1;
     v[k] = v[k] * c.beta2 + (g * g) * c.rest2;
     vh[k] = v[k] * c.c2;
-    plain = plain && (v[k] == 0.f || (in_range(v[k]) && in_range(vh[k])));
+    plain[k] = c.eps_in_range && (v[k] == 0.f || (in_range(v[k]) && in_range(vh[k])));
+    all = all && plain[k];
   }
   f32x4 u;
-  if (c.eps_in_range && __builtin_amdgcn_ballot_w64(!plain) == 0) {
+  if (__builtin_amdgcn_ballot_w64(!all) == 0) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       u[k] = div_near(m[k] * c.c1, sqrt_near(vh[k]) + c.eps);
@@ -139,8 +142,10 @@ PB_DEV void update(const AdamScalars& c, float decay, const f32x4& grad, f32x4& 
   } else {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      u[k] = (m[k] * c.c1) / (__builtin_sqrtf(vh[k]) + c.eps);
-      if (ROOT) r[k] = __builtin_sqrtf(v[k]);
+      // (an element in range has the same bits beside one that is not)
+      const float n = m[k] * c.c1, d = (plain[k] ? sqrt_near(vh[k]) : __builtin_sqrtf(vh[k])) + c.eps;
+      u[k] = plain[k] ? div_near(n, d) : n / d;
+      if (ROOT) r[k] = plain[k] ? sqrt_near(v[k]) : __builtin_sqrtf(v[k]);
     }
   }
 #pragma unroll
