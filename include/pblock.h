@@ -771,7 +771,7 @@ pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s,
  * In norm, where a result's rounding alone is 1.66e-3, PB_BF16 gives o 1.7e-3 to 2.1e-3,
  * dv 2.1e-3 to 2.4e-3, dq and dk 2.6e-3 to 2.8e-3 over rows of 500 keys and more, 5.2e-3
  * over rows of two (normal values, scores of a standard deviation of 2; of 6: 4.4e-3).
- * Its forward takes 0.75 of PB_F32's time, its backward 0.65 (4096 tokens and more).
+ * Its forward takes 0.75 to 0.9 of PB_F32's time, its backward 0.63 to 0.75.
  * (A backward over a part of the rows' keys, with o and lse of all of them, needs the row
  * term from o: PB_BF16 or PB_F32 tensors, without dtable.)
  *

@@ -6,7 +6,7 @@
 // Bound by HBM: each element of w, g and the states is read once and written
 // once (30 bytes with a bf16 copy of w, 18 with states of 8 bits), so the
 // arithmetic is free as long as it stays under about a hundred instructions an
-// element: 226.5 M parameters 1165 us (5.8 TB/s), in 8 bits 664 (6.1).  A launch
+// element: 226.5 M parameters 1180 us (5.8 TB/s), in 8 bits 667 (6.1).  A launch
 // takes up to kAdamMax tensors, cut into chunks of 1024 elements, a workgroup
 // each (2048: 1191 us, 4096: 1195); a thread has four elements, a wave the 256
 // that share the scales of an 8-bit state.

@@ -23,9 +23,11 @@
 // row terms put right.
 //
 // Bound by the vector instructions of the terms beside the products, at two waves a SIMD
-// (registers): 4096 tokens of packed documents, 16 heads over 4 x 128, capped 234 us, 424
-// TFLOP/s, matrix cores busy 26%, vector instructions 45%; 8192 x 40 heads, window 1024,
-// without terms 820 us (attn.hip 855), capped 890, with a table 840 and its gradient 970.
+// (registers).  Measured (WIDE, and without): 4096 tokens of packed documents, 16 heads over
+// 4 x 128, capped 344 us (231), 288 TFLOP/s of 10 d operations a pair, where 24 d (14 d) are
+// done; matrix cores busy 30% and vector instructions 41% of the two roles' launch, 20% and
+// 51% of the row terms'.  4096 x 16 heads of 64: without terms 265 (168; attn.hip 240), capped
+// 320 (214), with a table 299 (201) and its gradient 329 (231).
 //
 // Non-finite values behind the mask are met as in the forward.
 #include "kernels.h"
@@ -1164,7 +1166,7 @@ ScoreBwdPlan score_bwd_whole(const ScoreArgs& a) { return ScoreBwdPlan{{a.group 
 // keys are cut down to what the launch takes as a whole (over 512 workgroups at a time;
 // half the longest block's tiles on average under a causal mask) or the longest row block
 // takes, whichever is more; rows only where few of them see many keys.  Found by timing
-// 21 plans each for 12 shapes (us; keys' chunks 1, 2, 4, 8):
+// 21 plans each for 12 shapes without WIDE (us; keys' chunks 1, 2, 4, 8):
 //   4096 tokens, 16 heads over 4, 128        687 412 295 295
 //   the same, capped, three documents        632 361 278 266
 //   2048, 12 x 128                           113  88  95 115

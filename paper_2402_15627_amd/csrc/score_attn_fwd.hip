@@ -18,10 +18,14 @@
 // That leaves 16 KB of a CU's half for the rows' keys (read back in partial tiles only)
 // and the biases, so that two workgroups share a CU.
 //
-// Measured: 8192 tokens of packed documents, 16 heads over 4 x 128, window 4096, bias by
-// distance 154 us, 674 TFLOP/s, matrix cores busy 25%, vector instructions 46%; without terms
-// at 8192 x 40 heads, window 1024, as fast as attn.hip (270 us); a token over 4 x 8192 keys,
-// 40 heads over 8, 38 us, 28 of them K and V at 4.8 TB/s.
+// Measured (WIDE, and without): 8192 tokens of packed documents, 16 heads over 4 x 128,
+// window 4096, bias by distance 204 us (155), 508 TFLOP/s of 4 d operations a pair, matrix
+// cores busy 28% and vector instructions 43% of the longest blocks' time; 4096 x 16 heads of
+// 64 without terms 77 (62; attn.hip 61); a token over 4 x 8192 keys, 40 heads over 8, 39.6
+// (34), of which K and V at 4.1 TB/s 32.5 (28).
+//
+// At head_dim 128 registers are full: 4 to 18 spill with WIDE (7 to 17 without, none without
+// terms), nearly all of them around the loop and in partial tiles.
 //
 // A non-finite value behind the mask makes a product non-finite (0 x Inf).  A wave with a
 // non-finite output computes its rows again by the definition, which reads visible keys
@@ -660,7 +664,7 @@ size_t score_fwd_part_bytes(int head_dim, const ScoreArgs& a, const ScorePlan& p
 
 // Split as in attn.hip: where the grid has fewer than 2048 waves, into as many chunks as
 // bring it to 1536, of four tiles at least; a tile takes about 1.4 us, the merge 3.5 us
-// and its traffic.  Timed (us, 1, 2, 4, 8, 12, 16 chunks):
+// and its traffic.  Timed without WIDE (us, 1, 2, 4, 8, 12, 16 chunks):
 //   4 x 1 token over 8192, 40 heads over 8 x 128   232 123  68  42  35  36
 //   1 token over 1000, 8 x 64                       24  18  14  14  14  14
 //   2048, 12 x 128, capped                          60  49  50  64  72  81

@@ -790,7 +790,7 @@ def score_attn_config(batch, seq_q, seq_k, heads, kv_heads, head_dim, causal=Tru
     """window: no limit by default; scale: 1 / sqrt(head_dim) by default; buckets and
     max_distance go with a table. products (of bf16 tensors): "f32" (16 bits of P and of its
     gradient, results off by their own rounding) or "bf16" (rounded as the block's own
-    attention does; 0.65 to 0.75 of the time, gradients off by up to three roundings)."""
+    attention does; 0.63 to 0.9 of the time, gradients off by up to three roundings)."""
     return ScoreAttnConfig(batch, seq_q, seq_k, heads, kv_heads, head_dim, int(bool(causal)),
                            seq_k if window is None else window,
                            head_dim ** -0.5 if scale is None else scale, cap, buckets,
