@@ -773,7 +773,7 @@ pb_status pblock_rmsnorm_backward(const pb_rmsnorm_config* cfg, const void* s,
  * over rows of two (normal values, scores of a standard deviation of 2; of 6: 4.4e-3).
  * Its forward takes 0.75 to 0.9 of PB_F32's time, its backward 0.63 to 0.75.
  * (A backward over a part of the rows' keys, with o and lse of all of them, needs the row
- * term from o: PB_BF16 or PB_F32 tensors, without dtable.)
+ * term from o: PB_BF16 or PB_F32 tensors; without dtable, and the latter without a table.)
  *
  * ws, 256-byte aligned, pblock_score_attn_workspace_bytes(cfg, mode): the PB_ATTN_WS_*
  * modes.  PB_ATTN_WS_FORWARD is optional as for pblock_swattn_forward (less runs
