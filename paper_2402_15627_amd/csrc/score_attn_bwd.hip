@@ -24,10 +24,10 @@
 //
 // Bound by the vector instructions of the terms beside the products, at two waves a SIMD
 // (registers).  Measured (WIDE, and without): 4096 tokens of packed documents, 16 heads over
-// 4 x 128, capped 344 us (231), 288 TFLOP/s of 10 d operations a pair, where 24 d (14 d) are
-// done; matrix cores busy 30% and vector instructions 41% of the two roles' launch, 20% and
-// 51% of the row terms'.  4096 x 16 heads of 64: without terms 265 (168; attn.hip 240), capped
-// 320 (214), with a table 299 (201) and its gradient 329 (231).
+// 4 x 128, capped 346 us (229), 287 TFLOP/s of 10 d operations a pair, where 24 d (14 d) are
+// done; matrix cores busy 32% and vector instructions 42% of the two roles' launch, 21% and
+// 53% of the row terms'.  4096 x 16 heads of 64: without terms 265 (169; attn.hip 240), capped
+// 322 (217), with a table 301 (202) and its gradient 331 (232).
 //
 // Non-finite values behind the mask are met as in the forward.
 #include "kernels.h"

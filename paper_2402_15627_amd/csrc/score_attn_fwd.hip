@@ -11,7 +11,7 @@
 //
 // Probabilities enter O as bf16.  WIDE adds the products with what that rounding leaves
 // (16 bits of each in all), so that o is off by its own rounding alone (1.66e-3 in norm,
-// without 1.7e-3 to 2.1e-3): half as many matrix products again and three vector
+// without 1.7e-3 to 2.1e-3): half as many matrix products again and one and a half vector
 // instructions a score.
 //
 // LDS: K and V in two slots each; iteration t loads K of tile t + 2 and V of tile t + 1.
@@ -19,10 +19,10 @@
 // and the biases, so that two workgroups share a CU.
 //
 // Measured (WIDE, and without): 8192 tokens of packed documents, 16 heads over 4 x 128,
-// window 4096, bias by distance 204 us (155), 508 TFLOP/s of 4 d operations a pair, matrix
-// cores busy 28% and vector instructions 43% of the longest blocks' time; 4096 x 16 heads of
-// 64 without terms 77 (62; attn.hip 61); a token over 4 x 8192 keys, 40 heads over 8, 39.6
-// (34), of which K and V at 4.1 TB/s 32.5 (28).
+// window 4096, bias by distance 204 us (156), 508 TFLOP/s of 4 d operations a pair, matrix
+// cores busy 28% and vector instructions 43% under the profiler; 4096 x 16 heads of
+// 64 without terms 78 (62; attn.hip 62); a token over 4 x 8192 keys, 40 heads over 8, 39.7
+// (34), of which K and V at 4.1 TB/s 32.8 (28).
 //
 // At head_dim 128 registers are full: 4 to 18 spill with WIDE (7 to 17 without, none without
 // terms), nearly all of them around the loop and in partial tiles.
